@@ -460,6 +460,73 @@ int free_op_linear(int dtype, int epilogue, int out_dtype, int M, int N, int K,
 int free_op_ln_modulate(int out_dtype, int M, int D, int rows_per_seq, const float* x,
                         const float* shift, const float* scale, int64_t mod_stride, void* y, void* stream);
 
+/*
+ * free_op_layer_norm -- layer norm of rows with an optional weight and bias per group of rows.  For row i of x, in group
+ * g = i / rows_per_group:
+ *     mu = mean(x_i),  r = 1 / sqrt(mean((x_i - mu)^2) + eps),  y_i = (x_i - mu) r w_g + b_g
+ * A learned norm has one group; an adaptive norm (adaLN) has one group per sequence, with unit_offset for its 1 + scale.
+ *   x_dtype, y_dtype   FREE_FP32 or FREE_BF16, in any combination; statistics are fp32
+ *   n_groups, rows_per_group   M = n_groups * rows_per_group rows; M = 0 is allowed and does nothing
+ *   x, y       DEVICE [M, D], rows x_stride / y_stride (>= D) elements apart; elements between the rows are not touched.
+ *              y may be x where the types and strides are the same
+ *   weight     DEVICE fp32, element (g, c) at weight[g * mod_stride + c], or NULL for 1; unit_offset non-zero: 1 is added to it
+ *   bias       DEVICE fp32, laid out as weight, or NULL for 0
+ *   stats      DEVICE fp32 [M, 2] or NULL: mu and r of every row, what the backward pass needs
+ * No workspace.  weight, bias and stats need 4-byte alignment only.  A row with an infinity or NaN gives NaN, as the formula.
+ * Rows and strides that are multiples of 16 bytes (and D % 8 == 0) are the fast form.
+ * Errors: ARG, SHAPE, ALIGN, UNSUPPORTED (D > 8192), CUDA.
+ *
+ * free_op_layer_norm_bwd -- its gradients, from dy and the stats that the forward call kept.  With xh = (x - mu) r, v = dy w:
+ *     dx = dres + r (v - mean(v) - xh mean(v xh)),   dweight_g = sum over the group's rows of dy xh,   dbias_g = ... of dy
+ *   dy         DEVICE y_dtype [M, D], rows dy_stride apart
+ *   dres       DEVICE x_dtype [M, D], rows dres_stride apart, or NULL: the gradient that reaches x on another path (a
+ *              residual connection), added before dx is rounded
+ *   dx         DEVICE x_dtype [M, D], rows dx_stride apart; may be dres, x or dy where type and stride are the same
+ *   dweight, dbias   DEVICE fp32, element (g, c) at [g * dmod_stride + c]; either may be NULL.  Overwritten, zero for a group
+ *              without rows.  With unit_offset dweight is the gradient of the stored offset
+ *   ws         DEVICE, >= free_op_layer_norm_bwd_workspace_bytes() (0 for few rows; HOST-only function), not needed when both
+ *              gradients are NULL: partial column sums, added in a fixed order (repeats are bit-identical)
+ *   other arguments and errors as above, and WORKSPACE.
+ */
+int free_op_layer_norm(int x_dtype, int y_dtype, int n_groups, int rows_per_group, int D,
+                       const void* x, int64_t x_stride, const float* weight, const float* bias, int64_t mod_stride,
+                       int unit_offset, float eps, void* y, int64_t y_stride, float* stats, void* stream);
+size_t free_op_layer_norm_bwd_workspace_bytes(int n_groups, int rows_per_group, int D);
+int free_op_layer_norm_bwd(int x_dtype, int y_dtype, int n_groups, int rows_per_group, int D,
+                           const void* x, int64_t x_stride, const void* dy, int64_t dy_stride, const float* stats,
+                           const float* weight, int64_t mod_stride, int unit_offset,
+                           const void* dres, int64_t dres_stride, void* dx, int64_t dx_stride,
+                           float* dweight, float* dbias, int64_t dmod_stride, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * free_op_rope_axes -- rotary positions with one to four axes (time, height, width) on the heads of a token: rotated pair p
+ * of a head, which belongs to axis A(p), is turned by t = pos[token, A(p)] * freq(p):
+ *     (a, b) -> (a cos t - b sin t, a sin t + b cos t);   inverse non-zero turns by -t, which is also the backward pass.
+ *   dtype      FREE_FP32 or FREE_BF16 (x and y); angles are formed in fp64, the rotation in fp32
+ *   axis_dims  HOST int32 [n_axes]: elements of a head that belong to each axis (even, their sum R in 2 .. min(d_head, 256)).
+ *              Pairs are given to the axes in order: the first axis_dims[0] / 2 to axis 0, and so on.  The d_head - R
+ *              elements behind the rotated ones are copied
+ *   pairing    FREE_ROPE_INTERLEAVED: pair p is elements (2p, 2p + 1); FREE_ROPE_HALVES: elements (p, p + R / 2)
+ *   freq_mode  FREE_ROPE_FREQ_PER_AXIS: pair i of an axis has freq base^(-2 i / axis_dims); FREE_ROPE_FREQ_JOINT: pair p of the
+ *              head has freq base^(-2 p / R)
+ *   pos        DEVICE fp32 [n_tok, n_axes] for sequence s at pos + s * pos_seq_stride (0: all sequences share it); fractional,
+ *              negative and far positions are allowed
+ *   x, y       DEVICE, element (s, t, h, c) at s * seq_stride + t * tok_stride + h * head_stride + c, so that q and k are
+ *              rotated inside the packed matrix of the projection (heads = 2 * heads, d_head apart).  Elements that no
+ *              (s, t, h, c) names are not touched.  y may be x with the same strides (in place), and must not overlap it
+ *              otherwise.  The heads of y must not overlap one another
+ * No workspace; x and y need only their element's alignment (16-byte aligned heads are the fast form); n_seq = 0 or n_tok = 0
+ * does nothing.  Errors: ARG, SHAPE, ALIGN, UNSUPPORTED (odd d_head, R > 256), CUDA.
+ */
+#define FREE_ROPE_INTERLEAVED    0
+#define FREE_ROPE_HALVES         1
+#define FREE_ROPE_FREQ_PER_AXIS  0
+#define FREE_ROPE_FREQ_JOINT     1
+int free_op_rope_axes(int dtype, int pairing, int freq_mode, int inverse, int n_seq, int n_tok, int heads, int d_head,
+                      int n_axes, const int32_t* axis_dims, double base, const float* pos, int64_t pos_seq_stride,
+                      const void* x, int64_t x_seq_stride, int64_t x_tok_stride, int64_t x_head_stride,
+                      void* y, int64_t y_seq_stride, int64_t y_tok_stride, int64_t y_head_stride, void* stream);
+
 /* Non-causal multi-head self-attention of n_seq sequences: qkv [n_seq, n_tok, 3, heads, d_head] in
  * `dtype`, out [n_seq, n_tok, heads * d_head] in `dtype`; softmax(q k^T / sqrt(d_head)) v per head. */
 int free_op_attention(int dtype, int n_seq, int n_tok, int heads, int d_head,

@@ -107,6 +107,14 @@ _SIGNATURES = {
     "free_op_linear_workspace_bytes": (C.c_size_t, []),
     "free_op_linear": (C.c_int, [C.c_int] * 6 + [C.c_void_p] * 6 + [C.c_int64, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "free_op_ln_modulate": (C.c_int, [C.c_int] * 4 + [C.c_void_p] * 3 + [C.c_int64, C.c_void_p, C.c_void_p]),
+    "free_op_layer_norm": (C.c_int, [C.c_int] * 5 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_float,
+                                                     C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "free_op_layer_norm_bwd_workspace_bytes": (C.c_size_t, [C.c_int] * 3),
+    "free_op_layer_norm_bwd": (C.c_int, [C.c_int] * 5 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                                         C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                                         C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "free_op_rope_axes": (C.c_int, [C.c_int] * 9 + [C.c_void_p, C.c_double, C.c_void_p, C.c_int64] +
+                          [C.c_void_p, C.c_int64, C.c_int64, C.c_int64] * 2 + [C.c_void_p]),
     "free_op_attention": (C.c_int, [C.c_int] * 5 + [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "free_op_attention_workspace_bytes": (C.c_size_t, [C.c_int] * 5),
     "free_op_attention_static": (C.c_int, [C.c_int] * 4 + [C.c_void_p] * 4),
@@ -587,6 +595,142 @@ def op_ln_modulate(x, shift, scale, rows_per_seq, out_dtype=FREE_FP32):
     _check(lib().free_op_ln_modulate(out_dtype, M, D, rows_per_seq, _ptr(x), _ptr(shift), _ptr(scale),
                                      shift.stride(0), _ptr(y), _stream()), "free_op_ln_modulate")
     return y
+
+
+_DTYPE = {torch.float32: FREE_FP32, torch.bfloat16: FREE_BF16}
+
+
+def _code(dtype):
+    """FREE_* code of a torch dtype (the codes themselves pass through)."""
+    if dtype in (FREE_FP32, FREE_BF16):
+        return dtype
+    if dtype not in _DTYPE:
+        raise ValueError(f"expected float32 or bfloat16, got {dtype}")
+    return _DTYPE[dtype]
+
+
+def _same_device(first, *others):
+    for t in (first,) + others:
+        if t is not None and (not t.is_cuda or t.device != first.device):
+            raise ValueError("expected CUDA tensors on one device")
+
+
+def _run(device, fn, what):
+    """fn(stream) with `device` current, on the stream that is current there."""
+    if device.index == torch.cuda.current_device():
+        code = fn(_stream())
+    else:
+        with torch.cuda.device(device):
+            code = fn(_stream())
+    if code != 0:
+        raise FreeError(code, what)
+
+
+def _rows(t, M, D, what):
+    """Row stride of a [M, D] matrix whose rows are dense."""
+    if t.dim() != 2 or t.shape[0] != M or t.shape[1] != D or (D > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: expected a [{M}, {D}] matrix with dense rows")
+    return t.stride(0) if M > 1 else max(D, t.stride(0))
+
+
+def _group_rows(t, groups, D, what):
+    """Group stride of a [D] or [groups, D] fp32 table (rows of an adaLN table may be far apart)."""
+    if t.dtype != torch.float32 or t.shape[-1] != D or t.dim() > 2 or (D > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{what}: expected fp32 [{groups}, {D}] with dense rows")
+    if t.dim() == 1:
+        return 0                                                   # one row for every group
+    if t.shape[0] not in (1, groups):
+        raise ValueError(f"{what}: expected fp32 [{groups}, {D}]")
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _groups(M, rows_per_group):
+    rows = M if rows_per_group is None else int(rows_per_group)
+    if rows < 0 or (rows == 0 and M > 0) or (rows > 0 and M % rows):
+        raise ValueError(f"{M} rows are not whole groups of {rows}")
+    return (1, 0) if rows == 0 else (M // rows, rows)
+
+
+def op_layer_norm(x, weight=None, bias=None, rows_per_group=None, unit_offset=False, eps=1e-6, out_dtype=None, want_stats=False, out=None):
+    """Layer norm of the rows of x (CUDA fp32 or bf16 [M, D], dense rows any distance apart) with a weight and bias (fp32 [D],
+    or [groups, D] for groups of `rows_per_group` consecutive rows; unit_offset: the weight is stored as an offset from one, as
+    adaLN's scale).  Returns y [M, D] in out_dtype (default: x's), and with want_stats also (mean, 1 / sqrt(var + eps)) as fp32
+    [M, 2], what op_layer_norm_bwd needs."""
+    if x.dim() != 2:
+        raise ValueError("x: expected a matrix")
+    M, D = x.shape
+    groups, rows = _groups(M, rows_per_group)
+    _same_device(x, weight, bias, out)
+    xs = _rows(x, M, D, "x")
+    strides = [_group_rows(t, groups, D, n) for t, n in ((weight, "weight"), (bias, "bias")) if t is not None]
+    if len(set(strides)) > 1:
+        raise ValueError("weight and bias need the same distance between groups")
+    dt = _ACT[_code(x.dtype if out_dtype is None else out_dtype)] if out is None else out.dtype
+    if out is None:
+        out = torch.empty((M, D), dtype=dt, device=x.device)
+    stats = torch.empty((M, 2), dtype=torch.float32, device=x.device) if want_stats else None
+    _run(x.device, lambda s: lib().free_op_layer_norm(_code(x.dtype), _code(dt), groups, rows, D, _ptr(x), xs, _ptr(weight), _ptr(bias),
+                                                      strides[0] if strides else 0, int(bool(unit_offset)), float(eps), _ptr(out),
+                                                      _rows(out, M, D, "out"), _ptr(stats), s), "free_op_layer_norm")
+    return (out, stats) if want_stats else out
+
+
+def op_layer_norm_bwd(x, dy, stats, weight=None, rows_per_group=None, unit_offset=False, dres=None, want_dweight=True, want_dbias=True,
+                      dx=None):
+    """Gradients of op_layer_norm from dy [M, D] and the stats it kept.  dres: gradient of x from another path, added to dx.
+    Returns (dx in x's dtype, dweight, dbias), the last two fp32 [groups, D], or None where not wanted."""
+    if x.dim() != 2:
+        raise ValueError("x: expected a matrix")
+    M, D = x.shape
+    groups, rows = _groups(M, rows_per_group)
+    _same_device(x, dy, stats, weight, dres, dx)
+    xs, dys = _rows(x, M, D, "x"), _rows(dy, M, D, "dy")
+    if stats.dtype != torch.float32 or tuple(stats.shape) != (M, 2) or not stats.is_contiguous():
+        raise ValueError("stats: expected the contiguous fp32 [M, 2] of the forward call")
+    ms = 0 if weight is None else _group_rows(weight, groups, D, "weight")
+    for t, n in ((dres, "dres"), (dx, "dx")):
+        if t is not None and t.dtype != x.dtype:
+            raise ValueError(f"{n}: expected x's dtype")
+    if dx is None:
+        dx = torch.empty((M, D), dtype=x.dtype, device=x.device)
+    dw = torch.empty((groups, D), dtype=torch.float32, device=x.device) if want_dweight else None
+    db = torch.empty((groups, D), dtype=torch.float32, device=x.device) if want_dbias else None
+    need = lib().free_op_layer_norm_bwd_workspace_bytes(groups, rows, D) if want_dweight or want_dbias else 0
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    _run(x.device, lambda s: lib().free_op_layer_norm_bwd(
+        _code(x.dtype), _code(dy.dtype), groups, rows, D, _ptr(x), xs, _ptr(dy), dys, _ptr(stats), _ptr(weight), ms,
+        int(bool(unit_offset)), _ptr(dres), 0 if dres is None else _rows(dres, M, D, "dres"), _ptr(dx), _rows(dx, M, D, "dx"),
+        _ptr(dw), _ptr(db), D, _ptr(ws), need, s), "free_op_layer_norm_bwd")
+    return dx, dw, db
+
+
+ROPE_PAIRING = {"interleaved": 0, "halves": 1}
+
+
+def op_rope_axes(x, pos, axis_dims, base=10000.0, pairing="interleaved", joint_freq=False, inverse=False, out=None):
+    """Rotary positions with len(axis_dims) axes on x (CUDA fp32 or bf16 [n_seq, n_tok, heads, d_head], any strides with dense
+    heads: q and k may be views into the packed projection); axis_dims[a] elements of a head follow axis a.  pos: fp32 [n_tok, n_axes], or
+    [n_seq, n_tok, n_axes].  inverse turns back (the gradient of the forward call).  out=x rotates in place.  Returns the
+    rotated heads, contiguous unless `out` is given."""
+    if x.dim() != 4 or (x.shape[3] > 1 and x.stride(3) != 1):
+        raise ValueError("x: expected [n_seq, n_tok, heads, d_head] with dense heads")
+    if pairing not in ROPE_PAIRING:
+        raise ValueError("pairing: expected 'interleaved' or 'halves'")
+    n_seq, n_tok, heads, d_head = x.shape
+    _same_device(x, pos, out)
+    axes = (C.c_int32 * len(axis_dims))(*axis_dims)
+    _dev(pos, torch.float32)
+    if tuple(pos.shape) not in ((n_tok, len(axis_dims)), (n_seq, n_tok, len(axis_dims))):
+        raise ValueError("pos: expected [n_tok, n_axes] or [n_seq, n_tok, n_axes]")
+    if out is None:
+        out = torch.empty((n_seq, n_tok, heads, d_head), dtype=x.dtype, device=x.device)
+    elif out.shape != x.shape or out.dtype != x.dtype or (d_head > 1 and out.stride(3) != 1):
+        raise ValueError("out: expected x's shape and dtype with dense heads")
+    _run(x.device, lambda s: lib().free_op_rope_axes(
+        _code(x.dtype), ROPE_PAIRING[pairing], int(bool(joint_freq)), int(bool(inverse)), n_seq, n_tok, heads, d_head, len(axis_dims), axes,
+        float(base), _ptr(pos), n_tok * len(axis_dims) if pos.dim() == 3 else 0, _ptr(x), x.stride(0), x.stride(1), x.stride(2),
+        _ptr(out), out.stride(0), out.stride(1), out.stride(2), s), "free_op_rope_axes")
+    return out
 
 
 def op_attention(qkv, heads):
