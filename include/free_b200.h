@@ -461,6 +461,39 @@ int free_op_ln_modulate(int out_dtype, int M, int D, int rows_per_seq, const flo
                         const float* shift, const float* scale, int64_t mod_stride, void* y, void* stream);
 
 /*
+ * free_op_gated_linear -- the first half of a gated feed-forward layer in one kernel: both projections, the activation and
+ * the product.  W holds the F gate rows and then the F up rows, z = x W^T + bias:
+ *     h = act(z[:, 0:F]) * z[:, F:2F]
+ *   dtype      FREE_FP32 (CUDA cores, any sizes) or FREE_BF16 (tcgen05, fp32 accumulation; F % 8 == 0 and K % 8 == 0, the
+ *              16-byte rows that tile copies need, else UNSUPPORTED): type of x, w, h and preact
+ *   act        FREE_ACT_SILU: g / (1 + e^-g);  FREE_ACT_GELU: 0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
+ *   x          DEVICE [M, K]; M = 0 is allowed and does nothing
+ *   w          DEVICE [2F, K];  bias  DEVICE fp32 [2F] or NULL
+ *   h          DEVICE [M, F], computed from the fp32 accumulators
+ *   preact     DEVICE [M, 2F] or NULL: z, rounded to dtype, what the backward pass needs
+ *   device_error   DEVICE uint32, OR-ed into when a bounded device-side wait gave up (clear it first; not used and may be
+ *              NULL for FREE_FP32).  Calls on several streams may share one
+ * No workspace.  h and preact must not overlap the inputs.  Errors: ARG, SHAPE, ALIGN, UNSUPPORTED, CUDA.
+ *
+ * free_op_gated_linear_bwd -- its gradients, from dh and the preact that the forward call kept:
+ *     dz = [dh z_up act'(z_gate), dh act(z_gate)],   dx = dz W,   dw = dz^T x,   dbias = sum over rows of dz
+ *   dh         DEVICE `dtype` [M, F]
+ *   dx, dw     DEVICE `dtype` [M, K], [2F, K];  dbias  DEVICE fp32 [2F].  Each may be NULL (w is read for dx only, x for dw
+ *              only) and is overwritten; with M = 0 dw and dbias become zero.  In bf16 dz is rounded to bf16 for the products
+ *   ws         DEVICE, >= free_op_gated_linear_bwd_workspace_bytes() (HOST-only): dz and the parts of split sums.  Calls that
+ *              may overlap on the GPU need one each
+ *   other arguments and errors as above, and WORKSPACE.  Repeats are bit-identical.
+ */
+#define FREE_ACT_SILU 0
+#define FREE_ACT_GELU 1
+int free_op_gated_linear(int dtype, int act, int M, int F, int K, const void* x, const void* w, const float* bias,
+                         void* h, void* preact, uint32_t* device_error, void* stream);
+size_t free_op_gated_linear_bwd_workspace_bytes(int dtype, int M, int F, int K);
+int free_op_gated_linear_bwd(int dtype, int act, int M, int F, int K, const void* x, const void* w, const void* preact,
+                             const void* dh, void* dx, void* dw, float* dbias, void* ws, size_t ws_bytes,
+                             uint32_t* device_error, void* stream);
+
+/*
  * free_op_layer_norm -- layer norm of rows with an optional weight and bias per group of rows.  For row i of x, in group
  * g = i / rows_per_group:
  *     mu = mean(x_i),  r = 1 / sqrt(mean((x_i - mu)^2) + eps),  y_i = (x_i - mu) r w_g + b_g

@@ -107,6 +107,9 @@ _SIGNATURES = {
     "free_op_linear_workspace_bytes": (C.c_size_t, []),
     "free_op_linear": (C.c_int, [C.c_int] * 6 + [C.c_void_p] * 6 + [C.c_int64, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "free_op_ln_modulate": (C.c_int, [C.c_int] * 4 + [C.c_void_p] * 3 + [C.c_int64, C.c_void_p, C.c_void_p]),
+    "free_op_gated_linear": (C.c_int, [C.c_int] * 5 + [C.c_void_p] * 7),
+    "free_op_gated_linear_bwd_workspace_bytes": (C.c_size_t, [C.c_int] * 4),
+    "free_op_gated_linear_bwd": (C.c_int, [C.c_int] * 5 + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p, C.c_void_p]),
     "free_op_layer_norm": (C.c_int, [C.c_int] * 5 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_float,
                                                      C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
     "free_op_layer_norm_bwd_workspace_bytes": (C.c_size_t, [C.c_int] * 3),
@@ -731,6 +734,86 @@ def op_rope_axes(x, pos, axis_dims, base=10000.0, pairing="interleaved", joint_f
         float(base), _ptr(pos), n_tok * len(axis_dims) if pos.dim() == 3 else 0, _ptr(x), x.stride(0), x.stride(1), x.stride(2),
         _ptr(out), out.stride(0), out.stride(1), out.stride(2), s), "free_op_rope_axes")
     return out
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1}
+_ERROR_WORDS = {}
+
+
+def _error_word(device):
+    """The device error word that the gated layer's calls on `device` share: zeroed once, OR-ed into by a kernel whose bounded
+    wait gave up, never cleared in between (so calls on several streams and replays of captured graphs may share it)."""
+    w = _ERROR_WORDS.get(device)
+    if w is None:
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("call the operator once on this device before capturing it into a CUDA graph")
+        with torch.cuda.device(device):
+            w = torch.zeros(1, dtype=torch.int32, device=device)
+            torch.cuda.current_stream().synchronize()              # zero before any other stream can use it
+        _ERROR_WORDS[device] = w
+    return w
+
+
+def op_device_error(device=None):
+    """Waits for `device` and returns the error word of the gated layer's calls on it so far (0: no bounded wait gave up)."""
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    if device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    if device not in _ERROR_WORDS:
+        return 0
+    torch.cuda.synchronize(device)
+    return int(_ERROR_WORDS[device].item()) & 0xFFFFFFFF
+
+
+def _dense(t, dtype, shape, what):
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {list(shape)}")
+    return t
+
+
+def op_gated_linear(x, w, bias=None, act="silu", want_preact=False, out=None):
+    """First half of a gated feed-forward layer, h = act(z[:, :F]) * z[:, F:] with z = x w^T + bias, in one kernel.  x: CUDA
+    fp32 or bf16 [M, K]; w [2F, K], the gate rows and then the up rows; bias fp32 [2F]; act "silu" or "gelu" (tanh form).
+    bf16 needs F and K to be multiples of 8.  Returns h [M, F], and with want_preact also z [M, 2F], what op_gated_linear_bwd
+    needs.  Asynchronous: op_device_error() tells whether a device-side wait gave up."""
+    if x.dim() != 2 or w.dim() != 2 or w.shape[0] % 2:
+        raise ValueError("x, w: expected matrices, w with an even number of rows")
+    if act not in ACTIVATIONS:
+        raise ValueError("act: expected 'silu' or 'gelu'")
+    (M, K), F, dtype = x.shape, w.shape[0] // 2, x.dtype
+    _same_device(x, w, bias, out)
+    _dense(x, dtype, (M, K), "x"); _dense(w, dtype, (2 * F, K), "w")
+    if bias is not None:
+        _dense(bias, torch.float32, (2 * F,), "bias")
+    h = torch.empty((M, F), dtype=dtype, device=x.device) if out is None else _dense(out, dtype, (M, F), "out")
+    pre = torch.empty((M, 2 * F), dtype=dtype, device=x.device) if want_preact else None
+    err = _error_word(x.device) if dtype == torch.bfloat16 else None
+    _run(x.device, lambda s: lib().free_op_gated_linear(_code(dtype), ACTIVATIONS[act], M, F, K, _ptr(x), _ptr(w), _ptr(bias), _ptr(h),
+                                                        _ptr(pre), _ptr(err), s), "free_op_gated_linear")
+    return (h, pre) if want_preact else h
+
+
+def op_gated_linear_bwd(x, w, preact, dh, act="silu", want_dx=True, want_dw=True, want_dbias=True):
+    """Gradients of op_gated_linear from dh [M, F] and the preact it kept.  Returns (dx [M, K], dw [2F, K], both in x's dtype,
+    dbias fp32 [2F]), None where not wanted."""
+    if x.dim() != 2 or w.dim() != 2 or w.shape[0] % 2:
+        raise ValueError("x, w: expected matrices, w with an even number of rows")
+    if act not in ACTIVATIONS:
+        raise ValueError("act: expected 'silu' or 'gelu'")
+    (M, K), F, dtype = x.shape, w.shape[0] // 2, x.dtype
+    _same_device(x, w, preact, dh)
+    _dense(x, dtype, (M, K), "x"); _dense(w, dtype, (2 * F, K), "w")
+    _dense(preact, dtype, (M, 2 * F), "preact"); _dense(dh, dtype, (M, F), "dh")
+    code, dev = _code(dtype), x.device
+    dx = torch.empty((M, K), dtype=dtype, device=dev) if want_dx else None
+    dw = torch.empty((2 * F, K), dtype=dtype, device=dev) if want_dw else None
+    db = torch.empty(2 * F, dtype=torch.float32, device=dev) if want_dbias else None
+    need = lib().free_op_gated_linear_bwd_workspace_bytes(code, M, F, K)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    err = _error_word(dev) if dtype == torch.bfloat16 else None
+    _run(dev, lambda s: lib().free_op_gated_linear_bwd(code, ACTIVATIONS[act], M, F, K, _ptr(x), _ptr(w), _ptr(preact), _ptr(dh), _ptr(dx),
+                                                       _ptr(dw), _ptr(db), _ptr(ws), need, _ptr(err), s), "free_op_gated_linear_bwd")
+    return dx, dw, db
 
 
 def op_attention(qkv, heads):

@@ -1,0 +1,196 @@
+// fp32 products of the gated linear layer on CUDA cores (the exact-arithmetic mode), forward and backward: any sizes.
+//
+//   GATED   z = x W^T + b, h = act(z_gate) z_up;   DX  dx = dz W;   DW  dW = dz^T x
+//
+// A CTA computes a tile of TM x 128 outputs with 8 x 8 per thread, the contraction staged 16 deep through two shared-memory
+// buffers (the next stage's global loads are in flight while this one is multiplied).  A thread's eight columns are four of
+// each half of the tile: in GATED the halves are 64 gate columns and the matching 64 up columns, so the thread that holds
+// z_gate holds z_up.  Bound by the fp32 pipe: 64 multiply-adds against four 16-byte shared-memory reads per thread and step.
+// TM is 64 where 128-row tiles would leave SMs idle in the last wave.  Few tiles and a long contraction are split, the parts
+// added in order.
+#include "gated.h"
+
+namespace {
+
+enum { GATED = 0, DX = 1, DW = 2 };
+
+constexpr int TN = 128, TK = 16;
+constexpr int kSms = 148;
+
+struct Args {
+    int M, N, depth;                       // output rows and columns (GATED: N = F), contraction
+    const float *A, *B;
+    long long lda, ldb;
+    const float* bias;
+    int act, F;
+    float *out, *pre;                      // GATED: pre [M, 2F] or nullptr
+    int parts; long long plane;            // elements between the parts
+};
+
+// A stage of one operand: ROWS x 16 values, contraction-major in shared memory ([16][ROWS + 4]).
+// KMAJOR: memory holds rows of the contraction (element (r, k) at r * ld + k); otherwise k * ld + r.
+template <int ROWS, int THREADS, bool KMAJOR, bool VEC> struct Loader {
+    static constexpr int N = ROWS * TK / 4 / THREADS;       // 16-byte groups per thread
+    float v[N][4];
+    // split: the upper half of the rows is read from `shift` rows further on (gate rows, then up rows)
+    __device__ __forceinline__ void fetch(const float* p, long long ld, int row0, int rows, int half_rows, int shift, int k0, int k1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int idx = threadIdx.x + i * THREADS;
+            if (KMAJOR) {
+                const int lr = idx / 4, k = k0 + (idx % 4) * 4;
+                const int local = lr < half_rows ? lr : lr - half_rows;
+                const bool in = row0 + local < rows;
+                const float* q = p + (long long)(row0 + local + (lr < half_rows ? 0 : shift)) * ld + k;
+                if (VEC && in && k + 3 < k1) {
+                    const float4 f = __ldg(reinterpret_cast<const float4*>(q));
+                    v[i][0] = f.x; v[i][1] = f.y; v[i][2] = f.z; v[i][3] = f.w;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[i][e] = in && k + e < k1 ? __ldg(q + e) : 0.f;
+                }
+            } else {
+                const int k = k0 + idx / (ROWS / 4), r = row0 + idx % (ROWS / 4) * 4;
+                const float* q = p + (long long)k * ld + r;
+                if (VEC && k < k1 && r + 3 < rows) {
+                    const float4 f = __ldg(reinterpret_cast<const float4*>(q));
+                    v[i][0] = f.x; v[i][1] = f.y; v[i][2] = f.z; v[i][3] = f.w;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[i][e] = k < k1 && r + e < rows ? __ldg(q + e) : 0.f;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(float (*sm)[ROWS + 4]) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int idx = threadIdx.x + i * THREADS;
+            if (KMAJOR) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sm[(idx % 4) * 4 + e][idx / 4] = v[i][e];
+            } else {
+                *reinterpret_cast<float4*>(&sm[idx / (ROWS / 4)][idx % (ROWS / 4) * 4]) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+            }
+        }
+    }
+};
+
+template <int MODE, int TM, bool VEC>
+__global__ void __launch_bounds__(TM * 2) gated_simt_kernel(const Args a) {
+    constexpr int THREADS = TM * 2;
+    constexpr int HALF = MODE == GATED ? TN / 2 : TN;       // output columns of a tile
+    __shared__ __align__(16) float As[2][TK][TM + 4];
+    __shared__ __align__(16) float Bs[2][TK][TN + 4];
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    const int m0 = blockIdx.x * TM, n0 = blockIdx.y * HALF;
+    const int kbeg = (int)((long long)a.depth * blockIdx.z / a.parts), kend = (int)((long long)a.depth * (blockIdx.z + 1) / a.parts);
+    // parts begin at multiples of four so that 16-byte reads along the contraction stay aligned
+    const int k0 = kbeg / 4 * 4, k1 = blockIdx.z + 1 == a.parts ? kend : kend / 4 * 4;
+    Loader<TM, THREADS, MODE != DW, VEC> la;
+    Loader<TN, THREADS, MODE == GATED, VEC> lb;
+    float acc[8][8] = {};
+    auto fetch = [&](int k) {
+        la.fetch(a.A, a.lda, m0, a.M, TM, 0, k, k1);
+        lb.fetch(a.B, a.ldb, n0, a.N, HALF, MODE == GATED ? a.F : 0, k, k1);
+    };
+    if (k0 < k1) {
+        fetch(k0);
+        la.store(As[0]); lb.store(Bs[0]);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int k = k0; k < k1; k += TK, buf ^= 1) {
+        const bool more = k + TK < k1;
+        if (more) fetch(k + TK);
+#pragma unroll
+        for (int kk = 0; kk < TK; ++kk) {
+            float av[8], bv[8];
+            *reinterpret_cast<float4*>(av) = *reinterpret_cast<const float4*>(&As[buf][kk][ty * 4]);
+            *reinterpret_cast<float4*>(av + 4) = *reinterpret_cast<const float4*>(&As[buf][kk][TM / 2 + ty * 4]);
+            *reinterpret_cast<float4*>(bv) = *reinterpret_cast<const float4*>(&Bs[buf][kk][tx * 4]);
+            *reinterpret_cast<float4*>(bv + 4) = *reinterpret_cast<const float4*>(&Bs[buf][kk][TN / 2 + tx * 4]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(av[i], bv[j], acc[i][j]);
+        }
+        if (more) { la.store(As[buf ^ 1]); lb.store(Bs[buf ^ 1]); }   // last read before the previous barrier
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int m = m0 + (i < 4 ? ty * 4 + i : TM / 2 + ty * 4 + i - 4);
+        if (m >= a.M) continue;
+        if (MODE == GATED) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int n = n0 + tx * 4 + j;
+                if (n >= a.F) continue;
+                float g = acc[i][j], u = acc[i][4 + j];
+                if (a.bias) { g += __ldg(a.bias + n); u += __ldg(a.bias + a.F + n); }
+                a.out[(long long)m * a.F + n] = free_gate_act(a.act, g) * u;
+                if (a.pre) { a.pre[(long long)m * 2 * a.F + n] = g; a.pre[(long long)m * 2 * a.F + a.F + n] = u; }
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int n = n0 + h * (TN / 2) + tx * 4;
+                float* q = a.out + blockIdx.z * a.plane + (long long)m * a.N + n;
+                if (VEC && n + 3 < a.N) *reinterpret_cast<float4*>(q) = make_float4(acc[i][4 * h], acc[i][4 * h + 1], acc[i][4 * h + 2], acc[i][4 * h + 3]);
+                else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (n + j < a.N) q[j] = acc[i][4 * h + j];
+                }
+            }
+        }
+    }
+}
+
+template <int MODE>
+int launch(const Args& a, bool vec, cudaStream_t s) {
+    constexpr int cols = MODE == GATED ? TN / 2 : TN;
+    const long long nn = (a.N + cols - 1) / cols, m128 = ((long long)a.M + 127) / 128, m64 = ((long long)a.M + 63) / 64;
+    if (nn > 65535) return FREE_ERR_UNSUPPORTED;
+    // time of a wave in 64-row units; equal: the larger tile (fewer shared-memory reads per product)
+    const long long w128 = 2 * ((m128 * nn * a.parts + kSms - 1) / kSms), w64 = (m64 * nn * a.parts + kSms - 1) / kSms;
+    const dim3 grid((unsigned)(w64 < w128 ? m64 : m128), (unsigned)nn, (unsigned)a.parts);
+    if (w64 < w128) {
+        if (vec) gated_simt_kernel<MODE, 64, true><<<grid, 128, 0, s>>>(a);
+        else gated_simt_kernel<MODE, 64, false><<<grid, 128, 0, s>>>(a);
+    } else {
+        if (vec) gated_simt_kernel<MODE, 128, true><<<grid, 256, 0, s>>>(a);
+        else gated_simt_kernel<MODE, 128, false><<<grid, 256, 0, s>>>(a);
+    }
+    return free_check_launch();
+}
+
+}  // namespace
+
+int gated_simt_forward(int act, int M, int F, int K, const float* x, const float* w, const float* bias, float* h, float* preact, cudaStream_t s) {
+    Args a{};
+    a.M = M; a.N = F; a.depth = K; a.A = x; a.B = w; a.lda = K; a.ldb = K; a.bias = bias; a.act = act; a.F = F; a.out = h; a.pre = preact; a.parts = 1;
+    return launch<GATED>(a, K % 4 == 0, s);
+}
+
+// Enough parts to give every SM two tiles, each at least 256 deep.
+GatedSplit gated_simt_split(bool dw, int M, int F, int K) {
+    const long long rows = dw ? 2LL * F : M, depth = dw ? M : 2LL * F;
+    const long long tiles = (rows + 63) / 64 * (((long long)K + TN - 1) / TN);
+    long long s = (2 * kSms + tiles - 1) / tiles;
+    if (s > depth / 256) s = depth / 256;
+    if (s > 64) s = 64;
+    return {s < 1 ? 1 : (int)s, rows};
+}
+
+int gated_simt_backward(bool dw, int M, int F, int K, const float* x, const float* w, const float* dz, float* out, float* parts, cudaStream_t s) {
+    const GatedSplit g = gated_simt_split(dw, M, F, K);
+    Args a{};
+    a.M = dw ? 2 * F : M; a.N = K; a.depth = dw ? M : 2 * F; a.F = F;
+    a.A = dz; a.lda = 2LL * F; a.B = dw ? x : w; a.ldb = K;
+    a.parts = g.parts; a.plane = g.plane_rows * K; a.out = g.parts > 1 ? parts : out;
+    const bool vec = K % 4 == 0 && F % 2 == 0;
+    FREE_TRY(dw ? launch<DW>(a, vec, s) : launch<DX>(a, vec, s));
+    return g.parts > 1 ? gated_add_parts(FREE_FP32, g.parts, a.plane, (long long)a.M * K, parts, out, s) : FREE_OK;
+}

@@ -95,3 +95,54 @@ def test_binding_checks(L):
         free.op_rope_axes(torch.zeros(2, 3, 4), torch.zeros(3, 1), (4,))
     with pytest.raises(ValueError):
         free.op_rope_axes(torch.zeros(1, 3, 2, 4), torch.zeros(3, 1), (4,), pairing="thirds")
+
+
+def _gated(L, dt=1, act=0, M=4, F=64, K=64, x=P, w=P, b=P, h=P, pre=P, err=P):
+    return L.free_op_gated_linear(dt, act, M, F, K, x, w, b, h, pre, err, None)
+
+
+def _gated_bwd(L, dt=1, act=0, M=4, F=64, K=64, x=P, w=P, pre=P, dh=P, dx=P, dw=P, db=P, ws=None, need=0, err=P):
+    return L.free_op_gated_linear_bwd(dt, act, M, F, K, x, w, pre, dh, dx, dw, db, ws, need, err, None)
+
+
+def test_gated_linear(L):
+    assert _gated(L, dt=2) == ARG and _gated(L, act=2) == ARG and _gated(L, act=-1) == ARG
+    for k in ("x", "w", "h", "err"):
+        assert _gated(L, **{k: None}) == ARG
+    assert _gated(L, M=-1) == SHAPE and _gated(L, F=0) == SHAPE and _gated(L, K=0) == SHAPE
+    for k in ("x", "w", "h", "pre"):
+        assert _gated(L, **{k: ODD}) == ALIGN
+    assert _gated(L, b=C.c_void_p(4098)) == ALIGN
+    assert _gated(L, F=60) == UNSUPPORTED and _gated(L, K=36) == UNSUPPORTED        # rows that are not multiples of 16 bytes
+    assert _gated(L, M=0, x=None, w=None, h=None, err=None) == 0
+
+
+def test_gated_linear_bwd(L):
+    assert _gated_bwd(L, dt=3) == ARG and _gated_bwd(L, act=7) == ARG
+    for k in ("x", "w", "pre", "dh", "err"):
+        assert _gated_bwd(L, **{k: None}) == ARG
+    assert _gated_bwd(L, M=-1) == SHAPE and _gated_bwd(L, F=0) == SHAPE
+    for k in ("x", "w", "pre", "dh", "dx", "dw"):
+        assert _gated_bwd(L, **{k: ODD}) == ALIGN
+    assert _gated_bwd(L, F=60) == UNSUPPORTED and _gated_bwd(L, K=36) == UNSUPPORTED
+    need = L.free_op_gated_linear_bwd_workspace_bytes(1, 4, 64, 64)
+    assert need >= 4 * 128 * 2
+    assert _gated_bwd(L) == WORKSPACE and _gated_bwd(L, ws=P, need=need - 1) == WORKSPACE
+    assert _gated_bwd(L, dx=None, dw=None, db=None) == 0
+    assert L.free_op_gated_linear_bwd_workspace_bytes(1, 4, 60, 64) == 0 and L.free_op_gated_linear_bwd_workspace_bytes(0, 0, 60, 64) == 0
+    # dz and, where a product is split, its parts: bounded by a few times the operands
+    for dt, M, F, K in ((1, 24576, 4608, 1152), (1, 1, 4608, 1152), (1, 9000, 40, 64), (0, 6001, 33, 70), (0, 1, 1, 1)):
+        n = L.free_op_gated_linear_bwd_workspace_bytes(dt, M, F, K)
+        assert n >= M * 2 * F * (2 if dt else 4)
+        assert n <= M * 2 * F * 4 + 1200 * 2 * F * 4 + 64 * 4 * K * (max(M, 2 * F) + 256) + 1024
+
+
+def test_gated_binding_checks(L):
+    import paper_2511_20390_b200 as free
+    x, w = torch.zeros(4, 8), torch.zeros(16, 8)
+    for call in (lambda: free.op_gated_linear(x, w), lambda: free.op_gated_linear(x, torch.zeros(15, 8)),
+                 lambda: free.op_gated_linear(x, w, act="relu"), lambda: free.op_gated_linear(torch.zeros(4, 2, 4), w),
+                 lambda: free.op_gated_linear_bwd(x, w, torch.zeros(4, 16), torch.zeros(4, 8), act="tanh")):
+        with pytest.raises(ValueError):
+            call()
+    assert free.op_device_error("cuda:0") == 0                      # nothing has run there
