@@ -13,5 +13,6 @@ def __getattr__(name):
     if name in ("spec_verify", "spec_verify_fused", "spec_verify_host", "fit_lambda_profile", "drafter_loss", "Model", "DeviceSchedule", "lib", "FreeError",
                 "op_linear", "op_ln_modulate", "op_attention", "op_layer_norm", "op_layer_norm_bwd", "op_rope_axes", "op_gated_linear", "op_gated_linear_bwd", "op_device_error", "selftest_bounded_wait", "split_range", "LIB_PATH"):
         from . import binding
-        return getattr(binding, name)
+        value = globals()[name] = getattr(binding, name)               # found without this function from now on
+        return value
     raise AttributeError(name)

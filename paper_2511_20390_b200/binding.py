@@ -605,46 +605,59 @@ _DTYPE = {torch.float32: FREE_FP32, torch.bfloat16: FREE_BF16}
 
 def _code(dtype):
     """FREE_* code of a torch dtype (the codes themselves pass through)."""
-    if dtype in (FREE_FP32, FREE_BF16):
-        return dtype
-    if dtype not in _DTYPE:
-        raise ValueError(f"expected float32 or bfloat16, got {dtype}")
-    return _DTYPE[dtype]
+    c = _DTYPE.get(dtype)
+    if c is None:
+        if dtype not in (FREE_FP32, FREE_BF16):
+            raise ValueError(f"expected float32 or bfloat16, got {dtype}")
+        c = dtype
+    return c
 
 
-def _same_device(first, *others):
-    for t in (first,) + others:
-        if t is not None and (not t.is_cuda or t.device != first.device):
+# The calls below are short on the GPU (a few us for small batches), so the host's part is kept short: integers for
+# pointers, device indices instead of device objects, the raw handle of the current stream.
+def _device_of(first, *others):
+    d = first.get_device()                                         # -1 on the host
+    for t in others:
+        if t is not None and t.get_device() != d:
             raise ValueError("expected CUDA tensors on one device")
+    if d < 0:
+        raise ValueError("expected CUDA tensors on one device")
+    return d
 
 
-def _run(device, fn, what):
-    """fn(stream) with `device` current, on the stream that is current there."""
-    if device.index == torch.cuda.current_device():
-        code = fn(_stream())
+def _adr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _launch(what, device, *args):
+    """Library call `what` with `device` current, on the stream that is current there (its last argument)."""
+    fn = getattr(lib(), what)
+    if device == torch.cuda.current_device():
+        code = fn(*args, torch._C._cuda_getCurrentRawStream(device))
     else:
         with torch.cuda.device(device):
-            code = fn(_stream())
+            code = fn(*args, torch._C._cuda_getCurrentRawStream(device))
     if code != 0:
         raise FreeError(code, what)
 
 
 def _rows(t, M, D, what):
     """Row stride of a [M, D] matrix whose rows are dense."""
-    if t.dim() != 2 or t.shape[0] != M or t.shape[1] != D or (D > 1 and t.stride(1) != 1):
+    if t.shape != (M, D) or (D > 1 and t.stride(1) != 1):
         raise ValueError(f"{what}: expected a [{M}, {D}] matrix with dense rows")
     return t.stride(0) if M > 1 else max(D, t.stride(0))
 
 
 def _group_rows(t, groups, D, what):
     """Group stride of a [D] or [groups, D] fp32 table (rows of an adaLN table may be far apart)."""
-    if t.dtype != torch.float32 or t.shape[-1] != D or t.dim() > 2 or (D > 1 and t.stride(-1) != 1):
+    n = t.dim()
+    if t.dtype != torch.float32 or n > 2 or n < 1 or t.shape[n - 1] != D or (D > 1 and t.stride(n - 1) != 1):
         raise ValueError(f"{what}: expected fp32 [{groups}, {D}] with dense rows")
-    if t.dim() == 1:
+    if n == 1 or t.shape[0] == 1:
         return 0                                                   # one row for every group
-    if t.shape[0] not in (1, groups):
+    if t.shape[0] != groups:
         raise ValueError(f"{what}: expected fp32 [{groups}, {D}]")
-    return t.stride(0) if t.shape[0] > 1 else 0
+    return t.stride(0)
 
 
 def _groups(M, rows_per_group):
@@ -663,18 +676,23 @@ def op_layer_norm(x, weight=None, bias=None, rows_per_group=None, unit_offset=Fa
         raise ValueError("x: expected a matrix")
     M, D = x.shape
     groups, rows = _groups(M, rows_per_group)
-    _same_device(x, weight, bias, out)
-    xs = _rows(x, M, D, "x")
-    strides = [_group_rows(t, groups, D, n) for t, n in ((weight, "weight"), (bias, "bias")) if t is not None]
-    if len(set(strides)) > 1:
-        raise ValueError("weight and bias need the same distance between groups")
-    dt = _ACT[_code(x.dtype if out_dtype is None else out_dtype)] if out is None else out.dtype
+    dev = _device_of(x, weight, bias, out)
+    xc, xs = _code(x.dtype), _rows(x, M, D, "x")
+    ms = 0 if weight is None else _group_rows(weight, groups, D, "weight")
+    if bias is not None:
+        bs = _group_rows(bias, groups, D, "bias")
+        if weight is not None and bs != ms:
+            raise ValueError("weight and bias need the same distance between groups")
+        ms = bs
     if out is None:
-        out = torch.empty((M, D), dtype=dt, device=x.device)
+        yc = xc if out_dtype is None else _code(out_dtype)
+        out = torch.empty((M, D), dtype=_ACT[yc], device=x.device)
+        ys = D
+    else:
+        yc, ys = _code(out.dtype), _rows(out, M, D, "out")
     stats = torch.empty((M, 2), dtype=torch.float32, device=x.device) if want_stats else None
-    _run(x.device, lambda s: lib().free_op_layer_norm(_code(x.dtype), _code(dt), groups, rows, D, _ptr(x), xs, _ptr(weight), _ptr(bias),
-                                                      strides[0] if strides else 0, int(bool(unit_offset)), float(eps), _ptr(out),
-                                                      _rows(out, M, D, "out"), _ptr(stats), s), "free_op_layer_norm")
+    _launch("free_op_layer_norm", dev, xc, yc, groups, rows, D, x.data_ptr(), xs, _adr(weight), _adr(bias), ms, 1 if unit_offset else 0, eps,
+            out.data_ptr(), ys, _adr(stats))
     return (out, stats) if want_stats else out
 
 
@@ -686,28 +704,27 @@ def op_layer_norm_bwd(x, dy, stats, weight=None, rows_per_group=None, unit_offse
         raise ValueError("x: expected a matrix")
     M, D = x.shape
     groups, rows = _groups(M, rows_per_group)
-    _same_device(x, dy, stats, weight, dres, dx)
-    xs, dys = _rows(x, M, D, "x"), _rows(dy, M, D, "dy")
-    if stats.dtype != torch.float32 or tuple(stats.shape) != (M, 2) or not stats.is_contiguous():
+    dev = _device_of(x, dy, stats, weight, dres, dx)
+    if stats.dtype != torch.float32 or stats.shape != (M, 2) or not stats.is_contiguous():
         raise ValueError("stats: expected the contiguous fp32 [M, 2] of the forward call")
-    ms = 0 if weight is None else _group_rows(weight, groups, D, "weight")
-    for t, n in ((dres, "dres"), (dx, "dx")):
-        if t is not None and t.dtype != x.dtype:
-            raise ValueError(f"{n}: expected x's dtype")
+    if (dres is not None and dres.dtype != x.dtype) or (dx is not None and dx.dtype != x.dtype):
+        raise ValueError("dres, dx: expected x's dtype")
     if dx is None:
         dx = torch.empty((M, D), dtype=x.dtype, device=x.device)
     dw = torch.empty((groups, D), dtype=torch.float32, device=x.device) if want_dweight else None
     db = torch.empty((groups, D), dtype=torch.float32, device=x.device) if want_dbias else None
     need = lib().free_op_layer_norm_bwd_workspace_bytes(groups, rows, D) if want_dweight or want_dbias else 0
     ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
-    _run(x.device, lambda s: lib().free_op_layer_norm_bwd(
-        _code(x.dtype), _code(dy.dtype), groups, rows, D, _ptr(x), xs, _ptr(dy), dys, _ptr(stats), _ptr(weight), ms,
-        int(bool(unit_offset)), _ptr(dres), 0 if dres is None else _rows(dres, M, D, "dres"), _ptr(dx), _rows(dx, M, D, "dx"),
-        _ptr(dw), _ptr(db), D, _ptr(ws), need, s), "free_op_layer_norm_bwd")
+    _launch("free_op_layer_norm_bwd", dev, _code(x.dtype), _code(dy.dtype), groups, rows, D, x.data_ptr(), _rows(x, M, D, "x"),
+            dy.data_ptr(), _rows(dy, M, D, "dy"), stats.data_ptr(), _adr(weight),
+            0 if weight is None else _group_rows(weight, groups, D, "weight"), 1 if unit_offset else 0,
+            _adr(dres), 0 if dres is None else _rows(dres, M, D, "dres"), dx.data_ptr(), _rows(dx, M, D, "dx"),
+            _adr(dw), _adr(db), D, _adr(ws), need)
     return dx, dw, db
 
 
 ROPE_PAIRING = {"interleaved": 0, "halves": 1}
+_AXES = {n: C.c_int32 * n for n in range(1, 5)}
 
 
 def op_rope_axes(x, pos, axis_dims, base=10000.0, pairing="interleaved", joint_freq=False, inverse=False, out=None):
@@ -719,20 +736,25 @@ def op_rope_axes(x, pos, axis_dims, base=10000.0, pairing="interleaved", joint_f
         raise ValueError("x: expected [n_seq, n_tok, heads, d_head] with dense heads")
     if pairing not in ROPE_PAIRING:
         raise ValueError("pairing: expected 'interleaved' or 'halves'")
-    n_seq, n_tok, heads, d_head = x.shape
-    _same_device(x, pos, out)
-    axes = (C.c_int32 * len(axis_dims))(*axis_dims)
-    _dev(pos, torch.float32)
-    if tuple(pos.shape) not in ((n_tok, len(axis_dims)), (n_seq, n_tok, len(axis_dims))):
-        raise ValueError("pos: expected [n_tok, n_axes] or [n_seq, n_tok, n_axes]")
+    n_axes = len(axis_dims)
+    if n_axes not in _AXES:
+        raise ValueError("axis_dims: expected one to four axes")
+    shape = n_seq, n_tok, heads, d_head = x.shape
+    dev = _device_of(x, pos, out)
+    if pos.dtype != torch.float32 or not pos.is_contiguous() or (pos.shape != (n_tok, n_axes) and pos.shape != (n_seq, n_tok, n_axes)):
+        raise ValueError("pos: expected contiguous fp32 [n_tok, n_axes] or [n_seq, n_tok, n_axes]")
+    xs = x.stride()
     if out is None:
-        out = torch.empty((n_seq, n_tok, heads, d_head), dtype=x.dtype, device=x.device)
-    elif out.shape != x.shape or out.dtype != x.dtype or (d_head > 1 and out.stride(3) != 1):
-        raise ValueError("out: expected x's shape and dtype with dense heads")
-    _run(x.device, lambda s: lib().free_op_rope_axes(
-        _code(x.dtype), ROPE_PAIRING[pairing], int(bool(joint_freq)), int(bool(inverse)), n_seq, n_tok, heads, d_head, len(axis_dims), axes,
-        float(base), _ptr(pos), n_tok * len(axis_dims) if pos.dim() == 3 else 0, _ptr(x), x.stride(0), x.stride(1), x.stride(2),
-        _ptr(out), out.stride(0), out.stride(1), out.stride(2), s), "free_op_rope_axes")
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        hs = heads * d_head
+        ys = (n_tok * hs, hs, d_head)
+    else:
+        if out.shape != shape or out.dtype != x.dtype or (d_head > 1 and out.stride(3) != 1):
+            raise ValueError("out: expected x's shape and dtype with dense heads")
+        ys = out.stride()
+    _launch("free_op_rope_axes", dev, _code(x.dtype), ROPE_PAIRING[pairing], 1 if joint_freq else 0, 1 if inverse else 0, n_seq, n_tok, heads,
+            d_head, n_axes, _AXES[n_axes](*axis_dims), base, pos.data_ptr(), n_tok * n_axes if pos.dim() == 3 else 0,
+            x.data_ptr(), xs[0], xs[1], xs[2], out.data_ptr(), ys[0], ys[1], ys[2])
     return out
 
 
@@ -741,14 +763,14 @@ _ERROR_WORDS = {}
 
 
 def _error_word(device):
-    """The device error word that the gated layer's calls on `device` share: zeroed once, OR-ed into by a kernel whose bounded
+    """The device error word that the gated layer's calls on a device share: zeroed once, OR-ed into by a kernel whose bounded
     wait gave up, never cleared in between (so calls on several streams and replays of captured graphs may share it)."""
     w = _ERROR_WORDS.get(device)
     if w is None:
-        if torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("call the operator once on this device before capturing it into a CUDA graph")
         with torch.cuda.device(device):
-            w = torch.zeros(1, dtype=torch.int32, device=device)
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("call the operator once on this device before capturing it into a CUDA graph")
+            w = torch.zeros(1, dtype=torch.int32, device="cuda")
             torch.cuda.current_stream().synchronize()              # zero before any other stream can use it
         _ERROR_WORDS[device] = w
     return w
@@ -756,19 +778,18 @@ def _error_word(device):
 
 def op_device_error(device=None):
     """Waits for `device` and returns the error word of the gated layer's calls on it so far (0: no bounded wait gave up)."""
-    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-    if device.index is None:
-        device = torch.device("cuda", torch.cuda.current_device())
-    if device not in _ERROR_WORDS:
+    index = None if device is None else torch.device(device).index
+    if index is None:
+        index = torch.cuda.current_device()
+    if index not in _ERROR_WORDS:
         return 0
-    torch.cuda.synchronize(device)
-    return int(_ERROR_WORDS[device].item()) & 0xFFFFFFFF
+    torch.cuda.synchronize(index)
+    return int(_ERROR_WORDS[index].item()) & 0xFFFFFFFF
 
 
 def _dense(t, dtype, shape, what):
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {list(shape)}")
-    return t
 
 
 def op_gated_linear(x, w, bias=None, act="silu", want_preact=False, out=None):
@@ -781,16 +802,18 @@ def op_gated_linear(x, w, bias=None, act="silu", want_preact=False, out=None):
     if act not in ACTIVATIONS:
         raise ValueError("act: expected 'silu' or 'gelu'")
     (M, K), F, dtype = x.shape, w.shape[0] // 2, x.dtype
-    _same_device(x, w, bias, out)
+    dev, code = _device_of(x, w, bias, out), _code(dtype)
     _dense(x, dtype, (M, K), "x"); _dense(w, dtype, (2 * F, K), "w")
     if bias is not None:
         _dense(bias, torch.float32, (2 * F,), "bias")
-    h = torch.empty((M, F), dtype=dtype, device=x.device) if out is None else _dense(out, dtype, (M, F), "out")
+    if out is None:
+        out = torch.empty((M, F), dtype=dtype, device=x.device)
+    else:
+        _dense(out, dtype, (M, F), "out")
     pre = torch.empty((M, 2 * F), dtype=dtype, device=x.device) if want_preact else None
-    err = _error_word(x.device) if dtype == torch.bfloat16 else None
-    _run(x.device, lambda s: lib().free_op_gated_linear(_code(dtype), ACTIVATIONS[act], M, F, K, _ptr(x), _ptr(w), _ptr(bias), _ptr(h),
-                                                        _ptr(pre), _ptr(err), s), "free_op_gated_linear")
-    return (h, pre) if want_preact else h
+    _launch("free_op_gated_linear", dev, code, ACTIVATIONS[act], M, F, K, x.data_ptr(), w.data_ptr(), _adr(bias), out.data_ptr(), _adr(pre),
+            _error_word(dev).data_ptr() if code == FREE_BF16 else None)
+    return (out, pre) if want_preact else out
 
 
 def op_gated_linear_bwd(x, w, preact, dh, act="silu", want_dx=True, want_dw=True, want_dbias=True):
@@ -801,18 +824,16 @@ def op_gated_linear_bwd(x, w, preact, dh, act="silu", want_dx=True, want_dw=True
     if act not in ACTIVATIONS:
         raise ValueError("act: expected 'silu' or 'gelu'")
     (M, K), F, dtype = x.shape, w.shape[0] // 2, x.dtype
-    _same_device(x, w, preact, dh)
+    dev, code = _device_of(x, w, preact, dh), _code(dtype)
     _dense(x, dtype, (M, K), "x"); _dense(w, dtype, (2 * F, K), "w")
     _dense(preact, dtype, (M, 2 * F), "preact"); _dense(dh, dtype, (M, F), "dh")
-    code, dev = _code(dtype), x.device
-    dx = torch.empty((M, K), dtype=dtype, device=dev) if want_dx else None
-    dw = torch.empty((2 * F, K), dtype=dtype, device=dev) if want_dw else None
-    db = torch.empty(2 * F, dtype=torch.float32, device=dev) if want_dbias else None
+    dx = torch.empty((M, K), dtype=dtype, device=x.device) if want_dx else None
+    dw = torch.empty((2 * F, K), dtype=dtype, device=x.device) if want_dw else None
+    db = torch.empty(2 * F, dtype=torch.float32, device=x.device) if want_dbias else None
     need = lib().free_op_gated_linear_bwd_workspace_bytes(code, M, F, K)
-    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    err = _error_word(dev) if dtype == torch.bfloat16 else None
-    _run(dev, lambda s: lib().free_op_gated_linear_bwd(code, ACTIVATIONS[act], M, F, K, _ptr(x), _ptr(w), _ptr(preact), _ptr(dh), _ptr(dx),
-                                                       _ptr(dw), _ptr(db), _ptr(ws), need, _ptr(err), s), "free_op_gated_linear_bwd")
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    _launch("free_op_gated_linear_bwd", dev, code, ACTIVATIONS[act], M, F, K, x.data_ptr(), w.data_ptr(), preact.data_ptr(), dh.data_ptr(),
+            _adr(dx), _adr(dw), _adr(db), _adr(ws), need, _error_word(dev).data_ptr() if code == FREE_BF16 else None)
     return dx, dw, db
 
 

@@ -10,8 +10,12 @@
 
 __device__ __forceinline__ float free_logistic(float v) { return 1.f / (1.f + expf(-v)); }
 // The same from the fast exponential and division (a few units of 2^-22): for results that are rounded to bf16.
-// e^-v overflows to infinity for v < -88 and the quotient is 0, the limit.
-__device__ __forceinline__ float free_logistic_fast(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+// e^-v overflows to infinity for v < -88 and the reciprocal is 0, the limit.
+__device__ __forceinline__ float free_logistic_fast(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-v)));
+    return r;
+}
 __device__ __forceinline__ float free_gate_arg(int act, float g) { return act == FREE_ACT_SILU ? g : FREE_GELU_2K * (g + FREE_GELU_C * g * g * g); }
 __device__ __forceinline__ float free_gate_act_fast(int act, float g) { return g * free_logistic_fast(free_gate_arg(act, g)); }
 __device__ __forceinline__ float free_gate_act(int act, float g) { return g * free_logistic(free_gate_arg(act, g)); }

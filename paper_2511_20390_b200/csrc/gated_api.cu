@@ -10,50 +10,74 @@
 namespace {
 
 constexpr int kSms = 148;
-constexpr int kThreads = 128;
-constexpr int kRows = 4;                    // rows whose loads are in flight
+constexpr int kMaxThreads = 256;
+constexpr int kPerSm = 4;                    // such CTAs per SM (register budget)
+constexpr int kRows = 2;                     // rows whose loads are in flight
 
 template <typename T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
-__device__ __forceinline__ float to_f(float v) { return v; }
-__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void from_f(float& d, float v) { d = v; }
 __device__ __forceinline__ void from_f(__nv_bfloat16& d, float v) { d = __float2bfloat16(v); }
 
-// dz of a block of V * kThreads columns over a run of rows; a thread keeps its columns, so db stays in its registers.
-template <typename T, int V, bool FAST>
-__global__ void __launch_bounds__(kThreads) gated_grad_kernel(int act, int M, int F, int chunks, const T* pre, const T* dh, T* dz, float* db) {
+// V values as one access; bf16 pairs stay packed in 32-bit words
+template <typename T, int V> struct Vals {
+    Pack<uint32_t, V * (int)sizeof(T) / 4> d;
+    __device__ __forceinline__ float operator[](int i) const {
+        if (sizeof(T) == 4) return __uint_as_float(d.v[i]);
+        return __uint_as_float(i % 2 ? d.v[i / 2] & 0xffff0000u : d.v[i / 2] << 16);
+    }
+    __device__ __forceinline__ void set(const float (&f)[V]) {
+        if (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) d.v[i % (V * (int)sizeof(T) / 4)] = __float_as_uint(f[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+                d.v[i] = *reinterpret_cast<const uint32_t*>(&b);
+            }
+        }
+    }
+    __device__ __forceinline__ void load(const T* p) { d = *reinterpret_cast<const decltype(d)*>(p); }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<decltype(d)*>(p) = d; }
+};
+
+// dz of a block of columns over a run of rows; a thread keeps its V columns, so db stays in its registers.
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kMaxThreads, kPerSm) gated_grad_kernel(int M, int F, int chunks, const T* __restrict__ pre,
+                                                                         const T* __restrict__ dh, T* __restrict__ dz, float* __restrict__ db) {
     free_grid_dep_wait();
     free_grid_dep_launch();
-    const int col = (blockIdx.x * kThreads + threadIdx.x) * V;
+    const int col = (blockIdx.x * blockDim.x + threadIdx.x) * V;
     if (col >= F) return;
-    const int r0 = (int)((long long)M * blockIdx.y / chunks), r1 = (int)((long long)M * (blockIdx.y + 1) / chunks);
     float sg[V] = {}, su[V] = {};
-    using P = Pack<T, V>;
-    for (int r = r0; r < r1; r += kRows) {
+    using P = Vals<T, V>;
+    // rows blockIdx.y, blockIdx.y + chunks, ...: the CTAs in flight work on neighbouring rows
+    for (long long r = blockIdx.y; r < M; r += (long long)kRows * chunks) {
         P g[kRows], u[kRows], d[kRows];
 #pragma unroll
-        for (int k = 0; k < kRows; ++k)
-            if (r + k < r1) {
-                const long long row = r + k;
-                g[k] = *reinterpret_cast<const P*>(pre + row * 2 * F + col);
-                u[k] = *reinterpret_cast<const P*>(pre + row * 2 * F + F + col);
-                d[k] = *reinterpret_cast<const P*>(dh + row * F + col);
-            }
+        for (int k = 0; k < kRows; ++k) {                          // past the last row: this one again, not counted or stored
+            const long long row = r + (long long)k * chunks < M ? r + (long long)k * chunks : r;
+            g[k].load(pre + row * 2 * F + col);
+            u[k].load(pre + row * 2 * F + F + col);
+            d[k].load(dh + row * F + col);
+        }
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
-            if (r + k >= r1) break;
-            const long long row = r + k;
+            const long long row = r + (long long)k * chunks;
+            if (row >= M) break;
+            float dg[V], du[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float zg = to_f(g[k].v[e]), zu = to_f(u[k].v[e]), dd = to_f(d[k].v[e]);
-                const float arg = free_gate_arg(act, zg);
-                const float s = FAST ? free_logistic_fast(arg) : free_logistic(arg);
-                const float dg = dd * zu * free_gate_slope(act, zg, s), du = dd * zg * s;
-                sg[e] += dg; su[e] += du;
-                from_f(g[k].v[e], dg); from_f(u[k].v[e], du);
+                const float zg = g[k][e], dd = d[k][e], arg = free_gate_arg(ACT, zg);
+                const float s = sizeof(T) == 2 ? free_logistic_fast(arg) : free_logistic(arg);
+                dg[e] = dd * u[k][e] * free_gate_slope(ACT, zg, s); du[e] = dd * (zg * s);
+                sg[e] += dg[e]; su[e] += du[e];
             }
-            *reinterpret_cast<P*>(dz + row * 2 * F + col) = g[k];
-            *reinterpret_cast<P*>(dz + row * 2 * F + F + col) = u[k];
+            P o;
+            o.set(dg);
+            o.store(dz + row * 2 * F + col);
+            o.set(du);
+            o.store(dz + row * 2 * F + F + col);
         }
     }
     if (db) {
@@ -103,13 +127,19 @@ __global__ void __launch_bounds__(256) gated_add_kernel(int parts, long long pla
 
 int vec_of(int dtype, int F) { return dtype == FREE_BF16 ? 8 : (F % 4 == 0 ? 4 : 1); }
 
-// Runs of rows of the elementwise pass: enough CTAs for the GPU, at least 16 rows each.
-int chunks_of(int dtype, int M, int F) {
-    const int v = vec_of(dtype, F), blocks = (F / v + kThreads - 1) / kThreads;
-    int c = (kSms * 8 + blocks - 1) / blocks;
-    if (c > M / 16) c = M / 16;
-    return c < 1 ? 1 : (c > 65535 ? 65535 : c);
+// CTAs of the elementwise pass: column blocks of equal width, and runs of rows, enough for the GPU and at least 16 rows each.
+struct GradGrid { int blocks, threads, chunks; };
+GradGrid grad_grid(int dtype, int M, int F) {
+    const int v = vec_of(dtype, F), vecs = F / v;
+    GradGrid g;
+    g.blocks = (vecs + kMaxThreads - 1) / kMaxThreads;
+    g.threads = ((vecs + g.blocks - 1) / g.blocks + 31) / 32 * 32;
+    g.chunks = (int)(((long long)kSms * 16 * 128 / g.threads + g.blocks - 1) / g.blocks);
+    if (g.chunks > M / 16) g.chunks = M / 16;
+    if (g.chunks < 1) g.chunks = 1;
+    return g;
 }
+int chunks_of(int dtype, int M, int F) { return grad_grid(dtype, M, F).chunks; }
 
 struct Layout { size_t dz, db, parts, total; };
 Layout layout_of(int dtype, int M, int F, int K) {
@@ -132,11 +162,12 @@ Layout layout_of(int dtype, int M, int F, int K) {
 bool known(int dtype) { return dtype == FREE_FP32 || dtype == FREE_BF16; }
 bool known_act(int act) { return act == FREE_ACT_SILU || act == FREE_ACT_GELU; }
 
-template <typename T, int V, bool FAST>
-int grad(int act, int M, int F, int chunks, const void* pre, const void* dh, void* dz, float* db, cudaStream_t s) {
-    const dim3 grid((unsigned)((F / V + kThreads - 1) / kThreads), (unsigned)chunks);
-    return free_launch(free_overlap_for_rows(M), gated_grad_kernel<T, V, FAST>, grid, dim3(kThreads), 0, s, act, M, F, chunks, (const T*)pre,
-                       (const T*)dh, (T*)dz, db);
+template <typename T, int V>
+int grad(int dtype, int act, int M, int F, const void* pre, const void* dh, void* dz, float* db, cudaStream_t s) {
+    const GradGrid g = grad_grid(dtype, M, F);
+    auto kernel = act == FREE_ACT_SILU ? gated_grad_kernel<T, V, FREE_ACT_SILU> : gated_grad_kernel<T, V, FREE_ACT_GELU>;
+    return free_launch(free_overlap_for_rows(M), kernel, dim3((unsigned)g.blocks, (unsigned)g.chunks), dim3(g.threads), 0, s, M, F, g.chunks,
+                       (const T*)pre, (const T*)dh, (T*)dz, db);
 }
 
 }  // namespace
@@ -198,9 +229,9 @@ extern "C" int free_op_gated_linear_bwd(int dtype, int act, int M, int F, int K,
     float* parts = (float*)(base + l.parts);
     const int chunks = chunks_of(dtype, M, F);
     float* db = !dbias ? nullptr : (chunks > 1 ? (float*)(base + l.db) : dbias);
-    if (dtype == FREE_BF16) FREE_TRY((grad<__nv_bfloat16, 8, true>(act, M, F, chunks, preact, dh, dz, db, s)));
-    else if (vec_of(dtype, F) == 4) FREE_TRY((grad<float, 4, false>(act, M, F, chunks, preact, dh, dz, db, s)));
-    else FREE_TRY((grad<float, 1, false>(act, M, F, chunks, preact, dh, dz, db, s)));
+    if (dtype == FREE_BF16) FREE_TRY((grad<__nv_bfloat16, 8>(dtype, act, M, F, preact, dh, dz, db, s)));
+    else if (vec_of(dtype, F) == 4) FREE_TRY((grad<float, 4>(dtype, act, M, F, preact, dh, dz, db, s)));
+    else FREE_TRY((grad<float, 1>(dtype, act, M, F, preact, dh, dz, db, s)));
     if (dbias && chunks > 1)
         FREE_TRY(free_launch(free_launch_overlap_enabled(), gated_bias_kernel, dim3((2u * F + 31) / 32), dim3(512), 0, s, chunks, 2 * F, (const float*)db, dbias));
     if (dtype == FREE_BF16) {

@@ -9,6 +9,8 @@
 // warps beyond.  Statistics are fp32: each warp takes the mean of its own columns and their squared deviations from it,
 // and the parts are combined with the exact formula M2 = sum M2_k + n_k (mean_k - mean)^2, so that a large mean cancels
 // nothing and a row costs one CTA barrier.
+// Rows whose starts are 16-byte aligned are copied to shared memory asynchronously several rows ahead of their use, every
+// thread its own columns (no barrier is needed for that): the bytes in flight then do not cost registers, and more CTAs fit.
 // The gradients of w and b are column sums over a group's rows.  A CTA keeps them in fp32 registers over a run of rows of
 // one group and writes one partial row; a second, small launch adds the partial rows of a group in a fixed order, so that
 // repeats are bit-identical (no atomics).
@@ -19,58 +21,104 @@ namespace {
 constexpr int kMaxWarps = 32;
 constexpr int kMaxD = kMaxWarps * 256;
 constexpr int kSms = 148;
+constexpr int kWide = 5;                                           // blocks per warp of the forward kernel for several warps
 
-template <typename T> __device__ __forceinline__ void ld8(const T* p, float (&v)[8]);
-template <> __device__ __forceinline__ void ld8<float>(const float* p, float (&v)[8]) {
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-template <> __device__ __forceinline__ void ld8<__nv_bfloat16>(const __nv_bfloat16* p, float (&v)[8]) {
-    const uint4 u = __ldcs(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-}
-__device__ __forceinline__ void st8(float* p, const float (&v)[8]) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ void st8(__nv_bfloat16* p, const float (&v)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t*>(&b);
+// Eight columns as they come from memory (bf16 stays packed until it is used).
+template <typename T, bool VEC> struct Raw {
+    uint32_t r[VEC ? 2 * sizeof(T) : 8];
+    __device__ __forceinline__ float operator[](int i) const {
+        if (!VEC || sizeof(T) == 4) return __uint_as_float(r[i]);
+        return __uint_as_float(i % 2 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
     }
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+};
+// four columns, global to shared memory
+template <typename T> __device__ __forceinline__ void copy4_async(uint32_t smem, const T* g) {
+    if (sizeof(T) == 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(g) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem), "l"(g) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void st4(float* p, const float* v) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void st4(__nv_bfloat16* p, const float* v) {
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
 }
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void st1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st1(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
 
-// The columns of a lane.  Warp k of a team of W owns the 256-column blocks k, W + k, ...  (step i: block i W + k).
-// VEC: lane l holds columns 8 l .. 8 l + 7 of a block as 16-byte accesses (D % 8 == 0, row starts 16-byte aligned);
-// otherwise columns l, l + 32, ..., l + 224: any D, any row stride, whole-warp runs of consecutive elements.
-template <bool VEC> struct Cols {
-    int D, W, k, lane;
-    __device__ __forceinline__ int at(int i, int e) const { return (i * W + k) * 256 + (VEC ? lane * 8 + e : e * 32 + lane); }
-    __device__ __forceinline__ bool in(int i, int e) const { return at(i, VEC ? 0 : e) < D; }
-    template <typename E> __device__ __forceinline__ void load(const E* row, int i, float (&v)[8]) const {
+// The columns of a lane: warp k of a team owns the 256-column blocks k NV .. k NV + NV - 1.
+// VEC: lane l holds columns 4 l .. 4 l + 3 of each half of a block, so that the accesses of a warp are whole runs of 512
+// (fp32) or 256 (bf16) bytes; D % 4 == 0, rows aligned to four elements.  (Eight consecutive columns per lane, two 16-byte
+// accesses 32 bytes apart in fp32, make two half-used sectors of every sector: measured 20 to 40% slower.)
+// Otherwise columns l, l + 32, ..., l + 224: any D, any row stride.
+template <bool VEC, int NV> struct Cols {
+    int D, k, lane;
+    __device__ __forceinline__ int at(int i, int e) const {
+        return (k * NV + i) * 256 + (VEC ? (e / 4) * 128 + lane * 4 + e % 4 : e * 32 + lane);
+    }
+    __device__ __forceinline__ bool in(int i, int e) const { return at(i, VEC ? e / 4 * 4 : e) < D; }
+    // straight into registers
+    template <typename E> __device__ __forceinline__ void load(const E* row, int i, Raw<E, VEC>& v) const {
         if (VEC) {
-            if (in(i, 0)) ld8<E>(row + at(i, 0), v);
-            else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = 0.f;
+            for (int h = 0; h < 2; ++h) {
+                constexpr int N = (int)sizeof(E);                  // 32-bit words of four columns
+                const E* p = row + at(i, 4 * h);
+                const bool ok = in(i, 4 * h);
+                if (N == 4) {
+                    const uint4 u = ok ? __ldcs(reinterpret_cast<const uint4*>(p)) : make_uint4(0u, 0u, 0u, 0u);
+                    v.r[h * N] = u.x; v.r[h * N + 1] = u.y; v.r[h * N + N - 2] = u.z; v.r[h * N + N - 1] = u.w;
+                } else {
+                    const uint2 u = ok ? __ldcs(reinterpret_cast<const uint2*>(p)) : make_uint2(0u, 0u);
+                    v.r[h * N] = u.x; v.r[h * N + 1] = u.y;
+                }
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = in(i, e) ? to_f(row[at(i, e)]) : 0.f;
+            for (int e = 0; e < 8; ++e) v.r[e] = in(i, e) ? __float_as_uint(to_f(row[at(i, e)])) : 0u;
+        }
+    }
+    // a table's row (the L1 serves it: every row of a group reads the same).  aligned: four columns are one access
+    __device__ __forceinline__ void table(const float* row, int i, bool aligned, float add, float (&v)[8]) const {
+        if (VEC && aligned) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float4 f = in(i, 4 * h) ? __ldg(reinterpret_cast<const float4*>(row + at(i, 4 * h))) : make_float4(0.f, 0.f, 0.f, 0.f);
+                v[4 * h] = f.x + add; v[4 * h + 1] = f.y + add; v[4 * h + 2] = f.z + add; v[4 * h + 3] = f.w + add;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = in(i, e) ? __ldg(row + at(i, e)) + add : 0.f;
+        }
+    }
+    // vector form, ahead of time: into shared memory, [half][thread] of a region of 8 elements per thread, and back from there
+    template <typename E> __device__ __forceinline__ uint32_t place(uint32_t region, int half) const {
+        return region + (half * blockDim.x + threadIdx.x) * 4 * (uint32_t)sizeof(E);
+    }
+    template <typename E> __device__ __forceinline__ void send(const E* row, int i, uint32_t region) const {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (in(i, 4 * h)) copy4_async<E>(place<E>(region, h), row + at(i, 4 * h));
+    }
+    template <typename E> __device__ __forceinline__ void take(uint32_t region, int i, Raw<E, VEC>& v) const {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            constexpr int N = (int)sizeof(E);                      // 32-bit words of four columns
+            uint32_t u[4];
+            if (N == 4) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(place<E>(region, h)) : "memory");
+            else asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(u[0]), "=r"(u[1]) : "r"(place<E>(region, h)) : "memory");
+#pragma unroll
+            for (int q = 0; q < N; ++q) v.r[h * N + q] = in(i, 4 * h) ? u[q] : 0u;      // outside: nothing was copied there
         }
     }
     template <typename E> __device__ __forceinline__ void store(E* row, int i, const float (&v)[8]) const {
         if (VEC) {
-            if (in(i, 0)) st8(row + at(i, 0), v);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (in(i, 4 * h)) st4(row + at(i, 4 * h), v + 4 * h);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -86,6 +134,7 @@ struct NormArgs {
     const float *weight, *bias; long long mod_stride; float unit;   // unit: 1 where the weight is stored as an offset from one
     float eps;
     void* y; long long y_stride;
+    bool table_vec;                           // weight and bias rows are 16-byte aligned
     float* stats;                             // [M][2]: mu, r
     long long rows_per_team;                  // forward: consecutive rows of a team
     // backward
@@ -98,115 +147,132 @@ struct NormArgs {
     int chunks;
 };
 
-// NV: 256-column blocks per warp; R: rows in flight per team
-template <typename TX, typename TY, int NV, bool VEC, int MAXT, int R>
-__global__ void __launch_bounds__(MAXT) layer_norm_kernel(const NormArgs a) {
-    __shared__ float2 part[2][R][kMaxWarps];
+// Sums over a team's warps (at most MAXW), every thread for itself.
+template <int MAXW> __device__ __forceinline__ float2 team_sum(const float2* part, int W) {
+    float2 s = make_float2(0.f, 0.f);
+    if (MAXW <= 8) {
+#pragma unroll
+        for (int k = 0; k < MAXW; ++k)
+            if (k < W) { const float2 p = part[k]; s.x += p.x; s.y += p.y; }
+    } else {
+#pragma unroll 8
+        for (int k = 0; k < W; ++k) { const float2 p = part[k]; s.x += p.x; s.y += p.y; }
+    }
+    return s;
+}
+
+// NV: 256-column blocks per warp.  A team is one warp (eight teams per CTA) where NV blocks hold the row, else the CTA.
+template <typename TX, typename TY, int NV, bool VEC, int MINB, int MAXW>
+__global__ void __launch_bounds__(256, MINB) layer_norm_kernel(const NormArgs a) {
+    constexpr bool KEEP = NV <= 2;                                 // weight and bias stay in registers, else they come from the L1
+    __shared__ float2 part[2][MAXW];
     free_grid_dep_wait();
     free_grid_dep_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int W = NV > 1 ? 1 : a.warps;                            // several blocks per warp: teams of one warp
-    const int teams = W == 1 ? blockDim.x >> 5 : 1;
-    const Cols<VEC> c{a.D, W, W == 1 ? 0 : warp, lane};
+    const int W = MAXW > 1 ? a.warps : 1;
+    const Cols<VEC, NV> c{a.D, W > 1 ? warp : 0, lane};
     const TX* x = reinterpret_cast<const TX*>(a.x);
     TY* y = reinterpret_cast<TY*>(a.y);
-    const long long first = ((long long)blockIdx.x * teams + (W == 1 ? warp : 0)) * a.rows_per_team;
+    const long long team = W > 1 ? blockIdx.x : (long long)blockIdx.x * (blockDim.x >> 5) + warp;
+    const long long first = team * a.rows_per_team;
     const long long last = first + a.rows_per_team < a.M ? first + a.rows_per_team : a.M;
-    const float inv_d = 1.f / (float)a.D;
-    const float n_last = (float)(a.D - (W - 1) * 256);             // columns of the team's last warp; the others hold 256
-    const float inv_n = W == 1 ? inv_d : (c.k < W - 1 ? 1.f / 256.f : 1.f / n_last);
-    float w[NV][8], b[NV][8];
+    constexpr float full = NV * 256.f;                             // columns of all of a team's warps but the last
+    const float inv_d = 1.f / (float)a.D, n_last = (float)a.D - (float)(W - 1) * full;
+    const float inv_n = c.k < W - 1 ? 1.f / full : 1.f / n_last;
+    float w[KEEP ? NV : 1][8], b[KEEP ? NV : 1][8];
+    if (KEEP) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { w[i][e] = 1.f; b[i][e] = 0.f; }
-    long long group_end = a.weight || a.bias ? first : a.M;        // first row that the registers' w and b do not belong to
-    int buf = 0;
-    for (long long row = first; row < last; row += R, buf ^= 1) {
-        float v[R][NV][8], mu[R], m2[R];
+            for (int e = 0; e < 8; ++e) { w[i][e] = 1.f; b[i][e] = 0.f; }
+    }
+    const bool tables = a.weight || a.bias;
+    long long group_end = tables ? first : a.M;                    // first row that the weight and bias at hand do not belong to
+    const float *wp = a.weight, *bp = a.bias;
+    int it = 0;
+    for (long long row = first; row < last; ++row, ++it) {
+        float v[NV][8];
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int i = 0; i < NV; ++i) {
+            Raw<TX, VEC> raw;
+            c.load(x + row * a.x_stride, i, raw);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (row + r < last) c.load(x + (row + r) * a.x_stride, i, v[r][i]);
-                else {
+            for (int e = 0; e < 8; ++e) v[i][e] = raw[e];
+        }
+        float s = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[r][i][e] = 0.f;
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s += v[i][e];
+        float mu = free_warp_sum(s) * inv_n, q = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { const float d = v[i][e] - mu; q += c.in(i, e) ? d * d : 0.f; }
+        float m2 = free_warp_sum(q);                               // squared deviations from this warp's mean
+        if (MAXW > 1 && W > 1) {
+            float2* now = part[it & 1];                            // a buffer is rewritten two barriers after its last read
+            if (lane == 0) now[warp] = make_float2(mu, m2);
+            __syncthreads();
+            const float2 pl = now[W - 1], t = team_sum<MAXW>(now, W - 1);
+            mu = (full * t.x + n_last * pl.x) * inv_d;
+            float d2 = 0.f;
+#pragma unroll
+            for (int k = 0; k < MAXW; ++k)
+                if (k < W - 1) { const float d = now[k].x - mu; d2 = fmaf(d, d, d2); }
+            m2 = t.y + pl.y + full * d2 + n_last * (pl.x - mu) * (pl.x - mu);
+        }
+        const float rstd = rsqrtf(m2 * inv_d + a.eps);
+        if (row >= group_end) {                                    // uniform over the team
+            const long long g = row / a.rows_per_group, mo = g * a.mod_stride;
+            group_end = (g + 1) * a.rows_per_group;
+            if (a.weight) wp = a.weight + mo;
+            if (a.bias) bp = a.bias + mo;
+            if (KEEP) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (a.weight) c.table(wp, i, a.table_vec, a.unit, w[i]);
+                    if (a.bias) c.table(bp, i, a.table_vec, 0.f, b[i]);
                 }
             }
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float s = 0.f;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s += v[r][i][e];
-            mu[r] = free_warp_sum(s) * inv_n;
-            float q = 0.f;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) { const float d = v[r][i][e] - mu[r]; q += c.in(i, e) ? d * d : 0.f; }
-            m2[r] = free_warp_sum(q);                              // squared deviations from this warp's mean
-        }
-        if (W > 1) {
-            if (lane == 0) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) part[buf][r][warp] = make_float2(mu[r], m2[r]);
-            }
-            __syncthreads();                                       // a buffer is rewritten two barriers after its last read
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float s = 0.f;
-                for (int k = 0; k < W - 1; ++k) s += part[buf][r][k].x;
-                const float2 pl = part[buf][r][W - 1];
-                const float m = (256.f * s + n_last * pl.x) * inv_d;
-                float q = 0.f, t = 0.f;
-                for (int k = 0; k < W - 1; ++k) { const float2 p = part[buf][r][k]; q += p.y; t += (p.x - m) * (p.x - m); }
-                mu[r] = m;
-                m2[r] = q + pl.y + 256.f * t + n_last * (pl.x - m) * (pl.x - m);
-            }
         }
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const long long rr = row + r;
-            if (rr >= last) break;
-            const float rstd = rsqrtf(m2[r] * inv_d + a.eps);
-            if (rr >= group_end) {                                 // uniform over the team
-                const long long g = rr / a.rows_per_group, mo = g * a.mod_stride;
-                group_end = (g + 1) * a.rows_per_group;
+        for (int i = 0; i < NV; ++i) {
+            float o[8];
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
+            for (int e = 0; e < 8; ++e) o[e] = (v[i][e] - mu) * rstd;
+            if (KEEP) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (c.in(i, e)) {
-                            if (a.weight) w[i][e] = __ldg(a.weight + mo + c.at(i, e)) + a.unit;
-                            if (a.bias) b[i][e] = __ldg(a.bias + mo + c.at(i, e));
-                        }
+                for (int e = 0; e < 8; ++e) o[e] = o[e] * w[i][e] + b[i][e];
+            } else {
+                float t[8];
+                if (a.weight) {
+                    c.table(wp, i, a.table_vec, a.unit, t);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] *= t[e];
+                }
+                if (a.bias) {
+                    c.table(bp, i, a.table_vec, 0.f, t);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] += t[e];
+                }
             }
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                float o[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = (v[r][i][e] - mu[r]) * rstd * w[i][e] + b[i][e];
-                c.store(y + rr * a.y_stride, i, o);
-            }
-            if (a.stats && c.k == 0 && lane == 0) { a.stats[2 * rr] = mu[r]; a.stats[2 * rr + 1] = rstd; }
+            c.store(y + row * a.y_stride, i, o);
         }
+        if (a.stats && c.k == 0 && lane == 0) { a.stats[2 * row] = mu; a.stats[2 * row + 1] = rstd; }
     }
 }
 
-// One CTA per (group, chunk): a run of the group's rows, walked by the CTA's teams in turn.
-template <typename TX, typename TY, int NV, bool VEC, int MAXT, int R>
-__global__ void __launch_bounds__(MAXT) layer_norm_bwd_kernel(const NormArgs a) {
-    __shared__ float2 part[2][R][kMaxWarps];
-    __shared__ float cols[NV > 1 ? MAXT / 32 : 1][NV > 1 ? NV * 512 : 1];
+// One CTA, a team of ceil(D / 256) warps, per (group, chunk): a run of the group's rows, R of them per barrier.
+// DEPTH: groups of R rows in flight (vector form).  T: threads per SM that the register budget is set for.
+template <typename TX, typename TY, bool VEC, int MAXT, int T, int R, int DEPTH>
+__global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const NormArgs a) {
+    __shared__ float2 part[2][R][MAXT / 32];
+    extern __shared__ uint4 ring[];
     free_grid_dep_wait();
     free_grid_dep_launch();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int W = NV > 1 ? 1 : a.warps;
-    const int teams = NV > 1 ? blockDim.x >> 5 : 1;                // NV == 1: the CTA is one team
-    const Cols<VEC> c{a.D, W, NV > 1 ? 0 : warp, lane};
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, W = a.warps;
+    const Cols<VEC, 1> c{a.D, warp, lane};
     const TX* x = reinterpret_cast<const TX*>(a.x);
     const TY* dy = reinterpret_cast<const TY*>(a.dy);
     const TX* dres = reinterpret_cast<const TX*>(a.dres);
@@ -215,104 +281,106 @@ __global__ void __launch_bounds__(MAXT) layer_norm_bwd_kernel(const NormArgs a) 
     const long long base = (long long)g * a.rows_per_group;
     const long long lo = base + (long long)a.rows_per_group * ch / a.chunks, hi = base + (long long)a.rows_per_group * (ch + 1) / a.chunks;
     const float inv_d = 1.f / (float)a.D;
-    float w[NV][8], dw[NV][8], db[NV][8];
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            w[i][e] = 1.f; dw[i][e] = 0.f; db[i][e] = 0.f;
-            if (a.weight && c.in(i, e)) w[i][e] = __ldg(a.weight + (long long)g * a.mod_stride + c.at(i, e)) + a.unit;
-        }
-    int buf = 0;
-    for (long long row = lo + (NV > 1 ? warp * R : 0); row < hi; row += (long long)teams * R, buf ^= 1) {
-        float xh[R][NV][8], gy[R][NV][8], res[R][NV][8];
-        float2 st[R], sums[R];
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring);
+    const uint32_t bx = blockDim.x * 8 * (uint32_t)sizeof(TX), by = blockDim.x * 8 * (uint32_t)sizeof(TY);   // regions of x and dres, of dy
+    auto unit = [&](int it, int r) { return ring0 + (uint32_t)(it % DEPTH * R + r) * (2 * bx + by); };
+    auto fetch = [&](int it) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const long long rr = row + r < hi ? row + r : hi - 1;  // past the run: the last row again, not counted or stored
-            st[r] = make_float2(__ldg(a.stats_in + 2 * rr), __ldg(a.stats_in + 2 * rr + 1));
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                c.load(x + rr * a.x_stride, i, xh[r][i]);
-                c.load(dy + rr * a.dy_stride, i, gy[r][i]);
-                if (dres) c.load(dres + rr * a.dres_stride, i, res[r][i]);
-                else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) res[r][i][e] = 0.f;
-                }
+            const long long row = lo + (long long)it * R + r;
+            if (row < hi) {
+                const uint32_t u = unit(it, r);
+                c.send(x + row * a.x_stride, 0, u);
+                if (dres) c.send(dres + row * a.dres_stride, 0, u + bx);
+                c.send(dy + row * a.dy_stride, 0, u + 2 * bx);
             }
         }
+        copy_commit();
+    };
+    auto stats_of = [&](long long row) {
+        return row < hi ? make_float2(__ldg(a.stats_in + 2 * row), __ldg(a.stats_in + 2 * row + 1)) : make_float2(0.f, 0.f);
+    };
+    if (VEC) {
+#pragma unroll
+        for (int k = 0; k < DEPTH - 1; ++k) fetch(k);
+    }
+    float w[8], dw[8], db[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { w[e] = 1.f; dw[e] = 0.f; db[e] = 0.f; }
+    if (a.weight) c.table(a.weight + (long long)g * a.mod_stride, 0, a.table_vec, a.unit, w);
+    float2 next[R];                                                // statistics of the rows to come
+#pragma unroll
+    for (int r = 0; r < R; ++r) next[r] = stats_of(lo + r);
+    int it = 0;
+    for (long long row = lo; row < hi; row += R, ++it) {
+        Raw<TX, VEC> res[R];
+        float2 st[R], sum[R];
+        float xh[R][8], v[R][8];
+        if (VEC) {
+            fetch(it + DEPTH - 1);                                 // into the slot that the previous rows left
+            copy_wait<DEPTH - 1>();
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const bool live = row + r < hi;
+            Raw<TX, VEC> rx;
+            Raw<TY, VEC> ry;
+            const bool live = row + r < hi;                        // past the run: nothing is counted or stored
+            if (VEC) {
+                c.take(unit(it, r), 0, rx);
+                c.take(unit(it, r) + 2 * bx, 0, ry);
+            } else if (live) {
+                c.load(x + (row + r) * a.x_stride, 0, rx);
+                c.load(dy + (row + r) * a.dy_stride, 0, ry);
+                if (dres) c.load(dres + (row + r) * a.dres_stride, 0, res[r]);
+            }
+            st[r] = next[r];
+            next[r] = stats_of(row + R + r);
             float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float h = (xh[r][i][e] - st[r].x) * st[r].y, d = gy[r][i][e], v = d * w[i][e];
-                    const bool in = c.in(i, e);                    // outside the row d = 0, but h is not
-                    xh[r][i][e] = h; gy[r][i][e] = v;
-                    if (in) {
-                        s1 += v; s2 = fmaf(v, h, s2);
-                        if (live) { dw[i][e] = fmaf(d, h, dw[i][e]); db[i][e] += d; }
-                    }
-                }
-            sums[r] = make_float2(free_warp_sum(s1), free_warp_sum(s2));
+            for (int e = 0; e < 8; ++e) {
+                const bool in = live && c.in(0, e);
+                const float d = in ? ry[e] : 0.f;
+                xh[r][e] = in ? (rx[e] - st[r].x) * st[r].y : 0.f;
+                v[r][e] = d * w[e];
+                s1 += v[r][e]; s2 = fmaf(v[r][e], xh[r][e], s2);
+                dw[e] = fmaf(d, xh[r][e], dw[e]); db[e] += d;
+            }
+            sum[r] = make_float2(free_warp_sum(s1), free_warp_sum(s2));
         }
         if (W > 1) {
+            float2 (*now)[MAXT / 32] = part[it & 1];               // a buffer is rewritten two barriers after its last read
             if (lane == 0) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) part[buf][r][warp] = sums[r];
+                for (int r = 0; r < R; ++r) now[r][warp] = sum[r];
             }
-            __syncthreads();                                       // a buffer is rewritten two barriers after its last read
+            __syncthreads();
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float s1 = 0.f, s2 = 0.f;
-                for (int k = 0; k < W; ++k) { const float2 p = part[buf][r][k]; s1 += p.x; s2 += p.y; }
-                sums[r] = make_float2(s1, s2);
-            }
+            for (int r = 0; r < R; ++r) sum[r] = team_sum<MAXT / 32>(now[r], W);
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (row + r >= hi) break;
-            const float m1 = sums[r].x * inv_d, m2 = sums[r].y * inv_d;
+            const float m1 = sum[r].x * inv_d, m2 = sum[r].y * inv_d;
+            float o[8];
+            if (VEC && dres) c.take(unit(it, r) + bx, 0, res[r]);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                float o[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = fmaf(st[r].y, gy[r][i][e] - m1 - xh[r][i][e] * m2, res[r][i][e]);
-                c.store(dx + (row + r) * a.dx_stride, i, o);
-            }
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(st[r].y, v[r][e] - m1 - xh[r][e] * m2, dres ? res[r][e] : 0.f);
+            c.store(dx + (row + r) * a.dx_stride, 0, o);
         }
     }
+    if (VEC) copy_wait<0>();                                       // nothing is in flight when the CTA ends
     if (!a.dw && !a.db) return;
     float *ow = a.dw ? a.dw + (long long)g * a.dmod_stride : nullptr, *ob = a.db ? a.db + (long long)g * a.dmod_stride : nullptr;
     if (a.chunks > 1) {
         ow = a.partial + (long long)blockIdx.x * 2 * a.D;
         ob = ow + a.D;
     }
-    if (NV > 1) {                                                  // the teams' sums, added in the order of the warps
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (c.in(i, e)) { cols[warp][c.at(i, e)] = dw[i][e]; cols[warp][NV * 256 + c.at(i, e)] = db[i][e]; }
-        __syncthreads();
-        for (int j = threadIdx.x; j < a.D; j += blockDim.x) {
-            float s = 0.f, t = 0.f;
-            for (int k = 0; k < teams; ++k) { s += cols[k][j]; t += cols[k][NV * 256 + j]; }
-            if (ow) ow[j] = s;
-            if (ob) ob[j] = t;
+    for (int e = 0; e < 8; ++e)
+        if (c.in(0, e)) {
+            if (ow) ow[c.at(0, e)] = dw[e];
+            if (ob) ob[c.at(0, e)] = db[e];
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (c.in(0, e)) {
-                if (ow) ow[c.at(0, e)] = dw[0][e];
-                if (ob) ob[c.at(0, e)] = db[0][e];
-            }
-    }
 }
 
 // dw, db of a group = the sum of its chunks' partial rows: 32 columns x 16 slices of the chunks per CTA, slices joined in order.
@@ -337,57 +405,66 @@ __global__ void __launch_bounds__(512) layer_norm_reduce_kernel(const NormArgs a
     }
 }
 
-// Shape of a launch for width D: blocks per warp, warps of a team, threads of a CTA.
-// Rows of at most 512 columns fit one warp (two blocks): no barrier, eight rows side by side.
-struct Shape { int nv, warps, threads; };
-Shape shape_of(int D) {
-    if (D <= 512) return {2, 1, 256};
-    const int w = (D + 255) / 256;
-    return {1, w, w * 32};
-}
+constexpr int kBwdT = 1024, kBwdScalarT = 768;                     // threads per SM of the backward kernel
 
-// Chunks of a group in the backward pass: enough CTAs to fill the GPU, at least eight rows per team.
+int bwd_threads(int D) { return (D + 255) / 256 * 32; }
+
+// Chunks of a group in the backward pass: one wave of CTAs, at least eight rows each.  (A function of the sizes alone: the
+// workspace depends on it.)
 int chunks_of(int groups, int rows_per_group, int D) {
-    const Shape s = shape_of(D);
-    const int per_cta = 8 * (s.warps == 1 ? s.threads / 32 : 1);
-    const long long want = ((long long)kSms * (s.threads <= 256 ? 1024 / s.threads : 1) + groups - 1) / groups;
-    const long long most = rows_per_group / per_cta;
+    const int t = bwd_threads(D);
+    const int per_sm = t <= 256 ? kBwdT / t : 1;
+    const long long want = ((long long)kSms * per_sm + groups - 1) / groups;
+    const long long most = rows_per_group / 8;
     const long long c = want < most ? want : most;
     return c < 1 ? 1 : (int)c;
 }
 
-template <typename TX, typename TY, bool VEC>
-int launch_fwd(NormArgs a, cudaStream_t s) {
-    const Shape sh = shape_of(a.D);
-    const int teams = sh.warps == 1 ? sh.threads / 32 : 1;
-    a.warps = sh.warps;
-    // a whole number of waves of the CTAs that the GPU holds at once; few rows: as many teams as there are rows
-    const long long resident = (long long)kSms * (2048 / sh.threads < 1 ? 1 : 2048 / sh.threads) * teams;
+template <typename TX, typename TY, int NV, bool VEC, int MINB, int MAXW>
+int start_fwd(NormArgs a, int warps, cudaStream_t s) {
+    const int threads = MAXW > 1 ? warps * 32 : 256, teams = MAXW > 1 ? 1 : 8;
+    a.warps = warps;
+    // one wave of the CTAs that the GPU holds at once; few rows: as many teams as there are rows
+    const long long resident = (long long)kSms * (MINB * 256 / threads) * teams;
     a.rows_per_team = (a.M + resident - 1) / resident;
-    const unsigned grid = (unsigned)((a.M + a.rows_per_team * teams - 1) / (a.rows_per_team * teams));
-    const bool ov = free_overlap_for_rows(a.M);
-    if (sh.nv == 2) return free_launch(ov, layer_norm_kernel<TX, TY, 2, VEC, 256, 1>, dim3(grid), dim3(sh.threads), 0, s, a);
-    if (sh.threads <= 256) return free_launch(ov, layer_norm_kernel<TX, TY, 1, VEC, 256, 2>, dim3(grid), dim3(sh.threads), 0, s, a);
-    return free_launch(ov, layer_norm_kernel<TX, TY, 1, VEC, 1024, 1>, dim3(grid), dim3(sh.threads), 0, s, a);
+    const long long grid = (a.M + a.rows_per_team * teams - 1) / (a.rows_per_team * teams);
+    return free_launch(free_overlap_for_rows(a.M), layer_norm_kernel<TX, TY, NV, VEC, MINB, MAXW>, dim3((unsigned)grid), dim3(threads), 0, s, a);
+}
+
+// As many blocks per warp as the row needs (registers decide how many rows an SM holds); several warps beyond 2048 columns.
+template <typename TX, typename TY, bool VEC>
+int launch_fwd(const NormArgs& a, cudaStream_t s) {
+    if (a.D <= 512) return start_fwd<TX, TY, 2, VEC, 3, 1>(a, 1, s);
+    if (a.D <= 768) return start_fwd<TX, TY, 3, VEC, 4, 1>(a, 1, s);
+    if (a.D <= 1280) return start_fwd<TX, TY, 5, VEC, 3, 1>(a, 1, s);
+    if (a.D <= 2048) return start_fwd<TX, TY, 8, VEC, 2, 1>(a, 1, s);
+    return start_fwd<TX, TY, kWide, VEC, 3, (kMaxD + 256 * kWide - 1) / (256 * kWide)>(a, (a.D + 256 * kWide - 1) / (256 * kWide), s);
+}
+
+template <typename TX, typename TY, bool VEC, int MAXT, int T, int R>
+int start_bwd(const NormArgs& a, int threads, cudaStream_t s) {
+    constexpr int DEPTH = 2;
+    auto kernel = layer_norm_bwd_kernel<TX, TY, VEC, MAXT, T, R, DEPTH>;
+    const size_t smem = VEC ? (size_t)threads * DEPTH * R * 8 * (2 * sizeof(TX) + sizeof(TY)) : 0;
+    if (smem > 47 * 1024) FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    return free_launch(free_overlap_for_rows(a.M), kernel, dim3((unsigned)a.groups * (unsigned)a.chunks), dim3(threads), smem, s, a);
 }
 
 template <typename TX, typename TY, bool VEC>
 int launch_bwd(NormArgs a, cudaStream_t s) {
-    const Shape sh = shape_of(a.D);
-    a.warps = sh.warps;
-    const dim3 grid((unsigned)a.groups * (unsigned)a.chunks), block(sh.threads);
-    const bool ov = free_overlap_for_rows(a.M);
-    int r;
-    if (sh.nv == 2) r = free_launch(ov, layer_norm_bwd_kernel<TX, TY, 2, VEC, 256, 1>, grid, block, 0, s, a);
-    else if (sh.threads <= 256) r = free_launch(ov, layer_norm_bwd_kernel<TX, TY, 1, VEC, 256, 2>, grid, block, 0, s, a);
-    else r = free_launch(ov, layer_norm_bwd_kernel<TX, TY, 1, VEC, 1024, 1>, grid, block, 0, s, a);
+    const int threads = bwd_threads(a.D);
+    a.warps = threads / 32;
+    // wide rows leave an SM one CTA: two rows per barrier where shared memory holds them
+    const int r = threads <= 256 ? start_bwd<TX, TY, VEC, 256, VEC ? kBwdT : kBwdScalarT, 1>(a, threads, s)
+                : threads <= 576 ? start_bwd<TX, TY, VEC, 576, 576, 2>(a, threads, s) : start_bwd<TX, TY, VEC, 1024, 1024, 1>(a, threads, s);
     if (r != FREE_OK || a.chunks == 1 || (!a.dw && !a.db)) return r;
     return free_launch(free_launch_overlap_enabled(), layer_norm_reduce_kernel, dim3((unsigned)a.groups * ((2u * a.D + 31) / 32)), dim3(512), 0, s, a);
 }
 
-bool row_vec(int dtype, const void* p, long long stride) {
-    return !p || (stride % (dtype == FREE_BF16 ? 8 : 4) == 0);     // base pointers are 16-byte aligned (checked)
+bool tables_vec(const float* w, const float* b, int groups, long long stride) {
+    return ((reinterpret_cast<uintptr_t>(w) | reinterpret_cast<uintptr_t>(b)) & 15u) == 0 && (groups == 1 || stride % 4 == 0);
 }
+bool row_vec(const void* p, long long stride) { return !p || stride % 4 == 0; }    // base pointers are 16-byte aligned (checked)
 
 bool known(int dtype) { return dtype == FREE_FP32 || dtype == FREE_BF16; }
 
@@ -408,9 +485,10 @@ extern "C" int free_op_layer_norm(int x_dtype, int y_dtype, int n_groups, int ro
     NormArgs a{};
     a.M = M; a.D = D; a.groups = n_groups; a.rows_per_group = rows_per_group;
     a.x = x; a.x_stride = x_stride; a.weight = weight; a.bias = bias; a.mod_stride = mod_stride; a.unit = unit_offset ? 1.f : 0.f;
+    a.table_vec = tables_vec(weight, bias, n_groups, mod_stride);
     a.eps = eps; a.y = y; a.y_stride = y_stride; a.stats = stats;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    const bool vec = D % 8 == 0 && row_vec(x_dtype, x, x_stride) && row_vec(y_dtype, y, y_stride);
+    const bool vec = D % 4 == 0 && row_vec(x, x_stride) && row_vec(y, y_stride);
     const int which = (x_dtype == FREE_BF16 ? 4 : 0) + (y_dtype == FREE_BF16 ? 2 : 0) + (vec ? 1 : 0);
     using bf = __nv_bfloat16;
     switch (which) {
@@ -455,11 +533,12 @@ extern "C" int free_op_layer_norm_bwd(int x_dtype, int y_dtype, int n_groups, in
     NormArgs a{};
     a.M = M; a.D = D; a.groups = n_groups; a.rows_per_group = rows_per_group;
     a.x = x; a.x_stride = x_stride; a.weight = weight; a.mod_stride = mod_stride; a.unit = unit_offset ? 1.f : 0.f;
+    a.table_vec = tables_vec(weight, nullptr, n_groups, mod_stride);
     a.dy = dy; a.dy_stride = dy_stride; a.stats_in = stats; a.dres = dres; a.dres_stride = dres_stride; a.dx = dx; a.dx_stride = dx_stride;
     a.dw = dweight; a.db = dbias; a.dmod_stride = dmod_stride; a.partial = (float*)ws; a.chunks = chunks;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    const bool vec = D % 8 == 0 && row_vec(x_dtype, x, x_stride) && row_vec(y_dtype, dy, dy_stride) && row_vec(x_dtype, dres, dres_stride) &&
-                     row_vec(x_dtype, dx, dx_stride);
+    const bool vec = D % 4 == 0 && row_vec(x, x_stride) && row_vec(dy, dy_stride) && row_vec(dres, dres_stride) &&
+                     row_vec(dx, dx_stride);
     const int which = (x_dtype == FREE_BF16 ? 4 : 0) + (y_dtype == FREE_BF16 ? 2 : 0) + (vec ? 1 : 0);
     using bf = __nv_bfloat16;
     switch (which) {

@@ -4,10 +4,13 @@
 //
 // Bound by HBM (each element is read and written once; 3 FLOPs).  The angle of a far position needs more than fp32: it is
 // formed in turns, t / 2 pi, as one fp64 product, reduced to [-1/2, 1/2] there, and only the remainder goes to fp32
-// sincospif.  All heads of a token share its angles, so a CTA first fills a table [tokens][pairs] of (cos, sin) in shared
-// memory and then streams its tokens' heads through it.  A thread keeps one slot (one vector of a head, or the two that it
-// couples) and walks over the tokens, so that the index arithmetic is done once per thread, and has kUnroll tokens' loads
-// in flight.  The table of frequencies is formed on the host in fp64 and travels as a kernel argument.
+// sincospif.  All heads of a token share its angles, and so do the sequences that share positions: a CTA takes a few tokens of
+// a run of sequences, fills a table [tokens][pairs] of (cos, sin) in shared memory once while its first loads are in flight, and
+// streams the heads through it.  A thread keeps one slot (one vector of a head, or the two that it couples), so that the index
+// arithmetic is done once, and has kUnroll tokens' loads in flight.  The frequencies are formed on the host in fp64 and travel
+// as a kernel argument.
+// Measured on B200: 39 us for the 113 MB of queries and keys of 24 x 1024 tokens, 16 heads of 72, bf16 (5.8 TB/s read and
+// written), 73 us for the same in fp32 (6.2 TB/s).
 #include "internal.h"
 #include <math.h>
 
@@ -15,19 +18,21 @@ namespace {
 
 constexpr int kMaxPairs = 128;                     // rotated pairs of a head
 constexpr int kMaxAxes = 4;
-constexpr int kThreads = 512;                      // most threads of a CTA
-constexpr int kTable = 2048;                       // (cos, sin) entries of a CTA: 16 KB
-constexpr int kMaxTok = 256;                       // tokens of a CTA
-constexpr int kUnroll = 4;
+constexpr int kThreads = 512;                     // most threads of a CTA
+constexpr int kTableBytes = 16384;                 // (cos, sin) entries of a CTA
+// Tokens that a thread has in flight.
+// (A bf16 slot of two halves is eight pairs: more of them cost registers, 23 instead of 20 us for four on 8 x 4096 tokens of 12
+// heads of 64.)
+template <typename T, bool HALVES> constexpr int kUnroll = HALVES && sizeof(T) == 2 ? 1 : 4;
 constexpr int kSms = 148;
 
 struct RopeArgs {
-    long long tokens;                              // n_seq * n_tok
-    int n_tok, n_axes, pairs;                      // pairs: rotated pairs of a head
+    int n_seq, n_tok, n_axes, pairs;               // pairs: rotated pairs of a head
     int heads, d_head;
     int slots_per_head, slots;                     // slots: slots_per_head * heads
-    int tok_per_cta;
     int width, lanes_tok;                          // a CTA's threads: width slots side by side, for lanes_tok tokens at a time
+    int passes;                                    // runs of `width` slots that cover a token
+    int tok_per_cta, seq_per_cta;
     const float* pos; long long pos_seq_stride;
     const void* x; long long xs, xt, xh;           // strides of sequence, token, head in elements
     void* y; long long ys, yt, yh;
@@ -37,26 +42,80 @@ struct RopeArgs {
 };
 
 template <typename T, int N> struct alignas(sizeof(T) * N) Pack { T v[N]; };
-__device__ __forceinline__ float to_f(float v) { return v; }
-__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void from_f(float& d, float v) { d = v; }
-__device__ __forceinline__ void from_f(__nv_bfloat16& d, float v) { d = __float2bfloat16(v); }
 
-// V elements as one access, or (ALIGNED false) one by one
-template <typename T, int V, bool ALIGNED> __device__ __forceinline__ Pack<T, V> get(const T* p) {
-    Pack<T, V> r;
-    if (ALIGNED) r = *reinterpret_cast<const Pack<T, V>*>(p);
+// V elements of a head.  bf16 pairs stay packed in 32-bit words: one shift or mask to unpack, one conversion to pack two.
+template <typename T, int V> struct Vec;
+template <int V> struct Vec<float, V> {
+    Pack<float, V> d;
+    __device__ __forceinline__ void get2(int i, float& a, float& b) const { a = d.v[2 * i]; b = d.v[2 * i + 1]; }
+    __device__ __forceinline__ void set2(int i, float a, float b) { d.v[2 * i] = a; d.v[2 * i + 1] = b; }
+};
+template <int V> struct Vec<__nv_bfloat16, V> {
+    Pack<uint32_t, V / 2> d;
+    __device__ __forceinline__ void get2(int i, float& a, float& b) const {
+        a = __uint_as_float(d.v[i] << 16); b = __uint_as_float(d.v[i] & 0xffff0000u);
+    }
+    __device__ __forceinline__ void set2(int i, float a, float b) {
+        const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
+        d.v[i] = *reinterpret_cast<const uint32_t*>(&r);
+    }
+};
+// one element (halves of an odd number of pairs)
+template <> struct Vec<float, 1> {
+    Pack<float, 1> d;
+    __device__ __forceinline__ void get2(int, float& a, float& b) const { a = d.v[0]; b = 0.f; }
+    __device__ __forceinline__ void set2(int, float a, float) { d.v[0] = a; }
+};
+template <> struct Vec<__nv_bfloat16, 1> {
+    Pack<__nv_bfloat16, 1> d;
+    __device__ __forceinline__ void get2(int, float& a, float& b) const { a = __bfloat162float(d.v[0]); b = 0.f; }
+    __device__ __forceinline__ void set2(int, float a, float) { d.v[0] = __float2bfloat16(a); }
+};
+// as one access, or (ALIGNED false) element by element
+template <typename T, int V, bool ALIGNED> __device__ __forceinline__ Vec<T, V> get(const T* p) {
+    Vec<T, V> r;
+    using D = decltype(r.d);
+    if (ALIGNED) r.d = *reinterpret_cast<const D*>(p);
     else {
+        Pack<T, V> e;
 #pragma unroll
-        for (int i = 0; i < V; ++i) r.v[i] = p[i];
+        for (int i = 0; i < V; ++i) e.v[i] = p[i];
+        r.d = *reinterpret_cast<const D*>(&e);
     }
     return r;
 }
-template <typename T, int V, bool ALIGNED> __device__ __forceinline__ void put(T* p, const Pack<T, V>& r) {
-    if (ALIGNED) *reinterpret_cast<Pack<T, V>*>(p) = r;
+template <typename T, int V, bool ALIGNED> __device__ __forceinline__ void put(T* p, const Vec<T, V>& r) {
+    if (ALIGNED) *reinterpret_cast<decltype(r.d)*>(p) = r.d;
     else {
+        const Pack<T, V> e = *reinterpret_cast<const Pack<T, V>*>(&r.d);
 #pragma unroll
-        for (int i = 0; i < V; ++i) p[i] = r.v[i];
+        for (int i = 0; i < V; ++i) p[i] = e.v[i];
+    }
+}
+
+// One pair turned by (cos, sin).
+__device__ __forceinline__ void turn(float& a, float& b, float cs, float sn) {
+    const float p = a, q = b;
+    a = p * cs - q * sn;
+    b = p * sn + q * cs;
+}
+// The pairs of a slot, their (cos, sin) two by two in f[0], f[plane], ...  PART: only the first `pairs`, the elements behind
+// stay as they are (bit for bit).
+template <typename T, int V, bool HALVES, bool PART>
+__device__ __forceinline__ void rotate(Vec<T, V>& u, Vec<T, V>& w, const float4* f, int plane, int pairs) {
+    constexpr int PV = HALVES ? V : V / 2;
+#pragma unroll
+    for (int q = 0; q < (PV + 1) / 2; ++q) {
+        const float4 c = f[q * plane];
+        float a0, a1, b0, b1;
+        if (HALVES) {                                              // pairs (u0, w0), (u1, w1)
+            u.get2(q, a0, a1); w.get2(q, b0, b1);
+            turn(a0, b0, c.x, c.y); turn(a1, b1, c.z, c.w);
+            u.set2(q, a0, a1); w.set2(q, b0, b1);
+        } else {                                                   // pairs (u0, u1), (u2, u3)
+            if (!PART || 2 * q < pairs) { u.get2(2 * q, a0, b0); turn(a0, b0, c.x, c.y); u.set2(2 * q, a0, b0); }
+            if (2 * q + 1 < PV && (!PART || 2 * q + 1 < pairs)) { u.get2((2 * q + 1) % (V / 2), a1, b1); turn(a1, b1, c.z, c.w); u.set2((2 * q + 1) % (V / 2), a1, b1); }
+        }
     }
 }
 
@@ -65,75 +124,64 @@ template <typename T, int V, bool ALIGNED> __device__ __forceinline__ void put(T
 // elements behind both halves, which are copied.
 template <typename T, int V, bool HALVES, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads) rope_axes_kernel(const __grid_constant__ RopeArgs a) {
-    __shared__ float2 table[kTable];
-    __shared__ long long off_x[kMaxTok], off_y[kMaxTok];
+    constexpr int U = kUnroll<T, HALVES>;
+    // Pairs of a slot: PV.  They lie in planes of two, [plane][token][slot group], so that a warp's 16-byte reads are one run
+    // (with a slot's pairs side by side they would be 32 bytes apart and meet in the same banks: 61 instead of 44 us for the
+    // queries and keys of 24 x 1024 tokens, 16 heads of 72, before the words stayed packed).
+    constexpr int PV = HALVES ? V : V / 2;
+    __shared__ float4 table[kTableBytes / 16];
     free_grid_dep_wait();
     free_grid_dep_launch();
-    const long long tok0 = (long long)blockIdx.x * a.tok_per_cta;
-    const int n = (int)(a.tokens - tok0 < a.tok_per_cta ? a.tokens - tok0 : a.tok_per_cta);
-    const int P = a.pairs;
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const long long q = (tok0 + i) / a.n_tok, t = (tok0 + i) % a.n_tok;
-        off_x[i] = q * a.xs + t * a.xt;
-        off_y[i] = q * a.ys + t * a.yt;
-    }
-    for (int i = threadIdx.x; i < n * P; i += blockDim.x) {
-        const int k = i / P, p = i - k * P;
-        const long long q = (tok0 + k) / a.n_tok, t = (tok0 + k) % a.n_tok;
-        double turn = (double)a.pos[q * a.pos_seq_stride + t * a.n_axes + a.axis[p]] * a.turns[p];
-        turn -= rint(turn);
-        float s, c;
-        sincospif((float)(turn + turn), &s, &c);
-        table[i] = make_float2(c, a.sign * s);
-    }
-    __syncthreads();
-    const T* x = reinterpret_cast<const T*>(a.x);
-    T* y = reinterpret_cast<T*>(a.y);
-    const int width = a.width, lt = threadIdx.x / width;
-    if (lt >= a.lanes_tok) return;
-    for (int slot = threadIdx.x - lt * width; slot < a.slots; slot += width) {
-        const int h = slot / a.slots_per_head, j = slot - h * a.slots_per_head;
-        const int pair0 = HALVES ? j * V : j * (V / 2);            // first pair of the slot
-        const int col = HALVES ? (pair0 < P ? pair0 : pair0 + P) : j * V;
-        const T* xp = x + h * a.xh + col;
-        T* yp = y + h * a.yh + col;
-        for (int t0 = lt; t0 < n; t0 += a.lanes_tok * kUnroll) {
-            Pack<T, V> u[kUnroll], w[kUnroll];
+    const int P = a.pairs, G = (P + PV - 1) / PV, plane = a.tok_per_cta * G;
+    const int t0 = blockIdx.x * a.tok_per_cta, n = a.n_tok - t0 < a.tok_per_cta ? a.n_tok - t0 : a.tok_per_cta;
+    const int s0 = blockIdx.y * a.seq_per_cta, s1 = a.n_seq - s0 < a.seq_per_cta ? a.n_seq : s0 + a.seq_per_cta;
+    const int lt = threadIdx.x / a.width, lane = threadIdx.x - lt * a.width;
+    const long long xstep = a.lanes_tok * a.xt, ystep = a.lanes_tok * a.yt;
+    for (int s = s0; s < s1; ++s) {
+        const bool fill = s == s0 || a.pos_seq_stride != 0;        // sequences that share positions share the table
+        for (int pass = 0; pass < a.passes; ++pass) {
+            const int slot = pass * a.width + lane;
+            const bool live = lt < a.lanes_tok && lt < n && slot < a.slots;
+            const int h = slot / a.slots_per_head, j = slot - h * a.slots_per_head;
+            const int pair0 = j * PV;                              // first pair of the slot
+            const bool turned = pair0 < P;
+            const int col = HALVES && !turned ? pair0 + P : HALVES ? pair0 : j * V;
+            Vec<T, V> u[U], w[U];
+            if (live) {
+                const T* q = reinterpret_cast<const T*>(a.x) + s * a.xs + (t0 + lt) * a.xt + h * a.xh + col;
 #pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                const int t = t0 + k * a.lanes_tok;
-                if (t < n) {
-                    u[k] = get<T, V, ALIGNED>(xp + off_x[t]);
-                    if (HALVES && pair0 < P) w[k] = get<T, V, ALIGNED>(xp + off_x[t] + P);
+                for (int k = 0; k < U; ++k) {
+                    u[k] = get<T, V, ALIGNED>(q);
+                    if (HALVES && turned) w[k] = get<T, V, ALIGNED>(q + P);
+                    if (lt + (k + 1) * a.lanes_tok < n) q += xstep;   // past the last token: the last one again, not stored
                 }
             }
-#pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                const int t = t0 + k * a.lanes_tok;
-                if (t >= n) break;
-                const float2* cs = table + t * P + pair0;
-                if (HALVES) {
-                    if (pair0 < P) {
-#pragma unroll
-                        for (int e = 0; e < V; ++e) {
-                            const float2 f = cs[e];
-                            const float p = to_f(u[k].v[e]), q = to_f(w[k].v[e]);
-                            from_f(u[k].v[e], p * f.x - q * f.y);
-                            from_f(w[k].v[e], p * f.y + q * f.x);
-                        }
-                        put<T, V, ALIGNED>(yp + off_y[t] + P, w[k]);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V / 2; ++e)
-                        if (pair0 + e < P) {                       // elements past the rotated ones stay as they are
-                            const float2 f = cs[e];
-                            const float p = to_f(u[k].v[2 * e]), q = to_f(u[k].v[2 * e + 1]);
-                            from_f(u[k].v[2 * e], p * f.x - q * f.y);
-                            from_f(u[k].v[2 * e + 1], p * f.y + q * f.x);
-                        }
+            if (fill && pass == 0) {                               // while the first loads are in flight
+                if (s > s0) __syncthreads();
+                const float* pos = a.pos + s * a.pos_seq_stride + (long long)t0 * a.n_axes;
+                for (int i = threadIdx.x; i < n * P; i += blockDim.x) {
+                    const int k = i / P, p = i - k * P;
+                    double turns = (double)pos[k * a.n_axes + a.axis[p]] * a.turns[p];
+                    turns -= rint(turns);
+                    float cs, sn;
+                    sincospif((float)(turns + turns), &sn, &cs);
+                    const int r = p % PV;
+                    reinterpret_cast<float2*>(table + r / 2 * plane + k * G + p / PV)[r & 1] = make_float2(cs, a.sign * sn);
                 }
-                put<T, V, ALIGNED>(yp + off_y[t], u[k]);
+                __syncthreads();
+            }
+            if (!live) continue;
+            T* q = reinterpret_cast<T*>(a.y) + s * a.ys + (t0 + lt) * a.yt + h * a.yh + col;
+            const float4* f = table + lt * G + j;
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                if (lt + k * a.lanes_tok >= n) break;
+                if (pair0 + PV <= P) rotate<T, V, HALVES, false>(u[k], w[k], f, plane, PV);
+                else if (turned) rotate<T, V, HALVES, true>(u[k], w[k], f, plane, P - pair0);
+                if (HALVES && turned) put<T, V, ALIGNED>(q + P, w[k]);
+                put<T, V, ALIGNED>(q, u[k]);
+                q += ystep;
+                f += a.lanes_tok * G;
             }
         }
     }
@@ -146,21 +194,30 @@ int launch(RopeArgs& a, cudaStream_t s) {
     if (slots > (1 << 24)) return FREE_ERR_UNSUPPORTED;
     a.slots = (int)slots;
     // a token with few slots shares the CTA with others; one with many takes equal passes of at most kThreads slots
-    const int passes = (a.slots + kThreads - 1) / kThreads;
-    a.width = (a.slots + passes - 1) / passes;
+    a.passes = (a.slots + kThreads - 1) / kThreads;
+    a.width = (a.slots + a.passes - 1) / a.passes;
     a.lanes_tok = a.width >= 256 ? 1 : 256 / a.width;
-    const int threads = (a.width * a.lanes_tok + 31) / 32 * 32;
-    // tokens of a CTA: four slots of a thread's loads in flight, less when the table is full or the GPU would stand idle
-    long long tok = (long long)a.lanes_tok * kUnroll;
-    const long long spread = (a.tokens + 2 * kSms - 1) / (2 * kSms);
+    if (a.lanes_tok > a.n_tok) a.lanes_tok = a.n_tok;
+    constexpr int PV = HALVES ? V : V / 2, U = kUnroll<T, HALVES>;
+    // tokens of a CTA: as many as a thread unrolls, less when the table is full or the GPU would stand idle
+    long long tok = (long long)a.lanes_tok * U;
+    const long long spread = ((long long)a.n_tok * a.n_seq + 2 * kSms - 1) / (2 * kSms);
     if (tok > spread) tok = spread;
-    if (tok > kTable / a.pairs) tok = kTable / a.pairs;
-    if (tok > kMaxTok) tok = kMaxTok;
-    if (tok < 1) tok = 1;
+    const int entry = (a.pairs + PV - 1) / PV * ((PV + 1) / 2) * 16;   // table bytes of a token
+    if (tok > kTableBytes / entry) tok = kTableBytes / entry;
+    if (tok > a.n_tok) tok = a.n_tok;
     a.tok_per_cta = (int)tok;
-    const long long grid = (a.tokens + tok - 1) / tok;
-    if (grid > 0x7fffffffLL) return FREE_ERR_UNSUPPORTED;
-    return free_launch(free_overlap_for_rows(a.tokens), rope_axes_kernel<T, V, HALVES, ALIGNED>, dim3((unsigned)grid), dim3(threads), 0, s, a);
+    if (a.lanes_tok > tok) a.lanes_tok = (int)tok;
+    const int threads = (a.width * a.lanes_tok + 31) / 32 * 32;
+    // the sequences of a CTA follow one another (and share the table where they share positions): about two waves of CTAs
+    const long long tok_blocks = (a.n_tok + tok - 1) / tok, want = (long long)kSms * (2048 / threads);
+    long long seq_blocks = (want + tok_blocks - 1) / tok_blocks;
+    if (seq_blocks > a.n_seq || a.pos_seq_stride) seq_blocks = a.n_seq;
+    if (seq_blocks > 65535) seq_blocks = 65535;
+    a.seq_per_cta = (int)((a.n_seq + seq_blocks - 1) / seq_blocks);
+    seq_blocks = (a.n_seq + a.seq_per_cta - 1) / a.seq_per_cta;
+    return free_launch(free_overlap_for_rows((long long)a.n_tok * a.n_seq), rope_axes_kernel<T, V, HALVES, ALIGNED>,
+                       dim3((unsigned)tok_blocks, (unsigned)seq_blocks), dim3(threads), 0, s, a);
 }
 
 // The widest vector whose size divides every offset that a slot can have.
@@ -215,7 +272,7 @@ extern "C" int free_op_rope_axes(int dtype, int pairing, int freq_mode, int inve
     const uintptr_t elem = dtype == FREE_FP32 ? 4 : 2;
     if (reinterpret_cast<uintptr_t>(x) % elem || reinterpret_cast<uintptr_t>(y) % elem || (reinterpret_cast<uintptr_t>(pos) & 3u)) return FREE_ERR_ALIGN;
     RopeArgs a{};
-    a.tokens = (long long)n_seq * n_tok; a.n_tok = n_tok; a.n_axes = n_axes; a.pairs = (int)(total / 2);
+    a.n_seq = n_seq; a.n_tok = n_tok; a.n_axes = n_axes; a.pairs = (int)(total / 2);
     a.heads = heads; a.d_head = d_head; a.pos = pos; a.pos_seq_stride = pos_seq_stride;
     a.x = x; a.xs = x_seq_stride; a.xt = x_tok_stride; a.xh = x_head_stride;
     a.y = y; a.ys = y_seq_stride; a.yt = y_tok_stride; a.yh = y_head_stride;
