@@ -1,5 +1,5 @@
-// Internal interfaces of the gated linear layer: gated_tc.cu (bf16, tensor cores), gated_simt.cu (fp32, CUDA cores) and
-// gated_api.cu (elementwise gradients, sums of parts, entry points).
+// Internal interfaces of the gated linear layer: gated_tc.cu (bf16, tensor cores), gated_simt.cu (fp32, CUDA cores),
+// gated_rows.cu (few rows) and gated_api.cu (elementwise gradients, sums of parts, entry points).
 #pragma once
 #include "internal.h"
 
@@ -40,6 +40,10 @@ int gated_tc_forward(int act, int M, int F, int K, const void* x, const void* w,
 GatedSplit gated_tc_split(bool dw, int M, int F, int K);
 // dw false: out [M, K] = dz W; true: out [2F, K] = dz^T x.  parts: workspace of gated_tc_split() (unused when it is 1)
 int gated_tc_backward(bool dw, int M, int F, int K, const void* x, const void* w, const void* dz, void* out, float* parts, uint32_t* err, cudaStream_t s);
+
+// ---- few rows (CUDA cores, both types); bf16: K % 8 == 0 -----------------------------------------
+bool gated_rows_wanted(int dtype, int M);
+int gated_rows_forward(int dtype, int act, int M, int F, int K, const void* x, const void* w, const float* bias, void* h, void* preact, cudaStream_t s);
 
 // ---- fp32 (CUDA cores), any sizes ----------------------------------------------------------------
 int gated_simt_forward(int act, int M, int F, int K, const float* x, const float* w, const float* bias, float* h, float* preact, cudaStream_t s);

@@ -27,6 +27,17 @@ struct Args {
     int parts; long long plane;            // elements between the parts
 };
 
+// Two multiply-adds as one instruction (each rounded as fmaf): the FMA pipe is fed with half the issue slots.
+__device__ __forceinline__ void fma2(uint64_t& acc, uint64_t a, uint64_t b) {
+    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b));
+}
+__device__ __forceinline__ uint64_t both(float v) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ void split2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+
 // A stage of one operand: ROWS x 16 values, contraction-major in shared memory ([16][ROWS + 4]).
 // KMAJOR: memory holds rows of the contraction (element (r, k) at r * ld + k); otherwise k * ld + r.
 template <int ROWS, int THREADS, bool KMAJOR, bool VEC> struct Loader {
@@ -89,7 +100,7 @@ __global__ void __launch_bounds__(TM * 2) gated_simt_kernel(const Args a) {
     const int k0 = kbeg / 4 * 4, k1 = blockIdx.z + 1 == a.parts ? kend : kend / 4 * 4;
     Loader<TM, THREADS, MODE != DW, VEC> la;
     Loader<TN, THREADS, MODE == GATED, VEC> lb;
-    float acc[8][8] = {};
+    uint64_t acc2[8][4] = {};                              // columns (0, 1), (2, 3) of the lower half, then of the upper
     auto fetch = [&](int k) {
         la.fetch(a.A, a.lda, m0, a.M, TM, 0, k, k1);
         lb.fetch(a.B, a.ldb, n0, a.N, HALF, MODE == GATED ? a.F : 0, k, k1);
@@ -105,15 +116,17 @@ __global__ void __launch_bounds__(TM * 2) gated_simt_kernel(const Args a) {
         if (more) fetch(k + TK);
 #pragma unroll
         for (int kk = 0; kk < TK; ++kk) {
-            float av[8], bv[8];
+            float av[8];
             *reinterpret_cast<float4*>(av) = *reinterpret_cast<const float4*>(&As[buf][kk][ty * 4]);
             *reinterpret_cast<float4*>(av + 4) = *reinterpret_cast<const float4*>(&As[buf][kk][TM / 2 + ty * 4]);
-            *reinterpret_cast<float4*>(bv) = *reinterpret_cast<const float4*>(&Bs[buf][kk][tx * 4]);
-            *reinterpret_cast<float4*>(bv + 4) = *reinterpret_cast<const float4*>(&Bs[buf][kk][TN / 2 + tx * 4]);
+            const ulonglong2 b0 = *reinterpret_cast<const ulonglong2*>(&Bs[buf][kk][tx * 4]);
+            const ulonglong2 b1 = *reinterpret_cast<const ulonglong2*>(&Bs[buf][kk][TN / 2 + tx * 4]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(av[i], bv[j], acc[i][j]);
+            for (int i = 0; i < 8; ++i) {
+                const uint64_t a2 = both(av[i]);
+                fma2(acc2[i][0], a2, b0.x); fma2(acc2[i][1], a2, b0.y);
+                fma2(acc2[i][2], a2, b1.x); fma2(acc2[i][3], a2, b1.y);
+            }
         }
         if (more) { la.store(As[buf ^ 1]); lb.store(Bs[buf ^ 1]); }   // last read before the previous barrier
         __syncthreads();
@@ -122,12 +135,15 @@ __global__ void __launch_bounds__(TM * 2) gated_simt_kernel(const Args a) {
     for (int i = 0; i < 8; ++i) {
         const int m = m0 + (i < 4 ? ty * 4 + i : TM / 2 + ty * 4 + i - 4);
         if (m >= a.M) continue;
+        float acc[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) split2(acc2[i][j], acc[2 * j], acc[2 * j + 1]);
         if (MODE == GATED) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int n = n0 + tx * 4 + j;
                 if (n >= a.F) continue;
-                float g = acc[i][j], u = acc[i][4 + j];
+                float g = acc[j], u = acc[4 + j];
                 if (a.bias) { g += __ldg(a.bias + n); u += __ldg(a.bias + a.F + n); }
                 a.out[(long long)m * a.F + n] = free_gate_act(a.act, g) * u;
                 if (a.pre) { a.pre[(long long)m * 2 * a.F + n] = g; a.pre[(long long)m * 2 * a.F + a.F + n] = u; }
@@ -137,11 +153,11 @@ __global__ void __launch_bounds__(TM * 2) gated_simt_kernel(const Args a) {
             for (int h = 0; h < 2; ++h) {
                 const int n = n0 + h * (TN / 2) + tx * 4;
                 float* q = a.out + blockIdx.z * a.plane + (long long)m * a.N + n;
-                if (VEC && n + 3 < a.N) *reinterpret_cast<float4*>(q) = make_float4(acc[i][4 * h], acc[i][4 * h + 1], acc[i][4 * h + 2], acc[i][4 * h + 3]);
+                if (VEC && n + 3 < a.N) *reinterpret_cast<float4*>(q) = make_float4(acc[4 * h], acc[4 * h + 1], acc[4 * h + 2], acc[4 * h + 3]);
                 else {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (n + j < a.N) q[j] = acc[i][4 * h + j];
+                        if (n + j < a.N) q[j] = acc[4 * h + j];
                 }
             }
         }

@@ -31,7 +31,9 @@ constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kABytes = 128 * BK * 2, kStageBytes = 2 * kABytes;
 constexpr uint32_t kBoxBytes = 64 * BK * 2;             // one 64 x 64 box of an MN-major operand
 constexpr uint32_t kCtrlBytes = 1024, kBufBytes = 4096; // staging buffer: 32 rows x 128 bytes
-constexpr int kBufs = 4;                                // per epilogue warp
+// Staging buffers per epilogue warp.  (A chunk of GATED with the pre-activations fills three of the four; six, at the price of
+// a stage of operands, measured 4% slower.)
+constexpr int kBufs = 4;
 constexpr uint32_t kSmem = 1024 + kCtrlBytes + 4 * kBufs * kBufBytes + kStages * kStageBytes;
 static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 constexpr int kPairs = 74;                              // clusters of two on 148 SMs
@@ -41,8 +43,8 @@ struct Args {
     int num_m, num_n, nk, splits;           // tiles, 64-deep steps of the contraction, parts of it
     int half, last_half;                    // B rows per CTA of a tile, and of a tile in the last column block
     long long plane_rows;                   // splits > 1: rows between the parts
-    int F, act;
-    const float* bias;                      // GATED: [2F] or nullptr
+    int F;
+    const float* bias;                      // GATED: [2F] or nullptr, 16-byte aligned
     uint32_t* err;
 };
 
@@ -68,7 +70,7 @@ __device__ __forceinline__ uint4 pack8(const float* v) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <int MODE, bool F32OUT, bool PRE>
+template <int MODE, bool F32OUT, bool PRE, int ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 gated_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapO,
                 const __grid_constant__ CUtensorMap mapG, const __grid_constant__ CUtensorMap mapU, const Args a) {
@@ -231,10 +233,15 @@ gated_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
                             for (int i = 0; i < 8; ++i) { zg[i] = __uint_as_float(rg[8 * g + i]); zu[i] = __uint_as_float(ru[8 * g + i]); }
                             if (a.bias && n < a.F) {     // F % 8 == 0: a group of 8 columns is inside or outside
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) { zg[i] += __ldg(a.bias + n + i); zu[i] += __ldg(a.bias + a.F + n + i); }
+                                for (int i = 0; i < 2; ++i) {
+                                    const float4 bg = __ldg(reinterpret_cast<const float4*>(a.bias + n) + i);
+                                    const float4 bu = __ldg(reinterpret_cast<const float4*>(a.bias + a.F + n) + i);
+                                    zg[4 * i] += bg.x; zg[4 * i + 1] += bg.y; zg[4 * i + 2] += bg.z; zg[4 * i + 3] += bg.w;
+                                    zu[4 * i] += bu.x; zu[4 * i + 1] += bu.y; zu[4 * i + 2] += bu.z; zu[4 * i + 3] += bu.w;
+                                }
                             }
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) hv[i] = free_gate_act_fast(a.act, zg[i]) * zu[i];
+                            for (int i = 0; i < 8; ++i) hv[i] = free_gate_act_fast(ACT, zg[i]) * zu[i];
                             *unit(bufs[0], 4 * h + g) = pack8(hv);
                             if (PRE) { *unit(bufs[NB > 1 ? 1 : 0], 4 * h + g) = pack8(zg); *unit(bufs[NB > 2 ? 2 : 0], 4 * h + g) = pack8(zu); }
                         }
@@ -303,10 +310,10 @@ gated_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
     if (warp == 1) { tc::tc_fence_after(); tc::tmem_dealloc_pair(tmem_base, kTmemCols); }
 }
 
-template <int MODE, bool F32OUT, bool PRE>
+template <int MODE, bool F32OUT, bool PRE, int ACT = FREE_ACT_SILU>
 int launch(const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mO, const CUtensorMap& mG, const CUtensorMap& mU, const Args& a,
            long long rows, cudaStream_t s) {
-    auto kernel = gated_tc_kernel<MODE, F32OUT, PRE>;
+    auto kernel = gated_tc_kernel<MODE, F32OUT, PRE, ACT>;
     FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));   // of the current device
     const long long tiles = (long long)a.num_m * a.num_n * a.splits;
     const int grid = 2 * (int)(tiles < kPairs ? tiles : kPairs);
@@ -334,7 +341,7 @@ bool gated_tc_supported(int F, int K) { return F % 8 == 0 && K % 8 == 0; }
 
 int gated_tc_forward(int act, int M, int F, int K, const void* x, const void* w, const float* bias, void* h, void* preact, uint32_t* err, cudaStream_t s) {
     Args a{};
-    a.M = M; a.N = F; a.F = F; a.act = act; a.bias = bias; a.err = err;
+    a.M = M; a.N = F; a.F = F; a.bias = bias; a.err = err;
     // few rows: blocks of 64 columns put twice as many clusters on the weights
     a.num_m = (M + 255) / 256;
     a.half = (long long)a.num_m * ((F + 127) / 128) <= kPairs / 2 ? 64 : 128;
@@ -344,11 +351,15 @@ int gated_tc_forward(int act, int M, int F, int K, const void* x, const void* w,
     FREE_TRY(free_tensor_map_2d(&mA, x, (uint64_t)K, (uint64_t)M, (uint64_t)K * 2, BK, 128, 128));
     FREE_TRY(free_tensor_map_2d(&mB, w, (uint64_t)K, 2ull * F, (uint64_t)K * 2, BK, (uint32_t)a.half, 128));
     FREE_TRY(free_tensor_map_2d(&mO, h, (uint64_t)F, (uint64_t)M, (uint64_t)F * 2, 64, 32, 128));
-    if (!preact) return launch<GATED, false, false>(mA, mB, mO, mO, mO, a, M, s);
+    const bool silu = act == FREE_ACT_SILU;
+    if (!preact)
+        return silu ? launch<GATED, false, false, FREE_ACT_SILU>(mA, mB, mO, mO, mO, a, M, s)
+                    : launch<GATED, false, false, FREE_ACT_GELU>(mA, mB, mO, mO, mO, a, M, s);
     // one map per half of z, so that a ragged last block of gate columns cannot reach into the up columns
     FREE_TRY(free_tensor_map_2d(&mG, preact, (uint64_t)F, (uint64_t)M, (uint64_t)F * 4, 64, 32, 128));
     FREE_TRY(free_tensor_map_2d(&mU, (const char*)preact + 2ull * F, (uint64_t)F, (uint64_t)M, (uint64_t)F * 4, 64, 32, 128));
-    return launch<GATED, false, true>(mA, mB, mO, mG, mU, a, M, s);
+    return silu ? launch<GATED, false, true, FREE_ACT_SILU>(mA, mB, mO, mG, mU, a, M, s)
+                : launch<GATED, false, true, FREE_ACT_GELU>(mA, mB, mO, mG, mU, a, M, s);
 }
 
 GatedSplit gated_tc_split(bool dw, int M, int F, int K) {

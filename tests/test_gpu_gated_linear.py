@@ -61,7 +61,7 @@ def _check_forward(free, M, F, K, dt, act, bias=True, seed=1):
 
 
 BF16 = [  # M, F, K
-    (1, 8, 8), (1, 64, 64), (3, 72, 40), (1, 4608, 1152), (2, 1536, 384), (127, 136, 72), (128, 128, 128), (129, 200, 264),
+    (2, 16, 24), (4, 1000, 2056), (5, 72, 40), (8, 8, 16), (1, 8, 8), (1, 64, 64), (3, 72, 40), (1, 4608, 1152), (2, 1536, 384), (127, 136, 72), (128, 128, 128), (129, 200, 264),
     (255, 64, 1000), (256, 256, 64), (257, 1000, 136), (600, 1536, 384), (1000, 328, 1152), (5000, 136, 200), (77, 40, 4608),
 ]
 
@@ -73,7 +73,7 @@ def test_forward_bf16(M, F, K, act):
     _check_forward(free, M, F, K, "bf16", act, bias=(M + F) % 3 != 0, seed=M + F + K)
 
 
-FP32 = [(1, 1, 1), (1, 5, 3), (2, 64, 64), (33, 65, 31), (100, 130, 257), (129, 64, 16), (64, 256, 64), (500, 96, 384), (1030, 200, 100), (4000, 9, 33)]
+FP32 = [(7, 33, 1001), (9, 40, 260), (32, 17, 64), (1, 1, 1), (1, 5, 3), (2, 64, 64), (33, 65, 31), (100, 130, 257), (129, 64, 16), (64, 256, 64), (500, 96, 384), (1030, 200, 100), (4000, 9, 33)]
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
