@@ -631,7 +631,7 @@ def _adr(t):
 
 def _launch(what, device, *args):
     """Library call `what` with `device` current, on the stream that is current there (its last argument)."""
-    fn = getattr(lib(), what)
+    fn = getattr(_LIB or lib(), what)
     if device == torch.cuda.current_device():
         code = fn(*args, torch._C._cuda_getCurrentRawStream(device))
     else:

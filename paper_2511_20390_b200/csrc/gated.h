@@ -29,6 +29,7 @@ __device__ __forceinline__ float free_gate_slope(int act, float g, float s) {
 struct GatedSplit {
     int parts;                   // 1: written straight to the output
     long long plane_rows;        // rows of a part in the workspace
+    int half;                    // tensor cores: columns of a tile per CTA of a pair (128 or 64)
 };
 
 // out[i] = sum over parts of parts[p * plane + i], i < n, in the order of the parts; out in `dtype`

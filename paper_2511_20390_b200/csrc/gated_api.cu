@@ -70,14 +70,17 @@ __global__ void __launch_bounds__(kMaxThreads, kPerSm) gated_grad_kernel(int M, 
             for (int e = 0; e < V; ++e) {
                 const float zg = g[k][e], dd = d[k][e], arg = free_gate_arg(ACT, zg);
                 const float s = sizeof(T) == 2 ? free_logistic_fast(arg) : free_logistic(arg);
-                dg[e] = dd * u[k][e] * free_gate_slope(ACT, zg, s); du[e] = dd * (zg * s);
+                // rounded products: the sums take the same values whether dz is stored or not
+                dg[e] = __fmul_rn(dd * u[k][e], free_gate_slope(ACT, zg, s)); du[e] = __fmul_rn(dd, zg * s);
                 sg[e] += dg[e]; su[e] += du[e];
             }
-            P o;
-            o.set(dg);
-            o.store(dz + row * 2 * F + col);
-            o.set(du);
-            o.store(dz + row * 2 * F + F + col);
+            if (dz) {                                              // not where the bias gradient alone is wanted
+                P o;
+                o.set(dg);
+                o.store(dz + row * 2 * F + col);
+                o.set(du);
+                o.store(dz + row * 2 * F + F + col);
+            }
         }
     }
     if (db) {
@@ -226,7 +229,7 @@ extern "C" int free_op_gated_linear_bwd(int dtype, int act, int M, int F, int K,
     const Layout l = layout_of(dtype, M, F, K);
     if (!ws || ws_bytes < l.total) return FREE_ERR_WORKSPACE;
     char* base = (char*)ws;
-    void* dz = base + l.dz;
+    void* dz = dx || dw ? base + l.dz : nullptr;
     float* parts = (float*)(base + l.parts);
     const int chunks = chunks_of(dtype, M, F);
     float* db = !dbias ? nullptr : (chunks > 1 ? (float*)(base + l.db) : dbias);
@@ -236,8 +239,9 @@ extern "C" int free_op_gated_linear_bwd(int dtype, int act, int M, int F, int K,
     if (dbias && chunks > 1)
         FREE_TRY(free_launch(free_launch_overlap_enabled(), gated_bias_kernel, dim3((2u * F + 31) / 32), dim3(512), 0, s, chunks, 2 * F, (const float*)db, dbias));
     if (dtype == FREE_BF16) {
-        if (dw) FREE_TRY(gated_tc_backward(true, M, F, K, x, w, dz, dw, parts, device_error, s));
+        // dx walks over dz from its end, dw then from its start: each begins with what the L2 still holds
         if (dx) FREE_TRY(gated_tc_backward(false, M, F, K, x, w, dz, dx, parts, device_error, s));
+        if (dw) FREE_TRY(gated_tc_backward(true, M, F, K, x, w, dz, dw, parts, device_error, s));
     } else {
         if (dw) FREE_TRY(gated_simt_backward(true, M, F, K, (const float*)x, (const float*)w, (const float*)dz, (float*)dw, parts, s));
         if (dx) FREE_TRY(gated_simt_backward(false, M, F, K, (const float*)x, (const float*)w, (const float*)dz, (float*)dx, parts, s));

@@ -197,7 +197,7 @@ GatedSplit gated_simt_split(bool dw, int M, int F, int K) {
     long long s = (2 * kSms + tiles - 1) / tiles;
     if (s > depth / 256) s = depth / 256;
     if (s > 64) s = 64;
-    return {s < 1 ? 1 : (int)s, rows};
+    return {s < 1 ? 1 : (int)s, rows, 0};
 }
 
 int gated_simt_backward(bool dw, int M, int F, int K, const float* x, const float* w, const float* dz, float* out, float* parts, cudaStream_t s) {

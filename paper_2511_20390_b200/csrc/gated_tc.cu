@@ -26,16 +26,18 @@ enum { GATED = 0, DX = 1, DW = 2 };
 
 constexpr int BK = 64;
 constexpr int kThreads = 192;
-constexpr int kStages = 5;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kABytes = 128 * BK * 2, kStageBytes = 2 * kABytes;
 constexpr uint32_t kBoxBytes = 64 * BK * 2;             // one 64 x 64 box of an MN-major operand
-constexpr uint32_t kCtrlBytes = 1024, kBufBytes = 4096; // staging buffer: 32 rows x 128 bytes
-// Staging buffers per epilogue warp.  (A chunk of GATED with the pre-activations fills three of the four; six, at the price of
-// a stage of operands, measured 4% slower.)
-constexpr int kBufs = 4;
-constexpr uint32_t kSmem = 1024 + kCtrlBytes + 4 * kBufs * kBufBytes + kStages * kStageBytes;
-static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
+constexpr uint32_t kCtrlBytes = 1024;
+// Staging buffers per epilogue warp (GATED: of 32 rows x 64 bytes), and stages of operands: the loads are bound by their
+// latency under load, a sixth stage is worth 4% (24576 rows, F = 4608, K = 1152).
+template <int MODE> struct Mem {
+    static constexpr int bufs = 4, stages = MODE == GATED ? 6 : 5;
+    static constexpr uint32_t buf_bytes = MODE == GATED ? 2048 : 4096;
+    static constexpr uint32_t bytes = 1024 + kCtrlBytes + 4 * bufs * buf_bytes + stages * kStageBytes;
+    static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
+};
 constexpr int kPairs = 74;                              // clusters of two on 148 SMs
 
 struct Args {
@@ -74,6 +76,8 @@ template <int MODE, bool F32OUT, bool PRE, int ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 gated_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapO,
                 const __grid_constant__ CUtensorMap mapG, const __grid_constant__ CUtensorMap mapU, const Args a) {
+    constexpr int kStages = Mem<MODE>::stages, kBufs = Mem<MODE>::bufs;
+    constexpr uint32_t kBufBytes = Mem<MODE>::buf_bytes;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t* full = reinterpret_cast<uint64_t*>(smem);  // used in the even CTA only
@@ -89,6 +93,12 @@ gated_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
     const uint32_t rank = tc::cluster_ctarank();
     const long long per_split = (long long)a.num_m * a.num_n, total = per_split * a.splits;
     const long long first = tc::cluster_id_x(), step = tc::num_clusters_x();
+
+    // DX takes the last rows first: their dz is what the elementwise pass wrote last, and is still in the L2
+    auto row_block = [&](long long t) {
+        const int m = (int)(t % per_split / a.num_n);
+        return MODE == DX ? a.num_m - 1 - m : m;
+    };
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) { tc::mbar_init(&full[s], 1); tc::mbar_init(&empty[s], 1); }
@@ -115,7 +125,7 @@ gated_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
         bool ok = true;
         for (long long t = first; ok && t < total; t += step) {
             const int sp = (int)(t / per_split);
-            const int m_blk = (int)(t % per_split / a.num_n), n_blk = (int)(t % a.num_n);
+            const int m_blk = row_block(t), n_blk = (int)(t % a.num_n);
             const int half = n_blk == a.num_n - 1 ? a.last_half : a.half;
             const int m0 = m_blk * 256 + (int)rank * 128;
             // GATED: gate rows for the even CTA, up rows for the odd one
@@ -198,11 +208,13 @@ gated_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
         const uint32_t acce0 = tc::mapa(tc::smem_u32(&acce[0]), 0);
         uint8_t* mine = staging + (size_t)q * kBufs * kBufBytes;
         uint32_t tl = 0, nst = 0;
-        // 16-byte unit u of this lane's row in a staging buffer (swizzled as the tensor maps expect)
-        auto unit = [&](uint8_t* buf, int u) { return reinterpret_cast<uint4*>(buf + lane * 128 + ((u ^ (lane & 7)) << 4)); };
+        // 16-byte unit u of this lane's row in a staging buffer, rows of 128 bytes (GATED: 64), swizzled as the tensor maps expect
+        auto unit = [&](uint8_t* buf, int u) {
+            return reinterpret_cast<uint4*>(MODE == GATED ? buf + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4) : buf + lane * 128 + ((u ^ (lane & 7)) << 4));
+        };
         for (long long t = first; t < total; t += step, ++tl) {
             const int sp = (int)(t / per_split);
-            const int m_blk = (int)(t % per_split / a.num_n), n_blk = (int)(t % a.num_n);
+            const int m_blk = row_block(t), n_blk = (int)(t % a.num_n);
             const int half = n_blk == a.num_n - 1 ? a.last_half : a.half;
             const uint32_t acc = tl & 1u, aph = (tl >> 1) & 1u;
             if (!tc::wait_uniform(&accf[acc], aph, abort_flag)) { if (lane == 0) fail(FREE_DEV_ERR_ACC_FULL); break; }
@@ -210,41 +222,38 @@ gated_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
             const int row0 = m_blk * 256 + (int)rank * 128 + q * 32;
             const uint32_t t_addr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * 256u;
             if (MODE == GATED) {
-                constexpr int NB = PRE ? 3 : 1;          // staging buffers of a chunk of 64 columns: h, z_gate, z_up
+                constexpr int NB = PRE ? 3 : 1;          // staging buffers of a chunk of 32 columns: h, z_gate, z_up
                 const int n0 = n_blk * a.half;
 #pragma unroll 1
-                for (int c0 = 0; c0 < half && n0 + c0 < a.F; c0 += 64) {
+                for (int c0 = 0; c0 < half && n0 + c0 < a.F; c0 += 32) {
+                    uint32_t rg[32], ru[32];
+                    tc::tmem_ld32(t_addr + (uint32_t)c0, rg);
+                    tc::tmem_ld32(t_addr + (uint32_t)(half + c0), ru);
                     if (lane == 0) tc::bulk_wait_read<kBufs - NB>();   // the stores that last used these buffers have read them
                     __syncwarp();
                     uint8_t* bufs[NB];
 #pragma unroll
                     for (int i = 0; i < NB; ++i) bufs[i] = mine + ((nst + i) % kBufs) * kBufBytes;
-#pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t rg[32], ru[32];
-                        tc::tmem_ld32(t_addr + (uint32_t)(c0 + 32 * h), rg);
-                        tc::tmem_ld32(t_addr + (uint32_t)(half + c0 + 32 * h), ru);
-                        tc::tmem_wait_ld();
+                    tc::tmem_wait_ld();
 #pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const int n = n0 + c0 + 32 * h + 8 * g;
-                            float zg[8], zu[8], hv[8];
+                    for (int g = 0; g < 4; ++g) {
+                        const int n = n0 + c0 + 8 * g;
+                        float zg[8], zu[8], hv[8];
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) { zg[i] = __uint_as_float(rg[8 * g + i]); zu[i] = __uint_as_float(ru[8 * g + i]); }
-                            if (a.bias && n < a.F) {     // F % 8 == 0: a group of 8 columns is inside or outside
+                        for (int i = 0; i < 8; ++i) { zg[i] = __uint_as_float(rg[8 * g + i]); zu[i] = __uint_as_float(ru[8 * g + i]); }
+                        if (a.bias && n < a.F) {         // F % 8 == 0: a group of 8 columns is inside or outside
 #pragma unroll
-                                for (int i = 0; i < 2; ++i) {
-                                    const float4 bg = __ldg(reinterpret_cast<const float4*>(a.bias + n) + i);
-                                    const float4 bu = __ldg(reinterpret_cast<const float4*>(a.bias + a.F + n) + i);
-                                    zg[4 * i] += bg.x; zg[4 * i + 1] += bg.y; zg[4 * i + 2] += bg.z; zg[4 * i + 3] += bg.w;
-                                    zu[4 * i] += bu.x; zu[4 * i + 1] += bu.y; zu[4 * i + 2] += bu.z; zu[4 * i + 3] += bu.w;
-                                }
+                            for (int i = 0; i < 2; ++i) {
+                                const float4 bg = __ldg(reinterpret_cast<const float4*>(a.bias + n) + i);
+                                const float4 bu = __ldg(reinterpret_cast<const float4*>(a.bias + a.F + n) + i);
+                                zg[4 * i] += bg.x; zg[4 * i + 1] += bg.y; zg[4 * i + 2] += bg.z; zg[4 * i + 3] += bg.w;
+                                zu[4 * i] += bu.x; zu[4 * i + 1] += bu.y; zu[4 * i + 2] += bu.z; zu[4 * i + 3] += bu.w;
                             }
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) hv[i] = free_gate_act_fast(ACT, zg[i]) * zu[i];
-                            *unit(bufs[0], 4 * h + g) = pack8(hv);
-                            if (PRE) { *unit(bufs[NB > 1 ? 1 : 0], 4 * h + g) = pack8(zg); *unit(bufs[NB > 2 ? 2 : 0], 4 * h + g) = pack8(zu); }
                         }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) hv[i] = free_gate_act_fast(ACT, zg[i]) * zu[i];
+                        *unit(bufs[0], g) = pack8(hv);
+                        if (PRE) { *unit(bufs[NB > 1 ? 1 : 0], g) = pack8(zg); *unit(bufs[NB > 2 ? 2 : 0], g) = pack8(zu); }
                     }
                     tc::fence_proxy_async();
                     __syncwarp();
@@ -313,6 +322,7 @@ gated_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
 template <int MODE, bool F32OUT, bool PRE, int ACT = FREE_ACT_SILU>
 int launch(const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mO, const CUtensorMap& mG, const CUtensorMap& mU, const Args& a,
            long long rows, cudaStream_t s) {
+    constexpr uint32_t kSmem = Mem<MODE>::bytes;
     auto kernel = gated_tc_kernel<MODE, F32OUT, PRE, ACT>;
     FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));   // of the current device
     const long long tiles = (long long)a.num_m * a.num_n * a.splits;
@@ -320,19 +330,23 @@ int launch(const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mO, 
     return free_launch(free_overlap_for_rows(rows), kernel, dim3(grid), dim3(kThreads), kSmem, s, mA, mB, mO, mG, mU, a);
 }
 
-// Parts that a product of num_m x num_n tiles over nk steps is split into.  A tile costs its steps plus about 6 for filling
-// the pipe; every part adds 8 bytes of traffic per output element (written and read back), in units of a step (64-deep,
-// about 0.3 us on a full GPU, in which HBM moves 2 MB).
-int splits_for(int num_m, int num_n, int nk, long long out_elems) {
-    const long long tiles = (long long)num_m * num_n;
-    int best = 1;
-    double best_cost = 0;
-    for (int s = 1; s <= 32 && s <= nk; ++s) {
-        const long long waves = (tiles * s + kPairs - 1) / kPairs;
-        const double cost = (double)waves * ((double)((nk + s - 1) / s) + 6.0) + (s > 1 ? 10.0 + (double)s * (double)out_elems * 8.0 / 2.0e6 : 0.0);
-        if (s == 1 || cost < best_cost) { best = s; best_cost = cost; }
+// Width of the column blocks and parts of the contraction for a product of `rows` x K outputs over nk steps.  In units of a
+// step of a 256-wide tile (64 deep, about 0.3 us on a full GPU, in which HBM moves 2 MB): a tile costs its steps plus about 6
+// for filling the pipe, a step of a 128-wide tile 0.73 (it runs at the shared-memory bandwidth); parts cost a launch and 8
+// bytes of traffic per output element and part.
+GatedSplit choose_split(long long rows, int K, int nk) {
+    GatedSplit g{1, (rows + 255) / 256 * 256, 128};              // the last row block of a part stays inside its own plane
+    double best = 0;
+    for (int half = 128; half >= 64; half -= 64) {
+        const long long tiles = (rows + 255) / 256 * ((K + 2 * half - 1) / (2 * half));
+        for (int s = 1; s <= 32 && s <= nk; ++s) {
+            const long long waves = (tiles * s + kPairs - 1) / kPairs;
+            const double cost = (double)waves * ((half == 64 ? 0.73 : 1.0) * ((nk + s - 1) / s) + 6.0) +
+                                (s > 1 ? 10.0 + (double)s * (double)rows * K * 8.0 / 2.0e6 : 0.0);
+            if ((half == 128 && s == 1) || cost < best) { best = cost; g.parts = s; g.half = half; }
+        }
     }
-    return best;
+    return g;
 }
 
 }  // namespace
@@ -350,35 +364,31 @@ int gated_tc_forward(int act, int M, int F, int K, const void* x, const void* w,
     CUtensorMap mA, mB, mO, mG, mU;
     FREE_TRY(free_tensor_map_2d(&mA, x, (uint64_t)K, (uint64_t)M, (uint64_t)K * 2, BK, 128, 128));
     FREE_TRY(free_tensor_map_2d(&mB, w, (uint64_t)K, 2ull * F, (uint64_t)K * 2, BK, (uint32_t)a.half, 128));
-    FREE_TRY(free_tensor_map_2d(&mO, h, (uint64_t)F, (uint64_t)M, (uint64_t)F * 2, 64, 32, 128));
+    FREE_TRY(free_tensor_map_2d(&mO, h, (uint64_t)F, (uint64_t)M, (uint64_t)F * 2, 32, 32, 64));
     const bool silu = act == FREE_ACT_SILU;
     if (!preact)
         return silu ? launch<GATED, false, false, FREE_ACT_SILU>(mA, mB, mO, mO, mO, a, M, s)
                     : launch<GATED, false, false, FREE_ACT_GELU>(mA, mB, mO, mO, mO, a, M, s);
     // one map per half of z, so that a ragged last block of gate columns cannot reach into the up columns
-    FREE_TRY(free_tensor_map_2d(&mG, preact, (uint64_t)F, (uint64_t)M, (uint64_t)F * 4, 64, 32, 128));
-    FREE_TRY(free_tensor_map_2d(&mU, (const char*)preact + 2ull * F, (uint64_t)F, (uint64_t)M, (uint64_t)F * 4, 64, 32, 128));
+    FREE_TRY(free_tensor_map_2d(&mG, preact, (uint64_t)F, (uint64_t)M, (uint64_t)F * 4, 32, 32, 64));
+    FREE_TRY(free_tensor_map_2d(&mU, (const char*)preact + 2ull * F, (uint64_t)F, (uint64_t)M, (uint64_t)F * 4, 32, 32, 64));
     return silu ? launch<GATED, false, true, FREE_ACT_SILU>(mA, mB, mO, mG, mU, a, M, s)
                 : launch<GATED, false, true, FREE_ACT_GELU>(mA, mB, mO, mG, mU, a, M, s);
 }
 
 GatedSplit gated_tc_split(bool dw, int M, int F, int K) {
-    const int rows = dw ? 2 * F : M, depth = dw ? M : 2 * F;
-    GatedSplit g;
-    g.parts = splits_for((rows + 255) / 256, (K + 255) / 256, (depth + BK - 1) / BK, (long long)rows * K);
-    g.plane_rows = ((long long)rows + 255) / 256 * 256;      // the last row block of a part stays inside its own plane
-    return g;
+    return choose_split(dw ? 2LL * F : M, K, ((dw ? M : 2 * F) + BK - 1) / BK);
 }
 
 int gated_tc_backward(bool dw, int M, int F, int K, const void* x, const void* w, const void* dz, void* out, float* parts, uint32_t* err, cudaStream_t s) {
     const GatedSplit g = gated_tc_split(dw, M, F, K);
     Args a{};
     a.M = dw ? 2 * F : M; a.N = K; a.F = F; a.err = err;
-    a.num_m = (a.M + 255) / 256; a.num_n = (K + 255) / 256; a.nk = ((dw ? M : 2 * F) + BK - 1) / BK;
+    a.half = g.half;
+    a.num_m = (a.M + 255) / 256; a.num_n = (K + 2 * a.half - 1) / (2 * a.half); a.nk = ((dw ? M : 2 * F) + BK - 1) / BK;
     a.splits = g.parts; a.plane_rows = g.plane_rows;
     if (g.parts * g.plane_rows > 0x7fffffffLL) return FREE_ERR_UNSUPPORTED;
-    a.half = 128;
-    a.last_half = K - (a.num_n - 1) * 256 <= 128 ? 64 : 128;     // a ragged last column block is computed 128 wide where that holds it
+    a.last_half = K - (a.num_n - 1) * 2 * a.half <= 128 ? 64 : a.half;     // a ragged last column block is computed 128 wide where that holds it
     CUtensorMap mA, mB, mO;
     if (dw) {
         FREE_TRY(free_tensor_map_2d(&mA, dz, 2ull * F, (uint64_t)M, (uint64_t)F * 4, 64, BK, 128));
