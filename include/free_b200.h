@@ -465,7 +465,8 @@ int free_op_ln_modulate(int out_dtype, int M, int D, int rows_per_seq, const flo
  * the product.  W holds the F gate rows and then the F up rows, z = x W^T + bias:
  *     h = act(z[:, 0:F]) * z[:, F:2F]
  *   dtype      FREE_FP32 (CUDA cores, any sizes) or FREE_BF16 (tcgen05, fp32 accumulation; F % 8 == 0 and K % 8 == 0, the
- *              16-byte rows that tile copies need, else UNSUPPORTED): type of x, w, h and preact
+ *              16-byte rows that tile copies need, else UNSUPPORTED): type of x, w, h and preact.
+ *              M up to 2^30, F and K up to 2^28
  *   act        FREE_ACT_SILU: g / (1 + e^-g);  FREE_ACT_GELU: 0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
  *   x          DEVICE [M, K]; M = 0 is allowed and does nothing
  *   w          DEVICE [2F, K];  bias  DEVICE fp32 [2F] or NULL
@@ -506,7 +507,7 @@ int free_op_gated_linear_bwd(int dtype, int act, int M, int F, int K, const void
  *   bias       DEVICE fp32, laid out as weight, or NULL for 0
  *   stats      DEVICE fp32 [M, 2] or NULL: mu and r of every row, what the backward pass needs
  * No workspace.  weight, bias and stats need 4-byte alignment only.  A row with an infinity or NaN gives NaN, as the formula.
- * Rows and strides that are multiples of 16 bytes (and D % 8 == 0) are the fast form.
+ * D % 4 == 0 with strides that are multiples of four elements is the fast form (and 16-byte aligned weight and bias rows).
  * Errors: ARG, SHAPE, ALIGN, UNSUPPORTED (D > 8192), CUDA.
  *
  * free_op_layer_norm_bwd -- its gradients, from dy and the stats that the forward call kept.  With xh = (x - mu) r, v = dy w:

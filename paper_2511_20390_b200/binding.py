@@ -625,6 +625,11 @@ def _device_of(first, *others):
     return d
 
 
+def _like(t, dtype):
+    """Uninitialised contiguous tensor of t's shape and device (the cheapest of torch's ways to make one)."""
+    return torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format)
+
+
 def _adr(t):
     return None if t is None else t.data_ptr()
 
@@ -686,11 +691,11 @@ def op_layer_norm(x, weight=None, bias=None, rows_per_group=None, unit_offset=Fa
         ms = bs
     if out is None:
         yc = xc if out_dtype is None else _code(out_dtype)
-        out = torch.empty((M, D), dtype=_ACT[yc], device=x.device)
+        out = _like(x, _ACT[yc])
         ys = D
     else:
         yc, ys = _code(out.dtype), _rows(out, M, D, "out")
-    stats = torch.empty((M, 2), dtype=torch.float32, device=x.device) if want_stats else None
+    stats = x.new_empty((M, 2), dtype=torch.float32) if want_stats else None
     _launch("free_op_layer_norm", dev, xc, yc, groups, rows, D, x.data_ptr(), xs, _adr(weight), _adr(bias), ms, 1 if unit_offset else 0, eps,
             out.data_ptr(), ys, _adr(stats))
     return (out, stats) if want_stats else out
@@ -710,9 +715,9 @@ def op_layer_norm_bwd(x, dy, stats, weight=None, rows_per_group=None, unit_offse
     if (dres is not None and dres.dtype != x.dtype) or (dx is not None and dx.dtype != x.dtype):
         raise ValueError("dres, dx: expected x's dtype")
     if dx is None:
-        dx = torch.empty((M, D), dtype=x.dtype, device=x.device)
-    dw = torch.empty((groups, D), dtype=torch.float32, device=x.device) if want_dweight else None
-    db = torch.empty((groups, D), dtype=torch.float32, device=x.device) if want_dbias else None
+        dx = _like(x, x.dtype)
+    dw = stats.new_empty((groups, D)) if want_dweight else None
+    db = stats.new_empty((groups, D)) if want_dbias else None
     need = lib().free_op_layer_norm_bwd_workspace_bytes(groups, rows, D) if want_dweight or want_dbias else 0
     ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     _launch("free_op_layer_norm_bwd", dev, _code(x.dtype), _code(dy.dtype), groups, rows, D, x.data_ptr(), _rows(x, M, D, "x"),
@@ -745,7 +750,7 @@ def op_rope_axes(x, pos, axis_dims, base=10000.0, pairing="interleaved", joint_f
         raise ValueError("pos: expected contiguous fp32 [n_tok, n_axes] or [n_seq, n_tok, n_axes]")
     xs = x.stride()
     if out is None:
-        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        out = _like(x, x.dtype)
         hs = heads * d_head
         ys = (n_tok * hs, hs, d_head)
     else:
@@ -807,10 +812,10 @@ def op_gated_linear(x, w, bias=None, act="silu", want_preact=False, out=None):
     if bias is not None:
         _dense(bias, torch.float32, (2 * F,), "bias")
     if out is None:
-        out = torch.empty((M, F), dtype=dtype, device=x.device)
+        out = x.new_empty((M, F))
     else:
         _dense(out, dtype, (M, F), "out")
-    pre = torch.empty((M, 2 * F), dtype=dtype, device=x.device) if want_preact else None
+    pre = x.new_empty((M, 2 * F)) if want_preact else None
     _launch("free_op_gated_linear", dev, code, ACTIVATIONS[act], M, F, K, x.data_ptr(), w.data_ptr(), _adr(bias), out.data_ptr(), _adr(pre),
             _error_word(dev).data_ptr() if code == FREE_BF16 else None)
     return (out, pre) if want_preact else out
@@ -827,9 +832,9 @@ def op_gated_linear_bwd(x, w, preact, dh, act="silu", want_dx=True, want_dw=True
     dev, code = _device_of(x, w, preact, dh), _code(dtype)
     _dense(x, dtype, (M, K), "x"); _dense(w, dtype, (2 * F, K), "w")
     _dense(preact, dtype, (M, 2 * F), "preact"); _dense(dh, dtype, (M, F), "dh")
-    dx = torch.empty((M, K), dtype=dtype, device=x.device) if want_dx else None
-    dw = torch.empty((2 * F, K), dtype=dtype, device=x.device) if want_dw else None
-    db = torch.empty(2 * F, dtype=torch.float32, device=x.device) if want_dbias else None
+    dx = _like(x, dtype) if want_dx else None
+    dw = _like(w, dtype) if want_dw else None
+    db = x.new_empty(2 * F, dtype=torch.float32) if want_dbias else None
     need = lib().free_op_gated_linear_bwd_workspace_bytes(code, M, F, K)
     ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     _launch("free_op_gated_linear_bwd", dev, code, ACTIVATIONS[act], M, F, K, x.data_ptr(), w.data_ptr(), preact.data_ptr(), dh.data_ptr(),

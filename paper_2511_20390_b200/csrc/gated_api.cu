@@ -162,6 +162,9 @@ Layout layout_of(int dtype, int M, int F, int K) {
     return l;
 }
 
+// Sizes whose tile counts and coordinates fit 32 bits.
+constexpr int kMaxRows = 1 << 30, kMaxCols = 1 << 28;
+bool too_large(int M, int F, int K) { return M > kMaxRows || F > kMaxCols || K > kMaxCols; }
 bool known(int dtype) { return dtype == FREE_FP32 || dtype == FREE_BF16; }
 bool known_act(int act) { return act == FREE_ACT_SILU || act == FREE_ACT_GELU; }
 
@@ -190,7 +193,7 @@ extern "C" int free_op_gated_linear(int dtype, int act, int M, int F, int K, con
                                     void* h, void* preact, uint32_t* device_error, void* stream) {
     if (!known(dtype) || !known_act(act)) return FREE_ERR_ARG;
     if (M < 0 || F < 1 || K < 1) return FREE_ERR_SHAPE;
-    if (F > 0x3fffffff) return FREE_ERR_UNSUPPORTED;
+    if (too_large(M, F, K)) return FREE_ERR_UNSUPPORTED;
     if (dtype == FREE_BF16 && !gated_tc_supported(F, K)) return FREE_ERR_UNSUPPORTED;
     if (M == 0) return FREE_OK;
     if (!x || !w || !h || (dtype == FREE_BF16 && !device_error)) return FREE_ERR_ARG;
@@ -203,7 +206,7 @@ extern "C" int free_op_gated_linear(int dtype, int act, int M, int F, int K, con
 }
 
 extern "C" size_t free_op_gated_linear_bwd_workspace_bytes(int dtype, int M, int F, int K) {
-    if (!known(dtype) || M < 1 || F < 1 || F > 0x3fffffff || K < 1 || (dtype == FREE_BF16 && !gated_tc_supported(F, K))) return 0;
+    if (!known(dtype) || M < 1 || F < 1 || K < 1 || too_large(M, F, K) || (dtype == FREE_BF16 && !gated_tc_supported(F, K))) return 0;
     return layout_of(dtype, M, F, K).total;
 }
 
@@ -212,7 +215,7 @@ extern "C" int free_op_gated_linear_bwd(int dtype, int act, int M, int F, int K,
                                         uint32_t* device_error, void* stream) {
     if (!known(dtype) || !known_act(act)) return FREE_ERR_ARG;
     if (M < 0 || F < 1 || K < 1) return FREE_ERR_SHAPE;
-    if (F > 0x3fffffff) return FREE_ERR_UNSUPPORTED;
+    if (too_large(M, F, K)) return FREE_ERR_UNSUPPORTED;
     if (dtype == FREE_BF16 && !gated_tc_supported(F, K)) return FREE_ERR_UNSUPPORTED;
     if (!dx && !dw && !dbias) return FREE_OK;
     if (M > 0 && (!preact || !dh || (dx && !w) || (dw && !x))) return FREE_ERR_ARG;

@@ -18,7 +18,6 @@
 // Bound by the tensor pipe except for few rows, where the weights' bytes are.
 #include "gated.h"
 #include "tc_common.cuh"
-#include <mutex>
 
 namespace {
 

@@ -114,6 +114,7 @@ def test_gated_linear(L):
         assert _gated(L, **{k: ODD}) == ALIGN
     assert _gated(L, b=C.c_void_p(4098)) == ALIGN
     assert _gated(L, F=60) == UNSUPPORTED and _gated(L, K=36) == UNSUPPORTED        # rows that are not multiples of 16 bytes
+    assert _gated(L, M=(1 << 30) + 1) == UNSUPPORTED and _gated(L, F=(1 << 28) + 8) == UNSUPPORTED and _gated(L, K=1 << 30) == UNSUPPORTED
     assert _gated(L, M=0, x=None, w=None, h=None, err=None) == 0
 
 
@@ -125,6 +126,7 @@ def test_gated_linear_bwd(L):
     for k in ("x", "w", "pre", "dh", "dx", "dw"):
         assert _gated_bwd(L, **{k: ODD}) == ALIGN
     assert _gated_bwd(L, F=60) == UNSUPPORTED and _gated_bwd(L, K=36) == UNSUPPORTED
+    assert _gated_bwd(L, M=(1 << 30) + 1) == UNSUPPORTED and L.free_op_gated_linear_bwd_workspace_bytes(1, 4, 1 << 29, 64) == 0
     need = L.free_op_gated_linear_bwd_workspace_bytes(1, 4, 64, 64)
     assert need >= 4 * 128 * 2
     assert _gated_bwd(L) == WORKSPACE and _gated_bwd(L, ws=P, need=need - 1) == WORKSPACE

@@ -224,6 +224,26 @@ def test_streams_and_graphs():
         assert torch.equal(h2, h3) and all(torch.equal(p, q) for p, q in zip(got, want))
 
 
+def test_first_call_inside_a_capture_is_refused():
+    # the error word that the calls share must not be made (and zeroed) inside a graph
+    from paper_2511_20390_b200 import binding
+    x, w = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(32, 64, dtype=torch.bfloat16, device="cuda")
+    kept = dict(binding._ERROR_WORDS)
+    binding._ERROR_WORDS.clear()
+    refused = False
+    try:
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            try:
+                binding.op_gated_linear(x, w)
+            except RuntimeError:
+                refused = True
+            x.add_(0.0)                                            # a graph with something in it
+    finally:
+        binding._ERROR_WORDS.update(kept)
+    assert refused
+    assert not binding.op_gated_linear(x, w).any()
+
+
 def test_the_tolerance_sees_swapped_halves():
     # a mistake planted in the definition: gate and up rows exchanged
     x, w = synth.normal(1, 1, (20, 64)).astype(np.float64), synth.normal(1, 2, (32, 64)).astype(np.float64) / 8

@@ -156,6 +156,37 @@ def test_in_place_rows_between_and_bad_values():
         assert torch.equal(x, ref) and torch.isnan(base[:, D:]).all()
 
 
+def test_rows_far_apart():
+    # two rows more than 2^32 bytes apart in one allocation, in and out
+    import paper_2511_20390_b200 as free
+    step = (1 << 31) + 64
+    buf = torch.empty(step + 1152, dtype=torch.bfloat16, device="cuda")
+    x = buf.as_strided((2, 1152), (step, 1))
+    x.copy_(_mat(13, 1, 2, 1152, "bf16")[0])
+    ref, st = free.op_layer_norm(x.contiguous(), want_stats=True)
+    dref = free.op_layer_norm_bwd(x.contiguous(), ref, st)
+    assert torch.equal(free.op_layer_norm(x), ref)
+    got = free.op_layer_norm_bwd(x, ref, st, dx=x)
+    assert torch.equal(x, dref[0]) and torch.equal(got[1], dref[1])
+
+
+def test_unaligned_tables_and_gradients_over_their_inputs():
+    import paper_2511_20390_b200 as free
+    for D in (1152, 384, 2304, 513):
+        x, _ = _mat(14, 1, 30, D, "fp32")
+        dy, _ = _mat(14, 2, 30, D, "fp32")
+        table = torch.from_numpy(synth.normal(14, 3, (3, 2 * D + 3))).cuda()
+        w, b = table[:, 1:D + 1], table[:, D + 2:2 * D + 2]        # rows that start at any element
+        y, st = free.op_layer_norm(x, w, b, rows_per_group=10, want_stats=True)
+        assert torch.equal(y, free.op_layer_norm(x, w.contiguous(), b.contiguous(), rows_per_group=10))
+        ref = free.op_layer_norm_bwd(x, dy, st, w.contiguous(), rows_per_group=10)
+        for over in (x, dy):
+            a, g = x.clone(), dy.clone()
+            dst = a if over is x else g
+            got = free.op_layer_norm_bwd(a, g, st, w, rows_per_group=10, dx=dst)
+            assert torch.equal(dst, ref[0]) and torch.equal(got[1], ref[1]) and torch.equal(got[2], ref[2])
+
+
 def test_a_constant_row_and_a_tiny_variance():
     import paper_2511_20390_b200 as free
     x = torch.full((4, 1152), 2.5, device="cuda")
