@@ -8,8 +8,8 @@
 // the mean of its own columns and their squared deviations from it, and the parts are combined with the exact formula
 // M2 = sum M2_k + n_k (mean_k - mean)^2, so that a large mean cancels nothing.
 // Forward: a warp holds a row in registers (up to 2048 columns; several warps beyond), so a row costs ten exchanges and no
-// barrier; the weight and bias of a group come from the L1, or stay in registers for narrow rows.  24 x 1024 rows of 1152, fp32
-// to bf16, weight and bias per sequence: 29 us, 5.8 TB/s (a CTA per row with a barrier each: 41 us).
+// barrier; the weight and bias of a group come from the L1.  24 x 1024 rows of 1152, fp32 to bf16, weight and bias per sequence:
+// 29.5 us, 5.8 TB/s (a CTA per row with a barrier each: 41 us); 6144 rows of 4608: 33 us.
 // Backward: the column sums need registers too, so a row is spread over ceil(D / 256) warps, eight columns per lane, with one
 // barrier; rows are copied to shared memory one ahead of their use, every thread its own columns, so that the bytes in flight do
 // not cost registers.  The same rows with the residual path's gradient added: 65 us, 6.1 TB/s, and 5 us for the sums.
@@ -23,7 +23,6 @@ namespace {
 constexpr int kMaxWarps = 32;
 constexpr int kMaxD = kMaxWarps * 256;
 constexpr int kSms = 148;
-constexpr int kWide = 5;                                           // blocks per warp of the forward kernel for several warps
 
 // Eight columns as they come from memory (bf16 stays packed until it is used).
 template <typename T, bool VEC> struct Raw {
@@ -56,10 +55,10 @@ __device__ __forceinline__ void st1(__nv_bfloat16* p, float v) { *p = __float2bf
 // (fp32) or 256 (bf16) bytes; D % 4 == 0, rows aligned to four elements.  (Eight consecutive columns per lane, two 16-byte
 // accesses 32 bytes apart in fp32, make two half-used sectors of every sector: measured 20 to 40% slower.)
 // Otherwise columns l, l + 32, ..., l + 224: any D, any row stride.
-template <bool VEC, int NV> struct Cols {
+template <bool VEC> struct Cols {
     int D, k, lane;
     __device__ __forceinline__ int at(int i, int e) const {
-        return (k * NV + i) * 256 + (VEC ? (e / 4) * 128 + lane * 4 + e % 4 : e * 32 + lane);
+        return (k + i) * 256 + (VEC ? (e / 4) * 128 + lane * 4 + e % 4 : e * 32 + lane);
     }
     __device__ __forceinline__ bool in(int i, int e) const { return at(i, VEC ? e / 4 * 4 : e) < D; }
     // straight into registers
@@ -83,9 +82,9 @@ template <bool VEC, int NV> struct Cols {
             for (int e = 0; e < 8; ++e) v.r[e] = in(i, e) ? __float_as_uint(to_f(row[at(i, e)])) : 0u;
         }
     }
-    // a table's row (the L1 serves it: every row of a group reads the same).  aligned: four columns are one access
-    __device__ __forceinline__ void table(const float* row, int i, bool aligned, float add, float (&v)[8]) const {
-        if (VEC && aligned) {
+    // a table's row
+    __device__ __forceinline__ void table(const float* row, int i, float add, float (&v)[8]) const {
+        if (VEC) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const float4 f = in(i, 4 * h) ? __ldg(reinterpret_cast<const float4*>(row + at(i, 4 * h))) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -136,7 +135,6 @@ struct NormArgs {
     const float *weight, *bias; long long mod_stride; float unit;   // unit: 1 where the weight is stored as an offset from one
     float eps;
     void* y; long long y_stride;
-    bool table_vec;                           // weight and bias rows are 16-byte aligned
     float* stats;                             // [M][2]: mu, r
     long long rows_per_team;                  // forward: consecutive rows of a team
     // backward
@@ -163,56 +161,106 @@ template <int MAXW> __device__ __forceinline__ float2 team_sum(const float2* par
     return s;
 }
 
-// NV: 256-column blocks per warp.  A team is one warp (eight teams per CTA) where NV blocks hold the row, else the CTA.
-template <typename TX, typename TY, int NV, bool VEC, int MINB, int MAXW>
-__global__ void __launch_bounds__(256, MINB) layer_norm_kernel(const NormArgs a) {
-    constexpr bool KEEP = NV <= 2;                                 // weight and bias stay in registers, else they come from the L1
+// Forward: a warp of a team owns NH blocks of 128 columns, four per lane and block (Cols, with half the width).
+// FULL: the row is exactly the team's blocks, nothing is checked.
+template <bool VEC, int NH, bool FULL> struct Cols4 {
+    int D, k, lane;
+    __device__ __forceinline__ int at(int h, int e) const { return (k * NH + h) * 128 + (VEC ? lane * 4 + e : e * 32 + lane); }
+    __device__ __forceinline__ bool in(int h, int e) const { return FULL || at(h, VEC ? 0 : e) < D; }
+    template <typename E> __device__ __forceinline__ void load(const E* row, int h, uint32_t (&v)[VEC ? sizeof(E) : 4]) const {
+        if (VEC) {
+            const E* p = row + at(h, 0);
+            if (sizeof(E) == 4) {
+                const uint4 u = in(h, 0) ? __ldcs(reinterpret_cast<const uint4*>(p)) : make_uint4(0u, 0u, 0u, 0u);
+                v[0] = u.x; v[1] = u.y; v[sizeof(E) - 2] = u.z; v[sizeof(E) - 1] = u.w;
+            } else {
+                const uint2 u = in(h, 0) ? __ldcs(reinterpret_cast<const uint2*>(p)) : make_uint2(0u, 0u);
+                v[0] = u.x; v[1] = u.y;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = in(h, e) ? __float_as_uint(to_f(row[at(h, e)])) : 0u;
+        }
+    }
+    template <typename E> static __device__ __forceinline__ float value(const uint32_t (&v)[VEC ? sizeof(E) : 4], int e) {
+        if (!VEC || sizeof(E) == 4) return __uint_as_float(v[e]);
+        return __uint_as_float(e % 2 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
+    }
+    // a table's row
+    __device__ __forceinline__ void table(const float* row, int h, float add, float (&v)[4]) const {
+        if (VEC) {
+            const float4 f = in(h, 0) ? __ldg(reinterpret_cast<const float4*>(row + at(h, 0))) : make_float4(0.f, 0.f, 0.f, 0.f);
+            v[0] = f.x + add; v[1] = f.y + add; v[2] = f.z + add; v[3] = f.w + add;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = in(h, e) ? __ldg(row + at(h, e)) + add : 0.f;
+        }
+    }
+    template <typename E> __device__ __forceinline__ void store(E* row, int h, const float (&v)[4]) const {
+        if (VEC) {
+            if (in(h, 0)) st4(row + at(h, 0), v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (in(h, e)) st1(row + at(h, e), v[e]);
+        }
+    }
+};
+
+// A team is one warp where NH blocks hold the row (MAXW == 1), else the CTA.  The next row's loads are in flight while this one is
+// reduced; the weight and bias come from the L1 (in registers they cost more rows in flight than they save: 31.2 against 30.7 us
+// for 24 x 1024 rows of 1152, 4.8 against 3.5 for 2048 rows).
+template <typename TX, typename TY, int NH, bool VEC, bool FULL, int MAXT, int MINB, int MAXW>
+__global__ void __launch_bounds__(MAXT, MINB) layer_norm_kernel(const NormArgs a) {
     __shared__ float2 part[2][MAXW];
     free_grid_dep_wait();
     free_grid_dep_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int W = MAXW > 1 ? a.warps : 1;
-    const Cols<VEC, NV> c{a.D, W > 1 ? warp : 0, lane};
+    using C = Cols4<VEC, NH, FULL>;
+    const C c{a.D, W > 1 ? warp : 0, lane};
     const TX* x = reinterpret_cast<const TX*>(a.x);
     TY* y = reinterpret_cast<TY*>(a.y);
-    const long long team = W > 1 ? blockIdx.x : (long long)blockIdx.x * (blockDim.x >> 5) + warp;
+    const long long team = MAXW > 1 ? blockIdx.x : (long long)blockIdx.x * (blockDim.x >> 5) + warp;
     const long long first = team * a.rows_per_team;
     const long long last = first + a.rows_per_team < a.M ? first + a.rows_per_team : a.M;
-    constexpr float full = NV * 256.f;                             // columns of all of a team's warps but the last
+    constexpr float full = NH * 128.f;                             // columns of all of a team's warps but the last
     const float inv_d = 1.f / (float)a.D, n_last = (float)a.D - (float)(W - 1) * full;
     const float inv_n = c.k < W - 1 ? 1.f / full : 1.f / n_last;
-    float w[KEEP ? NV : 1][8], b[KEEP ? NV : 1][8];
-    if (KEEP) {
+    uint32_t nx[NH][VEC ? sizeof(TX) : 4];
+    auto fetch = [&](long long row) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { w[i][e] = 1.f; b[i][e] = 0.f; }
-    }
+        for (int h = 0; h < NH; ++h) c.template load<TX>(x + row * a.x_stride, h, nx[h]);
+    };
     const bool tables = a.weight || a.bias;
-    long long group_end = tables ? first : a.M;                    // first row that the weight and bias at hand do not belong to
-    const float *wp = a.weight, *bp = a.bias;
+    // the first row that the weight and bias at hand do not belong to, where they lie, and how far away the next group's are
+    // (one division per warp: the code stays short, which counts more than anything else for small calls)
+    const long long g0 = !tables ? 0 : first <= 0xffffffffLL ? (long long)((uint32_t)first / (uint32_t)a.rows_per_group) : first / a.rows_per_group;
+    long long group_end = tables ? g0 * a.rows_per_group : a.M, mo = g0 * a.mod_stride, step = 0;
+    if (first < last) fetch(first);
     int it = 0;
     for (long long row = first; row < last; ++row, ++it) {
-        float v[NV][8];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            Raw<TX, VEC> raw;
-            c.load(x + row * a.x_stride, i, raw);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = raw[e];
+        if (row >= group_end) {                                    // uniform over the team
+            mo += step;
+            step = a.mod_stride;
+            group_end += a.rows_per_group;
         }
+        float v[NH][4];
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[h][e] = C::template value<TX>(nx[h], e);
+        if (row + 1 < last) fetch(row + 1);
         float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s += v[i][e];
+        for (int h = 0; h < NH; ++h) s += (v[h][0] + v[h][1]) + (v[h][2] + v[h][3]);
         float mu = free_warp_sum(s) * inv_n, q = 0.f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int h = 0; h < NH; ++h)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { const float d = v[i][e] - mu; q += c.in(i, e) ? d * d : 0.f; }
+            for (int e = 0; e < 4; ++e) { const float d = v[h][e] - mu; q += c.in(h, e) ? d * d : 0.f; }
         float m2 = free_warp_sum(q);                               // squared deviations from this warp's mean
-        if (MAXW > 1 && W > 1) {
+        if (MAXW > 1) {
             float2* now = part[it & 1];                            // a buffer is rewritten two barriers after its last read
             if (lane == 0) now[warp] = make_float2(mu, m2);
             __syncthreads();
@@ -225,41 +273,23 @@ __global__ void __launch_bounds__(256, MINB) layer_norm_kernel(const NormArgs a)
             m2 = t.y + pl.y + full * d2 + n_last * (pl.x - mu) * (pl.x - mu);
         }
         const float rstd = rsqrtf(m2 * inv_d + a.eps);
-        if (row >= group_end) {                                    // uniform over the team
-            const long long g = row / a.rows_per_group, mo = g * a.mod_stride;
-            group_end = (g + 1) * a.rows_per_group;
-            if (a.weight) wp = a.weight + mo;
-            if (a.bias) bp = a.bias + mo;
-            if (KEEP) {
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (a.weight) c.table(wp, i, a.table_vec, a.unit, w[i]);
-                    if (a.bias) c.table(bp, i, a.table_vec, 0.f, b[i]);
-                }
+        for (int h = 0; h < NH; ++h) {
+            float o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = (v[h][e] - mu) * rstd;
+            float t[4];
+            if (a.weight) {
+                c.table(a.weight + mo, h, a.unit, t);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] *= t[e];
             }
-        }
+            if (a.bias) {
+                c.table(a.bias + mo, h, 0.f, t);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float o[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = (v[i][e] - mu) * rstd;
-            if (KEEP) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = o[e] * w[i][e] + b[i][e];
-            } else {
-                float t[8];
-                if (a.weight) {
-                    c.table(wp, i, a.table_vec, a.unit, t);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] *= t[e];
-                }
-                if (a.bias) {
-                    c.table(bp, i, a.table_vec, 0.f, t);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] += t[e];
-                }
+                for (int e = 0; e < 4; ++e) o[e] += t[e];
             }
-            c.store(y + row * a.y_stride, i, o);
+            c.store(y + row * a.y_stride, h, o);
         }
         if (a.stats && c.k == 0 && lane == 0) { a.stats[2 * row] = mu; a.stats[2 * row + 1] = rstd; }
     }
@@ -274,7 +304,7 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
     free_grid_dep_wait();
     free_grid_dep_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, W = a.warps;
-    const Cols<VEC, 1> c{a.D, warp, lane};
+    const Cols<VEC> c{a.D, warp, lane};
     const TX* x = reinterpret_cast<const TX*>(a.x);
     const TY* dy = reinterpret_cast<const TY*>(a.dy);
     const TX* dres = reinterpret_cast<const TX*>(a.dres);
@@ -309,7 +339,7 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
     float w[8], dw[8], db[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) { w[e] = 1.f; dw[e] = 0.f; db[e] = 0.f; }
-    if (a.weight) c.table(a.weight + (long long)g * a.mod_stride, 0, a.table_vec, a.unit, w);
+    if (a.weight) c.table(a.weight + (long long)g * a.mod_stride, 0, a.unit, w);
     float2 next[R];                                                // statistics of the rows to come
 #pragma unroll
     for (int r = 0; r < R; ++r) next[r] = stats_of(lo + r);
@@ -409,7 +439,8 @@ __global__ void __launch_bounds__(512) layer_norm_reduce_kernel(const NormArgs a
     }
 }
 
-constexpr int kBwdT = 1024, kBwdScalarT = 512;                     // threads per SM of the backward kernel
+// Threads per SM of the backward kernel.  The scalar form has no copies ahead of their use: two rows per barrier, in twice the registers.
+constexpr int kBwdT = 1024, kBwdScalarT = 512;
 
 int bwd_threads(int D) { return (D + 255) / 256 * 32; }
 
@@ -417,32 +448,53 @@ int bwd_threads(int D) { return (D + 255) / 256 * 32; }
 // workspace depends on it.)
 int chunks_of(int groups, int rows_per_group, int D) {
     const int t = bwd_threads(D);
-    const int per_sm = t <= 256 ? kBwdT / t : 1;
+    const int per_sm = t > 256 ? 1 : (D % 4 ? kBwdScalarT : kBwdT) / t;
     const long long want = ((long long)kSms * per_sm + groups - 1) / groups;
     const long long most = rows_per_group / 8;
     const long long c = want < most ? want : most;
     return c < 1 ? 1 : (int)c;
 }
 
-template <typename TX, typename TY, int NV, bool VEC, int MINB, int MAXW>
+template <typename TX, typename TY, int NH, bool VEC, bool FULL, int MAXT, int MINB, int MAXW>
 int start_fwd(NormArgs a, int warps, cudaStream_t s) {
-    const int threads = MAXW > 1 ? warps * 32 : 256, teams = MAXW > 1 ? 1 : 8;
+    const int threads = MAXW > 1 ? warps * 32 : MAXT, teams = MAXW > 1 ? 1 : MAXT / 32;
     a.warps = warps;
     // one wave of the CTAs that the GPU holds at once; few rows: as many teams as there are rows
-    const long long resident = (long long)kSms * (MINB * 256 / threads) * teams;
+    const long long resident = (long long)kSms * (MINB * MAXT / threads) * teams;
     a.rows_per_team = (a.M + resident - 1) / resident;
     const long long grid = (a.M + a.rows_per_team * teams - 1) / (a.rows_per_team * teams);
-    return free_launch(free_overlap_for_rows(a.M), layer_norm_kernel<TX, TY, NV, VEC, MINB, MAXW>, dim3((unsigned)grid), dim3(threads), 0, s, a);
+    return free_launch(free_overlap_for_rows(a.M), layer_norm_kernel<TX, TY, NH, VEC, FULL, MAXT, MINB, MAXW>, dim3((unsigned)grid), dim3(threads),
+                       0, s, a);
 }
 
-// As many blocks per warp as the row needs (registers decide how many rows an SM holds); several warps beyond 2048 columns.
+// As many blocks of 128 columns per warp as the row needs (registers decide how many rows an SM holds); several warps beyond 2048
+// columns.  Widths that the blocks fill exactly have kernels without checks (24 x 1024 rows of 1152: 29.5 us, with checks 34).
 template <typename TX, typename TY, bool VEC>
 int launch_fwd(const NormArgs& a, cudaStream_t s) {
-    if (a.D <= 512) return start_fwd<TX, TY, 2, VEC, 3, 1>(a, 1, s);
-    if (a.D <= 768) return start_fwd<TX, TY, 3, VEC, 4, 1>(a, 1, s);
-    if (a.D <= 1280) return start_fwd<TX, TY, 5, VEC, 3, 1>(a, 1, s);
-    if (a.D <= 2048) return start_fwd<TX, TY, 8, VEC, 2, 1>(a, 1, s);
-    return start_fwd<TX, TY, kWide, VEC, 3, (kMaxD + 256 * kWide - 1) / (256 * kWide)>(a, (a.D + 256 * kWide - 1) / (256 * kWide), s);
+    if constexpr (VEC) {
+        const int n = a.D % 128 == 0 ? a.D / 128 : 0;
+        switch (n) {
+            case 2: return start_fwd<TX, TY, 2, true, true, 128, 8, 1>(a, 1, s);
+            case 3: return start_fwd<TX, TY, 3, true, true, 128, 7, 1>(a, 1, s);
+            case 4: return start_fwd<TX, TY, 4, true, true, 128, 6, 1>(a, 1, s);
+            case 5: return start_fwd<TX, TY, 5, true, true, 128, 5, 1>(a, 1, s);
+            case 6: return start_fwd<TX, TY, 6, true, true, 128, 4, 1>(a, 1, s);
+            case 8: return start_fwd<TX, TY, 8, true, true, 128, 4, 1>(a, 1, s);
+            case 9: return start_fwd<TX, TY, 9, true, true, 128, 3, 1>(a, 1, s);
+            case 10: return start_fwd<TX, TY, 10, true, true, 128, 3, 1>(a, 1, s);
+            case 12: return start_fwd<TX, TY, 12, true, true, 128, 3, 1>(a, 1, s);
+            case 16: return start_fwd<TX, TY, 16, true, true, 128, 2, 1>(a, 1, s);
+            default: break;
+        }
+        if (n > 16 && n % 9 == 0) return start_fwd<TX, TY, 9, true, true, 256, 2, 8>(a, n / 9, s);
+        if (n > 16 && n % 8 == 0) return start_fwd<TX, TY, 8, true, true, 256, 2, 8>(a, n / 8, s);
+    }
+    if (a.D <= 512) return start_fwd<TX, TY, 4, VEC, false, 128, 6, 1>(a, 1, s);
+    if (a.D <= 768) return start_fwd<TX, TY, 6, VEC, false, 128, 5, 1>(a, 1, s);
+    if (a.D <= 1280) return start_fwd<TX, TY, 10, VEC, false, 128, 4, 1>(a, 1, s);
+    if (a.D <= 2048) return start_fwd<TX, TY, 16, VEC, false, 128, 2, 1>(a, 1, s);
+    constexpr int per = 1280;
+    return start_fwd<TX, TY, 10, VEC, false, 256, 2, (kMaxD + per - 1) / per>(a, (a.D + per - 1) / per, s);
 }
 
 template <typename TX, typename TY, bool VEC, int MAXT, int T, int R>
@@ -459,7 +511,7 @@ int launch_bwd(NormArgs a, cudaStream_t s) {
     const int threads = bwd_threads(a.D);
     a.warps = threads / 32;
     // wide rows leave an SM one CTA: two rows per barrier where shared memory holds them
-    const int r = threads <= 256 ? start_bwd<TX, TY, VEC, 256, VEC ? kBwdT : kBwdScalarT, 1>(a, threads, s)
+    const int r = threads <= 256 ? start_bwd<TX, TY, VEC, 256, VEC ? kBwdT : kBwdScalarT, VEC ? 1 : 2>(a, threads, s)
                 : threads <= 576 ? start_bwd<TX, TY, VEC, 576, 576, 2>(a, threads, s) : start_bwd<TX, TY, VEC, 1024, 1024, 1>(a, threads, s);
     if (r != FREE_OK || a.chunks == 1 || (!a.dw && !a.db)) return r;
     return free_launch(free_launch_overlap_enabled(), layer_norm_reduce_kernel, dim3((unsigned)a.groups * ((2u * a.D + 31) / 32)), dim3(512), 0, s, a);
@@ -489,10 +541,9 @@ extern "C" int free_op_layer_norm(int x_dtype, int y_dtype, int n_groups, int ro
     NormArgs a{};
     a.M = M; a.D = D; a.groups = n_groups; a.rows_per_group = rows_per_group;
     a.x = x; a.x_stride = x_stride; a.weight = weight; a.bias = bias; a.mod_stride = mod_stride; a.unit = unit_offset ? 1.f : 0.f;
-    a.table_vec = tables_vec(weight, bias, n_groups, mod_stride);
     a.eps = eps; a.y = y; a.y_stride = y_stride; a.stats = stats;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    const bool vec = D % 4 == 0 && row_vec(x, x_stride) && row_vec(y, y_stride);
+    const bool vec = D % 4 == 0 && row_vec(x, x_stride) && row_vec(y, y_stride) && tables_vec(weight, bias, n_groups, mod_stride);
     const int which = (x_dtype == FREE_BF16 ? 4 : 0) + (y_dtype == FREE_BF16 ? 2 : 0) + (vec ? 1 : 0);
     using bf = __nv_bfloat16;
     switch (which) {
@@ -537,12 +588,11 @@ extern "C" int free_op_layer_norm_bwd(int x_dtype, int y_dtype, int n_groups, in
     NormArgs a{};
     a.M = M; a.D = D; a.groups = n_groups; a.rows_per_group = rows_per_group;
     a.x = x; a.x_stride = x_stride; a.weight = weight; a.mod_stride = mod_stride; a.unit = unit_offset ? 1.f : 0.f;
-    a.table_vec = tables_vec(weight, nullptr, n_groups, mod_stride);
     a.dy = dy; a.dy_stride = dy_stride; a.stats_in = stats; a.dres = dres; a.dres_stride = dres_stride; a.dx = dx; a.dx_stride = dx_stride;
     a.dw = dweight; a.db = dbias; a.dmod_stride = dmod_stride; a.partial = (float*)ws; a.chunks = chunks;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     const bool vec = D % 4 == 0 && row_vec(x, x_stride) && row_vec(dy, dy_stride) && row_vec(dres, dres_stride) &&
-                     row_vec(dx, dx_stride);
+                     row_vec(dx, dx_stride) && tables_vec(weight, nullptr, n_groups, mod_stride);
     const int which = (x_dtype == FREE_BF16 ? 4 : 0) + (y_dtype == FREE_BF16 ? 2 : 0) + (vec ? 1 : 0);
     using bf = __nv_bfloat16;
     switch (which) {

@@ -171,20 +171,27 @@ def test_rows_far_apart():
 
 
 def test_unaligned_tables_and_gradients_over_their_inputs():
+    # tables whose rows start at any element take the scalar form: another order of the same sums
     import paper_2511_20390_b200 as free
     for D in (1152, 384, 2304, 513):
-        x, _ = _mat(14, 1, 30, D, "fp32")
-        dy, _ = _mat(14, 2, 30, D, "fp32")
+        x, xf = _mat(14, 1, 30, D, "fp32")
+        dy, dyf = _mat(14, 2, 30, D, "fp32")
         table = torch.from_numpy(synth.normal(14, 3, (3, 2 * D + 3))).cuda()
-        w, b = table[:, 1:D + 1], table[:, D + 2:2 * D + 2]        # rows that start at any element
+        w, b = table[:, 1:D + 1], table[:, D + 2:2 * D + 2]
         y, st = free.op_layer_norm(x, w, b, rows_per_group=10, want_stats=True)
-        assert torch.equal(y, free.op_layer_norm(x, w.contiguous(), b.contiguous(), rows_per_group=10))
-        ref = free.op_layer_norm_bwd(x, dy, st, w.contiguous(), rows_per_group=10)
-        for over in (x, dy):
-            a, g = x.clone(), dy.clone()
-            dst = a if over is x else g
-            got = free.op_layer_norm_bwd(a, g, st, w, rows_per_group=10, dx=dst)
-            assert torch.equal(dst, ref[0]) and torch.equal(got[1], ref[1]) and torch.equal(got[2], ref[2])
+        wf, bf = w.double().cpu().numpy(), b.double().cpu().numpy()
+        yo, so = ob.layer_norm(xf, wf, bf, 10)
+        assert (np.abs(y.double().cpu().numpy() - yo) <= _fwd_tol(xf, so, _per_row(wf, 10), _per_row(bf, 10), yo, "fp32")).all()
+        for tab in (w, w.contiguous()):
+            ref = free.op_layer_norm_bwd(x, dy, st, tab, rows_per_group=10)
+            dwo = ob.layer_norm_bwd(xf, dyf, st.double().cpu().numpy(), wf, 10)[1]
+            xh = np.abs(xf - st[:, :1].double().cpu().numpy()) * st[:, 1:].double().cpu().numpy()
+            assert (np.abs(ref[1].double().cpu().numpy() - dwo) <= 34 * U * (np.abs(dyf) * xh).reshape(3, 10, D).sum(1)).all()
+            for over in (x, dy):                                   # dx written over one of its inputs: the same bits
+                a, g = x.clone(), dy.clone()
+                dst = a if over is x else g
+                got = free.op_layer_norm_bwd(a, g, st, tab, rows_per_group=10, dx=dst)
+                assert torch.equal(dst, ref[0]) and torch.equal(got[1], ref[1]) and torch.equal(got[2], ref[2])
 
 
 def test_a_constant_row_and_a_tiny_variance():
