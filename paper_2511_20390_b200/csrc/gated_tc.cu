@@ -340,7 +340,7 @@ GatedSplit choose_split(long long rows, int K, int nk) {
     double best = 0;
     for (int half = 128; half >= 64; half -= 64) {
         const long long tiles = (rows + 255) / 256 * ((K + 2 * half - 1) / (2 * half));
-        for (int s = 1; s <= 32 && s <= nk; ++s) {
+        for (int s = 1; s <= 32 && s <= nk && (s == 1 || tiles * (s - 1) < 4 * kPairs); ++s) {     // beyond four waves: nothing to gain
             const long long waves = (tiles * s + kPairs - 1) / kPairs;
             const double cost = (double)waves * ((half == 64 ? 0.73 : 1.0) * ((nk + s - 1) / s) + 6.0) +
                                 (s > 1 ? 10.0 + (double)s * (double)rows * K * 8.0 / 2.0e6 : 0.0);

@@ -48,7 +48,7 @@ def _fwd_tol(x, stats, w_rows, b_rows, y, out):
 SHAPES = [  # groups, rows per group, D, extra elements between rows of x
     (1, 1, 1, 0), (1, 5, 2, 0), (1, 9, 8, 0), (3, 7, 40, 8), (2, 130, 256, 0), (4, 33, 384, 0), (1, 17, 511, 3), (1, 40, 512, 0),
     (1, 19, 513, 0), (3, 5, 520, 0), (2, 50, 1001, 0), (6, 41, 1152, 0), (1, 600, 1152, 40), (300, 1, 1152, 0), (700, 1, 72, 0),
-    (1, 6, 2048, 0), (1, 7, 2056, 0), (2, 3, 4608, 0), (1, 3, 8191, 0), (1, 2, 8192, 0), (1, 3000, 24, 0),
+    (1, 6, 2048, 0), (1, 7, 2056, 0), (2, 50, 870, 0), (1, 33, 1154, 2), (1, 9, 4602, 0), (2, 20, 384, 2), (1, 20, 384, 1), (1, 10, 2304, 2), (1, 300, 6, 0), (2, 3, 4608, 0), (1, 3, 8191, 0), (1, 2, 8192, 0), (1, 3000, 24, 0),
 ]
 
 
