@@ -480,7 +480,8 @@ int free_op_ln_modulate(int out_dtype, int M, int D, int rows_per_seq, const flo
  *     dz = [dh z_up act'(z_gate), dh act(z_gate)],   dx = dz W,   dw = dz^T x,   dbias = sum over rows of dz
  *   dh         DEVICE `dtype` [M, F]
  *   dx, dw     DEVICE `dtype` [M, K], [2F, K];  dbias  DEVICE fp32 [2F].  Each may be NULL (w is read for dx only, x for dw
- *              only) and is overwritten; with M = 0 dw and dbias become zero.  In bf16 dz is rounded to bf16 for the products
+ *              only) and is overwritten; with M = 0 dw and dbias become zero.  In bf16 dz is rounded to bf16 for the products.
+ *              They must not overlap the inputs, the workspace or one another
  *   ws         DEVICE, >= free_op_gated_linear_bwd_workspace_bytes() (HOST-only): dz and the parts of split sums.  Calls that
  *              may overlap on the GPU need one each
  *   other arguments and errors as above, and WORKSPACE.  Repeats are bit-identical.

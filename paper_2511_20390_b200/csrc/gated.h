@@ -32,15 +32,13 @@ struct GatedSplit {
     int half;                    // tensor cores: columns of a tile per CTA of a pair (128 or 64)
 };
 
-// out[i] = sum over parts of parts[p * plane + i], i < n, in the order of the parts; out in `dtype`
-int gated_add_parts(int dtype, int parts, long long plane, long long n, const float* src, void* out, cudaStream_t s);
-
 // ---- bf16 (tcgen05): F % 8 == 0, K % 8 == 0 ------------------------------------------------------
 bool gated_tc_supported(int F, int K);
 int gated_tc_forward(int act, int M, int F, int K, const void* x, const void* w, const float* bias, void* h, void* preact, uint32_t* err, cudaStream_t s);
 GatedSplit gated_tc_split(bool dw, int M, int F, int K);
-// dw false: out [M, K] = dz W; true: out [2F, K] = dz^T x.  parts: workspace of gated_tc_split() (unused when it is 1)
-int gated_tc_backward(bool dw, int M, int F, int K, const void* x, const void* w, const void* dz, void* out, float* parts, uint32_t* err, cudaStream_t s);
+// dw false: out [M, K] = dz W; true: out [2F, K] = dz^T x.  g: of gated_tc_split(); with several parts they go to `parts`,
+// plane_rows * K elements apart, and `out` is not written
+int gated_tc_backward(bool dw, const GatedSplit& g, int M, int F, int K, const void* x, const void* w, const void* dz, void* out, float* parts, uint32_t* err, cudaStream_t s);
 
 // ---- few rows (CUDA cores, both types); bf16: K % 8 == 0 -----------------------------------------
 bool gated_rows_wanted(int dtype, int M);
@@ -49,4 +47,4 @@ int gated_rows_forward(int dtype, int act, int M, int F, int K, const void* x, c
 // ---- fp32 (CUDA cores), any sizes ----------------------------------------------------------------
 int gated_simt_forward(int act, int M, int F, int K, const float* x, const float* w, const float* bias, float* h, float* preact, cudaStream_t s);
 GatedSplit gated_simt_split(bool dw, int M, int F, int K);
-int gated_simt_backward(bool dw, int M, int F, int K, const float* x, const float* w, const float* dz, float* out, float* parts, cudaStream_t s);
+int gated_simt_backward(bool dw, const GatedSplit& g, int M, int F, int K, const float* x, const float* w, const float* dz, float* out, float* parts, cudaStream_t s);

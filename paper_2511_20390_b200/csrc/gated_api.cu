@@ -1,4 +1,4 @@
-// Gated linear layer: the elementwise part of its backward pass, sums of split products, and the entry points.
+// Gated linear layer: the elementwise part of its backward pass, the sums that end it, and the entry points.
 //
 //   forward    z = x W^T + b;  h = act(z_gate) z_up                                      (one kernel)
 //   backward   dz_gate = dh z_up act'(z_gate),  dz_up = dh act(z_gate),  db = sum_rows dz  (one pass over z and dh)
@@ -91,43 +91,67 @@ __global__ void __launch_bounds__(kMaxThreads, kPerSm) gated_grad_kernel(int M, 
     }
 }
 
-// out[c] = sum of rows [n][cols]: 32 columns x 16 slices per CTA, slices joined in order
-__global__ void __launch_bounds__(512) gated_bias_kernel(int n, int cols, const float* p, float* out) {
-    __shared__ float sh[16][33];
-    free_grid_dep_wait();
-    free_grid_dep_launch();
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    const int c = blockIdx.x * 32 + tx;
-    float s = 0.f;
-    if (c < cols) {
-#pragma unroll 8
-        for (int k = ty; k < n; k += 16) s += p[(long long)k * cols + c];
-    }
-    sh[ty][tx] = s;
-    __syncthreads();
-    if (ty == 0 && c < cols) {
-        float t = 0.f;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) t += sh[k][tx];
-        out[c] = t;
-    }
-}
-
+// What is left once the products are done, in one launch: the parts of dx and of dw added in their order and rounded, and the
+// partial rows of db added (32 columns x 8 slices of the rows per CTA, slices joined in order).
+// Launched plainly: brought up early, as the kernels before it are, its blocks wait beside the product and the whole pass takes
+// longer (300 rows, F = 4608: 40 us against 35; 8192 rows, F = 1024: 64 against 58).  Two sums of a thread are in flight: one is 3 us slower where there are many,
+// four 13 us slower where there are few and many parts (20000 rows, F = 256).
+constexpr int kSums = 2;
+template <typename T> struct Sum { const float* src; T* out; long long n, plane; int parts, blocks; };
+template <typename T> struct FinishArgs {
+    Sum<T> dx, dw;
+    const float* db; float* dbias; int chunks, cols, db_blocks;
+};
 template <typename T, int V>
-__global__ void __launch_bounds__(256) gated_add_kernel(int parts, long long plane, long long n, const float* src, T* out) {
+__global__ void __launch_bounds__(256) gated_finish_kernel(const FinishArgs<T> a) {
     free_grid_dep_wait();
     free_grid_dep_launch();
-    for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * V; i < n; i += (long long)gridDim.x * 256 * V) {
-        Pack<float, V> s = *reinterpret_cast<const Pack<float, V>*>(src + i);
-        for (int p = 1; p < parts; ++p) {
-            const Pack<float, V> t = *reinterpret_cast<const Pack<float, V>*>(src + p * plane + i);
-#pragma unroll
-            for (int e = 0; e < V; ++e) s.v[e] += t.v[e];
+    int block = blockIdx.x;
+    if (block < a.db_blocks) {                  // first: these are the longest
+        __shared__ float sh[8][33];
+        const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+        const int c = block * 32 + tx;
+        float s = 0.f;
+        if (c < a.cols) {
+#pragma unroll 8
+            for (int k = ty; k < a.chunks; k += 8) s += a.db[(long long)k * a.cols + c];
         }
-        Pack<T, V> o;
+        sh[ty][tx] = s;
+        __syncthreads();
+        if (ty == 0 && c < a.cols) {
+            float t = 0.f;
 #pragma unroll
-        for (int e = 0; e < V; ++e) from_f(o.v[e], s.v[e]);
-        *reinterpret_cast<Pack<T, V>*>(out + i) = o;
+            for (int k = 0; k < 8; ++k) t += sh[k][tx];
+            a.dbias[c] = t;
+        }
+        return;
+    }
+    block -= a.db_blocks;
+    const Sum<T> j = block < a.dx.blocks ? a.dx : a.dw;
+    if (block >= a.dx.blocks) block -= a.dx.blocks;
+    for (long long i = ((long long)block * kSums * 256 + threadIdx.x) * V; i < j.n; i += (long long)j.blocks * kSums * 256 * V) {
+        Pack<float, V> s[kSums];
+#pragma unroll
+        for (int u = 0; u < kSums; ++u)
+            if (i + u * 256 * V < j.n) s[u] = *reinterpret_cast<const Pack<float, V>*>(j.src + i + u * 256 * V);
+#pragma unroll 2
+        for (int p = 1; p < j.parts; ++p) {
+#pragma unroll
+            for (int u = 0; u < kSums; ++u) {
+                if (i + u * 256 * V >= j.n) break;
+                const Pack<float, V> t = *reinterpret_cast<const Pack<float, V>*>(j.src + p * j.plane + i + u * 256 * V);
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[u].v[e] += t.v[e];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kSums; ++u) {
+            if (i + u * 256 * V >= j.n) break;
+            Pack<T, V> o;
+#pragma unroll
+            for (int e = 0; e < V; ++e) from_f(o.v[e], s[u].v[e]);
+            *reinterpret_cast<Pack<T, V>*>(j.out + i + u * 256 * V) = o;
+        }
     }
 }
 
@@ -150,24 +174,43 @@ GradGrid grad_grid(int dtype, int M, int F) {
     if (g.chunks < 1) g.chunks = 1;
     return g;
 }
-int chunks_of(int dtype, int M, int F) { return grad_grid(dtype, M, F).chunks; }
 
-struct Layout { size_t dz, db, parts, total; };
+// Workspace: dz, the partial rows of db, the parts of dx, the parts of dw.
+struct Layout { size_t dz, db, dx, dw, total; int chunks; GatedSplit gx, gw; };
 Layout layout_of(int dtype, int M, int F, int K) {
     Layout l{};
     const size_t e = dtype == FREE_BF16 ? 2 : 4;
+    l.chunks = grad_grid(dtype, M, F).chunks;
+    l.gx = dtype == FREE_BF16 ? gated_tc_split(false, M, F, K) : gated_simt_split(false, M, F, K);
+    l.gw = dtype == FREE_BF16 ? gated_tc_split(true, M, F, K) : gated_simt_split(true, M, F, K);
+    auto parts = [&](const GatedSplit& g) { return g.parts > 1 ? free_round_up((size_t)g.parts * g.plane_rows * K * 4, 256) : 0; };
     l.dz = 0;
     l.db = free_round_up((size_t)M * 2 * F * e, 256);
-    const int c = chunks_of(dtype, M, F);
-    l.parts = l.db + (c > 1 ? free_round_up((size_t)c * 2 * F * 4, 256) : 0);
-    size_t most = 0;                        // both products use the same part: they run one after the other
-    for (int dw = 0; dw < 2; ++dw) {
-        const GatedSplit g = dtype == FREE_BF16 ? gated_tc_split(dw != 0, M, F, K) : gated_simt_split(dw != 0, M, F, K);
-        const size_t b = g.parts > 1 ? (size_t)g.parts * g.plane_rows * K * 4 : 0;
-        if (b > most) most = b;
-    }
-    l.total = l.parts + most;
+    l.dx = l.db + (l.chunks > 1 ? free_round_up((size_t)l.chunks * 2 * F * 4, 256) : 0);
+    l.dw = l.dx + parts(l.gx);
+    l.total = l.dw + parts(l.gw);
     return l;
+}
+
+template <typename T, int V>
+Sum<T> sum_of(const GatedSplit& g, long long rows, int K, const float* src, void* out) {
+    Sum<T> j{src, (T*)out, rows * K, g.plane_rows * K, g.parts, 0};
+    if (!out || g.parts == 1) return j;
+    const long long want = (j.n / V + kSums * 256 - 1) / (kSums * 256);
+    j.blocks = (int)(want > kSms * 16 ? kSms * 16 : want);
+    return j;
+}
+
+template <typename T, int V>
+int finish(const Layout& l, int M, int F, int K, char* base, void* dx, void* dw, float* dbias, cudaStream_t s) {
+    FinishArgs<T> a{};
+    a.dx = sum_of<T, V>(l.gx, M, K, (const float*)(base + l.dx), dx);
+    a.dw = sum_of<T, V>(l.gw, 2LL * F, K, (const float*)(base + l.dw), dw);
+    a.db = (const float*)(base + l.db); a.dbias = dbias; a.chunks = l.chunks; a.cols = 2 * F;
+    a.db_blocks = dbias && l.chunks > 1 ? (a.cols + 31) / 32 : 0;
+    const long long grid = (long long)a.dx.blocks + a.dw.blocks + a.db_blocks;
+    if (grid == 0) return FREE_OK;
+    return free_launch(false, gated_finish_kernel<T, V>, dim3((unsigned)grid), dim3(256), 0, s, a);
 }
 
 // Sizes whose tile counts and coordinates fit 32 bits.
@@ -185,17 +228,6 @@ int grad(int dtype, int act, int M, int F, const void* pre, const void* dh, void
 }
 
 }  // namespace
-
-int gated_add_parts(int dtype, int parts, long long plane, long long n, const float* src, void* out, cudaStream_t s) {
-    const bool vec = n % 4 == 0 && plane % 4 == 0;
-    const long long want = (n / (vec ? 4 : 1) + 255) / 256;
-    const dim3 grid((unsigned)(want > kSms * 16 ? kSms * 16 : want));
-    const bool ov = free_launch_overlap_enabled();
-    if (dtype == FREE_BF16)                 // n and plane are multiples of K, a multiple of 8
-        return free_launch(ov, gated_add_kernel<__nv_bfloat16, 4>, grid, dim3(256), 0, s, parts, plane, n, src, (__nv_bfloat16*)out);
-    if (vec) return free_launch(ov, gated_add_kernel<float, 4>, grid, dim3(256), 0, s, parts, plane, n, src, (float*)out);
-    return free_launch(ov, gated_add_kernel<float, 1>, grid, dim3(256), 0, s, parts, plane, n, src, (float*)out);
-}
 
 extern "C" int free_op_gated_linear(int dtype, int act, int M, int F, int K, const void* x, const void* w, const float* bias,
                                     void* h, void* preact, uint32_t* device_error, void* stream) {
@@ -241,21 +273,19 @@ extern "C" int free_op_gated_linear_bwd(int dtype, int act, int M, int F, int K,
     if (!ws || ws_bytes < l.total) return FREE_ERR_WORKSPACE;
     char* base = (char*)ws;
     void* dz = dx || dw ? base + l.dz : nullptr;
-    float* parts = (float*)(base + l.parts);
-    const int chunks = chunks_of(dtype, M, F);
-    float* db = !dbias ? nullptr : (chunks > 1 ? (float*)(base + l.db) : dbias);
-    if (dtype == FREE_BF16) FREE_TRY((grad<__nv_bfloat16, 8>(dtype, act, M, F, preact, dh, dz, db, s)));
-    else if (vec_of(dtype, F) == 4) FREE_TRY((grad<float, 4>(dtype, act, M, F, preact, dh, dz, db, s)));
-    else FREE_TRY((grad<float, 1>(dtype, act, M, F, preact, dh, dz, db, s)));
-    if (dbias && chunks > 1)
-        FREE_TRY(free_launch(free_launch_overlap_enabled(), gated_bias_kernel, dim3((2u * F + 31) / 32), dim3(512), 0, s, chunks, 2 * F, (const float*)db, dbias));
+    float* db = !dbias ? nullptr : (l.chunks > 1 ? (float*)(base + l.db) : dbias);
+    float *px = (float*)(base + l.dx), *pw = (float*)(base + l.dw);
     if (dtype == FREE_BF16) {
+        FREE_TRY((grad<__nv_bfloat16, 8>(dtype, act, M, F, preact, dh, dz, db, s)));
         // dx walks over dz from its end, dw then from its start: each begins with what the L2 still holds
-        if (dx) FREE_TRY(gated_tc_backward(false, M, F, K, x, w, dz, dx, parts, device_error, s));
-        if (dw) FREE_TRY(gated_tc_backward(true, M, F, K, x, w, dz, dw, parts, device_error, s));
-    } else {
-        if (dw) FREE_TRY(gated_simt_backward(true, M, F, K, (const float*)x, (const float*)w, (const float*)dz, (float*)dw, parts, s));
-        if (dx) FREE_TRY(gated_simt_backward(false, M, F, K, (const float*)x, (const float*)w, (const float*)dz, (float*)dx, parts, s));
+        if (dx) FREE_TRY(gated_tc_backward(false, l.gx, M, F, K, x, w, dz, dx, px, device_error, s));
+        if (dw) FREE_TRY(gated_tc_backward(true, l.gw, M, F, K, x, w, dz, dw, pw, device_error, s));
+        return finish<__nv_bfloat16, 4>(l, M, F, K, base, dx, dw, dbias, s);        // K % 8 == 0
     }
-    return FREE_OK;
+    const float *xf = (const float*)x, *wf = (const float*)w, *zf = (const float*)dz;
+    if (vec_of(dtype, F) == 4) FREE_TRY((grad<float, 4>(dtype, act, M, F, preact, dh, dz, db, s)));
+    else FREE_TRY((grad<float, 1>(dtype, act, M, F, preact, dh, dz, db, s)));
+    if (dw) FREE_TRY(gated_simt_backward(true, l.gw, M, F, K, xf, wf, zf, (float*)dw, pw, s));
+    if (dx) FREE_TRY(gated_simt_backward(false, l.gx, M, F, K, xf, wf, zf, (float*)dx, px, s));
+    return K % 4 == 0 ? finish<float, 4>(l, M, F, K, base, dx, dw, dbias, s) : finish<float, 1>(l, M, F, K, base, dx, dw, dbias, s);
 }

@@ -207,13 +207,11 @@ GatedSplit gated_simt_split(bool dw, int M, int F, int K) {
     return {s < 1 ? 1 : (int)s, rows, 0};
 }
 
-int gated_simt_backward(bool dw, int M, int F, int K, const float* x, const float* w, const float* dz, float* out, float* parts, cudaStream_t s) {
-    const GatedSplit g = gated_simt_split(dw, M, F, K);
+int gated_simt_backward(bool dw, const GatedSplit& g, int M, int F, int K, const float* x, const float* w, const float* dz, float* out, float* parts, cudaStream_t s) {
     Args a{};
     a.M = dw ? 2 * F : M; a.N = K; a.depth = dw ? M : 2 * F; a.F = F;
     a.A = dz; a.lda = 2LL * F; a.B = dw ? x : w; a.ldb = K;
     a.parts = g.parts; a.plane = g.plane_rows * K; a.out = g.parts > 1 ? parts : out;
     const bool vec = K % 4 == 0 && F % 2 == 0;
-    FREE_TRY(dw ? launch<DW>(a, vec, s) : launch<DX>(a, vec, s));
-    return g.parts > 1 ? gated_add_parts(FREE_FP32, g.parts, a.plane, (long long)a.M * K, parts, out, s) : FREE_OK;
+    return dw ? launch<DW>(a, vec, s) : launch<DX>(a, vec, s);
 }

@@ -381,8 +381,7 @@ GatedSplit gated_tc_split(bool dw, int M, int F, int K) {
     return choose_split(dw ? 2LL * F : M, K, ((dw ? M : 2 * F) + BK - 1) / BK);
 }
 
-int gated_tc_backward(bool dw, int M, int F, int K, const void* x, const void* w, const void* dz, void* out, float* parts, uint32_t* err, cudaStream_t s) {
-    const GatedSplit g = gated_tc_split(dw, M, F, K);
+int gated_tc_backward(bool dw, const GatedSplit& g, int M, int F, int K, const void* x, const void* w, const void* dz, void* out, float* parts, uint32_t* err, cudaStream_t s) {
     Args a{};
     a.M = dw ? 2 * F : M; a.N = K; a.F = F; a.err = err;
     a.half = g.half;
@@ -400,8 +399,7 @@ int gated_tc_backward(bool dw, int M, int F, int K, const void* x, const void* w
     }
     if (g.parts > 1) {
         FREE_TRY(free_tensor_map_2d_typed(&mO, 4, parts, (uint64_t)K, (uint64_t)(g.parts * g.plane_rows), (uint64_t)K * 4, 32, 32, 128));
-        FREE_TRY(dw ? (launch<DW, true, false>(mA, mB, mO, mO, mO, a, M, s)) : (launch<DX, true, false>(mA, mB, mO, mO, mO, a, M, s)));
-        return gated_add_parts(FREE_BF16, g.parts, g.plane_rows * K, (long long)a.M * K, parts, out, s);
+        return dw ? launch<DW, true, false>(mA, mB, mO, mO, mO, a, M, s) : launch<DX, true, false>(mA, mB, mO, mO, mO, a, M, s);
     }
     FREE_TRY(free_tensor_map_2d(&mO, out, (uint64_t)K, (uint64_t)a.M, (uint64_t)K * 2, 64, 32, 128));
     return dw ? launch<DW, false, false>(mA, mB, mO, mO, mO, a, M, s) : launch<DX, false, false>(mA, mB, mO, mO, mO, a, M, s);
