@@ -23,6 +23,7 @@ namespace {
 constexpr int kMaxWarps = 32;
 constexpr int kMaxD = kMaxWarps * 256;
 constexpr int kSms = 148;
+constexpr int kNarrowPerSm = 4, kNarrowBwdPerSm = 2;   // CTAs of the kernels for narrow rows on an SM
 
 // ---- VW consecutive columns: 4 (rows aligned to four elements, D % 4 == 0), 2, or 1 (any D, any row stride) ------------------
 __device__ __forceinline__ float to_f(float v) { return v; }
@@ -390,6 +391,186 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
         }
 }
 
+// ---- narrow rows (norms over a head; up to 256 columns) ---------------------------------------------------------------------
+// L lanes hold a row, C columns each, and a warp 32 / L rows at a time: fewer exchanges per row and no idle lanes.  393216 rows of
+// 64, bf16: forward 22.5 us (a warp per row 160), backward 37 (139); 65536 rows of 192: 15 (19) and 26 (43).  Fewer columns per
+// lane are slower (forward 29, four instead of eight), but for single columns (65536 rows of 127: 15 against 17, backward 27
+// against 51).
+template <int VW> constexpr int kNarrowCols = VW == 1 ? 4 : 8;     // C, for rows of 33 to 128 columns
+template <int L> __device__ __forceinline__ float part_sum(float v) {
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    return v;
+}
+template <int L, int C, int VW> struct NarrowCols {
+    int D, lane;
+    __device__ __forceinline__ int at(int piece) const { return (piece * L + lane) * VW; }
+    __device__ __forceinline__ bool in(int piece) const { return at(piece) < D; }
+};
+
+// A warp takes rows_per_team consecutive rows, its parts neighbouring ones.  The tables stay in registers until the group changes.
+template <typename TX, typename TY, int L, int C, int VW>
+__global__ void __launch_bounds__(256, kNarrowPerSm) layer_norm_narrow_kernel(const NormArgs a) {
+    constexpr int P = C / VW, XW = kWords<TX, VW>, R = 32 / L;
+    free_grid_dep_wait();
+    free_grid_dep_launch();
+    const NarrowCols<L, C, VW> c{a.D, (int)(threadIdx.x % L)};
+    const TX* x = reinterpret_cast<const TX*>(a.x);
+    TY* y = reinterpret_cast<TY*>(a.y);
+    const long long first = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * a.rows_per_team;
+    const long long last = first + a.rows_per_team < a.M ? first + a.rows_per_team : a.M;
+    const float inv_d = 1.f / (float)a.D;
+    long long row = first + (threadIdx.x & 31) / L;
+    uint32_t nx[P][XW];
+    auto fetch = [&](long long r) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) load<TX, VW>(x + r * a.x_stride + c.at(p), r < last && c.in(p), nx[p]);
+    };
+    const bool tables = a.weight || a.bias;
+    const long long g0 = !tables ? 0 : first <= 0xffffffffLL ? (long long)((uint32_t)first / (uint32_t)a.rows_per_group) : first / a.rows_per_group;
+    long long group_end = tables ? g0 * a.rows_per_group : a.M, mo = g0 * a.mod_stride, step = 0;
+    fetch(row);
+    float w[P][VW], b[P][VW];
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int e = 0; e < VW; ++e) { w[p][e] = 1.f; b[p][e] = 0.f; }
+    for (long long base = first; base < last; base += R, row += R) {
+        const bool live = row < last;                              // all lanes take part in the exchanges
+        if (live && row >= group_end) {
+            do {
+                mo += step;
+                step = a.mod_stride;
+                group_end += a.rows_per_group;
+            } while (row >= group_end);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                if (a.weight) table<VW>(a.weight + mo + c.at(p), c.in(p), a.unit, w[p]);
+                if (a.bias) table<VW>(a.bias + mo + c.at(p), c.in(p), 0.f, b[p]);
+            }
+        }
+        float v[P][VW], s = 0.f, q = 0.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int e = 0; e < VW; ++e) { v[p][e] = value<TX, VW>(nx[p], e); s += v[p][e]; }
+        fetch(row + R);
+        const float mu = part_sum<L>(s) * inv_d;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int e = 0; e < VW; ++e) { v[p][e] -= mu; q += c.in(p) ? v[p][e] * v[p][e] : 0.f; }
+        const float rstd = rsqrtf(part_sum<L>(q) * inv_d + a.eps);
+        if (live) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                float o[VW];
+#pragma unroll
+                for (int e = 0; e < VW; ++e) o[e] = v[p][e] * rstd * w[p][e] + b[p][e];
+                if (c.in(p)) store<VW>(y + row * a.y_stride + c.at(p), o);
+            }
+            if (a.stats && c.lane == 0) { a.stats[2 * row] = mu; a.stats[2 * row + 1] = rstd; }
+        }
+    }
+}
+
+// One CTA per (group, chunk) as for wide rows; its warps take the run's rows in turn and their column sums are added at the end.
+template <typename TX, typename TY, int L, int C, int VW>
+__global__ void __launch_bounds__(256, kNarrowBwdPerSm) layer_norm_narrow_bwd_kernel(const NormArgs a) {
+    constexpr int P = C / VW, XW = kWords<TX, VW>, YW = kWords<TY, VW>, R = 32 / L, N = L * C;
+    __shared__ float sums[8][2][N];
+    free_grid_dep_wait();
+    free_grid_dep_launch();
+    const int warp = threadIdx.x >> 5, W = blockDim.x >> 5;
+    const NarrowCols<L, C, VW> c{a.D, (int)(threadIdx.x % L)};
+    const TX* x = reinterpret_cast<const TX*>(a.x);
+    const TY* dy = reinterpret_cast<const TY*>(a.dy);
+    const TX* dres = reinterpret_cast<const TX*>(a.dres);
+    TX* dx = reinterpret_cast<TX*>(a.dx);
+    const int g = blockIdx.x / a.chunks, ch = blockIdx.x % a.chunks;
+    const long long base = (long long)g * a.rows_per_group;
+    const long long lo = base + (long long)a.rows_per_group * ch / a.chunks, hi = base + (long long)a.rows_per_group * (ch + 1) / a.chunks;
+    const float inv_d = 1.f / (float)a.D;
+    uint32_t nx[P][XW], ny[P][YW], nr[P][XW];
+    float2 ns;
+    auto fetch = [&](long long r) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const bool ok = r < hi && c.in(p);
+            load<TX, VW>(x + r * a.x_stride + c.at(p), ok, nx[p]);
+            load<TY, VW>(dy + r * a.dy_stride + c.at(p), ok, ny[p]);
+            load<TX, VW>(dres + r * a.dres_stride + c.at(p), ok && dres, nr[p]);
+        }
+        ns = r < hi ? make_float2(__ldg(a.stats_in + 2 * r), __ldg(a.stats_in + 2 * r + 1)) : make_float2(0.f, 0.f);
+    };
+    long long row = lo + warp * R + (threadIdx.x & 31) / L;
+    fetch(row);
+    float w[P][VW], dw[P][VW], db[P][VW];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+#pragma unroll
+        for (int e = 0; e < VW; ++e) { w[p][e] = 1.f; dw[p][e] = 0.f; db[p][e] = 0.f; }
+        if (a.weight) table<VW>(a.weight + (long long)g * a.mod_stride + c.at(p), c.in(p), a.unit, w[p]);
+    }
+    for (long long first = lo + warp * R; first < hi; first += W * R, row += W * R) {
+        const bool live = row < hi;
+        const float2 st = ns;
+        float xh[P][VW], v[P][VW], s1 = 0.f, s2 = 0.f;
+        uint32_t res[P][XW];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const bool in = live && c.in(p);
+#pragma unroll
+            for (int e = 0; e < VW; ++e) {
+                const float d = value<TY, VW>(ny[p], e);           // zero outside the row
+                xh[p][e] = in ? (value<TX, VW>(nx[p], e) - st.x) * st.y : 0.f;
+                v[p][e] = d * w[p][e];
+                s1 += v[p][e]; s2 = fmaf(v[p][e], xh[p][e], s2);
+                dw[p][e] = fmaf(d, xh[p][e], dw[p][e]); db[p][e] += d;
+            }
+#pragma unroll
+            for (int q = 0; q < XW; ++q) res[p][q] = nr[p][q];
+        }
+        fetch(row + W * R);
+        const float m1 = part_sum<L>(s1) * inv_d, m2 = part_sum<L>(s2) * inv_d;
+        if (live) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                float o[VW];
+#pragma unroll
+                for (int e = 0; e < VW; ++e) o[e] = fmaf(st.y, v[p][e] - m1 - xh[p][e] * m2, value<TX, VW>(res[p], e));
+                if (c.in(p)) store<VW>(dx + row * a.dx_stride + c.at(p), o);
+            }
+        }
+    }
+    if (!a.dw && !a.db) return;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int e = 0; e < VW; ++e) {
+#pragma unroll
+            for (int o = L; o < 32; o <<= 1) {
+                dw[p][e] += __shfl_xor_sync(~0u, dw[p][e], o);
+                db[p][e] += __shfl_xor_sync(~0u, db[p][e], o);
+            }
+            if ((threadIdx.x & 31) < L) { sums[warp][0][c.at(p) + e] = dw[p][e]; sums[warp][1][c.at(p) + e] = db[p][e]; }
+        }
+    __syncthreads();
+    float *ow = a.dw ? a.dw + (long long)g * a.dmod_stride : nullptr, *ob = a.db ? a.db + (long long)g * a.dmod_stride : nullptr;
+    if (a.chunks > 1) {
+        ow = a.partial + (long long)blockIdx.x * 2 * a.D;
+        ob = ow + a.D;
+    }
+    for (int i = threadIdx.x; i < 2 * N; i += blockDim.x) {
+        const int col = i % N;
+        float* out = i < N ? ow : ob;
+        if (col >= a.D || !out) continue;
+        float t = 0.f;
+        for (int k = 0; k < W; ++k) t += sums[k][i / N][col];
+        out[col] = t;
+    }
+}
+
 // dw, db of a group = the sum of its chunks' partial rows: 32 columns x 16 slices of the chunks per CTA, slices joined in order.
 __global__ void __launch_bounds__(512) layer_norm_reduce_kernel(const NormArgs a) {
     __shared__ float sh[16][33];
@@ -418,14 +599,24 @@ __global__ void __launch_bounds__(512) layer_norm_reduce_kernel(const NormArgs a
 constexpr int kBwdT = 1024, kBwdDirectT = 512;
 
 int bwd_threads(int D) { return (D + 255) / 256 * 32; }
+bool narrow(int D) { return D <= 128 || (D <= 256 && D % 2 == 0); }      // (single columns beyond 128: 32 us the wide way, 56 this)
 
-// Chunks of a group in the backward pass: one wave of CTAs, at least eight rows each.  (A function of the sizes alone: the
+// Chunks of a group in the backward pass: full waves of CTAs, at least eight rows each (64 where rows are narrow).  (A function of the sizes alone: the
 // workspace depends on it.)
 int chunks_of(int groups, int rows_per_group, int D) {
     const int t = bwd_threads(D);
-    const int per_sm = t > 256 ? 1 : (D % 2 ? kBwdDirectT : kBwdT) / t;
-    const long long want = ((long long)kSms * per_sm + groups - 1) / groups;
-    const long long most = rows_per_group / 8;
+    const int per_sm = narrow(D) ? kNarrowBwdPerSm : t > 256 ? 1 : (D % 2 ? kBwdDirectT : kBwdT) / t;
+    // the first number of waves that whole chunks fill to nine tenths, or else the best of four (one wave and a few CTAs more
+    // take two: 4200 rows of 4608 in 14 groups 83 us, so 50)
+    const long long resident = (long long)kSms * per_sm;
+    long long want = 1;
+    double best = 1e30;
+    for (int k = 1; k <= 4 && best > 1.1; ++k) {
+        const long long n = k * resident / groups;
+        const double cost = n > 0 ? (double)k * resident / ((double)n * groups) : 1e30;
+        if (cost < best) { best = cost; want = n; }
+    }
+    const long long most = rows_per_group / (narrow(D) ? 64 : 8);
     const long long c = want < most ? want : most;
     return c < 1 ? 1 : (int)c;
 }
@@ -442,10 +633,31 @@ int start_fwd(NormArgs a, int warps, cudaStream_t s) {
                        0, s, a);
 }
 
+template <typename TX, typename TY, int L, int C, int VW>
+int start_narrow(NormArgs a, cudaStream_t s) {
+    constexpr int R = 32 / L;
+    const long long resident = (long long)kSms * kNarrowPerSm * 8;
+    const long long steps = (a.M + resident * R - 1) / (resident * R);
+    a.rows_per_team = steps * R;
+    const long long grid = (a.M + a.rows_per_team * 8 - 1) / (a.rows_per_team * 8);
+    return free_launch(free_overlap_for_rows(a.M), layer_norm_narrow_kernel<TX, TY, L, C, VW>, dim3((unsigned)grid), dim3(256), 0, s, a);
+}
+template <typename TX, typename TY, int L, int C, int VW>
+int start_narrow_bwd(const NormArgs& a, cudaStream_t s) {
+    const int steps = a.rows_per_group / a.chunks / (64 / L);      // a warp takes two steps of 32 / L rows at least
+    const int warps = steps < 1 ? 1 : steps > 8 ? 8 : steps;
+    return free_launch(free_overlap_for_rows(a.M), layer_norm_narrow_bwd_kernel<TX, TY, L, C, VW>, dim3((unsigned)a.groups * (unsigned)a.chunks),
+                       dim3(warps * 32), 0, s, a);
+}
+
 // As many blocks of 128 columns per warp as the row needs (registers decide how many rows an SM holds); several warps beyond 2048
 // columns.  Widths that the blocks fill exactly have kernels without checks (24 x 1024 rows of 1152: 29.5 us, with checks 34).
 template <typename TX, typename TY, int VW>
 int launch_fwd(const NormArgs& a, cudaStream_t s) {
+    constexpr int C = kNarrowCols<VW>;
+    if (a.D <= 32) return start_narrow<TX, TY, 8, 4, VW>(a, s);
+    if (a.D <= 64) return start_narrow<TX, TY, 64 / C, C, VW>(a, s);
+    if (a.D <= 128) return start_narrow<TX, TY, 128 / C, C, VW>(a, s);
     if constexpr (VW == 4) {
         const int n = a.D % 128 == 0 ? a.D / 128 : 0;
         switch (n) {
@@ -464,6 +676,7 @@ int launch_fwd(const NormArgs& a, cudaStream_t s) {
         if (n > 16 && n % 9 == 0) return start_fwd<TX, TY, 9, 4, true, 256, 2, 8>(a, n / 9, s);
         if (n > 16 && n % 8 == 0) return start_fwd<TX, TY, 8, 4, true, 256, 2, 8>(a, n / 8, s);
     }
+    if (a.D <= 256) return start_narrow<TX, TY, 32, 8, VW>(a, s);
     if (a.D <= 512) return start_fwd<TX, TY, 4, VW, false, 128, 6, 1>(a, 1, s);
     if (a.D <= 768) return start_fwd<TX, TY, 6, VW, false, 128, VW == 4 ? 5 : 4, 1>(a, 1, s);
     if constexpr (VW == 4) {
@@ -492,7 +705,11 @@ int launch_bwd(NormArgs a, cudaStream_t s) {
     a.warps = threads / 32;
     // wide rows leave an SM one CTA: two rows per barrier where shared memory holds them
     constexpr bool AHEAD = kAhead<TX, TY, VW>;
-    const int r = threads <= 256 ? start_bwd<TX, TY, VW, 256, AHEAD ? kBwdT : kBwdDirectT, AHEAD ? 1 : 2>(a, threads, s)
+    constexpr int C = kNarrowCols<VW>;
+    const int r = a.D <= 32 ? start_narrow_bwd<TX, TY, 8, 4, VW>(a, s) : a.D <= 64 ? start_narrow_bwd<TX, TY, 64 / C, C, VW>(a, s)
+                : a.D <= 128 ? start_narrow_bwd<TX, TY, 128 / C, C, VW>(a, s)
+                : narrow(a.D) ? start_narrow_bwd<TX, TY, 32, 8, VW>(a, s)
+                : threads <= 256 ? start_bwd<TX, TY, VW, 256, AHEAD ? kBwdT : kBwdDirectT, AHEAD ? 1 : 2>(a, threads, s)
                 : threads <= 576 ? start_bwd<TX, TY, VW, 576, 576, 2>(a, threads, s) : start_bwd<TX, TY, VW, 1024, 1024, 1>(a, threads, s);
     if (r != FREE_OK || a.chunks == 1 || (!a.dw && !a.db)) return r;
     return free_launch(free_launch_overlap_enabled(), layer_norm_reduce_kernel, dim3((unsigned)a.groups * ((2u * a.D + 31) / 32)), dim3(512), 0, s, a);

@@ -97,6 +97,17 @@ def test_a_large_mean_cancels_nothing():
         assert (np.abs(y.double().cpu().numpy() - yo) <= _fwd_tol(xf, so, 1.0, 0.0, yo, "fp32")).all()
 
 
+@pytest.mark.parametrize("xd,yd", [("fp32", "bf16"), ("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32")])
+@pytest.mark.parametrize("g,rows,D,pad", [
+    (1, 1, 1, 0), (3, 1, 2, 0), (5, 2, 3, 1), (2, 37, 8, 0), (1, 130, 30, 2), (9, 7, 32, 0), (1, 517, 33, 0), (4, 129, 40, 8),
+    (1, 1000, 62, 0), (70, 3, 64, 0), (2, 700, 64, 4), (1, 640, 65, 1), (3, 200, 100, 0), (1, 20011, 64, 0), (300, 65, 96, 0),
+    (1, 2500, 110, 0), (2, 300, 126, 2), (1, 333, 127, 0), (3, 257, 128, 0), (1, 150, 129, 0), (2, 90, 200, 0), (1, 77, 255, 0),
+])
+def test_narrow_rows(g, rows, D, pad, xd, yd):
+    """Up to 128 columns several rows share a warp: groups that begin and end inside one, runs that end inside one."""
+    test_forward_and_backward(g, rows, D, pad, xd, yd)
+
+
 @pytest.mark.parametrize("D", [8, 33, 512, 1152])
 def test_defaults_shared_tables_and_missing_parts(D):
     import paper_2511_20390_b200 as free
