@@ -650,8 +650,11 @@ int start_narrow_bwd(const NormArgs& a, cudaStream_t s) {
                        dim3(warps * 32), 0, s, a);
 }
 
-// As many blocks of 128 columns per warp as the row needs (registers decide how many rows an SM holds); several warps beyond 2048
+// As many blocks of 128 columns per warp as the row needs (registers decide how many rows an SM holds), several warps beyond 2048
 // columns.  Widths that the blocks fill exactly have kernels without checks (24 x 1024 rows of 1152: 29.5 us, with checks 34).
+// With checks a warp holds up to 1280 columns (20000 rows of 1300, fp32 to bf16: 35 us by three warps, 56 by one; of 700: 25 by
+// two, 18 by one); with one or two columns per access, where the tables need registers too, 256 (20000 rows of 1001, bf16: 35 us,
+// with all in one warp 60; 690 in pairs: 19 and 15).
 template <typename TX, typename TY, int VW>
 int launch_fwd(const NormArgs& a, cudaStream_t s) {
     constexpr int C = kNarrowCols<VW>;
@@ -677,17 +680,19 @@ int launch_fwd(const NormArgs& a, cudaStream_t s) {
         if (n > 16 && n % 8 == 0) return start_fwd<TX, TY, 8, 4, true, 256, 2, 8>(a, n / 8, s);
     }
     if (a.D <= 256) return start_narrow<TX, TY, 32, 8, VW>(a, s);
-    if (a.D <= 512) return start_fwd<TX, TY, 4, VW, false, 128, 6, 1>(a, 1, s);
-    if (a.D <= 768) return start_fwd<TX, TY, 6, VW, false, 128, VW == 4 ? 5 : 4, 1>(a, 1, s);
+    if constexpr (VW > 1) {
+        if (a.D <= 512) return start_fwd<TX, TY, 4, VW, false, 128, 6, 1>(a, 1, s);
+        if (a.D <= 768) return start_fwd<TX, TY, 6, VW, false, 128, VW == 4 ? 5 : 4, 1>(a, 1, s);
+    }
     if constexpr (VW == 4) {
         if (a.D <= 1024) return start_fwd<TX, TY, 8, VW, false, 128, 4, 1>(a, 1, s);
         if (a.D <= 1280) return start_fwd<TX, TY, 10, VW, false, 128, 4, 1>(a, 1, s);
-        if (a.D <= 2048) return start_fwd<TX, TY, 16, VW, false, 128, 2, 1>(a, 1, s);
+        if (a.D <= 4096) return start_fwd<TX, TY, 4, VW, false, 256, 3, 8>(a, (a.D + 511) / 512, s);
         constexpr int per = 1280;
         return start_fwd<TX, TY, 10, VW, false, 256, 2, (kMaxD + per - 1) / per>(a, (a.D + per - 1) / per, s);
-    } else {                                                       // the tables need registers too
-        if (a.D <= 1024) return start_fwd<TX, TY, 8, VW, false, 128, 3, 1>(a, 1, s);
-        return start_fwd<TX, TY, 8, VW, false, 256, 1, kMaxD / 1024>(a, (a.D + 1023) / 1024, s);
+    } else {
+        if (a.D <= 2048) return start_fwd<TX, TY, 2, VW, false, 256, 3, 8>(a, (a.D + 255) / 256, s);
+        return start_fwd<TX, TY, 4, VW, false, 512, 1, 16>(a, (a.D + 511) / 512, s);
     }
 }
 
