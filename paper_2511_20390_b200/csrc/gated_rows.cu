@@ -1,4 +1,4 @@
-// Gated linear layer for few rows (single tokens): h = act(x Wg^T + bg) (x Wu^T + bu) on CUDA cores.
+// Gated linear layer for few rows (single tokens) or few columns: h = act(x Wg^T + bg) (x Wu^T + bu) on CUDA cores.
 //
 // Bound by the weights' bytes, which are read once: a warp takes one gate row and the matching up row of W, 16 bytes per lane
 // and load with several loads in flight, and multiplies them with all MR rows of x (which come from the L1).  Sums are fp32,
@@ -109,9 +109,15 @@ int rows(int act, int M, int F, int K, const void* x, const void* w, const float
 
 }  // namespace
 
-// Measured for F = 4608, K = 1152 (us): bf16, 1 / 2 / 4 / 8 rows 5.6 / 6.8 / 8.9 / 19, the tensor-core kernel 12.6 for any of
-// them; fp32, 1 / 8 rows 8.7 / 20, the tiled fp32 kernel 98 for up to 64 rows (few, deep tiles).
-bool gated_rows_wanted(int dtype, int M) { return M <= (dtype == FREE_BF16 ? 4 : 32); }
+// The time here goes with M F K, that of the tiled kernels, while their tiles are few, with K alone.  Measured (us, rows here /
+// tiled): bf16, F = 4608, K = 1152, 1 / 4 / 8 rows 5.6 / 8.9 / 13.5, tiled 10.6 to 12.6; F = 1536, K = 384, 8 / 16 rows 4.7 / 7.3,
+// tiled 5.8; F = 216, K = 1144, 16 rows 5.8, tiled 8.2.  fp32, F = 4608, K = 1152, 1 / 8 / 32 / 64 rows 5.3 / 18 / 49 / 92, tiled 76;
+// F = 1536, K = 384, 96 / 128 rows 27 / 35, tiled 30; F = 216, K = 1146, 35 / 512 / 1024 rows 14 / 59 / 112, tiled 97;
+// F = 12288, K = 2048, 32 rows 223, tiled 221.
+bool gated_rows_wanted(int dtype, int M, int F) {
+    const long long work = (long long)M * F;
+    return dtype == FREE_BF16 ? M <= 4 || work <= 14000 : M <= 32 || work <= 160000;
+}
 
 int gated_rows_forward(int dtype, int act, int M, int F, int K, const void* x, const void* w, const float* bias, void* h, void* preact, cudaStream_t s) {
     if (dtype == FREE_BF16) return rows<__nv_bfloat16, 8>(act, M, F, K, x, w, bias, h, preact, s);

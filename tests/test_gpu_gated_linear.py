@@ -115,6 +115,16 @@ def _check_backward(free, M, F, K, dt, act, seed=1):
     assert torch.equal(free.op_gated_linear_bwd(x, w, pre, dh, act=act, want_dx=False, want_dw=False)[2], db)
 
 
+@pytest.mark.parametrize("dt,M,F,K", [
+    ("bf16", 64, 216, 8), ("bf16", 65, 224, 136), ("bf16", 130, 136, 72), ("bf16", 257, 64, 8), ("bf16", 1000, 24, 40), ("bf16", 1751, 8, 64), ("bf16", 1750, 8, 64),
+    ("fp32", 33, 4849, 5), ("fp32", 35, 216, 1146), ("fp32", 1300, 131, 257), ("fp32", 5000, 33, 31), ("fp32", 700, 250, 64), ("fp32", 20000, 8, 12), ("fp32", 160001, 1, 3),
+])
+def test_forward_beside_the_choice_of_kernel(dt, M, F, K):
+    """Few rows or a narrow layer, and just more than that."""
+    import paper_2511_20390_b200 as free
+    _check_forward(free, M, F, K, dt, "silu", bias=M % 2 == 0, seed=M + F + K)
+
+
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 @pytest.mark.parametrize("M,F,K", BF16 + [(3333, 64, 64), (20, 1536, 384)])
 def test_backward_bf16(M, F, K, act):
