@@ -41,7 +41,7 @@ GatedSplit gated_tc_split(bool dw, int M, int F, int K);
 int gated_tc_backward(bool dw, const GatedSplit& g, int M, int F, int K, const void* x, const void* w, const void* dz, void* out, float* parts, uint32_t* err, cudaStream_t s);
 
 // ---- few rows (CUDA cores, both types); bf16: K % 8 == 0 -----------------------------------------
-bool gated_rows_wanted(int dtype, int M, int F);
+bool gated_rows_wanted(int dtype, int M, int F, int K);
 int gated_rows_forward(int dtype, int act, int M, int F, int K, const void* x, const void* w, const float* bias, void* h, void* preact, cudaStream_t s);
 
 // ---- fp32 (CUDA cores), any sizes ----------------------------------------------------------------

@@ -240,7 +240,7 @@ extern "C" int free_op_gated_linear(int dtype, int act, int M, int F, int K, con
     if (!free_aligned16(x) || !free_aligned16(w) || !free_aligned16(bias) || !free_aligned16(h) || !free_aligned16(preact) ||
         (reinterpret_cast<uintptr_t>(device_error) & 3u)) return FREE_ERR_ALIGN;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if (gated_rows_wanted(dtype, M, F)) return gated_rows_forward(dtype, act, M, F, K, x, w, bias, h, preact, s);
+    if (gated_rows_wanted(dtype, M, F, K)) return gated_rows_forward(dtype, act, M, F, K, x, w, bias, h, preact, s);
     if (dtype == FREE_FP32) return gated_simt_forward(act, M, F, K, (const float*)x, (const float*)w, bias, (float*)h, (float*)preact, s);
     return gated_tc_forward(act, M, F, K, x, w, bias, h, preact, device_error, s);
 }

@@ -111,12 +111,12 @@ int rows(int act, int M, int F, int K, const void* x, const void* w, const float
 
 // The time here goes with M F K, that of the tiled kernels, while their tiles are few, with K alone.  Measured (us, rows here /
 // tiled): bf16, F = 4608, K = 1152, 1 / 4 / 8 rows 5.6 / 8.9 / 13.5, tiled 10.6 to 12.6; F = 1536, K = 384, 8 / 16 rows 4.7 / 7.3,
-// tiled 5.8; F = 216, K = 1144, 16 rows 5.8, tiled 8.2.  fp32, F = 4608, K = 1152, 1 / 8 / 32 / 64 rows 5.3 / 18 / 49 / 92, tiled 76;
-// F = 1536, K = 384, 96 / 128 rows 27 / 35, tiled 30; F = 216, K = 1146, 35 / 512 / 1024 rows 14 / 59 / 112, tiled 97;
-// F = 12288, K = 2048, 32 rows 223, tiled 221.
-bool gated_rows_wanted(int dtype, int M, int F) {
+// tiled 5.8; F = 216, K = 1144, 16 rows 5.8, tiled 8.2.  fp32, F = 4608, K = 1152, 1 / 8 / 24 / 32 rows 5.3 / 18 / 38 / 49, tiled 49;
+// F = 12288, K = 2048, 16 / 24 rows 115 / 174, tiled 164; F = 256, K = 4608, 96 / 128 rows 31 / 55, tiled 41; F = 216, K = 1146, 64 /
+// 96 rows 15 / 21, tiled 17.  Short contractions, which the tiled fp32 kernel does not split: F = K = 64, 1024 rows 9.9, tiled 10.7.
+bool gated_rows_wanted(int dtype, int M, int F, int K) {
     const long long work = (long long)M * F;
-    return dtype == FREE_BF16 ? M <= 4 || work <= 14000 : M <= 32 || work <= 160000;
+    return dtype == FREE_BF16 ? M <= 4 || work <= 14000 : M <= 24 || work <= (K < 128 ? 70000 : 20000);
 }
 
 int gated_rows_forward(int dtype, int act, int M, int F, int K, const void* x, const void* w, const float* bias, void* h, void* preact, cudaStream_t s) {

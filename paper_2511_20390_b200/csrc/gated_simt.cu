@@ -7,8 +7,9 @@
 // each half of the tile: in GATED the halves are 64 gate columns and the matching 64 up columns, so the thread that holds
 // z_gate holds z_up.  Bound by the fp32 pipe: 64 multiply-adds against four 16-byte shared-memory reads per thread and step.
 // 4096 rows, F = 1536, K = 384: 226 us forward, 43 TFLOP/s.
-// TM is 64 where 128-row tiles would leave SMs idle in the last wave.  Few tiles and a long contraction are split, the parts
-// added in order.
+// TM is 64 where 128-row tiles would leave SMs idle in the last wave.  Few tiles and a long contraction are split and the parts
+// added in order: forward by the CTAs of a cluster, through their shared memory (z has to be whole before the activation), backward
+// through the workspace.  F = 256, K = 4608, 1024 rows: 129 us, unsplit 291; F = 1536, K = 384, 100 rows: 16, unsplit 30.
 #include "gated.h"
 
 namespace {
@@ -88,12 +89,39 @@ template <int ROWS, int THREADS, bool KMAJOR, bool VEC> struct Loader {
     }
 };
 
-template <int MODE, int TM, bool VEC>
-__global__ void __launch_bounds__(TM * 2) gated_simt_kernel(const Args a) {
+// bias, activation and product of four columns of row m
+__device__ __forceinline__ void finish(const Args& a, int m, int n0, const float* gate, const float* up) {
+    if (m >= a.M) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + j;
+        if (n >= a.F) continue;
+        float g = gate[j], u = up[j];
+        if (a.bias) { g += __ldg(a.bias + n); u += __ldg(a.bias + a.F + n); }
+        a.out[(long long)m * a.F + n] = free_gate_act(a.act, g) * u;
+        if (a.pre) { a.pre[(long long)m * 2 * a.F + n] = g; a.pre[(long long)m * 2 * a.F + a.F + n] = u; }
+    }
+}
+__device__ __forceinline__ float4 cluster_read(const void* mine, int rank) {       // what another CTA has at the same place
+    uint32_t at;
+    float4 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");     // release, acquire
+}
+
+// S > 1 (GATED): the S CTAs of a cluster take parts of the contraction; each then joins and finishes 8 / S rows of every thread.
+template <int MODE, int TM, bool VEC, int S>
+__device__ __forceinline__ void gated_simt_tile(const Args& a) {
     constexpr int THREADS = TM * 2;
     constexpr int HALF = MODE == GATED ? TN / 2 : TN;       // output columns of a tile
-    __shared__ __align__(16) float As[2][TK][TM + 4];
-    __shared__ __align__(16) float Bs[2][TK][TN + 4];
+    constexpr int STAGES = 2 * TK * (TM + 4 + TN + 4), JOIN = S > 1 ? TM * TN : 0;
+    __shared__ __align__(16) float smem[STAGES > JOIN ? STAGES : JOIN];
+    float (*As)[TK][TM + 4] = reinterpret_cast<float (*)[TK][TM + 4]>(smem);
+    float (*Bs)[TK][TN + 4] = reinterpret_cast<float (*)[TK][TN + 4]>(smem + 2 * TK * (TM + 4));
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
     const int m0 = blockIdx.x * TM, n0 = blockIdx.y * HALF;
     const int kbeg = (int)((long long)a.depth * blockIdx.z / a.parts), kend = (int)((long long)a.depth * (blockIdx.z + 1) / a.parts);
@@ -138,6 +166,31 @@ __global__ void __launch_bounds__(TM * 2) gated_simt_kernel(const Args a) {
         if (more) { la.store(As[buf ^ 1]); lb.store(Bs[buf ^ 1]); }   // last read before the previous barrier
         __syncthreads();
     }
+    if constexpr (S > 1) {
+        float4* mine = reinterpret_cast<float4*>(smem) + threadIdx.x;          // [row][gate or up][thread]
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            ulonglong2 lo, hi;
+            lo.x = acc2[i][0]; lo.y = acc2[i][1]; hi.x = acc2[i][2]; hi.y = acc2[i][3];
+            *reinterpret_cast<ulonglong2*>(mine + (2 * i) * THREADS) = lo;
+            *reinterpret_cast<ulonglong2*>(mine + (2 * i + 1) * THREADS) = hi;
+        }
+        cluster_barrier();
+#pragma unroll
+        for (int r = 0; r < 8 / S; ++r) {
+            const int i = blockIdx.z * (8 / S) + r;
+            float4 g = make_float4(0.f, 0.f, 0.f, 0.f), u = g;
+#pragma unroll
+            for (int q = 0; q < S; ++q) {
+                const float4 p = cluster_read(mine + (2 * i) * THREADS, q), t = cluster_read(mine + (2 * i + 1) * THREADS, q);
+                g.x += p.x; g.y += p.y; g.z += p.z; g.w += p.w;
+                u.x += t.x; u.y += t.y; u.z += t.z; u.w += t.w;
+            }
+            finish(a, m0 + (i < 4 ? ty * 4 + i : TM / 2 + ty * 4 + i - 4), n0 + tx * 4, &g.x, &u.x);
+        }
+        cluster_barrier();                                  // nobody leaves while its sums are read
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int m = m0 + (i < 4 ? ty * 4 + i : TM / 2 + ty * 4 + i - 4);
@@ -146,15 +199,7 @@ __global__ void __launch_bounds__(TM * 2) gated_simt_kernel(const Args a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) split2(acc2[i][j], acc[2 * j], acc[2 * j + 1]);
         if (MODE == GATED) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int n = n0 + tx * 4 + j;
-                if (n >= a.F) continue;
-                float g = acc[j], u = acc[4 + j];
-                if (a.bias) { g += __ldg(a.bias + n); u += __ldg(a.bias + a.F + n); }
-                a.out[(long long)m * a.F + n] = free_gate_act(a.act, g) * u;
-                if (a.pre) { a.pre[(long long)m * 2 * a.F + n] = g; a.pre[(long long)m * 2 * a.F + a.F + n] = u; }
-            }
+            finish(a, m, n0 + tx * 4, acc, acc + 4);
         } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -169,6 +214,11 @@ __global__ void __launch_bounds__(TM * 2) gated_simt_kernel(const Args a) {
             }
         }
     }
+}
+
+template <int MODE, int TM, bool VEC> __global__ void __launch_bounds__(TM * 2) gated_simt_kernel(const Args a) { gated_simt_tile<MODE, TM, VEC, 1>(a); }
+template <bool VEC, int S> __global__ void __launch_bounds__(128) __cluster_dims__(1, 1, S) gated_simt_split_kernel(const Args a) {
+    gated_simt_tile<GATED, 64, VEC, S>(a);
 }
 
 template <int MODE>
@@ -194,7 +244,18 @@ int launch(const Args& a, bool vec, cudaStream_t s) {
 int gated_simt_forward(int act, int M, int F, int K, const float* x, const float* w, const float* bias, float* h, float* preact, cudaStream_t s) {
     Args a{};
     a.M = M; a.N = F; a.depth = K; a.A = x; a.B = w; a.lda = K; a.ldb = K; a.bias = bias; a.act = act; a.F = F; a.out = h; a.pre = preact; a.parts = 1;
-    return launch<GATED>(a, K % 4 == 0, s);
+    // few tiles: as many CTAs to each as leave an SM three at most, with at least 64 of the contraction (at most two: 0 to 30% slower,
+    // 12288 columns, 40 rows 223 against 164 us; at most four: 0 to 18% slower)
+    const long long tiles = ((long long)M + 63) / 64 * (((long long)F + TN / 2 - 1) / (TN / 2));
+    const bool vec = K % 4 == 0;
+    if (tiles * 2 <= 3 * kSms && K >= 128) {
+        a.parts = tiles * 8 <= 3 * kSms && K >= 512 ? 8 : tiles * 4 <= 3 * kSms && K >= 256 ? 4 : 2;
+        const dim3 grid((unsigned)((M + 63) / 64), (unsigned)((F + TN / 2 - 1) / (TN / 2)), (unsigned)a.parts);
+        if (vec) (a.parts == 8 ? gated_simt_split_kernel<true, 8> : a.parts == 4 ? gated_simt_split_kernel<true, 4> : gated_simt_split_kernel<true, 2>)<<<grid, 128, 0, s>>>(a);
+        else (a.parts == 8 ? gated_simt_split_kernel<false, 8> : a.parts == 4 ? gated_simt_split_kernel<false, 4> : gated_simt_split_kernel<false, 2>)<<<grid, 128, 0, s>>>(a);
+        return free_check_launch();
+    }
+    return launch<GATED>(a, vec, s);
 }
 
 // Enough parts to give every SM two tiles, each at least 256 deep.

@@ -117,10 +117,12 @@ def _check_backward(free, M, F, K, dt, act, seed=1):
 
 @pytest.mark.parametrize("dt,M,F,K", [
     ("bf16", 64, 216, 8), ("bf16", 65, 224, 136), ("bf16", 130, 136, 72), ("bf16", 257, 64, 8), ("bf16", 1000, 24, 40), ("bf16", 1751, 8, 64), ("bf16", 1750, 8, 64),
+    ("fp32", 130, 216, 1146), ("fp32", 600, 64, 1030), ("fp32", 65, 1000, 129), ("fp32", 200, 300, 260), ("fp32", 333, 700, 512),
+    ("fp32", 100, 500, 4096), ("fp32", 900, 800, 130), ("fp32", 25, 801, 128), ("fp32", 64, 64, 9001),
     ("fp32", 33, 4849, 5), ("fp32", 35, 216, 1146), ("fp32", 1300, 131, 257), ("fp32", 5000, 33, 31), ("fp32", 700, 250, 64), ("fp32", 20000, 8, 12), ("fp32", 160001, 1, 3),
 ])
 def test_forward_beside_the_choice_of_kernel(dt, M, F, K):
-    """Few rows or a narrow layer, and just more than that."""
+    """Few rows or a narrow layer, just more than that, and contractions that several CTAs share."""
     import paper_2511_20390_b200 as free
     _check_forward(free, M, F, K, dt, "silu", bias=M % 2 == 0, seed=M + F + K)
 
