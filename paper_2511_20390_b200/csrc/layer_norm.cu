@@ -681,7 +681,7 @@ int launch_fwd(const NormArgs& a, cudaStream_t s) {
     }
     if (a.D <= 256) return start_narrow<TX, TY, 32, 8, VW>(a, s);
     if constexpr (VW > 1) {
-        if (a.D <= 512) return start_fwd<TX, TY, 4, VW, false, 128, 6, 1>(a, 1, s);
+        if (a.D <= 512) return start_fwd<TX, TY, 4, VW, false, 128, VW == 4 ? 6 : 5, 1>(a, 1, s);
         if (a.D <= 768) return start_fwd<TX, TY, 6, VW, false, 128, VW == 4 ? 5 : 4, 1>(a, 1, s);
     }
     if constexpr (VW == 4) {

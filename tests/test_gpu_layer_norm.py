@@ -167,6 +167,45 @@ def test_in_place_rows_between_and_bad_values():
         assert torch.equal(x, ref) and torch.isnan(base[:, D:]).all()
 
 
+@pytest.mark.parametrize("D,pad", [(6, 2), (32, 0), (64, 8), (96, 3), (127, 0), (200, 4), (255, 1)])
+def test_narrow_rows_in_place_missing_parts_and_bad_values(D, pad):
+    import paper_2511_20390_b200 as free
+    M, T = 203, 29
+    x, _ = _mat(17, 1, M, D, "bf16", 1.0, 0.2, pad)
+    dy, _ = _mat(17, 2, M, D, "bf16", 1.0, 0.0, pad)
+    w, _ = _tab(17, 3, M // T, D)
+    b, _ = _tab(17, 4, M // T, D)
+    ref, st = free.op_layer_norm(x, w, b, rows_per_group=T, want_stats=True)
+    dref = free.op_layer_norm_bwd(x, dy, st, w, rows_per_group=T)
+    # either gradient of the tables alone, or none
+    for ww, wb in ((True, False), (False, True), (False, False)):
+        got = free.op_layer_norm_bwd(x, dy, st, w, rows_per_group=T, want_dweight=ww, want_dbias=wb)
+        assert torch.equal(got[0], dref[0]) and (got[1] is None) != ww and (got[2] is None) != wb
+        assert (not ww or torch.equal(got[1], dref[1])) and (not wb or torch.equal(got[2], dref[2]))
+    # either table alone
+    one = torch.ones_like(w)
+    assert torch.equal(free.op_layer_norm(x, None, b, rows_per_group=T), free.op_layer_norm(x, one, b, rows_per_group=T))
+    assert torch.equal(free.op_layer_norm(x, w, rows_per_group=T), free.op_layer_norm(x, w, torch.zeros_like(b), rows_per_group=T))
+    # a row with an infinity and one with a NaN, beside good ones in the same warp
+    xb = x.clone()
+    xb[3, D // 2] = float("inf"); xb[101, 0] = float("nan"); xb[M - 1, D - 1] = float("-inf")
+    yb = free.op_layer_norm(xb, w, b, rows_per_group=T)
+    keep = [i for i in range(M) if i not in (3, 101, M - 1)]
+    assert torch.equal(yb[keep], ref[keep]) and torch.isnan(yb[[3, 101, M - 1]]).all()
+    # dx over each of its inputs, then y over x; what lies between the rows stays
+    for which in (0, 1):
+        a, g = (torch.full((M, D + 4), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        a[:, :D], g[:, :D] = x, dy
+        dst, beside = (a, g)[which], torch.full_like(a, 7.0)
+        # (a result of the same strides: they may choose another width of access, another order of the same sums)
+        want = free.op_layer_norm_bwd(a[:, :D], g[:, :D], st, w, rows_per_group=T, dx=beside[:, :D])
+        got = free.op_layer_norm_bwd(a[:, :D], g[:, :D], st, w, rows_per_group=T, dx=dst[:, :D])
+        assert torch.equal(dst, beside) and (dst[:, D:] == 7.0).all() and torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
+    base = x.as_strided((M, D + pad), (D + pad, 1))
+    free.op_layer_norm(x, w, b, rows_per_group=T, out=x)
+    assert torch.equal(x, ref) and torch.isnan(base[:, D:]).all()
+
+
 def test_rows_far_apart():
     # two rows more than 2^32 bytes apart in one allocation, in and out
     import paper_2511_20390_b200 as free
