@@ -10,7 +10,7 @@
 // Forward: a warp holds a row in registers (up to 2048 columns; several warps beyond), so a row costs ten exchanges and no
 // barrier; the weight and bias of a group come from the L1.  24 x 1024 rows of 1152, fp32 to bf16, weight and bias per sequence:
 // 29.5 us, 5.8 TB/s (a CTA per row with a barrier each: 41 us); 6144 rows of 4608: 33 us.
-// Backward: the column sums need registers too, so a row is spread over ceil(D / 256) warps, eight columns per lane, with one
+// Backward: the column sums need registers too, so a row is spread over warps with 12 or 16 columns per lane and one
 // barrier; rows are copied to shared memory one ahead of their use, every thread its own columns, so that the bytes in flight do
 // not cost registers.  The same rows with the residual path's gradient added: 65 us, 6.1 TB/s, and 5 us for the sums.
 // The gradients of w and b are column sums over a group's rows.  A CTA keeps them in fp32 registers over a run of rows of
@@ -250,18 +250,18 @@ __global__ void __launch_bounds__(MAXT, MINB) layer_norm_kernel(const NormArgs a
 // Whether rows are copied to shared memory ahead of their use: copies are of 4, 8 or 16 bytes.
 template <typename TX, typename TY, int VW> constexpr bool kAhead = VW * sizeof(TX) >= 4 && VW * sizeof(TY) >= 4;
 
-// One CTA, a team of ceil(D / 256) warps, per (group, chunk): a run of the group's rows, R of them per barrier and R more in
+// One CTA, a team of warps with C columns per lane, per (group, chunk): a run of the group's rows, R of them per barrier and R more in
 // flight.  T: threads per SM that the register budget is set for.
-template <typename TX, typename TY, int VW, int MAXT, int T, int R>
+template <typename TX, typename TY, int C, int VW, int MAXT, int T, int R>
 __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const NormArgs a) {
-    constexpr int P = 8 / VW, XW = kWords<TX, VW>, YW = kWords<TY, VW>;      // pieces of a lane, words of a piece
+    constexpr int P = C / VW, XW = kWords<TX, VW>, YW = kWords<TY, VW>;      // pieces of a lane, words of a piece
     constexpr bool AHEAD = kAhead<TX, TY, VW>;
     __shared__ float2 part[2][R][MAXT / 32];
     extern __shared__ uint4 ring[];
     free_grid_dep_wait();
     free_grid_dep_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, W = a.warps;
-    const Cols<8, VW, false> c{a.D, warp * 256, lane};
+    const Cols<C, VW, false> c{a.D, warp * 32 * C, lane};
     const TX* x = reinterpret_cast<const TX*>(a.x);
     const TY* dy = reinterpret_cast<const TY*>(a.dy);
     const TX* dres = reinterpret_cast<const TX*>(a.dres);
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
     const float inv_d = 1.f / (float)a.D;
     // shared memory: two groups of R rows, of each the pieces of x, dres and dy, [piece][thread]
     const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), T0 = blockDim.x;
-    const uint32_t bx = T0 * 8 * (uint32_t)sizeof(TX), by = T0 * 8 * (uint32_t)sizeof(TY);
+    const uint32_t bx = T0 * C * (uint32_t)sizeof(TX), by = T0 * C * (uint32_t)sizeof(TY);
     auto unit = [&](int it, int r) { return ring0 + (uint32_t)(it % 2 * R + r) * (2 * bx + by); };
     auto px = [&](uint32_t u, int p) { return u + (p * T0 + threadIdx.x) * VW * (uint32_t)sizeof(TX); };
     auto py = [&](uint32_t u, int p) { return u + 2 * bx + (p * T0 + threadIdx.x) * VW * (uint32_t)sizeof(TY); };
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const bool live = row + r < hi;                        // past the run: nothing is counted or stored
+            const bool live = R == 1 || row + r < hi;              // past the run: nothing is counted or stored
             const long long rr = live ? row + r : row;
             st[r] = next[r];
             next[r] = stats_of(row + R + r);
@@ -595,17 +595,27 @@ __global__ void __launch_bounds__(512) layer_norm_reduce_kernel(const NormArgs a
     }
 }
 
-// Threads per SM of the backward kernel.  Single bf16 columns are not copied ahead: two rows per barrier, in twice the registers.
-constexpr int kBwdT = 1024, kBwdDirectT = 512;
-
-int bwd_threads(int D) { return (D + 255) / 256 * 32; }
+// Columns per lane of the backward kernel for wide rows.  It is bound by issue slots where the rows are bf16, and a row takes each of
+// its warps what 16 columns take besides (exchanges, addresses, the barrier): so the number whose warps cost least, 12 or 16.
+// 24 x 1024 rows of 1152 bf16: 48.6 us with 12, 61.6 with 8; 8192 rows of 4096: 53 with 16, 66 with 8.  Odd widths, which are not
+// copied ahead, take eight and two rows per barrier.
+int bwd_cols(int D) {
+    if (D % 2) return 8;
+    const int w12 = (D + 383) / 384, w16 = (D + 511) / 512;
+    return D <= 1536 && w12 * (12 + 16) < w16 * (16 + 16) ? 12 : 16;
+}
+// Threads of an SM that the registers are shared among: 512, so that sums and rows stay in registers (twelve columns, 640 and 768
+// threads: 3 and 7% slower); 576 where that makes room for a second CTA (8192 rows of 4608 bf16: 67 us, so 79).
+constexpr int kBwdT = 512, kBwdT9 = 576;
+int bwd_threads(int D) { return (D + 32 * bwd_cols(D) - 1) / (32 * bwd_cols(D)) * 32; }
 bool narrow(int D) { return D <= 128 || (D <= 256 && D % 2 == 0); }      // (single columns beyond 128: 32 us the wide way, 56 this)
 
 // Chunks of a group in the backward pass: full waves of CTAs, at least eight rows each (64 where rows are narrow).  (A function of the sizes alone: the
 // workspace depends on it.)
 int chunks_of(int groups, int rows_per_group, int D) {
     const int t = bwd_threads(D);
-    const int per_sm = narrow(D) ? kNarrowBwdPerSm : t > 256 ? 1 : (D % 2 ? kBwdDirectT : kBwdT) / t;
+    const int share = t > 256 && t <= 288 && D % 2 == 0 ? kBwdT9 : kBwdT;
+    const int per_sm = narrow(D) ? kNarrowBwdPerSm : t >= share ? 1 : share / t;
     // the first number of waves that whole chunks fill to nine tenths, or else the best of four (one wave and a few CTAs more
     // take two: 4200 rows of 4608 in 14 groups 83 us, so 50)
     const long long resident = (long long)kSms * per_sm;
@@ -696,26 +706,34 @@ int launch_fwd(const NormArgs& a, cudaStream_t s) {
     }
 }
 
-template <typename TX, typename TY, int VW, int MAXT, int T, int R>
+template <typename TX, typename TY, int C, int VW, int MAXT, int T, int R>
 int start_bwd(const NormArgs& a, int threads, cudaStream_t s) {
-    auto kernel = layer_norm_bwd_kernel<TX, TY, VW, MAXT, T, R>;
-    const size_t smem = kAhead<TX, TY, VW> ? (size_t)threads * 2 * R * 8 * (2 * sizeof(TX) + sizeof(TY)) : 0;
+    auto kernel = layer_norm_bwd_kernel<TX, TY, C, VW, MAXT, T, R>;
+    const size_t smem = kAhead<TX, TY, VW> ? (size_t)threads * 2 * R * C * (2 * sizeof(TX) + sizeof(TY)) : 0;
     if (smem > 47 * 1024) FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     return free_launch(free_overlap_for_rows(a.M), kernel, dim3((unsigned)a.groups * (unsigned)a.chunks), dim3(threads), smem, s, a);
+}
+template <typename TX, typename TY, int VW>
+int start_wide_bwd(const NormArgs& a, int threads, cudaStream_t s) {
+    const int cols = bwd_cols(a.D);
+    if (cols == 12) return start_bwd<TX, TY, 12, VW, 128, kBwdT, 1>(a, threads, s);
+    if (cols == 16 && threads == 288) return start_bwd<TX, TY, 16, VW, 288, kBwdT9, 1>(a, threads, s);
+    if (cols == 16) return start_bwd<TX, TY, 16, VW, 512, kBwdT, 1>(a, threads, s);
+    if constexpr (VW == 1) {
+        return threads <= 256 ? start_bwd<TX, TY, 8, 1, 256, kBwdT, 2>(a, threads, s)
+             : threads <= 576 ? start_bwd<TX, TY, 8, 1, 576, 576, 2>(a, threads, s) : start_bwd<TX, TY, 8, 1, 1024, 1024, 1>(a, threads, s);
+    }
+    return FREE_ERR_UNSUPPORTED;                                   // not reached: an odd width has VW == 1
 }
 
 template <typename TX, typename TY, int VW>
 int launch_bwd(NormArgs a, cudaStream_t s) {
     const int threads = bwd_threads(a.D);
     a.warps = threads / 32;
-    // wide rows leave an SM one CTA: two rows per barrier where shared memory holds them
-    constexpr bool AHEAD = kAhead<TX, TY, VW>;
     constexpr int C = kNarrowCols<VW>;
     const int r = a.D <= 32 ? start_narrow_bwd<TX, TY, 8, 4, VW>(a, s) : a.D <= 64 ? start_narrow_bwd<TX, TY, 64 / C, C, VW>(a, s)
                 : a.D <= 128 ? start_narrow_bwd<TX, TY, 128 / C, C, VW>(a, s)
-                : narrow(a.D) ? start_narrow_bwd<TX, TY, 32, 8, VW>(a, s)
-                : threads <= 256 ? start_bwd<TX, TY, VW, 256, AHEAD ? kBwdT : kBwdDirectT, AHEAD ? 1 : 2>(a, threads, s)
-                : threads <= 576 ? start_bwd<TX, TY, VW, 576, 576, 2>(a, threads, s) : start_bwd<TX, TY, VW, 1024, 1024, 1>(a, threads, s);
+                : narrow(a.D) ? start_narrow_bwd<TX, TY, 32, 8, VW>(a, s) : start_wide_bwd<TX, TY, VW>(a, threads, s);
     if (r != FREE_OK || a.chunks == 1 || (!a.dw && !a.db)) return r;
     return free_launch(free_launch_overlap_enabled(), layer_norm_reduce_kernel, dim3((unsigned)a.groups * ((2u * a.D + 31) / 32)), dim3(512), 0, s, a);
 }
