@@ -270,33 +270,37 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
     const long long base = (long long)g * a.rows_per_group;
     const long long lo = base + (long long)a.rows_per_group * ch / a.chunks, hi = base + (long long)a.rows_per_group * (ch + 1) / a.chunks;
     const float inv_d = 1.f / (float)a.D;
-    // shared memory: two groups of R rows, of each the pieces of x, dres and dy, [piece][thread]
-    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), T0 = blockDim.x;
-    const uint32_t bx = T0 * C * (uint32_t)sizeof(TX), by = T0 * C * (uint32_t)sizeof(TY);
-    auto unit = [&](int it, int r) { return ring0 + (uint32_t)(it % 2 * R + r) * (2 * bx + by); };
-    auto px = [&](uint32_t u, int p) { return u + (p * T0 + threadIdx.x) * VW * (uint32_t)sizeof(TX); };
-    auto py = [&](uint32_t u, int p) { return u + 2 * bx + (p * T0 + threadIdx.x) * VW * (uint32_t)sizeof(TY); };
-    auto fetch = [&](int it) {
+    // shared memory: two groups of R rows, of each x, dres and dy, [warp][piece][lane]; running addresses, for the pass counts every
+    // instruction (24 x 1024 rows of 1152 bf16: 46.3 us, with products of row and stride 48.4)
+    const uint32_t T0 = blockDim.x, bx = T0 * C * (uint32_t)sizeof(TX), one = 2 * bx + T0 * C * (uint32_t)sizeof(TY);
+    const uint32_t place = warp * 32 * C + lane * VW;
+    uint32_t now = (uint32_t)__cvta_generic_to_shared(ring), then = now + R * one;
+    auto px = [&](uint32_t u, int p) { return u + place * (uint32_t)sizeof(TX) + p * 32 * VW * (uint32_t)sizeof(TX); };
+    auto py = [&](uint32_t u, int p) { return u + 2 * bx + place * (uint32_t)sizeof(TY) + p * 32 * VW * (uint32_t)sizeof(TY); };
+    const TX *fx = x + lo * a.x_stride + c.at(0), *fr = dres + lo * a.dres_stride + c.at(0);
+    const TY* fy = dy + lo * a.dy_stride + c.at(0);
+    long long ahead = lo;                                          // the row to copy next
+    auto fetch = [&](uint32_t to) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const long long row = lo + (long long)it * R + r;
-            if (row < hi) {
-                const uint32_t u = unit(it, r);
+            if (ahead < hi) {
+                const uint32_t u = to + r * one;
 #pragma unroll
                 for (int p = 0; p < P; ++p)
                     if (c.in(p)) {
-                        send<TX, VW>(px(u, p), x + row * a.x_stride + c.at(p));
-                        if (dres) send<TX, VW>(px(u + bx, p), dres + row * a.dres_stride + c.at(p));
-                        send<TY, VW>(py(u, p), dy + row * a.dy_stride + c.at(p));
+                        send<TX, VW>(px(u, p), fx + p * 32 * VW);
+                        if (dres) send<TX, VW>(px(u + bx, p), fr + p * 32 * VW);
+                        send<TY, VW>(py(u, p), fy + p * 32 * VW);
                     }
             }
+            ++ahead; fx += a.x_stride; fr += a.dres_stride; fy += a.dy_stride;
         }
         copy_commit();
     };
     auto stats_of = [&](long long row) {
         return row < hi ? make_float2(__ldg(a.stats_in + 2 * row), __ldg(a.stats_in + 2 * row + 1)) : make_float2(0.f, 0.f);
     };
-    if (AHEAD) fetch(0);
+    if (AHEAD) fetch(now);
     float w[P][VW], dw[P][VW], db[P][VW];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -313,7 +317,7 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
         float2 st[R], sum[R];
         float xh[R][P][VW], v[R][P][VW];
         if (AHEAD) {
-            fetch(it + 1);                                         // into the slot that the previous rows left
+            fetch(then);                                           // into the slot that the previous rows left
             copy_wait<1>();
         }
 #pragma unroll
@@ -326,8 +330,8 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 if (AHEAD) {
-                    take<TX, VW>(px(unit(it, r), p), c.in(p), rx[p]);
-                    take<TY, VW>(py(unit(it, r), p), c.in(p), ry[p]);
+                    take<TX, VW>(px(now + r * one, p), c.in(p), rx[p]);
+                    take<TY, VW>(py(now + r * one, p), c.in(p), ry[p]);
                 } else {
                     load<TX, VW>(x + rr * a.x_stride + c.at(p), c.in(p), rx[p]);
                     load<TY, VW>(dy + rr * a.dy_stride + c.at(p), c.in(p), ry[p]);
@@ -350,14 +354,14 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
             sum[r] = make_float2(free_warp_sum(s1), free_warp_sum(s2));
         }
         if (W > 1) {
-            float2 (*now)[MAXT / 32] = part[it & 1];               // a buffer is rewritten two barriers after its last read
+            float2 (*sums)[MAXT / 32] = part[it & 1];               // a buffer is rewritten two barriers after its last read
             if (lane == 0) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) now[r][warp] = sum[r];
+                for (int r = 0; r < R; ++r) sums[r][warp] = sum[r];
             }
             __syncthreads();
 #pragma unroll
-            for (int r = 0; r < R; ++r) sum[r] = team_sum<MAXT / 32>(now[r], W);
+            for (int r = 0; r < R; ++r) sum[r] = team_sum<MAXT / 32>(sums[r], W);
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -366,12 +370,15 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 float o[VW];
-                if (AHEAD && dres) take<TX, VW>(px(unit(it, r) + bx, p), c.in(p), res[r][p]);
+                if (AHEAD && dres) take<TX, VW>(px(now + r * one + bx, p), c.in(p), res[r][p]);
 #pragma unroll
                 for (int e = 0; e < VW; ++e) o[e] = fmaf(st[r].y, v[r][p][e] - m1 - xh[r][p][e] * m2, dres ? value<TX, VW>(res[r][p], e) : 0.f);
                 if (c.in(p)) store<VW>(dx + (row + r) * a.dx_stride + c.at(p), o);
             }
         }
+        const uint32_t t = now;
+        now = then;
+        then = t;
     }
     if (AHEAD) copy_wait<0>();                                     // nothing is in flight when the CTA ends
     if (!a.dw && !a.db) return;
@@ -597,16 +604,17 @@ __global__ void __launch_bounds__(512) layer_norm_reduce_kernel(const NormArgs a
 
 // Columns per lane of the backward kernel for wide rows.  It is bound by issue slots where the rows are bf16, and a row takes each of
 // its warps what 16 columns take besides (exchanges, addresses, the barrier): so the number whose warps cost least, 12 or 16.
-// 24 x 1024 rows of 1152 bf16: 48.6 us with 12, 61.6 with 8; 8192 rows of 4096: 53 with 16, 66 with 8.  Odd widths, which are not
-// copied ahead, take eight and two rows per barrier.
+// 24 x 1024 rows of 1152 bf16: 48.6 us with 12, 61.6 with 8; 8192 rows of 4096: 53 with 16, 66 with 8.  Eight columns and two rows
+// per barrier: odd widths, which are not copied ahead, and those of which 16 leave an SM with one CTA of nine warps (8192 rows of
+// 4608, fp32 and bf16: 87 us; two such CTAs in fewer registers 95).
 int bwd_cols(int D) {
-    if (D % 2) return 8;
+    if (D % 2 || (D > 4096 && D <= 4608)) return 8;
     const int w12 = (D + 383) / 384, w16 = (D + 511) / 512;
     return D <= 1536 && w12 * (12 + 16) < w16 * (16 + 16) ? 12 : 16;
 }
-// Threads of an SM that the registers are shared among: 512, so that sums and rows stay in registers (twelve columns, 640 and 768
-// threads: 3 and 7% slower); 576 where that makes room for a second CTA (8192 rows of 4608 bf16: 67 us, so 79).
-constexpr int kBwdT = 512, kBwdT9 = 576;
+// Threads of an SM that the registers are shared among, so that sums and rows stay in them (twelve columns: 640 and 768 threads are
+// 3 and 7% slower).
+constexpr int kBwdT = 512;
 int bwd_threads(int D) { return (D + 32 * bwd_cols(D) - 1) / (32 * bwd_cols(D)) * 32; }
 bool narrow(int D) { return D <= 128 || (D <= 256 && D % 2 == 0); }      // (single columns beyond 128: 32 us the wide way, 56 this)
 
@@ -614,8 +622,7 @@ bool narrow(int D) { return D <= 128 || (D <= 256 && D % 2 == 0); }      // (sin
 // workspace depends on it.)
 int chunks_of(int groups, int rows_per_group, int D) {
     const int t = bwd_threads(D);
-    const int share = t > 256 && t <= 288 && D % 2 == 0 ? kBwdT9 : kBwdT;
-    const int per_sm = narrow(D) ? kNarrowBwdPerSm : t >= share ? 1 : share / t;
+    const int per_sm = narrow(D) ? kNarrowBwdPerSm : t >= kBwdT ? 1 : kBwdT / t;
     // the first number of waves that whole chunks fill to nine tenths, or else the best of four (one wave and a few CTAs more
     // take two: 4200 rows of 4608 in 14 groups 83 us, so 50)
     const long long resident = (long long)kSms * per_sm;
@@ -717,13 +724,12 @@ template <typename TX, typename TY, int VW>
 int start_wide_bwd(const NormArgs& a, int threads, cudaStream_t s) {
     const int cols = bwd_cols(a.D);
     if (cols == 12) return start_bwd<TX, TY, 12, VW, 128, kBwdT, 1>(a, threads, s);
-    if (cols == 16 && threads == 288) return start_bwd<TX, TY, 16, VW, 288, kBwdT9, 1>(a, threads, s);
     if (cols == 16) return start_bwd<TX, TY, 16, VW, 512, kBwdT, 1>(a, threads, s);
     if constexpr (VW == 1) {
-        return threads <= 256 ? start_bwd<TX, TY, 8, 1, 256, kBwdT, 2>(a, threads, s)
-             : threads <= 576 ? start_bwd<TX, TY, 8, 1, 576, 576, 2>(a, threads, s) : start_bwd<TX, TY, 8, 1, 1024, 1024, 1>(a, threads, s);
+        if (threads <= 256) return start_bwd<TX, TY, 8, VW, 256, kBwdT, 2>(a, threads, s);
+        if (threads > 576) return start_bwd<TX, TY, 8, VW, 1024, 1024, 1>(a, threads, s);
     }
-    return FREE_ERR_UNSUPPORTED;                                   // not reached: an odd width has VW == 1
+    return start_bwd<TX, TY, 8, VW, 576, 576, 2>(a, threads, s);
 }
 
 template <typename TX, typename TY, int VW>
