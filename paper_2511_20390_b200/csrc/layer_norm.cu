@@ -34,7 +34,9 @@ template <typename E, int VW> __device__ __forceinline__ float value(const uint3
     if (sizeof(E) == 4 || VW == 1) return __uint_as_float(w[e]);
     return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
 }
-template <typename E, int VW> __device__ __forceinline__ void load(const E* p, bool ok, uint32_t* w) {
+// ONCE: read past the caches' older lines.  Not for single fp32 columns in the backward and narrow kernels, where two accesses share a
+// line and the second comes late (20000 x 1001, fp32 and bf16, backward: 63 us, with it 152; forward the other way, 39 and 32).
+template <typename E, int VW, bool ONCE = true> __device__ __forceinline__ void load(const E* p, bool ok, uint32_t* w) {
     constexpr int B = VW * (int)sizeof(E);
     if (B == 16) {
         const uint4 u = ok ? __ldcs(reinterpret_cast<const uint4*>(p)) : make_uint4(0u, 0u, 0u, 0u);
@@ -43,7 +45,8 @@ template <typename E, int VW> __device__ __forceinline__ void load(const E* p, b
         const uint2 u = ok ? __ldcs(reinterpret_cast<const uint2*>(p)) : make_uint2(0u, 0u);
         w[0] = u.x; w[1 % kWords<E, VW>] = u.y;
     } else if (B == 4) {
-        w[0] = ok ? __ldcs(reinterpret_cast<const uint32_t*>(p)) : 0u;
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
+        w[0] = !ok ? 0u : ONCE || VW > 1 ? __ldcs(q) : *q;
     } else {
         w[0] = ok ? __float_as_uint(to_f(*p)) : 0u;
     }
@@ -333,9 +336,9 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
                     take<TX, VW>(px(now + r * one, p), c.in(p), rx[p]);
                     take<TY, VW>(py(now + r * one, p), c.in(p), ry[p]);
                 } else {
-                    load<TX, VW>(x + rr * a.x_stride + c.at(p), c.in(p), rx[p]);
-                    load<TY, VW>(dy + rr * a.dy_stride + c.at(p), c.in(p), ry[p]);
-                    if (dres) load<TX, VW>(dres + rr * a.dres_stride + c.at(p), c.in(p), res[r][p]);
+                    load<TX, VW, false>(x + rr * a.x_stride + c.at(p), c.in(p), rx[p]);
+                    load<TY, VW, false>(dy + rr * a.dy_stride + c.at(p), c.in(p), ry[p]);
+                    if (dres) load<TX, VW, false>(dres + rr * a.dres_stride + c.at(p), c.in(p), res[r][p]);
                 }
             }
             float s1 = 0.f, s2 = 0.f;
@@ -431,7 +434,7 @@ __global__ void __launch_bounds__(256, kNarrowPerSm) layer_norm_narrow_kernel(co
     uint32_t nx[P][XW];
     auto fetch = [&](long long r) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) load<TX, VW>(x + r * a.x_stride + c.at(p), r < last && c.in(p), nx[p]);
+        for (int p = 0; p < P; ++p) load<TX, VW, false>(x + r * a.x_stride + c.at(p), r < last && c.in(p), nx[p]);
     };
     const bool tables = a.weight || a.bias;
     const long long g0 = !tables ? 0 : first <= 0xffffffffLL ? (long long)((uint32_t)first / (uint32_t)a.rows_per_group) : first / a.rows_per_group;
@@ -504,9 +507,9 @@ __global__ void __launch_bounds__(256, kNarrowBwdPerSm) layer_norm_narrow_bwd_ke
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const bool ok = r < hi && c.in(p);
-            load<TX, VW>(x + r * a.x_stride + c.at(p), ok, nx[p]);
-            load<TY, VW>(dy + r * a.dy_stride + c.at(p), ok, ny[p]);
-            load<TX, VW>(dres + r * a.dres_stride + c.at(p), ok && dres, nr[p]);
+            load<TX, VW, false>(x + r * a.x_stride + c.at(p), ok, nx[p]);
+            load<TY, VW, false>(dy + r * a.dy_stride + c.at(p), ok, ny[p]);
+            load<TX, VW, false>(dres + r * a.dres_stride + c.at(p), ok && dres, nr[p]);
         }
         ns = r < hi ? make_float2(__ldg(a.stats_in + 2 * r), __ldg(a.stats_in + 2 * r + 1)) : make_float2(0.f, 0.f);
     };
