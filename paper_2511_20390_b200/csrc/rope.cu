@@ -21,9 +21,9 @@ constexpr int kMaxAxes = 4;
 constexpr int kThreads = 512;                     // most threads of a CTA
 constexpr int kTableBytes = 16384;                 // (cos, sin) entries of a CTA
 // Tokens that a thread has in flight.
-// (A bf16 slot of two halves is eight pairs: more of them cost registers, 23 instead of 20 us for four on 8 x 4096 tokens of 12
-// heads of 64.)
-template <typename T, bool HALVES> constexpr int kUnroll = HALVES && sizeof(T) == 2 ? 1 : 4;
+// (A bf16 slot of two halves is up to eight pairs: more of those cost registers, 23 instead of 20 us for four on 8 x 4096 tokens of
+// 12 heads of 64.  Narrower slots take four: 16 heads of 72 on 24 x 1024 tokens 22.7 us, one 30.8.)
+template <typename T, int V, bool HALVES> constexpr int kUnroll = HALVES && sizeof(T) == 2 && V > 4 ? 1 : 4;
 constexpr int kSms = 148;
 
 struct RopeArgs {
@@ -124,7 +124,7 @@ __device__ __forceinline__ void rotate(Vec<T, V>& u, Vec<T, V>& w, const float4*
 // elements behind both halves, which are copied.
 template <typename T, int V, bool HALVES, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads) rope_axes_kernel(const __grid_constant__ RopeArgs a) {
-    constexpr int U = kUnroll<T, HALVES>;
+    constexpr int U = kUnroll<T, V, HALVES>;
     // Pairs of a slot: PV.  They lie in planes of two, [plane][token][slot group], so that a warp's 16-byte reads are one run
     // (with a slot's pairs side by side they would be 32 bytes apart and meet in the same banks: 61 instead of 44 us for the
     // queries and keys of 24 x 1024 tokens, 16 heads of 72, before the words stayed packed).
@@ -205,7 +205,7 @@ int launch(RopeArgs& a, cudaStream_t s) {
     a.width = (a.slots + a.passes - 1) / a.passes;
     a.lanes_tok = a.width >= 256 ? 1 : 256 / a.width;
     if (a.lanes_tok > a.n_tok) a.lanes_tok = a.n_tok;
-    constexpr int PV = HALVES ? V : V / 2, U = kUnroll<T, HALVES>;
+    constexpr int PV = HALVES ? V : V / 2, U = kUnroll<T, V, HALVES>;
     // tokens of a CTA: as many as a thread unrolls, less when the table is full or the GPU would stand idle
     long long tok = (long long)a.lanes_tok * U;
     const long long spread = ((long long)a.n_tok * a.n_seq + 2 * kSms - 1) / (2 * kSms);
