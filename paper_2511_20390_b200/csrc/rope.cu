@@ -9,7 +9,7 @@
 // streams the heads through it.  A thread keeps one slot (one vector of a head, or the two that it couples), so that the index
 // arithmetic is done once, and has kUnroll tokens' loads in flight.  The frequencies are formed on the host in fp64 and travel
 // as a kernel argument.
-// Measured on B200: 39 us for the 113 MB of queries and keys of 24 x 1024 tokens, 16 heads of 72, bf16 (5.8 TB/s read and
+// Measured on B200: 40 us for the 113 MB of queries and keys of 24 x 1024 tokens, 16 heads of 72, bf16 (5.6 TB/s read and
 // written), 73 us for the same in fp32 (6.2 TB/s).
 #include "internal.h"
 #include <math.h>
