@@ -5,6 +5,7 @@ the current stream.  Nothing here computes any part of the method.
 """
 import ctypes as C
 import os
+from operator import index
 
 import numpy as np
 import torch
@@ -62,65 +63,77 @@ class TrajStats(C.Structure):
 
 _LIB = None
 
+
+class _Int:
+    """A C int argument.  C.c_int cuts larger numbers to 32 bits without a word (2^32 + 64 rows would be computed as 64);
+    here they are an error (C.ArgumentError).  No slower than C.c_int, which makes an object per argument."""
+    @staticmethod
+    def from_param(v):
+        n = index(v)
+        if -0x80000000 <= n <= 0x7fffffff:
+            return n
+        raise ValueError(f"{n} does not fit a C int")
+
+
 _SIGNATURES = {
-    "free_strerror": (C.c_char_p, [C.c_int]),
+    "free_strerror": (C.c_char_p, [_Int]),
     "free_create": (C.c_int, [C.POINTER(ModelDesc), C.POINTER(DrafterDesc), C.POINTER(C.c_void_p)]),
     "free_destroy": (C.c_int, [C.c_void_p]),
-    "free_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_int]),
-    "dit_verify_pass": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
+    "free_workspace_bytes": (C.c_size_t, [C.c_void_p, _Int]),
+    "dit_verify_pass": (C.c_int, [C.c_void_p, _Int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
                                   C.POINTER(ScheduleDesc), C.c_void_p, C.c_void_p, C.c_void_p,
                                   C.c_void_p, C.c_size_t, C.c_void_p]),
-    "dit_verify_pass_raw": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+    "dit_verify_pass_raw": (C.c_int, [C.c_void_p, _Int, C.c_void_p, C.c_void_p, C.c_void_p, _Int,
                                       C.POINTER(ScheduleDesc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "spec_verify": (C.c_int, [C.c_int, C.c_int, C.c_int64] + [C.c_void_p] * 11),
-    "spec_verify_fused": (C.c_int, [C.c_int, C.c_int, C.c_int64, C.c_int, C.c_float] + [C.c_void_p] * 10 + [C.c_int] + [C.c_void_p] * 6),
-    "draft_step": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
+    "spec_verify": (C.c_int, [_Int, _Int, C.c_int64] + [C.c_void_p] * 11),
+    "spec_verify_fused": (C.c_int, [_Int, _Int, C.c_int64, _Int, C.c_float] + [C.c_void_p] * 10 + [_Int] + [C.c_void_p] * 6),
+    "draft_step": (C.c_int, [C.c_void_p, _Int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
                              C.POINTER(ScheduleDesc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                              C.c_void_p, C.c_size_t, C.c_void_p]),
-    "sample_trajectory": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.POINTER(ScheduleDesc),
+    "sample_trajectory": (C.c_int, [C.c_void_p, _Int, C.c_void_p, C.c_void_p, C.POINTER(ScheduleDesc),
                                     C.POINTER(SpecParams), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                     C.POINTER(TrajStats), C.c_void_p, C.c_size_t, C.c_void_p]),
-    "free_spec_round": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(ScheduleDesc),
+    "free_spec_round": (C.c_int, [C.c_void_p, _Int, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(ScheduleDesc),
                                   C.POINTER(SpecParams), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                   C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "free_split_range": (C.c_int, [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_int), C.POINTER(C.c_int)]),
-    "free_spec_round_begin": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(ScheduleDesc),
-                                        C.POINTER(SpecParams), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p,
+    "free_split_range": (C.c_int, [_Int, _Int, _Int, C.POINTER(C.c_int), C.POINTER(C.c_int)]),
+    "free_spec_round_begin": (C.c_int, [C.c_void_p, _Int, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(ScheduleDesc),
+                                        C.POINTER(SpecParams), C.c_void_p, C.c_void_p, C.c_void_p, _Int, _Int, C.c_void_p,
                                         C.c_void_p, C.c_size_t, C.c_void_p]),
-    "free_spec_round_finish": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.POINTER(ScheduleDesc), C.POINTER(SpecParams),
+    "free_spec_round_finish": (C.c_int, [C.c_void_p, _Int, C.c_void_p, C.POINTER(ScheduleDesc), C.POINTER(SpecParams),
                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                          C.c_void_p, C.c_size_t, C.c_void_p]),
-    "free_uncertainty_profile": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.POINTER(ScheduleDesc),
+    "free_uncertainty_profile": (C.c_int, [C.c_void_p, _Int, C.c_void_p, C.c_void_p, C.POINTER(ScheduleDesc),
                                            C.POINTER(SpecParams), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                            C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "free_schedule_linear": (C.c_int, [C.c_int, C.c_double, C.c_double, C.c_int, C.c_double, C.c_double] + [C.c_void_p] * 4),
-    "free_schedule_respaced": (C.c_int, [C.c_int, C.c_int, C.c_double, C.c_double, C.c_int, C.c_double, C.c_double] + [C.c_void_p] * 4),
-    "free_fit_lambda_profile": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p]),
+    "free_schedule_linear": (C.c_int, [_Int, C.c_double, C.c_double, _Int, C.c_double, C.c_double] + [C.c_void_p] * 4),
+    "free_schedule_respaced": (C.c_int, [_Int, _Int, C.c_double, C.c_double, _Int, C.c_double, C.c_double] + [C.c_void_p] * 4),
+    "free_fit_lambda_profile": (C.c_int, [C.c_void_p, C.c_void_p, _Int, _Int, C.c_void_p]),
     "free_drafter_loss_workspace_bytes": (C.c_size_t, []),
-    "free_drafter_loss": (C.c_int, [C.c_int] * 4 + [C.c_int64] + [C.c_void_p] * 4 + [C.c_float] * 4 +
+    "free_drafter_loss": (C.c_int, [_Int] * 4 + [C.c_int64] + [C.c_void_p] * 4 + [C.c_float] * 4 +
                           [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "free_set_launch_overlap": (C.c_int, [C.c_int]),
+    "free_set_launch_overlap": (C.c_int, [_Int]),
     "free_device_error_code": (C.c_int, [C.c_uint32]),
     "free_selftest_bounded_wait": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
     "free_profile_begin": (C.c_int, [C.c_void_p]),
-    "free_profile_end": (C.c_int, [C.c_void_p, C.POINTER(ProfEntry), C.c_int, C.POINTER(C.c_int)]),
+    "free_profile_end": (C.c_int, [C.c_void_p, C.POINTER(ProfEntry), _Int, C.POINTER(C.c_int)]),
     "free_op_linear_workspace_bytes": (C.c_size_t, []),
-    "free_op_linear": (C.c_int, [C.c_int] * 6 + [C.c_void_p] * 6 + [C.c_int64, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "free_op_ln_modulate": (C.c_int, [C.c_int] * 4 + [C.c_void_p] * 3 + [C.c_int64, C.c_void_p, C.c_void_p]),
-    "free_op_gated_linear": (C.c_int, [C.c_int] * 5 + [C.c_void_p] * 7),
-    "free_op_gated_linear_bwd_workspace_bytes": (C.c_size_t, [C.c_int] * 4),
-    "free_op_gated_linear_bwd": (C.c_int, [C.c_int] * 5 + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p, C.c_void_p]),
-    "free_op_layer_norm": (C.c_int, [C.c_int] * 5 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_float,
+    "free_op_linear": (C.c_int, [_Int] * 6 + [C.c_void_p] * 6 + [C.c_int64, _Int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "free_op_ln_modulate": (C.c_int, [_Int] * 4 + [C.c_void_p] * 3 + [C.c_int64, C.c_void_p, C.c_void_p]),
+    "free_op_gated_linear": (C.c_int, [_Int] * 5 + [C.c_void_p] * 7),
+    "free_op_gated_linear_bwd_workspace_bytes": (C.c_size_t, [_Int] * 4),
+    "free_op_gated_linear_bwd": (C.c_int, [_Int] * 5 + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p, C.c_void_p]),
+    "free_op_layer_norm": (C.c_int, [_Int] * 5 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, _Int, C.c_float,
                                                      C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
-    "free_op_layer_norm_bwd_workspace_bytes": (C.c_size_t, [C.c_int] * 3),
-    "free_op_layer_norm_bwd": (C.c_int, [C.c_int] * 5 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
-                                                         C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+    "free_op_layer_norm_bwd_workspace_bytes": (C.c_size_t, [_Int] * 3),
+    "free_op_layer_norm_bwd": (C.c_int, [_Int] * 5 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                                         C.c_int64, _Int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                                          C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "free_op_rope_axes": (C.c_int, [C.c_int] * 9 + [C.c_void_p, C.c_double, C.c_void_p, C.c_int64] +
+    "free_op_rope_axes": (C.c_int, [_Int] * 9 + [C.c_void_p, C.c_double, C.c_void_p, C.c_int64] +
                           [C.c_void_p, C.c_int64, C.c_int64, C.c_int64] * 2 + [C.c_void_p]),
-    "free_op_attention": (C.c_int, [C.c_int] * 5 + [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "free_op_attention_workspace_bytes": (C.c_size_t, [C.c_int] * 5),
-    "free_op_attention_static": (C.c_int, [C.c_int] * 4 + [C.c_void_p] * 4),
+    "free_op_attention": (C.c_int, [_Int] * 5 + [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "free_op_attention_workspace_bytes": (C.c_size_t, [_Int] * 5),
+    "free_op_attention_static": (C.c_int, [_Int] * 4 + [C.c_void_p] * 4),
 }
 
 
@@ -744,6 +757,8 @@ def op_rope_axes(x, pos, axis_dims, base=10000.0, pairing="interleaved", joint_f
     n_axes = len(axis_dims)
     if n_axes not in _AXES:
         raise ValueError("axis_dims: expected one to four axes")
+    if max(axis_dims) > 0x7fffffff or min(axis_dims) < -0x80000000:          # an array of C ints would cut them
+        raise ValueError("axis_dims: expected even widths that fit into a head")
     shape = n_seq, n_tok, heads, d_head = x.shape
     dev = _device_of(x, pos, out)
     if pos.dtype != torch.float32 or not pos.is_contiguous() or (pos.shape != (n_tok, n_axes) and pos.shape != (n_seq, n_tok, n_axes)):
