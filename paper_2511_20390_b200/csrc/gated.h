@@ -19,9 +19,10 @@ __device__ __forceinline__ float free_logistic_fast(float v) {
 __device__ __forceinline__ float free_gate_arg(int act, float g) { return act == FREE_ACT_SILU ? g : FREE_GELU_2K * (g + FREE_GELU_C * g * g * g); }
 __device__ __forceinline__ float free_gate_act_fast(int act, float g) { return g * free_logistic_fast(free_gate_arg(act, g)); }
 __device__ __forceinline__ float free_gate_act(int act, float g) { return g * free_logistic(free_gate_arg(act, g)); }
-// derivative from the logistic value s: s + g s (1 - s) d(arg)/dg
+// derivative from the logistic value s: s + g s (1 - s) d(arg)/dg.  Beyond |g| = 20 s is 0 or 1 and the second term 0; its last factor
+// is kept finite (the square of 2e19 is not, and 0 times infinity is NaN).
 __device__ __forceinline__ float free_gate_slope(int act, float g, float s) {
-    const float d = act == FREE_ACT_SILU ? 1.f : FREE_GELU_2K * (1.f + 3.f * FREE_GELU_C * g * g);
+    const float d = act == FREE_ACT_SILU ? 1.f : FREE_GELU_2K * fminf(1.f + 3.f * FREE_GELU_C * g * g, 1e7f);
     return s + g * s * (1.f - s) * d;
 }
 
