@@ -18,6 +18,7 @@ enum { GATED = 0, DX = 1, DW = 2 };
 
 constexpr int TN = 128, TK = 16;
 constexpr int kSms = 148;
+constexpr int kMaxGridY = 65535;           // column tiles of a launch
 
 struct Args {
     int M, N, depth;                       // output rows and columns (GATED: N = F), contraction
@@ -27,6 +28,7 @@ struct Args {
     int act, F;
     float *out, *pre;                      // GATED: pre [M, 2F] or nullptr
     int parts; long long plane;            // elements between the parts
+    int tile_n0;                           // first column tile of the launch
 };
 
 // Two multiply-adds as one instruction (each rounded as fmaf): the FMA pipe is fed with half the issue slots.
@@ -123,7 +125,7 @@ __device__ __forceinline__ void gated_simt_tile(const Args& a) {
     float (*As)[TK][TM + 4] = reinterpret_cast<float (*)[TK][TM + 4]>(smem);
     float (*Bs)[TK][TN + 4] = reinterpret_cast<float (*)[TK][TN + 4]>(smem + 2 * TK * (TM + 4));
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    const int m0 = blockIdx.x * TM, n0 = blockIdx.y * HALF;
+    const int m0 = blockIdx.x * TM, n0 = (a.tile_n0 + blockIdx.y) * HALF;
     const int kbeg = (int)((long long)a.depth * blockIdx.z / a.parts), kend = (int)((long long)a.depth * (blockIdx.z + 1) / a.parts);
     // parts begin at multiples of four so that 16-byte reads along the contraction stay aligned
     const int k0 = kbeg / 4 * 4, k1 = blockIdx.z + 1 == a.parts ? kend : kend / 4 * 4;
@@ -222,21 +224,23 @@ template <bool VEC, int S> __global__ void __launch_bounds__(128) __cluster_dims
 }
 
 template <int MODE>
-int launch(const Args& a, bool vec, cudaStream_t s) {
+int launch(Args a, bool vec, cudaStream_t s) {
     constexpr int cols = MODE == GATED ? TN / 2 : TN;
     const long long nn = (a.N + cols - 1) / cols, m128 = ((long long)a.M + 127) / 128, m64 = ((long long)a.M + 63) / 64;
-    if (nn > 65535) return FREE_ERR_UNSUPPORTED;
     // time of a wave in 64-row units; equal: the larger tile (fewer shared-memory reads per product)
     const long long w128 = 2 * ((m128 * nn * a.parts + kSms - 1) / kSms), w64 = (m64 * nn * a.parts + kSms - 1) / kSms;
-    const dim3 grid((unsigned)(w64 < w128 ? m64 : m128), (unsigned)nn, (unsigned)a.parts);
-    if (w64 < w128) {
-        if (vec) gated_simt_kernel<MODE, 64, true><<<grid, 128, 0, s>>>(a);
-        else gated_simt_kernel<MODE, 64, false><<<grid, 128, 0, s>>>(a);
-    } else {
-        if (vec) gated_simt_kernel<MODE, 128, true><<<grid, 256, 0, s>>>(a);
-        else gated_simt_kernel<MODE, 128, false><<<grid, 256, 0, s>>>(a);
+    for (a.tile_n0 = 0; a.tile_n0 < nn; a.tile_n0 += kMaxGridY) {
+        const dim3 grid((unsigned)(w64 < w128 ? m64 : m128), (unsigned)(nn - a.tile_n0 < kMaxGridY ? nn - a.tile_n0 : kMaxGridY), (unsigned)a.parts);
+        if (w64 < w128) {
+            if (vec) gated_simt_kernel<MODE, 64, true><<<grid, 128, 0, s>>>(a);
+            else gated_simt_kernel<MODE, 64, false><<<grid, 128, 0, s>>>(a);
+        } else {
+            if (vec) gated_simt_kernel<MODE, 128, true><<<grid, 256, 0, s>>>(a);
+            else gated_simt_kernel<MODE, 128, false><<<grid, 256, 0, s>>>(a);
+        }
+        FREE_TRY(free_check_launch());
     }
-    return free_check_launch();
+    return FREE_OK;
 }
 
 }  // namespace

@@ -34,3 +34,36 @@ def test_gradients_of_gates_far_out(act, dt):
     half = torch.finfo(DT[dt]).eps / 2
     assert (np.abs(dw[F:].double().cpu().numpy() - (M * step * a)[:, None]) <= (2.0 ** -21 + half) * (M * step * a)[:, None]).all()
     assert not dx.any() and not torch.isnan(dx).any()
+
+
+def test_fp32_columns_past_a_grid_dimension():
+    # 65536 column tiles and more; a contraction of four terms: off by at most 12 units of 2^-24 of the terms' sizes, the
+    # activation by (16 + 1.2 |argument|) 2^-23 besides (the bounds of the operator's other tests)
+    import paper_2511_20390_b200 as free
+    U = 2.0 ** -24
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    M, F, K = 26, 64 * 65536 + 5, 4                                # forward: 64 columns of each half per tile
+    x, w, b = rnd(M, K), rnd(2 * F, K), rnd(2 * F)
+    h, pre = free.op_gated_linear(x, w, b, want_preact=True)
+    for lo, hi in ((0, 100000), (F - 100000, F)):
+        rows = torch.cat([torch.arange(lo, hi), torch.arange(F + lo, F + hi)]).cuda()
+        size = x.double().abs() @ w[rows].double().abs().t() + b[rows].double().abs()
+        z = x.double() @ w[rows].double().t() + b[rows].double()
+        assert ((pre[:, rows].double() - z).abs() <= 12 * U * size).all()
+        n = hi - lo
+        zg, zu = z[:, :n], z[:, n:]
+        tol = 1.2 * 12 * U * size[:, :n] * (zu.abs() + 12 * U * size[:, n:]) + zg.abs() * 12 * U * size[:, n:] + (16 + 1.2 * zg.abs()) * 2 * U * (zg * zu).abs()
+        assert ((h[:, lo:hi].double() - zg * torch.sigmoid(zg) * zu).abs() <= tol + 1e-37).all()
+    del w, b, h, pre
+    M, F, K = 3, 2, 128 * 65536 + 77                               # backward: 128 columns per tile of dx and of dw
+    x, w, pre, dh = rnd(M, K), rnd(2 * F, K), rnd(M, 2 * F), rnd(M, F)
+    dx, dw, db = free.op_gated_linear_bwd(x, w, pre, dh)
+    zg, zu = pre[:, :F].double(), pre[:, F:].double()
+    s = torch.sigmoid(zg)
+    dz = torch.cat([dh.double() * zu * (s + zg * s * (1 - s)), dh.double() * zg * s], 1)
+    err = (16 + 1.2 * torch.cat([zg, zg], 1).abs()) * 2 * U * torch.cat([(dh.double() * zu).abs() * (1 + 1.2 * zg.abs()), (dh.double() * zg).abs()], 1)
+    for got, a, e, m in ((dx, dz, err, w), (dw, dz.t(), err.t(), x)):
+        ref, size = a @ m.double(), (a.abs() + e) @ m.double().abs()
+        assert ((got.double() - ref).abs() <= e @ m.double().abs() + 12 * U * size + 1e-37).all()
+    assert ((db.double() - dz.sum(0)).abs() <= (err + 12 * U * dz.abs()).sum(0)).all()
