@@ -5,6 +5,7 @@ the current stream.  Nothing here computes any part of the method.
 """
 import ctypes as C
 import os
+import threading
 from operator import index
 
 import numpy as np
@@ -780,6 +781,7 @@ def op_rope_axes(x, pos, axis_dims, base=10000.0, pairing="interleaved", joint_f
 
 ACTIVATIONS = {"silu": 0, "gelu": 1}
 _ERROR_WORDS = {}
+_ERROR_WORDS_LOCK = threading.Lock()
 
 
 def _error_word(device):
@@ -787,12 +789,15 @@ def _error_word(device):
     wait gave up, never cleared in between (so calls on several streams and replays of captured graphs may share it)."""
     w = _ERROR_WORDS.get(device)
     if w is None:
-        with torch.cuda.device(device):
-            if torch.cuda.is_current_stream_capturing():
-                raise RuntimeError("call the operator once on this device before capturing it into a CUDA graph")
-            w = torch.zeros(1, dtype=torch.int32, device="cuda")
-            torch.cuda.current_stream().synchronize()              # zero before any other stream can use it
-        _ERROR_WORDS[device] = w
+        with _ERROR_WORDS_LOCK:                                    # threads that come first at once share one word
+            w = _ERROR_WORDS.get(device)
+            if w is None:
+                with torch.cuda.device(device):
+                    if torch.cuda.is_current_stream_capturing():
+                        raise RuntimeError("call the operator once on this device before capturing it into a CUDA graph")
+                    w = torch.zeros(1, dtype=torch.int32, device="cuda")
+                    torch.cuda.current_stream().synchronize()      # zero before any other stream can use it
+                _ERROR_WORDS[device] = w
     return w
 
 

@@ -56,3 +56,33 @@ def test_axis_widths_past_32_bits_are_refused():
         free.op_rope_axes(torch.zeros(1, 3, 2, 8), torch.zeros(3, 1), (FAR + 8,))
     with pytest.raises(ValueError, match="axis_dims"):
         free.op_rope_axes(torch.zeros(1, 3, 2, 8), torch.zeros(3, 2), (4, 4 - FAR))
+
+
+def test_threads_that_come_first_share_one_error_word(monkeypatch):
+    # a word that is made twice is lost once, with what a kernel reports in it; torch's part is played by fakes
+    import contextlib
+    import threading
+    import time
+    from types import SimpleNamespace
+    from paper_2511_20390_b200 import binding
+    made = []
+
+    def zeros(*args, **kw):
+        time.sleep(0.05)
+        made.append(torch.empty(1, dtype=torch.int32))
+        return made[-1]
+    stream = SimpleNamespace(synchronize=lambda: None)
+    cuda = SimpleNamespace(device=lambda d: contextlib.nullcontext(), is_current_stream_capturing=lambda: False, current_stream=lambda: stream)
+    monkeypatch.setattr(binding, "torch", SimpleNamespace(zeros=zeros, cuda=cuda, int32=torch.int32))
+    monkeypatch.setattr(binding, "_ERROR_WORDS", {})
+    got = [None] * 4
+
+    def first(i):
+        got[i] = binding._error_word(i % 2)
+    threads = [threading.Thread(target=first, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(made) == 2 and got[0] is got[2] and got[1] is got[3] and got[0] is not got[1]
+    assert binding._ERROR_WORDS == {0: got[0], 1: got[1]}
