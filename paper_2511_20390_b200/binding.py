@@ -709,6 +709,8 @@ def op_layer_norm(x, weight=None, bias=None, rows_per_group=None, unit_offset=Fa
         ys = D
     else:
         yc, ys = _code(out.dtype), _rows(out, M, D, "out")
+        if out_dtype is not None and _code(out_dtype) != yc:
+            raise ValueError("out_dtype: out has another type")
     stats = x.new_empty((M, 2), dtype=torch.float32) if want_stats else None
     _launch("free_op_layer_norm", dev, xc, yc, groups, rows, D, x.data_ptr(), xs, _adr(weight), _adr(bias), ms, 1 if unit_offset else 0, eps,
             out.data_ptr(), ys, _adr(stats))

@@ -67,3 +67,13 @@ def test_fp32_columns_past_a_grid_dimension():
         ref, size = a @ m.double(), (a.abs() + e) @ m.double().abs()
         assert ((got.double() - ref).abs() <= e @ m.double().abs() + 12 * U * size + 1e-37).all()
     assert ((db.double() - dz.sum(0)).abs() <= (err + 12 * U * dz.abs()).sum(0)).all()
+
+
+def test_out_dtype_beside_out():
+    import paper_2511_20390_b200 as free
+    x = torch.randn(3, 64, device="cuda")
+    out = torch.empty(3, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="out_dtype"):
+        free.op_layer_norm(x, out=out, out_dtype=torch.float32)
+    assert free.op_layer_norm(x, out=out, out_dtype=torch.bfloat16) is out
+    assert torch.equal(out, free.op_layer_norm(x, out_dtype=torch.bfloat16))
