@@ -667,6 +667,58 @@ def _rows(t, M, D, what):
     return t.stride(0) if M > 1 else max(D, t.stride(0))
 
 
+def _layout(t):
+    """(size, stride) of the axes that a tensor's addresses depend on, and the elements from its first to behind its last."""
+    axes = [(n, s) for n, s in zip(t.shape, t.stride()) if n > 1]
+    return axes, 1 + sum((n - 1) * s for n, s in axes)
+
+
+def _meet(a, b):
+    """Whether two tensors share memory.  Exact where both fill their range or are laid out alike (nested strides, as views
+    of a matrix have); False where the layouts cannot be compared."""
+    if a.numel() == 0 or b.numel() == 0:
+        return False
+    (la, na), (lb, nb) = _layout(a), _layout(b)
+    pa, pb, size = a.data_ptr(), b.data_ptr(), a.element_size()
+    if pa + na * size <= pb or pb + nb * b.element_size() <= pa:
+        return False
+    if na == a.numel() and nb == b.numel():
+        return True
+    if la != lb or a.dtype != b.dtype:
+        return False
+    apart, rest = divmod(pb - pa, size)
+    if rest:
+        return True
+    left = {apart}                                                 # the distance, less whole steps along one axis after the other
+    for n, s in sorted(la, key=lambda v: -v[1]):
+        if s > 0:
+            left = {d - k * s for d in left for k in (d // s, d // s + 1) if abs(k) < n}
+    return 0 in left
+
+
+def _end(t):
+    """Address behind a tensor's last element."""
+    return t.data_ptr() + (t.nbytes if t.is_contiguous() else _layout(t)[1] * t.element_size())
+
+
+def _apart(out, what, over, *others):
+    """Refuses a result that the caller gave and that shares memory with an input; `over` are the inputs that it may replace
+    element for element."""
+    lo, hi = out.data_ptr(), None
+    for i, t in enumerate(over + others):
+        if t is None or (i < len(over) and (t is out or (t.data_ptr() == lo and t.dtype == out.dtype and t.shape == out.shape and t.stride() == out.stride()))):
+            continue
+        if hi is None:
+            hi = _end(out)
+        p = t.data_ptr()
+        if p >= hi or (p < lo and _end(t) <= lo):                  # the usual case, found out cheaply
+            continue
+        if i < len(over) and p == lo and t.dtype == out.dtype and _layout(t) == _layout(out):      # strides of single entries differ
+            continue
+        if _meet(out, t):
+            raise ValueError(f"{what}: overlaps an input")
+
+
 def _group_rows(t, groups, D, what):
     """Group stride of a [D] or [groups, D] fp32 table (rows of an adaLN table may be far apart)."""
     n = t.dim()
@@ -711,6 +763,7 @@ def op_layer_norm(x, weight=None, bias=None, rows_per_group=None, unit_offset=Fa
         yc, ys = _code(out.dtype), _rows(out, M, D, "out")
         if out_dtype is not None and _code(out_dtype) != yc:
             raise ValueError("out_dtype: out has another type")
+        _apart(out, "out", (x,), weight, bias)
     stats = x.new_empty((M, 2), dtype=torch.float32) if want_stats else None
     _launch("free_op_layer_norm", dev, xc, yc, groups, rows, D, x.data_ptr(), xs, _adr(weight), _adr(bias), ms, 1 if unit_offset else 0, eps,
             out.data_ptr(), ys, _adr(stats))
@@ -732,6 +785,8 @@ def op_layer_norm_bwd(x, dy, stats, weight=None, rows_per_group=None, unit_offse
         raise ValueError("dres, dx: expected x's dtype")
     if dx is None:
         dx = _like(x, x.dtype)
+    else:
+        _apart(dx, "dx", (x, dy, dres), stats, weight)
     dw = stats.new_empty((groups, D)) if want_dweight else None
     db = stats.new_empty((groups, D)) if want_dbias else None
     need = lib().free_op_layer_norm_bwd_workspace_bytes(groups, rows, D) if want_dweight or want_dbias else 0
@@ -774,6 +829,7 @@ def op_rope_axes(x, pos, axis_dims, base=10000.0, pairing="interleaved", joint_f
     else:
         if out.shape != shape or out.dtype != x.dtype or (d_head > 1 and out.stride(3) != 1):
             raise ValueError("out: expected x's shape and dtype with dense heads")
+        _apart(out, "out", (x,))
         ys = out.stride()
     _launch("free_op_rope_axes", dev, _code(x.dtype), ROPE_PAIRING[pairing], 1 if joint_freq else 0, 1 if inverse else 0, n_seq, n_tok, heads,
             d_head, n_axes, _AXES[n_axes](*axis_dims), base, pos.data_ptr(), n_tok * n_axes if pos.dim() == 3 else 0,
@@ -837,6 +893,7 @@ def op_gated_linear(x, w, bias=None, act="silu", want_preact=False, out=None):
         out = x.new_empty((M, F))
     else:
         _dense(out, dtype, (M, F), "out")
+        _apart(out, "out", (), x, w, bias)
     pre = x.new_empty((M, 2 * F)) if want_preact else None
     _launch("free_op_gated_linear", dev, code, ACTIVATIONS[act], M, F, K, x.data_ptr(), w.data_ptr(), _adr(bias), out.data_ptr(), _adr(pre),
             _error_word(dev).data_ptr() if code == FREE_BF16 else None)

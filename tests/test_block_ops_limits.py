@@ -86,3 +86,43 @@ def test_threads_that_come_first_share_one_error_word(monkeypatch):
         t.join()
     assert len(made) == 2 and got[0] is got[2] and got[1] is got[3] and got[0] is not got[1]
     assert binding._ERROR_WORDS == {0: got[0], 1: got[1]}
+
+
+def test_shared_elements_are_found():
+    # against the sets of element addresses, for pairs of views of one buffer as results and inputs are
+    from paper_2511_20390_b200.binding import _meet
+    rng = np.random.default_rng(3)
+    buf = torch.zeros(4000)
+    base = buf.data_ptr()
+
+    def addresses(t):
+        idx = np.zeros(1, np.int64) + (t.data_ptr() - base)
+        for n, s in zip(t.shape, t.stride()):
+            idx = (idx[:, None] + np.arange(n) * s * t.element_size()).reshape(-1)
+        return set((idx[:, None] + np.arange(t.element_size())).reshape(-1).tolist())
+    met = apart = 0
+    for _ in range(3000):
+        kind = rng.integers(4)
+        if kind == 0:                                              # dense matrices anywhere
+            M, D = int(rng.integers(1, 12)), int(rng.integers(1, 20))
+            a, b = (buf[o:o + M * D].view(M, D) for o in rng.integers(0, 400, 2).tolist())
+        elif kind == 1:                                            # rows with gaps, columns beside one another
+            M, D, s = int(rng.integers(1, 8)), int(rng.integers(1, 10)), int(rng.integers(10, 30))
+            a, b = (buf.as_strided((M, D), (s, 1), o) for o in rng.integers(0, 60, 2).tolist())
+        elif kind == 2:                                            # heads inside a packed projection, either order of strides
+            n, t, h, d = rng.integers(1, 5, 4).tolist()
+            H = 3 * h
+            o = rng.integers(0, 2 * h + 1, 2).tolist()
+            a, b = (buf[:n * t * H * d].view(n, t, H, d)[:, :, q:q + h] for q in o)
+            if rng.random() < 0.5:
+                a, b = a.transpose(1, 2), b.transpose(1, 2)
+        else:                                                      # dense, of different types
+            n, (p, q) = int(rng.integers(1, 50)), rng.integers(0, 120, 2).tolist()
+            a, b = buf[p:p + n], buf.view(torch.bfloat16)[2 * q:2 * q + n]
+        want = bool(addresses(a) & addresses(b))
+        assert _meet(a, b) == want and _meet(b, a) == want, (kind, a.shape, a.stride(), b.shape, b.stride(), a.data_ptr() - base, b.data_ptr() - base)
+        met += want; apart += not want
+    assert met > 500 and apart > 500
+    assert not _meet(buf[:0], buf) and not _meet(buf[:8].view(8, 1)[:, :0], buf[:8].view(8, 1))
+    # broadcast inputs, and layouts that cannot be compared: not called shared
+    assert _meet(buf[3:4].expand(5), buf[:8].view(8)[3:4].expand(5)) and not _meet(buf.as_strided((3, 2), (5, 1)), buf.as_strided((2, 2), (7, 1), 2))

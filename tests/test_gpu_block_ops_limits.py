@@ -77,3 +77,47 @@ def test_out_dtype_beside_out():
         free.op_layer_norm(x, out=out, out_dtype=torch.float32)
     assert free.op_layer_norm(x, out=out, out_dtype=torch.bfloat16) is out
     assert torch.equal(out, free.op_layer_norm(x, out_dtype=torch.bfloat16))
+
+
+def test_results_that_overlap_an_input_are_refused():
+    import paper_2511_20390_b200 as free
+    buf = torch.randn(200 * 64, device="cuda")
+    x, dy = buf[:100 * 64].view(100, 64), torch.randn(100, 64, device="cuda")
+    want, st = free.op_layer_norm(x, want_stats=True)
+    kept = buf.clone()
+    for at in (64, 4, 99 * 64):                                    # rows or a few elements further on
+        out = buf[at:at + 100 * 64].view(100, 64)
+        with pytest.raises(ValueError, match="overlap"):
+            free.op_layer_norm(x, out=out)
+        with pytest.raises(ValueError, match="overlap"):
+            free.op_layer_norm_bwd(x, dy, st, dx=out)
+        with pytest.raises(ValueError, match="overlap"):
+            free.op_layer_norm_bwd(dy, x, st, dx=out)
+        with pytest.raises(ValueError, match="overlap"):
+            free.op_layer_norm_bwd(dy, dy, st, dres=x, dx=out)
+    with pytest.raises(ValueError, match="overlap"):               # the same place, another type
+        free.op_layer_norm(x, out=buf.view(torch.bfloat16)[:100 * 64].view(100, 64))
+    with pytest.raises(ValueError, match="overlap"):
+        free.op_layer_norm(x, buf[:64], out=x)                     # the weight is one of the rows
+    pos = torch.arange(10, dtype=torch.float32, device="cuda")[:, None]
+    qkv = torch.randn(2, 10, 6, 16, device="cuda")
+    for lo, hi in ((1, 5), (2, 6)):
+        with pytest.raises(ValueError, match="overlap"):
+            free.op_rope_axes(qkv[:, :, :4], pos, (16,), out=qkv[:, :, lo:hi])
+    w, h = torch.randn(2 * 64, 64, device="cuda"), torch.empty(100, 64, device="cuda")
+    for out in (x, buf[64:101 * 64].view(100, 64)):
+        with pytest.raises(ValueError, match="overlap"):
+            free.op_gated_linear(x, w, out=out)
+    with pytest.raises(ValueError, match="overlap"):
+        free.op_gated_linear(x, w, out=w[:100])
+    assert torch.equal(buf, kept)
+    # beside one another in one buffer, and element for element over an input
+    assert torch.equal(free.op_layer_norm(x, out=buf[100 * 64:].view(100, 64)), want)
+    two = torch.zeros(100, 128, device="cuda")
+    two[:, :64] = x
+    assert torch.equal(free.op_layer_norm(two[:, :64], out=two[:, 64:]), want) and torch.equal(two[:, :64], x)
+    rot = free.op_rope_axes(qkv[:, :, :2], pos, (16,))
+    assert torch.equal(free.op_rope_axes(qkv[:, :, :2], pos, (16,), out=qkv[:, :, 2:4]), rot)
+    assert torch.equal(free.op_rope_axes(qkv[:, :, :2], pos, (16,), out=qkv[:, :, :2]), rot)
+    assert torch.equal(free.op_gated_linear(x, w, out=h), free.op_gated_linear(x, w))
+    assert torch.equal(free.op_layer_norm(x, out=x), want)
