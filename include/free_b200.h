@@ -470,17 +470,20 @@ int free_op_ln_modulate(int out_dtype, int M, int D, int rows_per_seq, const flo
  *   act        FREE_ACT_SILU: g / (1 + e^-g);  FREE_ACT_GELU: 0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
  *   x          DEVICE [M, K]; M = 0 is allowed and does nothing
  *   w          DEVICE [2F, K];  bias  DEVICE fp32 [2F] or NULL
- *   h          DEVICE [M, F], computed from the fp32 accumulators
+ *   h          DEVICE [M, F], computed from the fp32 accumulators (bf16: the activation's logistic function from
+ *              fast instructions, off by (8 + 1.2 |its argument|) 2^-23 of the value)
  *   preact     DEVICE [M, 2F] or NULL: z, rounded to dtype, what the backward pass needs
  *   device_error   DEVICE uint32, OR-ed into when a bounded device-side wait gave up (clear it first; not used and may be
- *              NULL for FREE_FP32).  Calls on several streams may share one
+ *              NULL for FREE_FP32).  The outputs are then invalid, and nothing else tells: read the word after synchronising.
+ *              Calls on several streams may share one
  * No workspace.  h and preact must not overlap the inputs.  Errors: ARG, SHAPE, ALIGN, UNSUPPORTED, CUDA.
  *
  * free_op_gated_linear_bwd -- its gradients, from dh and the preact that the forward call kept:
  *     dz = [dh z_up act'(z_gate), dh act(z_gate)],   dx = dz W,   dw = dz^T x,   dbias = sum over rows of dz
  *   dh         DEVICE `dtype` [M, F]
  *   dx, dw     DEVICE `dtype` [M, K], [2F, K];  dbias  DEVICE fp32 [2F].  Each may be NULL (w is read for dx only, x for dw
- *              only) and is overwritten; with M = 0 dw and dbias become zero.  In bf16 dz is rounded to bf16 for the products.
+ *              only) and is overwritten; with M = 0 dw and dbias become zero.  In bf16 dz is rounded to bf16 for the products (the
+ *              gradients are then off by 2.3e-3 in the 2-norm, where their own rounding is 1.7e-3).
  *              They must not overlap the inputs, the workspace or one another
  *   ws         DEVICE, >= free_op_gated_linear_bwd_workspace_bytes() (HOST-only): dz and the parts of split sums.  Calls that
  *              may overlap on the GPU need one each
@@ -503,11 +506,13 @@ int free_op_gated_linear_bwd(int dtype, int act, int M, int F, int K, const void
  *   x_dtype, y_dtype   FREE_FP32 or FREE_BF16, in any combination; statistics are fp32
  *   n_groups, rows_per_group   M = n_groups * rows_per_group rows; M = 0 is allowed and does nothing
  *   x, y       DEVICE [M, D], rows x_stride / y_stride (>= D) elements apart; elements between the rows are not touched.
- *              y may be x where the types and strides are the same
+ *              The first row is 16-byte aligned as every DEVICE pointer, the others may lie anywhere.
+ *              y may be x where the types and strides are the same, and must not overlap it otherwise
  *   weight     DEVICE fp32, element (g, c) at weight[g * mod_stride + c], or NULL for 1; unit_offset non-zero: 1 is added to it
  *   bias       DEVICE fp32, laid out as weight, or NULL for 0
  *   stats      DEVICE fp32 [M, 2] or NULL: mu and r of every row, what the backward pass needs
  * No workspace.  weight, bias and stats need 4-byte alignment only.  A row with an infinity or NaN gives NaN, as the formula.
+ * Sums of squares are fp32: deviations from the mean of up to 1e17 are handled, larger ones overflow (r = 0, y = b).
  * D % 4 == 0 with strides that are multiples of four elements is the fast form (and 16-byte aligned weight and bias rows).
  * Errors: ARG, SHAPE, ALIGN, UNSUPPORTED (D > 8192), CUDA.
  *
@@ -516,7 +521,8 @@ int free_op_gated_linear_bwd(int dtype, int act, int M, int F, int K, const void
  *   dy         DEVICE y_dtype [M, D], rows dy_stride apart
  *   dres       DEVICE x_dtype [M, D], rows dres_stride apart, or NULL: the gradient that reaches x on another path (a
  *              residual connection), added before dx is rounded
- *   dx         DEVICE x_dtype [M, D], rows dx_stride apart; may be dres, x or dy where type and stride are the same
+ *   dx         DEVICE x_dtype [M, D], rows dx_stride apart; may be dres, x or dy where type and stride are the same,
+ *              and must not overlap them otherwise
  *   dweight, dbias   DEVICE fp32, element (g, c) at [g * dmod_stride + c]; either may be NULL.  Overwritten, zero for a group
  *              without rows.  With unit_offset dweight is the gradient of the stored offset
  *   ws         DEVICE, >= free_op_layer_norm_bwd_workspace_bytes() (0 for few rows; HOST-only function), not needed when both

@@ -742,7 +742,8 @@ def op_layer_norm(x, weight=None, bias=None, rows_per_group=None, unit_offset=Fa
     """Layer norm of the rows of x (CUDA fp32 or bf16 [M, D], dense rows any distance apart) with a weight and bias (fp32 [D],
     or [groups, D] for groups of `rows_per_group` consecutive rows; unit_offset: the weight is stored as an offset from one, as
     adaLN's scale).  Returns y [M, D] in out_dtype (default: x's), and with want_stats also (mean, 1 / sqrt(var + eps)) as fp32
-    [M, 2], what op_layer_norm_bwd needs."""
+    [M, 2], what op_layer_norm_bwd needs.  x and out begin on 16 bytes; weight and bias rows of several groups lie the same distance
+    apart; out may be x.  Like all operators here it records nothing for autograd."""
     if x.dim() != 2:
         raise ValueError("x: expected a matrix")
     M, D = x.shape
@@ -773,7 +774,8 @@ def op_layer_norm(x, weight=None, bias=None, rows_per_group=None, unit_offset=Fa
 def op_layer_norm_bwd(x, dy, stats, weight=None, rows_per_group=None, unit_offset=False, dres=None, want_dweight=True, want_dbias=True,
                       dx=None):
     """Gradients of op_layer_norm from dy [M, D] and the stats it kept.  dres: gradient of x from another path, added to dx.
-    Returns (dx in x's dtype, dweight, dbias), the last two fp32 [groups, D], or None where not wanted."""
+    Returns (dx in x's dtype, dweight, dbias), the last two fp32 [groups, D], or None where not wanted; a weight that all groups share
+    has their sum as its gradient (or one group, of all rows).  dx may be x, dy or dres."""
     if x.dim() != 2:
         raise ValueError("x: expected a matrix")
     M, D = x.shape
@@ -879,7 +881,8 @@ def op_gated_linear(x, w, bias=None, act="silu", want_preact=False, out=None):
     """First half of a gated feed-forward layer, h = act(z[:, :F]) * z[:, F:] with z = x w^T + bias, in one kernel.  x: CUDA
     fp32 or bf16 [M, K]; w [2F, K], the gate rows and then the up rows; bias fp32 [2F]; act "silu" or "gelu" (tanh form).
     bf16 needs F and K to be multiples of 8.  Returns h [M, F], and with want_preact also z [M, 2F], what op_gated_linear_bwd
-    needs.  Asynchronous: op_device_error() tells whether a device-side wait gave up."""
+    needs.  Tensors are contiguous and begin on 16 bytes.  Asynchronous: op_device_error() tells whether a device-side wait gave
+    up, in which case the outputs are invalid."""
     if x.dim() != 2 or w.dim() != 2 or w.shape[0] % 2:
         raise ValueError("x, w: expected matrices, w with an even number of rows")
     if act not in ACTIVATIONS:
@@ -902,7 +905,7 @@ def op_gated_linear(x, w, bias=None, act="silu", want_preact=False, out=None):
 
 def op_gated_linear_bwd(x, w, preact, dh, act="silu", want_dx=True, want_dw=True, want_dbias=True):
     """Gradients of op_gated_linear from dh [M, F] and the preact it kept.  Returns (dx [M, K], dw [2F, K], both in x's dtype,
-    dbias fp32 [2F]), None where not wanted."""
+    dbias fp32 [2F]), None where not wanted.  Asynchronous as the forward call: op_device_error()."""
     if x.dim() != 2 or w.dim() != 2 or w.shape[0] % 2:
         raise ValueError("x, w: expected matrices, w with an even number of rows")
     if act not in ACTIVATIONS:

@@ -9,8 +9,10 @@
 #define FREE_GELU_C  0.044715f
 
 __device__ __forceinline__ float free_logistic(float v) { return 1.f / (1.f + expf(-v)); }
-// The same from the fast exponential and division (a few units of 2^-22): for results that are rounded to bf16.
-// e^-v overflows to infinity for v < -88 and the reciprocal is 0, the limit.
+// The same from the fast exponential and reciprocal, for the bf16 mode: off by at most (8 + 1.2 |v|) 2^-23 of the value (the
+// exponential's argument is rounded after its scaling by log2 e, so its error grows with |v|).  Everything that is rounded to bf16 (half a step:
+// 2^-8) uses it, and so does the bias gradient of that mode, whose terms come from the same pass: it is fp32 but holds this
+// error.  e^-v overflows to infinity for v < -88 and the reciprocal is 0, the limit.
 __device__ __forceinline__ float free_logistic_fast(float v) {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-v)));

@@ -16,8 +16,8 @@
 //   - Few tiles and a long contraction (DW over many rows of a small layer, DX over few rows) are split along the
 //     contraction; the fp32 parts go to the workspace and are added in order, so repeats are bit-identical.
 // Bound by the tensor pipe and the power cap except for few rows.  24576 rows, F = 4608, K = 1152 (0.52 TFLOP per product): forward
-// without z 340 us in a burst, 395 under sustained load (1.32 PFLOP/s; a library product of that size 423), with z 406 and
-// 459 us (the 453 MB more to HBM are not hidden); DX and DW 350 us each in a burst.
+// without z 340 us in a burst, 395 to 413 under sustained load (1.32 to 1.26 PFLOP/s; a library product of that size 423), with z 406
+// and 459 to 476 us (the 453 MB more to HBM are not hidden); DX and DW 350 us each in a burst.
 #include "gated.h"
 #include "tc_common.cuh"
 

@@ -7,12 +7,16 @@
 // Both directions are one pass over the data and bound by HBM: every row is read once.  Statistics are fp32: each warp takes
 // the mean of its own columns and their squared deviations from it, and the parts are combined with the exact formula
 // M2 = sum M2_k + n_k (mean_k - mean)^2, so that a large mean cancels nothing.
-// Forward: a warp holds a row in registers (up to 2048 columns; several warps beyond), so a row costs ten exchanges and no
-// barrier; the weight and bias of a group come from the L1.  24 x 1024 rows of 1152, fp32 to bf16, weight and bias per sequence:
-// 29.5 us, 5.8 TB/s (a CTA per row with a barrier each: 41 us); 6144 rows of 4608: 33 us.
+// Forward: where a warp can hold a row in registers it does, so that a row costs ten exchanges and no barrier: up to 2048 columns in
+// whole blocks of 128, 1280 of other widths, 768 in accesses of two columns, 256 of one; wider rows take the warps of a CTA
+// (launch_fwd).  With four columns per access the weight and bias of a group come from the L1, with fewer they stay in
+// registers.  24 x 1024 rows of 1152, fp32 to bf16, weight and bias per sequence: 31 us as calls on new inputs (5.5 TB/s), 27 without
+// the statistics, 25 where a replayed graph finds part of its one input in the L2; a CTA per row with a barrier each took 41.
+// 6144 rows of 4608: 33 us.
 // Backward: the column sums need registers too, so a row is spread over warps with 12 or 16 columns per lane and one
 // barrier; rows are copied to shared memory one ahead of their use, every thread its own columns, so that the bytes in flight do
-// not cost registers.  The same rows with the residual path's gradient added: 65 us, 6.1 TB/s, and 5 us for the sums.
+// not cost registers.  The same rows with the residual path's gradient added: 72 us as calls (5.5 TB/s), of which the kernel takes
+// 62 to 65 and the sums 5.
 // The gradients of w and b are column sums over a group's rows.  A CTA keeps them in fp32 registers over a run of rows of
 // one group and writes one partial row; a second, small launch adds the partial rows of a group in a fixed order, so that
 // repeats are bit-identical (no atomics).
@@ -274,7 +278,7 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
     const long long lo = base + (long long)a.rows_per_group * ch / a.chunks, hi = base + (long long)a.rows_per_group * (ch + 1) / a.chunks;
     const float inv_d = 1.f / (float)a.D;
     // shared memory: two groups of R rows, of each x, dres and dy, [warp][piece][lane]; running addresses, for the pass counts every
-    // instruction (24 x 1024 rows of 1152 bf16: 46.3 us, with products of row and stride 48.4)
+    // instruction (24 x 1024 rows of 1152 bf16, this kernel alone: 46.3 us, with products of row and stride 48.4)
     const uint32_t T0 = blockDim.x, bx = T0 * C * (uint32_t)sizeof(TX), one = 2 * bx + T0 * C * (uint32_t)sizeof(TY);
     const uint32_t place = warp * 32 * C + lane * VW;
     uint32_t now = (uint32_t)__cvta_generic_to_shared(ring), then = now + R * one;
@@ -608,8 +612,10 @@ __global__ void __launch_bounds__(512) layer_norm_reduce_kernel(const NormArgs a
 // Columns per lane of the backward kernel for wide rows.  It is bound by issue slots where the rows are bf16, and a row takes each of
 // its warps what 16 columns take besides (exchanges, addresses, the barrier): so the number whose warps cost least, 12 or 16.
 // 24 x 1024 rows of 1152 bf16: 48.6 us with 12, 61.6 with 8; 8192 rows of 4096: 53 with 16, 66 with 8.  Eight columns and two rows
-// per barrier: odd widths, which are not copied ahead, and those of which 16 leave an SM with one CTA of nine warps (8192 rows of
-// 4608, fp32 and bf16: 87 us; two such CTAs in fewer registers 95).
+// per barrier: odd widths, which are not copied ahead, and 4097 to 4608 columns, of which 16 would leave an SM with one CTA of nine
+// warps.  8192 rows of 4608 bf16: 77 us, with 16 columns 83 (fp32 rows, bf16 gradients: 102 and 99).  Beyond 4608 eight columns
+// would take more than 576 threads, whose registers hold one row instead of two: 8192 rows of 5000 bf16 114 us, with 16 columns 86
+// (fp32 115 and 106), of 8192 153 and 110 (162 and 150).
 int bwd_cols(int D) {
     if (D % 2 || (D > 4096 && D <= 4608)) return 8;
     const int w12 = (D + 383) / 384, w16 = (D + 511) / 512;
@@ -671,7 +677,9 @@ int start_narrow_bwd(const NormArgs& a, cudaStream_t s) {
 }
 
 // As many blocks of 128 columns per warp as the row needs (registers decide how many rows an SM holds), several warps beyond 2048
-// columns.  Widths that the blocks fill exactly have kernels without checks (24 x 1024 rows of 1152: 29.5 us, with checks 34).
+// columns.  Widths that the blocks fill exactly have kernels without checks (24 x 1024 rows of 1152: 29.5 us, with checks 34).  7, 11 and
+// 13 to 15 blocks have none as yet and take the kernels with checks, which costs them 24 x 1024 rows, fp32 / bf16 to bf16: 896 columns
+// 29 / 27 us, without checks 20 / 16; 1408 49 / 46, 33 / 25; 1664 66 / 61, 43 / 35; 1920 65 / 59, 49 / 39.
 // With checks a warp holds up to 1280 columns (20000 rows of 1300, fp32 to bf16: 35 us by three warps, 56 by one; of 700: 25 by
 // two, 18 by one); with one or two columns per access, where the tables need registers too, 256 (20000 rows of 1001, bf16: 35 us,
 // with all in one warp 60; 690 in pairs: 19 and 15).

@@ -9,8 +9,8 @@
 // streams the heads through it.  A thread keeps one slot (one vector of a head, or the two that it couples), so that the index
 // arithmetic is done once, and has kUnroll tokens' loads in flight.  The frequencies are formed on the host in fp64 and travel
 // as a kernel argument.
-// Measured on B200: 40 us for the 113 MB of queries and keys of 24 x 1024 tokens, 16 heads of 72, bf16 (5.6 TB/s read and
-// written), 73 us for the same in fp32 (6.2 TB/s).
+// Measured on B200: 41 us in a replayed graph, 43 as calls on new inputs, for the 113 MB of queries and keys of 24 x 1024 tokens,
+// 16 heads of 72, bf16 (5.5 and 5.3 TB/s read and written; in place 44), 73 us for the same in fp32 (6.2 TB/s).
 #include "internal.h"
 #include <math.h>
 
@@ -126,8 +126,8 @@ template <typename T, int V, bool HALVES, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads) rope_axes_kernel(const __grid_constant__ RopeArgs a) {
     constexpr int U = kUnroll<T, V, HALVES>;
     // Pairs of a slot: PV.  They lie in planes of two, [plane][token][slot group], so that a warp's 16-byte reads are one run
-    // (with a slot's pairs side by side they would be 32 bytes apart and meet in the same banks: 61 instead of 44 us for the
-    // queries and keys of 24 x 1024 tokens, 16 heads of 72, before the words stayed packed).
+    // (with a slot's pairs side by side they would be 32 bytes apart and meet in the same banks: 61 against 44 us for the
+    // queries and keys of 24 x 1024 tokens, 16 heads of 72, both in an older form that unpacked its words; this one takes 41).
     constexpr int PV = HALVES ? V : V / 2;
     __shared__ float4 table[kTableBytes / 16];
     free_grid_dep_wait();
@@ -285,7 +285,8 @@ extern "C" int free_op_rope_axes(int dtype, int pairing, int freq_mode, int inve
     a.y = y; a.ys = y_seq_stride; a.yt = y_tok_stride; a.yh = y_head_stride;
     a.sign = inverse ? -1.f : 1.f;
     const double two_pi = 6.283185307179586476925286766559;
-    // consecutive pairs differ by one factor: 128 products in fp64 are off by 128 units of 2^-53 at most, and cost less than 128 powers
+    // consecutive pairs differ by one factor.  Each product adds its own rounding (2^-53) and the factor's error (pow: 2^-52) once
+    // more, so the last of 128 is off by 3 x 128 units of 2^-53 at most: 4e-14, 4e-9 of a turn after 100000 turns.  128 powers cost more.
     int p = 0;
     double ratio = pow(base, -1.0 / a.pairs), t = 1.0 / two_pi;
     for (int ax = 0; ax < n_axes; ++ax) {
