@@ -622,8 +622,8 @@ int bwd_cols(int D) {
     return D <= 1536 && w12 * (12 + 16) < w16 * (16 + 16) ? 12 : 16;
 }
 // Threads of an SM that the registers are shared among, so that sums and rows stay in them (twelve columns: 640 and 768 threads are
-// 3 and 7% slower).  Sixteen columns of fp32 rows still spill 32 to 80 bytes per thread, and so do a few forward kernels whose third or
-// later CTA on an SM is worth more than that (4 to 72 bytes).
+// 3 and 7% slower).  Sixteen columns of fp32 rows still spill 32 to 80 bytes per thread, and so do a few forward kernels at their
+// numbers of CTAs per SM (4 to 72 bytes).
 constexpr int kBwdT = 512;
 int bwd_threads(int D) { return (D + 32 * bwd_cols(D) - 1) / (32 * bwd_cols(D)) * 32; }
 bool narrow(int D) { return D <= 128 || (D <= 256 && D % 2 == 0); }      // (single columns beyond 128: 32 us the wide way, 56 this)
