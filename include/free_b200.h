@@ -540,6 +540,50 @@ int free_op_layer_norm_bwd(int x_dtype, int y_dtype, int n_groups, int rows_per_
                            float* dweight, float* dbias, int64_t dmod_stride, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * free_op_rms_norm -- root-mean-square norm of rows, with the addition of a residual stream in front of it.  For row i, in group
+ * g = i / rows_per_group:
+ *     h_i = x_i + residual_i,   r = 1 / sqrt(mean(h_i^2) + eps),   y_i = h_i r w_g
+ * The norm is of the unrounded sum.  Rows may be the heads of tokens: row i is head i % heads of token i / heads.
+ *   x_dtype    FREE_FP32 or FREE_BF16;  y_dtype  FREE_FP32, FREE_BF16 or FREE_E4M3;  in any combination, sums are fp32
+ *   n_groups, rows_per_group   n_groups * rows_per_group rows, whole tokens; none is allowed and does nothing
+ *   x, y       DEVICE, element (token, head, c) at token * x_tok + head * x_head + c (y_tok, y_head), rows >= D elements
+ *              apart, aligned to their element; elements between the rows are not touched.  y may be x where types and strides are the same
+ *   residual   DEVICE `res_dtype` (FREE_FP32 or FREE_BF16), one row of D per row of x, res_stride apart, or NULL (h = x).  heads = 1 only
+ *   res_out    DEVICE `res_dtype`, rows res_out_stride apart, or NULL: h, rounded.  May be residual with its stride
+ *   weight     DEVICE fp32, element (g, c) at weight[g * mod_stride + c], or NULL for 1; unit_offset non-zero: 1 is added to it
+ *   scales     DEVICE fp32, for FREE_E4M3: y holds y_i / scale, rounded to nearest, where a row's run of scale_block columns (128, or
+ *              0: the row) shares the scale max |y_i| / 448, stored at scales[i * scale_stride + run] (scale 1 for runs without
+ *              anything above 2^-100, NaN for runs with a NaN).  heads = 1 only
+ *   rstd       DEVICE fp32 [rows] or NULL: r, what the backward pass needs
+ * Outputs must not overlap the inputs otherwise.  Squares are summed in fp32: rows of up to 1e18 are handled, larger ones overflow
+ * (r = 0).  D % 4 == 0 with strides and addresses that are multiples of four elements is the fast form.
+ * Errors: ARG, SHAPE, ALIGN, UNSUPPORTED (D > 8192), CUDA.
+ *
+ * free_op_rms_norm_bwd -- its gradients, from dy, the h and the r that the forward call kept.  With xh = h r, v = dy w:
+ *     dx = dres + r (v - xh mean(v xh)),   dweight_g = sum over the group's rows of dy xh
+ * dx is the gradient of x and of the residual alike.
+ *   h          DEVICE x_dtype: the sum, or x where there was no residual;  dy  DEVICE dy_dtype (an 8-bit result's gradient, too)
+ *   dres       DEVICE x_dtype or NULL: the gradient that reaches h on another path, added before dx is rounded
+ *   dx         DEVICE x_dtype; may be dres, h or dy where type and strides are the same
+ *   strides as in the forward call; heads > 1 takes heads of up to 128 columns (256 where D is even), or rows that lie evenly apart
+ *   dweight    DEVICE fp32, element (g, c) at [g * dmod_stride + c], or NULL.  Overwritten, zero for a group without rows
+ *   ws         DEVICE, >= free_op_rms_norm_bwd_workspace_bytes() (HOST-only; 0 for few rows), not needed without dweight.  Calls that
+ *              may overlap on the GPU need one each
+ * Sums run in a fixed order: repeats are bit-identical.  Errors as above, and WORKSPACE.
+ */
+#define FREE_E4M3 2   /* 8-bit results: 4 bits of exponent, 3 of mantissa, up to 448 */
+int free_op_rms_norm(int x_dtype, int res_dtype, int y_dtype, int n_groups, int rows_per_group, int heads, int D,
+                     const void* x, int64_t x_tok, int64_t x_head, const void* residual, int64_t res_stride,
+                     void* res_out, int64_t res_out_stride, const float* weight, int64_t mod_stride, int unit_offset, float eps,
+                     void* y, int64_t y_tok, int64_t y_head, float* scales, int64_t scale_stride, int scale_block, float* rstd, void* stream);
+size_t free_op_rms_norm_bwd_workspace_bytes(int n_groups, int rows_per_group, int D);
+int free_op_rms_norm_bwd(int x_dtype, int dy_dtype, int n_groups, int rows_per_group, int heads, int D,
+                         const void* h, int64_t h_tok, int64_t h_head, const void* dy, int64_t dy_tok, int64_t dy_head, const float* rstd,
+                         const float* weight, int64_t mod_stride, int unit_offset, const void* dres, int64_t dres_tok, int64_t dres_head,
+                         void* dx, int64_t dx_tok, int64_t dx_head, float* dweight, int64_t dmod_stride,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/*
  * free_op_rope_axes -- rotary positions with one to four axes (time, height, width) on the heads of a token: rotated pair p
  * of a head, which belongs to axis A(p), is turned by t = pos[token, A(p)] * freq(p):
  *     (a, b) -> (a cos t - b sin t, a sin t + b cos t);   inverse non-zero turns by -t, which is also the backward pass.
@@ -567,6 +611,62 @@ int free_op_rope_axes(int dtype, int pairing, int freq_mode, int inverse, int n_
                       int n_axes, const int32_t* axis_dims, double base, const float* pos, int64_t pos_seq_stride,
                       const void* x, int64_t x_seq_stride, int64_t x_tok_stride, int64_t x_head_stride,
                       void* y, int64_t y_seq_stride, int64_t y_tok_stride, int64_t y_head_stride, void* stream);
+
+/*
+ * free_op_cross_attention -- attention of a sequence's tokens to an encoder's states of another length.  Token t of sequence s
+ * and head h attends to the states j of encoder sequence e(s) that count, with key head h / (heads / kv_heads):
+ *     S_j = scale <q, k_j>,   p = softmax over those j of S,   out = sum_j p_j v_j,   lse = log sum_j e^(S_j)
+ * A token without any state gets out = 0 and lse = -infinity.  The shape and the inputs are one HOST struct:
+ *   q          DEVICE `dtype`, element (s, t, h, c) at s * q_seq + t * q_tok + h * q_head + c
+ *   k, v       DEVICE `dtype`, element (e, j, h, c) at e * k_seq + j * k_tok + h * k_head + c, so that both may lie inside one
+ *              packed projection; strides of 0 (a state that several share) are allowed
+ *   kv_lens    DEVICE int32 [n_enc] or NULL: states of each encoder sequence, taken as 0 .. n_kv (NULL: n_kv)
+ *   kv_offsets DEVICE int32 [n_enc + 1] or NULL.  Not NULL: the states lie one behind the other in kv_rows rows (k_seq and
+ *              v_seq are not used) and sequence e has the rows kv_offsets[e] .. kv_offsets[e + 1] - 1, at most n_kv of them;
+ *              parts outside 0 .. kv_rows - 1 do not count.  kv_lens has to be NULL
+ *   kv_mask    DEVICE, one byte per state, [n_enc, n_kv] or [kv_rows], or NULL: states with a zero do not count
+ *   kv_seq     DEVICE int32 [n_seq] or NULL: e(s), outside 0 .. n_enc - 1 for none.  NULL: n_seq is a multiple of n_enc, and
+ *              n_seq / n_enc consecutive sequences share one (the drafts of an image share its prompt)
+ *   dtype      FREE_FP32 (CUDA cores) or FREE_BF16 (tcgen05, fp32 accumulation and softmax; probabilities are rounded to bf16,
+ *              which their product takes).  bf16 inputs that are not 16-byte aligned in every stride, or whose d_head is no
+ *              multiple of 8, take the CUDA cores
+ *   d_head     up to 128, else UNSUPPORTED;  heads a multiple of kv_heads;  scale > 0
+ * What does not count is not used: NaN and infinities in it change nothing.
+ *   out        DEVICE `dtype`, strides (elements) like q's; must not overlap the inputs
+ *   lse        DEVICE fp32 [n_seq, heads, n_q] or NULL (the backward pass needs it)
+ *   ws         DEVICE, >= free_op_cross_attention_workspace_bytes() (HOST-only; often 0): parts of long state sequences where there
+ *              are few tokens, added in order.  Calls that may overlap on the GPU need one each
+ *   device_error   DEVICE uint32, OR-ed into when a bounded device-side wait gave up (not used and may be NULL for FREE_FP32)
+ * n_seq = 0 or n_q = 0 does nothing.  Errors: ARG, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE, CUDA.
+ *
+ * free_op_cross_attention_bwd -- its gradients, from dout and the out and lse that the forward call kept.  With p as above,
+ * dS_j = p_j (<dout, v_j> - <dout, out>) scale:
+ *     dq = sum_j dS_j k_j,   dk_j = sum of dS_j q,   dv_j = sum of p_j dout   over the tokens, heads and sequences that share j
+ *   out, dout, dq   DEVICE `dtype`, strides like q's;  dk, dv   DEVICE `dtype`, strides like k's
+ *              dq may be NULL, dk and dv may both be.  dq is overwritten; of dk and dv the rows of every encoder sequence
+ *              (padded: all n_kv, packed: those that kv_offsets names), zero where a state does not count or nothing attends
+ *              to it.  They must not overlap the inputs or one another.  In bf16 dS and p are rounded to bf16 for the products
+ *   ws         DEVICE, >= free_op_cross_attention_bwd_workspace_bytes() (HOST-only)
+ *   other arguments and errors as above.  Sums run in a fixed order: repeats are bit-identical.
+ */
+typedef struct free_cross_attn {
+    const void *q, *k, *v;
+    int64_t q_seq, q_tok, q_head, k_seq, k_tok, k_head, v_seq, v_tok, v_head;
+    const int32_t *kv_lens, *kv_offsets, *kv_seq;
+    const uint8_t* kv_mask;
+    int32_t dtype, n_seq, n_q, heads, kv_heads, d_head, n_enc, n_kv, kv_rows;
+    float   scale;
+} free_cross_attn;
+size_t free_op_cross_attention_workspace_bytes(const free_cross_attn* shape);
+int free_op_cross_attention(const free_cross_attn* a, void* out, int64_t o_seq, int64_t o_tok, int64_t o_head, float* lse,
+                            void* ws, size_t ws_bytes, uint32_t* device_error, void* stream);
+size_t free_op_cross_attention_bwd_workspace_bytes(const free_cross_attn* shape);
+int free_op_cross_attention_bwd(const free_cross_attn* a, const void* out, int64_t o_seq, int64_t o_tok, int64_t o_head, const float* lse,
+                                const void* dout, int64_t g_seq, int64_t g_tok, int64_t g_head,
+                                void* dq, int64_t dq_seq, int64_t dq_tok, int64_t dq_head,
+                                void* dk, int64_t dk_seq, int64_t dk_tok, int64_t dk_head,
+                                void* dv, int64_t dv_seq, int64_t dv_tok, int64_t dv_head,
+                                void* ws, size_t ws_bytes, uint32_t* device_error, void* stream);
 
 /* Non-causal multi-head self-attention of n_seq sequences: qkv [n_seq, n_tok, 3, heads, d_head] in
  * `dtype`, out [n_seq, n_tok, heads * d_head] in `dtype`; softmax(q k^T / sqrt(d_head)) v per head. */

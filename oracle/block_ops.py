@@ -1,5 +1,5 @@
 """fp64 definitions of the transformer-block operators (numpy): layer norm with groups of rows, rotary positions with several
-axes, the gated linear layer, and their backward passes.  Formulas only; shares no code with the library."""
+axes, the gated linear layer, the root-mean-square norm, attention to an encoder's states, and their backward passes.  Formulas only; shares no code with the library."""
 import numpy as np
 
 
@@ -83,3 +83,94 @@ def gated_linear_bwd(x, w, preact, dh, act="silu"):
     a, da = gate_act(act, z[:, :F])
     dz = np.concatenate([dh * z[:, F:] * da, dh * a], 1)
     return dz @ w, dz.T @ x, dz.sum(0)
+
+
+def round_e4m3(v):
+    """Nearest 8-bit number (4 bits of exponent, 3 of mantissa, up to 448), ties to the even one; NaN stays."""
+    v = np.asarray(v, np.float64)
+    a = np.abs(v)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        e = np.maximum(np.floor(np.log2(np.where(a > 0, a, 1.0))), -6.0)
+    step = 2.0 ** (e - 3)
+    return np.where(np.isnan(v), np.nan, np.copysign(np.minimum(np.round(a / step) * step, 448.0), v))
+
+
+def rms_norm(x, weight=None, residual=None, rows_per_group=None, unit_offset=False, eps=1e-6):
+    """x [M, D]; weight [groups, D].  Returns (y, h, r [M])."""
+    h = np.asarray(x, np.float64)
+    if residual is not None:
+        h = h + np.asarray(residual, np.float64)
+    r = 1.0 / np.sqrt((h * h).mean(1) + eps)
+    y = h * r[:, None]
+    if weight is not None:
+        y = y * (_per_row(weight, len(h) if rows_per_group is None else rows_per_group) + (1.0 if unit_offset else 0.0))
+    return y, h, r
+
+
+def quantise(y, block=None):
+    """8-bit values and scales [M, runs] of rows y: a run of `block` columns (None: the row) shares max |y| / 448."""
+    M, D = y.shape
+    n = D if block is None else block
+    runs = -(-D // n)
+    top = np.stack([np.abs(y[:, i * n:(i + 1) * n]).max(1) for i in range(runs)], 1)
+    scales = np.where(top < 2.0 ** -100, 1.0, top / 448.0)
+    return round_e4m3(y / np.repeat(scales, n, 1)[:, :D]), scales
+
+
+def rms_norm_bwd(h, dy, rstd, weight=None, rows_per_group=None, unit_offset=False, dres=None):
+    """Returns (dx [M, D], dweight [groups, D]) for the given 1 / sqrt(mean square + eps) of every row."""
+    h, dy, r = (np.asarray(a, np.float64) for a in (h, dy, rstd))
+    M, D = h.shape
+    rows = M if rows_per_group is None else rows_per_group
+    xh = h * r[:, None]
+    v = dy if weight is None else dy * (_per_row(weight, rows) + (1.0 if unit_offset else 0.0))
+    dx = r[:, None] * (v - xh * (v * xh).mean(1, keepdims=True))
+    if dres is not None:
+        dx = dx + np.asarray(dres, np.float64)
+    return dx, (dy * xh).reshape(M // rows if rows else 1, rows, D).sum(1)
+
+
+def cross_attention(q, ks, vs, counts, enc_of, scale):
+    """q [n_seq, n_q, heads, d]; ks, vs: per encoder sequence [n, kv_heads, d]; counts: per encoder sequence, which states count;
+    enc_of [n_seq] (out of range: none).  Returns (out like q, lse [n_seq, heads, n_q])."""
+    q = np.asarray(q, np.float64)
+    out, lse = np.zeros(q.shape), np.full((q.shape[0], q.shape[2], q.shape[1]), -np.inf)
+    for s, e in enumerate(enc_of):
+        use = np.flatnonzero(counts[e]) if 0 <= e < len(ks) else []
+        if len(use) == 0:
+            continue
+        for h in range(q.shape[2]):
+            kh = h // (q.shape[2] // ks[e].shape[1])
+            S = scale * q[s, :, h] @ np.asarray(ks[e], np.float64)[use, kh].T
+            top = S.max(1, keepdims=True)
+            p = np.exp(S - top)
+            lse[s, h] = top[:, 0] + np.log(p.sum(1))
+            out[s, :, h] = (p / p.sum(1, keepdims=True)) @ np.asarray(vs[e], np.float64)[use, kh]
+    return out, lse
+
+
+def cross_attention_bwd(q, ks, vs, counts, enc_of, scale, out, lse, dout):
+    """Gradients (dq, [dk], [dv] per encoder sequence) for the given out and lse, and for each the sum of its terms' magnitudes that a
+    rounding error of every term scales with: (dq, dk, dv, mag_dq, mag_dk, mag_dv)."""
+    q, out, lse, g = (np.asarray(a, np.float64) for a in (q, out, lse, dout))
+    dq, mq = np.zeros(q.shape), np.zeros(q.shape)
+    dk, dv, mk, mv = ([np.zeros(k.shape) for k in ks] for _ in range(4))
+    for s, e in enumerate(enc_of):
+        use = np.flatnonzero(counts[e]) if 0 <= e < len(ks) else []
+        if len(use) == 0:
+            continue
+        for h in range(q.shape[2]):
+            kh = h // (q.shape[2] // ks[e].shape[1])
+            k, v = np.asarray(ks[e], np.float64)[use, kh], np.asarray(vs[e], np.float64)[use, kh]
+            p = np.exp(scale * q[s, :, h] @ k.T - lse[s, h][:, None])
+            delta = (g[s, :, h] * out[s, :, h]).sum(1, keepdims=True)
+            dS = p * (g[s, :, h] @ v.T - delta) * scale
+            # the bracket is a difference of sums: its error goes by the sums' terms, not by the difference
+            terms = p * scale * (np.abs(g[s, :, h]) @ np.abs(v).T + np.abs(g[s, :, h] * out[s, :, h]).sum(1, keepdims=True))
+            dq[s, :, h] = dS @ k
+            mq[s, :, h] = terms @ np.abs(k)
+            dk[e][use, kh] += dS.T @ q[s, :, h]
+            mk[e][use, kh] += terms.T @ np.abs(q[s, :, h])
+            dv[e][use, kh] += p.T @ g[s, :, h]
+            mv[e][use, kh] += p.T @ np.abs(g[s, :, h])
+    return dq, dk, dv, mq, mk, mv

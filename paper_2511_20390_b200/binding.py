@@ -5,7 +5,9 @@ the current stream.  Nothing here computes any part of the method.
 """
 import ctypes as C
 import os
+import struct
 import threading
+import typing
 from operator import index
 
 import numpy as np
@@ -13,7 +15,7 @@ import torch
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfree_b200.so")
 
-FREE_FP32, FREE_BF16 = 0, 1
+FREE_FP32, FREE_BF16, FREE_E4M3 = 0, 1, 2
 FREE_MAX_K = 64
 EPI_BIAS, EPI_BIAS_GELU, EPI_BIAS_SILU, EPI_GATE_RESIDUAL = 0, 1, 2, 3
 
@@ -130,8 +132,19 @@ _SIGNATURES = {
     "free_op_layer_norm_bwd": (C.c_int, [_Int] * 5 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
                                                          C.c_int64, _Int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                                          C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "free_op_rms_norm": (C.c_int, [_Int] * 7 + [C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                                C.c_int64, _Int, C.c_float, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, _Int,
+                                                C.c_void_p, C.c_void_p]),
+    "free_op_rms_norm_bwd_workspace_bytes": (C.c_size_t, [_Int] * 3),
+    "free_op_rms_norm_bwd": (C.c_int, [_Int] * 6 + [C.c_void_p, C.c_int64, C.c_int64] * 2 + [C.c_void_p, C.c_void_p, C.c_int64, _Int] +
+                             [C.c_void_p, C.c_int64, C.c_int64] * 2 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
     "free_op_rope_axes": (C.c_int, [_Int] * 9 + [C.c_void_p, C.c_double, C.c_void_p, C.c_int64] +
                           [C.c_void_p, C.c_int64, C.c_int64, C.c_int64] * 2 + [C.c_void_p]),
+    "free_op_cross_attention_workspace_bytes": (C.c_size_t, [C.c_char_p]),
+    "free_op_cross_attention": (C.c_int, [C.c_char_p, C.c_void_p] + [C.c_int64] * 3 + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]),
+    "free_op_cross_attention_bwd_workspace_bytes": (C.c_size_t, [C.c_char_p]),
+    "free_op_cross_attention_bwd": (C.c_int, [C.c_char_p, C.c_void_p] + [C.c_int64] * 3 + [C.c_void_p] + ([C.c_void_p] + [C.c_int64] * 3) * 4 +
+                                    [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]),
     "free_op_attention": (C.c_int, [_Int] * 5 + [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "free_op_attention_workspace_bytes": (C.c_size_t, [_Int] * 5),
     "free_op_attention_static": (C.c_int, [_Int] * 4 + [C.c_void_p] * 4),
@@ -801,6 +814,118 @@ def op_layer_norm_bwd(x, dy, stats, weight=None, rows_per_group=None, unit_offse
     return dx, dw, db
 
 
+class RmsNorm(typing.NamedTuple):
+    """Results of op_rms_norm: y; the scales of an 8-bit y; the new residual stream; 1 / sqrt(mean square + eps).  None where there is none."""
+    y: torch.Tensor
+    scales: torch.Tensor | None
+    residual: torch.Tensor | None
+    rstd: torch.Tensor | None
+
+
+def _tokens(t, shape, what):
+    """(token stride, head stride) of a [tokens, D] or [tokens, heads, D] tensor whose rows are dense."""
+    if t.shape != shape or (shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{what}: expected {list(shape)} with dense rows")
+    M, D = shape[0], shape[-1]
+    if len(shape) == 2:
+        return (t.stride(0) if M > 1 else max(D, t.stride(0))), 0
+    H = shape[1]
+    head = t.stride(1) if H > 1 else D
+    return (t.stride(0) if M > 1 else max(H * head, t.stride(0))), head
+
+
+def op_rms_norm(x, weight=None, residual=None, rows_per_group=None, unit_offset=False, eps=1e-6, out_dtype=None, scale_block=None,
+                want_rstd=False, out=None, residual_out=None):
+    """Root-mean-square norm of the rows of x (CUDA fp32 or bf16 [M, D] with dense rows any distance apart, or the heads [tokens, heads, D]
+    of a packed projection), y = h / sqrt(mean(h^2) + eps) * weight with h = x + residual (fp32 or bf16 [M, D]; not for heads).  weight: fp32
+    [D], or [groups, D] for groups of `rows_per_group` consecutive rows (of a head's: tokens times heads); unit_offset: stored as an
+    offset from one.  out_dtype (default: x's) may be torch.float8_e4m3fn: y then is a value times its scale, fp32 [M, runs], one
+    for every scale_block (128; None: the row's) columns.  Returns RmsNorm(y, scales, residual, rstd): residual is h in the residual's type,
+    a new tensor unless residual_out is given (the residual itself: in place); rstd, fp32 with want_rstd, is what op_rms_norm_bwd
+    needs.  out may be x."""
+    nd = x.dim()
+    if nd not in (2, 3):
+        raise ValueError("x: expected [rows, D] or [tokens, heads, D]")
+    shape = x.shape
+    H, D = (shape[1] if nd == 3 else 1), shape[-1]
+    M = shape[0] * H
+    groups, rows = _groups(M, rows_per_group)
+    dev = _device_of(x, weight, residual, out, residual_out)
+    xc, (xt, xh) = _code(x.dtype), _tokens(x, shape, "x")
+    ms = 0 if weight is None else _group_rows(weight, groups, D, "weight")
+    if out is None:
+        out = _like(x, x.dtype if out_dtype is None else _ACT.get(out_dtype, out_dtype))
+    elif out_dtype is not None and _ACT.get(out_dtype, out_dtype) != out.dtype:
+        raise ValueError("out_dtype: out has another type")
+    else:
+        _apart(out, "out", (x,), weight, residual)
+    yt, yh = _tokens(out, shape, "out")
+    scales = None
+    if out.dtype == torch.float8_e4m3fn:
+        yc, runs = FREE_E4M3, 1
+        if nd == 3:
+            raise ValueError("out_dtype: 8-bit results are of rows [M, D]")
+        if scale_block not in (None, 128):
+            raise ValueError("scale_block: expected 128, or None for a scale per row")
+        if scale_block:
+            runs = -(-D // 128)
+        scales = x.new_empty((M, runs), dtype=torch.float32)
+    else:
+        yc, runs = _code(out.dtype), 0
+        if scale_block is not None:
+            raise ValueError("scale_block: only for 8-bit results")
+    rc = rs = hs = 0
+    if residual is not None:
+        if nd == 3:
+            raise ValueError("residual: expected rows, not heads")
+        rc, rs = _code(residual.dtype), _rows(residual, M, D, "residual")
+        if residual_out is None:
+            residual_out = _like(residual, residual.dtype)
+        elif residual_out.dtype != residual.dtype:
+            raise ValueError("residual_out: expected the residual's dtype")
+        else:
+            _apart(residual_out, "residual_out", (residual,), x, weight)
+            _apart(residual_out, "residual_out", (), out)
+        hs = _rows(residual_out, M, D, "residual_out")
+    elif residual_out is not None:
+        raise ValueError("residual_out: there is no residual")
+    rstd = x.new_empty(M, dtype=torch.float32) if want_rstd else None
+    _launch("free_op_rms_norm", dev, xc, rc, yc, groups, rows, H, D, x.data_ptr(), xt, xh, _adr(residual), rs, _adr(residual_out), hs,
+            _adr(weight), ms, 1 if unit_offset else 0, eps, out.data_ptr(), yt, yh, _adr(scales), runs, scale_block or 0, _adr(rstd))
+    return RmsNorm(out, scales, residual_out, rstd)
+
+
+def op_rms_norm_bwd(h, dy, rstd, weight=None, rows_per_group=None, unit_offset=False, dres=None, want_dweight=True, dx=None):
+    """Gradients of op_rms_norm from dy (like h, fp32 or bf16), the h that it normed (its residual, or x where there was none) and the
+    rstd it kept.  dres: gradient of h from another path, added to dx.  Returns (dx in h's dtype, which is the gradient of x and of the
+    residual alike, dweight fp32 [groups, D] or None).  dx may be h, dy or dres.  Heads [tokens, heads, D] of more than 128 columns (256 where
+    D is even) have to lie evenly apart."""
+    nd = h.dim()
+    if nd not in (2, 3):
+        raise ValueError("h: expected [rows, D] or [tokens, heads, D]")
+    shape = h.shape
+    H, D = (shape[1] if nd == 3 else 1), shape[-1]
+    M = shape[0] * H
+    groups, rows = _groups(M, rows_per_group)
+    dev = _device_of(h, dy, rstd, weight, dres, dx)
+    if rstd.dtype != torch.float32 or rstd.shape != (M,) or not rstd.is_contiguous():
+        raise ValueError("rstd: expected the contiguous fp32 [rows] of the forward call")
+    if (dres is not None and dres.dtype != h.dtype) or (dx is not None and dx.dtype != h.dtype):
+        raise ValueError("dres, dx: expected h's dtype")
+    if dx is None:
+        dx = _like(h, h.dtype)
+    else:
+        _apart(dx, "dx", (h, dy, dres), rstd, weight)
+    dw = rstd.new_empty((groups, D)) if want_dweight else None
+    need = lib().free_op_rms_norm_bwd_workspace_bytes(groups, rows, D) if want_dweight else 0
+    ws = torch.empty(need, dtype=torch.uint8, device=h.device) if need else None
+    _launch("free_op_rms_norm_bwd", dev, _code(h.dtype), _code(dy.dtype), groups, rows, H, D, h.data_ptr(), *_tokens(h, shape, "h"),
+            dy.data_ptr(), *_tokens(dy, shape, "dy"), rstd.data_ptr(), _adr(weight), 0 if weight is None else _group_rows(weight, groups, D, "weight"),
+            1 if unit_offset else 0, _adr(dres), *((0, 0) if dres is None else _tokens(dres, shape, "dres")), dx.data_ptr(),
+            *_tokens(dx, shape, "dx"), _adr(dw), D, _adr(ws), need)
+    return dx, dw
+
+
 ROPE_PAIRING = {"interleaved": 0, "halves": 1}
 _AXES = {n: C.c_int32 * n for n in range(1, 5)}
 
@@ -938,6 +1063,113 @@ def op_attention(qkv, heads):
     if err:
         raise FreeError(-8, f"free_op_attention (device error word {err:#x})")
     return out
+
+
+# struct free_cross_attn of the public header
+_CROSS = struct.Struct("<3Q9q4Q9if4x")
+
+
+def _cross_shape(q, k, v, kv_lens, kv_mask, kv_seq, kv_offsets, max_kv, scale):
+    """(device, packed free_cross_attn) of a call, after the checks that both directions share."""
+    if q.dim() != 4 or (q.shape[3] > 1 and q.stride(3) != 1):
+        raise ValueError("q: expected [n_seq, n_q, heads, d_head] with dense heads")
+    packed = kv_offsets is not None
+    nd = 3 if packed else 4
+    if k.dim() != nd or k.shape != v.shape or k.shape[-1] != q.shape[3] or (k.shape[-1] > 1 and (k.stride(-1) != 1 or v.stride(-1) != 1)):
+        raise ValueError("k, v: expected [n_enc, n_kv, kv_heads, d_head] (with kv_offsets [rows, kv_heads, d_head]) with dense heads of q's size")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("k, v: expected q's dtype")
+    (n_seq, n_q, heads, d), kv_heads = q.shape, k.shape[-2]
+    dev = _device_of(q, k, v, kv_lens, kv_mask, kv_seq, kv_offsets)
+    if packed:
+        if kv_lens is not None:
+            raise ValueError("kv_lens: not with kv_offsets")
+        _ints(kv_offsets, None, "kv_offsets")
+        n_enc, rows = kv_offsets.shape[0] - 1, k.shape[0]
+        if n_enc < 0:
+            raise ValueError("kv_offsets: expected n_enc + 1 numbers")
+        n_kv = rows if max_kv is None else min(int(max_kv), rows)
+        if n_kv < 0:
+            raise ValueError("max_kv: expected a length")
+        ks, vs = (0, *k.stride()), (0, *v.stride())
+    else:
+        if max_kv is not None:
+            raise ValueError("max_kv: only with kv_offsets")
+        n_enc, n_kv = k.shape[:2]
+        rows = n_kv
+        if kv_lens is not None:
+            _ints(kv_lens, n_enc, "kv_lens")
+        ks, vs = k.stride(), v.stride()
+    if kv_mask is not None and (kv_mask.dtype not in (torch.bool, torch.uint8) or kv_mask.shape != k.shape[:nd - 2] or not kv_mask.is_contiguous()):
+        raise ValueError("kv_mask: expected contiguous bool of the states' shape")
+    if kv_seq is not None:
+        _ints(kv_seq, n_seq, "kv_seq")
+    elif n_seq % n_enc if n_enc else n_seq:
+        raise ValueError(f"{n_seq} sequences do not share {n_enc} encoder sequences evenly: give kv_seq")
+    qs = q.stride()
+    try:
+        return dev, _CROSS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                                _adr(kv_lens) or 0, _adr(kv_offsets) or 0, _adr(kv_seq) or 0, _adr(kv_mask) or 0, _code(q.dtype), n_seq, n_q, heads,
+                                kv_heads, d, n_enc, n_kv, rows, d ** -0.5 if scale is None else scale)
+    except (struct.error, OverflowError) as e:
+        raise ValueError(f"sizes that do not fit a C int, or a scale that is no float: {e}") from None
+
+
+def _ints(t, n, what):
+    if t.dtype != torch.int32 or t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
+        raise ValueError(f"{what}: expected contiguous int32 [{'n_enc + 1' if n is None else n}]")
+
+
+def op_cross_attention(q, k, v, kv_lens=None, kv_mask=None, kv_seq=None, kv_offsets=None, max_kv=None, scale=None, want_lse=False, out=None):
+    """Attention of tokens q (CUDA fp32 or bf16 [n_seq, n_q, heads, d_head], any strides with dense heads, d_head up to 128) to an
+    encoder's states k, v [n_enc, n_kv, kv_heads, d_head] (heads a multiple of kv_heads; views into a packed projection are fine).
+    Encoder sequence e has kv_lens[e] states (int32, default n_kv); with kv_offsets (int32 [n_enc + 1]) the states are packed, k and v
+    [rows, kv_heads, d_head], and sequence e has the rows kv_offsets[e] .. kv_offsets[e + 1] - 1, at most max_kv (default: all).  States
+    whose kv_mask is False do not count either.  Sequence s reads encoder sequence kv_seq[s] (int32); by default n_seq / n_enc consecutive
+    sequences share one.  scale defaults to d_head ** -0.5.  Returns out like q, zero for tokens without a state, and with want_lse also
+    the log of the sums of exponentials, fp32 [n_seq, heads, n_q] (-inf for those), what op_cross_attention_bwd needs.  Asynchronous:
+    op_device_error() tells whether a device-side wait gave up."""
+    dev, shape = _cross_shape(q, k, v, kv_lens, kv_mask, kv_seq, kv_offsets, max_kv, scale)
+    if out is None:
+        out = _like(q, q.dtype)
+    else:
+        if out.shape != q.shape or out.dtype != q.dtype or (q.shape[3] > 1 and out.stride(3) != 1):
+            raise ValueError("out: expected q's shape and dtype with dense heads")
+        _device_of(q, out)
+        _apart(out, "out", (), q, k, v)
+    lse = q.new_empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32) if want_lse else None
+    need = (_LIB or lib()).free_op_cross_attention_workspace_bytes(shape)
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    os = out.stride()
+    _launch("free_op_cross_attention", dev, shape, out.data_ptr(), os[0], os[1], os[2], _adr(lse), _adr(ws), need,
+            _error_word(dev).data_ptr() if q.dtype == torch.bfloat16 else None)
+    return (out, lse) if want_lse else out
+
+
+def op_cross_attention_bwd(q, k, v, out, lse, dout, kv_lens=None, kv_mask=None, kv_seq=None, kv_offsets=None, max_kv=None, scale=None,
+                           want_dq=True, want_dkv=True):
+    """Gradients of op_cross_attention from dout (like q) and the out and lse of the forward call; the other arguments as there.
+    Returns (dq, dk, dv), contiguous and in q's dtype, None where not wanted; a state's gradients are summed over the tokens, heads and
+    sequences that read it, zero where none does.  Asynchronous as the forward call: op_device_error()."""
+    dev, shape = _cross_shape(q, k, v, kv_lens, kv_mask, kv_seq, kv_offsets, max_kv, scale)
+    _device_of(q, out, lse, dout)
+    for t, what in ((out, "out"), (dout, "dout")):
+        if t.shape != q.shape or t.dtype != q.dtype or (q.shape[3] > 1 and t.stride(3) != 1):
+            raise ValueError(f"{what}: expected q's shape and dtype with dense heads")
+    if lse.dtype != torch.float32 or lse.shape != (q.shape[0], q.shape[2], q.shape[1]) or not lse.is_contiguous():
+        raise ValueError("lse: expected the contiguous fp32 [n_seq, heads, n_q] of the forward call")
+    dq = _like(q, q.dtype) if want_dq else None
+    dk = dv = None
+    if want_dkv:
+        make = torch.empty_like if kv_offsets is None else torch.zeros_like       # packed rows that no sequence has
+        dk, dv = (make(k, memory_format=torch.contiguous_format) for _ in range(2))
+    need = lib().free_op_cross_attention_bwd_workspace_bytes(shape)
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    strides = lambda t: (0, 0, 0) if t is None else t.stride()[:3] if t.dim() == 4 else (0, *t.stride()[:2])
+    _launch("free_op_cross_attention_bwd", dev, shape, out.data_ptr(), *strides(out), lse.data_ptr(), dout.data_ptr(), *strides(dout),
+            _adr(dq), *strides(dq), _adr(dk), *strides(dk), _adr(dv), *strides(dv), _adr(ws), need,
+            _error_word(dev).data_ptr() if q.dtype == torch.bfloat16 else None)
+    return dq, dk, dv
 
 
 STATIC_ATTN_MAX_ELEMS = 1 << 21

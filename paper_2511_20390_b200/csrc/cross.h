@@ -1,0 +1,53 @@
+// Internal interfaces of the attention to an encoder's states (cross_*.cu).
+#pragma once
+#include "internal.h"
+
+constexpr int kCrossMaxD = 128;
+
+// A matrix of heads: element (s, t, h, c) at p[s * seq + t * tok + h * head + c].
+struct CrossMat {
+    const void* p;
+    long long seq, tok, head;
+};
+
+// What every kernel needs to find the states of a sequence.
+struct CrossWhere {
+    const int32_t *lens, *offsets, *seq_of;
+    const uint8_t* mask;
+    int n_enc, n_kv, kv_rows, share;          // share: consecutive sequences that read one encoder sequence (seq_of == nullptr)
+};
+
+struct CrossSpan { int enc, row0, len; };     // states row0 .. row0 + len - 1 of encoder sequence `enc` (0 where packed)
+
+__device__ __forceinline__ CrossSpan cross_span_of_enc(const CrossWhere& w, int e) {
+    if ((unsigned)e >= (unsigned)w.n_enc) return CrossSpan{0, 0, 0};
+    if (w.offsets) {
+        const int b = __ldg(w.offsets + e), n = __ldg(w.offsets + e + 1);
+        const int lo = max(b, 0), hi = min(n, w.kv_rows);
+        return CrossSpan{0, lo, lo < hi ? min(hi - lo, w.n_kv) : 0};
+    }
+    return CrossSpan{e, 0, w.lens ? min(max(__ldg(w.lens + e), 0), w.n_kv) : w.n_kv};
+}
+__device__ __forceinline__ int cross_enc_of(const CrossWhere& w, int s) { return w.seq_of ? __ldg(w.seq_of + s) : s / w.share; }
+__device__ __forceinline__ CrossSpan cross_span(const CrossWhere& w, int s) { return cross_span_of_enc(w, cross_enc_of(w, s)); }
+// the mask's bytes of a span (nullptr: all states count)
+__device__ __forceinline__ const uint8_t* cross_mask(const CrossWhere& w, const CrossSpan& sp) {
+    return w.mask ? w.mask + (w.offsets ? (long long)sp.row0 : (long long)sp.enc * w.n_kv) : nullptr;
+}
+
+struct CrossArgs {
+    CrossMat q, k, v, o;                      // o: forward's result
+    CrossMat g, dq, dk, dv;                   // backward: dout and the gradients
+    CrossWhere where;
+    int n_seq, n_q, heads, kv_heads, d, group;    // group: heads / kv_heads
+    float scale;
+    float* lse;                               // [n_seq, heads, n_q]
+    float* delta;                             // backward: <dout, out>, laid out as lse
+    uint32_t* err;
+};
+
+// CUDA cores, fp32 or bf16, any strides and alignment
+int cross_simt_forward(int dtype, const CrossArgs& a, cudaStream_t s);
+int cross_delta(int dtype, const CrossArgs& a, cudaStream_t s);
+int cross_simt_dq(int dtype, const CrossArgs& a, cudaStream_t s);
+int cross_simt_dkv(int dtype, const CrossArgs& a, cudaStream_t s);

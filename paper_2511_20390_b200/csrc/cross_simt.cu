@@ -1,0 +1,338 @@
+// Attention to an encoder's states on CUDA cores (fp32 arithmetic throughout): the exact mode, and bf16 inputs that the tensor
+// cores' tile copies cannot take (rows that are not 16-byte aligned, odd head sizes).
+//
+//   forward   S = scale q k^T, p = e^(S - max), out = p v / sum p, lse = max + log sum p     one pass, running maximum and sum
+//   dq        p = e^(S - lse), dS = p (g v^T - delta) scale, dq = dS k                        g: the gradient of out
+//   dk, dv    dk = dS^T q, dv = p^T g, summed over the queries, heads and sequences that share the states
+//
+// Tiles of 64 x 64 scores, 256 threads.  Thread (ty, tx) forms the scores of rows 4 ty .. and columns tx, tx + 16, ..: both
+// operands are read as four consecutive channels (16 bytes), eight reads for 64 multiply-adds; a row of a tile is d + 4 floats
+// (rounded up), so that eight threads' reads lie in different banks.  Scores go through shared memory to be the left operand
+// of the second product.  Bound by the fp32 pipe and shared memory's bandwidth.
+// States that do not count are read as zeros and their scores are masked, so nothing in them reaches a result.
+#include "cross.h"
+#include <mutex>
+
+namespace {
+
+constexpr int T = 64, kThreads = 256, PS = T + 4;
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ void from_f(float& d, float v) { d = v; }
+__device__ __forceinline__ void from_f(__nv_bfloat16& d, float v) { d = __float2bfloat16(v); }
+
+__host__ __device__ constexpr int pitch(int d) { return (d + 7) / 8 * 8 + 4; }
+
+// rows [r0, r0 + T) of a matrix of heads -> shared memory; rows that are not `live` and channels behind d are zeros
+template <typename E, typename Live>
+__device__ __forceinline__ void load_tile(float* dst, const E* base, long long stride, int r0, int d, int P, Live live) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int r = warp; r < T; r += kThreads / 32) {
+        const bool ok = live(r0 + r);
+        const E* src = base + (long long)(r0 + r) * stride;
+        for (int c = lane; c < P; c += 32) dst[r * P + c] = ok && c < d ? to_f(src[c]) : 0.f;
+    }
+}
+
+// s[r][k] = <A row 4 ty + r, B row tx + 16 k>
+__device__ __forceinline__ void scores(const float* A, const float* B, int P, int ty, int tx, float (&s)[4][4]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[r][k] = 0.f;
+    for (int c = 0; c < P - 4; c += 4) {
+        float4 a[4], b[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) a[r] = *reinterpret_cast<const float4*>(A + (4 * ty + r) * P + c);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) b[k] = *reinterpret_cast<const float4*>(B + (tx + 16 * k) * P + c);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                s[r][k] = fmaf(a[r].x, b[k].x, fmaf(a[r].y, b[k].y, fmaf(a[r].z, b[k].z, fmaf(a[r].w, b[k].w, s[r][k]))));
+    }
+}
+// acc[r][i] += sum over j of W[4 ty + r][j] * B[j][channel], channels 4 tx + 64 (i / 4) + i % 4
+template <int ND> __device__ __forceinline__ void product(const float* W, const float* B, int P, int ty, int tx, float (&acc)[4][4 * ND]) {
+    for (int j = 0; j < T; j += 4) {
+        float4 w[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w[r] = *reinterpret_cast<const float4*>(W + (4 * ty + r) * PS + j);
+#pragma unroll
+        for (int q = 0; q < ND; ++q) {
+            if (ND > 1 && 4 * tx + 64 * q >= P - 4) break;
+            const int c = ND == 1 ? min(4 * tx, P - 4) : 4 * tx + 64 * q;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float4 b = *reinterpret_cast<const float4*>(B + (j + u) * P + c);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float x = u == 0 ? w[r].x : u == 1 ? w[r].y : u == 2 ? w[r].z : w[r].w;
+                    acc[r][4 * q] = fmaf(x, b.x, acc[r][4 * q]);
+                    acc[r][4 * q + 1] = fmaf(x, b.y, acc[r][4 * q + 1]);
+                    acc[r][4 * q + 2] = fmaf(x, b.z, acc[r][4 * q + 2]);
+                    acc[r][4 * q + 3] = fmaf(x, b.w, acc[r][4 * q + 3]);
+                }
+            }
+        }
+    }
+}
+template <typename E, int ND> __device__ __forceinline__ void store_rows(E* base, long long stride, int r0, int rows, int d, int ty, int tx, const float (&acc)[4][4 * ND]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int row = r0 + 4 * ty + r;
+        if (row >= rows) continue;
+#pragma unroll
+        for (int q = 0; q < ND; ++q)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int c = 4 * tx + 64 * q + u;
+                if (c < d) from_f(base[(long long)row * stride + c], acc[r][4 * q + u]);
+            }
+    }
+}
+template <typename E> __device__ __forceinline__ const E* at(const CrossMat& m, int s, long long row, int h) {
+    return reinterpret_cast<const E*>(m.p) + s * m.seq + row * m.tok + h * m.head;
+}
+template <typename E> __device__ __forceinline__ E* at_out(const CrossMat& m, int s, long long row, int h) { return const_cast<E*>(at<E>(m, s, row, h)); }
+
+__device__ __forceinline__ float row_max(float v) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
+    return v;
+}
+__device__ __forceinline__ float row_sum(float v) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    return v;
+}
+
+template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_simt_kernel(const CrossArgs a) {
+    extern __shared__ float smem[];
+    const int d = a.d, P = pitch(d);
+    float *Q = smem, *K = Q + T * P, *V = K + T * P, *W = V + T * P;
+    const int tiles = (a.n_q + T - 1) / T;
+    const int tile = (int)(blockIdx.x % tiles), sh = (int)(blockIdx.x / tiles), h = sh % a.heads, s = sh / a.heads, kh = h / a.group;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, q0 = tile * T;
+    const CrossSpan sp = cross_span(a.where, s);
+    const uint8_t* mask = cross_mask(a.where, sp);
+    auto counts = [&](int j) { return j < sp.len && (!mask || mask[j]); };
+    load_tile<E>(Q, at<E>(a.q, s, 0, h), a.q.tok, q0, d, P, [&](int r) { return r < a.n_q; });
+    const E *kb = at<E>(a.k, sp.enc, sp.row0, kh), *vb = at<E>(a.v, sp.enc, sp.row0, kh);
+    float acc[4][4 * ND], top[4], sum[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        top[r] = -INFINITY; sum[r] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4 * ND; ++i) acc[r][i] = 0.f;
+    }
+    for (int j0 = 0; j0 < sp.len; j0 += T) {
+        __syncthreads();
+        load_tile<E>(K, kb, a.k.tok, j0, d, P, counts);
+        load_tile<E>(V, vb, a.v.tok, j0, d, P, counts);
+        __syncthreads();
+        float sc[4][4];
+        scores(Q, K, P, ty, tx, sc);
+        bool ok[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) ok[k] = counts(j0 + tx + 16 * k);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { sc[r][k] = ok[k] ? sc[r][k] * a.scale : -INFINITY; m = fmaxf(m, sc[r][k]); }
+            m = fmaxf(top[r], row_max(m));
+            const float base = m == -INFINITY ? 0.f : m;           // no state so far
+            const float alpha = expf(top[r] - base);
+            float part = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float p = expf(sc[r][k] - base);
+                part += p;
+                W[(4 * ty + r) * PS + tx + 16 * k] = p;
+            }
+            sum[r] = sum[r] * alpha + row_sum(part);
+            top[r] = m;
+#pragma unroll
+            for (int i = 0; i < 4 * ND; ++i) acc[r][i] *= alpha;
+        }
+        __syncwarp();                                              // a row of W is written and read by one half of a warp
+        product<ND>(W, V, P, ty, tx, acc);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float inv = sum[r] == 0.f ? 0.f : 1.f / sum[r];
+#pragma unroll
+        for (int i = 0; i < 4 * ND; ++i) acc[r][i] *= inv;
+        const int row = q0 + 4 * ty + r;
+        if (a.lse && tx == 0 && row < a.n_q) a.lse[((long long)s * a.heads + h) * a.n_q + row] = top[r] == -INFINITY ? -INFINITY : top[r] + logf(sum[r]);
+    }
+    store_rows<E, ND>(at_out<E>(a.o, s, 0, h), a.o.tok, q0, a.n_q, d, ty, tx, acc);
+}
+
+// delta = <dout, out> of every token and head: a warp per row
+template <typename E> __global__ void __launch_bounds__(256) cross_delta_kernel(const CrossArgs a) {
+    const long long rows = (long long)a.n_seq * a.n_q * a.heads;
+    const int lane = threadIdx.x & 31;
+    for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * 8) {
+        const int h = (int)(i % a.heads);
+        const long long st = i / a.heads;
+        const int t = (int)(st % a.n_q), s = (int)(st / a.n_q);
+        const E *g = at<E>(a.g, s, t, h), *o = at<E>(a.o, s, t, h);
+        float v = 0.f;
+        for (int c = lane; c < a.d; c += 32) v = fmaf(to_f(g[c]), to_f(o[c]), v);
+        v = free_warp_sum(v);
+        if (lane == 0) a.delta[((long long)s * a.heads + h) * a.n_q + t] = v;
+    }
+}
+
+template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_simt_dq_kernel(const CrossArgs a) {
+    extern __shared__ float smem[];
+    const int d = a.d, P = pitch(d);
+    float *Q = smem, *G = Q + T * P, *K = G + T * P, *V = K + T * P, *W = V + T * P;
+    const int tiles = (a.n_q + T - 1) / T;
+    const int tile = (int)(blockIdx.x % tiles), sh = (int)(blockIdx.x / tiles), h = sh % a.heads, s = sh / a.heads, kh = h / a.group;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, q0 = tile * T;
+    const CrossSpan sp = cross_span(a.where, s);
+    const uint8_t* mask = cross_mask(a.where, sp);
+    auto counts = [&](int j) { return j < sp.len && (!mask || mask[j]); };
+    auto live = [&](int r) { return r < a.n_q; };
+    load_tile<E>(Q, at<E>(a.q, s, 0, h), a.q.tok, q0, d, P, live);
+    load_tile<E>(G, at<E>(a.g, s, 0, h), a.g.tok, q0, d, P, live);
+    const E *kb = at<E>(a.k, sp.enc, sp.row0, kh), *vb = at<E>(a.v, sp.enc, sp.row0, kh);
+    float acc[4][4 * ND], lse[4], delta[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int row = q0 + 4 * ty + r;
+        const long long i = ((long long)s * a.heads + h) * a.n_q + row;
+        lse[r] = row < a.n_q ? a.lse[i] : 0.f;
+        delta[r] = row < a.n_q ? a.delta[i] : 0.f;
+#pragma unroll
+        for (int k = 0; k < 4 * ND; ++k) acc[r][k] = 0.f;
+    }
+    for (int j0 = 0; j0 < sp.len; j0 += T) {
+        __syncthreads();
+        load_tile<E>(K, kb, a.k.tok, j0, d, P, counts);
+        load_tile<E>(V, vb, a.v.tok, j0, d, P, counts);
+        __syncthreads();
+        float sc[4][4], dp[4][4];
+        scores(Q, K, P, ty, tx, sc);
+        scores(G, V, P, ty, tx, dp);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool ok = counts(j0 + tx + 16 * k);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                W[(4 * ty + r) * PS + tx + 16 * k] = ok ? expf(sc[r][k] * a.scale - lse[r]) * (dp[r][k] - delta[r]) * a.scale : 0.f;
+        }
+        __syncwarp();
+        product<ND>(W, K, P, ty, tx, acc);
+    }
+    store_rows<E, ND>(at_out<E>(a.dq, s, 0, h), a.dq.tok, q0, a.n_q, d, ty, tx, acc);
+}
+
+// One CTA per (64 states, key head, encoder sequence); it walks over every sequence that reads it, its query heads and tokens.
+template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_simt_dkv_kernel(const CrossArgs a) {
+    extern __shared__ float smem[];
+    const int d = a.d, P = pitch(d);
+    float *K = smem, *V = K + T * P, *Q = V + T * P, *G = Q + T * P, *W = G + T * P, *L = W + T * PS, *D = L + T;
+    const int tiles = (a.where.n_kv + T - 1) / T;
+    const int tile = (int)(blockIdx.x % tiles), eh = (int)(blockIdx.x / tiles), kh = eh % a.kv_heads, e = eh / a.kv_heads;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, j0 = tile * T;
+    const CrossSpan sp = cross_span_of_enc(a.where, e);
+    const int rows = a.where.offsets ? sp.len : a.where.n_kv;      // rows that are written
+    if (j0 >= rows) return;
+    const uint8_t* mask = cross_mask(a.where, sp);
+    auto counts = [&](int j) { return j < sp.len && (!mask || mask[j]); };
+    load_tile<E>(K, at<E>(a.k, sp.enc, sp.row0, kh), a.k.tok, j0, d, P, counts);
+    load_tile<E>(V, at<E>(a.v, sp.enc, sp.row0, kh), a.v.tok, j0, d, P, counts);
+    float dk[4][4 * ND], dv[4][4 * ND];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < 4 * ND; ++i) dk[r][i] = dv[r][i] = 0.f;
+    bool ok[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) ok[r] = counts(j0 + 4 * ty + r);
+    const int first = a.where.seq_of ? 0 : e * a.where.share, last = a.where.seq_of ? a.n_seq : first + a.where.share;
+    for (int s = first; s < last && j0 < sp.len; ++s) {
+        if (cross_enc_of(a.where, s) != e) continue;
+        for (int h = kh * a.group; h < (kh + 1) * a.group; ++h)
+            for (int q0 = 0; q0 < a.n_q; q0 += T) {
+                __syncthreads();
+                auto live = [&](int r) { return r < a.n_q; };
+                load_tile<E>(Q, at<E>(a.q, s, 0, h), a.q.tok, q0, d, P, live);
+                load_tile<E>(G, at<E>(a.g, s, 0, h), a.g.tok, q0, d, P, live);
+                if (threadIdx.x < T) {
+                    const int row = q0 + threadIdx.x;
+                    const long long i = ((long long)s * a.heads + h) * a.n_q + row;
+                    L[threadIdx.x] = row < a.n_q ? a.lse[i] : INFINITY;      // rows behind the last: p = 0
+                    D[threadIdx.x] = row < a.n_q ? a.delta[i] : 0.f;
+                }
+                __syncthreads();
+                float sc[4][4], dp[4][4];
+                scores(K, Q, P, ty, tx, sc);
+                scores(V, G, P, ty, tx, dp);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int t = tx + 16 * k;
+                        sc[r][k] = ok[r] ? expf(sc[r][k] * a.scale - L[t]) : 0.f;
+                        dp[r][k] = ok[r] ? sc[r][k] * (dp[r][k] - D[t]) * a.scale : 0.f;
+                        W[(4 * ty + r) * PS + t] = sc[r][k];
+                    }
+                __syncwarp();
+                product<ND>(W, G, P, ty, tx, dv);
+                __syncwarp();
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) W[(4 * ty + r) * PS + tx + 16 * k] = dp[r][k];
+                __syncwarp();
+                product<ND>(W, Q, P, ty, tx, dk);
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (!ok[r]) {                                              // whatever dout and q hold
+#pragma unroll
+            for (int i = 0; i < 4 * ND; ++i) dk[r][i] = dv[r][i] = 0.f;
+        }
+    store_rows<E, ND>(at_out<E>(a.dk, sp.enc, sp.row0, kh), a.dk.tok, j0, rows, d, ty, tx, dk);
+    store_rows<E, ND>(at_out<E>(a.dv, sp.enc, sp.row0, kh), a.dv.tok, j0, rows, d, ty, tx, dv);
+}
+
+template <typename K> int launch(K kernel, long long ctas, int tiles_held, int extra, const CrossArgs& a, cudaStream_t s) {
+    if (ctas > 0x7fffffffLL) return FREE_ERR_SHAPE;
+    const int smem = (tiles_held * T * pitch(a.d) + T * PS + extra) * (int)sizeof(float);
+    FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    kernel<<<(unsigned)ctas, kThreads, smem, s>>>(a);
+    return free_check_launch();
+}
+long long q_tiles(const CrossArgs& a) { return (long long)((a.n_q + T - 1) / T) * a.n_seq * a.heads; }
+
+}  // namespace
+
+int cross_simt_forward(int dtype, const CrossArgs& a, cudaStream_t s) {
+    if (dtype == FREE_FP32) return a.d <= 64 ? launch(cross_simt_kernel<float, 1>, q_tiles(a), 3, 0, a, s) : launch(cross_simt_kernel<float, 2>, q_tiles(a), 3, 0, a, s);
+    return a.d <= 64 ? launch(cross_simt_kernel<__nv_bfloat16, 1>, q_tiles(a), 3, 0, a, s) : launch(cross_simt_kernel<__nv_bfloat16, 2>, q_tiles(a), 3, 0, a, s);
+}
+int cross_delta(int dtype, const CrossArgs& a, cudaStream_t s) {
+    const long long rows = (long long)a.n_seq * a.n_q * a.heads, ctas = (rows + 7) / 8;
+    const unsigned grid = (unsigned)(ctas < 148 * 8 ? ctas : 148 * 8);
+    if (dtype == FREE_FP32) cross_delta_kernel<float><<<grid, 256, 0, s>>>(a);
+    else cross_delta_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(a);
+    return free_check_launch();
+}
+int cross_simt_dq(int dtype, const CrossArgs& a, cudaStream_t s) {
+    if (dtype == FREE_FP32) return a.d <= 64 ? launch(cross_simt_dq_kernel<float, 1>, q_tiles(a), 4, 0, a, s) : launch(cross_simt_dq_kernel<float, 2>, q_tiles(a), 4, 0, a, s);
+    return a.d <= 64 ? launch(cross_simt_dq_kernel<__nv_bfloat16, 1>, q_tiles(a), 4, 0, a, s) : launch(cross_simt_dq_kernel<__nv_bfloat16, 2>, q_tiles(a), 4, 0, a, s);
+}
+int cross_simt_dkv(int dtype, const CrossArgs& a, cudaStream_t s) {
+    const long long n = (long long)((a.where.n_kv + T - 1) / T) * a.where.n_enc * a.kv_heads;
+    if (dtype == FREE_FP32) return a.d <= 64 ? launch(cross_simt_dkv_kernel<float, 1>, n, 4, 2 * T, a, s) : launch(cross_simt_dkv_kernel<float, 2>, n, 4, 2 * T, a, s);
+    return a.d <= 64 ? launch(cross_simt_dkv_kernel<__nv_bfloat16, 1>, n, 4, 2 * T, a, s) : launch(cross_simt_dkv_kernel<__nv_bfloat16, 2>, n, 4, 2 * T, a, s);
+}

@@ -20,7 +20,7 @@
 // The gradients of w and b are column sums over a group's rows.  A CTA keeps them in fp32 registers over a run of rows of
 // one group and writes one partial row; a second, small launch adds the partial rows of a group in a fixed order, so that
 // repeats are bit-identical (no atomics).
-#include "internal.h"
+#include "rms_norm.h"
 
 namespace {
 
@@ -127,6 +127,9 @@ struct NormArgs {
     const void* dres; long long dres_stride;
     void* dx; long long dx_stride;
     float *dw, *db; long long dmod_stride;    // final gradients
+    const float* rstd_in;                     // without a mean: [M], in place of stats_in
+    int heads;                                // without a mean: row i is head i % heads of token i / heads; the strides above are the
+    long long x_head, dy_head, dres_head, dx_head;    // tokens', these the heads' (narrow rows only)
     float* partial;                           // [groups][chunks][2][D]; with one chunk per group the kernel writes dw, db itself
     int chunks;
 };
@@ -259,7 +262,8 @@ template <typename TX, typename TY, int VW> constexpr bool kAhead = VW * sizeof(
 
 // One CTA, a team of warps with C columns per lane, per (group, chunk): a run of the group's rows, R of them per barrier and R more in
 // flight.  T: threads per SM that the register budget is set for.
-template <typename TX, typename TY, int C, int VW, int MAXT, int T, int R>
+// RMS: the norm without a mean and bias, dx = r (v - xh mean(v xh)) + dres with xh = x r.
+template <typename TX, typename TY, int C, int VW, int MAXT, int T, int R, bool RMS>
 __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const NormArgs a) {
     constexpr int P = C / VW, XW = kWords<TX, VW>, YW = kWords<TY, VW>;      // pieces of a lane, words of a piece
     constexpr bool AHEAD = kAhead<TX, TY, VW>;
@@ -305,6 +309,7 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
         copy_commit();
     };
     auto stats_of = [&](long long row) {
+        if (RMS) return make_float2(0.f, row < hi ? __ldg(a.rstd_in + row) : 0.f);
         return row < hi ? make_float2(__ldg(a.stats_in + 2 * row), __ldg(a.stats_in + 2 * row + 1)) : make_float2(0.f, 0.f);
     };
     if (AHEAD) fetch(now);
@@ -352,13 +357,15 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
 #pragma unroll
                 for (int e = 0; e < VW; ++e) {
                     const float d = in ? value<TY, VW>(ry[p], e) : 0.f;
-                    xh[r][p][e] = in ? (value<TX, VW>(rx[p], e) - st[r].x) * st[r].y : 0.f;
+                    xh[r][p][e] = in ? (RMS ? value<TX, VW>(rx[p], e) : value<TX, VW>(rx[p], e) - st[r].x) * st[r].y : 0.f;
                     v[r][p][e] = d * w[p][e];
-                    s1 += v[r][p][e]; s2 = fmaf(v[r][p][e], xh[r][p][e], s2);
-                    dw[p][e] = fmaf(d, xh[r][p][e], dw[p][e]); db[p][e] += d;
+                    if (!RMS) s1 += v[r][p][e];
+                    s2 = fmaf(v[r][p][e], xh[r][p][e], s2);
+                    dw[p][e] = fmaf(d, xh[r][p][e], dw[p][e]);
+                    if (!RMS) db[p][e] += d;
                 }
             }
-            sum[r] = make_float2(free_warp_sum(s1), free_warp_sum(s2));
+            sum[r] = make_float2(RMS ? 0.f : free_warp_sum(s1), free_warp_sum(s2));
         }
         if (W > 1) {
             float2 (*sums)[MAXT / 32] = part[it & 1];               // a buffer is rewritten two barriers after its last read
@@ -379,7 +386,7 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
                 float o[VW];
                 if (AHEAD && dres) take<TX, VW>(px(now + r * one + bx, p), c.in(p), res[r][p]);
 #pragma unroll
-                for (int e = 0; e < VW; ++e) o[e] = fmaf(st[r].y, v[r][p][e] - m1 - xh[r][p][e] * m2, dres ? value<TX, VW>(res[r][p], e) : 0.f);
+                for (int e = 0; e < VW; ++e) o[e] = fmaf(st[r].y, (RMS ? v[r][p][e] : v[r][p][e] - m1) - xh[r][p][e] * m2, dres ? value<TX, VW>(res[r][p], e) : 0.f);
                 if (c.in(p)) store<VW>(dx + (row + r) * a.dx_stride + c.at(p), o);
             }
         }
@@ -391,8 +398,8 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
     if (!a.dw && !a.db) return;
     float *ow = a.dw ? a.dw + (long long)g * a.dmod_stride : nullptr, *ob = a.db ? a.db + (long long)g * a.dmod_stride : nullptr;
     if (a.chunks > 1) {
-        ow = a.partial + (long long)blockIdx.x * 2 * a.D;
-        ob = ow + a.D;
+        ow = a.partial + (long long)blockIdx.x * (RMS ? 1 : 2) * a.D;
+        ob = RMS ? nullptr : ow + a.D;
     }
 #pragma unroll
     for (int p = 0; p < P; ++p)
@@ -400,7 +407,7 @@ __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const No
 #pragma unroll
             for (int e = 0; e < VW; ++e) {
                 if (ow) ow[c.at(p) + e] = dw[p][e];
-                if (ob) ob[c.at(p) + e] = db[p][e];
+                if (ob && !RMS) ob[c.at(p) + e] = db[p][e];
             }
         }
 }
@@ -489,7 +496,7 @@ __global__ void __launch_bounds__(256, kNarrowPerSm) layer_norm_narrow_kernel(co
 }
 
 // One CTA per (group, chunk) as for wide rows; its warps take the run's rows in turn and their column sums are added at the end.
-template <typename TX, typename TY, int L, int C, int VW>
+template <typename TX, typename TY, int L, int C, int VW, bool RMS>
 __global__ void __launch_bounds__(256, kNarrowBwdPerSm) layer_norm_narrow_bwd_kernel(const NormArgs a) {
     constexpr int P = C / VW, XW = kWords<TX, VW>, YW = kWords<TY, VW>, R = 32 / L, N = L * C;
     __shared__ float sums[8][2][N];
@@ -507,15 +514,28 @@ __global__ void __launch_bounds__(256, kNarrowBwdPerSm) layer_norm_narrow_bwd_ke
     const float inv_d = 1.f / (float)a.D;
     uint32_t nx[P][XW], ny[P][YW], nr[P][XW];
     float2 ns;
+    // without a mean: heads of tokens; the row's token and head are counted on
+    const int H = RMS ? a.heads : 1;
+    long long tok = lo + warp * R + (threadIdx.x & 31) / L;
+    int head = 0;
+    if (RMS && H > 1) { head = (int)(tok % H); tok /= H; }
+    const int step_tok = W * R / H, step_head = W * R % H;
     auto fetch = [&](long long r) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const bool ok = r < hi && c.in(p);
+            if (RMS) {
+                load<TX, VW, false>(x + tok * a.x_stride + head * a.x_head + c.at(p), ok, nx[p]);
+                load<TY, VW, false>(dy + tok * a.dy_stride + head * a.dy_head + c.at(p), ok, ny[p]);
+                load<TX, VW, false>(dres + tok * a.dres_stride + head * a.dres_head + c.at(p), ok && dres, nr[p]);
+                continue;
+            }
             load<TX, VW, false>(x + r * a.x_stride + c.at(p), ok, nx[p]);
             load<TY, VW, false>(dy + r * a.dy_stride + c.at(p), ok, ny[p]);
             load<TX, VW, false>(dres + r * a.dres_stride + c.at(p), ok && dres, nr[p]);
         }
-        ns = r < hi ? make_float2(__ldg(a.stats_in + 2 * r), __ldg(a.stats_in + 2 * r + 1)) : make_float2(0.f, 0.f);
+        if (RMS) ns = make_float2(0.f, r < hi ? __ldg(a.rstd_in + r) : 0.f);
+        else ns = r < hi ? make_float2(__ldg(a.stats_in + 2 * r), __ldg(a.stats_in + 2 * r + 1)) : make_float2(0.f, 0.f);
     };
     long long row = lo + warp * R + (threadIdx.x & 31) / L;
     fetch(row);
@@ -537,23 +557,30 @@ __global__ void __launch_bounds__(256, kNarrowBwdPerSm) layer_norm_narrow_bwd_ke
 #pragma unroll
             for (int e = 0; e < VW; ++e) {
                 const float d = value<TY, VW>(ny[p], e);           // zero outside the row
-                xh[p][e] = in ? (value<TX, VW>(nx[p], e) - st.x) * st.y : 0.f;
+                xh[p][e] = in ? (RMS ? value<TX, VW>(nx[p], e) : value<TX, VW>(nx[p], e) - st.x) * st.y : 0.f;
                 v[p][e] = d * w[p][e];
-                s1 += v[p][e]; s2 = fmaf(v[p][e], xh[p][e], s2);
-                dw[p][e] = fmaf(d, xh[p][e], dw[p][e]); db[p][e] += d;
+                if (!RMS) s1 += v[p][e];
+                s2 = fmaf(v[p][e], xh[p][e], s2);
+                dw[p][e] = fmaf(d, xh[p][e], dw[p][e]);
+                if (!RMS) db[p][e] += d;
             }
 #pragma unroll
             for (int q = 0; q < XW; ++q) res[p][q] = nr[p][q];
         }
+        TX* out = dx + (RMS ? tok * a.dx_stride + head * a.dx_head : row * a.dx_stride);
+        if (RMS) {
+            tok += step_tok; head += step_head;
+            if (head >= H) { head -= H; ++tok; }
+        }
         fetch(row + W * R);
-        const float m1 = part_sum<L>(s1) * inv_d, m2 = part_sum<L>(s2) * inv_d;
+        const float m1 = RMS ? 0.f : part_sum<L>(s1) * inv_d, m2 = part_sum<L>(s2) * inv_d;
         if (live) {
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 float o[VW];
 #pragma unroll
-                for (int e = 0; e < VW; ++e) o[e] = fmaf(st.y, v[p][e] - m1 - xh[p][e] * m2, value<TX, VW>(res[p], e));
-                if (c.in(p)) store<VW>(dx + row * a.dx_stride + c.at(p), o);
+                for (int e = 0; e < VW; ++e) o[e] = fmaf(st.y, (RMS ? v[p][e] : v[p][e] - m1) - xh[p][e] * m2, value<TX, VW>(res[p], e));
+                if (c.in(p)) store<VW>(out + c.at(p), o);
             }
         }
     }
@@ -565,17 +592,17 @@ __global__ void __launch_bounds__(256, kNarrowBwdPerSm) layer_norm_narrow_bwd_ke
 #pragma unroll
             for (int o = L; o < 32; o <<= 1) {
                 dw[p][e] += __shfl_xor_sync(~0u, dw[p][e], o);
-                db[p][e] += __shfl_xor_sync(~0u, db[p][e], o);
+                if (!RMS) db[p][e] += __shfl_xor_sync(~0u, db[p][e], o);
             }
-            if ((threadIdx.x & 31) < L) { sums[warp][0][c.at(p) + e] = dw[p][e]; sums[warp][1][c.at(p) + e] = db[p][e]; }
+            if ((threadIdx.x & 31) < L) { sums[warp][0][c.at(p) + e] = dw[p][e]; if (!RMS) sums[warp][1][c.at(p) + e] = db[p][e]; }
         }
     __syncthreads();
     float *ow = a.dw ? a.dw + (long long)g * a.dmod_stride : nullptr, *ob = a.db ? a.db + (long long)g * a.dmod_stride : nullptr;
     if (a.chunks > 1) {
-        ow = a.partial + (long long)blockIdx.x * 2 * a.D;
-        ob = ow + a.D;
+        ow = a.partial + (long long)blockIdx.x * (RMS ? 1 : 2) * a.D;
+        ob = RMS ? nullptr : ow + a.D;
     }
-    for (int i = threadIdx.x; i < 2 * N; i += blockDim.x) {
+    for (int i = threadIdx.x; i < (RMS ? 1 : 2) * N; i += blockDim.x) {
         const int col = i % N;
         float* out = i < N ? ow : ob;
         if (col >= a.D || !out) continue;
@@ -586,21 +613,21 @@ __global__ void __launch_bounds__(256, kNarrowBwdPerSm) layer_norm_narrow_bwd_ke
 }
 
 // dw, db of a group = the sum of its chunks' partial rows: 32 columns x 16 slices of the chunks per CTA, slices joined in order.
-__global__ void __launch_bounds__(512) layer_norm_reduce_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(512) layer_norm_reduce_kernel(const NormArgs a, int width) {
     __shared__ float sh[16][33];
     free_grid_dep_wait();
     free_grid_dep_launch();
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    const int blocks = (2 * a.D + 31) / 32, g = blockIdx.x / blocks, j = (blockIdx.x % blocks) * 32 + tx;   // j: column of [2][D]
-    const float* p = a.partial + (long long)g * a.chunks * 2 * a.D;
+    const int blocks = (width + 31) / 32, g = blockIdx.x / blocks, j = (blockIdx.x % blocks) * 32 + tx;   // j: column of a partial row, [2][D] or, without a mean, [D]
+    const float* p = a.partial + (long long)g * a.chunks * width;
     float s = 0.f;
-    if (j < 2 * a.D) {
+    if (j < width) {
 #pragma unroll 8
-        for (int k = ty; k < a.chunks; k += 16) s += p[(long long)k * 2 * a.D + j];
+        for (int k = ty; k < a.chunks; k += 16) s += p[(long long)k * width + j];
     }
     sh[ty][tx] = s;
     __syncthreads();
-    if (ty == 0 && j < 2 * a.D) {
+    if (ty == 0 && j < width) {
         float t = 0.f;
 #pragma unroll
         for (int k = 0; k < 16; ++k) t += sh[k][tx];
@@ -669,11 +696,11 @@ int start_narrow(NormArgs a, cudaStream_t s) {
     const long long grid = (a.M + a.rows_per_team * 8 - 1) / (a.rows_per_team * 8);
     return free_launch(free_overlap_for_rows(a.M), layer_norm_narrow_kernel<TX, TY, L, C, VW>, dim3((unsigned)grid), dim3(256), 0, s, a);
 }
-template <typename TX, typename TY, int L, int C, int VW>
+template <typename TX, typename TY, int L, int C, int VW, bool RMS>
 int start_narrow_bwd(const NormArgs& a, cudaStream_t s) {
     const int steps = a.rows_per_group / a.chunks / (64 / L);      // a warp takes two steps of 32 / L rows at least
     const int warps = steps < 1 ? 1 : steps > 8 ? 8 : steps;
-    return free_launch(free_overlap_for_rows(a.M), layer_norm_narrow_bwd_kernel<TX, TY, L, C, VW>, dim3((unsigned)a.groups * (unsigned)a.chunks),
+    return free_launch(free_overlap_for_rows(a.M), layer_norm_narrow_bwd_kernel<TX, TY, L, C, VW, RMS>, dim3((unsigned)a.groups * (unsigned)a.chunks),
                        dim3(warps * 32), 0, s, a);
 }
 
@@ -725,44 +752,45 @@ int launch_fwd(const NormArgs& a, cudaStream_t s) {
     }
 }
 
-template <typename TX, typename TY, int C, int VW, int MAXT, int T, int R>
+template <typename TX, typename TY, int C, int VW, int MAXT, int T, int R, bool RMS>
 int start_bwd(const NormArgs& a, int threads, cudaStream_t s) {
-    auto kernel = layer_norm_bwd_kernel<TX, TY, C, VW, MAXT, T, R>;
+    auto kernel = layer_norm_bwd_kernel<TX, TY, C, VW, MAXT, T, R, RMS>;
     const size_t smem = kAhead<TX, TY, VW> ? (size_t)threads * 2 * R * C * (2 * sizeof(TX) + sizeof(TY)) : 0;
     if (smem > 47 * 1024) FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     return free_launch(free_overlap_for_rows(a.M), kernel, dim3((unsigned)a.groups * (unsigned)a.chunks), dim3(threads), smem, s, a);
 }
-template <typename TX, typename TY, int VW>
+template <typename TX, typename TY, int VW, bool RMS>
 int start_wide_bwd(const NormArgs& a, int threads, cudaStream_t s) {
     const int cols = bwd_cols(a.D);
-    if (cols == 12) return start_bwd<TX, TY, 12, VW, 128, kBwdT, 1>(a, threads, s);
-    if (cols == 16) return start_bwd<TX, TY, 16, VW, 512, kBwdT, 1>(a, threads, s);
+    if (cols == 12) return start_bwd<TX, TY, 12, VW, 128, kBwdT, 1, RMS>(a, threads, s);
+    if (cols == 16) return start_bwd<TX, TY, 16, VW, 512, kBwdT, 1, RMS>(a, threads, s);
     if constexpr (VW == 1) {
-        if (threads <= 256) return start_bwd<TX, TY, 8, VW, 256, kBwdT, 2>(a, threads, s);
-        if (threads > 576) return start_bwd<TX, TY, 8, VW, 1024, 1024, 1>(a, threads, s);
+        if (threads <= 256) return start_bwd<TX, TY, 8, VW, 256, kBwdT, 2, RMS>(a, threads, s);
+        if (threads > 576) return start_bwd<TX, TY, 8, VW, 1024, 1024, 1, RMS>(a, threads, s);
     }
-    return start_bwd<TX, TY, 8, VW, 576, 576, 2>(a, threads, s);
+    return start_bwd<TX, TY, 8, VW, 576, 576, 2, RMS>(a, threads, s);
 }
 
-template <typename TX, typename TY, int VW>
+template <typename TX, typename TY, int VW, bool RMS>
 int launch_bwd(NormArgs a, cudaStream_t s) {
     const int threads = bwd_threads(a.D);
     a.warps = threads / 32;
     constexpr int C = kNarrowCols<VW>;
-    const int r = a.D <= 32 ? start_narrow_bwd<TX, TY, 8, 4, VW>(a, s) : a.D <= 64 ? start_narrow_bwd<TX, TY, 64 / C, C, VW>(a, s)
-                : a.D <= 128 ? start_narrow_bwd<TX, TY, 128 / C, C, VW>(a, s)
-                : narrow(a.D) ? start_narrow_bwd<TX, TY, 32, 8, VW>(a, s) : start_wide_bwd<TX, TY, VW>(a, threads, s);
+    const int r = a.D <= 32 ? start_narrow_bwd<TX, TY, 8, 4, VW, RMS>(a, s) : a.D <= 64 ? start_narrow_bwd<TX, TY, 64 / C, C, VW, RMS>(a, s)
+                : a.D <= 128 ? start_narrow_bwd<TX, TY, 128 / C, C, VW, RMS>(a, s)
+                : narrow(a.D) ? start_narrow_bwd<TX, TY, 32, 8, VW, RMS>(a, s) : start_wide_bwd<TX, TY, VW, RMS>(a, threads, s);
     if (r != FREE_OK || a.chunks == 1 || (!a.dw && !a.db)) return r;
-    return free_launch(free_launch_overlap_enabled(), layer_norm_reduce_kernel, dim3((unsigned)a.groups * ((2u * a.D + 31) / 32)), dim3(512), 0, s, a);
+    return free_launch(free_launch_overlap_enabled(), layer_norm_reduce_kernel,
+                       dim3((unsigned)a.groups * (((RMS ? 1u : 2u) * a.D + 31) / 32)), dim3(512), 0, s, a, (RMS ? 1 : 2) * a.D);
 }
 
 template <typename TX, typename TY>
 int launch_fwd_vw(const NormArgs& a, int vw, cudaStream_t s) {
     return vw == 4 ? launch_fwd<TX, TY, 4>(a, s) : vw == 2 ? launch_fwd<TX, TY, 2>(a, s) : launch_fwd<TX, TY, 1>(a, s);
 }
-template <typename TX, typename TY>
+template <typename TX, typename TY, bool RMS = false>
 int launch_bwd_vw(const NormArgs& a, int vw, cudaStream_t s) {
-    return vw == 4 ? launch_bwd<TX, TY, 4>(a, s) : vw == 2 ? launch_bwd<TX, TY, 2>(a, s) : launch_bwd<TX, TY, 1>(a, s);
+    return vw == 4 ? launch_bwd<TX, TY, 4, RMS>(a, s) : vw == 2 ? launch_bwd<TX, TY, 2, RMS>(a, s) : launch_bwd<TX, TY, 1, RMS>(a, s);
 }
 
 // Consecutive columns of one access: what D, the row strides and the tables' rows are aligned to (base pointers of rows are
@@ -839,4 +867,29 @@ extern "C" int free_op_layer_norm_bwd(int x_dtype, int y_dtype, int n_groups, in
     using bf = __nv_bfloat16;
     if (x_dtype == FREE_FP32) return y_dtype == FREE_FP32 ? launch_bwd_vw<float, float>(a, vw, s) : launch_bwd_vw<float, bf>(a, vw, s);
     return y_dtype == FREE_FP32 ? launch_bwd_vw<bf, float>(a, vw, s) : launch_bwd_vw<bf, bf>(a, vw, s);
+}
+
+size_t rms_norm_bwd_bytes(int groups, int rows_per_group, int D) { return free_op_layer_norm_bwd_workspace_bytes(groups, rows_per_group, D) / 2; }
+
+bool rms_norm_bwd_takes_heads(int D) { return narrow(D); }
+
+int rms_norm_bwd(const RmsBwdArgs& b, cudaStream_t s) {
+    NormArgs a{};
+    a.M = (long long)b.groups * b.rows_per_group; a.D = b.D; a.groups = b.groups; a.rows_per_group = b.rows_per_group;
+    a.heads = b.heads;
+    a.x = b.x; a.x_stride = b.x_tok; a.x_head = b.x_head; a.dy = b.dy; a.dy_stride = b.dy_tok; a.dy_head = b.dy_head;
+    a.rstd_in = b.rstd; a.weight = b.weight; a.mod_stride = b.mod_stride; a.unit = b.unit;
+    a.dres = b.dres; a.dres_stride = b.dres_tok; a.dres_head = b.dres_head; a.dx = b.dx; a.dx_stride = b.dx_tok; a.dx_head = b.dx_head;
+    a.dw = b.dw; a.dmod_stride = b.dmod_stride; a.partial = b.ws;
+    a.chunks = b.rows_per_group ? chunks_of(b.groups, b.rows_per_group, b.D) : 1;
+    if ((long long)b.groups * a.chunks > 0x7fffffffLL || (long long)b.groups * ((b.D + 31LL) / 32) > 0x7fffffffLL) return FREE_ERR_UNSUPPORTED;
+    if (b.dw && a.chunks > 1 && (!b.ws || b.ws_bytes < rms_norm_bwd_bytes(b.groups, b.rows_per_group, b.D))) return FREE_ERR_WORKSPACE;
+    const long long strides = b.x_tok | b.dy_tok | b.dx_tok | (b.dres ? b.dres_tok : 0) | (b.heads > 1 ? b.x_head | b.dy_head | b.dx_head | (b.dres ? b.dres_head : 0) : 0);
+    // addresses counted in elements: accesses are as wide as their low bits allow
+    auto place = [](const void* p, int dtype) { return (long long)(reinterpret_cast<uintptr_t>(p) / (dtype == FREE_FP32 ? 4 : 2)) & 7; };
+    const long long places = place(b.x, b.x_dtype) | place(b.dy, b.dy_dtype) | place(b.dx, b.x_dtype) | place(b.dres, b.x_dtype);
+    const int vw = width_of(b.D, strides | places, b.weight, nullptr, b.groups, b.mod_stride);
+    using bf = __nv_bfloat16;
+    if (b.x_dtype == FREE_FP32) return b.dy_dtype == FREE_FP32 ? launch_bwd_vw<float, float, true>(a, vw, s) : launch_bwd_vw<float, bf, true>(a, vw, s);
+    return b.dy_dtype == FREE_FP32 ? launch_bwd_vw<bf, float, true>(a, vw, s) : launch_bwd_vw<bf, bf, true>(a, vw, s);
 }
