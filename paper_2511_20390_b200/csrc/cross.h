@@ -35,6 +35,13 @@ __device__ __forceinline__ const uint8_t* cross_mask(const CrossWhere& w, const 
     return w.mask ? w.mask + (w.offsets ? (long long)sp.row0 : (long long)sp.enc * w.n_kv) : nullptr;
 }
 
+// Parts of the states of a call with few tokens (cross_join adds them): part p of row r = (sequence, head, token)
+struct CrossParts {
+    int n;                                    // parts; 1: results are written at once
+    float* out;                               // [n][rows][d], each part's own softmax
+    float* lse;                               // [n][rows]
+};
+
 struct CrossArgs {
     CrossMat q, k, v, o;                      // o: forward's result
     CrossMat g, dq, dk, dv;                   // backward: dout and the gradients
@@ -45,6 +52,12 @@ struct CrossArgs {
     float* delta;                             // backward: <dout, out>, laid out as lse
     uint32_t* err;
 };
+
+// Tensor cores, bf16
+bool cross_tc_supported(const CrossArgs& a);
+CrossParts cross_tc_parts(const CrossArgs& a);
+int cross_tc_forward(const CrossArgs& a, const CrossParts& parts, cudaStream_t s);
+int cross_join(int dtype, const CrossArgs& a, const CrossParts& parts, cudaStream_t s);
 
 // CUDA cores, fp32 or bf16, any strides and alignment
 int cross_simt_forward(int dtype, const CrossArgs& a, cudaStream_t s);

@@ -38,7 +38,7 @@ CrossArgs args_of(const free_cross_attn* c) {
     a.q = CrossMat{c->q, c->q_seq, c->q_tok, c->q_head};
     a.k = CrossMat{c->k, c->kv_offsets ? 0 : c->k_seq, c->k_tok, c->k_head};
     a.v = CrossMat{c->v, c->kv_offsets ? 0 : c->v_seq, c->v_tok, c->v_head};
-    a.where = CrossWhere{c->kv_lens, c->kv_offsets, c->kv_seq, c->kv_mask, c->n_enc, states(c) ? c->n_kv : 0, c->kv_rows, 1};
+    a.where = CrossWhere{c->kv_lens, c->kv_offsets, c->kv_seq, c->kv_mask, c->n_enc, states(c) ? c->n_kv : 0, c->kv_offsets ? c->kv_rows : c->n_kv, 1};
     if (!c->kv_seq && c->n_enc) a.where.share = c->n_seq / c->n_enc > 0 ? c->n_seq / c->n_enc : 1;
     a.n_seq = c->n_seq; a.n_q = c->n_q; a.heads = c->heads; a.kv_heads = c->kv_heads; a.d = c->d_head; a.group = c->heads / c->kv_heads;
     a.scale = c->scale;
@@ -70,6 +70,15 @@ int result(const void* p, int e, long long seq, long long tok, long long head, i
     return FREE_OK;
 }
 
+size_t row_count(const free_cross_attn* c) { return (size_t)c->n_seq * c->heads * c->n_q; }
+
+// parts of the states, and where they lie in the workspace
+CrossParts parts_of(const CrossArgs& a, int dtype) {
+    if (dtype == FREE_BF16 && cross_tc_supported(a)) return cross_tc_parts(a);
+    return CrossParts{1, nullptr, nullptr};
+}
+size_t part_bytes(const free_cross_attn* c, int parts) { return parts > 1 ? free_round_up(row_count(c) * parts * 4, 256) + row_count(c) * parts * c->d_head * 4 : 0; }
+
 size_t stat_bytes(const free_cross_attn* c) { return free_round_up((size_t)c->n_seq * c->heads * c->n_q * 4, 256); }
 
 }  // namespace
@@ -77,7 +86,10 @@ size_t stat_bytes(const free_cross_attn* c) { return free_round_up((size_t)c->n_
 extern "C" size_t free_op_cross_attention_workspace_bytes(const free_cross_attn* c) {
     bool empty;
     if (check(c, &empty) != FREE_OK || empty) return 0;
-    return 0;
+    // where the inputs turn out to be no matter for the tensor cores, less is used
+    CrossArgs a = args_of(c);
+    a.o = a.q;
+    return part_bytes(c, parts_of(a, c->dtype).n);
 }
 
 extern "C" int free_op_cross_attention(const free_cross_attn* c, void* out, int64_t o_seq, int64_t o_tok, int64_t o_head, float* lse, void* ws,
@@ -92,7 +104,16 @@ extern "C" int free_op_cross_attention(const free_cross_attn* c, void* out, int6
     CrossArgs a = args_of(c);
     a.o = CrossMat{out, o_seq, o_tok, o_head};
     a.lse = lse; a.err = device_error;
-    (void)ws; (void)ws_bytes;
+    if (c->dtype == FREE_BF16 && cross_tc_supported(a)) {
+        CrossParts p = cross_tc_parts(a);
+        if (p.n > 1) {
+            if (!ws || ws_bytes < part_bytes(c, p.n)) return FREE_ERR_WORKSPACE;
+            if (!free_aligned16(ws)) return FREE_ERR_ALIGN;
+            p.lse = (float*)ws;
+            p.out = (float*)((char*)ws + free_round_up(row_count(c) * p.n * 4, 256));
+        }
+        return cross_tc_forward(a, p, (cudaStream_t)stream);
+    }
     return cross_simt_forward(c->dtype, a, (cudaStream_t)stream);
 }
 

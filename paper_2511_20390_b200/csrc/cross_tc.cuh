@@ -1,0 +1,57 @@
+// What the tensor-core kernels of the attention to an encoder's states share: tile copies of heads and operands in tensor memory.
+#pragma once
+#include "cross.h"
+#include "tc_common.cuh"
+
+namespace cross_tc {
+
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c, int head, int tok, int seq) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"((uint64_t)map), "r"(tc::smem_u32(bar)), "r"(c), "r"(head), "r"(tok), "r"(seq) : "memory");
+}
+__device__ __forceinline__ void store_4d(const CUtensorMap* map, uint32_t src, int c, int head, int tok, int seq) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+                 ::"l"((uint64_t)map), "r"(src), "r"(c), "r"(head), "r"(tok), "r"(seq) : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem], one step of 16: lane m of A is row m, its 32-bit column c holds elements 2 c and 2 c + 1
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Operand whose contraction runs along the rows of memory: blocks of 64 columns (128 bytes, swizzled) `block` bytes apart, groups of
+// 8 rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_mn(uint32_t saddr, uint32_t block) {
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(block >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+constexpr uint32_t kBMajorMN = 1u << 16;      // instruction descriptor: B's contraction runs along rows
+
+// The 128 states from j0 on that count, one bit each.
+struct Bits {
+    uint32_t w[4];
+};
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+template <int WORDS> __device__ __forceinline__ void count_bits(uint32_t (&w)[WORDS], const uint8_t* mask, int j0, int len, int lane) {   // whole warp
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+        w[i] = low_bits(len - j0 - 32 * i);
+        if (mask) {
+            const int j = j0 + 32 * i + lane;
+            w[i] &= __ballot_sync(0xffffffffu, j < len && mask[j] != 0);
+        }
+    }
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------
+// bf16 heads [seq][tok][head][d] as a tensor map whose boxes are 64 channels x `heads_box` heads x `tok_box` tokens (128-byte
+// swizzle; zero outside).  Dimensions of one element and strides of zero (a matrix that several share) become dimensions of one:
+// their coordinates have to be 0.
+bool mappable(const CrossMat& m, int n_seq, int n_tok, int heads);
+int map_heads(CUtensorMap* map, const CrossMat& m, int n_seq, int n_tok, int heads, int d, int heads_box, int tok_box);
+
+}  // namespace cross_tc

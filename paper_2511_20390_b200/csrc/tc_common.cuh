@@ -278,3 +278,5 @@ int free_tensor_map_2d_typed(CUtensorMap* map, int elem_bytes, const void* base,
                              uint64_t outer_stride_bytes, uint32_t box_inner, uint32_t box_outer, int swizzle_bytes);
 int free_tensor_map_3d(CUtensorMap* map, const void* base, uint64_t d0, uint64_t d1, uint64_t d2,
                        uint64_t stride1_bytes, uint64_t stride2_bytes, uint32_t b0, uint32_t b1, uint32_t b2, int swizzle_bytes);
+// 4-D bf16 tensor map, 128-byte swizzle; dims[0] is contiguous, strides (bytes) of the others
+int free_tensor_map_4d(CUtensorMap* map, const void* base, const uint64_t (&dims)[4], const uint64_t (&strides_bytes)[3], const uint32_t (&box)[4]);

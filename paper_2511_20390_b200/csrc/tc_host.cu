@@ -66,3 +66,19 @@ int free_tensor_map_3d(CUtensorMap* map, const void* base, uint64_t d0, uint64_t
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? FREE_OK : FREE_ERR_CUDA;
 }
+
+int free_tensor_map_4d(CUtensorMap* map, const void* base, const uint64_t (&dims)[4], const uint64_t (&strides_bytes)[3], const uint32_t (&box)[4]) {
+    auto fn = encode_fn();
+    if (!fn) return FREE_ERR_CUDA;
+    cuuint64_t d[4], st[3];
+    cuuint32_t b[4], one[4] = {1, 1, 1, 1};
+    for (int i = 0; i < 4; ++i) { d[i] = dims[i]; b[i] = box[i]; }
+    for (int i = 0; i < 3; ++i) {
+        st[i] = strides_bytes[i];
+        if (st[i] % 16) return FREE_ERR_UNSUPPORTED;
+    }
+    if (b[0] * 2u > 128 || b[0] * 2u % 16 || b[1] > 256 || b[2] > 256 || b[3] > 256) return FREE_ERR_UNSUPPORTED;
+    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), d, st, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? FREE_OK : FREE_ERR_CUDA;
+}

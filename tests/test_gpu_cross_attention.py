@@ -190,3 +190,13 @@ def test_flat_and_sharp_scores(dt, spread):
     """Scores of hundreds: single states take everything; offsets of the running maximum move."""
     Case(13, dt, 2, 2, 140, 400, 2, 2, 64, spread=spread).check()
     Case(14, dt, 1, 1, 70, 300, 2, 1, 72, spread=spread, scale=0.5).check()
+
+
+@pytest.mark.parametrize("layout", ["padded", "packed"])
+@pytest.mark.parametrize("shape,lens", [
+    ((16, 4, 520, 300, 12, 12, 72), [300, 1, 0, 257]), ((40, 8, 130, 90, 8, 2, 64), "ragged"), ((30, 30, 33, 140, 10, 5, 128), "ragged"),
+    ((200, 1, 5, 130, 4, 1, 40), "full"), ((3, 3, 1500, 520, 16, 16, 48), [520, 512, 513]),
+])
+def test_more_items_than_sms(shape, lens, layout):
+    """CTAs walk over several items each, long and short ones, some without a state."""
+    Case(21, "bf16", *shape, lens=lens, layout=layout, mask=shape[0] == 30).check()
