@@ -3,11 +3,11 @@
 //   S = Q K^T (tcgen05, fp32 in tensor memory);  p = 2^(c S - m), c = scale log2 e;  O += p V;  out = O / sum p
 //
 // Persistent CTAs, one per SM.  An item is two tiles of 128 rows of one (sequence, key head), rows being (token, query head of the key
-// head's group), so that shared key heads are read once.  A warpgroup per tile does the softmax, a thread per row; one warp
-// loads tiles by TMA, one issues the MMAs.  While one tile's exponentials run, the tensor pipe does the other tile's products.
-//   - p goes back to tensor memory, over its own scores, as the left operand of O += p V: it never passes shared memory.
-//   - Blocks of 64 states, the scores of two of them per tile in tensor memory: while the softmax works on one, the next (of the next
-//     item, too) is there already.  Scores are issued right behind the O += p V that reads the p in their columns; the pipe runs in order.
+// head's group), so that shared key heads are read once.  Blocks of 64 states.  A warpgroup per tile does the softmax, a thread per
+// row; one warp finds the items and loads tiles by TMA, four issue MMAs (per tile the scores, and O += p V), a warpgroup writes
+// results while the softmax is at the next item.
+//   - p goes back to tensor memory as the left operand of O += p V: it never passes shared memory.  Scores are free for the next block
+//     as soon as they are in registers, so the two products and the softmax of a tile run beside one another.
 //   - V is the right operand as it lies in memory (contraction along its rows), so nothing is transposed.
 //   - The maximum that p is taken against moves only when it has grown by 2^8; then O is rescaled in tensor memory.
 //   - The last block of a sequence costs the 16-column steps that it has.  States that do not count: scores are replaced by -inf, and the
@@ -36,17 +36,26 @@ namespace {
 using namespace cross_tc;
 
 constexpr int BQ = 128, BK = 64;
-constexpr int kThreads = 512, kSms = 148;     // warps 0 - 7 softmax, 8 - 11 results, 12 loads, 13, 14 MMAs
-// Registers: 512 x 128 at launch, of which the softmax takes 152 each (64 scores of a row at a time) and the others keep 104.
-constexpr int kSoftmaxRegs = 152, kOtherRegs = 104;
-static_assert(256 * (kSoftmaxRegs + kOtherRegs) <= kThreads * 128, "registers of the launch");
+// warps 0 - 7 softmax, 8 - 11 results, 12 loads, 13 tokens without a state, 14 and 15 idle, 16, 17 Q K^T of the tiles, 18, 19 p V
+constexpr int kThreads = 640, kSms = 148;
+// Registers: 640 x 96 at launch.
+constexpr int kSoftmaxRegs = 152, kOtherRegs = 56;
+static_assert(256 * kSoftmaxRegs + 384 * kOtherRegs <= kThreads * 96, "registers of the launch");
 constexpr uint32_t kChunk = BQ * 128, kKvChunk = BK * 128;      // rows x 64 channels, 128-byte rows
-constexpr uint32_t kTmemCols = 512;           // scores: tile w, buffer b at column 128 w + 64 b; O of tile w at 256 + 128 w
-constexpr uint32_t kCtrl = 2048;              // barriers, and 1 / sum p of the rows of both tiles
-template <int NCH> struct Mem {               // NCH: chunks of 64 channels
-    static constexpr int slots = NCH == 1 ? 12 : 6;
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kCtrl = 3072;              // barriers, the queue of items, maxima and sums of the rows of both tiles
+constexpr uint32_t kQueue = 8;
+constexpr uint32_t kStage = 32 * 128;         // 32 rows x 64 channels on their way out
+// State sequences up to this length take two sets of the tiles of Q: with nothing but a block or two per item, Q has to be on its way
+// while the item before is worked on.  Longer ones take the room for K and V.
+constexpr int kShort = 128;
+// NCH: chunks of 64 channels; QB: sets of the two tiles of Q; SB, PB: buffers of a tile's scores and of its p in tensor memory.  Scores
+// are free for the next block as soon as they are in registers, p when O += p V has read it.
+template <int NCH, int QB, int SB, int PB> struct Mem {
+    static constexpr uint32_t s_col = 0, p_col = 2 * SB * 64, o_col = p_col + 2 * PB * 32, o_width = (512 - o_col) / 2;    // columns, O per tile
+    static constexpr uint32_t slots = NCH == 1 ? 12 : QB == 1 ? 6 : 4, stages = NCH == 2 && QB == 2 ? 1 : 2;    // stages: of every warp of results
     static constexpr uint32_t q = NCH * kChunk, kv = NCH * kKvChunk;
-    static constexpr uint32_t bytes = 1024 + kCtrl + 2 * q + slots * kv + 2 * q;
+    static constexpr uint32_t bytes = 1024 + kCtrl + QB * 2 * q + slots * kv + 4 * stages * kStage;
     static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
 };
 
@@ -71,58 +80,47 @@ struct Args {
     uint32_t kv_heads;
     int kv_head_mul, kv_seq_mul, v_head_mul, v_seq_mul, q_seq_mul, q_head_mul;      // 0 where one matrix serves all
     long long rows;                           // n_seq * heads * n_q
-    float c, ln2_over_c, scale;               // c: scale * log2 e
+    float c, scale;                           // c: scale * log2 e
     float *lse, *part_out, *part_lse;
+    CrossMat o;
+    bool boxed;
     uint32_t* err;
 };
 
-// One item: its place and the blocks of states that it covers.
-struct Item {
-    int s, kh, t0, part, tiles, b0, nb, limit;      // limit: tokens; blocks b0 .. b0 + nb - 1
-    CrossSpan sp;
+// One item: its place, and the blocks of states that it covers.  The warp that loads tiles finds them out, once for all.
+struct alignas(16) Item {
+    int s, kh, t0, part, tiles, nb;           // s < 0: no more items
+    int left;                                 // states from the item's first on
+    int enc, row;                             // its first state: encoder sequence and row
+    int pad[3];
 };
 __device__ __forceinline__ Item item_of(const Args& a, uint32_t i) {
     Item it;
+    if (i >= a.items) { it.s = -1; it.nb = 0; it.tiles = 0; return it; }
     const uint32_t k = a.by_parts(i), sh = a.by_pairs(k);
     it.part = (int)(i - k * a.parts);
     const int pair = (int)(k - sh * a.pairs);
     it.s = (int)a.by_kv_heads(sh); it.kh = (int)(sh - it.s * a.kv_heads);
     it.t0 = pair * a.tiles * a.tt;
     it.tiles = a.tiles == 2 && it.t0 + a.tt < a.n_q ? 2 : 1;
-    it.sp = cross_span_of_enc(a.where, a.where.seq_of ? __ldg(a.where.seq_of + it.s) : (int)a.by_share(it.s));
-    const int blocks = (it.sp.len + BK - 1) / BK;
-    it.b0 = 0; it.nb = blocks;
+    const CrossSpan sp = cross_span_of_enc(a.where, a.where.seq_of ? __ldg(a.where.seq_of + it.s) : (int)a.by_share(it.s));
+    const int blocks = (sp.len + BK - 1) / BK;
+    int b0 = 0;
+    it.nb = blocks;
     if (a.parts > 1) {
-        it.b0 = (int)((long long)blocks * it.part / a.parts);
-        it.nb = (int)((long long)blocks * (it.part + 1) / a.parts) - it.b0;
+        b0 = (int)((long long)blocks * it.part / a.parts);
+        it.nb = (int)((long long)blocks * (it.part + 1) / a.parts) - b0;
     }
+    it.left = sp.len - b0 * BK; it.enc = sp.enc; it.row = sp.row0 + b0 * BK;
     return it;
 }
-__device__ __forceinline__ int columns_of(const Item& it, int j) {       // of scores, in steps of 16
-    const int left = it.sp.len - (it.b0 + j) * BK;
-    return left >= BK ? BK : (left + 15) & ~15;
-}
 
-// Walks over the blocks of all of a CTA's items that have any.
-struct Steps {
-    const Args& a;
-    uint32_t i, step;
-    Item it;
-    int j;
-    bool live;
-    __device__ __forceinline__ Steps(const Args& args, uint32_t first, uint32_t stride) : a(args), i(first - stride), step(stride), j(0), live(true) { next_item(); }
-    __device__ __forceinline__ void next_item() {
-        for (;;) {
-            i += step;
-            if (i >= a.items) { live = false; return; }
-            it = item_of(a, i);
-            j = 0;
-            if (it.nb > 0) return;
-        }
-    }
-    __device__ __forceinline__ void next() { if (++j == it.nb) next_item(); }
-    __device__ __forceinline__ bool last() const { return j == it.nb - 1; }
-};
+// Two fp32 numbers side by side: one instruction for both.
+__device__ __forceinline__ uint64_t pair(float a, float b) { uint64_t v; asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); return v; }
+__device__ __forceinline__ float low(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float high(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 
 // One step of 16 of a product, issued by the leader of a converged warp; descriptors differ in their low words only.
 __device__ __forceinline__ void mma_ts_if(uint32_t issue, uint32_t d, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -131,42 +129,42 @@ __device__ __forceinline__ void mma_ts_if(uint32_t issue, uint32_t d, uint32_t a
                  ::"r"(d), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate), "r"(issue) : "memory");
 }
 
-template <int NCH>
+template <int NCH, int QB, int SB, int PB>
 __global__ void __launch_bounds__(kThreads, 1)
 cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
                 const __grid_constant__ CUtensorMap mapO, const Args a) {
-    using M = Mem<NCH>;
+    using M = Mem<NCH, QB, SB, PB>;
     constexpr uint32_t NS = M::slots;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t* kv_full = reinterpret_cast<uint64_t*>(smem);
     uint64_t* kv_empty = kv_full + NS;
-    uint64_t* q_full = kv_empty + NS;         // [tile]
-    uint64_t* q_empty = q_full + 2;
-    uint64_t* o_free = q_empty + 2;           // results have been read from tensor memory
-    uint64_t* pv_done = o_free + 2;           // every O += p V
-    uint64_t* o_full = pv_done + 2;           // an item's last
-    uint64_t* inv_full = o_full + 2;
-    uint64_t* inv_free = inv_full + 2;
-    uint64_t* s_full = inv_free + 2;          // [tile][buffer]
-    uint64_t* p_full = s_full + 4;
-    uint64_t* group = p_full + 4;             // the warps that write results meet
-    uint64_t* turn = group + 1;               // tile 0 has done an item's first exponentials
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(turn + 1);
+    uint64_t* item_full = kv_empty + NS;
+    uint64_t* item_free = item_full + kQueue;
+    uint64_t* q_full = item_free + kQueue;    // [tile][set]
+    uint64_t* q_empty = q_full + 4;
+    uint64_t* s_full = q_empty + 4;           // [tile][buffer]
+    uint64_t* s_free = s_full + 4;
+    uint64_t* p_full = s_free + 4;
+    uint64_t* pv_done = p_full + 4;           // O += p V is complete, p is free
+    uint64_t* o_free = pv_done + 4;           // [tile]: results have been read from tensor memory
+    uint64_t* o_full = o_free + 2;            // an item's last O += p V
+    uint64_t* sums_full = o_full + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sums_full + 2);
     volatile uint32_t* abort_flag = tmem_slot + 1;
-    float* invs = reinterpret_cast<float*>(smem + 1024);      // [tile][row]
+    Item* queue = reinterpret_cast<Item*>(smem + 640);
+    float2* sums = reinterpret_cast<float2*>(smem + 1024);    // [tile][row]: maximum in use, sum
+    static_assert((2 * NS + 2 * kQueue + 24 + 6 + 1) * 8 <= 640 && 640 + kQueue * sizeof(Item) <= 1024 && 1024 + 2 * BQ * 8 <= kCtrl, "control block");
     uint8_t* sQ = smem + kCtrl;
-    uint8_t* ring = sQ + 2 * M::q;
+    uint8_t* ring = sQ + QB * 2 * M::q;
     uint8_t* staging = ring + NS * M::kv;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < NS; ++i) { tc::mbar_init(&kv_full[i], 1); tc::mbar_init(&kv_empty[i], 2); }
-        for (int i = 0; i < 2; ++i) { tc::mbar_init(&q_full[i], 1); tc::mbar_init(&q_empty[i], 1); tc::mbar_init(&o_free[i], 4); tc::mbar_init(&pv_done[i], 1); }
-        for (int i = 0; i < 2; ++i) { tc::mbar_init(&o_full[i], 1); tc::mbar_init(&inv_full[i], 4); tc::mbar_init(&inv_free[i], 4); }
-        tc::mbar_init(group, 4);
-        tc::mbar_init(turn, 4);
-        for (int i = 0; i < 4; ++i) { tc::mbar_init(&s_full[i], 1); tc::mbar_init(&p_full[i], 4); }
+        for (uint32_t i = 0; i < kQueue; ++i) { tc::mbar_init(&item_full[i], 1); tc::mbar_init(&item_free[i], 16); }     // 8 softmax, 4 results, 4 MMA
+        for (int i = 0; i < 4; ++i) { tc::mbar_init(&q_full[i], 1); tc::mbar_init(&q_empty[i], 1); tc::mbar_init(&s_full[i], 1); tc::mbar_init(&s_free[i], 4); tc::mbar_init(&p_full[i], 4); tc::mbar_init(&pv_done[i], 1); }
+        for (int i = 0; i < 2; ++i) { tc::mbar_init(&o_free[i], 4); tc::mbar_init(&o_full[i], 1); tc::mbar_init(&sums_full[i], 4); }
         *abort_flag = 0;
         tc::fence_barrier_init();
         tc::fence_proxy_async();
@@ -180,37 +178,47 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     free_grid_dep_wait();                                // only this CTA's shared and tensor memory was touched so far
     free_grid_dep_launch();
     const int ks = (a.d + 15) / 16;                      // 16-channel steps
+    auto see = [&](uint32_t n) { return cross_tc::wait(&item_full[n % kQueue], n / kQueue & 1u, abort_flag); };
+    auto leave = [&](uint32_t n) {
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&item_free[n % kQueue]);
+    };
 
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         // ------------------------------------------------------------------ softmax: a warpgroup per tile, a thread per row
         const int w = warp >> 2, q = warp & 3, r = q * 32 + lane;
-        const uint32_t ts = tmem + w * 128u + ((uint32_t)(q * 32) << 16), to = ts + 256u;
-        const int row_t = r / a.group, row_h = r - row_t * a.group;
-        uint32_t n = 0, ns = 0, inv_ph = 1, turn_ph = 0;    // blocks of the CTA (a pair of slots each), and of this tile, so far
+        const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16), to = lanes + M::o_col + w * M::o_width;
+        uint32_t ns = 0, slot0 = 0, slot_ph = 0, free_ph = 1;    // blocks of this tile so far; ring position of the block's K
         bool ok = true;
-        Item ahead = item_of(a, blockIdx.x);             // its loads are under way while the item before is worked on
-        for (uint32_t i = blockIdx.x; ok && i < a.items; i += gridDim.x) {
-            const Item it = ahead;
-            if (i + gridDim.x < a.items) ahead = item_of(a, i + gridDim.x);
-            const uint32_t first = n;
-            n += (uint32_t)it.nb;
-            if (w >= it.tiles) continue;
-            const uint8_t* mask = cross_mask(a.where, it.sp);
+        for (uint32_t n = 0; ok; ++n) {
+            ok = see(n);
+            if (!ok) break;
+            const Item& it = queue[n % kQueue];
+            if (it.s < 0) break;
+            const int nb = it.nb, states = it.left, tiles = it.tiles;
+            const uint8_t* mask = a.where.mask ? a.where.mask + (a.where.offsets ? 0 : (long long)it.enc * a.where.n_kv) + it.row : nullptr;
+            leave(n);
+            if (w >= tiles) {
+                slot0 += 2u * nb;
+                while (slot0 >= NS) { slot0 -= NS; slot_ph ^= 1u; }
+                continue;
+            }
             float top = -INFINITY, sum = 0.f;            // maximum in use
-            for (int j = 0; j < it.nb; ++j, ++ns) {
-                const uint32_t tsb = ts + (ns & 1u) * 64u, bar = 2 * w + (ns & 1u);
-                const int left = it.sp.len - (it.b0 + j) * BK;
-                const bool whole = left >= BK && !mask;
-                ok = tc::wait_uniform(&s_full[bar], ns >> 1 & 1u, abort_flag);
+            for (int j = 0; j < nb; ++j, ++ns) {
+                const uint32_t buf = 2 * w + ns % SB, pbuf = 2 * w + ns % PB;
+                const bool whole = states - j * BK >= BK && !mask;
+                ok = cross_tc::wait(&s_full[buf], ns / SB & 1u, abort_flag);
                 if (!ok) break;
                 tc::tc_fence_after();
-                uint32_t x[64];
-                tc::tmem_ld64(tsb, x);
+                uint32_t x[64], bits[2];
+                tc::tmem_ld64(lanes + M::s_col + (w * SB + ns % SB) * 64u, x);
                 tc::tmem_wait_ld();
-                uint32_t bits[2];
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&s_free[buf]);
                 if (!whole) {
-                    count_bits(bits, mask, (it.b0 + j) * BK, it.sp.len, lane);
+                    count_bits(bits, mask, j * BK, states, lane);
 #pragma unroll
                     for (int e = 0; e < 64; ++e) x[e] = bits[e >> 5] >> (e & 31) & 1u ? x[e] : 0xff800000u;
                 }
@@ -225,7 +233,8 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                     top = nt;
                     sum *= alpha;
                     if (j > 0) {
-                        ok = tc::wait_uniform(&pv_done[w], (ns - 1u) & 1u, abort_flag);
+                        // the product before (the one before that is complete, or p of the last block could not have been stored)
+                        ok = cross_tc::wait(&pv_done[2 * w + (ns - 1u) % PB], (ns - 1u) / PB & 1u, abort_flag);
                         if (!ok) break;
                         tc::tc_fence_after();
                         for (int c = 0; c < ks; ++c) {
@@ -239,39 +248,29 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                     }
                 }
                 const float base = top == -INFINITY ? 0.f : top * a.c;
-                // the tiles start an item one behind the other, so that one's exponentials run beside the other's remaining work
-                if (j == 0 && it.tiles == 2 && w == 1) {
-                    ok = tc::wait_uniform(turn, turn_ph, abort_flag);
-                    turn_ph ^= 1u;
-                    if (!ok) break;
-                }
-                float s4[4] = {0.f, 0.f, 0.f, 0.f};
+                const uint64_t c2 = pair(a.c, a.c), b2 = pair(-base, -base);
+                uint64_t s2[2] = {0ull, 0ull};
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float p0 = ex2(fmaf(__uint_as_float(x[32 * c + 2 * e]), a.c, -base)), p1 = ex2(fmaf(__uint_as_float(x[32 * c + 2 * e + 1]), a.c, -base));
-                        s4[e & 3] += p0;
-                        s4[(e + 2) & 3] += p1;
-                        pk[e] = pack2(p0, p1);
-                    }
-                    tc::tmem_st16(tsb + 16 * c, pk);
+                for (int e = 0; e < 32; ++e) {
+                    const uint64_t y = fma2(pair(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), c2, b2);
+                    const float p0 = ex2(low(y)), p1 = ex2(high(y));
+                    s2[e & 1] = add2(s2[e & 1], pair(p0, p1));
+                    x[e] = pack2(p0, p1);
                 }
-                sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-                if (j == 0 && it.tiles == 2 && w == 0) {
-                    __syncwarp();
-                    if (lane == 0) tc::mbar_arrive(turn);
-                }
+                ok = cross_tc::wait(&pv_done[pbuf], (ns / PB & 1u) ^ 1u, abort_flag);
+                if (!ok) break;
+                tc::tc_fence_after();
+                tc::tmem_st32(lanes + M::p_col + (w * PB + ns % PB) * 32u, *reinterpret_cast<uint32_t (*)[32]>(x));
+                const uint64_t s1 = add2(s2[0], s2[1]);
+                sum += low(s1) + high(s1);
                 if (!whole) {
                     // rows of V that do not count and that the product would read (both tiles' groups write the same zeros)
-                    const int cols = left >= BK ? BK : (left + 15) & ~15;
+                    const int cols = states - j * BK >= BK ? BK : (states - j * BK + 15) & ~15;
                     const uint32_t out0 = ~bits[0] & low_bits(cols), out1 = ~bits[1] & low_bits(cols - 32);
                     if (out0 | out1) {
-                        const uint32_t v = 2u * (first + j) + 1u, slot = v % NS;
-                        ok = tc::wait_uniform(&kv_full[slot], v / NS & 1u, abort_flag);
+                        ok = cross_tc::wait(&kv_full[slot0 + 1], slot_ph, abort_flag);
                         if (!ok) break;
-                        uint8_t* vt = ring + slot * M::kv;
+                        uint8_t* vt = ring + (slot0 + 1) * M::kv;
 #pragma unroll 1
                         for (uint32_t o = out0, k0 = 0;; o = out1, k0 = 32) {
                             for (; o; o &= o - 1u) {
@@ -284,219 +283,256 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                         tc::fence_proxy_async();
                     }
                 }
+                slot0 += 2;
+                if (slot0 == NS) { slot0 = 0; slot_ph ^= 1u; }
                 tc::tmem_wait_st();
                 tc::tc_fence_before();
-                // at most one product of the tile is under way, so that the parity tells which one was the last
-                if (j > 0) ok = tc::wait_uniform(&pv_done[w], (ns - 1u) & 1u, abort_flag);
-                if (!ok) break;
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&p_full[bar]);
+                if (lane == 0) tc::mbar_arrive(&p_full[pbuf]);
             }
             if (!ok) break;
-            const int t = it.t0 + w * a.tt + row_t;
-            if (row_t < a.tt && t < a.n_q) {
-                const long long row = ((long long)it.s * a.heads + it.kh * a.group + row_h) * a.n_q + t;
-                const float lse = top == -INFINITY ? -INFINITY : top * a.scale + logf(sum);
-                if (a.parts > 1) a.part_lse[it.part * a.rows + row] = lse;
-                else if (a.lse) a.lse[row] = lse;
-            }
-            if (it.nb > 0) {
-                ok = tc::wait_uniform(&inv_free[w], inv_ph, abort_flag);
-                inv_ph ^= 1u;
-                if (!ok) break;
-                invs[w * BQ + r] = sum == 0.f ? 0.f : 1.f / sum;
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&inv_full[w]);
-            }
+            ok = cross_tc::wait(&o_free[w], free_ph, abort_flag);        // the last item's results are out: so are its sums
+            free_ph ^= 1u;
+            if (!ok) break;
+            sums[w * BQ + r] = make_float2(top, sum);
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sums_full[w]);
         }
         if (!ok && lane == 0) fail();
+        __syncwarp();
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        // ------------------------------------------------------------------ results, tile after tile, while the softmax is at the next item
+        const int q = warp & 3, r = q * 32 + lane;
+        const int row_t = r / a.group, row_h = r - row_t * a.group;
+        uint8_t* mine = staging + (uint32_t)q * M::stages * kStage;
+        uint32_t staged = 0, ph = 0;                 // ph: bit w, parity of tile w's barriers
+        bool ok = true;
+        for (uint32_t n = 0; ok; ++n) {
+            ok = see(n);
+            if (!ok) break;
+            const Item it = queue[n % kQueue];
+            leave(n);
+            if (it.s < 0) break;
+            for (int w = 0; w < it.tiles; ++w) {
+                const uint32_t to = tmem + M::o_col + w * M::o_width + ((uint32_t)(q * 32) << 16);
+                ok = cross_tc::wait(&sums_full[w], ph >> w & 1u, abort_flag);
+                if (!ok) break;
+                const float2 ts = sums[w * BQ + r];
+                const float top = ts.x, sum = ts.y, inv = sum == 0.f ? 0.f : 1.f / sum;
+                const int t = it.t0 + w * a.tt + row_t, h = it.kh * a.group + row_h;
+                const bool row_ok = row_t < a.tt && t < a.n_q;
+                const long long row = ((long long)it.s * a.heads + h) * a.n_q + t;
+                if (row_ok && (a.parts > 1 || a.lse)) {
+                    const float lse = top == -INFINITY ? -INFINITY : top * a.scale + logf(sum);
+                    if (a.parts > 1) a.part_lse[it.part * a.rows + row] = lse;
+                    else a.lse[row] = lse;
+                }
+                ok = cross_tc::wait(&o_full[w], ph >> w & 1u, abort_flag);
+                if (!ok) break;
+                ph ^= 1u << w;
+                tc::tc_fence_after();
+                if (a.parts == 1 && a.boxed) {
+#pragma unroll 1
+                    for (int ch = 0; ch < NCH; ++ch, ++staged) {
+                        uint8_t* stage = mine + staged % M::stages * kStage;
+                        if (lane == 0) tc::bulk_wait_read<(int)M::stages - 1>();      // the copy that last used this buffer has read it
+                        __syncwarp();
+#pragma unroll 1
+                        for (int half = 0; half < 2 && 4 * ch + 2 * half < ks; ++half) {
+                            uint32_t o[32];
+                            tc::tmem_ld32(to + 64 * ch + 32 * half, o);
+                            tc::tmem_wait_ld();
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t pk[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    pk[e] = pack2(__uint_as_float(o[8 * c + 2 * e]) * inv, __uint_as_float(o[8 * c + 2 * e + 1]) * inv);
+                                *reinterpret_cast<uint4*>(stage + lane * 128 + (((4 * half + c) ^ (lane & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                            }
+                        }
+                        if (ch == NCH - 1) {
+                            tc::tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) tc::mbar_arrive(&o_free[w]);
+                        }
+                        tc::fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            const int t_box = it.t0 + w * a.tt + q * 32 / a.group;
+                            if (t_box < a.n_q) store_4d(&mapO, tc::smem_u32(stage), 64 * ch, it.kh * a.group, t_box, it.s);
+                            tc::bulk_commit();
+                        }
+                    }
+                } else {
+                    float* part = a.part_out + (it.part * a.rows + row) * a.d;
+                    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(a.o.p)) + it.s * a.o.seq + t * a.o.tok + h * a.o.head;
+#pragma unroll 1
+                    for (int c = 0; c < ks; ++c) {
+                        uint32_t o[16];
+                        tc::tmem_ld16(to + 16 * c, o);
+                        tc::tmem_wait_ld();
+                        if (!row_ok) continue;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (16 * c + e < a.d) {
+                                const float v = __uint_as_float(o[e]) * inv;
+                                if (a.parts == 1) out[16 * c + e] = __float2bfloat16(v);
+                                else part[16 * c + e] = v;
+                            }
+                    }
+                    tc::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&o_free[w]);
+                }
+            }
+            if (!ok) break;
+        }
+        if (!ok && lane == 0) fail();
+        if (lane == 0) tc::bulk_wait<0>();           // every store complete before the CTA ends
         __syncwarp();
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (warp == 12) {
-            // ------------------------------------------------------------------ TMA producer
+            // ------------------------------------------------------------------ items, and TMA loads
             if (lane == 0) { tc::tma_prefetch_desc(&mapQ); tc::tma_prefetch_desc(&mapK); tc::tma_prefetch_desc(&mapV); }
             const uint32_t q_bytes = (uint32_t)(a.tt * a.group) * 128u * NCH;
-            uint32_t slot = 0, ph = 0, q_ph = 0;             // bit w of q_ph: parity of tile w's loads
+            uint32_t slot = 0, ph = 1, q_set[2] = {0, 0}, q_ph[2] = {1, 1};      // (parity of the first use's wait: passes at once)
             bool ok = true;
-            for (Steps st(a, blockIdx.x, gridDim.x); ok && st.live; st.next()) {
-                const Item& it = st.it;
-                if (st.j == 0)
-                    for (int w = 0; ok && w < it.tiles; ++w, __syncwarp()) {
-                        ok = tc::wait_uniform(&q_empty[w], (q_ph >> w & 1u) ^ 1u, abort_flag);
-                        q_ph ^= 1u << w;
+            uint32_t i = blockIdx.x;
+            auto next_item = [&]() {                     // the next that has a state
+                Item it = item_of(a, i);
+                while (it.s >= 0) {
+                    i = a.items - i > gridDim.x ? i + gridDim.x : a.items;
+                    if (it.nb > 0) break;
+                    it = item_of(a, i);
+                }
+                return it;
+            };
+            Item ahead = next_item();
+            for (uint32_t n = 0; ok; ++n) {
+                const Item it = ahead;
+                ok = cross_tc::wait(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
+                if (!ok) break;
+                if (lane == 0) {
+                    queue[n % kQueue] = it;
+                    tc::mbar_arrive(&item_full[n % kQueue]);
+                }
+                __syncwarp();
+                if (it.s < 0) break;
+                ahead = next_item();
+                for (int j = 0; ok && j < it.nb; ++j) {
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        if (j > 0 || w >= it.tiles || !ok) break;
+                        const uint32_t set = q_set[w], b = w * QB + set;
+                        ok = cross_tc::wait(&q_empty[b], q_ph[w], abort_flag);
+                        if (QB == 1 || set == 1) q_ph[w] ^= 1u;
+                        if (QB == 2) q_set[w] ^= 1u;
                         if (ok && tc::elect_one()) {
-                            tc::mbar_expect_tx(&q_full[w], q_bytes);
+                            tc::mbar_expect_tx(&q_full[b], q_bytes);
                             for (int ch = 0; ch < NCH; ++ch)
-                                load_4d(tc::smem_u32(sQ + w * M::q + ch * kChunk), &mapQ, &q_full[w], 64 * ch, it.kh * a.group * a.q_head_mul, it.t0 + w * a.tt, it.s * a.q_seq_mul);
+                                load_4d(tc::smem_u32(sQ + b * M::q + ch * kChunk), &mapQ, &q_full[b], 64 * ch, it.kh * a.group * a.q_head_mul, it.t0 + w * a.tt, it.s * a.q_seq_mul);
                         }
+                        __syncwarp();
                     }
-                for (int kv = 0; ok && kv < 2; ++kv, __syncwarp()) {
-                    ok = tc::wait_uniform(&kv_empty[slot], ph ^ 1u, abort_flag);
-                    if (ok && tc::elect_one()) {
-                        tc::mbar_expect_tx(&kv_full[slot], M::kv);
-                        for (int ch = 0; ch < NCH; ++ch)
-                            load_4d(tc::smem_u32(ring + slot * M::kv + ch * kKvChunk), kv ? &mapV : &mapK, &kv_full[slot], 64 * ch,
-                                    it.kh * (kv ? a.v_head_mul : a.kv_head_mul), it.sp.row0 + (it.b0 + st.j) * BK, it.sp.enc * (kv ? a.v_seq_mul : a.kv_seq_mul));
+                    for (int kv = 0; ok && kv < 2; ++kv) {
+                        ok = cross_tc::wait(&kv_empty[slot], ph, abort_flag);
+                        if (ok && tc::elect_one()) {
+                            tc::mbar_expect_tx(&kv_full[slot], M::kv);
+                            for (int ch = 0; ch < NCH; ++ch)
+                                load_4d(tc::smem_u32(ring + slot * M::kv + ch * kKvChunk), kv ? &mapV : &mapK, &kv_full[slot], 64 * ch,
+                                        it.kh * (kv ? a.v_head_mul : a.kv_head_mul), it.row + j * BK, it.enc * (kv ? a.v_seq_mul : a.kv_seq_mul));
+                        }
+                        __syncwarp();
+                        if (++slot == NS) { slot = 0; ph ^= 1u; }
                     }
-                    if (++slot == NS) { slot = 0; ph ^= 1u; }
                 }
             }
             if (!ok) {
                 if (lane == 0) fail();
-                const long long t0 = clock64();              // loads in flight must land before the shared memory is given back
+                const long long t0 = clock64();          // loads in flight must land before the shared memory is given back
                 while (clock64() - t0 < 400000ll) { }
             }
             __syncwarp();
-        } else if (warp == 13 || warp == 14) {
-            // ------------------------------------------------------------------ MMA issuers, one per tile: O += p V of a block, then the scores of the block after next
-            const int w = warp - 13;
+        } else if (warp >= 16) {
+            // ------------------------------------------------------------------ MMA issuers, one per tile for the scores and one for O += p V
+            const bool scores = warp < 18;
+            const int w = warp & 1;
             const uint32_t leader = tc::elect_one() ? 1u : 0u;
             const uint32_t idesc_o = tc::idesc_bf16(BQ, ks * 16) | kBMajorMN;
-            const uint64_t q_desc = tc::smem_desc(tc::smem_u32(sQ + w * M::q), 1024, 2), k_desc = tc::smem_desc(tc::smem_u32(ring), 1024, 2);
+            const uint64_t q_desc = tc::smem_desc(tc::smem_u32(sQ + w * QB * M::q), 1024, 2), k_desc = tc::smem_desc(tc::smem_u32(ring), 1024, 2);
             const uint64_t v_desc = desc_mn(tc::smem_u32(ring), kKvChunk);
-            const uint32_t d_s = tmem + w * 128u, d_o = tmem + 256u + w * 128u;
-            uint32_t q_ph = 0, o_ph = 1, s_buf = 0, p_buf = 0, p_ph = 0;
-            uint32_t k_slot = 0, k_ph = 0, v_slot = 1, v_ph = 0;
+            const uint32_t d_s = tmem + M::s_col + w * SB * 64u, d_o = tmem + M::o_col + w * M::o_width, a_p = tmem + M::p_col + w * PB * 32u;
+            uint32_t slot = scores ? 0 : 1, ph = 0;      // ring: K at even places, V at odd ones
+            uint32_t b = 0, b_ph = 0, set = 0, item_ph = 0;    // buffer of scores or p; set of Q; parities
             bool ok = true;
-            Steps sc(a, blockIdx.x, gridDim.x), pv = sc;
-            // a slot is free when both issuers are done with it: one that has no tile in this item is so as soon as it is full (not
-            // earlier, or it would count twice for one use of the slot)
-            auto scores = [&]() {
-                if (w < sc.it.tiles) {
-                    if (sc.j == 0) {
-                        ok = tc::wait_uniform(&q_full[w], q_ph, abort_flag);
-                        q_ph ^= 1u;
-                    }
-                    if (ok) ok = tc::wait_uniform(&kv_full[k_slot], k_ph, abort_flag);
-                    if (!ok) return;
-                    tc::tc_fence_after();
-                    const uint32_t idesc = tc::idesc_bf16(BQ, columns_of(sc.it, sc.j)), d = d_s + s_buf * 64u;
-                    const uint64_t kd = k_desc + k_slot * (M::kv >> 4);
-    #pragma unroll
-                    for (int k = 0; k < 4 * NCH; ++k)
-                        if (k < ks) tc::mma_bf16_if(leader, d, q_desc + ((k >> 2) * (kChunk >> 4) + (k & 3) * 2), kd + ((k >> 2) * (kKvChunk >> 4) + (k & 3) * 2), idesc, k != 0);
-                    tc::mma_commit_if(leader, &s_full[2 * w + s_buf]);
-                    s_buf ^= 1u;
-                    if (sc.last()) tc::mma_commit_if(leader, &q_empty[w]);
-                    tc::mma_commit_if(leader, &kv_empty[k_slot]);
-                } else {
-                    ok = tc::wait_uniform(&kv_full[k_slot], k_ph, abort_flag);
-                    if (!ok) return;
-                    if (leader) tc::mbar_arrive(&kv_empty[k_slot]);
-                }
-                sc.next();
-                k_slot += 2;
-                if (k_slot >= NS) { k_slot -= NS; k_ph ^= 1u; }
-            };
-            for (int i = 0; i < 2 && ok && sc.live; ++i) scores();
-            while (ok && pv.live) {
-                if (w < pv.it.tiles) {
-                    if (pv.j == 0) {
-                        ok = tc::wait_uniform(&o_free[w], o_ph, abort_flag);
-                        o_ph ^= 1u;
-                    }
-                    if (ok) ok = tc::wait_uniform(&kv_full[v_slot], v_ph, abort_flag);
-                    if (ok) ok = tc::wait_uniform(&p_full[2 * w + p_buf], p_ph >> p_buf & 1u, abort_flag);
-                    if (!ok) break;
-                    tc::tc_fence_after();
-                    const int steps = columns_of(pv.it, pv.j) / 16;
-                    const uint32_t p = d_s + p_buf * 64u;
-                    const uint64_t vd = v_desc + v_slot * (M::kv >> 4);
-                    p_ph ^= 1u << p_buf;
-                    p_buf ^= 1u;
-    #pragma unroll
-                    for (int k = 0; k < BK / 16; ++k)
-                        if (k < steps) mma_ts_if(leader, d_o, p + 8u * k, vd + k * (2048u >> 4), idesc_o, pv.j > 0 || k > 0);
-                    tc::mma_commit_if(leader, &pv_done[w]);
-                    if (pv.last()) tc::mma_commit_if(leader, &o_full[w]);
-                    tc::mma_commit_if(leader, &kv_empty[v_slot]);
-                } else {
-                    ok = tc::wait_uniform(&kv_full[v_slot], v_ph, abort_flag);
-                    if (!ok) break;
-                    if (leader) tc::mbar_arrive(&kv_empty[v_slot]);
-                }
-                if (sc.live) scores();
-                pv.next();
-                v_slot += 2;
-                if (v_slot >= NS) { v_slot -= NS; v_ph ^= 1u; }
-            }
-            if (!ok && lane == 0) fail();
-            __syncwarp();
-        } else if (warp < 12) {
-            // ------------------------------------------------------------------ results, tile after tile, while the softmax is at the next item
-            const int q = warp & 3, r = q * 32 + lane;
-            const int row_t = r / a.group, row_h = r - row_t * a.group;
-            const bool writer = q == 0 && lane == 0;         // the thread that issues the copies
-            uint32_t met = 0, staged = 0, ph = 0;            // ph: bit w, parity of tile w's barriers
-            bool ok = true;
-            auto meet = [&]() {                              // a bounded wait, as everywhere: a warp that gave up does not come
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(group);
-                ok = tc::wait_uniform(group, met++ & 1u, abort_flag);
-            };
-            for (uint32_t i = blockIdx.x; ok && i < a.items; i += gridDim.x) {
-                const Item it = item_of(a, i);
-                for (int w = 0; ok && w < it.tiles; ++w) {
-                    const uint32_t to = tmem + 256u + w * 128u + ((uint32_t)(q * 32) << 16);
-                    uint8_t* mine = staging + (staged & 1u) * M::q;
-                    if (a.parts == 1) {
-                        if (writer) tc::bulk_wait_read<1>(); // the copies that last used this staging tile have read it
-                        meet();
-                    }
-                    float inv = 0.f;
-                    if (ok && it.nb > 0) {
-                        ok = tc::wait_uniform(&inv_full[w], ph >> w & 1u, abort_flag);
-                        if (ok) ok = tc::wait_uniform(&o_full[w], ph >> w & 1u, abort_flag);
-                        ph ^= 1u << w;
+            for (uint32_t n = 0; ok; ++n) {
+                ok = see(n);
+                if (!ok) break;
+                const Item& it = queue[n % kQueue];
+                const int s = it.s, nb = it.nb, tiles = it.tiles, states = it.left;
+                leave(n);
+                if (s < 0) break;
+                const bool mine = w < tiles;
+                if (mine) ok = scores ? cross_tc::wait(&q_full[w * QB + set], item_ph, abort_flag) : cross_tc::wait(&o_free[w], item_ph ^ 1u, abort_flag);
+                for (int j = 0; ok && j < nb; ++j) {
+                    ok = cross_tc::wait(&kv_full[slot], ph, abort_flag);
+                    if (mine) {
+                        const int left = states - j * BK, cols = left >= BK ? BK : (left + 15) & ~15;
+                        if (ok) ok = scores ? cross_tc::wait(&s_free[2 * w + b], b_ph ^ 1u, abort_flag) : cross_tc::wait(&p_full[2 * w + b], b_ph, abort_flag);
+                        if (!ok) break;
                         tc::tc_fence_after();
-                        inv = invs[w * BQ + r];
-                    }
-                    if (!ok) break;
-                    const int t = it.t0 + w * a.tt + row_t;
-                    const bool row_ok = row_t < a.tt && t < a.n_q;
-                    float* dst = a.part_out + (it.part * a.rows + ((long long)it.s * a.heads + it.kh * a.group + row_h) * a.n_q + t) * a.d;
-    #pragma unroll 1
-                    for (int h = 0; 2 * h < ks; ++h) {       // 32 channels
-                        uint32_t o[32];
-                        tc::tmem_ld32(to + 32 * h, o);
-                        tc::tmem_wait_ld();
-                        if (a.parts > 1) {
-                            if (row_ok && it.nb > 0) {
-    #pragma unroll
-                                for (int e = 0; e < 32; ++e)
-                                    if (32 * h + e < a.d) dst[32 * h + e] = __uint_as_float(o[e]) * inv;
-                            }
+                        if (scores) {
+                            const uint32_t idesc = tc::idesc_bf16(BQ, cols), d = d_s + b * 64u;
+                            const uint64_t qd = q_desc + set * (M::q >> 4), kd = k_desc + slot * (M::kv >> 4);
+#pragma unroll
+                            for (int k = 0; k < 4 * NCH; ++k)
+                                if (k < ks) tc::mma_bf16_if(leader, d, qd + ((k >> 2) * (kChunk >> 4) + (k & 3) * 2), kd + ((k >> 2) * (kKvChunk >> 4) + (k & 3) * 2), idesc, k != 0);
+                            tc::mma_commit_if(leader, &s_full[2 * w + b]);
                         } else {
-    #pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                uint32_t pk[4];
-    #pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    pk[e] = it.nb > 0 ? pack2(__uint_as_float(o[8 * c + 2 * e]) * inv, __uint_as_float(o[8 * c + 2 * e + 1]) * inv) : 0u;
-                                *reinterpret_cast<uint4*>(mine + (h >> 1) * kChunk + r * 128 + (((4 * (h & 1) + c) ^ (r & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-                            }
+                            const uint32_t p = a_p + b * 32u;
+                            const uint64_t vd = v_desc + slot * (M::kv >> 4);
+#pragma unroll
+                            for (int k = 0; k < BK / 16; ++k)
+                                if (16 * k < cols) mma_ts_if(leader, d_o, p + 8u * k, vd + k * (2048u >> 4), idesc_o, j > 0 || k > 0);
+                            tc::mma_commit_if(leader, &pv_done[2 * w + b]);
                         }
+                        tc::mma_commit_if(leader, &kv_empty[slot]);
+                        if (++b == (scores ? SB : PB)) { b = 0; b_ph ^= 1u; }
+                    } else {
+                        // a slot is free when both tiles are done with it: one that the item does not have is so as soon as it is full
+                        // (not earlier, or it would count twice for one use of the slot)
+                        if (ok && leader) tc::mbar_arrive(&kv_empty[slot]);
                     }
-                    if (it.nb > 0) {
-                        tc::tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) { tc::mbar_arrive(&o_free[w]); tc::mbar_arrive(&inv_free[w]); }
-                    }
-                    if (a.parts == 1) {
-                        tc::fence_proxy_async();
-                        meet();
-                        if (ok && writer) {
-                            for (int ch = 0; ch < NCH; ++ch) store_4d(&mapO, tc::smem_u32(mine + ch * kChunk), 64 * ch, it.kh * a.group, it.t0 + w * a.tt, it.s);
-                            tc::bulk_commit();
-                        }
-                        ++staged;
-                    }
+                    slot += 2;
+                    if (slot >= NS) { slot -= NS; ph ^= 1u; }
+                }
+                if (ok && mine) {
+                    tc::mma_commit_if(leader, scores ? &q_empty[w * QB + set] : &o_full[w]);
+                    if (!scores || ++set == QB) { set = 0; item_ph ^= 1u; }
                 }
             }
             if (!ok && lane == 0) fail();
-            if (writer) tc::bulk_wait<0>();                  // every store complete before the CTA ends
             __syncwarp();
+        } else if (warp == 13) {
+            // ------------------------------------------------------------------ tokens without a state
+            for (uint32_t i = blockIdx.x; i < a.items; i = a.items - i > gridDim.x ? i + gridDim.x : a.items) {
+                const Item it = item_of(a, i);
+                if (it.nb > 0) continue;
+                const int last = it.t0 + it.tiles * a.tt < a.n_q ? it.t0 + it.tiles * a.tt : a.n_q;
+                for (int t = it.t0; t < last; ++t)
+                    for (int h = it.kh * a.group; h < (it.kh + 1) * a.group; ++h) {
+                        const long long row = ((long long)it.s * a.heads + h) * a.n_q + t;
+                        if (lane == 0) {
+                            if (a.parts > 1) a.part_lse[it.part * a.rows + row] = -INFINITY;
+                            else if (a.lse) a.lse[row] = -INFINITY;
+                        }
+                        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(a.o.p)) + it.s * a.o.seq + t * a.o.tok + h * a.o.head;
+                        for (int c = lane; a.parts == 1 && c < a.d; c += 32) out[c] = __float2bfloat16(0.f);
+                    }
+            }
         }
     }
     // ---------------------------------------------------------------------- teardown
@@ -542,10 +578,11 @@ template <typename E> __global__ void __launch_bounds__(256) cross_join_kernel(c
 
 int tokens_per_tile(const CrossArgs& a) { return BQ / a.group; }
 
-template <int NCH> int launch(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mo, const Args& a, cudaStream_t s) {
-    FREE_CUDA_TRY(cudaFuncSetAttribute(cross_tc_kernel<NCH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Mem<NCH>::bytes));
+template <int NCH, int QB, int SB, int PB> int launch(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mo, const Args& a, cudaStream_t s) {
+    constexpr uint32_t bytes = Mem<NCH, QB, SB, PB>::bytes;
+    FREE_CUDA_TRY(cudaFuncSetAttribute(cross_tc_kernel<NCH, QB, SB, PB>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
     const int grid = (int)(a.items < kSms ? a.items : kSms);
-    return free_launch(free_overlap_for_rows(a.rows / a.heads), cross_tc_kernel<NCH>, dim3(grid), dim3(kThreads), Mem<NCH>::bytes, s, mq, mk, mv, mo, a);
+    return free_launch(free_overlap_for_rows(a.rows / a.heads), cross_tc_kernel<NCH, QB, SB, PB>, dim3(grid), dim3(kThreads), bytes, s, mq, mk, mv, mo, a);
 }
 
 // Tiles per item and parts of the states.  Two tiles share the tiles of K and V that are loaded, but where that leaves SMs without an
@@ -601,8 +638,16 @@ int cross_tc_forward(const CrossArgs& c, const CrossParts& parts, cudaStream_t s
     FREE_TRY(map_heads(&mq, c.q, c.n_seq, c.n_q, c.heads, c.d, c.group, a.tt));
     FREE_TRY(map_heads(&mk, c.k, enc, rows, c.kv_heads, c.d, 1, BK));
     FREE_TRY(map_heads(&mv, c.v, enc, rows, c.kv_heads, c.d, 1, BK));
-    FREE_TRY(map_heads(&mo, c.o, c.n_seq, c.n_q, c.heads, c.d, c.group, a.tt));
-    FREE_TRY(c.d <= 64 ? launch<1>(mq, mk, mv, mo, a, s) : launch<2>(mq, mk, mv, mo, a, s));
+    // results leave by tile copies of 32 rows, where these are whole tokens
+    a.boxed = 32 % c.group == 0;
+    a.o = c.o;
+    FREE_TRY(map_heads(&mo, c.o, c.n_seq, c.n_q, c.heads, c.d, a.boxed ? c.group : 1, a.boxed ? 32 / c.group : 32));
+    const bool brief = c.where.n_kv <= kShort;
+    int code;
+    if (c.d <= 64) code = launch<1, 2, 2, 2>(mq, mk, mv, mo, a, s);
+    else if (c.d <= 96) code = brief ? launch<2, 2, 2, 1>(mq, mk, mv, mo, a, s) : launch<2, 1, 2, 1>(mq, mk, mv, mo, a, s);
+    else code = brief ? launch<2, 2, 1, 2>(mq, mk, mv, mo, a, s) : launch<2, 1, 1, 2>(mq, mk, mv, mo, a, s);
+    FREE_TRY(code);
     return parts.n > 1 ? cross_join(FREE_BF16, c, parts, s) : FREE_OK;
 }
 

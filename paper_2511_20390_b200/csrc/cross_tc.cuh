@@ -10,6 +10,23 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
+// Warp-uniform bounded wait as tc::wait_uniform, but the hardware is told that it may suspend the warp for long (HINT ns): many warps
+// wait here at once, and those that ask again and again take the issue slots of the ones that work (measured: two thirds of all
+// instructions were polls).
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
+    constexpr uint32_t HINT = 1000000u;
+    bool r = tc::mbar_try_wait(bar, parity);
+    if (!r) {
+        const long long t0 = clock64();
+        do {
+            uint32_t done;
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                         : "=r"(done) : "r"(tc::smem_u32(bar)), "r"(parity), "r"(HINT) : "memory");
+            r = done != 0;
+        } while (!r && !*abort_flag && clock64() - t0 < 4000000000ll);
+    }
+    return __all_sync(0xffffffffu, r);
+}
 __device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c, int head, int tok, int seq) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                  ::"r"(dst), "l"((uint64_t)map), "r"(tc::smem_u32(bar)), "r"(c), "r"(head), "r"(tok), "r"(seq) : "memory");
