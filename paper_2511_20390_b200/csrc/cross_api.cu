@@ -1,5 +1,5 @@
 // Attention to an encoder's states: argument checks, choice of kernel and entry points.
-#include "cross.h"
+#include "cross_tc.cuh"
 
 namespace {
 
@@ -79,6 +79,10 @@ CrossParts parts_of(const CrossArgs& a, int dtype) {
 }
 size_t part_bytes(const free_cross_attn* c, int parts) { return parts > 1 ? free_round_up(row_count(c) * parts * 4, 256) + row_count(c) * parts * c->d_head * 4 : 0; }
 
+// parts of dk and dv
+size_t sum_bytes(const free_cross_attn* c, int parts) {
+    return parts > 1 ? (size_t)parts * 2 * (c->kv_offsets ? 1 : c->n_enc) * (c->kv_offsets ? c->kv_rows : c->n_kv) * c->kv_heads * c->d_head * 4 : 0;
+}
 size_t stat_bytes(const free_cross_attn* c) { return free_round_up((size_t)c->n_seq * c->heads * c->n_q * 4, 256); }
 
 }  // namespace
@@ -120,7 +124,9 @@ extern "C" int free_op_cross_attention(const free_cross_attn* c, void* out, int6
 extern "C" size_t free_op_cross_attention_bwd_workspace_bytes(const free_cross_attn* c) {
     bool empty;
     if (check(c, &empty) != FREE_OK || empty) return 0;
-    return stat_bytes(c);
+    CrossArgs a = args_of(c);
+    a.g = a.q;
+    return stat_bytes(c) + (c->dtype == FREE_BF16 && cross_bwd_tc_supported(a) ? sum_bytes(c, cross_bwd_tc_parts(a)) : 0);
 }
 
 extern "C" int free_op_cross_attention_bwd(const free_cross_attn* c, const void* out, int64_t o_seq, int64_t o_tok, int64_t o_head, const float* lse,
@@ -158,7 +164,14 @@ extern "C" int free_op_cross_attention_bwd(const free_cross_attn* c, const void*
     a.dv = CrossMat{dv, c->kv_offsets ? 0 : dv_seq, dv_tok, dv_head};
     a.lse = const_cast<float*>(lse); a.delta = (float*)ws; a.err = device_error;
     if (!empty && (dq || dk)) FREE_TRY(cross_delta(c->dtype, a, s));
-    if (!empty && dq) FREE_TRY(cross_simt_dq(c->dtype, a, s));
-    if (dk && states(c)) FREE_TRY(cross_simt_dkv(c->dtype, a, s));
+    // the tensor cores where the tile copies take every matrix (an empty call only writes zeros)
+    const bool tc = c->dtype == FREE_BF16 && !empty && cross_bwd_tc_supported(a);
+    if (!empty && dq) FREE_TRY(tc && cross_tc::mappable(a.dq, c->n_seq, c->n_q, c->heads) ? cross_bwd_tc_dq(a, s) : cross_simt_dq(c->dtype, a, s));
+    if (dk && states(c)) {
+        if (tc && cross_tc::mappable(a.dk, enc, rows, c->kv_heads) && cross_tc::mappable(a.dv, enc, rows, c->kv_heads))
+            FREE_TRY(cross_bwd_tc_dkv(a, cross_bwd_tc_parts(a), (float*)((char*)ws + stat_bytes(c)), s));
+        else
+            FREE_TRY(cross_simt_dkv(c->dtype, a, s));
+    }
     return FREE_OK;
 }

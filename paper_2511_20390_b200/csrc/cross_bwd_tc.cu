@@ -1,0 +1,670 @@
+// Gradients of the attention to an encoder's states on the tensor cores (bf16 operands, fp32 accumulation).
+//
+//   p = 2^(c S - lse log2 e), S = q k^T;   dP = g v^T (g: the gradient of out);   dS = p (dP - delta) scale, delta = <g, out>
+//   dq = dS k                 rows are 128 tokens of one head, columns the states
+//   dk = dS^T q, dv = p^T g   rows are 128 states of one key head, columns the tokens of every head and sequence that reads them
+//
+// Both are one kernel: two 128 x 64 products S and dP from the rows' two operands (resident) and a column tile's two (a ring), the
+// elementwise part in registers, and p and dS, rounded to bf16, back to tensor memory as left operands of the products that
+// accumulate.  Transposing the problem for dk and dv (rows are states) leaves every operand as it lies in memory: a column tile serves
+// as K-major operand of S or dP and, read along its rows, as operand of the accumulation.
+// Persistent CTAs, one per SM: two warpgroups for the elementwise part, a column tile each in turn; one that writes results; a warp that
+// finds items and loads tiles; one that brings the tokens' lse and delta (dk, dv); one each that issues S, dP and the accumulating
+// products, in order, so that sums have a fixed order.  Nothing is added atomically; S and dP are formed twice instead (once here, once
+// for the other direction).
+// States that do not count: p and dS are replaced by zeros, and (dq) their rows of K zeroed in shared memory, for 0 x NaN is NaN.
+#include "cross_tc.cuh"
+
+namespace {
+
+using namespace cross_tc;
+
+constexpr int BR = 128, BC = 64;
+constexpr int kThreads = 640, kSms = 148;     // warps 0 - 7 elementwise, 8 - 11 results, 12 loads, 13 statistics, 14 S and dP, 15 sums, 16 zeros
+constexpr int kMathRegs = 136, kOtherRegs = 64;
+static_assert(256 * kMathRegs + 384 * kOtherRegs <= kThreads * 96, "registers of the launch");
+constexpr uint32_t kChunk = BR * 128, kColChunk = BC * 128;
+constexpr uint32_t kQueue = 4, kStage = 32 * 128;
+
+// NCH: chunks of 64 channels; AB: sets of the rows' operands; N1, N2: ring slots of the columns' operands; NB: buffers of S and dP
+template <bool DKV, int NCH, int AB, int N1, int N2, int NB, int SG> struct Mem {
+    static constexpr uint32_t a = NCH * kChunk, b = NCH * kColChunk;
+    static constexpr uint32_t ctrl = 1024 + (DKV ? N1 * BC * 8 : 0);
+    static constexpr uint32_t ctrl_bytes = (ctrl + 1023) / 1024 * 1024;
+    static constexpr uint32_t bytes = 1024 + ctrl_bytes + AB * 2 * a + (N1 + N2) * b + 4 * SG * kStage;
+    static constexpr uint32_t acc_col = NB * 128, acc_width = (512 - acc_col) / (DKV ? 2 : 1);
+    static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
+    static_assert((2 * AB + 2 * N1 + 2 * N2 + 3 * NB + 2 + 2 * kQueue + 1) * 8 <= 512, "barriers");
+};
+
+struct Args {
+    CrossWhere where;
+    int n_seq, n_q, heads, kv_heads, d, group;
+    int q_seq_mul, q_head_mul, g_seq_mul, g_head_mul, k_seq_mul, k_head_mul, v_seq_mul, v_head_mul;     // 0 where one matrix serves all
+    int blocks, parts;                        // row blocks of a (sequence, head) or (encoder sequence, key head); parts of the columns
+    long long items;
+    float c, scale;
+    const float *lse, *delta;
+    CrossMat o1, o2;                          // results: dq, or dk and dv
+    float* part_out;                          // [part][2][encoder row][key head][d]
+    long long part_rows;
+    uint32_t* err;
+};
+
+struct alignas(16) Item {
+    int live, idx, head, row0;                // idx: sequence (dq) or encoder sequence (dk, dv); head: of the rows; row0: first row's token or state
+    int tiles, part, enc, row;                // column tiles; enc, row: where the first state lies
+    int left, first, limit, kv_head;          // states from `row` on; first column tile of the part; rows that are written
+};
+
+template <bool DKV> __device__ __forceinline__ int sequences_of(const Args& a, int e) {      // that read encoder sequence e; whole warp
+    if (!a.where.seq_of) return a.n_seq ? a.where.share : 0;
+    int n = 0;
+    for (int s0 = 0; s0 < a.n_seq; s0 += 32) {
+        const int s = s0 + (threadIdx.x & 31);
+        n += __popc(__ballot_sync(0xffffffffu, s < a.n_seq && __ldg(a.where.seq_of + s) == e));
+    }
+    return n;
+}
+
+template <bool DKV> __device__ __forceinline__ Item item_of(const Args& a, long long i) {     // whole warp
+    Item it;
+    it.live = i < a.items;
+    it.tiles = it.part = it.first = 0;
+    if (!it.live) return it;
+    if (DKV) {
+        it.part = (int)(i % a.parts); i /= a.parts;
+    }
+    const int blk = (int)(i % a.blocks); i /= a.blocks;
+    if (DKV) {
+        it.head = it.kv_head = (int)(i % a.kv_heads);
+        it.idx = (int)(i / a.kv_heads);
+        const CrossSpan sp = cross_span_of_enc(a.where, it.idx);
+        it.row0 = blk * BR;
+        it.enc = sp.enc; it.row = sp.row0 + it.row0; it.left = sp.len - it.row0;
+        it.limit = (a.where.offsets ? sp.len : a.where.n_kv) - it.row0;
+        if (it.left > 0) {
+            const long long all = (long long)sequences_of<DKV>(a, it.idx) * a.group * ((a.n_q + BC - 1) / BC);
+            it.first = (int)(all * it.part / a.parts);
+            it.tiles = (int)(all * (it.part + 1) / a.parts) - it.first;
+        }
+    } else {
+        it.head = (int)(i % a.heads); it.idx = (int)(i / a.heads);
+        it.kv_head = it.head / a.group;
+        const CrossSpan sp = cross_span(a.where, it.idx);
+        it.row0 = blk * BR;
+        it.enc = sp.enc; it.row = sp.row0; it.left = sp.len;
+        it.limit = a.n_q - it.row0;
+        it.tiles = (sp.len + BC - 1) / BC;
+    }
+    return it;
+}
+
+// dk, dv: the column tiles of an item, in order: (sequence, head of the group, 64 tokens)
+struct Columns {
+    int s, g, t, tiles_q;
+    __device__ __forceinline__ void seek(const Args& a, const Item& it) {
+        tiles_q = (a.n_q + BC - 1) / BC;
+        const int per = a.group * tiles_q, skip = it.first / per, rest = it.first % per;
+        g = rest / tiles_q; t = rest % tiles_q;
+        if (!a.where.seq_of) { s = it.idx * a.where.share + skip; return; }
+        s = -1;
+        for (int k = 0; k <= skip; ++k) next_sequence(a, it.idx);
+    }
+    __device__ __forceinline__ void next_sequence(const Args& a, int e) {
+        ++s;
+        if (a.where.seq_of)
+            while (s < a.n_seq && __ldg(a.where.seq_of + s) != e) ++s;
+    }
+    __device__ __forceinline__ void next(const Args& a, int e) {
+        if (++t < tiles_q) return;
+        t = 0;
+        if (++g < a.group) return;
+        g = 0;
+        next_sequence(a, e);
+    }
+};
+
+template <bool DKV, int NCH, int AB, int N1, int N2, int NB, int SG>
+__global__ void __launch_bounds__(kThreads, 1)
+cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constant__ CUtensorMap mapA2, const __grid_constant__ CUtensorMap mapB1,
+                 const __grid_constant__ CUtensorMap mapB2, const __grid_constant__ CUtensorMap mapO1, const __grid_constant__ CUtensorMap mapO2, const Args a) {
+    using M = Mem<DKV, NCH, AB, N1, N2, NB, SG>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t* a_full = reinterpret_cast<uint64_t*>(smem);
+    uint64_t* a_empty = a_full + AB;
+    uint64_t* b1_full = a_empty + AB;
+    uint64_t* b1_empty = b1_full + N1;
+    uint64_t* b2_full = b1_empty + N1;
+    uint64_t* b2_empty = b2_full + N2;
+    uint64_t* s_full = b2_empty + N2;         // S and dP of a buffer
+    uint64_t* p_full = s_full + NB;           // p and dS
+    uint64_t* s_free = p_full + NB;           // the accumulating products have read them
+    uint64_t* acc_full = s_free + NB;
+    uint64_t* acc_free = acc_full + 1;
+    uint64_t* item_full = acc_free + 1;
+    uint64_t* item_free = item_full + kQueue;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(item_free + kQueue);
+    volatile uint32_t* abort_flag = tmem_slot + 1;
+    Item* queue = reinterpret_cast<Item*>(smem + 512);
+    static_assert(512 + kQueue * sizeof(Item) <= 1024, "control block");
+    float* stats = reinterpret_cast<float*>(smem + 1024);     // dk, dv: [slot of B1][lse log2 e, delta][column]
+    uint8_t* sA = smem + M::ctrl_bytes;
+    uint8_t* ring1 = sA + AB * 2 * M::a;
+    uint8_t* ring2 = ring1 + N1 * M::b;
+    uint8_t* staging = ring2 + N2 * M::b;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < AB; ++i) { tc::mbar_init(&a_full[i], 1); tc::mbar_init(&a_empty[i], 1); }
+        for (int i = 0; i < N1; ++i) { tc::mbar_init(&b1_full[i], DKV ? 2 : 1); tc::mbar_init(&b1_empty[i], 1); }
+        for (int i = 0; i < N2; ++i) { tc::mbar_init(&b2_full[i], 1); tc::mbar_init(&b2_empty[i], 1); }
+        for (int i = 0; i < NB; ++i) { tc::mbar_init(&s_full[i], 1); tc::mbar_init(&p_full[i], 4); tc::mbar_init(&s_free[i], 1); }
+        tc::mbar_init(acc_full, 1); tc::mbar_init(acc_free, 4);
+        for (uint32_t i = 0; i < kQueue; ++i) { tc::mbar_init(&item_full[i], 1); tc::mbar_init(&item_free[i], DKV ? 15 : 14); }    // 8 + 4 + 2 (+ statistics)
+        *abort_flag = 0;
+        tc::fence_barrier_init();
+        tc::fence_proxy_async();
+    }
+    if (warp == 12) { tc::tmem_alloc(tmem_slot, 512); tc::tmem_relinquish(); }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    auto fail = [&]() { *abort_flag = 1; atomicOr(a.err, FREE_DEV_ERR_ATTN); };
+    free_grid_dep_wait();
+    free_grid_dep_launch();
+    const int ks = (a.d + 15) / 16;
+    auto see = [&](uint32_t n) { return cross_tc::wait(&item_full[n % kQueue], n / kQueue & 1u, abort_flag); };
+    auto leave = [&](uint32_t n) {
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&item_free[n % kQueue]);
+    };
+
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMathRegs));
+        // ------------------------------------------------------------------ elementwise: a warpgroup per column tile, a thread per row
+        const int w = warp >> 2, q = warp & 3, r = q * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
+        uint32_t tile = 0, buf = 0, buf_ph = 0, slot = 0, slot_ph = 0;       // column tiles of the CTA so far; buffer and ring slot of the next
+        bool ok = true;
+        for (uint32_t n = 0; ok; ++n) {
+            ok = see(n);
+            if (!ok) break;
+            const Item& item = queue[n % kQueue];
+            const int live = item.live, tiles = item.tiles, left = item.left, idx = item.idx, head = item.head, row0 = item.row0;
+            const uint8_t* mask = a.where.mask ? a.where.mask + (a.where.offsets ? 0 : (long long)item.enc * a.where.n_kv) + item.row : nullptr;
+            leave(n);
+            if (!live) break;
+            float row_l = 0.f, row_d = 0.f;
+            bool row_counts = true;
+            if (DKV) {
+                row_counts = r < left && (!mask || mask[r] != 0);
+            } else if (row0 + r < a.n_q) {
+                const long long i = ((long long)idx * a.heads + head) * a.n_q + row0 + r;
+                row_l = __ldg(a.lse + i) * 1.4426950408889634f;
+                row_d = __ldg(a.delta + i);
+            }
+            for (int j = 0; ok && j < tiles; ++j, ++tile) {
+                if ((tile & 1u) == (uint32_t)w) {
+                    uint32_t bits[2] = {0xffffffffu, 0xffffffffu};
+                    const bool whole = DKV || (left - j * BC >= BC && !mask);
+                    if (!whole) count_bits(bits, mask, j * BC, left, lane);
+                    ok = cross_tc::wait(&s_full[buf], buf_ph, abort_flag);
+                    if (DKV && ok) ok = cross_tc::wait(&b1_full[slot], slot_ph, abort_flag);       // the statistics, first hand
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    const uint32_t ts = lanes + buf * 128u, td = ts + 64u;
+                    const float4 *cl = reinterpret_cast<const float4*>(stats + slot * 2 * BC), *cd = cl + BC / 4;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t s[32], d[32], ps[16], ds[16];
+                        tc::tmem_ld32(ts + 32 * h, s);
+                        tc::tmem_ld32(td + 32 * h, d);
+                        tc::tmem_wait_ld();
+                        const uint32_t bit = h ? bits[1] : bits[0];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            float pv[4], dv[4];
+                            float4 l4, d4;
+                            if (DKV) { l4 = cl[8 * h + e / 4]; d4 = cd[8 * h + e / 4]; }
+                            else { l4 = make_float4(row_l, row_l, row_l, row_l); d4 = make_float4(row_d, row_d, row_d, row_d); }
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {
+                                const float l = u == 0 ? l4.x : u == 1 ? l4.y : u == 2 ? l4.z : l4.w, dl = u == 0 ? d4.x : u == 1 ? d4.y : u == 2 ? d4.z : d4.w;
+                                pv[u] = ex2(fmaf(__uint_as_float(s[e + u]), a.c, -l));
+                                dv[u] = pv[u] * a.scale * (__uint_as_float(d[e + u]) - dl);
+                                if (DKV ? !row_counts : !whole && !(bit >> (e + u) & 1u)) pv[u] = dv[u] = 0.f;
+                            }
+                            if (DKV) { ps[e / 2] = pack2(pv[0], pv[1]); ps[e / 2 + 1] = pack2(pv[2], pv[3]); }
+                            ds[e / 2] = pack2(dv[0], dv[1]); ds[e / 2 + 1] = pack2(dv[2], dv[3]);
+                        }
+                        // over scores that have been read: column 16 h of 32 (h + 1)
+                        if (DKV) tc::tmem_st16(ts + 16 * h, ps);
+                        tc::tmem_st16(td + 16 * h, ds);
+                    }
+                    if (!whole) {
+                        const int cols = left - j * BC >= BC ? BC : (left - j * BC + 15) & ~15;
+                        const uint32_t out0 = ~bits[0] & low_bits(cols), out1 = ~bits[1] & low_bits(cols - 32);
+                        if (out0 | out1) {                         // K has landed: S is complete
+                            uint8_t* kt = ring1 + slot * M::b;
+#pragma unroll 1
+                            for (uint32_t o = out0, k0 = 0;; o = out1, k0 = 32) {
+                                for (; o; o &= o - 1u) {
+                                    const uint32_t k = k0 + (uint32_t)__ffs((int)o) - 1u;
+                                    if ((k & 3u) == (uint32_t)q && lane < 8 * NCH)
+                                        *reinterpret_cast<uint4*>(kt + (lane >> 3) * kColChunk + k * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                                }
+                                if (k0) break;
+                            }
+                            tc::fence_proxy_async();
+                        }
+                    }
+                    tc::tmem_wait_st();
+                    tc::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&p_full[buf]);
+                }
+                if (++buf == NB) { buf = 0; buf_ph ^= 1u; }
+                if (++slot == N1) { slot = 0; slot_ph ^= 1u; }
+            }
+        }
+        if (!ok && lane == 0) fail();
+        __syncwarp();
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        // ------------------------------------------------------------------ results
+        const int q = warp & 3, r = q * 32 + lane;
+        uint8_t* mine = staging + (uint32_t)q * SG * kStage;
+        uint32_t staged = 0, ph = 0;
+        bool ok = true;
+        for (uint32_t n = 0; ok; ++n) {
+            ok = see(n);
+            if (!ok) break;
+            const Item it = queue[n % kQueue];
+            leave(n);
+            if (!it.live) break;
+            const uint8_t* mask = a.where.mask ? a.where.mask + (a.where.offsets ? 0 : (long long)it.enc * a.where.n_kv) + it.row : nullptr;
+            const bool keep = !DKV || (r < it.left && (!mask || mask[r] != 0));    // states that do not count: zeros, whatever the sums are
+            const int seq = DKV ? it.enc : it.idx, tok0 = DKV ? it.row : it.row0;
+            ok = cross_tc::wait(acc_full, ph, abort_flag);
+            ph ^= 1u;
+            if (!ok) break;
+            tc::tc_fence_after();
+#pragma unroll 1
+            for (int o = 0; o < (DKV ? 2 : 1); ++o) {
+                const uint32_t acc = tmem + M::acc_col + o * M::acc_width + ((uint32_t)(q * 32) << 16);
+                const CrossMat& mat = o ? a.o2 : a.o1;
+                const bool last = o == (DKV ? 1 : 0);
+                const bool boxed = a.parts == 1 && 32 * (q + 1) <= it.limit;
+                __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(mat.p)) + seq * mat.seq + (long long)(tok0 + r) * mat.tok + it.head * mat.head;
+                float* part = a.part_out + (((long long)it.part * 2 + o) * a.part_rows + ((long long)seq * a.where.kv_rows + tok0 + r) * a.kv_heads + it.head) * a.d;
+#pragma unroll 1
+                for (int ch = 0; ch < NCH; ++ch) {
+                    uint8_t* stage = mine + staged % SG * kStage;
+                    if (boxed) {
+                        if (lane == 0) tc::bulk_wait_read<SG - 1>();     // the copy that last used this buffer has read it
+                        __syncwarp();
+                    }
+#pragma unroll 1
+                    for (int half = 0; half < 2 && 4 * ch + 2 * half < ks; ++half) {
+                        uint32_t v[32];
+                        tc::tmem_ld32(acc + 64 * ch + 32 * half, v);
+                        tc::tmem_wait_ld();
+                        if (boxed) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t pk[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) pk[e] = keep ? pack2(__uint_as_float(v[8 * c + 2 * e]), __uint_as_float(v[8 * c + 2 * e + 1])) : 0u;
+                                *reinterpret_cast<uint4*>(stage + lane * 128 + (((4 * half + c) ^ (lane & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                            }
+                        } else if (r < it.limit) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                const int c = 64 * ch + 32 * half + e;
+                                const float x = keep ? __uint_as_float(v[e]) : 0.f;
+                                if (c < a.d) {
+                                    if (a.parts > 1) part[c] = x;
+                                    else dst[c] = __float2bfloat16(x);
+                                }
+                            }
+                        }
+                    }
+                    if (last && ch == NCH - 1) {
+                        tc::tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive(acc_free);
+                    }
+                    if (boxed) {
+                        tc::fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            store_4d(o ? &mapO2 : &mapO1, tc::smem_u32(stage), 64 * ch, it.head, tok0 + 32 * q, seq);
+                            tc::bulk_commit();
+                        }
+                        ++staged;
+                    }
+                }
+            }
+        }
+        if (!ok && lane == 0) fail();
+        if (lane == 0) tc::bulk_wait<0>();               // every store complete before the CTA ends
+        __syncwarp();
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp == 12) {
+            // ------------------------------------------------------------------ items, and TMA loads
+            if (lane == 0) { tc::tma_prefetch_desc(&mapA1); tc::tma_prefetch_desc(&mapA2); tc::tma_prefetch_desc(&mapB1); tc::tma_prefetch_desc(&mapB2); }
+            uint32_t set = 0, a_ph = 1, s1 = 0, ph1 = 1, s2 = 0, ph2 = 1;
+            bool ok = true;
+            long long i = blockIdx.x;
+            auto next_item = [&]() {                     // the next that has a column tile
+                Item it = item_of<DKV>(a, i);
+                while (it.live) {
+                    i += gridDim.x;
+                    if (it.tiles > 0) break;
+                    it = item_of<DKV>(a, i);
+                }
+                return it;
+            };
+            Item ahead = next_item();
+            for (uint32_t n = 0; ok; ++n) {
+                const Item it = ahead;
+                ok = cross_tc::wait(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
+                if (!ok) break;
+                if (lane == 0) {
+                    queue[n % kQueue] = it;
+                    tc::mbar_arrive(&item_full[n % kQueue]);
+                }
+                __syncwarp();
+                if (!it.live) break;
+                ok = cross_tc::wait(&a_empty[set], a_ph, abort_flag);
+                if (!ok) break;
+                if (tc::elect_one()) {
+                    tc::mbar_expect_tx(&a_full[set], 2 * M::a);
+                    const int seq = DKV ? it.enc : it.idx, tok = DKV ? it.row : it.row0;
+                    for (int ch = 0; ch < NCH; ++ch) {
+                        load_4d(tc::smem_u32(sA + (2 * set) * M::a + ch * kChunk), &mapA1, &a_full[set], 64 * ch, it.head * (DKV ? a.k_head_mul : a.q_head_mul), tok,
+                                seq * (DKV ? a.k_seq_mul : a.q_seq_mul));
+                        load_4d(tc::smem_u32(sA + (2 * set + 1) * M::a + ch * kChunk), &mapA2, &a_full[set], 64 * ch, it.head * (DKV ? a.v_head_mul : a.g_head_mul), tok,
+                                seq * (DKV ? a.v_seq_mul : a.g_seq_mul));
+                    }
+                }
+                __syncwarp();
+                if (++set == AB) { set = 0; a_ph ^= 1u; }
+                ahead = next_item();
+                Columns col;
+                if (DKV) col.seek(a, it);
+                for (int j = 0; ok && j < it.tiles; ++j) {
+                    const int seq = DKV ? col.s : it.enc, head = DKV ? it.kv_head * a.group + col.g : it.kv_head, tok = DKV ? col.t * BC : it.row + j * BC;
+                    ok = cross_tc::wait(&b1_empty[s1], ph1, abort_flag);
+                    if (ok && tc::elect_one()) {
+                        tc::mbar_expect_tx(&b1_full[s1], M::b);
+                        for (int ch = 0; ch < NCH; ++ch)
+                            load_4d(tc::smem_u32(ring1 + s1 * M::b + ch * kColChunk), &mapB1, &b1_full[s1], 64 * ch, head * (DKV ? a.q_head_mul : a.k_head_mul), tok,
+                                    seq * (DKV ? a.q_seq_mul : a.k_seq_mul));
+                    }
+                    __syncwarp();
+                    if (ok) ok = cross_tc::wait(&b2_empty[s2], ph2, abort_flag);
+                    if (ok && tc::elect_one()) {
+                        tc::mbar_expect_tx(&b2_full[s2], M::b);
+                        for (int ch = 0; ch < NCH; ++ch)
+                            load_4d(tc::smem_u32(ring2 + s2 * M::b + ch * kColChunk), &mapB2, &b2_full[s2], 64 * ch, head * (DKV ? a.g_head_mul : a.v_head_mul), tok,
+                                    seq * (DKV ? a.g_seq_mul : a.v_seq_mul));
+                    }
+                    __syncwarp();
+                    if (++s1 == N1) { s1 = 0; ph1 ^= 1u; }
+                    if (++s2 == N2) { s2 = 0; ph2 ^= 1u; }
+                    if (DKV) col.next(a, it.idx);
+                }
+            }
+            if (!ok) {
+                if (lane == 0) fail();
+                const long long t0 = clock64();          // loads in flight must land before the shared memory is given back
+                while (clock64() - t0 < 400000ll) { }
+            }
+            __syncwarp();
+        } else if (warp == 13 && DKV) {
+            // ------------------------------------------------------------------ the tokens' lse (in log2) and delta, beside their tiles
+            uint32_t slot = 0, ph = 1;
+            bool ok = true;
+            for (uint32_t n = 0; ok; ++n) {
+                ok = see(n);
+                if (!ok) break;
+                const Item it = queue[n % kQueue];
+                leave(n);
+                if (!it.live) break;
+                Columns col;
+                col.seek(a, it);
+                for (int j = 0; ok && j < it.tiles; ++j) {
+                    float l[2], dl[2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int t = col.t * BC + lane + 32 * u;
+                        const long long i = ((long long)col.s * a.heads + it.kv_head * a.group + col.g) * a.n_q + t;
+                        const float v = t < a.n_q ? __ldg(a.lse + i) : -INFINITY;
+                        l[u] = v == -INFINITY ? INFINITY : v * 1.4426950408889634f;      // tokens without a state, or behind the last: p = 0
+                        dl[u] = t < a.n_q ? __ldg(a.delta + i) : 0.f;
+                    }
+                    ok = cross_tc::wait(&b1_empty[slot], ph, abort_flag);
+                    if (!ok) break;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        stats[slot * 2 * BC + lane + 32 * u] = l[u];
+                        stats[slot * 2 * BC + BC + lane + 32 * u] = dl[u];
+                    }
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&b1_full[slot]);
+                    if (++slot == N1) { slot = 0; ph ^= 1u; }
+                    col.next(a, it.idx);
+                }
+            }
+            if (!ok && lane == 0) fail();
+            __syncwarp();
+        } else if (warp == 14) {
+            // ------------------------------------------------------------------ S and dP
+            const uint32_t leader = tc::elect_one() ? 1u : 0u, idesc = tc::idesc_bf16(BR, BC);
+            const uint64_t a_desc = tc::smem_desc(tc::smem_u32(sA), 1024, 2), d1 = tc::smem_desc(tc::smem_u32(ring1), 1024, 2), d2 = tc::smem_desc(tc::smem_u32(ring2), 1024, 2);
+            uint32_t set = 0, a_ph = 0, s1 = 0, ph1 = 0, s2 = 0, ph2 = 0, buf = 0, buf_ph = 1;
+            bool ok = true;
+            for (uint32_t n = 0; ok; ++n) {
+                ok = see(n);
+                if (!ok) break;
+                const int live = queue[n % kQueue].live, tiles = queue[n % kQueue].tiles;
+                leave(n);
+                if (!live) break;
+                ok = cross_tc::wait(&a_full[set], a_ph, abort_flag);
+                for (int j = 0; ok && j < tiles; ++j) {
+                    ok = cross_tc::wait(&b1_full[s1], ph1, abort_flag);
+                    if (ok) ok = cross_tc::wait(&b2_full[s2], ph2, abort_flag);
+                    if (ok) ok = cross_tc::wait(&s_free[buf], buf_ph, abort_flag);
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    const uint64_t x1 = a_desc + (2 * set) * (M::a >> 4), x2 = x1 + (M::a >> 4), y1 = d1 + s1 * (M::b >> 4), y2 = d2 + s2 * (M::b >> 4);
+                    const uint32_t ts = tmem + buf * 128u;
+#pragma unroll
+                    for (int k = 0; k < 4 * NCH; ++k)
+                        if (k < ks) tc::mma_bf16_if(leader, ts, x1 + ((k >> 2) * (kChunk >> 4) + (k & 3) * 2), y1 + ((k >> 2) * (kColChunk >> 4) + (k & 3) * 2), idesc, k != 0);
+#pragma unroll
+                    for (int k = 0; k < 4 * NCH; ++k)
+                        if (k < ks) tc::mma_bf16_if(leader, ts + 64u, x2 + ((k >> 2) * (kChunk >> 4) + (k & 3) * 2), y2 + ((k >> 2) * (kColChunk >> 4) + (k & 3) * 2), idesc, k != 0);
+                    tc::mma_commit_if(leader, &s_full[buf]);
+                    if (!DKV) tc::mma_commit_if(leader, &b2_empty[s2]);
+                    if (++s1 == N1) { s1 = 0; ph1 ^= 1u; }
+                    if (++s2 == N2) { s2 = 0; ph2 ^= 1u; }
+                    if (++buf == NB) { buf = 0; buf_ph ^= 1u; }
+                }
+                if (ok) tc::mma_commit_if(leader, &a_empty[set]);
+                if (++set == AB) { set = 0; a_ph ^= 1u; }
+            }
+            if (!ok && lane == 0) fail();
+            __syncwarp();
+        } else if (warp == 15) {
+            // ------------------------------------------------------------------ the accumulating products
+            const uint32_t leader = tc::elect_one() ? 1u : 0u, idesc = tc::idesc_bf16(BR, ks * 16) | kBMajorMN;
+            const uint64_t d1 = desc_mn(tc::smem_u32(ring1), kColChunk), d2 = desc_mn(tc::smem_u32(ring2), kColChunk);
+            const uint32_t acc = tmem + M::acc_col;
+            uint32_t s1 = 0, s2 = 0, buf = 0, buf_ph = 0, acc_ph = 1;
+            bool ok = true;
+            for (uint32_t n = 0; ok; ++n) {
+                ok = see(n);
+                if (!ok) break;
+                const int live = queue[n % kQueue].live, tiles = queue[n % kQueue].tiles, left = queue[n % kQueue].left;
+                leave(n);
+                if (!live) break;
+                ok = cross_tc::wait(acc_free, acc_ph, abort_flag);
+                acc_ph ^= 1u;
+                for (int j = 0; ok && j < tiles; ++j) {
+                    ok = cross_tc::wait(&p_full[buf], buf_ph, abort_flag);
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    const int cols = DKV || left - j * BC >= BC ? BC : (left - j * BC + 15) & ~15;
+                    const uint32_t ps = tmem + buf * 128u, ds = ps + 64u;
+                    const uint64_t y1 = d1 + s1 * (M::b >> 4), y2 = d2 + s2 * (M::b >> 4);
+#pragma unroll
+                    for (int k = 0; k < BC / 16; ++k)
+                        if (16 * k < cols) mma_ts_if(leader, acc, ds + 8u * k, y1 + k * (2048u >> 4), idesc, j > 0 || k > 0);
+                    if (DKV) {
+#pragma unroll
+                        for (int k = 0; k < BC / 16; ++k)
+                            mma_ts_if(leader, acc + M::acc_width, ps + 8u * k, y2 + k * (2048u >> 4), idesc, j > 0 || k > 0);
+                    }
+                    tc::mma_commit_if(leader, &s_free[buf]);
+                    tc::mma_commit_if(leader, &b1_empty[s1]);
+                    if (DKV) tc::mma_commit_if(leader, &b2_empty[s2]);
+                    if (++s1 == N1) s1 = 0;
+                    if (++s2 == N2) s2 = 0;
+                    if (++buf == NB) { buf = 0; buf_ph ^= 1u; }
+                }
+                if (ok) tc::mma_commit_if(leader, acc_full);
+            }
+            if (!ok && lane == 0) fail();
+            __syncwarp();
+        } else if (warp == 16) {
+            // ------------------------------------------------------------------ rows that nothing reaches
+            for (long long i = blockIdx.x; i < a.items; i += gridDim.x) {
+                const Item it = item_of<DKV>(a, i);
+                if (it.tiles > 0) continue;
+                const int rows = it.limit < BR ? it.limit : BR, seq = DKV ? it.enc : it.idx, tok0 = DKV ? it.row : it.row0;
+                for (int r = 0; r < rows; ++r)
+                    for (int o = 0; o < (DKV ? 2 : 1); ++o) {
+                        const CrossMat& mat = o ? a.o2 : a.o1;
+                        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(mat.p)) + seq * mat.seq + (long long)(tok0 + r) * mat.tok + it.head * mat.head;
+                        float* part = a.part_out + (((long long)it.part * 2 + o) * a.part_rows + ((long long)seq * a.where.kv_rows + tok0 + r) * a.kv_heads + it.head) * a.d;
+                        for (int c = lane; c < a.d; c += 32) {
+                            if (a.parts > 1) part[c] = 0.f;
+                            else dst[c] = __float2bfloat16(0.f);
+                        }
+                    }
+            }
+        }
+    }
+    // ---------------------------------------------------------------------- teardown
+    tc::tc_fence_before();
+    __syncthreads();
+    if (warp == 12) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, 512); }
+}
+
+// dk and dv from their parts: a warp per state and key head, parts in order
+__global__ void __launch_bounds__(256) cross_bwd_join_kernel(const Args a) {
+    free_grid_dep_wait();
+    free_grid_dep_launch();
+    const int lane = threadIdx.x & 31;
+    const long long all = (long long)a.where.n_enc * a.where.n_kv * a.kv_heads;
+    for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += (long long)gridDim.x * 8) {
+        const int h = (int)(i % a.kv_heads), j = (int)(i / a.kv_heads % a.where.n_kv), e = (int)(i / a.kv_heads / a.where.n_kv);
+        const CrossSpan sp = cross_span_of_enc(a.where, e);
+        if (a.where.offsets && j >= sp.len) continue;
+        const long long row = ((long long)sp.enc * a.where.kv_rows + sp.row0 + j) * a.kv_heads + h;
+        for (int o = 0; o < 2; ++o) {
+            const CrossMat& mat = o ? a.o2 : a.o1;
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(mat.p)) + sp.enc * mat.seq + (long long)(sp.row0 + j) * mat.tok + h * mat.head;
+            for (int c = lane; c < a.d; c += 32) {
+                float v = 0.f;
+                for (int p = 0; p < a.parts; ++p) v += a.part_out[(((long long)p * 2 + o) * a.part_rows + row) * a.d + c];
+                dst[c] = __float2bfloat16(v);
+            }
+        }
+    }
+}
+
+template <bool DKV, int NCH, int AB, int N1, int N2, int NB, int SG>
+int launch(const CUtensorMap (&m)[6], const Args& a, cudaStream_t s) {
+    auto kernel = cross_bwd_kernel<DKV, NCH, AB, N1, N2, NB, SG>;
+    constexpr uint32_t bytes = Mem<DKV, NCH, AB, N1, N2, NB, SG>::bytes;
+    FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    const int grid = (int)(a.items < kSms ? a.items : kSms);
+    return free_launch(free_overlap_for_rows((long long)a.n_seq * a.n_q), kernel, dim3(grid), dim3(kThreads), bytes, s, m[0], m[1], m[2], m[3], m[4], m[5], a);
+}
+
+Args args_of(const CrossArgs& c) {
+    Args a{};
+    a.where = c.where;
+    a.n_seq = c.n_seq; a.n_q = c.n_q; a.heads = c.heads; a.kv_heads = c.kv_heads; a.d = c.d; a.group = c.group;
+    a.q_seq_mul = c.q.seq > 0; a.q_head_mul = c.q.head > 0; a.g_seq_mul = c.g.seq > 0; a.g_head_mul = c.g.head > 0;
+    a.k_seq_mul = c.k.seq > 0; a.k_head_mul = c.k.head > 0; a.v_seq_mul = c.v.seq > 0; a.v_head_mul = c.v.head > 0;
+    a.scale = c.scale; a.c = c.scale * 1.4426950408889634f;
+    a.lse = c.lse; a.delta = c.delta; a.err = c.err;
+    a.parts = 1;
+    return a;
+}
+
+}  // namespace
+
+bool cross_bwd_tc_supported(const CrossArgs& c) {
+    if (c.where.n_kv < 1 || c.n_seq < 1 || c.n_q < 1) return false;
+    const int enc = c.where.offsets ? 1 : c.where.n_enc, rows = c.where.kv_rows;
+    using cross_tc::mappable;
+    return mappable(c.q, c.n_seq, c.n_q, c.heads) && mappable(c.g, c.n_seq, c.n_q, c.heads) && mappable(c.k, enc, rows, c.kv_heads) && mappable(c.v, enc, rows, c.kv_heads);
+}
+
+// Parts of the tokens' tiles where the blocks of states leave SMs without one: two tiles at least, an fp32 row of dk and dv each.
+int cross_bwd_tc_parts(const CrossArgs& c) {
+    const long long items = (long long)c.where.n_enc * c.kv_heads * ((c.where.n_kv + BR - 1) / BR);
+    const long long tiles = (long long)c.n_seq * c.group * ((c.n_q + BC - 1) / BC) / (c.where.n_enc > 0 ? c.where.n_enc : 1);
+    if (items >= kSms) return 1;
+    long long p = (2 * kSms + items - 1) / items;
+    if (p > tiles / 2) p = tiles / 2;
+    return p < 1 ? 1 : (int)p;
+}
+
+int cross_bwd_tc_dq(const CrossArgs& c, cudaStream_t s) {
+    Args a = args_of(c);
+    const int enc = c.where.offsets ? 1 : c.where.n_enc, rows = c.where.kv_rows;
+    a.blocks = (c.n_q + BR - 1) / BR;
+    a.items = (long long)c.n_seq * c.heads * a.blocks;
+    a.o1 = a.o2 = c.dq;
+    CUtensorMap m[6];
+    using cross_tc::map_heads;
+    FREE_TRY(map_heads(&m[0], c.q, c.n_seq, c.n_q, c.heads, c.d, 1, BR));
+    FREE_TRY(map_heads(&m[1], c.g, c.n_seq, c.n_q, c.heads, c.d, 1, BR));
+    FREE_TRY(map_heads(&m[2], c.k, enc, rows, c.kv_heads, c.d, 1, BC));
+    FREE_TRY(map_heads(&m[3], c.v, enc, rows, c.kv_heads, c.d, 1, BC));
+    FREE_TRY(map_heads(&m[4], c.dq, c.n_seq, c.n_q, c.heads, c.d, 1, 32));
+    m[5] = m[4];
+    return c.d <= 64 ? launch<false, 1, 2, 6, 4, 3, 2>(m, a, s) : launch<false, 2, 2, 3, 2, 3, 1>(m, a, s);
+}
+
+int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_t s) {
+    Args a = args_of(c);
+    const int enc = c.where.offsets ? 1 : c.where.n_enc, rows = c.where.kv_rows;
+    a.blocks = (c.where.n_kv + BR - 1) / BR;
+    a.parts = parts; a.part_out = part_out; a.part_rows = (long long)enc * rows * c.kv_heads;
+    a.items = (long long)c.where.n_enc * c.kv_heads * a.blocks * parts;
+    a.o1 = c.dk; a.o2 = c.dv;
+    CUtensorMap m[6];
+    using cross_tc::map_heads;
+    FREE_TRY(map_heads(&m[0], c.k, enc, rows, c.kv_heads, c.d, 1, BR));
+    FREE_TRY(map_heads(&m[1], c.v, enc, rows, c.kv_heads, c.d, 1, BR));
+    FREE_TRY(map_heads(&m[2], c.q, c.n_seq, c.n_q, c.heads, c.d, 1, BC));
+    FREE_TRY(map_heads(&m[3], c.g, c.n_seq, c.n_q, c.heads, c.d, 1, BC));
+    FREE_TRY(map_heads(&m[4], c.dk, enc, rows, c.kv_heads, c.d, 1, 32));
+    FREE_TRY(map_heads(&m[5], c.dv, enc, rows, c.kv_heads, c.d, 1, 32));
+    const int code = c.d <= 64 ? launch<true, 1, 2, 6, 6, 3, 2>(m, a, s) : launch<true, 2, 1, 4, 4, 2, 1>(m, a, s);
+    FREE_TRY(code);
+    if (parts == 1) return FREE_OK;
+    const long long n = (long long)c.where.n_enc * c.where.n_kv * c.kv_heads, ctas = (n + 7) / 8;
+    return free_launch(false, cross_bwd_join_kernel, dim3((unsigned)(ctas < kSms * 8 ? ctas : kSms * 8)), dim3(256), 0, s, a);
+}

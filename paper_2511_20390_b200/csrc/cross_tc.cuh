@@ -35,11 +35,12 @@ __device__ __forceinline__ void store_4d(const CUtensorMap* map, uint32_t src, i
     asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
                  ::"l"((uint64_t)map), "r"(src), "r"(c), "r"(head), "r"(tok), "r"(seq) : "memory");
 }
-// D[tmem] (+)= A[tmem] * B[smem], one step of 16: lane m of A is row m, its 32-bit column c holds elements 2 c and 2 c + 1
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+// D[tmem] (+)= A[tmem] * B[smem], one step of 16, issued by the leader of a converged warp: lane m of A is row m, its 32-bit column c holds
+// elements 2 c and 2 c + 1
+__device__ __forceinline__ void mma_ts_if(uint32_t issue, uint32_t d, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate), "r"(issue) : "memory");
 }
 // Operand whose contraction runs along the rows of memory: blocks of 64 columns (128 bytes, swizzled) `block` bytes apart, groups of
 // 8 rows 1024 bytes apart.
