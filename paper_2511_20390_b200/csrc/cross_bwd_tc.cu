@@ -149,7 +149,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
     volatile uint32_t* abort_flag = tmem_slot + 1;
     Item* queue = reinterpret_cast<Item*>(smem + 512);
     static_assert(512 + kQueue * sizeof(Item) <= 1024, "control block");
-    float* stats = reinterpret_cast<float*>(smem + 1024);     // dk, dv: [slot of B1][lse log2 e, delta][column]
+    float* stats = reinterpret_cast<float*>(smem + 1024);     // dk, dv: [slot of B1][-lse log2 e, -scale delta][column]
     uint8_t* sA = smem + M::ctrl_bytes;
     uint8_t* ring1 = sA + AB * 2 * M::a;
     uint8_t* ring2 = ring1 + N1 * M::b;
@@ -187,6 +187,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
         // ------------------------------------------------------------------ elementwise: a warpgroup per column tile, a thread per row
         const int w = warp >> 2, q = warp & 3, r = q * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
+        const uint64_t c2 = pair(a.c, a.c), sc2 = pair(a.scale, a.scale);
         uint32_t tile = 0, buf = 0, buf_ph = 0, slot = 0, slot_ph = 0;       // column tiles of the CTA so far; buffer and ring slot of the next
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
@@ -197,14 +198,12 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
             const uint8_t* mask = a.where.mask ? a.where.mask + (a.where.offsets ? 0 : (long long)item.enc * a.where.n_kv) + item.row : nullptr;
             leave(n);
             if (!live) break;
-            float row_l = 0.f, row_d = 0.f;
-            bool row_counts = true;
-            if (DKV) {
-                row_counts = r < left && (!mask || mask[r] != 0);
-            } else if (row0 + r < a.n_q) {
+            uint64_t row_l = 0ull, row_d = 0ull;         // -lse log2 e and -scale delta of the row, twice
+            if (!DKV && row0 + r < a.n_q) {
                 const long long i = ((long long)idx * a.heads + head) * a.n_q + row0 + r;
-                row_l = __ldg(a.lse + i) * 1.4426950408889634f;
-                row_d = __ldg(a.delta + i);
+                const float l = -1.4426950408889634f * __ldg(a.lse + i), dl = -a.scale * __ldg(a.delta + i);
+                row_l = pair(l, l);
+                row_d = pair(dl, dl);
             }
             for (int j = 0; ok && j < tiles; ++j, ++tile) {
                 if ((tile & 1u) == (uint32_t)w) {
@@ -216,7 +215,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                     if (!ok) break;
                     tc::tc_fence_after();
                     const uint32_t ts = lanes + buf * 128u, td = ts + 64u;
-                    const float4 *cl = reinterpret_cast<const float4*>(stats + slot * 2 * BC), *cd = cl + BC / 4;
+                    const ulonglong2 *cl = reinterpret_cast<const ulonglong2*>(stats + slot * 2 * BC), *cd = cl + BC / 4;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t s[32], d[32], ps[16], ds[16];
@@ -226,19 +225,27 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                         const uint32_t bit = h ? bits[1] : bits[0];
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {
-                            float pv[4], dv[4];
-                            float4 l4, d4;
-                            if (DKV) { l4 = cl[8 * h + e / 4]; d4 = cd[8 * h + e / 4]; }
-                            else { l4 = make_float4(row_l, row_l, row_l, row_l); d4 = make_float4(row_d, row_d, row_d, row_d); }
-#pragma unroll
-                            for (int u = 0; u < 4; ++u) {
-                                const float l = u == 0 ? l4.x : u == 1 ? l4.y : u == 2 ? l4.z : l4.w, dl = u == 0 ? d4.x : u == 1 ? d4.y : u == 2 ? d4.z : d4.w;
-                                pv[u] = ex2(fmaf(__uint_as_float(s[e + u]), a.c, -l));
-                                dv[u] = pv[u] * a.scale * (__uint_as_float(d[e + u]) - dl);
-                                if (DKV ? !row_counts : !whole && !(bit >> (e + u) & 1u)) pv[u] = dv[u] = 0.f;
+                            // pairs: p = 2^(c S - lse'), dS = p (scale dP - scale delta)
+                            uint64_t l2[2] = {row_l, row_l}, d2[2] = {row_d, row_d};
+                            if (DKV) {
+                                const ulonglong2 lv = cl[8 * h + e / 4], dv = cd[8 * h + e / 4];
+                                l2[0] = lv.x; l2[1] = lv.y; d2[0] = dv.x; d2[1] = dv.y;
                             }
-                            if (DKV) { ps[e / 2] = pack2(pv[0], pv[1]); ps[e / 2 + 1] = pack2(pv[2], pv[3]); }
-                            ds[e / 2] = pack2(dv[0], dv[1]); ds[e / 2 + 1] = pack2(dv[2], dv[3]);
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                const int k = e + 2 * u;
+                                const uint64_t y = fma2(pair(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, l2[u]);
+                                const uint64_t z = fma2(pair(__uint_as_float(d[k]), __uint_as_float(d[k + 1])), sc2, d2[u]);
+                                float p0 = ex2(low(y)), p1 = ex2(high(y));
+                                const uint64_t x = mul2(pair(p0, p1), z);
+                                float x0 = low(x), x1 = high(x);
+                                if (!whole) {                      // (dk, dv: rows that do not count are dropped at the end)
+                                    x0 = bit >> k & 1u ? x0 : 0.f;
+                                    x1 = bit >> (k + 1) & 1u ? x1 : 0.f;
+                                }
+                                if (DKV) ps[k / 2] = pack2(p0, p1);
+                                ds[k / 2] = pack2(x0, x1);
+                            }
                         }
                         // over scores that have been read: column 16 h of 32 (h + 1)
                         if (DKV) tc::tmem_st16(ts + 16 * h, ps);
@@ -288,7 +295,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
             const uint8_t* mask = a.where.mask ? a.where.mask + (a.where.offsets ? 0 : (long long)it.enc * a.where.n_kv) + it.row : nullptr;
             const bool keep = !DKV || (r < it.left && (!mask || mask[r] != 0));    // states that do not count: zeros, whatever the sums are
             const int seq = DKV ? it.enc : it.idx, tok0 = DKV ? it.row : it.row0;
-            ok = cross_tc::wait(acc_full, ph, abort_flag);
+            ok = cross_tc::wait<SLEEP1>(acc_full, ph, abort_flag);
             ph ^= 1u;
             if (!ok) break;
             tc::tc_fence_after();
@@ -372,7 +379,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
             Item ahead = next_item();
             for (uint32_t n = 0; ok; ++n) {
                 const Item it = ahead;
-                ok = cross_tc::wait(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
+                ok = cross_tc::wait<SLEEP1>(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
                 if (!ok) break;
                 if (lane == 0) {
                     queue[n % kQueue] = it;
@@ -380,7 +387,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                 }
                 __syncwarp();
                 if (!it.live) break;
-                ok = cross_tc::wait(&a_empty[set], a_ph, abort_flag);
+                ok = cross_tc::wait<SLEEP1>(&a_empty[set], a_ph, abort_flag);
                 if (!ok) break;
                 if (tc::elect_one()) {
                     tc::mbar_expect_tx(&a_full[set], 2 * M::a);
@@ -399,7 +406,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                 if (DKV) col.seek(a, it);
                 for (int j = 0; ok && j < it.tiles; ++j) {
                     const int seq = DKV ? col.s : it.enc, head = DKV ? it.kv_head * a.group + col.g : it.kv_head, tok = DKV ? col.t * BC : it.row + j * BC;
-                    ok = cross_tc::wait(&b1_empty[s1], ph1, abort_flag);
+                    ok = cross_tc::wait<SLEEP1>(&b1_empty[s1], ph1, abort_flag);
                     if (ok && tc::elect_one()) {
                         tc::mbar_expect_tx(&b1_full[s1], M::b);
                         for (int ch = 0; ch < NCH; ++ch)
@@ -407,7 +414,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                                     seq * (DKV ? a.q_seq_mul : a.k_seq_mul));
                     }
                     __syncwarp();
-                    if (ok) ok = cross_tc::wait(&b2_empty[s2], ph2, abort_flag);
+                    if (ok) ok = cross_tc::wait<SLEEP1>(&b2_empty[s2], ph2, abort_flag);
                     if (ok && tc::elect_one()) {
                         tc::mbar_expect_tx(&b2_full[s2], M::b);
                         for (int ch = 0; ch < NCH; ++ch)
@@ -445,10 +452,10 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                         const int t = col.t * BC + lane + 32 * u;
                         const long long i = ((long long)col.s * a.heads + it.kv_head * a.group + col.g) * a.n_q + t;
                         const float v = t < a.n_q ? __ldg(a.lse + i) : -INFINITY;
-                        l[u] = v == -INFINITY ? INFINITY : v * 1.4426950408889634f;      // tokens without a state, or behind the last: p = 0
-                        dl[u] = t < a.n_q ? __ldg(a.delta + i) : 0.f;
+                        l[u] = v == -INFINITY ? -INFINITY : -1.4426950408889634f * v;    // tokens without a state, or behind the last: p = 0
+                        dl[u] = t < a.n_q ? -a.scale * __ldg(a.delta + i) : 0.f;
                     }
-                    ok = cross_tc::wait(&b1_empty[slot], ph, abort_flag);
+                    ok = cross_tc::wait<SLEEP1>(&b1_empty[slot], ph, abort_flag);
                     if (!ok) break;
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {

@@ -172,19 +172,58 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
     store_rows<E, ND>(at_out<E>(a.o, s, 0, h), a.o.tok, q0, a.n_q, d, ty, tx, acc);
 }
 
-// delta = <dout, out> of every token and head: a warp per row
-template <typename E> __global__ void __launch_bounds__(256) cross_delta_kernel(const CrossArgs a) {
+// delta = <dout, out> of every token and head.  L lanes hold a row, V consecutive channels each (16 bytes, or 1 element where the rows
+// allow no more), R rows of a group of lanes are in flight: bound by HBM.  Rows are counted on, not divided out.
+template <typename E, int V> struct Chunk {
+    E v[V];
+    __device__ __forceinline__ void load(const E* p, bool ok) {
+        if constexpr (V == 1) {
+            v[0] = ok ? *p : E(0.f);
+        } else {
+            const uint4 u = ok ? __ldg(reinterpret_cast<const uint4*>(p)) : make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(v) = u;
+        }
+    }
+};
+template <typename E, int V, int L> __global__ void __launch_bounds__(256) cross_delta_kernel(const CrossArgs a) {
+    constexpr int R = V == 1 ? 1 : 4, P = V == 1 ? kCrossMaxD / L : 1;        // pieces of a lane
+    free_grid_dep_wait();
+    free_grid_dep_launch();
     const long long rows = (long long)a.n_seq * a.n_q * a.heads;
-    const int lane = threadIdx.x & 31;
-    for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * 8) {
-        const int h = (int)(i % a.heads);
-        const long long st = i / a.heads;
-        const int t = (int)(st % a.n_q), s = (int)(st / a.n_q);
-        const E *g = at<E>(a.g, s, t, h), *o = at<E>(a.o, s, t, h);
-        float v = 0.f;
-        for (int c = lane; c < a.d; c += 32) v = fmaf(to_f(g[c]), to_f(o[c]), v);
-        v = free_warp_sum(v);
-        if (lane == 0) a.delta[((long long)s * a.heads + h) * a.n_q + t] = v;
+    const int lane = threadIdx.x % L, groups = (int)(gridDim.x * (256 / L)), step_t = groups / a.heads, step_h = groups % a.heads;
+    long long i = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
+    int h = (int)(i % a.heads), t, s;
+    { const long long st = i / a.heads; t = (int)(st % a.n_q); s = (int)(st / a.n_q); }
+    // whole groups of lanes leave together, so the exchanges name the group's lanes only
+    const unsigned mates = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << ((threadIdx.x & 31) / L * L);
+    while (i < rows) {
+        Chunk<E, V> g[R][P], o[R][P];
+        long long out[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool ok = i < rows;
+            const E *pg = at<E>(a.g, s, t, h) + lane * V, *po = at<E>(a.o, s, t, h) + lane * V;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                g[r][p].load(pg + p * L * V, ok && lane * V + p * L * V < a.d);
+                o[r][p].load(po + p * L * V, ok && lane * V + p * L * V < a.d);
+            }
+            out[r] = ok ? ((long long)s * a.heads + h) * a.n_q + t : -1;
+            i += groups; h += step_h; t += step_t;
+            if (h >= a.heads) { h -= a.heads; ++t; }
+            while (t >= a.n_q) { t -= a.n_q; ++s; }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float v = 0.f;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int e = 0; e < V; ++e) v = fmaf(to_f(g[r][p].v[e]), to_f(o[r][p].v[e]), v);
+#pragma unroll
+            for (int k = L / 2; k > 0; k >>= 1) v += __shfl_xor_sync(mates, v, k);
+            if (lane == 0 && out[r] >= 0) a.delta[out[r]] = v;
+        }
     }
 }
 
@@ -320,13 +359,24 @@ int cross_simt_forward(int dtype, const CrossArgs& a, cudaStream_t s) {
     if (dtype == FREE_FP32) return a.d <= 64 ? launch(cross_simt_kernel<float, 1>, q_tiles(a), 3, 0, a, s) : launch(cross_simt_kernel<float, 2>, q_tiles(a), 3, 0, a, s);
     return a.d <= 64 ? launch(cross_simt_kernel<__nv_bfloat16, 1>, q_tiles(a), 3, 0, a, s) : launch(cross_simt_kernel<__nv_bfloat16, 2>, q_tiles(a), 3, 0, a, s);
 }
-int cross_delta(int dtype, const CrossArgs& a, cudaStream_t s) {
-    const long long rows = (long long)a.n_seq * a.n_q * a.heads, ctas = (rows + 7) / 8;
-    const unsigned grid = (unsigned)(ctas < 148 * 8 ? ctas : 148 * 8);
-    if (dtype == FREE_FP32) cross_delta_kernel<float><<<grid, 256, 0, s>>>(a);
-    else cross_delta_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(a);
-    return free_check_launch();
+namespace {
+
+template <typename E, int V, int L> int start_delta(const CrossArgs& a, cudaStream_t s) {
+    const long long rows = (long long)a.n_seq * a.n_q * a.heads, ctas = (rows + 256 / L - 1) / (256 / L);
+    return free_launch(free_overlap_for_rows((long long)a.n_seq * a.n_q), cross_delta_kernel<E, V, L>, dim3((unsigned)(ctas < 148 * 8 ? ctas : 148 * 8)), dim3(256), 0, s, a);
 }
+template <typename E> int delta_of(const CrossArgs& a, cudaStream_t s) {
+    constexpr int V = 16 / (int)sizeof(E);
+    bool wide = a.d % V == 0;
+    for (const CrossMat* m : {&a.g, &a.o}) wide = wide && free_aligned16(m->p) && m->seq % V == 0 && m->tok % V == 0 && m->head % V == 0;
+    if (!wide) return start_delta<E, 1, 32>(a, s);
+    const int units = a.d / V;
+    return units <= 8 ? start_delta<E, V, 8>(a, s) : units <= 16 ? start_delta<E, V, 16>(a, s) : start_delta<E, V, 32>(a, s);
+}
+
+}  // namespace
+
+int cross_delta(int dtype, const CrossArgs& a, cudaStream_t s) { return dtype == FREE_FP32 ? delta_of<float>(a, s) : delta_of<__nv_bfloat16>(a, s); }
 int cross_simt_dq(int dtype, const CrossArgs& a, cudaStream_t s) {
     if (dtype == FREE_FP32) return a.d <= 64 ? launch(cross_simt_dq_kernel<float, 1>, q_tiles(a), 4, 0, a, s) : launch(cross_simt_dq_kernel<float, 2>, q_tiles(a), 4, 0, a, s);
     return a.d <= 64 ? launch(cross_simt_dq_kernel<__nv_bfloat16, 1>, q_tiles(a), 4, 0, a, s) : launch(cross_simt_dq_kernel<__nv_bfloat16, 2>, q_tiles(a), 4, 0, a, s);

@@ -115,13 +115,6 @@ __device__ __forceinline__ Item item_of(const Args& a, uint32_t i) {
     return it;
 }
 
-// Two fp32 numbers side by side: one instruction for both.
-__device__ __forceinline__ uint64_t pair(float a, float b) { uint64_t v; asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); return v; }
-__device__ __forceinline__ float low(uint64_t v) { return __uint_as_float((uint32_t)v); }
-__device__ __forceinline__ float high(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
-
 template <int NCH, int QB, int SB, int PB>
 __global__ void __launch_bounds__(kThreads, 1)
 cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
@@ -309,7 +302,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             if (it.s < 0) break;
             for (int w = 0; w < it.tiles; ++w) {
                 const uint32_t to = tmem + M::o_col + w * M::o_width + ((uint32_t)(q * 32) << 16);
-                ok = cross_tc::wait(&sums_full[w], ph >> w & 1u, abort_flag);
+                ok = cross_tc::wait<SLEEP1>(&sums_full[w], ph >> w & 1u, abort_flag);
                 if (!ok) break;
                 const float2 ts = sums[w * BQ + r];
                 const float top = ts.x, sum = ts.y, inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -321,7 +314,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                     if (a.parts > 1) a.part_lse[it.part * a.rows + row] = lse;
                     else a.lse[row] = lse;
                 }
-                ok = cross_tc::wait(&o_full[w], ph >> w & 1u, abort_flag);
+                ok = cross_tc::wait<SLEEP1>(&o_full[w], ph >> w & 1u, abort_flag);
                 if (!ok) break;
                 ph ^= 1u << w;
                 tc::tc_fence_after();
@@ -406,7 +399,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             Item ahead = next_item();
             for (uint32_t n = 0; ok; ++n) {
                 const Item it = ahead;
-                ok = cross_tc::wait(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
+                ok = cross_tc::wait<SLEEP1>(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
                 if (!ok) break;
                 if (lane == 0) {
                     queue[n % kQueue] = it;
@@ -420,7 +413,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                     for (int w = 0; w < 2; ++w) {
                         if (j > 0 || w >= it.tiles || !ok) break;
                         const uint32_t set = q_set[w], b = w * QB + set;
-                        ok = cross_tc::wait(&q_empty[b], q_ph[w], abort_flag);
+                        ok = cross_tc::wait<SLEEP1>(&q_empty[b], q_ph[w], abort_flag);
                         if (QB == 1 || set == 1) q_ph[w] ^= 1u;
                         if (QB == 2) q_set[w] ^= 1u;
                         if (ok && tc::elect_one()) {
@@ -431,7 +424,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                         __syncwarp();
                     }
                     for (int kv = 0; ok && kv < 2; ++kv) {
-                        ok = cross_tc::wait(&kv_empty[slot], ph, abort_flag);
+                        ok = cross_tc::wait<SLEEP1>(&kv_empty[slot], ph, abort_flag);
                         if (ok && tc::elect_one()) {
                             tc::mbar_expect_tx(&kv_full[slot], M::kv);
                             for (int ch = 0; ch < NCH; ++ch)

@@ -3,6 +3,12 @@
 #include "cross.h"
 #include "tc_common.cuh"
 
+#ifndef SLEEP0
+#define SLEEP0 0
+#endif
+#ifndef SLEEP1
+#define SLEEP1 0
+#endif
 namespace cross_tc {
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
@@ -10,20 +16,21 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-// Warp-uniform bounded wait as tc::wait_uniform, but the hardware is told that it may suspend the warp for long (HINT ns): many warps
-// wait here at once, and those that ask again and again take the issue slots of the ones that work (measured: two thirds of all
-// instructions were polls).
+// Warp-uniform bounded wait as tc::wait_uniform, for kernels in which many warps wait at once: one that asks again and again takes issue
+// slots of those that work, so it sleeps in between, longer (NS) where nothing waits for this warp in turn.
+template <int NS = SLEEP0>
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
-    constexpr uint32_t HINT = 1000000u;
     bool r = tc::mbar_try_wait(bar, parity);
     if (!r) {
         const long long t0 = clock64();
-        do {
-            uint32_t done;
-            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
-                         : "=r"(done) : "r"(tc::smem_u32(bar)), "r"(parity), "r"(HINT) : "memory");
-            r = done != 0;
-        } while (!r && !*abort_flag && clock64() - t0 < 4000000000ll);
+        for (;;) {
+#pragma unroll 1
+            for (int i = 0; i < 16 && !r; ++i) {
+                if (NS) __nanosleep(NS);
+                r = tc::mbar_try_wait(bar, parity);
+            }
+            if (r || *abort_flag || clock64() - t0 > 4000000000ll) break;
+        }
     }
     return __all_sync(0xffffffffu, r);
 }
@@ -42,6 +49,14 @@ __device__ __forceinline__ void mma_ts_if(uint32_t issue, uint32_t d, uint32_t a
                  "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
                  ::"r"(d), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate), "r"(issue) : "memory");
 }
+// Two fp32 numbers side by side: one instruction for both.
+__device__ __forceinline__ uint64_t pair(float a, float b) { uint64_t v; asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); return v; }
+__device__ __forceinline__ float low(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float high(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+
 // Operand whose contraction runs along the rows of memory: blocks of 64 columns (128 bytes, swizzled) `block` bytes apart, groups of
 // 8 rows 1024 bytes apart.
 __device__ __forceinline__ uint64_t desc_mn(uint32_t saddr, uint32_t block) {
