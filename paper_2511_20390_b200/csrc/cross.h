@@ -55,13 +55,18 @@ struct CrossArgs {
 
 // Tensor cores, bf16
 bool cross_tc_supported(const CrossArgs& a);
-CrossParts cross_tc_parts(const CrossArgs& a);
+int cross_tc_parts(const CrossArgs& a);
 int cross_tc_forward(const CrossArgs& a, const CrossParts& parts, cudaStream_t s);
 bool cross_bwd_tc_supported(const CrossArgs& a);
 int cross_bwd_tc_parts(const CrossArgs& a);   // of the tokens, for dk and dv: fp32 [part][2][state rows][key heads][d] in the workspace where there are several
 int cross_bwd_tc_dq(const CrossArgs& a, cudaStream_t s);
 int cross_bwd_tc_dkv(const CrossArgs& a, int parts, float* part_out, cudaStream_t s);
 int cross_join(int dtype, const CrossArgs& a, const CrossParts& parts, cudaStream_t s);
+
+// Few tokens, fp32 or bf16
+bool cross_rows_supported(int dtype, const CrossArgs& a);
+int cross_rows_parts(const CrossArgs& a);
+int cross_rows_forward(int dtype, const CrossArgs& a, const CrossParts& parts, cudaStream_t s);
 
 // CUDA cores, fp32 or bf16, any strides and alignment
 int cross_simt_forward(int dtype, const CrossArgs& a, cudaStream_t s);

@@ -72,10 +72,13 @@ int result(const void* p, int e, long long seq, long long tok, long long head, i
 
 size_t row_count(const free_cross_attn* c) { return (size_t)c->n_seq * c->heads * c->n_q; }
 
-// parts of the states, and where they lie in the workspace
-CrossParts parts_of(const CrossArgs& a, int dtype) {
-    if (dtype == FREE_BF16 && cross_tc_supported(a)) return cross_tc_parts(a);
-    return CrossParts{1, nullptr, nullptr};
+// Which kernel, and parts of the states: few rows on their own, bf16 on the tensor cores, the rest on CUDA cores.
+enum Way { ROWS, TENSOR, SIMT };
+Way way_of(const CrossArgs& a, int dtype, int* parts) {
+    *parts = 1;
+    if (cross_rows_supported(dtype, a)) { *parts = cross_rows_parts(a); return ROWS; }
+    if (dtype == FREE_BF16 && cross_tc_supported(a)) { *parts = cross_tc_parts(a); return TENSOR; }
+    return SIMT;
 }
 size_t part_bytes(const free_cross_attn* c, int parts) { return parts > 1 ? free_round_up(row_count(c) * parts * 4, 256) + row_count(c) * parts * c->d_head * 4 : 0; }
 
@@ -93,7 +96,9 @@ extern "C" size_t free_op_cross_attention_workspace_bytes(const free_cross_attn*
     // where the inputs turn out to be no matter for the tensor cores, less is used
     CrossArgs a = args_of(c);
     a.o = a.q;
-    return part_bytes(c, parts_of(a, c->dtype).n);
+    int parts;
+    way_of(a, c->dtype, &parts);
+    return part_bytes(c, parts);
 }
 
 extern "C" int free_op_cross_attention(const free_cross_attn* c, void* out, int64_t o_seq, int64_t o_tok, int64_t o_head, float* lse, void* ws,
@@ -108,16 +113,16 @@ extern "C" int free_op_cross_attention(const free_cross_attn* c, void* out, int6
     CrossArgs a = args_of(c);
     a.o = CrossMat{out, o_seq, o_tok, o_head};
     a.lse = lse; a.err = device_error;
-    if (c->dtype == FREE_BF16 && cross_tc_supported(a)) {
-        CrossParts p = cross_tc_parts(a);
-        if (p.n > 1) {
-            if (!ws || ws_bytes < part_bytes(c, p.n)) return FREE_ERR_WORKSPACE;
-            if (!free_aligned16(ws)) return FREE_ERR_ALIGN;
-            p.lse = (float*)ws;
-            p.out = (float*)((char*)ws + free_round_up(row_count(c) * p.n * 4, 256));
-        }
-        return cross_tc_forward(a, p, (cudaStream_t)stream);
+    CrossParts p{1, nullptr, nullptr};
+    const Way way = way_of(a, c->dtype, &p.n);
+    if (p.n > 1) {
+        if (!ws || ws_bytes < part_bytes(c, p.n)) return FREE_ERR_WORKSPACE;
+        if (!free_aligned16(ws)) return FREE_ERR_ALIGN;
+        p.lse = (float*)ws;
+        p.out = (float*)((char*)ws + free_round_up(row_count(c) * p.n * 4, 256));
     }
+    if (way == ROWS) return cross_rows_forward(c->dtype, a, p, (cudaStream_t)stream);
+    if (way == TENSOR) return cross_tc_forward(a, p, (cudaStream_t)stream);
     return cross_simt_forward(c->dtype, a, (cudaStream_t)stream);
 }
 

@@ -295,7 +295,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
             const uint8_t* mask = a.where.mask ? a.where.mask + (a.where.offsets ? 0 : (long long)it.enc * a.where.n_kv) + it.row : nullptr;
             const bool keep = !DKV || (r < it.left && (!mask || mask[r] != 0));    // states that do not count: zeros, whatever the sums are
             const int seq = DKV ? it.enc : it.idx, tok0 = DKV ? it.row : it.row0;
-            ok = cross_tc::wait<SLEEP1>(acc_full, ph, abort_flag);
+            ok = cross_tc::wait(acc_full, ph, abort_flag);
             ph ^= 1u;
             if (!ok) break;
             tc::tc_fence_after();
@@ -379,7 +379,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
             Item ahead = next_item();
             for (uint32_t n = 0; ok; ++n) {
                 const Item it = ahead;
-                ok = cross_tc::wait<SLEEP1>(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
+                ok = cross_tc::wait(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
                 if (!ok) break;
                 if (lane == 0) {
                     queue[n % kQueue] = it;
@@ -387,7 +387,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                 }
                 __syncwarp();
                 if (!it.live) break;
-                ok = cross_tc::wait<SLEEP1>(&a_empty[set], a_ph, abort_flag);
+                ok = cross_tc::wait(&a_empty[set], a_ph, abort_flag);
                 if (!ok) break;
                 if (tc::elect_one()) {
                     tc::mbar_expect_tx(&a_full[set], 2 * M::a);
@@ -406,7 +406,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                 if (DKV) col.seek(a, it);
                 for (int j = 0; ok && j < it.tiles; ++j) {
                     const int seq = DKV ? col.s : it.enc, head = DKV ? it.kv_head * a.group + col.g : it.kv_head, tok = DKV ? col.t * BC : it.row + j * BC;
-                    ok = cross_tc::wait<SLEEP1>(&b1_empty[s1], ph1, abort_flag);
+                    ok = cross_tc::wait(&b1_empty[s1], ph1, abort_flag);
                     if (ok && tc::elect_one()) {
                         tc::mbar_expect_tx(&b1_full[s1], M::b);
                         for (int ch = 0; ch < NCH; ++ch)
@@ -414,7 +414,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                                     seq * (DKV ? a.q_seq_mul : a.k_seq_mul));
                     }
                     __syncwarp();
-                    if (ok) ok = cross_tc::wait<SLEEP1>(&b2_empty[s2], ph2, abort_flag);
+                    if (ok) ok = cross_tc::wait(&b2_empty[s2], ph2, abort_flag);
                     if (ok && tc::elect_one()) {
                         tc::mbar_expect_tx(&b2_full[s2], M::b);
                         for (int ch = 0; ch < NCH; ++ch)
@@ -455,7 +455,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                         l[u] = v == -INFINITY ? -INFINITY : -1.4426950408889634f * v;    // tokens without a state, or behind the last: p = 0
                         dl[u] = t < a.n_q ? -a.scale * __ldg(a.delta + i) : 0.f;
                     }
-                    ok = cross_tc::wait<SLEEP1>(&b1_empty[slot], ph, abort_flag);
+                    ok = cross_tc::wait(&b1_empty[slot], ph, abort_flag);
                     if (!ok) break;
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {

@@ -302,7 +302,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             if (it.s < 0) break;
             for (int w = 0; w < it.tiles; ++w) {
                 const uint32_t to = tmem + M::o_col + w * M::o_width + ((uint32_t)(q * 32) << 16);
-                ok = cross_tc::wait<SLEEP1>(&sums_full[w], ph >> w & 1u, abort_flag);
+                ok = cross_tc::wait(&sums_full[w], ph >> w & 1u, abort_flag);
                 if (!ok) break;
                 const float2 ts = sums[w * BQ + r];
                 const float top = ts.x, sum = ts.y, inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -314,7 +314,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                     if (a.parts > 1) a.part_lse[it.part * a.rows + row] = lse;
                     else a.lse[row] = lse;
                 }
-                ok = cross_tc::wait<SLEEP1>(&o_full[w], ph >> w & 1u, abort_flag);
+                ok = cross_tc::wait(&o_full[w], ph >> w & 1u, abort_flag);
                 if (!ok) break;
                 ph ^= 1u << w;
                 tc::tc_fence_after();
@@ -399,7 +399,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             Item ahead = next_item();
             for (uint32_t n = 0; ok; ++n) {
                 const Item it = ahead;
-                ok = cross_tc::wait<SLEEP1>(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
+                ok = cross_tc::wait(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
                 if (!ok) break;
                 if (lane == 0) {
                     queue[n % kQueue] = it;
@@ -413,7 +413,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                     for (int w = 0; w < 2; ++w) {
                         if (j > 0 || w >= it.tiles || !ok) break;
                         const uint32_t set = q_set[w], b = w * QB + set;
-                        ok = cross_tc::wait<SLEEP1>(&q_empty[b], q_ph[w], abort_flag);
+                        ok = cross_tc::wait(&q_empty[b], q_ph[w], abort_flag);
                         if (QB == 1 || set == 1) q_ph[w] ^= 1u;
                         if (QB == 2) q_set[w] ^= 1u;
                         if (ok && tc::elect_one()) {
@@ -424,7 +424,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                         __syncwarp();
                     }
                     for (int kv = 0; ok && kv < 2; ++kv) {
-                        ok = cross_tc::wait<SLEEP1>(&kv_empty[slot], ph, abort_flag);
+                        ok = cross_tc::wait(&kv_empty[slot], ph, abort_flag);
                         if (ok && tc::elect_one()) {
                             tc::mbar_expect_tx(&kv_full[slot], M::kv);
                             for (int ch = 0; ch < NCH; ++ch)
@@ -596,10 +596,10 @@ bool cross_tc_supported(const CrossArgs& a) {
            mappable(a.o, a.n_seq, a.n_q, a.heads) && (a.group == 1 || a.q.head > 0);
 }
 
-CrossParts cross_tc_parts(const CrossArgs& a) {
+int cross_tc_parts(const CrossArgs& a) {
     int tiles, pairs, parts;
     shape_of(a, &tiles, &pairs, &parts);
-    return CrossParts{parts, nullptr, nullptr};
+    return parts;
 }
 
 int cross_tc_forward(const CrossArgs& c, const CrossParts& parts, cudaStream_t s) {

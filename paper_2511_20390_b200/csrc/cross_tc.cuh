@@ -3,12 +3,6 @@
 #include "cross.h"
 #include "tc_common.cuh"
 
-#ifndef SLEEP0
-#define SLEEP0 0
-#endif
-#ifndef SLEEP1
-#define SLEEP1 0
-#endif
 namespace cross_tc {
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
@@ -16,19 +10,14 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-// Warp-uniform bounded wait as tc::wait_uniform, for kernels in which many warps wait at once: one that asks again and again takes issue
-// slots of those that work, so it sleeps in between, longer (NS) where nothing waits for this warp in turn.
-template <int NS = SLEEP0>
+// Warp-uniform bounded wait as tc::wait_uniform; the abort flag and the clock are only looked at every 16 polls.
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
     bool r = tc::mbar_try_wait(bar, parity);
     if (!r) {
         const long long t0 = clock64();
         for (;;) {
 #pragma unroll 1
-            for (int i = 0; i < 16 && !r; ++i) {
-                if (NS) __nanosleep(NS);
-                r = tc::mbar_try_wait(bar, parity);
-            }
+            for (int i = 0; i < 16 && !r; ++i) r = tc::mbar_try_wait(bar, parity);
             if (r || *abort_flag || clock64() - t0 > 4000000000ll) break;
         }
     }
