@@ -5,27 +5,31 @@
 // Bound by HBM (K and V are read once, 2 rows of multiply-adds per element) or, for short state sequences, by latency: no tensor
 // memory, no tile copies, one launch.  L lanes hold a state's row, one 16-byte unit each, and a warp 32 / L states; every group of
 // lanes takes KEYS states at a time.  Units are copied to shared memory several steps ahead, every lane its own, so that the bytes in
-// flight do not cost registers.  Scores are summed over the lanes by exchanges, which leaves them in every lane: nothing is passed on.  The parts of a CTA's groups are joined through shared memory; long state sequences
+// flight do not cost registers.  Scores
+// are summed over the lanes by exchanges that halve the values as they go, so that every lane ends with its own (row, state) and takes
+// its exponential; the probabilities are then passed to all lanes of the group.  The parts of a CTA's groups are joined through shared memory; long state sequences
 // are split over CTAs as well and joined by cross_join_kernel.
-#include "cross.h"
+#include "cross_tc.cuh"
 
 namespace {
 
+using namespace cross_tc;
+
 constexpr int kThreads = 128, kWarps = kThreads / 32, kSms = 148, kSteps = 4;     // steps of copies in the ring
 
-template <typename E> struct Unit;            // 16 bytes of a row, as fp32
+template <typename E> struct Unit;            // 16 bytes of a row, as pairs of fp32 numbers
 template <> struct Unit<float> {
     static constexpr int V = 4;
-    static __device__ __forceinline__ void values(const uint4& u, float (&f)[4]) {
-        f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
+    static __device__ __forceinline__ void values(const uint4& u, uint64_t (&f)[2]) {
+        f[0] = pair(__uint_as_float(u.x), __uint_as_float(u.y)); f[1] = pair(__uint_as_float(u.z), __uint_as_float(u.w));
     }
 };
 template <> struct Unit<__nv_bfloat16> {
     static constexpr int V = 8;
-    static __device__ __forceinline__ void values(const uint4& u, float (&f)[8]) {
+    static __device__ __forceinline__ void values(const uint4& u, uint64_t (&f)[4]) {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+        for (int i = 0; i < 4; ++i) f[i] = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
     }
 };
 __device__ __forceinline__ float to_f(float v) { return v; }
@@ -46,7 +50,6 @@ template <typename E, int R, int L> __global__ void __launch_bounds__(kThreads) 
     extern __shared__ uint4 ring[];           // [step][warp][2 KEYS][lane]; at the end the groups' parts
     __shared__ float2 stats[GROUPS][R];       // maximum, sum
     float* acc_of = reinterpret_cast<float*>(ring);      // [group][row][channel]
-    static_assert(GROUPS * R * L * V * 4 <= kSteps * kThreads * 2 * KEYS * 16, "parts fit into the ring");
     free_grid_dep_wait();
     free_grid_dep_launch();
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
@@ -58,31 +61,45 @@ template <typename E, int R, int L> __global__ void __launch_bounds__(kThreads) 
     const bool in = lane * V < a.d;
     const E* kb = reinterpret_cast<const E*>(a.k.p) + sp.enc * a.k.seq + (long long)sp.row0 * a.k.tok + kh * a.k.head + lane * V;
     const E* vb = reinterpret_cast<const E*>(a.v.p) + sp.enc * a.v.seq + (long long)sp.row0 * a.v.tok + kh * a.v.head + lane * V;
-    float q[R][V], acc[R][V], top[R], sum[R];
+    constexpr int N = R * KEYS, NF = N >= L ? N / L : 1, D = N >= L ? 1 : L / N;     // scores of a group and step, of a lane; lanes of a score
+    constexpr int SAME = NF < KEYS ? NF : KEYS, ROWL = KEYS * D / NF > 1 ? KEYS * D / NF : 1;      // of a lane's scores, those of one row; lanes of a row
+    uint64_t q[R][V / 2], acc[R][V / 2];
+    float top[NF], sum[NF];
     const float c = a.scale * 1.4426950408889634f;
 #pragma unroll
+    for (int v = 0; v < NF; ++v) { top[v] = -INFINITY; sum[v] = 0.f; }
+#pragma unroll
     for (int r = 0; r < R; ++r) {
-        top[r] = -INFINITY; sum[r] = 0.f;
         const E* qp = reinterpret_cast<const E*>(a.q.p) + s * a.q.seq + (r / a.group) * a.q.tok + (kh * a.group + r % a.group) * a.q.head + lane * V;
 #pragma unroll
-        for (int e = 0; e < V; ++e) { q[r][e] = r < rows && in ? to_f(qp[e]) : 0.f; acc[r][e] = 0.f; }
+        for (int e = 0; e < V / 2; ++e) {
+            q[r][e] = r < rows && in ? pair(to_f(qp[2 * e]), to_f(qp[2 * e + 1])) : 0ull;
+            acc[r][e] = 0ull;
+        }
     }
+    // score i of a group is in slot i % NF of lane i / NF * D
+    auto from_lane = [&](const float (&v)[NF], int i) { return __shfl_sync(0xffffffffu, v[i % NF], i / NF * D, L); };
     const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + ((threadIdx.x >> 5) * 2 * KEYS * 32 + (threadIdx.x & 31)) * 16u;
     constexpr uint32_t STEP = kThreads * 2 * KEYS * 16;
     auto counts = [&](int j) { return j < hi && (!mask || mask[j] != 0); };
     int ahead = lo + group * KEYS;                                 // first state of the step to copy next
     uint32_t to = 0;
+    const E *kp = kb + (long long)ahead * a.k.tok, *vp = vb + (long long)ahead * a.v.tok;     // running addresses, which may lie behind the last state
+    const long long k_step = (long long)(GROUPS * KEYS) * a.k.tok, v_step = (long long)(GROUPS * KEYS) * a.v.tok;
     auto copy = [&]() {
+        const int left = in ? hi - ahead : 0;
+        const E *k1 = kp, *v1 = vp;
 #pragma unroll
         for (int k = 0; k < KEYS; ++k) {
-            const int j = ahead + k;
-            const bool ok = in && counts(j);                       // else zeros, and nothing is read
-            const uint32_t dst = mine + to + k * 512u;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(kb + (ok ? j : 0) * a.k.tok), "r"(ok ? 16 : 0) : "memory");
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + KEYS * 512u), "l"(vb + (ok ? j : 0) * a.v.tok), "r"(ok ? 16 : 0) : "memory");
+            const bool ok = k < left && (!mask || mask[ahead + k] != 0);      // else zeros, and nothing is read
+            const uint32_t dst = mine + to + k * 512u, size = ok ? 16u : 0u;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(ok ? k1 : kb), "r"(size) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + KEYS * 512u), "l"(ok ? v1 : vb), "r"(size) : "memory");
+            k1 += a.k.tok; v1 += a.v.tok;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         ahead += GROUPS * KEYS;
+        kp += k_step; vp += v_step;
         to = to + STEP == kSteps * STEP ? 0 : to + STEP;
     };
 #pragma unroll
@@ -101,59 +118,101 @@ template <typename E, int R, int L> __global__ void __launch_bounds__(kThreads) 
         }
         from = from + STEP == kSteps * STEP ? 0 : from + STEP;
         copy();                                                    // into the step that was read before this one
-        float sc[R][KEYS];
+        float sc[N];
 #pragma unroll
         for (int k = 0; k < KEYS; ++k) {
-            float f[V];
+            uint64_t f[V / 2];
             Unit<E>::values(ku[k], f);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                float t = 0.f;
+                uint64_t t = 0ull;
 #pragma unroll
-                for (int e = 0; e < V; ++e) t = fmaf(q[r][e], f[e], t);
-                sc[r][k] = t;
+                for (int e = 0; e < V / 2; ++e) t = fma2(q[r][e], f[e], t);
+                sc[r * KEYS + k] = low(t) + high(t);
             }
         }
+        {
+            int n = N;
 #pragma unroll
-        for (int o = L / 2; o > 0; o >>= 1)
+            for (int o = L / 2; o > 0; o >>= 1) {
+                if (n > 1) {
+                    n >>= 1;
+                    const bool up = lane & o;
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int k = 0; k < KEYS; ++k) sc[r][k] += __shfl_xor_sync(0xffffffffu, sc[r][k], o);
-        float p[R][KEYS];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float m = top[r];
-#pragma unroll
-            for (int k = 0; k < KEYS; ++k) { sc[r][k] = ok[k] ? sc[r][k] : -INFINITY; m = fmaxf(m, sc[r][k]); }
-            if (m != top[r]) {                                     // the same in all lanes of a group
-                const float alpha = power<E>((top[r] - m) * c);
-                sum[r] *= alpha;
-#pragma unroll
-                for (int e = 0; e < V; ++e) acc[r][e] *= alpha;
-                top[r] = m;
+                    for (int i = 0; i < N / 2; ++i)
+                        if (i < n) {
+                            const float keep = up ? sc[n + i] : sc[i], give = up ? sc[i] : sc[n + i];
+                            sc[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                        }
+                } else {
+                    sc[0] += __shfl_xor_sync(0xffffffffu, sc[0], o);
+                }
             }
-            const float base = m == -INFINITY ? 0.f : m;
+        }
+        float p[NF], alpha[NF];
+        bool moved = false;
 #pragma unroll
-            for (int k = 0; k < KEYS; ++k) { p[r][k] = power<E>((sc[r][k] - base) * c); sum[r] += p[r][k]; }
+        for (int v = 0; v < NF; ++v) {
+            const int k = (lane / D * NF + v) % KEYS;              // this score's state
+            bool good = ok[0];
+#pragma unroll
+            for (int u = 1; u < KEYS; ++u) good = k == u ? ok[u] : good;
+            p[v] = good ? sc[v] : -INFINITY;
+        }
+#pragma unroll
+        for (int v = 0; v < NF; v += SAME) {
+            float m = p[v];
+#pragma unroll
+            for (int u = 1; u < SAME; ++u) m = fmaxf(m, p[v + u]);
+#pragma unroll
+            for (int o = D; o < ROWL; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            const float now = fmaxf(top[v], m), base = now == -INFINITY ? 0.f : now;
+            const float al = now == top[v] ? 1.f : power<E>((top[v] - base) * c);
+            moved = moved || now != top[v];
+#pragma unroll
+            for (int u = 0; u < SAME; ++u) {
+                p[v + u] = power<E>((p[v + u] - base) * c);
+                sum[v + u] = fmaf(sum[v + u], al, p[v + u]);
+                top[v + u] = now;
+                alpha[v + u] = al;
+            }
+        }
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float al = from_lane(alpha, r * KEYS);
+                const uint64_t a2 = pair(al, al);
+#pragma unroll
+                for (int e = 0; e < V / 2; ++e) acc[r][e] = mul2(acc[r][e], a2);
+            }
         }
 #pragma unroll
         for (int k = 0; k < KEYS; ++k) {
-            float f[V];
+            uint64_t f[V / 2];
             Unit<E>::values(vu[k], f);
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int r = 0; r < R; ++r) {
+                const float pr = from_lane(p, r * KEYS + k);
+                const uint64_t p2 = pair(pr, pr);
 #pragma unroll
-                for (int e = 0; e < V; ++e) acc[r][e] = fmaf(p[r][k], f[e], acc[r][e]);
+                for (int e = 0; e < V / 2; ++e) acc[r][e] = fma2(p2, f[e], acc[r][e]);
+            }
         }
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();                                               // the ring is free for the parts
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        if (lane == 0) stats[group][r] = make_float2(top[r], sum[r]);
+        const float m = from_lane(top, r * KEYS);
+        float l = 0.f;
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc_of[(group * R + r) * L * V + lane * V + e] = acc[r][e];
+        for (int k = 0; k < KEYS; ++k) l += from_lane(sum, r * KEYS + k);
+        if (lane == 0) stats[group][r] = make_float2(m, l);
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) {
+            acc_of[(group * R + r) * L * V + lane * V + 2 * e] = low(acc[r][e]);
+            acc_of[(group * R + r) * L * V + lane * V + 2 * e + 1] = high(acc[r][e]);
+        }
     }
     __syncthreads();
     const long long all = (long long)a.n_seq * a.heads * a.n_q;
@@ -189,7 +248,7 @@ template <typename E, int R> int start(const CrossArgs& a, const CrossParts& par
     const long long ctas = (long long)a.n_seq * a.kv_heads * parts.n;
     if (ctas > 0x7fffffffLL) return FREE_ERR_UNSUPPORTED;
     auto kernel = units <= 4 ? cross_rows_kernel<E, R, 4> : units <= 8 ? cross_rows_kernel<E, R, 8> : units <= 16 ? cross_rows_kernel<E, R, 16> : cross_rows_kernel<E, R, 32>;
-    constexpr int smem = kSteps * kThreads * 2 * (R <= 4 ? 4 : 2) * 16;
+    constexpr int copies = kSteps * kThreads * 2 * (R <= 4 ? 4 : 2) * 16, joined = kThreads * R * Unit<E>::V * 4, smem = copies > joined ? copies : joined;
     if (smem > 47 * 1024) FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     return free_launch(free_overlap_for_rows(a.n_seq), kernel, dim3((unsigned)ctas), dim3(kThreads), smem, s, a, parts);
 }

@@ -527,39 +527,57 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     if (warp == 12) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, kTmemCols); }
 }
 
-// out, lse of a row from its parts' own: a warp per row.
+// out, lse of a row from its parts' own: a CTA per row, the parts' weights in shared memory, two slices of the parts per channel.
+constexpr int kMaxParts = 2048;
 template <typename E> __global__ void __launch_bounds__(256) cross_join_kernel(const CrossArgs a, const CrossParts p, long long rows) {
+    __shared__ float weight[kMaxParts], part_of[2][kCrossMaxD], reduce[8];
     free_grid_dep_wait();
     free_grid_dep_launch();
-    const int lane = threadIdx.x & 31;
-    for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * 8) {
-        float top = -INFINITY;
-        for (int k = lane; k < p.n; k += 32) top = fmaxf(top, p.lse[k * rows + i]);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, ch = threadIdx.x & 127, slice = threadIdx.x >> 7;
+    const long long i = blockIdx.x;
+    float top = -INFINITY;
+    for (int k = threadIdx.x; k < p.n; k += 256) {
+        weight[k] = p.lse[k * rows + i];
+        top = fmaxf(top, weight[k]);
+    }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-        float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-        if (top != -INFINITY)
-            for (int k = 0; k < p.n; ++k) {
-                const float l = p.lse[k * rows + i];
-                if (l == -INFINITY) continue;                      // a part without a state wrote nothing else
-                const float f = expf(l - top);
-                sum += f;
-                const float* o = p.out + (k * rows + i) * a.d;
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    if (lane == 0) reduce[warp] = top;
+    __syncthreads();
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (lane + 32 * c < a.d) acc[c] = fmaf(f, o[lane + 32 * c], acc[c]);
-            }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    for (int k = 0; k < 8; ++k) top = fmaxf(top, reduce[k]);
+    __syncthreads();
+    float sum = 0.f;
+    for (int k = threadIdx.x; k < p.n; k += 256) {
+        weight[k] = top == -INFINITY ? 0.f : expf(weight[k] - top);       // 0: a part without a state, which wrote nothing else
+        sum += weight[k];
+    }
+    sum = free_warp_sum(sum);
+    if (lane == 0) reduce[warp] = sum;
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += reduce[k];
+    float acc = 0.f;
+    if (ch < a.d) {
+        const float* o = p.out + i * a.d + ch;
+        const long long step = rows * a.d;
+#pragma unroll 8
+        for (int k = slice; k < p.n; k += 2) {
+            const float f = weight[k], v = f != 0.f ? o[k * step] : 0.f;
+            acc = fmaf(f, v, acc);
+        }
+    }
+    part_of[slice][ch] = acc;
+    __syncthreads();
+    if (threadIdx.x < a.d) {
+        const float v = sum == 0.f ? 0.f : (part_of[0][ch] + part_of[1][ch]) / sum;
         const int t = (int)(i % a.n_q), h = (int)(i / a.n_q % a.heads), s = (int)(i / a.n_q / a.heads);
         E* out = reinterpret_cast<E*>(const_cast<void*>(a.o.p)) + s * a.o.seq + t * a.o.tok + h * a.o.head;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (lane + 32 * c < a.d) {
-                if constexpr (sizeof(E) == 4) out[lane + 32 * c] = acc[c] * inv;
-                else out[lane + 32 * c] = __float2bfloat16(acc[c] * inv);
-            }
-        if (a.lse && lane == 0) a.lse[i] = top == -INFINITY ? -INFINITY : top + logf(sum);
+        if constexpr (sizeof(E) == 4) out[ch] = v;
+        else out[ch] = __float2bfloat16(v);
     }
+    if (a.lse && threadIdx.x == 0) a.lse[i] = top == -INFINITY ? -INFINITY : top + logf(sum);
 }
 
 int tokens_per_tile(const CrossArgs& a) { return BQ / a.group; }
@@ -638,8 +656,9 @@ int cross_tc_forward(const CrossArgs& c, const CrossParts& parts, cudaStream_t s
 }
 
 int cross_join(int dtype, const CrossArgs& a, const CrossParts& parts, cudaStream_t s) {
-    const long long rows = (long long)a.n_seq * a.heads * a.n_q, ctas = (rows + 7) / 8;
-    const dim3 grid((unsigned)(ctas < kSms * 8 ? ctas : kSms * 8));
+    const long long rows = (long long)a.n_seq * a.heads * a.n_q;
+    if (parts.n > kMaxParts || rows > 0x7fffffffLL) return FREE_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)rows);
     const bool early = free_overlap_for_rows(rows);
     return dtype == FREE_FP32 ? free_launch(early, cross_join_kernel<float>, grid, dim3(256), 0, s, a, parts, rows)
                               : free_launch(early, cross_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, a, parts, rows);
