@@ -1066,7 +1066,7 @@ def op_attention(qkv, heads):
 
 
 # struct free_cross_attn of the public header
-_CROSS = struct.Struct("<3Q9q4Q9if4x")
+_CROSS = struct.Struct("<3Q9q4Q9if")
 
 
 def _cross_shape(q, k, v, kv_lens, kv_mask, kv_seq, kv_offsets, max_kv, scale):
@@ -1140,8 +1140,8 @@ def op_cross_attention(q, k, v, kv_lens=None, kv_mask=None, kv_seq=None, kv_offs
     lse = q.new_empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32) if want_lse else None
     need = (_LIB or lib()).free_op_cross_attention_workspace_bytes(shape)
     ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    os = out.stride()
-    _launch("free_op_cross_attention", dev, shape, out.data_ptr(), os[0], os[1], os[2], _adr(lse), _adr(ws), need,
+    ys = out.stride()
+    _launch("free_op_cross_attention", dev, shape, out.data_ptr(), ys[0], ys[1], ys[2], _adr(lse), _adr(ws), need,
             _error_word(dev).data_ptr() if q.dtype == torch.bfloat16 else None)
     return (out, lse) if want_lse else out
 

@@ -43,7 +43,7 @@ constexpr int kSoftmaxRegs = 152, kOtherRegs = 56;
 static_assert(256 * kSoftmaxRegs + 384 * kOtherRegs <= kThreads * 96, "registers of the launch");
 constexpr uint32_t kChunk = BQ * 128, kKvChunk = BK * 128;      // rows x 64 channels, 128-byte rows
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kCtrl = 3072;              // barriers, the queue of items, maxima and sums of the rows of both tiles
+constexpr uint32_t kCtrl = 3 * 1024;             // barriers, the queue of items, maxima and sums of the rows of both tiles
 constexpr uint32_t kQueue = 8;
 constexpr uint32_t kStage = 32 * 128;         // 32 rows x 64 channels on their way out
 // State sequences up to this length take two sets of the tiles of Q: with nothing but a block or two per item, Q has to be on its way

@@ -44,7 +44,12 @@ extern "C" int free_op_rms_norm(int x_dtype, int res_dtype, int y_dtype, int n_g
     const long long strides = x_tok | y_tok | (heads > 1 ? x_head | y_head : 0) | (residual ? res_stride : 0) | (res_out ? res_out_stride : 0) |
                               (weight && n_groups > 1 ? mod_stride : 0) | place(x, x_dtype) | place(y, y_dtype) |
                               (residual ? place(residual, res_dtype) : 0) | (res_out ? place(res_out, res_dtype) : 0);
-    const int vw = D % 4 == 0 && strides % 4 == 0 && free_aligned16(weight) ? 4 : 1;
+    // (eight where every type has 16 bits or fewer, but for widths that whole blocks of 128 columns in one warp serve as well, and for
+    // heads that would leave lanes idle: 24 x 1024 tokens, 16 heads of 72, 25 us by four, 27 by eight; of 64, 22 by eight)
+    int vw = D % 4 == 0 && strides % 4 == 0 && free_aligned16(weight) ? 4 : 1;
+    const bool thin = x_dtype == FREE_BF16 && y_dtype != FREE_FP32 && (!residual || res_dtype == FREE_BF16);
+    const bool idle = !residual && y_dtype != FREE_E4M3 && D > 64 && D < 96;
+    if (vw == 4 && thin && D % 8 == 0 && strides % 8 == 0 && (D > 1152 || D % 128) && !idle) vw = 8;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     const bool rf = residual && res_dtype == FREE_FP32;            // without a residual its type does not matter
     if (x_dtype == FREE_FP32) return rf ? rms_norm_ff(a, vw, y_dtype, s) : rms_norm_fb(a, vw, y_dtype, s);

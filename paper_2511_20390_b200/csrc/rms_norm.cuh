@@ -17,8 +17,6 @@ namespace rms {
 constexpr int kSms = 148;
 using e4m3 = __nv_fp8_e4m3;
 
-template <int VW> struct Words { uint32_t w[VW]; };
-
 // VW columns as they come from memory, bf16 packed two by two (single ones as floats)
 template <typename E, int VW> constexpr int kWords = sizeof(E) == 4 || VW == 1 ? VW : VW / 2;
 template <typename E, int VW> __device__ __forceinline__ float value(const uint32_t* w, int e) {
@@ -26,7 +24,7 @@ template <typename E, int VW> __device__ __forceinline__ float value(const uint3
     return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
 }
 template <typename E, int VW> __device__ __forceinline__ void load(const E* p, bool ok, uint32_t* w) {
-    if constexpr (VW == 4 && sizeof(E) == 4) {
+    if constexpr (VW * sizeof(E) == 16) {
         const uint4 u = ok ? __ldcs(reinterpret_cast<const uint4*>(p)) : make_uint4(0u, 0u, 0u, 0u);
         w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
     } else if constexpr (VW == 4) {
@@ -43,28 +41,34 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 template <int VW> __device__ __forceinline__ void store(float* p, const float* v) {
+    static_assert(VW <= 4, "16-byte accesses");
     if constexpr (VW == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
     else *p = v[0];
 }
 template <int VW> __device__ __forceinline__ void store(__nv_bfloat16* p, const float* v) {
-    if constexpr (VW == 4) *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+    if constexpr (VW == 8) *reinterpret_cast<uint4*>(p) = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+    else if constexpr (VW == 4) *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
     else *p = __float2bfloat16(v[0]);
 }
+__device__ __forceinline__ uint32_t pack4(const float* v) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
+    return lo | hi << 16;
+}
 template <int VW> __device__ __forceinline__ void store(e4m3* p, const float* v) {
-    if constexpr (VW == 4) {
-        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
-        *reinterpret_cast<uint32_t*>(p) = lo | hi << 16;
-    } else {
-        *reinterpret_cast<__nv_fp8_storage_t*>(p) = __nv_cvt_float_to_fp8(v[0], __NV_SATFINITE, __NV_E4M3);
-    }
+    if constexpr (VW == 8) *reinterpret_cast<uint2*>(p) = make_uint2(pack4(v), pack4(v + 4));
+    else if constexpr (VW == 4) *reinterpret_cast<uint32_t*>(p) = pack4(v);
+    else *reinterpret_cast<__nv_fp8_storage_t*>(p) = __nv_cvt_float_to_fp8(v[0], __NV_SATFINITE, __NV_E4M3);
 }
 template <int VW> __device__ __forceinline__ void table(const float* p, bool ok, float add, float* v) {
-    if constexpr (VW == 4) {
-        const float4 f = ok ? __ldg(reinterpret_cast<const float4*>(p)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        v[0] = f.x + add; v[1] = f.y + add; v[2] = f.z + add; v[3] = f.w + add;
-    } else {
+    if constexpr (VW == 1) {
         v[0] = (ok ? __ldg(p) : 0.f) + add;
+    } else {
+#pragma unroll
+        for (int k = 0; k < VW; k += 4) {
+            const float4 f = ok ? __ldg(reinterpret_cast<const float4*>(p + k)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            v[k] = f.x + add; v[k + 1] = f.y + add; v[k + 2] = f.z + add; v[k + 3] = f.w + add;
+        }
     }
 }
 // NaN is kept: a run with a NaN gets a NaN scale
@@ -73,9 +77,9 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-__device__ __forceinline__ float warp_max(float v) {
+template <int L = 32> __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(~0u, v, o));
+    for (int o = L / 2; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(~0u, v, o));
     return v;
 }
 // scale of a run whose largest magnitude is `top`, and its inverse; a run without anything above 2^-100 is zeros at scale 1
@@ -89,7 +93,8 @@ template <typename TX, typename TR, typename TY, int P, int VW, bool FULL, int M
 __global__ void __launch_bounds__(MAXT, MINB) rms_norm_kernel(const RmsArgs a) {
     __shared__ float part[2][MAXT / 32], tops[2][MAXT / 32];
     constexpr bool Y8 = sizeof(TY) == 1;
-    constexpr int XW = kWords<TX, VW>, RW = kWords<TR, VW>, RUN = 4 / VW;      // RUN: pieces of 128 columns
+    constexpr int XW = kWords<TX, VW>, RW = kWords<TR, VW>;
+    constexpr int RUN = VW == 8 ? 1 : 4 / VW, SHARE = VW == 8 ? 16 : 32;      // pieces and lanes of a run of 128 columns
     free_grid_dep_wait();
     free_grid_dep_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, W = a.warps;
@@ -182,13 +187,13 @@ __global__ void __launch_bounds__(MAXT, MINB) rms_norm_kernel(const RmsArgs a) {
                     for (int p = b * RUN; p < (b + 1) * RUN && p < P; ++p)
 #pragma unroll
                         for (int e = 0; e < VW; ++e) top = max_nan(top, fabsf(v[p][e]));
-                    const float2 f = scale_of(warp_max(top));
+                    const float2 f = scale_of(warp_max<SHARE>(top));
 #pragma unroll
                     for (int p = b * RUN; p < (b + 1) * RUN && p < P; ++p)
 #pragma unroll
                         for (int e = 0; e < VW; ++e) v[p][e] *= f.y;
-                    const int run = (at(b * RUN) - lane * VW) >> 7;
-                    if (lane == 0 && run * 128 < a.D) a.scales[row * a.scale_stride + run] = f.x;
+                    const int run = at(b * RUN) >> 7;
+                    if (lane % SHARE == 0 && run * 128 < a.D) a.scales[row * a.scale_stride + run] = f.x;
                 }
             } else {
                 float top = 0.f;
@@ -302,14 +307,26 @@ template <typename TX, typename TY, int L, int C, int VW> int start_heads(RmsArg
 template <typename TX, typename TR, typename TY, int VW> int launch(const RmsArgs& a, cudaStream_t s) {
     if constexpr (sizeof(TY) > 1) {
         if (!a.res && a.D <= 128) {
-            if (a.D <= 32) return start_heads<TX, TY, 4, 8, VW>(a, s);
-            if (a.D <= 64) return start_heads<TX, TY, 8, 8, VW>(a, s);
-            if (a.D <= 96) return start_heads<TX, TY, 8, 12, VW>(a, s);
-            return start_heads<TX, TY, 8, 16, VW>(a, s);
+            if constexpr (VW == 8) {
+                if (a.D <= 32) return start_heads<TX, TY, 4, 8, VW>(a, s);
+                if (a.D <= 64) return start_heads<TX, TY, 8, 8, VW>(a, s);
+                return start_heads<TX, TY, 8, 16, VW>(a, s);
+            } else {
+                if (a.D <= 32) return start_heads<TX, TY, 4, 8, VW>(a, s);
+                if (a.D <= 64) return start_heads<TX, TY, 8, 8, VW>(a, s);
+                if (a.D <= 96) return start_heads<TX, TY, 8, 12, VW>(a, s);
+                return start_heads<TX, TY, 8, 16, VW>(a, s);
+            }
         }
     }
     const int D = a.D;
-    if constexpr (VW == 4) {
+    if constexpr (VW == 8) {
+        if (D > 1024 && D % 1024 == 0) return start<TX, TR, TY, 4, 8, true, 256, 2>(a, D / 1024, s);
+        if (D <= 256) return start<TX, TR, TY, 1, 8, false, 128, 8>(a, 1, s);
+        if (D <= 512) return start<TX, TR, TY, 2, 8, false, 128, 6>(a, 1, s);
+        if (D <= 1024) return start<TX, TR, TY, 4, 8, false, 128, 4>(a, 1, s);
+        return start<TX, TR, TY, 4, 8, false, 256, 2>(a, (D + 1023) / 1024, s);
+    } else if constexpr (VW == 4) {
         switch (D % 128 == 0 ? D / 128 : 0) {
             case 3: return start<TX, TR, TY, 3, 4, true, 128, 6>(a, 1, s);
             case 6: return start<TX, TR, TY, 6, 4, true, 128, 4>(a, 1, s);
@@ -329,6 +346,8 @@ template <typename TX, typename TR, typename TY, int VW> int launch(const RmsArg
 }
 template <typename TX, typename TR> int launch_y(const RmsArgs& a, int vw, int y_dtype, cudaStream_t s) {
     using bf = __nv_bfloat16;
+    if constexpr (sizeof(TX) == 2 && sizeof(TR) == 2)
+        if (vw == 8) return y_dtype == FREE_BF16 ? launch<TX, TR, bf, 8>(a, s) : launch<TX, TR, e4m3, 8>(a, s);
     if (y_dtype == FREE_FP32) return vw == 4 ? launch<TX, TR, float, 4>(a, s) : launch<TX, TR, float, 1>(a, s);
     if (y_dtype == FREE_BF16) return vw == 4 ? launch<TX, TR, bf, 4>(a, s) : launch<TX, TR, bf, 1>(a, s);
     return vw == 4 ? launch<TX, TR, e4m3, 4>(a, s) : launch<TX, TR, e4m3, 1>(a, s);

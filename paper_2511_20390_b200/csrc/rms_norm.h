@@ -18,7 +18,7 @@ struct RmsArgs {
     long long rows_per_team;
 };
 
-// vw: consecutive columns of one access, 4 or 1.  One function per pair of types (x, residual).
+// vw: consecutive columns of one access, 8 (bf16 only), 4 or 1.  One function per pair of types (x, residual).
 int rms_norm_ff(const RmsArgs& a, int vw, int y_dtype, cudaStream_t s);
 int rms_norm_fb(const RmsArgs& a, int vw, int y_dtype, cudaStream_t s);
 int rms_norm_bf(const RmsArgs& a, int vw, int y_dtype, cudaStream_t s);
