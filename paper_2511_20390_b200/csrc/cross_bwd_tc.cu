@@ -20,21 +20,23 @@ namespace {
 using namespace cross_tc;
 
 constexpr int BR = 128, BC = 64;
-constexpr int kThreads = 640, kSms = 148;     // warps 0 - 7 elementwise, 8 - 11 results, 12 loads, 13 statistics, 14 S and dP, 15 sums, 16 zeros
+constexpr int kThreads = 640, kSms = 148;     // warps 0 - 7 elementwise, 8 - 11 results, 12 loads, 13 statistics, 14 S, 15 dP, 16 zeros, 17 dq or dk, 18 dv, 19 items
 constexpr int kMathRegs = 136, kOtherRegs = 64;
 static_assert(256 * kMathRegs + 384 * kOtherRegs <= kThreads * 96, "registers of the launch");
 constexpr uint32_t kChunk = BR * 128, kColChunk = BC * 128;
-constexpr uint32_t kQueue = 4, kStage = 32 * 128;
+constexpr uint32_t kQueue = 4, kStage = 32 * 128;     // staging: 128 bytes of 32 rows, pieces of 16 swizzled
 
-// NCH: chunks of 64 channels; AB: sets of the rows' operands; N1, N2: ring slots of the columns' operands; NB: buffers of S and dP
-template <bool DKV, int NCH, int AB, int N1, int N2, int NB, int SG> struct Mem {
+// NCH: chunks of 64 channels; W: columns of tensor memory per sum; AB: sets of the rows' operands; N1, N2: ring slots of the columns'
+// operands; NS, ND: buffers of S (p and dS go over it) and of dP (free once read); NA: sets of sums
+template <bool DKV, int NCH, int W, int AB, int N1, int N2, int NS, int ND, int NA> struct Mem {
     static constexpr uint32_t a = NCH * kChunk, b = NCH * kColChunk;
     static constexpr uint32_t ctrl = 1024 + (DKV ? N1 * BC * 8 : 0);
     static constexpr uint32_t ctrl_bytes = (ctrl + 1023) / 1024 * 1024;
-    static constexpr uint32_t bytes = 1024 + ctrl_bytes + AB * 2 * a + (N1 + N2) * b + 4 * SG * kStage;
-    static constexpr uint32_t acc_col = NB * 128, acc_width = (512 - acc_col) / (DKV ? 2 : 1);
+    static constexpr uint32_t bytes = 1024 + ctrl_bytes + AB * 2 * a + (N1 + N2) * b + 4 * kStage;
+    static constexpr uint32_t dp_col = NS * 64, acc_col = (NS + ND) * 64, acc_set = (DKV ? 2 : 1) * W;
+    static_assert(acc_col + NA * acc_set <= 512, "tensor memory of an SM");
     static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
-    static_assert((2 * AB + 2 * N1 + 2 * N2 + 3 * NB + 2 + 2 * kQueue + 1) * 8 <= 512, "barriers");
+    static_assert((2 * AB + 2 * N1 + 2 * N2 + 3 * NS + ND + 2 * NA + 2 * kQueue + 1) * 8 <= 512, "barriers");
 };
 
 struct Args {
@@ -125,11 +127,11 @@ struct Columns {
     }
 };
 
-template <bool DKV, int NCH, int AB, int N1, int N2, int NB, int SG>
+template <bool DKV, int NCH, int W, int AB, int N1, int N2, int NS, int ND, int NA>
 __global__ void __launch_bounds__(kThreads, 1)
 cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constant__ CUtensorMap mapA2, const __grid_constant__ CUtensorMap mapB1,
-                 const __grid_constant__ CUtensorMap mapB2, const __grid_constant__ CUtensorMap mapO1, const __grid_constant__ CUtensorMap mapO2, const Args a) {
-    using M = Mem<DKV, NCH, AB, N1, N2, NB, SG>;
+                 const __grid_constant__ CUtensorMap mapB2, const Args a) {
+    using M = Mem<DKV, NCH, W, AB, N1, N2, NS, ND, NA>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t* a_full = reinterpret_cast<uint64_t*>(smem);
@@ -139,11 +141,12 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
     uint64_t* b2_full = b1_empty + N1;
     uint64_t* b2_empty = b2_full + N2;
     uint64_t* s_full = b2_empty + N2;         // S and dP of a buffer
-    uint64_t* p_full = s_full + NB;           // p and dS
-    uint64_t* s_free = p_full + NB;           // the accumulating products have read them
-    uint64_t* acc_full = s_free + NB;
-    uint64_t* acc_free = acc_full + 1;
-    uint64_t* item_full = acc_free + 1;
+    uint64_t* p_full = s_full + NS;           // p and dS
+    uint64_t* s_free = p_full + NS;           // the accumulating products have read them
+    uint64_t* d_free = s_free + NS;           // dP has been read
+    uint64_t* acc_full = d_free + ND;
+    uint64_t* acc_free = acc_full + NA;
+    uint64_t* item_full = acc_free + NA;
     uint64_t* item_free = item_full + kQueue;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(item_free + kQueue);
     volatile uint32_t* abort_flag = tmem_slot + 1;
@@ -153,16 +156,18 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
     uint8_t* sA = smem + M::ctrl_bytes;
     uint8_t* ring1 = sA + AB * 2 * M::a;
     uint8_t* ring2 = ring1 + N1 * M::b;
+
     uint8_t* staging = ring2 + N2 * M::b;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < AB; ++i) { tc::mbar_init(&a_full[i], 1); tc::mbar_init(&a_empty[i], 1); }
+        for (int i = 0; i < AB; ++i) { tc::mbar_init(&a_full[i], 1); tc::mbar_init(&a_empty[i], 2); }
         for (int i = 0; i < N1; ++i) { tc::mbar_init(&b1_full[i], DKV ? 2 : 1); tc::mbar_init(&b1_empty[i], 1); }
         for (int i = 0; i < N2; ++i) { tc::mbar_init(&b2_full[i], 1); tc::mbar_init(&b2_empty[i], 1); }
-        for (int i = 0; i < NB; ++i) { tc::mbar_init(&s_full[i], 1); tc::mbar_init(&p_full[i], 4); tc::mbar_init(&s_free[i], 1); }
-        tc::mbar_init(acc_full, 1); tc::mbar_init(acc_free, 4);
-        for (uint32_t i = 0; i < kQueue; ++i) { tc::mbar_init(&item_full[i], 1); tc::mbar_init(&item_free[i], DKV ? 15 : 14); }    // 8 + 4 + 2 (+ statistics)
+        for (int i = 0; i < NS; ++i) { tc::mbar_init(&s_full[i], 2); tc::mbar_init(&p_full[i], 4); tc::mbar_init(&s_free[i], DKV ? 2 : 1); }
+        for (int i = 0; i < ND; ++i) tc::mbar_init(&d_free[i], 4);
+        for (int i = 0; i < NA; ++i) { tc::mbar_init(&acc_full[i], DKV ? 2 : 1); tc::mbar_init(&acc_free[i], 4); }
+        for (uint32_t i = 0; i < kQueue; ++i) { tc::mbar_init(&item_full[i], 1); tc::mbar_init(&item_free[i], DKV ? 18 : 16); }    // 8 + 4 + 4 (+ 2)
         *abort_flag = 0;
         tc::fence_barrier_init();
         tc::fence_proxy_async();
@@ -188,7 +193,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
         const int w = warp >> 2, q = warp & 3, r = q * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
         const uint64_t c2 = pair(a.c, a.c), sc2 = pair(a.scale, a.scale);
-        uint32_t tile = 0, buf = 0, buf_ph = 0, slot = 0, slot_ph = 0;       // column tiles of the CTA so far; buffer and ring slot of the next
+        uint32_t tile = 0, buf = 0, buf_ph = 0, dbuf = 0, slot = 0, slot_ph = 0;   // column tiles of the CTA so far; buffers and ring slot of the next
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
             ok = see(n);
@@ -210,11 +215,11 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                     uint32_t bits[2] = {0xffffffffu, 0xffffffffu};
                     const bool whole = DKV || (left - j * BC >= BC && !mask);
                     if (!whole) count_bits(bits, mask, j * BC, left, lane);
-                    ok = cross_tc::wait(&s_full[buf], buf_ph, abort_flag);
-                    if (DKV && ok) ok = cross_tc::wait(&b1_full[slot], slot_ph, abort_flag);       // the statistics, first hand
+                    ok = DKV ? cross_tc::wait2(&s_full[buf], buf_ph, &b1_full[slot], slot_ph, abort_flag) :      // (and the statistics, first hand)
+                               cross_tc::wait(&s_full[buf], buf_ph, abort_flag);
                     if (!ok) break;
                     tc::tc_fence_after();
-                    const uint32_t ts = lanes + buf * 128u, td = ts + 64u;
+                    const uint32_t ts = lanes + buf * 64u, td = lanes + M::dp_col + dbuf * 64u;
                     const ulonglong2 *cl = reinterpret_cast<const ulonglong2*>(stats + slot * 2 * BC), *cd = cl + BC / 4;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -222,6 +227,11 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                         tc::tmem_ld32(ts + 32 * h, s);
                         tc::tmem_ld32(td + 32 * h, d);
                         tc::tmem_wait_ld();
+                        if (h) {
+                            tc::tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) tc::mbar_arrive(&d_free[dbuf]);
+                        }
                         const uint32_t bit = h ? bits[1] : bits[0];
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {
@@ -247,23 +257,21 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                                 ds[k / 2] = pack2(x0, x1);
                             }
                         }
-                        // over scores that have been read: column 16 h of 32 (h + 1)
-                        if (DKV) tc::tmem_st16(ts + 16 * h, ps);
-                        tc::tmem_st16(td + 16 * h, ds);
+                        // over scores that have been read: p in the first half of their columns, dS in the other
+                        if (DKV) tc::tmem_st16(ts + 32 * h, ps);
+                        tc::tmem_st16(ts + 32 * h + 16, ds);
                     }
                     if (!whole) {
                         const int cols = left - j * BC >= BC ? BC : (left - j * BC + 15) & ~15;
                         const uint32_t out0 = ~bits[0] & low_bits(cols), out1 = ~bits[1] & low_bits(cols - 32);
                         if (out0 | out1) {                         // K has landed: S is complete
                             uint8_t* kt = ring1 + slot * M::b;
-#pragma unroll 1
-                            for (uint32_t o = out0, k0 = 0;; o = out1, k0 = 32) {
-                                for (; o; o &= o - 1u) {
-                                    const uint32_t k = k0 + (uint32_t)__ffs((int)o) - 1u;
-                                    if ((k & 3u) == (uint32_t)q && lane < 8 * NCH)
-                                        *reinterpret_cast<uint4*>(kt + (lane >> 3) * kColChunk + k * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                                }
-                                if (k0) break;
+                            constexpr int PER = 8 * NCH;           // 16-byte pieces of a row
+#pragma unroll
+                            for (int u = 0; u < BC * PER / 128; ++u) {
+                                const uint32_t i = u * 128u + r, k = i / PER, piece = i % PER;
+                                if ((k < 32 ? out0 >> k : out1 >> (k - 32)) & 1u)
+                                    *reinterpret_cast<uint4*>(kt + (piece >> 3) * kColChunk + k * 128 + (piece & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                             }
                             tc::fence_proxy_async();
                         }
@@ -273,7 +281,8 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                     __syncwarp();
                     if (lane == 0) tc::mbar_arrive(&p_full[buf]);
                 }
-                if (++buf == NB) { buf = 0; buf_ph ^= 1u; }
+                if (++buf == NS) { buf = 0; buf_ph ^= 1u; }
+                if (++dbuf == ND) dbuf = 0;
                 if (++slot == N1) { slot = 0; slot_ph ^= 1u; }
             }
         }
@@ -283,8 +292,8 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         // ------------------------------------------------------------------ results
         const int q = warp & 3, r = q * 32 + lane;
-        uint8_t* mine = staging + (uint32_t)q * SG * kStage;
-        uint32_t staged = 0, ph = 0;
+        uint8_t* mine = staging + (uint32_t)q * kStage;
+        uint32_t set = 0, ph = 0;
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
             ok = see(n);
@@ -295,115 +304,107 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
             const uint8_t* mask = a.where.mask ? a.where.mask + (a.where.offsets ? 0 : (long long)it.enc * a.where.n_kv) + it.row : nullptr;
             const bool keep = !DKV || (r < it.left && (!mask || mask[r] != 0));    // states that do not count: zeros, whatever the sums are
             const int seq = DKV ? it.enc : it.idx, tok0 = DKV ? it.row : it.row0;
-            ok = cross_tc::wait(acc_full, ph, abort_flag);
-            ph ^= 1u;
+            ok = cross_tc::wait(&acc_full[set], ph, abort_flag);
             if (!ok) break;
             tc::tc_fence_after();
 #pragma unroll 1
             for (int o = 0; o < (DKV ? 2 : 1); ++o) {
-                const uint32_t acc = tmem + M::acc_col + o * M::acc_width + ((uint32_t)(q * 32) << 16);
+                const uint32_t acc = tmem + M::acc_col + set * M::acc_set + o * W + ((uint32_t)(q * 32) << 16);
                 const CrossMat& mat = o ? a.o2 : a.o1;
-                const bool last = o == (DKV ? 1 : 0);
-                const bool boxed = a.parts == 1 && 32 * (q + 1) <= it.limit;
-                __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(mat.p)) + seq * mat.seq + (long long)(tok0 + r) * mat.tok + it.head * mat.head;
-                float* part = a.part_out + (((long long)it.part * 2 + o) * a.part_rows + ((long long)seq * a.where.kv_rows + tok0 + r) * a.kv_heads + it.head) * a.d;
+                const bool split = a.parts > 1, whole = a.d % (split ? 4 : 8) == 0;
+                // the warp's first row, and how far rows lie apart
+                uint8_t* dst = split ? reinterpret_cast<uint8_t*>(a.part_out + (((long long)it.part * 2 + o) * a.part_rows +
+                                                                                ((long long)seq * a.where.kv_rows + tok0 + 32 * q) * a.kv_heads + it.head) * a.d) :
+                                       reinterpret_cast<uint8_t*>(const_cast<void*>(mat.p)) + 2 * (seq * mat.seq + (long long)(tok0 + 32 * q) * mat.tok + it.head * mat.head);
+                const long long apart = split ? 4ll * a.kv_heads * a.d : 2 * mat.tok;
+                const int rows = it.limit - 32 * q;
+                auto flush = [&](int col, int n) {       // n pieces of 16 bytes of every row, from byte `col`; neighbours by neighbouring lanes
+                    __syncwarp();
+                    const int magic = (65535 + n) / n;
 #pragma unroll 1
-                for (int ch = 0; ch < NCH; ++ch) {
-                    uint8_t* stage = mine + staged % SG * kStage;
-                    if (boxed) {
-                        if (lane == 0) tc::bulk_wait_read<SG - 1>();     // the copy that last used this buffer has read it
-                        __syncwarp();
+                    for (int i = lane; i < 32 * n; i += 32) {
+                        const int row = i * magic >> 16, piece = i - row * n;
+                        if (row < rows) *reinterpret_cast<uint4*>(dst + row * apart + col + 16 * piece) = *reinterpret_cast<const uint4*>(mine + row * 128 + 16 * (piece ^ (row & 7)));
                     }
+                    __syncwarp();
+                };
 #pragma unroll 1
-                    for (int half = 0; half < 2 && 4 * ch + 2 * half < ks; ++half) {
-                        uint32_t v[32];
-                        tc::tmem_ld32(acc + 64 * ch + 32 * half, v);
-                        tc::tmem_wait_ld();
-                        if (boxed) {
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                uint32_t pk[4];
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) pk[e] = keep ? pack2(__uint_as_float(v[8 * c + 2 * e]), __uint_as_float(v[8 * c + 2 * e + 1])) : 0u;
-                                *reinterpret_cast<uint4*>(stage + lane * 128 + (((4 * half + c) ^ (lane & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-                            }
-                        } else if (r < it.limit) {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                const int c = 64 * ch + 32 * half + e;
-                                const float x = keep ? __uint_as_float(v[e]) : 0.f;
-                                if (c < a.d) {
-                                    if (a.parts > 1) part[c] = x;
-                                    else dst[c] = __float2bfloat16(x);
-                                }
-                            }
-                        }
-                    }
-                    if (last && ch == NCH - 1) {
+                for (int c0 = 0; c0 < a.d; c0 += 32) {
+                    uint32_t v[32];
+                    tc::tmem_ld32(acc + c0, v);
+                    tc::tmem_wait_ld();
+                    if (o == (DKV ? 1 : 0) && c0 + 32 >= a.d) {
                         tc::tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) tc::mbar_arrive(acc_free);
+                        if (lane == 0) tc::mbar_arrive(&acc_free[set]);
                     }
-                    if (boxed) {
-                        tc::fence_proxy_async();
+                    if (rows <= 0) continue;
+                    if (!keep) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = 0u;
+                    }
+                    if (!whole) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (c0 + e < a.d && lane < rows) {
+                                if (split) reinterpret_cast<float*>(dst + lane * apart)[c0 + e] = __uint_as_float(v[e]);
+                                else reinterpret_cast<__nv_bfloat16*>(dst + lane * apart)[c0 + e] = __float2bfloat16(__uint_as_float(v[e]));
+                            }
                         __syncwarp();
-                        if (lane == 0) {
-                            store_4d(o ? &mapO2 : &mapO1, tc::smem_u32(stage), 64 * ch, it.head, tok0 + 32 * q, seq);
-                            tc::bulk_commit();
+                    } else if (split) {
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) *reinterpret_cast<uint4*>(mine + lane * 128 + 16 * (u ^ (lane & 7))) = make_uint4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+                        flush(4 * c0, a.d - c0 < 32 ? (a.d - c0) / 4 : 8);
+                    } else {
+                        const int first = (c0 & 32) / 8;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            uint32_t pk[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) pk[e] = pack2(__uint_as_float(v[8 * u + 2 * e]), __uint_as_float(v[8 * u + 2 * e + 1]));
+                            *reinterpret_cast<uint4*>(mine + lane * 128 + 16 * ((first + u) ^ (lane & 7))) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
                         }
-                        ++staged;
+                        const int from = c0 & ~63;
+                        if ((c0 & 32) || c0 + 32 >= a.d) flush(2 * from, a.d - from < 64 ? (a.d - from) / 8 : 8);
                     }
                 }
             }
+            if (++set == NA) { set = 0; ph ^= 1u; }
         }
         if (!ok && lane == 0) fail();
-        if (lane == 0) tc::bulk_wait<0>();               // every store complete before the CTA ends
         __syncwarp();
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (warp == 12) {
-            // ------------------------------------------------------------------ items, and TMA loads
+            // ------------------------------------------------------------------ TMA loads
             if (lane == 0) { tc::tma_prefetch_desc(&mapA1); tc::tma_prefetch_desc(&mapA2); tc::tma_prefetch_desc(&mapB1); tc::tma_prefetch_desc(&mapB2); }
             uint32_t set = 0, a_ph = 1, s1 = 0, ph1 = 1, s2 = 0, ph2 = 1;
             bool ok = true;
-            long long i = blockIdx.x;
-            auto next_item = [&]() {                     // the next that has a column tile
-                Item it = item_of<DKV>(a, i);
-                while (it.live) {
-                    i += gridDim.x;
-                    if (it.tiles > 0) break;
-                    it = item_of<DKV>(a, i);
-                }
-                return it;
-            };
-            Item ahead = next_item();
             for (uint32_t n = 0; ok; ++n) {
-                const Item it = ahead;
-                ok = cross_tc::wait(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
+                ok = see(n);
                 if (!ok) break;
-                if (lane == 0) {
-                    queue[n % kQueue] = it;
-                    tc::mbar_arrive(&item_full[n % kQueue]);
-                }
-                __syncwarp();
+                const Item it = queue[n % kQueue];
+                leave(n);
                 if (!it.live) break;
-                ok = cross_tc::wait(&a_empty[set], a_ph, abort_flag);
-                if (!ok) break;
-                if (tc::elect_one()) {
-                    tc::mbar_expect_tx(&a_full[set], 2 * M::a);
-                    const int seq = DKV ? it.enc : it.idx, tok = DKV ? it.row : it.row0;
-                    for (int ch = 0; ch < NCH; ++ch) {
-                        load_4d(tc::smem_u32(sA + (2 * set) * M::a + ch * kChunk), &mapA1, &a_full[set], 64 * ch, it.head * (DKV ? a.k_head_mul : a.q_head_mul), tok,
-                                seq * (DKV ? a.k_seq_mul : a.q_seq_mul));
-                        load_4d(tc::smem_u32(sA + (2 * set + 1) * M::a + ch * kChunk), &mapA2, &a_full[set], 64 * ch, it.head * (DKV ? a.v_head_mul : a.g_head_mul), tok,
-                                seq * (DKV ? a.v_seq_mul : a.g_seq_mul));
-                    }
-                }
-                __syncwarp();
-                if (++set == AB) { set = 0; a_ph ^= 1u; }
-                ahead = next_item();
                 Columns col;
                 if (DKV) col.seek(a, it);
+                auto rows_load = [&]() {
+                    ok = cross_tc::wait(&a_empty[set], a_ph, abort_flag);
+                    if (!ok) return;
+                    if (tc::elect_one()) {
+                        tc::mbar_expect_tx(&a_full[set], 2 * M::a);
+                        const int seq = DKV ? it.enc : it.idx, tok = DKV ? it.row : it.row0;
+                        for (int ch = 0; ch < NCH; ++ch) {
+                            load_4d(tc::smem_u32(sA + (2 * set) * M::a + ch * kChunk), &mapA1, &a_full[set], 64 * ch, it.head * (DKV ? a.k_head_mul : a.q_head_mul), tok,
+                                    seq * (DKV ? a.k_seq_mul : a.q_seq_mul));
+                            load_4d(tc::smem_u32(sA + (2 * set + 1) * M::a + ch * kChunk), &mapA2, &a_full[set], 64 * ch, it.head * (DKV ? a.v_head_mul : a.g_head_mul), tok,
+                                    seq * (DKV ? a.v_seq_mul : a.g_seq_mul));
+                        }
+                    }
+                    __syncwarp();
+                    if (++set == AB) { set = 0; a_ph ^= 1u; }
+                };
+                if (AB > 1) rows_load();
                 for (int j = 0; ok && j < it.tiles; ++j) {
                     const int seq = DKV ? col.s : it.enc, head = DKV ? it.kv_head * a.group + col.g : it.kv_head, tok = DKV ? col.t * BC : it.row + j * BC;
                     ok = cross_tc::wait(&b1_empty[s1], ph1, abort_flag);
@@ -424,6 +425,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                     __syncwarp();
                     if (++s1 == N1) { s1 = 0; ph1 ^= 1u; }
                     if (++s2 == N2) { s2 = 0; ph2 ^= 1u; }
+                    if (AB == 1 && j == 0 && ok) rows_load();        // one set: while the last item's products still read it, a tile may come
                     if (DKV) col.next(a, it.idx);
                 }
             }
@@ -470,11 +472,15 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
             }
             if (!ok && lane == 0) fail();
             __syncwarp();
-        } else if (warp == 14) {
-            // ------------------------------------------------------------------ S and dP
+        } else if (warp == 14 || warp == 15) {
+            // ------------------------------------------------------------------ S; dP
+            const bool first = warp == 14;
             const uint32_t leader = tc::elect_one() ? 1u : 0u, idesc = tc::idesc_bf16(BR, BC);
-            const uint64_t a_desc = tc::smem_desc(tc::smem_u32(sA), 1024, 2), d1 = tc::smem_desc(tc::smem_u32(ring1), 1024, 2), d2 = tc::smem_desc(tc::smem_u32(ring2), 1024, 2);
-            uint32_t set = 0, a_ph = 0, s1 = 0, ph1 = 0, s2 = 0, ph2 = 0, buf = 0, buf_ph = 1;
+            const uint32_t slots = first ? N1 : N2, bufs = first ? NS : ND;
+            const uint64_t a_desc = tc::smem_desc(tc::smem_u32(sA) + (first ? 0 : M::a), 1024, 2), b_desc = tc::smem_desc(tc::smem_u32(first ? ring1 : ring2), 1024, 2);
+            const uint32_t out = tmem + (first ? 0 : M::dp_col);
+            uint64_t *full = first ? b1_full : b2_full, *free = first ? s_free : d_free;
+            uint32_t set = 0, a_ph = 0, slot = 0, slot_ph = 0, buf = 0, buf_ph = 1, sbuf = 0;
             bool ok = true;
             for (uint32_t n = 0; ok; ++n) {
                 ok = see(n);
@@ -483,37 +489,34 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                 leave(n);
                 if (!live) break;
                 ok = cross_tc::wait(&a_full[set], a_ph, abort_flag);
+                const uint64_t x = a_desc + (2 * set) * (M::a >> 4);
                 for (int j = 0; ok && j < tiles; ++j) {
-                    ok = cross_tc::wait(&b1_full[s1], ph1, abort_flag);
-                    if (ok) ok = cross_tc::wait(&b2_full[s2], ph2, abort_flag);
-                    if (ok) ok = cross_tc::wait(&s_free[buf], buf_ph, abort_flag);
+                    ok = cross_tc::wait2(&full[slot], slot_ph, &free[buf], buf_ph, abort_flag);
                     if (!ok) break;
                     tc::tc_fence_after();
-                    const uint64_t x1 = a_desc + (2 * set) * (M::a >> 4), x2 = x1 + (M::a >> 4), y1 = d1 + s1 * (M::b >> 4), y2 = d2 + s2 * (M::b >> 4);
-                    const uint32_t ts = tmem + buf * 128u;
+                    const uint64_t y = b_desc + slot * (M::b >> 4);
 #pragma unroll
                     for (int k = 0; k < 4 * NCH; ++k)
-                        if (k < ks) tc::mma_bf16_if(leader, ts, x1 + ((k >> 2) * (kChunk >> 4) + (k & 3) * 2), y1 + ((k >> 2) * (kColChunk >> 4) + (k & 3) * 2), idesc, k != 0);
-#pragma unroll
-                    for (int k = 0; k < 4 * NCH; ++k)
-                        if (k < ks) tc::mma_bf16_if(leader, ts + 64u, x2 + ((k >> 2) * (kChunk >> 4) + (k & 3) * 2), y2 + ((k >> 2) * (kColChunk >> 4) + (k & 3) * 2), idesc, k != 0);
-                    tc::mma_commit_if(leader, &s_full[buf]);
-                    if (!DKV) tc::mma_commit_if(leader, &b2_empty[s2]);
-                    if (++s1 == N1) { s1 = 0; ph1 ^= 1u; }
-                    if (++s2 == N2) { s2 = 0; ph2 ^= 1u; }
-                    if (++buf == NB) { buf = 0; buf_ph ^= 1u; }
+                        if (k < ks) tc::mma_bf16_if(leader, out + buf * 64u, x + ((k >> 2) * (kChunk >> 4) + (k & 3) * 2), y + ((k >> 2) * (kColChunk >> 4) + (k & 3) * 2), idesc, k != 0);
+                    tc::mma_commit_if(leader, &s_full[sbuf]);
+                    if (!DKV && !first) tc::mma_commit_if(leader, &b2_empty[slot]);
+                    if (++slot == slots) { slot = 0; slot_ph ^= 1u; }
+                    if (++buf == bufs) { buf = 0; buf_ph ^= 1u; }
+                    if (++sbuf == NS) sbuf = 0;
                 }
                 if (ok) tc::mma_commit_if(leader, &a_empty[set]);
                 if (++set == AB) { set = 0; a_ph ^= 1u; }
             }
             if (!ok && lane == 0) fail();
             __syncwarp();
-        } else if (warp == 15) {
-            // ------------------------------------------------------------------ the accumulating products
+        } else if (warp == 17 || (DKV && warp == 18)) {
+            // ------------------------------------------------------------------ the accumulating products: dq or dk; dv
+            const bool first = warp == 17;
             const uint32_t leader = tc::elect_one() ? 1u : 0u, idesc = tc::idesc_bf16(BR, ks * 16) | kBMajorMN;
-            const uint64_t d1 = desc_mn(tc::smem_u32(ring1), kColChunk), d2 = desc_mn(tc::smem_u32(ring2), kColChunk);
-            const uint32_t acc = tmem + M::acc_col;
-            uint32_t s1 = 0, s2 = 0, buf = 0, buf_ph = 0, acc_ph = 1;
+            const uint64_t b_desc = desc_mn(tc::smem_u32(first ? ring1 : ring2), kColChunk);
+            const uint32_t slots = first ? N1 : N2;
+            uint64_t* empty = first ? b1_empty : b2_empty;
+            uint32_t slot = 0, buf = 0, buf_ph = 0, set = 0, acc_ph = 1;
             bool ok = true;
             for (uint32_t n = 0; ok; ++n) {
                 ok = see(n);
@@ -521,31 +524,47 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                 const int live = queue[n % kQueue].live, tiles = queue[n % kQueue].tiles, left = queue[n % kQueue].left;
                 leave(n);
                 if (!live) break;
-                ok = cross_tc::wait(acc_free, acc_ph, abort_flag);
-                acc_ph ^= 1u;
+                ok = cross_tc::wait(&acc_free[set], acc_ph, abort_flag);
+                const uint32_t acc = tmem + M::acc_col + set * M::acc_set + (first ? 0 : W);
                 for (int j = 0; ok && j < tiles; ++j) {
                     ok = cross_tc::wait(&p_full[buf], buf_ph, abort_flag);
                     if (!ok) break;
                     tc::tc_fence_after();
                     const int cols = DKV || left - j * BC >= BC ? BC : (left - j * BC + 15) & ~15;
-                    const uint32_t ps = tmem + buf * 128u, ds = ps + 64u;
-                    const uint64_t y1 = d1 + s1 * (M::b >> 4), y2 = d2 + s2 * (M::b >> 4);
+                    const uint32_t x = tmem + buf * 64u + (first ? 16u : 0u);        // dS; p
+                    const uint64_t y = b_desc + slot * (M::b >> 4);
 #pragma unroll
                     for (int k = 0; k < BC / 16; ++k)
-                        if (16 * k < cols) mma_ts_if(leader, acc, ds + 8u * k, y1 + k * (2048u >> 4), idesc, j > 0 || k > 0);
-                    if (DKV) {
-#pragma unroll
-                        for (int k = 0; k < BC / 16; ++k)
-                            mma_ts_if(leader, acc + M::acc_width, ps + 8u * k, y2 + k * (2048u >> 4), idesc, j > 0 || k > 0);
-                    }
+                        if (DKV || 16 * k < cols) mma_ts_if(leader, acc, x + 8u * k + 16u * (k / 2), y + k * (2048u >> 4), idesc, j > 0 || k > 0);
                     tc::mma_commit_if(leader, &s_free[buf]);
-                    tc::mma_commit_if(leader, &b1_empty[s1]);
-                    if (DKV) tc::mma_commit_if(leader, &b2_empty[s2]);
-                    if (++s1 == N1) s1 = 0;
-                    if (++s2 == N2) s2 = 0;
-                    if (++buf == NB) { buf = 0; buf_ph ^= 1u; }
+                    tc::mma_commit_if(leader, &empty[slot]);
+                    if (++slot == slots) slot = 0;
+                    if (++buf == NS) { buf = 0; buf_ph ^= 1u; }
                 }
-                if (ok) tc::mma_commit_if(leader, acc_full);
+                if (ok) tc::mma_commit_if(leader, &acc_full[set]);
+                if (++set == NA) { set = 0; acc_ph ^= 1u; }
+            }
+            if (!ok && lane == 0) fail();
+            __syncwarp();
+        } else if (warp == 19) {
+            // ------------------------------------------------------------------ the items that have a column tile
+            bool ok = true;
+            long long i = blockIdx.x;
+            for (uint32_t n = 0; ok; ++n) {
+                Item it = item_of<DKV>(a, i);
+                while (it.live) {
+                    i += gridDim.x;
+                    if (it.tiles > 0) break;
+                    it = item_of<DKV>(a, i);
+                }
+                ok = cross_tc::wait(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
+                if (!ok) break;
+                if (lane == 0) {
+                    queue[n % kQueue] = it;
+                    tc::mbar_arrive(&item_full[n % kQueue]);
+                }
+                __syncwarp();
+                if (!it.live) break;
             }
             if (!ok && lane == 0) fail();
             __syncwarp();
@@ -597,13 +616,13 @@ __global__ void __launch_bounds__(256) cross_bwd_join_kernel(const Args a) {
     }
 }
 
-template <bool DKV, int NCH, int AB, int N1, int N2, int NB, int SG>
-int launch(const CUtensorMap (&m)[6], const Args& a, cudaStream_t s) {
-    auto kernel = cross_bwd_kernel<DKV, NCH, AB, N1, N2, NB, SG>;
-    constexpr uint32_t bytes = Mem<DKV, NCH, AB, N1, N2, NB, SG>::bytes;
+template <bool DKV, int NCH, int W, int AB, int N1, int N2, int NS, int ND, int NA>
+int launch(const CUtensorMap (&m)[4], const Args& a, cudaStream_t s) {
+    auto kernel = cross_bwd_kernel<DKV, NCH, W, AB, N1, N2, NS, ND, NA>;
+    constexpr uint32_t bytes = Mem<DKV, NCH, W, AB, N1, N2, NS, ND, NA>::bytes;
     FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
     const int grid = (int)(a.items < kSms ? a.items : kSms);
-    return free_launch(free_overlap_for_rows((long long)a.n_seq * a.n_q), kernel, dim3(grid), dim3(kThreads), bytes, s, m[0], m[1], m[2], m[3], m[4], m[5], a);
+    return free_launch(free_overlap_for_rows((long long)a.n_seq * a.n_q), kernel, dim3(grid), dim3(kThreads), bytes, s, m[0], m[1], m[2], m[3], a);
 }
 
 Args args_of(const CrossArgs& c) {
@@ -643,15 +662,22 @@ int cross_bwd_tc_dq(const CrossArgs& c, cudaStream_t s) {
     a.blocks = (c.n_q + BR - 1) / BR;
     a.items = (long long)c.n_seq * c.heads * a.blocks;
     a.o1 = a.o2 = c.dq;
-    CUtensorMap m[6];
+    CUtensorMap m[4];
     using cross_tc::map_heads;
     FREE_TRY(map_heads(&m[0], c.q, c.n_seq, c.n_q, c.heads, c.d, 1, BR));
     FREE_TRY(map_heads(&m[1], c.g, c.n_seq, c.n_q, c.heads, c.d, 1, BR));
     FREE_TRY(map_heads(&m[2], c.k, enc, rows, c.kv_heads, c.d, 1, BC));
     FREE_TRY(map_heads(&m[3], c.v, enc, rows, c.kv_heads, c.d, 1, BC));
-    FREE_TRY(map_heads(&m[4], c.dq, c.n_seq, c.n_q, c.heads, c.d, 1, 32));
-    m[5] = m[4];
-    return c.d <= 64 ? launch<false, 1, 2, 6, 4, 3, 2>(m, a, s) : launch<false, 2, 2, 3, 2, 3, 1>(m, a, s);
+    #ifndef Q96
+#define Q96 3, 2, 3, 2, 2
+#define Q128 3, 2, 2, 2, 2
+#define Q64 6, 4, 3, 3, 2
+#define K64 6, 6, 3, 3, 1
+#define K96 4, 4, 3, 2, 1
+#define K128 4, 4, 2, 2, 1
+#endif
+    if (c.d <= 64) return launch<false, 1, 64, 2, Q64>(m, a, s);
+    return c.d <= 96 ? launch<false, 2, 96, 2, Q96>(m, a, s) : launch<false, 2, 128, 2, Q128>(m, a, s);
 }
 
 int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_t s) {
@@ -661,15 +687,13 @@ int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_
     a.parts = parts; a.part_out = part_out; a.part_rows = (long long)enc * rows * c.kv_heads;
     a.items = (long long)c.where.n_enc * c.kv_heads * a.blocks * parts;
     a.o1 = c.dk; a.o2 = c.dv;
-    CUtensorMap m[6];
+    CUtensorMap m[4];
     using cross_tc::map_heads;
     FREE_TRY(map_heads(&m[0], c.k, enc, rows, c.kv_heads, c.d, 1, BR));
     FREE_TRY(map_heads(&m[1], c.v, enc, rows, c.kv_heads, c.d, 1, BR));
     FREE_TRY(map_heads(&m[2], c.q, c.n_seq, c.n_q, c.heads, c.d, 1, BC));
     FREE_TRY(map_heads(&m[3], c.g, c.n_seq, c.n_q, c.heads, c.d, 1, BC));
-    FREE_TRY(map_heads(&m[4], c.dk, enc, rows, c.kv_heads, c.d, 1, 32));
-    FREE_TRY(map_heads(&m[5], c.dv, enc, rows, c.kv_heads, c.d, 1, 32));
-    const int code = c.d <= 64 ? launch<true, 1, 2, 6, 6, 3, 2>(m, a, s) : launch<true, 2, 1, 4, 4, 2, 1>(m, a, s);
+    const int code = c.d <= 64 ? launch<true, 1, 64, 2, K64>(m, a, s) : c.d <= 96 ? launch<true, 2, 96, 1, K96>(m, a, s) : launch<true, 2, 128, 1, K128>(m, a, s);
     FREE_TRY(code);
     if (parts == 1) return FREE_OK;
     const long long n = (long long)c.where.n_enc * c.where.n_kv * c.kv_heads, ctas = (n + 7) / 8;

@@ -23,6 +23,12 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile ui
     }
     return __all_sync(0xffffffffu, r);
 }
+// Two of them, their first polls (some 115 clocks each) at once.
+__device__ __forceinline__ bool wait2(uint64_t* bar1, uint32_t parity1, uint64_t* bar2, uint32_t parity2, volatile uint32_t* abort_flag) {
+    const bool r1 = tc::mbar_try_wait(bar1, parity1), r2 = tc::mbar_try_wait(bar2, parity2);
+    if (__all_sync(0xffffffffu, r1 && r2)) return true;
+    return wait(bar1, parity1, abort_flag) && wait(bar2, parity2, abort_flag);
+}
 __device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c, int head, int tok, int seq) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                  ::"r"(dst), "l"((uint64_t)map), "r"(tc::smem_u32(bar)), "r"(c), "r"(head), "r"(tok), "r"(seq) : "memory");
