@@ -50,6 +50,7 @@ struct CrossArgs {
     float scale;
     float* lse;                               // [n_seq, heads, n_q]
     float* delta;                             // backward: <dout, out>, laid out as lse
+    unsigned long long* next;                           // backward: a counter that the kernel of delta sets to zero
     uint32_t* err;
 };
 

@@ -86,6 +86,7 @@ size_t part_bytes(const free_cross_attn* c, int parts) { return parts > 1 ? free
 size_t sum_bytes(const free_cross_attn* c, int parts) {
     return parts > 1 ? (size_t)parts * 2 * (c->kv_offsets ? 1 : c->n_enc) * (c->kv_offsets ? c->kv_rows : c->n_kv) * c->kv_heads * c->d_head * 4 : 0;
 }
+constexpr size_t kNextBytes = 256;
 size_t stat_bytes(const free_cross_attn* c) { return free_round_up((size_t)c->n_seq * c->heads * c->n_q * 4, 256); }
 
 }  // namespace
@@ -131,7 +132,7 @@ extern "C" size_t free_op_cross_attention_bwd_workspace_bytes(const free_cross_a
     if (check(c, &empty) != FREE_OK || empty) return 0;
     CrossArgs a = args_of(c);
     a.g = a.q;
-    return stat_bytes(c) + (c->dtype == FREE_BF16 && cross_bwd_tc_supported(a) ? sum_bytes(c, cross_bwd_tc_parts(a)) : 0);
+    return stat_bytes(c) + kNextBytes + (c->dtype == FREE_BF16 && cross_bwd_tc_supported(a) ? sum_bytes(c, cross_bwd_tc_parts(a)) : 0);
 }
 
 extern "C" int free_op_cross_attention_bwd(const free_cross_attn* c, const void* out, int64_t o_seq, int64_t o_tok, int64_t o_head, const float* lse,
@@ -167,14 +168,14 @@ extern "C" int free_op_cross_attention_bwd(const free_cross_attn* c, const void*
     a.dq = CrossMat{dq, dq_seq, dq_tok, dq_head};
     a.dk = CrossMat{dk, c->kv_offsets ? 0 : dk_seq, dk_tok, dk_head};
     a.dv = CrossMat{dv, c->kv_offsets ? 0 : dv_seq, dv_tok, dv_head};
-    a.lse = const_cast<float*>(lse); a.delta = (float*)ws; a.err = device_error;
+    a.lse = const_cast<float*>(lse); a.delta = (float*)ws; a.next = (unsigned long long*)((char*)ws + stat_bytes(c)); a.err = device_error;
     if (!empty && (dq || dk)) FREE_TRY(cross_delta(c->dtype, a, s));
     // the tensor cores where the tile copies take every matrix (an empty call only writes zeros)
     const bool tc = c->dtype == FREE_BF16 && !empty && cross_bwd_tc_supported(a);
     if (!empty && dq) FREE_TRY(tc && cross_tc::mappable(a.dq, c->n_seq, c->n_q, c->heads) ? cross_bwd_tc_dq(a, s) : cross_simt_dq(c->dtype, a, s));
     if (dk && states(c)) {
         if (tc && cross_tc::mappable(a.dk, enc, rows, c->kv_heads) && cross_tc::mappable(a.dv, enc, rows, c->kv_heads))
-            FREE_TRY(cross_bwd_tc_dkv(a, cross_bwd_tc_parts(a), (float*)((char*)ws + stat_bytes(c)), s));
+            FREE_TRY(cross_bwd_tc_dkv(a, cross_bwd_tc_parts(a), (float*)((char*)ws + stat_bytes(c) + kNextBytes), s));
         else
             FREE_TRY(cross_simt_dkv(c->dtype, a, s));
     }

@@ -24,11 +24,12 @@ constexpr int kThreads = 640, kSms = 148;     // warps 0 - 7 elementwise, 8 - 11
 constexpr int kMathRegs = 136, kOtherRegs = 64;
 static_assert(256 * kMathRegs + 384 * kOtherRegs <= kThreads * 96, "registers of the launch");
 constexpr uint32_t kChunk = BR * 128, kColChunk = BC * 128;
-constexpr uint32_t kQueue = 4, kStage = 32 * 128;     // staging: 128 bytes of 32 rows, pieces of 16 swizzled
+constexpr uint32_t kStage = 32 * 128;     // staging: 128 bytes of 32 rows, pieces of 16 swizzled
 
 // NCH: chunks of 64 channels; W: columns of tensor memory per sum; AB: sets of the rows' operands; N1, N2: ring slots of the columns'
 // operands; NS, ND: buffers of S (p and dS go over it) and of dP (free once read); NA: sets of sums
 template <bool DKV, int NCH, int W, int AB, int N1, int N2, int NS, int ND, int NA> struct Mem {
+    static constexpr uint32_t queue = DKV ? 2 : 4;        // items
     static constexpr uint32_t a = NCH * kChunk, b = NCH * kColChunk;
     static constexpr uint32_t ctrl = 1024 + (DKV ? N1 * BC * 8 : 0);
     static constexpr uint32_t ctrl_bytes = (ctrl + 1023) / 1024 * 1024;
@@ -36,7 +37,7 @@ template <bool DKV, int NCH, int W, int AB, int N1, int N2, int NS, int ND, int 
     static constexpr uint32_t dp_col = NS * 64, acc_col = (NS + ND) * 64, acc_set = (DKV ? 2 : 1) * W;
     static_assert(acc_col + NA * acc_set <= 512, "tensor memory of an SM");
     static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
-    static_assert((2 * AB + 2 * N1 + 2 * N2 + 3 * NS + ND + 2 * NA + 2 * kQueue + 1) * 8 <= 512, "barriers");
+    static_assert((2 * AB + 2 * N1 + 2 * N2 + 3 * NS + ND + 2 * NA + 2 * queue + 1) * 8 <= 512, "barriers");
 };
 
 struct Args {
@@ -50,6 +51,7 @@ struct Args {
     CrossMat o1, o2;                          // results: dq, or dk and dv
     float* part_out;                          // [part][2][encoder row][key head][d]
     long long part_rows;
+    unsigned long long* next;                 // dk, dv: the next item that no CTA has
     uint32_t* err;
 };
 
@@ -132,6 +134,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constant__ CUtensorMap mapA2, const __grid_constant__ CUtensorMap mapB1,
                  const __grid_constant__ CUtensorMap mapB2, const Args a) {
     using M = Mem<DKV, NCH, W, AB, N1, N2, NS, ND, NA>;
+    constexpr uint32_t kQueue = M::queue;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t* a_full = reinterpret_cast<uint64_t*>(smem);
@@ -221,7 +224,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                     tc::tc_fence_after();
                     const uint32_t ts = lanes + buf * 64u, td = lanes + M::dp_col + dbuf * 64u;
                     const ulonglong2 *cl = reinterpret_cast<const ulonglong2*>(stats + slot * 2 * BC), *cd = cl + BC / 4;
-#pragma unroll
+#pragma unroll 1                                                         // (half the code: instructions come in time)
                     for (int h = 0; h < 2; ++h) {
                         uint32_t s[32], d[32], ps[16], ds[16];
                         tc::tmem_ld32(ts + 32 * h, s);
@@ -304,27 +307,43 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
             const uint8_t* mask = a.where.mask ? a.where.mask + (a.where.offsets ? 0 : (long long)it.enc * a.where.n_kv) + it.row : nullptr;
             const bool keep = !DKV || (r < it.left && (!mask || mask[r] != 0));    // states that do not count: zeros, whatever the sums are
             const int seq = DKV ? it.enc : it.idx, tok0 = DKV ? it.row : it.row0;
+            const bool split = a.parts > 1, whole = a.d % (split ? 4 : 8) == 0;
+            const int rows = it.limit - 32 * q;
+            // the warp's first row of either result, and how far rows lie apart
+            uint8_t* dst[DKV ? 2 : 1];
+            long long apart[DKV ? 2 : 1];
+#pragma unroll
+            for (int o = 0; o < (DKV ? 2 : 1); ++o) {
+                const CrossMat& mat = o ? a.o2 : a.o1;
+                dst[o] = split ? reinterpret_cast<uint8_t*>(a.part_out + (((long long)it.part * 2 + o) * a.part_rows +
+                                                                          ((long long)seq * a.where.kv_rows + tok0 + 32 * q) * a.kv_heads + it.head) * a.d) :
+                                 reinterpret_cast<uint8_t*>(const_cast<void*>(mat.p)) + 2 * (seq * mat.seq + (long long)(tok0 + 32 * q) * mat.tok + it.head * mat.head);
+                apart[o] = split ? 4ll * a.kv_heads * a.d : 2 * mat.tok;
+            }
             ok = cross_tc::wait(&acc_full[set], ph, abort_flag);
             if (!ok) break;
             tc::tc_fence_after();
-#pragma unroll 1
+#pragma unroll
             for (int o = 0; o < (DKV ? 2 : 1); ++o) {
                 const uint32_t acc = tmem + M::acc_col + set * M::acc_set + o * W + ((uint32_t)(q * 32) << 16);
-                const CrossMat& mat = o ? a.o2 : a.o1;
-                const bool split = a.parts > 1, whole = a.d % (split ? 4 : 8) == 0;
-                // the warp's first row, and how far rows lie apart
-                uint8_t* dst = split ? reinterpret_cast<uint8_t*>(a.part_out + (((long long)it.part * 2 + o) * a.part_rows +
-                                                                                ((long long)seq * a.where.kv_rows + tok0 + 32 * q) * a.kv_heads + it.head) * a.d) :
-                                       reinterpret_cast<uint8_t*>(const_cast<void*>(mat.p)) + 2 * (seq * mat.seq + (long long)(tok0 + 32 * q) * mat.tok + it.head * mat.head);
-                const long long apart = split ? 4ll * a.kv_heads * a.d : 2 * mat.tok;
-                const int rows = it.limit - 32 * q;
                 auto flush = [&](int col, int n) {       // n pieces of 16 bytes of every row, from byte `col`; neighbours by neighbouring lanes
                     __syncwarp();
-                    const int magic = (65535 + n) / n;
+                    if (n == 8) {
+                        uint8_t* to = dst[o] + (lane >> 3) * apart[o] + col + 16 * (lane & 7);
+                        const uint8_t* from = mine + (lane >> 3) * 128;
+                        uint4 v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const uint4*>(from + i * 512 + 16 * ((lane & 7) ^ (lane >> 3) ^ (4 * (i & 1))));
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (4 * i + (lane >> 3) < rows) *reinterpret_cast<uint4*>(to + 4 * i * apart[o]) = v[i];
+                    } else {
+                        const int magic = (65535 + n) / n;
 #pragma unroll 1
-                    for (int i = lane; i < 32 * n; i += 32) {
-                        const int row = i * magic >> 16, piece = i - row * n;
-                        if (row < rows) *reinterpret_cast<uint4*>(dst + row * apart + col + 16 * piece) = *reinterpret_cast<const uint4*>(mine + row * 128 + 16 * (piece ^ (row & 7)));
+                        for (int i = lane; i < 32 * n; i += 32) {
+                            const int row = i * magic >> 16, piece = i - row * n;
+                            if (row < rows) *reinterpret_cast<uint4*>(dst[o] + row * apart[o] + col + 16 * piece) = *reinterpret_cast<const uint4*>(mine + row * 128 + 16 * (piece ^ (row & 7)));
+                        }
                     }
                     __syncwarp();
                 };
@@ -347,8 +366,8 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
                             if (c0 + e < a.d && lane < rows) {
-                                if (split) reinterpret_cast<float*>(dst + lane * apart)[c0 + e] = __uint_as_float(v[e]);
-                                else reinterpret_cast<__nv_bfloat16*>(dst + lane * apart)[c0 + e] = __float2bfloat16(__uint_as_float(v[e]));
+                                if (split) reinterpret_cast<float*>(dst[o] + lane * apart[o])[c0 + e] = __uint_as_float(v[e]);
+                                else reinterpret_cast<__nv_bfloat16*>(dst[o] + lane * apart[o])[c0 + e] = __float2bfloat16(__uint_as_float(v[e]));
                             }
                         __syncwarp();
                     } else if (split) {
@@ -550,14 +569,23 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
             // ------------------------------------------------------------------ the items that have a column tile
             bool ok = true;
             long long i = blockIdx.x;
-            for (uint32_t n = 0; ok; ++n) {
-                Item it = item_of<DKV>(a, i);
-                while (it.live) {
-                    i += gridDim.x;
-                    if (it.tiles > 0) break;
-                    it = item_of<DKV>(a, i);
+            auto next_item = [&]() {
+                if (DKV) {
+                    unsigned long long v = 0;
+                    if (lane == 0) v = atomicAdd(a.next, 1ull);
+                    i = (long long)__shfl_sync(0xffffffffu, v, 0);
                 }
-                ok = cross_tc::wait(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
+                const Item it = item_of<DKV>(a, i);
+                if (!DKV) i += gridDim.x;
+                return it;
+            };
+            for (uint32_t n = 0; ok; ++n) {
+                // dk, dv: no sooner than the item before is begun, so that the CTAs end together
+                if (DKV) ok = cross_tc::wait(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
+                if (!ok) break;
+                Item it = next_item();
+                while (it.live && it.tiles == 0) it = next_item();
+                if (!DKV) ok = cross_tc::wait(&item_free[n % kQueue], (n / kQueue & 1u) ^ 1u, abort_flag);
                 if (!ok) break;
                 if (lane == 0) {
                     queue[n % kQueue] = it;
@@ -574,16 +602,15 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                 const Item it = item_of<DKV>(a, i);
                 if (it.tiles > 0) continue;
                 const int rows = it.limit < BR ? it.limit : BR, seq = DKV ? it.enc : it.idx, tok0 = DKV ? it.row : it.row0;
-                for (int r = 0; r < rows; ++r)
-                    for (int o = 0; o < (DKV ? 2 : 1); ++o) {
-                        const CrossMat& mat = o ? a.o2 : a.o1;
-                        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(mat.p)) + seq * mat.seq + (long long)(tok0 + r) * mat.tok + it.head * mat.head;
-                        float* part = a.part_out + (((long long)it.part * 2 + o) * a.part_rows + ((long long)seq * a.where.kv_rows + tok0 + r) * a.kv_heads + it.head) * a.d;
-                        for (int c = lane; c < a.d; c += 32) {
-                            if (a.parts > 1) part[c] = 0.f;
-                            else dst[c] = __float2bfloat16(0.f);
-                        }
-                    }
+                for (int o = 0; o < (DKV ? 2 : 1); ++o) {
+                    const CrossMat& mat = o ? a.o2 : a.o1;
+                    if (a.parts > 1)
+                        zero_rows(a.part_out + (((long long)it.part * 2 + o) * a.part_rows + ((long long)seq * a.where.kv_rows + tok0) * a.kv_heads + it.head) * a.d, 4ll * a.kv_heads * a.d,
+                                  rows, 4 * a.d, lane);
+                    else
+                        zero_rows(reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(mat.p)) + seq * mat.seq + (long long)tok0 * mat.tok + it.head * mat.head, 2 * mat.tok, rows,
+                                  2 * a.d, lane);
+                }
             }
         }
     }
@@ -686,6 +713,7 @@ int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_
     a.blocks = (c.where.n_kv + BR - 1) / BR;
     a.parts = parts; a.part_out = part_out; a.part_rows = (long long)enc * rows * c.kv_heads;
     a.items = (long long)c.where.n_enc * c.kv_heads * a.blocks * parts;
+    a.next = c.next;
     a.o1 = c.dk; a.o2 = c.dv;
     CUtensorMap m[4];
     using cross_tc::map_heads;

@@ -189,6 +189,7 @@ template <typename E, int V, int L> __global__ void __launch_bounds__(256) cross
     constexpr int R = V == 1 ? 1 : 4, P = V == 1 ? kCrossMaxD / L : 1;        // pieces of a lane
     free_grid_dep_wait();
     free_grid_dep_launch();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.next = 0;
     const long long rows = (long long)a.n_seq * a.n_q * a.heads;
     const int lane = threadIdx.x % L, groups = (int)(gridDim.x * (256 / L)), step_t = groups / a.heads, step_h = groups % a.heads;
     long long i = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
@@ -223,6 +224,44 @@ template <typename E, int V, int L> __global__ void __launch_bounds__(256) cross
 #pragma unroll
             for (int k = L / 2; k > 0; k >>= 1) v += __shfl_xor_sync(mates, v, k);
             if (lane == 0 && out[r] >= 0) a.delta[out[r]] = v;
+        }
+    }
+}
+
+// The same of matrices without gaps: a warp takes 32 rows and reads their pieces of 16 bytes in the order of memory; the pieces' sums meet
+// in shared memory, where each lane adds those of a row.
+template <typename E> __global__ void __launch_bounds__(256) cross_delta_dense_kernel(const CrossArgs a) {
+    constexpr int V = 16 / (int)sizeof(E), kMost = kCrossMaxD / V;
+    __shared__ float part[8][32 * (kMost + 1)];
+    free_grid_dep_wait();
+    free_grid_dep_launch();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.next = 0;
+    const int lane = threadIdx.x & 31, units = a.d / V, pitch = units | 1, magic = (65535 + units) / units;
+    const long long rows = (long long)a.n_seq * a.n_q * a.heads;
+    float* mine = part[threadIdx.x >> 5];
+    for (long long i0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * 32; i0 < rows; i0 += (long long)gridDim.x * 256) {
+        const E *g = static_cast<const E*>(a.g.p) + i0 * a.d, *o = static_cast<const E*>(a.o.p) + i0 * a.d;
+        const int n = (int)(rows - i0 < 32 ? rows - i0 : 32) * units;
+#pragma unroll 4
+        for (int x = lane; x < 32 * units; x += 32) {
+            Chunk<E, V> cg, co;
+            cg.load(g + (long long)x * V, x < n);
+            co.load(o + (long long)x * V, x < n);
+            float v = 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) v = fmaf(to_f(cg.v[e]), to_f(co.v[e]), v);
+            const int row = x * magic >> 16;
+            mine[row * pitch + x - row * units] = v;
+        }
+        __syncwarp();
+        float v = 0.f;
+        for (int u = 0; u < units; ++u) v += mine[lane * pitch + u];
+        __syncwarp();
+        const long long i = i0 + lane;
+        if (i < rows) {
+            const int h = (int)(i % a.heads);
+            const long long st = i / a.heads;
+            a.delta[(st / a.n_q * a.heads + h) * a.n_q + st % a.n_q] = v;
         }
     }
 }
@@ -371,6 +410,13 @@ template <typename E> int delta_of(const CrossArgs& a, cudaStream_t s) {
     for (const CrossMat* m : {&a.g, &a.o}) wide = wide && free_aligned16(m->p) && m->seq % V == 0 && m->tok % V == 0 && m->head % V == 0;
     if (!wide) return start_delta<E, 1, 32>(a, s);
     const int units = a.d / V;
+    bool dense = true;
+    for (const CrossMat* m : {&a.g, &a.o})
+        dense = dense && (a.heads == 1 || m->head == a.d) && (a.n_q == 1 || m->tok == (long long)a.heads * a.d) && (a.n_seq == 1 || m->seq == (long long)a.n_q * a.heads * a.d);
+    if (dense) {
+        const long long ctas = ((long long)a.n_seq * a.n_q * a.heads + 255) / 256;
+        return free_launch(free_overlap_for_rows((long long)a.n_seq * a.n_q), cross_delta_dense_kernel<E>, dim3((unsigned)(ctas < 148 * 6 ? ctas : 148 * 6)), dim3(256), 0, s, a);
+    }
     return units <= 8 ? start_delta<E, V, 8>(a, s) : units <= 16 ? start_delta<E, V, 16>(a, s) : start_delta<E, V, 32>(a, s);
 }
 

@@ -508,16 +508,12 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 const Item it = item_of(a, i);
                 if (it.nb > 0) continue;
                 const int last = it.t0 + it.tiles * a.tt < a.n_q ? it.t0 + it.tiles * a.tt : a.n_q;
-                for (int t = it.t0; t < last; ++t)
-                    for (int h = it.kh * a.group; h < (it.kh + 1) * a.group; ++h) {
-                        const long long row = ((long long)it.s * a.heads + h) * a.n_q + t;
-                        if (lane == 0) {
-                            if (a.parts > 1) a.part_lse[it.part * a.rows + row] = -INFINITY;
-                            else if (a.lse) a.lse[row] = -INFINITY;
-                        }
-                        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(a.o.p)) + it.s * a.o.seq + t * a.o.tok + h * a.o.head;
-                        for (int c = lane; a.parts == 1 && c < a.d; c += 32) out[c] = __float2bfloat16(0.f);
-                    }
+                for (int h = it.kh * a.group; h < (it.kh + 1) * a.group; ++h) {
+                    float* lse = a.parts > 1 ? a.part_lse + it.part * a.rows : a.lse;
+                    for (int t = it.t0 + lane; lse && t < last; t += 32) lse[((long long)it.s * a.heads + h) * a.n_q + t] = -INFINITY;
+                    if (a.parts == 1)
+                        zero_rows(reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(a.o.p)) + it.s * a.o.seq + it.t0 * a.o.tok + h * a.o.head, 2 * a.o.tok, last - it.t0, 2 * a.d, lane);
+                }
             }
         }
     }

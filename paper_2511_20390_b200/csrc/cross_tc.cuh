@@ -72,6 +72,18 @@ template <int WORDS> __device__ __forceinline__ void count_bits(uint32_t (&w)[WO
     }
 }
 
+// Zeros into rows of `bytes` bytes, `apart` bytes from one to the next; whole warp.  Rows of whole pieces of 16 bytes are aligned to them.
+__device__ __forceinline__ void zero_rows(void* p, long long apart, int rows, int bytes, int lane) {
+    uint8_t* to = static_cast<uint8_t*>(p);
+    const bool wide = bytes % 16 == 0;
+    const int n = bytes / (wide ? 16 : 2);
+    for (int r = lane / n, c = lane % n; r < rows;) {
+        if (wide) *reinterpret_cast<uint4*>(to + r * apart + 16 * c) = make_uint4(0u, 0u, 0u, 0u);
+        else *reinterpret_cast<uint16_t*>(to + r * apart + 2 * c) = 0;
+        for (c += 32; c >= n; c -= n) ++r;
+    }
+}
+
 // ---- host -----------------------------------------------------------------------------------------------------------------
 // bf16 heads [seq][tok][head][d] as a tensor map whose boxes are 64 channels x `heads_box` heads x `tok_box` tokens (128-byte
 // swizzle; zero outside).  Dimensions of one element and strides of zero (a matrix that several share) become dimensions of one:
