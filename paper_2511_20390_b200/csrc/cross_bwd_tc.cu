@@ -9,9 +9,14 @@
 // accumulate.  Transposing the problem for dk and dv (rows are states) leaves every operand as it lies in memory: a column tile serves
 // as K-major operand of S or dP and, read along its rows, as operand of the accumulation.
 // Persistent CTAs, one per SM: two warpgroups for the elementwise part, a column tile each in turn; one that writes results; a warp that
-// finds items and loads tiles; one that brings the tokens' lse and delta (dk, dv); one each that issues S, dP and the accumulating
-// products, in order, so that sums have a fixed order.  Nothing is added atomically; S and dP are formed twice instead (once here, once
-// for the other direction).
+// finds items (dk, dv: takes the next as its CTA comes free; 24 x 1024 tokens of 16 heads of 72 leave some SMs seven blocks of states and
+// others four where they are dealt out), one that loads tiles, one that brings the tokens' lse and delta (dk, dv); one each that issues S,
+// dP and either accumulating product, in order, so that sums have a fixed order whichever CTA forms them.  Nothing is added atomically; S
+// and dP are formed twice instead (once here, once for the other direction).
+// What bounds it: the way of a tile through the warps.  Those 24 x 1024 tokens take 92 us for dq and 107 for dk, dv; the tensor cores
+// work for 20% of that, the exponentials' unit for 22%; a tile's elementwise part takes 1300 to 2000 clocks, its copies 2300 when they
+// compete with a block of rows, a wait 115 when it is over already.  Before S, dP, dk and dv had a warp each, and dP its own tensor memory,
+// free once it is read: 95 and 160.
 // States that do not count: p and dS are replaced by zeros, and (dq) their rows of K zeroed in shared memory, for 0 x NaN is NaN.
 #include "cross_tc.cuh"
 
@@ -695,16 +700,10 @@ int cross_bwd_tc_dq(const CrossArgs& c, cudaStream_t s) {
     FREE_TRY(map_heads(&m[1], c.g, c.n_seq, c.n_q, c.heads, c.d, 1, BR));
     FREE_TRY(map_heads(&m[2], c.k, enc, rows, c.kv_heads, c.d, 1, BC));
     FREE_TRY(map_heads(&m[3], c.v, enc, rows, c.kv_heads, c.d, 1, BC));
-    #ifndef Q96
-#define Q96 3, 2, 3, 2, 2
-#define Q128 3, 2, 2, 2, 2
-#define Q64 6, 4, 3, 3, 2
-#define K64 6, 6, 3, 3, 1
-#define K96 4, 4, 3, 2, 1
-#define K128 4, 4, 2, 2, 1
-#endif
-    if (c.d <= 64) return launch<false, 1, 64, 2, Q64>(m, a, s);
-    return c.d <= 96 ? launch<false, 2, 96, 2, Q96>(m, a, s) : launch<false, 2, 128, 2, Q128>(m, a, s);
+    // two sets of sums, so that results leave while the next item's are formed (24 x 1024 tokens of 16 heads of 72: 92 us; one set and a
+    // third buffer of dP 95)
+    if (c.d <= 64) return launch<false, 1, 64, 2, 6, 4, 3, 3, 2>(m, a, s);
+    return c.d <= 96 ? launch<false, 2, 96, 2, 3, 2, 3, 2, 2>(m, a, s) : launch<false, 2, 128, 2, 3, 2, 2, 2, 2>(m, a, s);
 }
 
 int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_t s) {
@@ -721,7 +720,9 @@ int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_
     FREE_TRY(map_heads(&m[1], c.v, enc, rows, c.kv_heads, c.d, 1, BR));
     FREE_TRY(map_heads(&m[2], c.q, c.n_seq, c.n_q, c.heads, c.d, 1, BC));
     FREE_TRY(map_heads(&m[3], c.g, c.n_seq, c.n_q, c.heads, c.d, 1, BC));
-    const int code = c.d <= 64 ? launch<true, 1, 64, 2, K64>(m, a, s) : c.d <= 96 ? launch<true, 2, 96, 1, K96>(m, a, s) : launch<true, 2, 128, 1, K128>(m, a, s);
+    // (heads of 72 with two buffers of S instead of three: 116 us for 107; with five and three slots of the ring for four each 114)
+    const int code = c.d <= 64 ? launch<true, 1, 64, 2, 6, 6, 3, 3, 1>(m, a, s) : c.d <= 96 ? launch<true, 2, 96, 1, 4, 4, 3, 2, 1>(m, a, s) :
+                                 launch<true, 2, 128, 1, 4, 4, 2, 2, 1>(m, a, s);
     FREE_TRY(code);
     if (parts == 1) return FREE_OK;
     const long long n = (long long)c.where.n_enc * c.where.n_kv * c.kv_heads, ctas = (n + 7) / 8;
