@@ -25,10 +25,10 @@ int check(const free_cross_attn* c, bool* empty) {
 }
 bool states(const free_cross_attn* c) { return c->n_enc > 0 && c->n_kv > 0 && (!c->kv_offsets || c->kv_rows > 0); }
 
-int pointers(const free_cross_attn* c) {
+int pointers(const free_cross_attn* c, bool tokens) {              // (a call without tokens reads the states still: which of them count)
     const int e = c->dtype == FREE_FP32 ? 4 : 2;
-    if (!c->q || (states(c) && (!c->k || !c->v))) return FREE_ERR_ARG;
-    if (!aligned(c->q, e) || !aligned(c->k, e) || !aligned(c->v, e)) return FREE_ERR_ALIGN;
+    if ((tokens && !c->q) || (states(c) && (!c->k || !c->v))) return FREE_ERR_ARG;
+    if ((tokens && !aligned(c->q, e)) || !aligned(c->k, e) || !aligned(c->v, e)) return FREE_ERR_ALIGN;
     if (!aligned(c->kv_lens, 4) || !aligned(c->kv_offsets, 4) || !aligned(c->kv_seq, 4)) return FREE_ERR_ALIGN;
     return FREE_OK;
 }
@@ -107,7 +107,7 @@ extern "C" int free_op_cross_attention(const free_cross_attn* c, void* out, int6
     bool empty;
     FREE_TRY(check(c, &empty));
     if (empty) return FREE_OK;
-    FREE_TRY(pointers(c));
+    FREE_TRY(pointers(c, true));
     FREE_TRY(result(out, c->dtype == FREE_FP32 ? 4 : 2, o_seq, o_tok, o_head, c->n_seq, c->n_q, c->heads, c->d_head));
     if (!aligned(lse, 4)) return FREE_ERR_ALIGN;
     if (c->dtype == FREE_BF16 && !device_error) return FREE_ERR_ARG;
@@ -148,11 +148,12 @@ extern "C" int free_op_cross_attention_bwd(const free_cross_attn* c, const void*
     if (!dk != !dv) return FREE_ERR_ARG;
     const int enc = c->kv_offsets ? 1 : c->n_enc, rows = c->kv_offsets ? c->kv_rows : c->n_kv;
     if (dk && states(c)) {
+        FREE_TRY(pointers(c, !empty));
         FREE_TRY(result(dk, e, c->kv_offsets ? 0 : dk_seq, dk_tok, dk_head, enc, rows, c->kv_heads, c->d_head));
         FREE_TRY(result(dv, e, c->kv_offsets ? 0 : dv_seq, dv_tok, dv_head, enc, rows, c->kv_heads, c->d_head));
     }
     if (!empty) {
-        FREE_TRY(pointers(c));
+        FREE_TRY(pointers(c, true));
         if (!out || !lse || !dout) return FREE_ERR_ARG;
         if (!aligned(out, e) || !aligned(dout, e) || !aligned(lse, 4)) return FREE_ERR_ALIGN;
         for (long long v : {o_seq, o_tok, o_head, g_seq, g_tok, g_head})

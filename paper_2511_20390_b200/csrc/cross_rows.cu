@@ -261,7 +261,7 @@ template <typename E> int rows_of(const CrossArgs& a, const CrossParts& parts, c
 
 // Whole 16-byte units of K and V, and few rows
 bool cross_rows_supported(int dtype, const CrossArgs& a) {
-    if ((long long)a.n_q * a.group > 8) return false;
+    if ((long long)a.n_q * a.group > 8 || a.where.n_kv < 1) return false;
     const int v = dtype == FREE_FP32 ? 4 : 8;
     bool ok = a.d % v == 0;
     for (const CrossMat* m : {&a.k, &a.v}) ok = ok && free_aligned16(m->p) && m->seq % v == 0 && m->tok % v == 0 && m->head % v == 0;

@@ -230,9 +230,9 @@ template <typename E, int V, int L> __global__ void __launch_bounds__(256) cross
 
 // The same of matrices without gaps: a warp takes 32 rows and reads their pieces of 16 bytes in the order of memory; the pieces' sums meet
 // in shared memory, where each lane adds those of a row.
-template <typename E> __global__ void __launch_bounds__(256) cross_delta_dense_kernel(const CrossArgs a) {
-    constexpr int V = 16 / (int)sizeof(E), kMost = kCrossMaxD / V;
-    __shared__ float part[8][32 * (kMost + 1)];
+template <typename E, int L> __global__ void __launch_bounds__(256) cross_delta_dense_kernel(const CrossArgs a) {
+    constexpr int V = 16 / (int)sizeof(E);
+    __shared__ float part[8][32 * (L + 1)];
     free_grid_dep_wait();
     free_grid_dep_launch();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.next = 0;
@@ -254,14 +254,19 @@ template <typename E> __global__ void __launch_bounds__(256) cross_delta_dense_k
             mine[row * pitch + x - row * units] = v;
         }
         __syncwarp();
-        float v = 0.f;
-        for (int u = 0; u < units; ++u) v += mine[lane * pitch + u];
+        float t[L];                                                // added in the order of the kernel above: the same sums
+#pragma unroll
+        for (int u = 0; u < L; ++u) t[u] = u < units ? mine[lane * pitch + u] : 0.f;
+#pragma unroll
+        for (int k = L / 2; k > 0; k >>= 1)
+#pragma unroll
+            for (int u = 0; u < k; ++u) t[u] += t[u + k];
         __syncwarp();
         const long long i = i0 + lane;
         if (i < rows) {
             const int h = (int)(i % a.heads);
             const long long st = i / a.heads;
-            a.delta[(st / a.n_q * a.heads + h) * a.n_q + st % a.n_q] = v;
+            a.delta[(st / a.n_q * a.heads + h) * a.n_q + st % a.n_q] = t[0];
         }
     }
 }
@@ -334,7 +339,7 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
     bool ok[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) ok[r] = counts(j0 + 4 * ty + r);
-    const int first = a.where.seq_of ? 0 : e * a.where.share, last = a.where.seq_of ? a.n_seq : first + a.where.share;
+    const int first = a.where.seq_of ? 0 : e * a.where.share, last = a.where.seq_of || first + a.where.share > a.n_seq ? a.n_seq : first + a.where.share;
     for (int s = first; s < last && j0 < sp.len; ++s) {
         if (cross_enc_of(a.where, s) != e) continue;
         for (int h = kh * a.group; h < (kh + 1) * a.group; ++h)
@@ -415,7 +420,8 @@ template <typename E> int delta_of(const CrossArgs& a, cudaStream_t s) {
         dense = dense && (a.heads == 1 || m->head == a.d) && (a.n_q == 1 || m->tok == (long long)a.heads * a.d) && (a.n_seq == 1 || m->seq == (long long)a.n_q * a.heads * a.d);
     if (dense) {
         const long long ctas = ((long long)a.n_seq * a.n_q * a.heads + 255) / 256;
-        return free_launch(free_overlap_for_rows((long long)a.n_seq * a.n_q), cross_delta_dense_kernel<E>, dim3((unsigned)(ctas < 148 * 6 ? ctas : 148 * 6)), dim3(256), 0, s, a);
+        auto kernel = units <= 8 ? cross_delta_dense_kernel<E, 8> : units <= 16 ? cross_delta_dense_kernel<E, 16> : cross_delta_dense_kernel<E, 32>;
+        return free_launch(free_overlap_for_rows((long long)a.n_seq * a.n_q), kernel, dim3((unsigned)(ctas < 148 * 6 ? ctas : 148 * 6)), dim3(256), 0, s, a);
     }
     return units <= 8 ? start_delta<E, V, 8>(a, s) : units <= 16 ? start_delta<E, V, 16>(a, s) : start_delta<E, V, 32>(a, s);
 }

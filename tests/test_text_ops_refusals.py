@@ -109,6 +109,9 @@ def test_cross_attention_bwd(L):
     # nothing to be written: no gradient wanted, or no token and no state
     assert _bwd(L, n_seq=0, n_enc=0, q=0, k=0, v=0, out=None, lse=None, g=None, dq=None, ws=None, err=None) == 0
     assert _bwd(L, n_q=0, n_kv=0, out=None, lse=None, g=None, dq=None, ws=None, err=None) == 0
+    # without tokens the states' gradients are zeros, and their inputs are looked at all the same
+    none = dict(n_seq=0, q=0, out=None, lse=None, g=None, dq=None, ws=None, err=None)
+    assert _bwd(L, k=0, **none) == ARG and _bwd(L, v=0, **none) == ARG and _bwd(L, kv_lens=ODD, **none) == ALIGN and _bwd(L, k=4097, **none) == ALIGN
     assert L.free_op_cross_attention_bwd_workspace_bytes(_pack(kv_heads=0)) == 0
 
 
