@@ -191,10 +191,11 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 continue;
             }
             float top = -INFINITY, sum = 0.f;            // maximum in use
+            bool early_s = false;
             for (int j = 0; j < nb; ++j, ++ns) {
                 const uint32_t buf = 2 * w + ns % SB, pbuf = 2 * w + ns % PB;
                 const bool whole = states - j * BK >= BK && !mask;
-                ok = cross_tc::wait(&s_full[buf], ns / SB & 1u, abort_flag);
+                ok = (j > 0 && __all_sync(0xffffffffu, early_s)) || cross_tc::wait(&s_full[buf], ns / SB & 1u, abort_flag);
                 if (!ok) break;
                 tc::tc_fence_after();
                 uint32_t x[64], bits[2];
@@ -234,6 +235,8 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                     }
                 }
                 const float base = top == -INFINITY ? 0.f : top * a.c;
+                // (polled before the exponentials, and the next scores before p is stored: 115 clocks each that nothing waits for)
+                const bool early_p = poll(&pv_done[pbuf], (ns / PB & 1u) ^ 1u);
                 const uint64_t c2 = pair(a.c, a.c), b2 = pair(-base, -base);
                 uint64_t s2[2] = {0ull, 0ull};
 #pragma unroll
@@ -243,7 +246,8 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                     s2[e & 1] = add2(s2[e & 1], pair(p0, p1));
                     x[e] = pack2(p0, p1);
                 }
-                ok = cross_tc::wait(&pv_done[pbuf], (ns / PB & 1u) ^ 1u, abort_flag);
+                ok = __all_sync(0xffffffffu, early_p) || cross_tc::wait(&pv_done[pbuf], (ns / PB & 1u) ^ 1u, abort_flag);
+                early_s = poll(&s_full[2 * w + (ns + 1u) % SB], (ns + 1u) / SB & 1u);
                 if (!ok) break;
                 tc::tc_fence_after();
                 tc::tmem_st32(lanes + M::p_col + (w * PB + ns % PB) * 32u, *reinterpret_cast<uint32_t (*)[32]>(x));
@@ -257,14 +261,12 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                         ok = cross_tc::wait(&kv_full[slot0 + 1], slot_ph, abort_flag);
                         if (!ok) break;
                         uint8_t* vt = ring + (slot0 + 1) * M::kv;
-#pragma unroll 1
-                        for (uint32_t o = out0, k0 = 0;; o = out1, k0 = 32) {
-                            for (; o; o &= o - 1u) {
-                                const uint32_t k = k0 + (uint32_t)__ffs((int)o) - 1u;
-                                if ((k & 3u) == (uint32_t)q && lane < 8 * NCH)
-                                    *reinterpret_cast<uint4*>(vt + (lane >> 3) * kKvChunk + k * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                            }
-                            if (k0) break;
+                        constexpr int PER = 8 * NCH;               // 16-byte pieces of a row
+#pragma unroll
+                        for (int u = 0; u < BK * PER / 128; ++u) {
+                            const uint32_t i = u * 128u + r, k = i / PER, piece = i % PER;
+                            if ((k < 32 ? out0 >> k : out1 >> (k - 32)) & 1u)
+                                *reinterpret_cast<uint4*>(vt + (piece >> 3) * kKvChunk + k * 128 + (piece & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                         }
                         tc::fence_proxy_async();
                     }

@@ -23,6 +23,12 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile ui
     }
     return __all_sync(0xffffffffu, r);
 }
+// One poll, which does not wait.
+__device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
 // Two of them, their first polls (some 115 clocks each) at once.
 __device__ __forceinline__ bool wait2(uint64_t* bar1, uint32_t parity1, uint64_t* bar2, uint32_t parity2, volatile uint32_t* abort_flag) {
     const bool r1 = tc::mbar_try_wait(bar1, parity1), r2 = tc::mbar_try_wait(bar2, parity2);

@@ -7,7 +7,7 @@
 // sum; what is stored of h is rounded to the residual's type).  Rows of up to 2048 columns take one warp, P pieces of 128 columns
 // (four consecutive ones per lane: whole 16- or 8-byte accesses, and one piece is one run of an 8-bit result's scale); wider
 // rows take several warps of a CTA, joined through shared memory.  The next row's loads are in flight while this one is reduced.
-// Heads of up to 128 columns: four rows share a warp (rms_norm_heads_kernel).
+// Heads of up to 128 columns: four rows share a warp, or eight (rms_norm_heads_kernel).
 #pragma once
 #include "rms_norm.h"
 #include <cuda_fp8.h>
@@ -307,16 +307,11 @@ template <typename TX, typename TY, int L, int C, int VW> int start_heads(RmsArg
 template <typename TX, typename TR, typename TY, int VW> int launch(const RmsArgs& a, cudaStream_t s) {
     if constexpr (sizeof(TY) > 1) {
         if (!a.res && a.D <= 128) {
-            if constexpr (VW == 8) {
-                if (a.D <= 32) return start_heads<TX, TY, 4, 8, VW>(a, s);
-                if (a.D <= 64) return start_heads<TX, TY, 8, 8, VW>(a, s);
-                return start_heads<TX, TY, 8, 16, VW>(a, s);
-            } else {
-                if (a.D <= 32) return start_heads<TX, TY, 4, 8, VW>(a, s);
-                if (a.D <= 64) return start_heads<TX, TY, 8, 8, VW>(a, s);
+            if (a.D <= 32) return start_heads<TX, TY, 4, 8, VW>(a, s);
+            if (a.D <= 64) return start_heads<TX, TY, 8, 8, VW>(a, s);
+            if constexpr (VW < 8)
                 if (a.D <= 96) return start_heads<TX, TY, 8, 12, VW>(a, s);
-                return start_heads<TX, TY, 8, 16, VW>(a, s);
-            }
+            return start_heads<TX, TY, 8, 16, VW>(a, s);
         }
     }
     const int D = a.D;
