@@ -525,16 +525,17 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     if (warp == 12) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, kTmemCols); }
 }
 
-// out, lse of a row from its parts' own: a CTA per row, the parts' weights in shared memory, two slices of the parts per channel.
+// out, lse of a row from its parts' own: a CTA per row, the parts' weights in shared memory, a slice of the parts per channel and 128 threads.
 constexpr int kMaxParts = 2048;
-template <typename E> __global__ void __launch_bounds__(256) cross_join_kernel(const CrossArgs a, const CrossParts p, long long rows) {
-    __shared__ float weight[kMaxParts], part_of[2][kCrossMaxD], reduce[8];
+template <typename E, int THREADS> __global__ void __launch_bounds__(THREADS) cross_join_kernel(const CrossArgs a, const CrossParts p, long long rows) {
+    constexpr int SLICES = THREADS / 128, WARPS = THREADS / 32;
+    __shared__ float weight[kMaxParts], part_of[SLICES][kCrossMaxD], reduce[WARPS];
     free_grid_dep_wait();
     free_grid_dep_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, ch = threadIdx.x & 127, slice = threadIdx.x >> 7;
     const long long i = blockIdx.x;
     float top = -INFINITY;
-    for (int k = threadIdx.x; k < p.n; k += 256) {
+    for (int k = threadIdx.x; k < p.n; k += THREADS) {
         weight[k] = p.lse[k * rows + i];
         top = fmaxf(top, weight[k]);
     }
@@ -543,10 +544,10 @@ template <typename E> __global__ void __launch_bounds__(256) cross_join_kernel(c
     if (lane == 0) reduce[warp] = top;
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 8; ++k) top = fmaxf(top, reduce[k]);
+    for (int k = 0; k < WARPS; ++k) top = fmaxf(top, reduce[k]);
     __syncthreads();
     float sum = 0.f;
-    for (int k = threadIdx.x; k < p.n; k += 256) {
+    for (int k = threadIdx.x; k < p.n; k += THREADS) {
         weight[k] = top == -INFINITY ? 0.f : expf(weight[k] - top);       // 0: a part without a state, which wrote nothing else
         sum += weight[k];
     }
@@ -555,13 +556,13 @@ template <typename E> __global__ void __launch_bounds__(256) cross_join_kernel(c
     __syncthreads();
     sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum += reduce[k];
+    for (int k = 0; k < WARPS; ++k) sum += reduce[k];
     float acc = 0.f;
     if (ch < a.d) {
         const float* o = p.out + i * a.d + ch;
         const long long step = rows * a.d;
 #pragma unroll 8
-        for (int k = slice; k < p.n; k += 2) {
+        for (int k = slice; k < p.n; k += SLICES) {
             const float f = weight[k], v = f != 0.f ? o[k * step] : 0.f;
             acc = fmaf(f, v, acc);
         }
@@ -569,7 +570,10 @@ template <typename E> __global__ void __launch_bounds__(256) cross_join_kernel(c
     part_of[slice][ch] = acc;
     __syncthreads();
     if (threadIdx.x < a.d) {
-        const float v = sum == 0.f ? 0.f : (part_of[0][ch] + part_of[1][ch]) / sum;
+        float v = 0.f;
+#pragma unroll
+        for (int k = 0; k < SLICES; ++k) v += part_of[k][ch];
+        v = sum == 0.f ? 0.f : v / sum;
         const int t = (int)(i % a.n_q), h = (int)(i / a.n_q % a.heads), s = (int)(i / a.n_q / a.heads);
         E* out = reinterpret_cast<E*>(const_cast<void*>(a.o.p)) + s * a.o.seq + t * a.o.tok + h * a.o.head;
         if constexpr (sizeof(E) == 4) out[ch] = v;
@@ -656,8 +660,8 @@ int cross_tc_forward(const CrossArgs& c, const CrossParts& parts, cudaStream_t s
 int cross_join(int dtype, const CrossArgs& a, const CrossParts& parts, cudaStream_t s) {
     const long long rows = (long long)a.n_seq * a.heads * a.n_q;
     if (parts.n > kMaxParts || rows > 0x7fffffffLL) return FREE_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)rows);
-    const bool early = free_overlap_for_rows(rows);
-    return dtype == FREE_FP32 ? free_launch(early, cross_join_kernel<float>, grid, dim3(256), 0, s, a, parts, rows)
-                              : free_launch(early, cross_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, a, parts, rows);
+    // many parts: more threads to read them (8 rows of 1184 parts, with the kernel before: 78 -> 54 us)
+    const bool many = parts.n >= 128, exact = dtype == FREE_FP32;
+    auto kernel = exact ? many ? cross_join_kernel<float, 1024> : cross_join_kernel<float, 256> : many ? cross_join_kernel<__nv_bfloat16, 1024> : cross_join_kernel<__nv_bfloat16, 256>;
+    return free_launch(free_overlap_for_rows(rows), kernel, dim3((unsigned)rows), dim3(many ? 1024 : 256), 0, s, a, parts, rows);
 }
