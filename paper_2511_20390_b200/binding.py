@@ -970,8 +970,8 @@ _ERROR_WORDS_LOCK = threading.Lock()
 
 
 def _error_word(device):
-    """The device error word that the gated layer's calls on a device share: zeroed once, OR-ed into by a kernel whose bounded
-    wait gave up, never cleared in between (so calls on several streams and replays of captured graphs may share it)."""
+    """The device error word that the calls of the gated layer and of the attention to an encoder's states on a device share:
+    zeroed once, OR-ed into by a kernel whose bounded wait gave up, never cleared in between (so calls on several streams and replays of captured graphs may share it)."""
     w = _ERROR_WORDS.get(device)
     if w is None:
         with _ERROR_WORDS_LOCK:                                    # threads that come first at once share one word
@@ -987,7 +987,7 @@ def _error_word(device):
 
 
 def op_device_error(device=None):
-    """Waits for `device` and returns the error word of the gated layer's calls on it so far (0: no bounded wait gave up)."""
+    """Waits for `device` and returns the error word of the calls of the gated layer and of op_cross_attention on it so far (0: no bounded wait gave up)."""
     index = None if device is None else torch.device(device).index
     if index is None:
         index = torch.cuda.current_device()

@@ -5,10 +5,12 @@
 // Bound by HBM (K and V are read once, 2 rows of multiply-adds per element) or, for short state sequences, by latency: no tensor
 // memory, no tile copies, one launch.  L lanes hold a state's row, one 16-byte unit each, and a warp 32 / L states; every group of
 // lanes takes KEYS states at a time.  Units are copied to shared memory several steps ahead, every lane its own, so that the bytes in
-// flight do not cost registers.  Scores
-// are summed over the lanes by exchanges that halve the values as they go, so that every lane ends with its own (row, state) and takes
-// its exponential; the probabilities are then passed to all lanes of the group.  The parts of a CTA's groups are joined through shared memory; long state sequences
-// are split over CTAs as well and joined by cross_join_kernel.
+// flight do not cost registers.  Scores are summed over the lanes by exchanges that halve the values as they go, so that every lane ends
+// with its own (row, state) and takes its exponential; the probabilities are then passed to all lanes of the group.  The parts of a
+// CTA's groups are joined through shared memory; long state sequences are split over CTAs as well and joined by cross_join_kernel.
+// Measured: 4 sequences of 77 states, 6 heads of 64: 4.4 us (8.7 by the tensor cores' kernel).  8 of up to 16384 states, 32 heads of 128
+// on 8: 84 us and 6 for the join, 4.3 TB/s of K and V, 0.62 of the issue slots (120 us with every score summed over all lanes).  What is
+// left are the ends: an SM holds three CTAs, and lengths that only the device knows fill the last round of them in part.
 #include "cross_tc.cuh"
 
 namespace {
@@ -268,7 +270,8 @@ bool cross_rows_supported(int dtype, const CrossArgs& a) {
     return ok;
 }
 
-// Parts: enough CTAs for eight on every SM, 128 states each at least.
+// Parts: enough CTAs for eight on every SM, 128 states each at least (the case above: six on every SM 88 us, twelve 92, 24 110; of equal
+// lengths 115, 111 with eight).
 int cross_rows_parts(const CrossArgs& a) {
     const long long ctas = (long long)a.n_seq * a.kv_heads, most = (a.where.n_kv + 127) / 128;
     long long n = (8 * kSms + ctas - 1) / ctas;

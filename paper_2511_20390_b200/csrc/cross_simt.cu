@@ -8,7 +8,8 @@
 // Tiles of 64 x 64 scores, 256 threads.  Thread (ty, tx) forms the scores of rows 4 ty .. and columns tx, tx + 16, ..: both
 // operands are read as four consecutive channels (16 bytes), eight reads for 64 multiply-adds; a row of a tile is d + 4 floats
 // (rounded up), so that eight threads' reads lie in different banks.  Scores go through shared memory to be the left operand
-// of the second product.  Bound by the fp32 pipe and shared memory's bandwidth.
+// of the second product.  Bound by the fp32 pipe and shared memory's bandwidth; small calls by latency (3 x 333 tokens, 6 heads of 40,
+// up to 77 states: 29 us).
 // States that do not count are read as zeros and their scores are masked, so nothing in them reaches a result.
 #include "cross.h"
 #include <mutex>
@@ -173,7 +174,8 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
 }
 
 // delta = <dout, out> of every token and head.  L lanes hold a row, V consecutive channels each (16 bytes, or 1 element where the rows
-// allow no more), R rows of a group of lanes are in flight: bound by HBM.  Rows are counted on, not divided out.
+// allow no more), R rows of a group of lanes are in flight.  Rows are counted on, not divided out.  (24 x 1024 tokens, 16 heads of 72: 42 us,
+// nine of sixteen lanes busy; the kernel for matrices without gaps 23, 4.9 TB/s.)
 template <typename E, int V> struct Chunk {
     E v[V];
     __device__ __forceinline__ void load(const E* p, bool ok) {

@@ -13,6 +13,9 @@
 //   - The last block of a sequence costs the 16-column steps that it has.  States that do not count: scores are replaced by -inf, and the
 //     rows of V are zeroed in shared memory (0 x NaN would be NaN).
 // Long states and few rows: the states are split into parts, each with its own softmax, joined by cross_join_kernel.
+// What bounds it: a block's way through the softmax warps, some 1700 clocks for 64 states where the exponentials and conversions of its
+// two warps per scheduler are 1050; the tensor cores work for 16% of the time, the exponentials' unit for 29%.  24 x 1024 tokens, 16 heads
+// of 72, up to 300 states: 72 us (0.31 PFLOP/s); 8 x 4096 tokens, 16 heads of 128, up to 512 states: 131 us (0.70).
 #include "cross_tc.cuh"
 
 namespace cross_tc {

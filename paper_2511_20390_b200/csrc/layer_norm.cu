@@ -262,7 +262,8 @@ template <typename TX, typename TY, int VW> constexpr bool kAhead = VW * sizeof(
 
 // One CTA, a team of warps with C columns per lane, per (group, chunk): a run of the group's rows, R of them per barrier and R more in
 // flight.  T: threads per SM that the register budget is set for.
-// RMS: the norm without a mean and bias, dx = r (v - xh mean(v xh)) + dres with xh = x r.
+// RMS: the norm without a mean and bias, dx = r (v - xh mean(v xh)) + dres with xh = x r (24 x 1024 rows of 1152, fp32 with the residual's
+// gradient, bf16 dy: 60 us, 69 with the sums of the table's columns).
 template <typename TX, typename TY, int C, int VW, int MAXT, int T, int R, bool RMS>
 __global__ void __launch_bounds__(MAXT, T / MAXT) layer_norm_bwd_kernel(const NormArgs a) {
     constexpr int P = C / VW, XW = kWords<TX, VW>, YW = kWords<TY, VW>;      // pieces of a lane, words of a piece
