@@ -628,8 +628,8 @@ int free_op_rope_axes(int dtype, int pairing, int freq_mode, int inverse, int n_
  *   kv_seq     DEVICE int32 [n_seq] or NULL: e(s), outside 0 .. n_enc - 1 for none.  NULL: n_seq is a multiple of n_enc, and
  *              n_seq / n_enc consecutive sequences share one (the drafts of an image share its prompt)
  *   dtype      FREE_FP32 (CUDA cores) or FREE_BF16 (tcgen05, fp32 accumulation and softmax; probabilities are rounded to bf16,
- *              which their product takes).  bf16 inputs that are not 16-byte aligned in every stride, or whose d_head is no
- *              multiple of 8, take the CUDA cores
+ *              which their product takes).  bf16 matrices that are not 16-byte aligned in every stride take the CUDA cores;
+ *              so do, in a kernel of their own, tokens times heads per key head of up to eight, whose probabilities stay fp32
  *   d_head     up to 128, else UNSUPPORTED;  heads a multiple of kv_heads;  scale > 0
  * What does not count is not used: NaN and infinities in it change nothing.
  *   out        DEVICE `dtype`, strides (elements) like q's; must not overlap the inputs

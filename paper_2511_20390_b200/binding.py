@@ -971,7 +971,8 @@ _ERROR_WORDS_LOCK = threading.Lock()
 
 def _error_word(device):
     """The device error word that the calls of the gated layer and of the attention to an encoder's states on a device share:
-    zeroed once, OR-ed into by a kernel whose bounded wait gave up, never cleared in between (so calls on several streams and replays of captured graphs may share it)."""
+    zeroed once, OR-ed into by a kernel whose bounded wait gave up, never cleared in between (so calls on several streams and
+    replays of captured graphs may share it)."""
     w = _ERROR_WORDS.get(device)
     if w is None:
         with _ERROR_WORDS_LOCK:                                    # threads that come first at once share one word

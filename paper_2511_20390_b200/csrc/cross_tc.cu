@@ -362,6 +362,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
 #pragma unroll 1
                     for (int c = 0; c < ks; ++c) {
                         uint32_t o[16];
+                        __syncwarp();
                         tc::tmem_ld16(to + 16 * c, o);
                         tc::tmem_wait_ld();
                         if (!row_ok) continue;
@@ -647,8 +648,8 @@ int cross_tc_forward(const CrossArgs& c, const CrossParts& parts, cudaStream_t s
     FREE_TRY(map_heads(&mq, c.q, c.n_seq, c.n_q, c.heads, c.d, c.group, a.tt));
     FREE_TRY(map_heads(&mk, c.k, enc, rows, c.kv_heads, c.d, 1, BK));
     FREE_TRY(map_heads(&mv, c.v, enc, rows, c.kv_heads, c.d, 1, BK));
-    // results leave by tile copies of 32 rows, where these are whole tokens
-    a.boxed = 32 % c.group == 0;
+    // results leave by tile copies of 32 rows, where these are whole tokens and heads end with a piece of 16 bytes (copies write whole ones)
+    a.boxed = 32 % c.group == 0 && c.d % 8 == 0;
     a.o = c.o;
     FREE_TRY(map_heads(&mo, c.o, c.n_seq, c.n_q, c.heads, c.d, a.boxed ? c.group : 1, a.boxed ? 32 / c.group : 32));
     const bool brief = c.where.n_kv <= kShort;

@@ -197,6 +197,27 @@ def test_layouts(n_q, n_kv, d, dt):
     assert torch.equal(free.op_cross_attention(q, k, v, kv_mask=mask), free.op_cross_attention(q, k, v, kv_mask=mask.to(torch.uint8) * 3))
 
 
+@pytest.mark.parametrize("n_q,d", [(1, 36), (100, 36), (150, 20), (90, 68), (70, 100), (130, 127)])
+def test_heads_with_gaps(n_q, d):
+    """Head sizes of no whole 16 bytes whose heads lie 16-byte aligned take the tensor cores; dense ones do not.  Both round p and dS or
+    the results to bf16 (2^-8 of each term, which add up like errors of either sign): 1e-2 in the 2-norm."""
+    import paper_2511_20390_b200 as free
+    n_seq, n_kv, heads, kvh = 2, 150, 4, 2
+    wide = lambda role, *s: _t(9, role, (*s, (d + 7) // 8 * 8), torch.bfloat16)[..., :d]
+    q, g, k, v = wide(1, n_seq, n_q, heads), wide(2, n_seq, n_q, heads), wide(3, n_seq, n_kv, kvh), wide(4, n_seq, n_kv, kvh)
+    lens = torch.tensor([150, 70], dtype=torch.int32, device="cuda")
+    out = torch.full((n_seq, n_q, heads, (d + 7) // 8 * 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    got, lse = free.op_cross_attention(q, k, v, kv_lens=lens, want_lse=True, out=out[..., :d])
+    c = lambda t: t.double().cpu().numpy()
+    f = lambda t: t.double().requires_grad_()
+    leaves = [f(q), f(k), f(v)]
+    want = _cross64(*leaves, [150, 70], 1)
+    assert rms_rel(c(got), c(want.detach())) < 1e-2 and (out[..., d:] == 7).all()
+    for a, b in zip(free.op_cross_attention_bwd(q, k, v, got, lse, g, kv_lens=lens), torch.autograd.grad(want, leaves, g.double())):
+        assert rms_rel(c(a), c(b)) < 1e-2
+    assert free.op_device_error() == 0
+
+
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("n_q", [1, 70])
 def test_lengths_that_say_too_much(n_q, dt):
