@@ -25,14 +25,22 @@ __device__ __forceinline__ void from_f(__nv_bfloat16& d, float v) { d = __float2
 
 __host__ __device__ constexpr int pitch(int d) { return (d + 7) / 8 * 8 + 4; }
 
-// rows [r0, r0 + T) of a matrix of heads -> shared memory; rows that are not `live` and channels behind d are zeros
+// rows [r0, r0 + T) of a matrix of heads -> shared memory; rows that are not `live` and channels behind d are zeros.  A warp's eight rows
+// are under way together (one after the other, 3 x 333 tokens, 6 heads of 40 took 29 us).
 template <typename E, typename Live>
 __device__ __forceinline__ void load_tile(float* dst, const E* base, long long stride, int r0, int d, int P, Live live) {
+    constexpr int WARPS = kThreads / 32, R = T / WARPS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int r = warp; r < T; r += kThreads / 32) {
-        const bool ok = live(r0 + r);
-        const E* src = base + (long long)(r0 + r) * stride;
-        for (int c = lane; c < P; c += 32) dst[r * P + c] = ok && c < d ? to_f(src[c]) : 0.f;
+    bool ok[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) ok[i] = live(r0 + warp + i * WARPS);
+    const E* src = base + (long long)(r0 + warp) * stride;
+    for (int c = lane; c < P; c += 32) {
+        E v[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) v[i] = ok[i] && c < d ? src[i * WARPS * stride + c] : E(0.f);
+#pragma unroll
+        for (int i = 0; i < R; ++i) dst[(warp + i * WARPS) * P + c] = to_f(v[i]);
     }
 }
 
