@@ -50,7 +50,7 @@ struct CrossArgs {
     float scale;
     float* lse;                               // [n_seq, heads, n_q]
     float* delta;                             // backward: <dout, out>, laid out as lse
-    unsigned long long* next;                           // backward: a counter that the kernel of delta sets to zero
+    unsigned long long* next;                 // backward: a counter that the kernel of delta sets to zero
     uint32_t* err;
 };
 
@@ -63,6 +63,7 @@ int cross_bwd_tc_parts(const CrossArgs& a);   // of the tokens, for dk and dv: f
 int cross_bwd_tc_dq(const CrossArgs& a, cudaStream_t s);
 int cross_bwd_tc_dkv(const CrossArgs& a, int parts, float* part_out, cudaStream_t s);
 int cross_join(int dtype, const CrossArgs& a, const CrossParts& parts, cudaStream_t s);
+int cross_bwd_join(int dtype, const CrossArgs& a, int parts, const float* part_out, cudaStream_t s);      // dk and dv from their parts
 
 // Few tokens, fp32 or bf16
 bool cross_rows_supported(int dtype, const CrossArgs& a);
@@ -73,4 +74,5 @@ int cross_rows_forward(int dtype, const CrossArgs& a, const CrossParts& parts, c
 int cross_simt_forward(int dtype, const CrossArgs& a, cudaStream_t s);
 int cross_delta(int dtype, const CrossArgs& a, cudaStream_t s);
 int cross_simt_dq(int dtype, const CrossArgs& a, cudaStream_t s);
-int cross_simt_dkv(int dtype, const CrossArgs& a, cudaStream_t s);
+int cross_simt_dkv_parts(const CrossArgs& a); // as cross_bwd_tc_parts
+int cross_simt_dkv(int dtype, const CrossArgs& a, int parts, float* part_out, cudaStream_t s);

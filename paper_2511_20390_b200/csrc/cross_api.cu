@@ -132,7 +132,8 @@ extern "C" size_t free_op_cross_attention_bwd_workspace_bytes(const free_cross_a
     if (check(c, &empty) != FREE_OK || empty) return 0;
     CrossArgs a = args_of(c);
     a.g = a.q;
-    return stat_bytes(c) + kNextBytes + (c->dtype == FREE_BF16 && cross_bwd_tc_supported(a) ? sum_bytes(c, cross_bwd_tc_parts(a)) : 0);
+    const size_t simt = sum_bytes(c, cross_simt_dkv_parts(a)), tc = c->dtype == FREE_BF16 && cross_bwd_tc_supported(a) ? sum_bytes(c, cross_bwd_tc_parts(a)) : 0;
+    return stat_bytes(c) + kNextBytes + (simt > tc ? simt : tc);
 }
 
 extern "C" int free_op_cross_attention_bwd(const free_cross_attn* c, const void* out, int64_t o_seq, int64_t o_tok, int64_t o_head, const float* lse,
@@ -175,10 +176,11 @@ extern "C" int free_op_cross_attention_bwd(const free_cross_attn* c, const void*
     const bool tc = c->dtype == FREE_BF16 && !empty && cross_bwd_tc_supported(a);
     if (!empty && dq) FREE_TRY(tc && cross_tc::mappable(a.dq, c->n_seq, c->n_q, c->heads) ? cross_bwd_tc_dq(a, s) : cross_simt_dq(c->dtype, a, s));
     if (dk && states(c)) {
+        float* parts = empty ? nullptr : (float*)((char*)ws + stat_bytes(c) + kNextBytes);
         if (tc && cross_tc::mappable(a.dk, enc, rows, c->kv_heads) && cross_tc::mappable(a.dv, enc, rows, c->kv_heads))
-            FREE_TRY(cross_bwd_tc_dkv(a, cross_bwd_tc_parts(a), (float*)((char*)ws + stat_bytes(c) + kNextBytes), s));
+            FREE_TRY(cross_bwd_tc_dkv(a, cross_bwd_tc_parts(a), parts, s));
         else
-            FREE_TRY(cross_simt_dkv(c->dtype, a, s));
+            FREE_TRY(cross_simt_dkv(c->dtype, a, empty ? 1 : cross_simt_dkv_parts(a), parts, s));
     }
     return FREE_OK;
 }

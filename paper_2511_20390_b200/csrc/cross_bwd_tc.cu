@@ -626,7 +626,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
 }
 
 // dk and dv from their parts: a warp per state and key head, parts in order
-__global__ void __launch_bounds__(256) cross_bwd_join_kernel(const Args a) {
+template <typename E> __global__ void __launch_bounds__(256) cross_bwd_join_kernel(const CrossArgs a, int parts, const float* part_out, long long part_rows) {
     free_grid_dep_wait();
     free_grid_dep_launch();
     const int lane = threadIdx.x & 31;
@@ -637,12 +637,13 @@ __global__ void __launch_bounds__(256) cross_bwd_join_kernel(const Args a) {
         if (a.where.offsets && j >= sp.len) continue;
         const long long row = ((long long)sp.enc * a.where.kv_rows + sp.row0 + j) * a.kv_heads + h;
         for (int o = 0; o < 2; ++o) {
-            const CrossMat& mat = o ? a.o2 : a.o1;
-            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(mat.p)) + sp.enc * mat.seq + (long long)(sp.row0 + j) * mat.tok + h * mat.head;
+            const CrossMat& mat = o ? a.dv : a.dk;
+            E* dst = reinterpret_cast<E*>(const_cast<void*>(mat.p)) + sp.enc * mat.seq + (long long)(sp.row0 + j) * mat.tok + h * mat.head;
             for (int c = lane; c < a.d; c += 32) {
                 float v = 0.f;
-                for (int p = 0; p < a.parts; ++p) v += a.part_out[(((long long)p * 2 + o) * a.part_rows + row) * a.d + c];
-                dst[c] = __float2bfloat16(v);
+                for (int p = 0; p < parts; ++p) v += part_out[(((long long)p * 2 + o) * part_rows + row) * a.d + c];
+                if constexpr (sizeof(E) == 4) dst[c] = v;
+                else dst[c] = __float2bfloat16(v);
             }
         }
     }
@@ -725,6 +726,12 @@ int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_
                                  launch<true, 2, 128, 1, 4, 4, 2, 2, 1>(m, a, s);
     FREE_TRY(code);
     if (parts == 1) return FREE_OK;
+    return cross_bwd_join(FREE_BF16, c, parts, part_out, s);
+}
+
+int cross_bwd_join(int dtype, const CrossArgs& c, int parts, const float* part_out, cudaStream_t s) {
     const long long n = (long long)c.where.n_enc * c.where.n_kv * c.kv_heads, ctas = (n + 7) / 8;
-    return free_launch(false, cross_bwd_join_kernel, dim3((unsigned)(ctas < kSms * 8 ? ctas : kSms * 8)), dim3(256), 0, s, a);
+    const long long rows = (long long)(c.where.offsets ? 1 : c.where.n_enc) * c.where.kv_rows * c.kv_heads;
+    auto kernel = dtype == FREE_FP32 ? cross_bwd_join_kernel<float> : cross_bwd_join_kernel<__nv_bfloat16>;
+    return free_launch(false, kernel, dim3((unsigned)(ctas < kSms * 8 ? ctas : kSms * 8)), dim3(256), 0, s, c, parts, part_out, rows);
 }

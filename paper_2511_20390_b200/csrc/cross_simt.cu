@@ -3,13 +3,13 @@
 //
 //   forward   S = scale q k^T, p = e^(S - max), out = p v / sum p, lse = max + log sum p     one pass, running maximum and sum
 //   dq        p = e^(S - lse), dS = p (g v^T - delta) scale, dq = dS k                        g: the gradient of out
-//   dk, dv    dk = dS^T q, dv = p^T g, summed over the queries, heads and sequences that share the states
+//   dk, dv    dk = dS^T q, dv = p^T g, summed over the queries, heads and sequences that share the states (in parts, joined in order)
 //
 // Tiles of 64 x 64 scores, 256 threads.  Thread (ty, tx) forms the scores of rows 4 ty .. and columns tx, tx + 16, ..: both
 // operands are read as four consecutive channels (16 bytes), eight reads for 64 multiply-adds; a row of a tile is d + 4 floats
 // (rounded up), so that eight threads' reads lie in different banks.  Scores go through shared memory to be the left operand
 // of the second product.  Bound by the fp32 pipe and shared memory's bandwidth; small calls by latency (3 x 333 tokens, 6 heads of 40,
-// up to 77 states: 29 us).
+// up to 77 states: 17 us).
 // States that do not count are read as zeros and their scores are masked, so nothing in them reaches a result.
 #include "cross.h"
 #include <mutex>
@@ -326,13 +326,14 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
     store_rows<E, ND>(at_out<E>(a.dq, s, 0, h), a.dq.tok, q0, a.n_q, d, ty, tx, acc);
 }
 
-// One CTA per (64 states, key head, encoder sequence); it walks over every sequence that reads it, its query heads and tokens.
-template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_simt_dkv_kernel(const CrossArgs a) {
+// A CTA per (64 states, key head, encoder sequence, part); it walks over its part of the tiles of tokens: of every sequence that reads the
+// states, in order, the query heads of the key head and 64 tokens.
+template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_simt_dkv_kernel(const CrossArgs a, int parts, float* part_out) {
     extern __shared__ float smem[];
     const int d = a.d, P = pitch(d);
     float *K = smem, *V = K + T * P, *Q = V + T * P, *G = Q + T * P, *W = G + T * P, *L = W + T * PS, *D = L + T;
     const int tiles = (a.where.n_kv + T - 1) / T;
-    const int tile = (int)(blockIdx.x % tiles), eh = (int)(blockIdx.x / tiles), kh = eh % a.kv_heads, e = eh / a.kv_heads;
+    const int part = (int)(blockIdx.x % parts), te = (int)(blockIdx.x / parts), tile = te % tiles, eh = te / tiles, kh = eh % a.kv_heads, e = eh / a.kv_heads;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, j0 = tile * T;
     const CrossSpan sp = cross_span_of_enc(a.where, e);
     const int rows = a.where.offsets ? sp.len : a.where.n_kv;      // rows that are written
@@ -350,10 +351,23 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
 #pragma unroll
     for (int r = 0; r < 4; ++r) ok[r] = counts(j0 + 4 * ty + r);
     const int first = a.where.seq_of ? 0 : e * a.where.share, last = a.where.seq_of || first + a.where.share > a.n_seq ? a.n_seq : first + a.where.share;
-    for (int s = first; s < last && j0 < sp.len; ++s) {
+    const long long per = (long long)a.group * ((a.n_q + T - 1) / T);           // tiles of a sequence
+    long long lo = 0, hi = per * (last - first), at_tile = 0;
+    if (parts > 1) {
+        if (a.where.seq_of) {
+            int n = 0;
+            for (int s = 0; s < a.n_seq; s += kThreads) n += __syncthreads_count(s + (int)threadIdx.x < a.n_seq && cross_enc_of(a.where, s + threadIdx.x) == e);
+            hi = per * n;
+        }
+        lo = hi * part / parts;
+        hi = hi * (part + 1) / parts;
+    }
+    for (int s = first; s < last && j0 < sp.len && at_tile < hi; ++s) {
         if (cross_enc_of(a.where, s) != e) continue;
+        if (at_tile + per <= lo) { at_tile += per; continue; }
         for (int h = kh * a.group; h < (kh + 1) * a.group; ++h)
-            for (int q0 = 0; q0 < a.n_q; q0 += T) {
+            for (int q0 = 0; q0 < a.n_q; q0 += T, ++at_tile) {
+                if (at_tile < lo || at_tile >= hi) continue;
                 __syncthreads();
                 auto live = [&](int r) { return r < a.n_q; };
                 load_tile<E>(Q, at<E>(a.q, s, 0, h), a.q.tok, q0, d, P, live);
@@ -394,15 +408,22 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
 #pragma unroll
             for (int i = 0; i < 4 * ND; ++i) dk[r][i] = dv[r][i] = 0.f;
         }
+    if (parts > 1) {
+        const long long all = (long long)(a.where.offsets ? 1 : a.where.n_enc) * a.where.kv_rows * a.kv_heads * d, step = (long long)a.kv_heads * d;
+        float* out = part_out + 2 * part * all + (((long long)sp.enc * a.where.kv_rows + sp.row0) * a.kv_heads + kh) * d;
+        store_rows<float, ND>(out, step, j0, rows, d, ty, tx, dk);
+        store_rows<float, ND>(out + all, step, j0, rows, d, ty, tx, dv);
+        return;
+    }
     store_rows<E, ND>(at_out<E>(a.dk, sp.enc, sp.row0, kh), a.dk.tok, j0, rows, d, ty, tx, dk);
     store_rows<E, ND>(at_out<E>(a.dv, sp.enc, sp.row0, kh), a.dv.tok, j0, rows, d, ty, tx, dv);
 }
 
-template <typename K> int launch(K kernel, long long ctas, int tiles_held, int extra, const CrossArgs& a, cudaStream_t s) {
+template <typename K, typename... A> int launch(K kernel, long long ctas, int tiles_held, int extra, cudaStream_t s, const CrossArgs& a, A... rest) {
     if (ctas > 0x7fffffffLL) return FREE_ERR_SHAPE;
     const int smem = (tiles_held * T * pitch(a.d) + T * PS + extra) * (int)sizeof(float);
     FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    kernel<<<(unsigned)ctas, kThreads, smem, s>>>(a);
+    kernel<<<(unsigned)ctas, kThreads, smem, s>>>(a, rest...);
     return free_check_launch();
 }
 long long q_tiles(const CrossArgs& a) { return (long long)((a.n_q + T - 1) / T) * a.n_seq * a.heads; }
@@ -410,8 +431,8 @@ long long q_tiles(const CrossArgs& a) { return (long long)((a.n_q + T - 1) / T) 
 }  // namespace
 
 int cross_simt_forward(int dtype, const CrossArgs& a, cudaStream_t s) {
-    if (dtype == FREE_FP32) return a.d <= 64 ? launch(cross_simt_kernel<float, 1>, q_tiles(a), 3, 0, a, s) : launch(cross_simt_kernel<float, 2>, q_tiles(a), 3, 0, a, s);
-    return a.d <= 64 ? launch(cross_simt_kernel<__nv_bfloat16, 1>, q_tiles(a), 3, 0, a, s) : launch(cross_simt_kernel<__nv_bfloat16, 2>, q_tiles(a), 3, 0, a, s);
+    if (dtype == FREE_FP32) return a.d <= 64 ? launch(cross_simt_kernel<float, 1>, q_tiles(a), 3, 0, s, a) : launch(cross_simt_kernel<float, 2>, q_tiles(a), 3, 0, s, a);
+    return a.d <= 64 ? launch(cross_simt_kernel<__nv_bfloat16, 1>, q_tiles(a), 3, 0, s, a) : launch(cross_simt_kernel<__nv_bfloat16, 2>, q_tiles(a), 3, 0, s, a);
 }
 namespace {
 
@@ -440,11 +461,27 @@ template <typename E> int delta_of(const CrossArgs& a, cudaStream_t s) {
 
 int cross_delta(int dtype, const CrossArgs& a, cudaStream_t s) { return dtype == FREE_FP32 ? delta_of<float>(a, s) : delta_of<__nv_bfloat16>(a, s); }
 int cross_simt_dq(int dtype, const CrossArgs& a, cudaStream_t s) {
-    if (dtype == FREE_FP32) return a.d <= 64 ? launch(cross_simt_dq_kernel<float, 1>, q_tiles(a), 4, 0, a, s) : launch(cross_simt_dq_kernel<float, 2>, q_tiles(a), 4, 0, a, s);
-    return a.d <= 64 ? launch(cross_simt_dq_kernel<__nv_bfloat16, 1>, q_tiles(a), 4, 0, a, s) : launch(cross_simt_dq_kernel<__nv_bfloat16, 2>, q_tiles(a), 4, 0, a, s);
+    if (dtype == FREE_FP32) return a.d <= 64 ? launch(cross_simt_dq_kernel<float, 1>, q_tiles(a), 4, 0, s, a) : launch(cross_simt_dq_kernel<float, 2>, q_tiles(a), 4, 0, s, a);
+    return a.d <= 64 ? launch(cross_simt_dq_kernel<__nv_bfloat16, 1>, q_tiles(a), 4, 0, s, a) : launch(cross_simt_dq_kernel<__nv_bfloat16, 2>, q_tiles(a), 4, 0, s, a);
 }
-int cross_simt_dkv(int dtype, const CrossArgs& a, cudaStream_t s) {
-    const long long n = (long long)((a.where.n_kv + T - 1) / T) * a.where.n_enc * a.kv_heads;
-    if (dtype == FREE_FP32) return a.d <= 64 ? launch(cross_simt_dkv_kernel<float, 1>, n, 4, 2 * T, a, s) : launch(cross_simt_dkv_kernel<float, 2>, n, 4, 2 * T, a, s);
-    return a.d <= 64 ? launch(cross_simt_dkv_kernel<__nv_bfloat16, 1>, n, 4, 2 * T, a, s) : launch(cross_simt_dkv_kernel<__nv_bfloat16, 2>, n, 4, 2 * T, a, s);
+namespace {
+long long dkv_items(const CrossArgs& a) { return (long long)((a.where.n_kv + T - 1) / T) * a.where.n_enc * a.kv_heads; }
+}  // namespace
+
+// Parts of the tokens where the blocks of states leave SMs without one (all gradients of 2 x 512 tokens, 8 heads of 64, 300 states: 158 ->
+// 139 us; of 3 x 333 tokens, 77 states, 6 heads of 40: 84 -> 52)
+int cross_simt_dkv_parts(const CrossArgs& a) {
+    const long long items = dkv_items(a), tiles = (long long)a.n_seq * a.group * ((a.n_q + T - 1) / T) / (a.where.n_enc > 0 ? a.where.n_enc : 1);
+    if (items < 1 || items >= 2 * 148) return 1;
+    long long p = (3 * 148 + items - 1) / items;
+    if (p > tiles) p = tiles;
+    return p < 1 ? 1 : (int)p;
+}
+int cross_simt_dkv(int dtype, const CrossArgs& a, int parts, float* part_out, cudaStream_t s) {
+    const long long n = dkv_items(a) * parts;
+    const bool slim = a.d <= 64;
+    auto kernel = dtype == FREE_FP32 ? slim ? cross_simt_dkv_kernel<float, 1> : cross_simt_dkv_kernel<float, 2>
+                                     : slim ? cross_simt_dkv_kernel<__nv_bfloat16, 1> : cross_simt_dkv_kernel<__nv_bfloat16, 2>;
+    FREE_TRY(launch(kernel, n, 4, 2 * T, s, a, parts, part_out));
+    return parts > 1 ? cross_bwd_join(dtype, a, parts, part_out, s) : FREE_OK;
 }
