@@ -54,6 +54,12 @@ struct CrossArgs {
     uint32_t* err;
 };
 
+// Parts of dk and dv that 64 MB hold: packed states may lie in many more rows than their sequences name
+inline long long cross_parts_held(const CrossArgs& a) {
+    const long long bytes = 8LL * (a.where.offsets ? 1 : a.where.n_enc) * a.where.kv_rows * a.kv_heads * a.d;
+    return bytes > 0 && (64LL << 20) / bytes > 1 ? (64LL << 20) / bytes : 1;
+}
+
 // Tensor cores, bf16
 bool cross_tc_supported(const CrossArgs& a);
 int cross_tc_parts(const CrossArgs& a);

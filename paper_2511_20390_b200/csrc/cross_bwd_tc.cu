@@ -686,6 +686,7 @@ int cross_bwd_tc_parts(const CrossArgs& c) {
     if (items >= kSms) return 1;
     long long p = (2 * kSms + items - 1) / items;
     if (p > tiles / 2) p = tiles / 2;
+    if (p > cross_parts_held(c)) p = cross_parts_held(c);
     return p < 1 ? 1 : (int)p;
 }
 

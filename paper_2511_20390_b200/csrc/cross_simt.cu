@@ -475,6 +475,7 @@ int cross_simt_dkv_parts(const CrossArgs& a) {
     if (items < 1 || items >= 2 * 148) return 1;
     long long p = (3 * 148 + items - 1) / items;
     if (p > tiles) p = tiles;
+    if (p > cross_parts_held(a)) p = cross_parts_held(a);
     return p < 1 ? 1 : (int)p;
 }
 int cross_simt_dkv(int dtype, const CrossArgs& a, int parts, float* part_out, cudaStream_t s) {

@@ -106,6 +106,11 @@ def test_cross_attention_bwd(L):
     need = L.free_op_cross_attention_bwd_workspace_bytes(_pack())
     assert need >= 2 * 5 * 2 * 4
     assert _bwd(L, ws=None) == WORKSPACE and _bwd(L, need=need - 1) == WORKSPACE and _bwd(L, ws=P + 8) == ALIGN
+    # parts of dk and dv stay small beside states of which few are named
+    for dt in (0, 1):
+        for rows, n_kv, d in ((1 << 20, 64, 64), (100, 100, 128), (3000, 3000, 40), (1 << 24, 1, 8)):
+            n = L.free_op_cross_attention_bwd_workspace_bytes(_pack(dtype=dt, n_seq=1, n_enc=1, n_q=4096, kv_offsets=P, kv_rows=rows, n_kv=n_kv, d_head=d, kv_heads=1))
+            assert 0 < n <= (64 << 20) + 1024 + 2 * 4096 * 4
     # nothing to be written: no gradient wanted, or no token and no state
     assert _bwd(L, n_seq=0, n_enc=0, q=0, k=0, v=0, out=None, lse=None, g=None, dq=None, ws=None, err=None) == 0
     assert _bwd(L, n_q=0, n_kv=0, out=None, lse=None, g=None, dq=None, ws=None, err=None) == 0
