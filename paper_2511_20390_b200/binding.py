@@ -664,7 +664,7 @@ def _adr(t):
 def _launch(what, device, *args):
     """Library call `what` with `device` current, on the stream that is current there (its last argument)."""
     fn = getattr(_LIB or lib(), what)
-    if device == torch.cuda.current_device():
+    if device == torch._C._cuda_getDevice():
         code = fn(*args, torch._C._cuda_getCurrentRawStream(device))
     else:
         with torch.cuda.device(device):
@@ -824,14 +824,14 @@ class RmsNorm(typing.NamedTuple):
 
 def _tokens(t, shape, what):
     """(token stride, head stride) of a [tokens, D] or [tokens, heads, D] tensor whose rows are dense."""
-    if t.shape != shape or (shape[-1] > 1 and t.stride(-1) != 1):
+    st, D = t.stride(), shape[-1]
+    if t.shape != shape or (D > 1 and st[-1] != 1):
         raise ValueError(f"{what}: expected {list(shape)} with dense rows")
-    M, D = shape[0], shape[-1]
-    if len(shape) == 2:
-        return (t.stride(0) if M > 1 else max(D, t.stride(0))), 0
+    if len(st) == 2:
+        return (st[0] if shape[0] > 1 else max(D, st[0])), 0
     H = shape[1]
-    head = t.stride(1) if H > 1 else D
-    return (t.stride(0) if M > 1 else max(H * head, t.stride(0))), head
+    head = st[1] if H > 1 else D
+    return (st[0] if shape[0] > 1 else max(H * head, st[0])), head
 
 
 def op_rms_norm(x, weight=None, residual=None, rows_per_group=None, unit_offset=False, eps=1e-6, out_dtype=None, scale_block=None,
@@ -843,23 +843,26 @@ def op_rms_norm(x, weight=None, residual=None, rows_per_group=None, unit_offset=
     for every scale_block (128; None: the row's) columns.  Returns RmsNorm(y, scales, residual, rstd): residual is h in the residual's type,
     a new tensor unless residual_out is given (the residual itself: in place); rstd, fp32 with want_rstd, is what op_rms_norm_bwd
     needs.  out may be x."""
-    nd = x.dim()
+    shape = x.shape
+    nd = len(shape)
     if nd not in (2, 3):
         raise ValueError("x: expected [rows, D] or [tokens, heads, D]")
-    shape = x.shape
-    H, D = (shape[1] if nd == 3 else 1), shape[-1]
-    M = shape[0] * H
-    groups, rows = _groups(M, rows_per_group)
+    M, D, H = shape[0], shape[-1], 1
+    if nd == 3:
+        H = shape[1]
+        M *= H
+    groups, rows = (1, M) if rows_per_group is None else _groups(M, rows_per_group)
     dev = _device_of(x, weight, residual, out, residual_out)
     xc, (xt, xh) = _code(x.dtype), _tokens(x, shape, "x")
     ms = 0 if weight is None else _group_rows(weight, groups, D, "weight")
     if out is None:
         out = _like(x, x.dtype if out_dtype is None else _ACT.get(out_dtype, out_dtype))
-    elif out_dtype is not None and _ACT.get(out_dtype, out_dtype) != out.dtype:
-        raise ValueError("out_dtype: out has another type")
+        yt, yh = H * D, D
     else:
+        if out_dtype is not None and _ACT.get(out_dtype, out_dtype) != out.dtype:
+            raise ValueError("out_dtype: out has another type")
         _apart(out, "out", (x,), weight, residual)
-    yt, yh = _tokens(out, shape, "out")
+        yt, yh = _tokens(out, shape, "out")
     scales = None
     if out.dtype == torch.float8_e4m3fn:
         yc, runs = FREE_E4M3, 1
@@ -880,13 +883,13 @@ def op_rms_norm(x, weight=None, residual=None, rows_per_group=None, unit_offset=
             raise ValueError("residual: expected rows, not heads")
         rc, rs = _code(residual.dtype), _rows(residual, M, D, "residual")
         if residual_out is None:
-            residual_out = _like(residual, residual.dtype)
+            residual_out, hs = _like(residual, residual.dtype), D
         elif residual_out.dtype != residual.dtype:
             raise ValueError("residual_out: expected the residual's dtype")
         else:
             _apart(residual_out, "residual_out", (residual,), x, weight)
             _apart(residual_out, "residual_out", (), out)
-        hs = _rows(residual_out, M, D, "residual_out")
+            hs = _rows(residual_out, M, D, "residual_out")
     elif residual_out is not None:
         raise ValueError("residual_out: there is no residual")
     rstd = x.new_empty(M, dtype=torch.float32) if want_rstd else None
@@ -1072,42 +1075,42 @@ _CROSS = struct.Struct("<3Q9q4Q9if")
 
 def _cross_shape(q, k, v, kv_lens, kv_mask, kv_seq, kv_offsets, max_kv, scale):
     """(device, packed free_cross_attn) of a call, after the checks that both directions share."""
-    if q.dim() != 4 or (q.shape[3] > 1 and q.stride(3) != 1):
+    qshape, qs, kshape, ks, vs = q.shape, q.stride(), k.shape, k.stride(), v.stride()
+    if len(qs) != 4 or (qshape[3] > 1 and qs[3] != 1):
         raise ValueError("q: expected [n_seq, n_q, heads, d_head] with dense heads")
     packed = kv_offsets is not None
     nd = 3 if packed else 4
-    if k.dim() != nd or k.shape != v.shape or k.shape[-1] != q.shape[3] or (k.shape[-1] > 1 and (k.stride(-1) != 1 or v.stride(-1) != 1)):
+    n_seq, n_q, heads, d = qshape
+    if len(ks) != nd or kshape != v.shape or kshape[-1] != d or (d > 1 and (ks[-1] != 1 or vs[-1] != 1)):
         raise ValueError("k, v: expected [n_enc, n_kv, kv_heads, d_head] (with kv_offsets [rows, kv_heads, d_head]) with dense heads of q's size")
     if k.dtype != q.dtype or v.dtype != q.dtype:
         raise ValueError("k, v: expected q's dtype")
-    (n_seq, n_q, heads, d), kv_heads = q.shape, k.shape[-2]
+    kv_heads = kshape[-2]
     dev = _device_of(q, k, v, kv_lens, kv_mask, kv_seq, kv_offsets)
     if packed:
         if kv_lens is not None:
             raise ValueError("kv_lens: not with kv_offsets")
         _ints(kv_offsets, None, "kv_offsets")
-        n_enc, rows = kv_offsets.shape[0] - 1, k.shape[0]
+        n_enc, rows = kv_offsets.shape[0] - 1, kshape[0]
         if n_enc < 0:
             raise ValueError("kv_offsets: expected n_enc + 1 numbers")
         n_kv = rows if max_kv is None else min(int(max_kv), rows)
         if n_kv < 0:
             raise ValueError("max_kv: expected a length")
-        ks, vs = (0, *k.stride()), (0, *v.stride())
+        ks, vs = (0, *ks), (0, *vs)
     else:
         if max_kv is not None:
             raise ValueError("max_kv: only with kv_offsets")
-        n_enc, n_kv = k.shape[:2]
+        n_enc, n_kv = kshape[:2]
         rows = n_kv
         if kv_lens is not None:
             _ints(kv_lens, n_enc, "kv_lens")
-        ks, vs = k.stride(), v.stride()
-    if kv_mask is not None and (kv_mask.dtype not in (torch.bool, torch.uint8) or kv_mask.shape != k.shape[:nd - 2] or not kv_mask.is_contiguous()):
+    if kv_mask is not None and (kv_mask.dtype not in (torch.bool, torch.uint8) or kv_mask.shape != kshape[:nd - 2] or not kv_mask.is_contiguous()):
         raise ValueError("kv_mask: expected contiguous bool of the states' shape")
     if kv_seq is not None:
         _ints(kv_seq, n_seq, "kv_seq")
     elif n_seq % n_enc if n_enc else n_seq:
         raise ValueError(f"{n_seq} sequences do not share {n_enc} encoder sequences evenly: give kv_seq")
-    qs = q.stride()
     try:
         return dev, _CROSS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
                                 _adr(kv_lens) or 0, _adr(kv_offsets) or 0, _adr(kv_seq) or 0, _adr(kv_mask) or 0, _code(q.dtype), n_seq, n_q, heads,
@@ -1138,7 +1141,8 @@ def op_cross_attention(q, k, v, kv_lens=None, kv_mask=None, kv_seq=None, kv_offs
             raise ValueError("out: expected q's shape and dtype with dense heads")
         _device_of(q, out)
         _apart(out, "out", (), q, k, v)
-    lse = q.new_empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32) if want_lse else None
+    n_seq, n_q, heads, _ = q.shape
+    lse = q.new_empty((n_seq, heads, n_q), dtype=torch.float32) if want_lse else None
     need = (_LIB or lib()).free_op_cross_attention_workspace_bytes(shape)
     ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     ys = out.stride()
