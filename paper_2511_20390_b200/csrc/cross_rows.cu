@@ -9,15 +9,18 @@
 // with its own (row, state) and takes its exponential; the probabilities are then passed to all lanes of the group.  The parts of a
 // CTA's groups are joined through shared memory; long state sequences are split over CTAs as well and joined by cross_join_kernel.
 // Measured: 4 sequences of 77 states, 6 heads of 64: 4.4 us (8.7 by the tensor cores' kernel).  8 of up to 16384 states, 32 heads of 128
-// on 8: 84 us and 6 for the join, 4.3 TB/s of K and V, 0.62 of the issue slots (120 us with every score summed over all lanes).  What is
-// left are the ends: an SM holds three CTAs, and lengths that only the device knows fill the last round of them in part.
+// on 8: 78 us and 6 for the join, 4.6 TB/s of K and V, bound by issue slots (120 us with every score summed over all lanes).  What is left
+// are the ends: lengths that only the device knows fill the last round of CTAs in part.
 #include "cross_tc.cuh"
 
 namespace {
 
 using namespace cross_tc;
 
-constexpr int kThreads = 128, kWarps = kThreads / 32, kSms = 148, kSteps = 4;     // steps of copies in the ring
+constexpr int kThreads = 128, kWarps = kThreads / 32, kSms = 148;
+// Steps of copies in the ring.  Four rows: three, with 128 registers a thread, so that an SM holds four CTAs (8 of up to 16384 states 90 -> 84 us;
+// eight rows have no registers to spare, 33 -> 41 us for 2 x 8192 states, and one row with three steps 91 -> 98 us).
+template <int ROWS> constexpr int kStepsOf = ROWS == 4 ? 3 : 4;
 
 template <typename E> struct Unit;            // 16 bytes of a row, as pairs of fp32 numbers
 template <> struct Unit<float> {
@@ -47,7 +50,8 @@ template <typename E> __device__ __forceinline__ float power(float x) {
 }
 
 // R: rows held; L: lanes of a state's row
-template <typename E, int R, int L> __global__ void __launch_bounds__(kThreads) cross_rows_kernel(const CrossArgs a, const CrossParts parts) {
+template <typename E, int R, int L> __global__ void __launch_bounds__(kThreads, R == 4 ? 4 : 1) cross_rows_kernel(const CrossArgs a, const CrossParts parts) {
+    constexpr int kSteps = kStepsOf<R>;
     constexpr int V = Unit<E>::V, G = 32 / L, GROUPS = kWarps * G, KEYS = R <= 4 ? 4 : 2;
     extern __shared__ uint4 ring[];           // [step][warp][2 KEYS][lane]; at the end the groups' parts
     __shared__ float2 stats[GROUPS][R];       // maximum, sum
@@ -250,7 +254,7 @@ template <typename E, int R> int start(const CrossArgs& a, const CrossParts& par
     const long long ctas = (long long)a.n_seq * a.kv_heads * parts.n;
     if (ctas > 0x7fffffffLL) return FREE_ERR_UNSUPPORTED;
     auto kernel = units <= 4 ? cross_rows_kernel<E, R, 4> : units <= 8 ? cross_rows_kernel<E, R, 8> : units <= 16 ? cross_rows_kernel<E, R, 16> : cross_rows_kernel<E, R, 32>;
-    constexpr int copies = kSteps * kThreads * 2 * (R <= 4 ? 4 : 2) * 16, joined = kThreads * R * Unit<E>::V * 4, smem = copies > joined ? copies : joined;
+    constexpr int copies = kStepsOf<R> * kThreads * 2 * (R <= 4 ? 4 : 2) * 16, joined = kThreads * R * Unit<E>::V * 4, smem = copies > joined ? copies : joined;
     if (smem > 47 * 1024) FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     return free_launch(free_overlap_for_rows(a.n_seq), kernel, dim3((unsigned)ctas), dim3(kThreads), smem, s, a, parts);
 }
@@ -270,8 +274,7 @@ bool cross_rows_supported(int dtype, const CrossArgs& a) {
     return ok;
 }
 
-// Parts: enough CTAs for eight on every SM, 128 states each at least (the case above: six on every SM 88 us, twelve 92, 24 110; of equal
-// lengths 115, 111 with eight).
+// Parts: enough CTAs for eight on every SM, 128 states each at least (twelve took 2% longer, 24 a fifth).
 int cross_rows_parts(const CrossArgs& a) {
     const long long ctas = (long long)a.n_seq * a.kv_heads, most = (a.where.n_kv + 127) / 128;
     long long n = (8 * kSms + ctas - 1) / ctas;
