@@ -1166,8 +1166,8 @@ def op_cross_attention_bwd(q, k, v, out, lse, dout, kv_lens=None, kv_mask=None, 
     dq = _like(q, q.dtype) if want_dq else None
     dk = dv = None
     if want_dkv:
-        make = torch.empty_like if kv_offsets is None else torch.zeros_like       # packed rows that no sequence has
-        dk, dv = (make(k, memory_format=torch.contiguous_format) for _ in range(2))
+        # packed rows that no sequence has are zeros: both cleared in one launch
+        dk, dv = (_like(k, k.dtype), _like(v, k.dtype)) if kv_offsets is None else k.new_zeros((2, *k.shape)).unbind(0)
     need = lib().free_op_cross_attention_bwd_workspace_bytes(shape)
     ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     strides = lambda t: (0, 0, 0) if t is None else t.stride()[:3] if t.dim() == 4 else (0, *t.stride()[:2])

@@ -197,6 +197,41 @@ def test_layouts(n_q, n_kv, d, dt):
     assert torch.equal(free.op_cross_attention(q, k, v, kv_mask=mask), free.op_cross_attention(q, k, v, kv_mask=mask.to(torch.uint8) * 3))
 
 
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n_q", [1, 7, 140])
+def test_results_one_by_one_and_elsewhere(n_q, dt):
+    """Either gradient without the other, no lse, heads before tokens in the result: the same numbers."""
+    import paper_2511_20390_b200 as free
+    q, g = _t(10, 1, (4, n_q, 6, 64), dt), _t(10, 2, (4, n_q, 6, 64), dt)
+    k, v = _t(10, 3, (2, 200, 3, 64), dt), _t(10, 4, (2, 200, 3, 64), dt)
+    out, lse = free.op_cross_attention(q, k, v, want_lse=True)
+    assert torch.equal(free.op_cross_attention(q, k, v), out)
+    assert torch.equal(free.op_cross_attention(q, k, v, out=torch.empty(4, 6, n_q, 64, dtype=dt, device="cuda").transpose(1, 2)), out)
+    assert torch.equal(free.op_cross_attention(q, k, v, out=torch.empty(n_q, 6, 4, 64, dtype=dt, device="cuda").permute(2, 0, 1, 3)), out)
+    dq, dk, dv = free.op_cross_attention_bwd(q, k, v, out, lse, g)
+    one = free.op_cross_attention_bwd(q, k, v, out, lse, g, want_dkv=False)
+    two = free.op_cross_attention_bwd(q, k, v, out, lse, g, want_dq=False)
+    assert one[1] is None and one[2] is None and two[0] is None
+    assert torch.equal(one[0], dq) and torch.equal(two[1], dk) and torch.equal(two[2], dv)
+    assert free.op_cross_attention_bwd(q, k, v, out, lse, g, want_dq=False, want_dkv=False) == (None, None, None)
+    # one sequence of states for all, read in an order of its own, is what every sequence's own copy gives
+    seq = torch.tensor([1, 0, 0, 1], dtype=torch.int32, device="cuda")
+    got, lse2 = free.op_cross_attention(q, k, v, kv_seq=seq, want_lse=True)
+    pick = seq.long()
+    assert torch.equal(got, free.op_cross_attention(q, k[pick], v[pick]))
+    dks = free.op_cross_attention_bwd(q, k[pick], v[pick], got, lse2, g)[1].double()
+    dk2 = free.op_cross_attention_bwd(q, k, v, got, lse2, g, kv_seq=seq)[1].double()
+    # every copy's gradient is rounded, and their sum: half a step each; and sums of 4 n_q terms at most run in another order
+    f = lambda t: t.double().repeat_interleave(2, 2) if t.shape[2] == 3 else t.double()
+    p = torch.softmax(torch.einsum("sqhd,skhd->shqk", f(q), f(k[pick])) / 8, -1)
+    ds = p * (torch.einsum("sqhd,skhd->shqk", f(g), f(v[pick])) - (f(g) * f(got)).sum(-1).transpose(1, 2)[..., None]) / 8
+    terms = torch.einsum("shqk,sqhd->skhd", ds.abs(), f(q).abs()).view(4, 200, 3, 2, 64).sum(3)
+    half = torch.finfo(dt).eps / 2
+    add = lambda t: torch.zeros_like(dk2).index_add(0, pick, t)
+    want = add(dks)
+    assert ((dk2 - want).abs() <= half * 1.01 * (add(dks.abs()) + want.abs()) + (8 * n_q + 32) * U * add(terms) + 1e-30).all()
+
+
 @pytest.mark.parametrize("n_q,d", [(1, 36), (100, 36), (150, 20), (90, 68), (70, 100), (130, 127)])
 def test_heads_with_gaps(n_q, d):
     """Head sizes of no whole 16 bytes whose heads lie 16-byte aligned take the tensor cores; dense ones do not.  Both round p and dS or
