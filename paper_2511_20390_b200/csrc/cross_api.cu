@@ -174,7 +174,9 @@ extern "C" int free_op_cross_attention_bwd(const free_cross_attn* c, const void*
     if (!empty && (dq || dk)) FREE_TRY(cross_delta(c->dtype, a, s));
     // the tensor cores where the tile copies take every matrix (an empty call only writes zeros)
     const bool tc = c->dtype == FREE_BF16 && !empty && cross_bwd_tc_supported(a);
-    if (!empty && dq) FREE_TRY(tc && cross_tc::mappable(a.dq, c->n_seq, c->n_q, c->heads) ? cross_bwd_tc_dq(a, s) : cross_simt_dq(c->dtype, a, s));
+    // (more than a million tiles of states are over a second's work for an item, whose waits give up after two)
+    if (!empty && dq)
+        FREE_TRY(tc && c->n_kv >> 6 <= 1 << 20 && cross_tc::mappable(a.dq, c->n_seq, c->n_q, c->heads) ? cross_bwd_tc_dq(a, s) : cross_simt_dq(c->dtype, a, s));
     if (dk && states(c)) {
         float* parts = empty ? nullptr : (float*)((char*)ws + stat_bytes(c) + kNextBytes);
         if (tc && cross_tc::mappable(a.dk, enc, rows, c->kv_heads) && cross_tc::mappable(a.dv, enc, rows, c->kv_heads))

@@ -679,14 +679,16 @@ bool cross_bwd_tc_supported(const CrossArgs& c) {
     return mappable(c.q, c.n_seq, c.n_q, c.heads) && mappable(c.g, c.n_seq, c.n_q, c.heads) && mappable(c.k, enc, rows, c.kv_heads) && mappable(c.v, enc, rows, c.kv_heads);
 }
 
-// Parts of the tokens' tiles where the blocks of states leave SMs without one: two tiles at least, an fp32 row of dk and dv each.
+// Parts of the tokens' tiles where the blocks of states leave SMs without one: two tiles at least, an fp32 row of dk and dv each.  Items of
+// more than a million tiles, a second's work, are split too: waits for them give up after two.
 int cross_bwd_tc_parts(const CrossArgs& c) {
     const long long items = (long long)c.where.n_enc * c.kv_heads * ((c.where.n_kv + BR - 1) / BR);
-    const long long tiles = (long long)c.n_seq * c.group * ((c.n_q + BC - 1) / BC) / (c.where.n_enc > 0 ? c.where.n_enc : 1);
-    if (items >= kSms) return 1;
-    long long p = (2 * kSms + items - 1) / items;
+    const long long all = (long long)c.n_seq * c.group * ((c.n_q + BC - 1) / BC), tiles = all / (c.where.n_enc > 0 ? c.where.n_enc : 1);
+    long long p = items >= kSms || items < 1 ? 1 : (2 * kSms + items - 1) / items;
     if (p > tiles / 2) p = tiles / 2;
     if (p > cross_parts_held(c)) p = cross_parts_held(c);
+    const long long least = ((c.where.seq_of ? all : tiles) + (1 << 20) - 1) >> 20;
+    if (p < least) p = least;
     return p < 1 ? 1 : (int)p;
 }
 

@@ -606,7 +606,8 @@ void shape_of(const CrossArgs& a, int* tiles, int* pairs, int* parts) {
     const int most = (a.where.n_kv + 8 * BK - 1) / (8 * BK);
     long long want = items >= kSms ? 1 : (4 * kSms + items - 1) / items;
     if (want > most) want = most;
-    *parts = want < 1 ? 1 : (int)want;
+    const int least = ((a.where.n_kv + BK - 1) / BK >> 20) + 1;      // a million blocks are a second's work: waits for an item give up after two
+    *parts = want < least ? least : (int)want;
 }
 
 }  // namespace

@@ -111,6 +111,11 @@ def test_cross_attention_bwd(L):
         for rows, n_kv, d in ((1 << 20, 64, 64), (100, 100, 128), (3000, 3000, 40), (1 << 24, 1, 8)):
             n = L.free_op_cross_attention_bwd_workspace_bytes(_pack(dtype=dt, n_seq=1, n_enc=1, n_q=4096, kv_offsets=P, kv_rows=rows, n_kv=n_kv, d_head=d, kv_heads=1))
             assert 0 < n <= (64 << 20) + 1024 + 2 * 4096 * 4
+    # and items of millions of tiles are split whatever the blocks of states
+    many = dict(n_seq=1 << 20, n_enc=1, n_q=128, heads=1, kv_heads=1, n_kv=20000, kv_rows=20000, q_seq=128 * 64, q_tok=64, k_seq=20000 * 64, v_seq=20000 * 64)
+    rows = (1 << 20) * 128 * 4
+    assert L.free_op_cross_attention_bwd_workspace_bytes(_pack(**many)) >= rows + 2 * 2 * 20000 * 64 * 4
+    assert L.free_op_cross_attention_bwd_workspace_bytes(_pack(**{**many, "n_seq": 1 << 12})) < (1 << 12) * 128 * 4 + 1024
     # nothing to be written: no gradient wanted, or no token and no state
     assert _bwd(L, n_seq=0, n_enc=0, q=0, k=0, v=0, out=None, lse=None, g=None, dq=None, ws=None, err=None) == 0
     assert _bwd(L, n_q=0, n_kv=0, out=None, lse=None, g=None, dq=None, ws=None, err=None) == 0
