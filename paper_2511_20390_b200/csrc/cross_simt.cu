@@ -176,7 +176,7 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
 #pragma unroll
         for (int i = 0; i < 4 * ND; ++i) acc[r][i] *= inv;
         const int row = q0 + 4 * ty + r;
-        if (a.lse && tx == 0 && row < a.n_q) a.lse[((long long)s * a.heads + h) * a.n_q + row] = top[r] == -INFINITY ? -INFINITY : top[r] + logf(sum[r]);
+        if (a.lse && tx == 0 && row < a.n_q) a.lse[((long long)s * a.heads + h) * a.n_q + row] = sum[r] == 0.f ? -INFINITY : top[r] + logf(sum[r]);
     }
     store_rows<E, ND>(at_out<E>(a.o, s, 0, h), a.o.tok, q0, a.n_q, d, ty, tx, acc);
 }

@@ -10,6 +10,7 @@
 //     as soon as they are in registers, so the two products and the softmax of a tile run beside one another.
 //   - V is the right operand as it lies in memory (contraction along its rows), so nothing is transposed.
 //   - The maximum that p is taken against moves only when it has grown by 2^8; then O is rescaled in tensor memory.
+//   - Maxima leave NaN out, sums do not: a row without a state is one whose sum is zero, and a NaN that counts reaches out and lse.
 //   - The last block of a sequence costs the 16-column steps that it has.  States that do not count: scores are replaced by -inf, and the
 //     rows of V are zeroed in shared memory (0 x NaN would be NaN).
 // Long states and few rows: the states are split into parts, each with its own softmax, joined by cross_join_kernel.
@@ -315,7 +316,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 const bool row_ok = row_t < a.tt && t < a.n_q;
                 const long long row = ((long long)it.s * a.heads + h) * a.n_q + t;
                 if (row_ok && (a.parts > 1 || a.lse)) {
-                    const float lse = top == -INFINITY ? -INFINITY : top * a.scale + logf(sum);
+                    const float lse = sum == 0.f ? -INFINITY : top * a.scale + logf(sum);
                     if (a.parts > 1) a.part_lse[it.part * a.rows + row] = lse;
                     else a.lse[row] = lse;
                 }
@@ -529,7 +530,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     if (warp == 12) { tc::tc_fence_after(); tc::tmem_dealloc(tmem, kTmemCols); }
 }
 
-// out, lse of a row from its parts' own: a CTA per row, the parts' weights in shared memory, a slice of the parts per channel and 128 threads.
+// out, lse of a row from its parts' own (NaN where a part's lse is): a CTA per row, the parts' weights in shared memory, a slice of the parts per channel and 128 threads.
 constexpr int kMaxParts = 2048;
 template <typename E, int THREADS> __global__ void __launch_bounds__(THREADS) cross_join_kernel(const CrossArgs a, const CrossParts p, long long rows) {
     constexpr int SLICES = THREADS / 128, WARPS = THREADS / 32;
@@ -552,7 +553,7 @@ template <typename E, int THREADS> __global__ void __launch_bounds__(THREADS) cr
     __syncthreads();
     float sum = 0.f;
     for (int k = threadIdx.x; k < p.n; k += THREADS) {
-        weight[k] = top == -INFINITY ? 0.f : expf(weight[k] - top);       // 0: a part without a state, which wrote nothing else
+        weight[k] = weight[k] == -INFINITY ? 0.f : expf(weight[k] - top);       // 0: a part without a state, which wrote nothing else
         sum += weight[k];
     }
     sum = free_warp_sum(sum);
@@ -583,7 +584,7 @@ template <typename E, int THREADS> __global__ void __launch_bounds__(THREADS) cr
         if constexpr (sizeof(E) == 4) out[ch] = v;
         else out[ch] = __float2bfloat16(v);
     }
-    if (a.lse && threadIdx.x == 0) a.lse[i] = top == -INFINITY ? -INFINITY : top + logf(sum);
+    if (a.lse && threadIdx.x == 0) a.lse[i] = sum == 0.f ? -INFINITY : top + logf(sum);
 }
 
 int tokens_per_tile(const CrossArgs& a) { return BQ / a.group; }
