@@ -623,7 +623,9 @@ int free_op_rope_axes(int dtype, int pairing, int freq_mode, int inverse, int n_
  *   kv_lens    DEVICE int32 [n_enc] or NULL: states of each encoder sequence, taken as 0 .. n_kv (NULL: n_kv)
  *   kv_offsets DEVICE int32 [n_enc + 1] or NULL.  Not NULL: the states lie one behind the other in kv_rows rows (k_seq and
  *              v_seq are not used) and sequence e has the rows kv_offsets[e] .. kv_offsets[e + 1] - 1, at most n_kv of them;
- *              parts outside 0 .. kv_rows - 1 do not count.  kv_lens has to be NULL
+ *              parts outside 0 .. kv_rows - 1 do not count.  kv_lens has to be NULL.  Offsets do not decrease, so that no row is
+ *              two sequences': where they do, out and lse are still those of the rows that every sequence names, but which
+ *              gradient of the backward pass the rows named twice get, and whether any row gets one, is undefined
  *   kv_mask    DEVICE, one byte per state, [n_enc, n_kv] or [kv_rows], or NULL: states with a zero do not count
  *   kv_seq     DEVICE int32 [n_seq] or NULL: e(s), outside 0 .. n_enc - 1 for none.  NULL: n_seq is a multiple of n_enc, and
  *              n_seq / n_enc consecutive sequences share one (the drafts of an image share its prompt)

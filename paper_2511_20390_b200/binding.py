@@ -1128,8 +1128,8 @@ def op_cross_attention(q, k, v, kv_lens=None, kv_mask=None, kv_seq=None, kv_offs
     """Attention of tokens q (CUDA fp32 or bf16 [n_seq, n_q, heads, d_head], any strides with dense heads, d_head up to 128) to an
     encoder's states k, v [n_enc, n_kv, kv_heads, d_head] (heads a multiple of kv_heads; views into a packed projection are fine).
     Encoder sequence e has kv_lens[e] states (int32, default n_kv); with kv_offsets (int32 [n_enc + 1]) the states are packed, k and v
-    [rows, kv_heads, d_head], and sequence e has the rows kv_offsets[e] .. kv_offsets[e + 1] - 1, at most max_kv (default: all).  States
-    whose kv_mask is False do not count either.  Sequence s reads encoder sequence kv_seq[s] (int32); by default n_seq / n_enc consecutive
+    [rows, kv_heads, d_head], and sequence e has the rows kv_offsets[e] .. kv_offsets[e + 1] - 1, at most max_kv (default: all); offsets must
+    not decrease, or dk and dv of the backward pass are undefined.  States whose kv_mask is False do not count either.  Sequence s reads encoder sequence kv_seq[s] (int32); by default n_seq / n_enc consecutive
     sequences share one.  scale defaults to d_head ** -0.5.  Returns out like q, zero for tokens without a state, and with want_lse also
     the log of the sums of exponentials, fp32 [n_seq, heads, n_q] (-inf for those), what op_cross_attention_bwd needs.  Asynchronous:
     op_device_error() tells whether a device-side wait gave up."""
