@@ -17,16 +17,18 @@ struct CrossWhere {
     int n_enc, n_kv, kv_rows, share;          // share: consecutive sequences that read one encoder sequence (seq_of == nullptr)
 };
 
-struct CrossSpan { int enc, row0, len; };     // states row0 .. row0 + len - 1 of encoder sequence `enc` (0 where packed)
+// States row0 .. row0 + len - 1 of encoder sequence `enc` (0 where packed); rows: those that it has, len of them at most can count
+struct CrossSpan { int enc, row0, len, rows; };
 
 __device__ __forceinline__ CrossSpan cross_span_of_enc(const CrossWhere& w, int e) {
-    if ((unsigned)e >= (unsigned)w.n_enc) return CrossSpan{0, 0, 0};
+    if ((unsigned)e >= (unsigned)w.n_enc) return CrossSpan{0, 0, 0, 0};
     if (w.offsets) {
         const int b = __ldg(w.offsets + e), n = __ldg(w.offsets + e + 1);
         const int lo = max(b, 0), hi = min(n, w.kv_rows);
-        return CrossSpan{0, lo, lo < hi ? min(hi - lo, w.n_kv) : 0};
+        const int rows = lo < hi ? hi - lo : 0;
+        return CrossSpan{0, lo, min(rows, w.n_kv), rows};
     }
-    return CrossSpan{e, 0, w.lens ? min(max(__ldg(w.lens + e), 0), w.n_kv) : w.n_kv};
+    return CrossSpan{e, 0, w.lens ? min(max(__ldg(w.lens + e), 0), w.n_kv) : w.n_kv, w.n_kv};
 }
 __device__ __forceinline__ int cross_enc_of(const CrossWhere& w, int s) { return w.seq_of ? __ldg(w.seq_of + s) : s / w.share; }
 __device__ __forceinline__ CrossSpan cross_span(const CrossWhere& w, int s) { return cross_span_of_enc(w, cross_enc_of(w, s)); }
@@ -34,6 +36,9 @@ __device__ __forceinline__ CrossSpan cross_span(const CrossWhere& w, int s) { re
 __device__ __forceinline__ const uint8_t* cross_mask(const CrossWhere& w, const CrossSpan& sp) {
     return w.mask ? w.mask + (w.offsets ? (long long)sp.row0 : (long long)sp.enc * w.n_kv) : nullptr;
 }
+
+// dk, dv: blocks of B states of an encoder sequence.  The last takes the rows of a packed sequence behind n_kv with it, whose gradients are zero.
+__host__ __device__ __forceinline__ int cross_blocks(const CrossWhere& w, int B) { return w.n_kv > 0 ? (w.n_kv - 1) / B + 1 : 1; }
 
 // Parts of the states of a call with few tokens (cross_join adds them): part p of row r = (sequence, head, token)
 struct CrossParts {

@@ -23,7 +23,8 @@ int check(const free_cross_attn* c, bool* empty) {
     *empty = c->n_seq == 0 || c->n_q == 0;
     return FREE_OK;
 }
-bool states(const free_cross_attn* c) { return c->n_enc > 0 && c->n_kv > 0 && (!c->kv_offsets || c->kv_rows > 0); }
+bool rows_of_states(const free_cross_attn* c) { return c->n_enc > 0 && (c->kv_offsets ? c->kv_rows : c->n_kv) > 0; }
+bool states(const free_cross_attn* c) { return rows_of_states(c) && c->n_kv > 0; }
 
 int pointers(const free_cross_attn* c, bool tokens) {              // (a call without tokens reads the states still: which of them count)
     const int e = c->dtype == FREE_FP32 ? 4 : 2;
@@ -148,7 +149,7 @@ extern "C" int free_op_cross_attention_bwd(const free_cross_attn* c, const void*
     const int e = c->dtype == FREE_FP32 ? 4 : 2;
     if (!dk != !dv) return FREE_ERR_ARG;
     const int enc = c->kv_offsets ? 1 : c->n_enc, rows = c->kv_offsets ? c->kv_rows : c->n_kv;
-    if (dk && states(c)) {
+    if (dk && rows_of_states(c)) {
         FREE_TRY(pointers(c, !empty));
         FREE_TRY(result(dk, e, c->kv_offsets ? 0 : dk_seq, dk_tok, dk_head, enc, rows, c->kv_heads, c->d_head));
         FREE_TRY(result(dv, e, c->kv_offsets ? 0 : dv_seq, dv_tok, dv_head, enc, rows, c->kv_heads, c->d_head));
@@ -177,7 +178,7 @@ extern "C" int free_op_cross_attention_bwd(const free_cross_attn* c, const void*
     // (more than a million tiles of states are over a second's work for an item, whose waits give up after two)
     if (!empty && dq)
         FREE_TRY(tc && c->n_kv >> 6 <= 1 << 20 && cross_tc::mappable(a.dq, c->n_seq, c->n_q, c->heads) ? cross_bwd_tc_dq(a, s) : cross_simt_dq(c->dtype, a, s));
-    if (dk && states(c)) {
+    if (dk && rows_of_states(c)) {
         float* parts = empty ? nullptr : (float*)((char*)ws + stat_bytes(c) + kNextBytes);
         if (tc && cross_tc::mappable(a.dk, enc, rows, c->kv_heads) && cross_tc::mappable(a.dv, enc, rows, c->kv_heads))
             FREE_TRY(cross_bwd_tc_dkv(a, cross_bwd_tc_parts(a), parts, s));

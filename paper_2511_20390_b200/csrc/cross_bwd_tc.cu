@@ -63,7 +63,7 @@ struct Args {
 struct alignas(16) Item {
     int live, idx, head, row0;                // idx: sequence (dq) or encoder sequence (dk, dv); head: of the rows; row0: first row's token or state
     int tiles, part, enc, row;                // column tiles; enc, row: where the first state lies
-    int left, first, limit, kv_head;          // states from `row` on; first column tile of the part; rows that are written
+    int left, first, limit, kv_head;          // states from `row` on; first column tile of the part; rows that are written (the last block of states: behind it, too)
 };
 
 template <bool DKV> __device__ __forceinline__ int sequences_of(const Args& a, int e) {      // that read encoder sequence e; whole warp
@@ -91,7 +91,7 @@ template <bool DKV> __device__ __forceinline__ Item item_of(const Args& a, long 
         const CrossSpan sp = cross_span_of_enc(a.where, it.idx);
         it.row0 = blk * BR;
         it.enc = sp.enc; it.row = sp.row0 + it.row0; it.left = sp.len - it.row0;
-        it.limit = (a.where.offsets ? sp.len : a.where.n_kv) - it.row0;
+        it.limit = blk + 1 < a.blocks ? min(sp.rows - it.row0, BR) : sp.rows - it.row0;
         if (it.left > 0) {
             const long long all = (long long)sequences_of<DKV>(a, it.idx) * a.group * ((a.n_q + BC - 1) / BC);
             it.first = (int)(all * it.part / a.parts);
@@ -605,8 +605,8 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
             // ------------------------------------------------------------------ rows that nothing reaches
             for (long long i = blockIdx.x; i < a.items; i += gridDim.x) {
                 const Item it = item_of<DKV>(a, i);
-                if (it.tiles > 0) continue;
-                const int rows = it.limit < BR ? it.limit : BR, seq = DKV ? it.enc : it.idx, tok0 = DKV ? it.row : it.row0;
+                const int skip = it.tiles > 0 ? BR : 0, rows = (DKV || it.limit < BR ? it.limit : BR) - skip, seq = DKV ? it.enc : it.idx, tok0 = (DKV ? it.row : it.row0) + skip;
+                if (rows <= 0) continue;
                 for (int o = 0; o < (DKV ? 2 : 1); ++o) {
                     const CrossMat& mat = o ? a.o2 : a.o1;
                     if (a.parts > 1)
@@ -630,18 +630,22 @@ template <typename E> __global__ void __launch_bounds__(256) cross_bwd_join_kern
     free_grid_dep_wait();
     free_grid_dep_launch();
     const int lane = threadIdx.x & 31;
-    const long long all = (long long)a.where.n_enc * a.where.n_kv * a.kv_heads;
-    for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += (long long)gridDim.x * 8) {
-        const int h = (int)(i % a.kv_heads), j = (int)(i / a.kv_heads % a.where.n_kv), e = (int)(i / a.kv_heads / a.where.n_kv);
-        const CrossSpan sp = cross_span_of_enc(a.where, e);
-        if (a.where.offsets && j >= sp.len) continue;
-        const long long row = ((long long)sp.enc * a.where.kv_rows + sp.row0 + j) * a.kv_heads + h;
+    // packed: the rows from the first sequence's first to the last's last
+    long long first = 0, last = (long long)a.where.n_enc * a.where.n_kv;
+    if (a.where.offsets) {
+        first = min(max(__ldg(a.where.offsets), 0), a.where.kv_rows);
+        last = min(max(__ldg(a.where.offsets + a.where.n_enc), 0), a.where.kv_rows);
+    }
+    for (long long i = first * a.kv_heads + (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < last * a.kv_heads; i += (long long)gridDim.x * 8) {
+        const int h = (int)(i % a.kv_heads);
+        const long long row = i / a.kv_heads;
+        const int e = a.where.offsets ? 0 : (int)(row / a.where.n_kv), j = (int)(row - (long long)e * a.where.n_kv);
         for (int o = 0; o < 2; ++o) {
             const CrossMat& mat = o ? a.dv : a.dk;
-            E* dst = reinterpret_cast<E*>(const_cast<void*>(mat.p)) + sp.enc * mat.seq + (long long)(sp.row0 + j) * mat.tok + h * mat.head;
+            E* dst = reinterpret_cast<E*>(const_cast<void*>(mat.p)) + e * mat.seq + j * mat.tok + h * mat.head;
             for (int c = lane; c < a.d; c += 32) {
                 float v = 0.f;
-                for (int p = 0; p < parts; ++p) v += part_out[(((long long)p * 2 + o) * part_rows + row) * a.d + c];
+                for (int p = 0; p < parts; ++p) v += part_out[(((long long)p * 2 + o) * part_rows + i) * a.d + c];
                 if constexpr (sizeof(E) == 4) dst[c] = v;
                 else dst[c] = __float2bfloat16(v);
             }
@@ -682,7 +686,7 @@ bool cross_bwd_tc_supported(const CrossArgs& c) {
 // Parts of the tokens' tiles where the blocks of states leave SMs without one: two tiles at least, an fp32 row of dk and dv each.  Items of
 // more than a million tiles, a second's work, are split too: waits for them give up after two.
 int cross_bwd_tc_parts(const CrossArgs& c) {
-    const long long items = (long long)c.where.n_enc * c.kv_heads * ((c.where.n_kv + BR - 1) / BR);
+    const long long items = (long long)c.where.n_enc * c.kv_heads * cross_blocks(c.where, BR);
     const long long all = (long long)c.n_seq * c.group * ((c.n_q + BC - 1) / BC), tiles = all / (c.where.n_enc > 0 ? c.where.n_enc : 1);
     long long p = items >= kSms || items < 1 ? 1 : (2 * kSms + items - 1) / items;
     if (p > tiles / 2) p = tiles / 2;
@@ -713,7 +717,7 @@ int cross_bwd_tc_dq(const CrossArgs& c, cudaStream_t s) {
 int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_t s) {
     Args a = args_of(c);
     const int enc = c.where.offsets ? 1 : c.where.n_enc, rows = c.where.kv_rows;
-    a.blocks = (c.where.n_kv + BR - 1) / BR;
+    a.blocks = cross_blocks(c.where, BR);
     a.parts = parts; a.part_out = part_out; a.part_rows = (long long)enc * rows * c.kv_heads;
     a.items = (long long)c.where.n_enc * c.kv_heads * a.blocks * parts;
     a.next = c.next;
@@ -733,7 +737,7 @@ int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_
 }
 
 int cross_bwd_join(int dtype, const CrossArgs& c, int parts, const float* part_out, cudaStream_t s) {
-    const long long n = (long long)c.where.n_enc * c.where.n_kv * c.kv_heads, ctas = (n + 7) / 8;
+    const long long n = (c.where.offsets ? c.where.kv_rows : (long long)c.where.n_enc * c.where.n_kv) * c.kv_heads, ctas = (n + 7) / 8;
     const long long rows = (long long)(c.where.offsets ? 1 : c.where.n_enc) * c.where.kv_rows * c.kv_heads;
     auto kernel = dtype == FREE_FP32 ? cross_bwd_join_kernel<float> : cross_bwd_join_kernel<__nv_bfloat16>;
     return free_launch(false, kernel, dim3((unsigned)(ctas < kSms * 8 ? ctas : kSms * 8)), dim3(256), 0, s, c, parts, part_out, rows);

@@ -102,6 +102,10 @@ template <typename E, int ND> __device__ __forceinline__ void store_rows(E* base
             }
     }
 }
+template <typename E> __device__ __forceinline__ void zero_rows(E* base, long long stride, int r0, int rows, int d) {
+    for (int r = r0 + (int)(threadIdx.x >> 5); r < rows; r += kThreads / 32)
+        for (int c = threadIdx.x & 31; c < d; c += 32) base[(long long)r * stride + c] = E(0.f);
+}
 template <typename E> __device__ __forceinline__ const E* at(const CrossMat& m, int s, long long row, int h) {
     return reinterpret_cast<const E*>(m.p) + s * m.seq + row * m.tok + h * m.head;
 }
@@ -332,11 +336,11 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
     extern __shared__ float smem[];
     const int d = a.d, P = pitch(d);
     float *K = smem, *V = K + T * P, *Q = V + T * P, *G = Q + T * P, *W = G + T * P, *L = W + T * PS, *D = L + T;
-    const int tiles = (a.where.n_kv + T - 1) / T;
+    const int tiles = cross_blocks(a.where, T);
     const int part = (int)(blockIdx.x % parts), te = (int)(blockIdx.x / parts), tile = te % tiles, eh = te / tiles, kh = eh % a.kv_heads, e = eh / a.kv_heads;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, j0 = tile * T;
     const CrossSpan sp = cross_span_of_enc(a.where, e);
-    const int rows = a.where.offsets ? sp.len : a.where.n_kv;      // rows that are written
+    const int rows = tile + 1 < tiles ? min(sp.rows, j0 + T) : sp.rows;      // that are written up to
     if (j0 >= rows) return;
     const uint8_t* mask = cross_mask(a.where, sp);
     auto counts = [&](int j) { return j < sp.len && (!mask || mask[j]); };
@@ -413,10 +417,14 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
         float* out = part_out + 2 * part * all + (((long long)sp.enc * a.where.kv_rows + sp.row0) * a.kv_heads + kh) * d;
         store_rows<float, ND>(out, step, j0, rows, d, ty, tx, dk);
         store_rows<float, ND>(out + all, step, j0, rows, d, ty, tx, dv);
+        zero_rows(out, step, j0 + T, rows, d);
+        zero_rows(out + all, step, j0 + T, rows, d);
         return;
     }
     store_rows<E, ND>(at_out<E>(a.dk, sp.enc, sp.row0, kh), a.dk.tok, j0, rows, d, ty, tx, dk);
     store_rows<E, ND>(at_out<E>(a.dv, sp.enc, sp.row0, kh), a.dv.tok, j0, rows, d, ty, tx, dv);
+    zero_rows(at_out<E>(a.dk, sp.enc, sp.row0, kh), a.dk.tok, j0 + T, rows, d);
+    zero_rows(at_out<E>(a.dv, sp.enc, sp.row0, kh), a.dv.tok, j0 + T, rows, d);
 }
 
 template <typename K, typename... A> int launch(K kernel, long long ctas, int tiles_held, int extra, cudaStream_t s, const CrossArgs& a, A... rest) {
@@ -465,7 +473,7 @@ int cross_simt_dq(int dtype, const CrossArgs& a, cudaStream_t s) {
     return a.d <= 64 ? launch(cross_simt_dq_kernel<__nv_bfloat16, 1>, q_tiles(a), 4, 0, s, a) : launch(cross_simt_dq_kernel<__nv_bfloat16, 2>, q_tiles(a), 4, 0, s, a);
 }
 namespace {
-long long dkv_items(const CrossArgs& a) { return (long long)((a.where.n_kv + T - 1) / T) * a.where.n_enc * a.kv_heads; }
+long long dkv_items(const CrossArgs& a) { return (long long)cross_blocks(a.where, T) * a.where.n_enc * a.kv_heads; }
 }  // namespace
 
 // Parts of the tokens where the blocks of states leave SMs without one (all gradients of 2 x 512 tokens, 8 heads of 64, 300 states: 158 ->
