@@ -37,8 +37,45 @@ __device__ __forceinline__ const uint8_t* cross_mask(const CrossWhere& w, const 
     return w.mask ? w.mask + (w.offsets ? (long long)sp.row0 : (long long)sp.enc * w.n_kv) : nullptr;
 }
 
-// dk, dv: blocks of B states of an encoder sequence.  The last takes the rows of a packed sequence behind n_kv with it, whose gradients are zero.
-__host__ __device__ __forceinline__ int cross_blocks(const CrossWhere& w, int B) { return w.n_kv > 0 ? (w.n_kv - 1) / B + 1 : 1; }
+// dk, dv: blocks of B states of every encoder sequence and key head.  Either as many of every sequence, `per` for n_kv states, of which the
+// last takes the rows of a packed sequence behind n_kv with it, whose gradients are zero; or (per = 0) of all its rows, packed ones only:
+// a sequence's begin at number (its first row) / B + (its index), counted from the first sequence's, which leaves each the blocks that it needs
+// (n rows from row a on are at most (a + n) / B - a / B + 1), so that there are n_enc + kv_rows / B of them however long a single one may be.
+inline int cross_blocks_per(const CrossWhere& w, int B) {          // whichever are fewer
+    const int per = w.n_kv > 0 ? (w.n_kv - 1) / B + 1 : 1;
+    return w.offsets && w.n_enc + (long long)(w.kv_rows / B) < (long long)w.n_enc * per ? 0 : per;
+}
+inline long long cross_blocks(const CrossWhere& w, int B) {
+    const int per = cross_blocks_per(w, B);
+    return per ? (long long)w.n_enc * per : w.n_enc + (long long)(w.kv_rows / B);
+}
+struct CrossBlock {
+    int e, head, row0;                        // encoder sequence, key head and the block's first of the sequence's rows; row0 < 0: no block
+    bool more, last;                          // more = false: there are no blocks from this one on
+};
+template <int B> __device__ __forceinline__ CrossBlock cross_block(const CrossWhere& w, int kv_heads, int per, long long i) {     // whole warp, the same block
+    if (per) {
+        const int blk = (int)(i % per);
+        const long long eh = i / per;
+        return CrossBlock{(int)(eh / kv_heads), (int)(eh % kv_heads), blk * B, true, blk + 1 == per};
+    }
+    const int head = (int)(i % kv_heads);
+    i /= kv_heads;
+    auto first = [&](int e) { return min(max(__ldg(w.offsets + e), 0), w.kv_rows) / B; };
+    i += first(0);
+    if (i >= (long long)first(w.n_enc) + w.n_enc) return CrossBlock{0, head, -1, false, false};
+    // the last sequence that begins at i or before: a warp looks at 32 of those that are left
+    int e = 0;
+    for (int n = w.n_enc; n > 1;) {
+        const int step = (n + 31) / 32, at = (int)(threadIdx.x & 31) * step;
+        const unsigned before = __ballot_sync(0xffffffffu, at < n && first(e + min(at, n - 1)) + (long long)(e + at) <= i);
+        const int skip = before ? (31 - __clz(before)) * step : 0;
+        e += skip;
+        n = min(step, n - skip);
+    }
+    const long long row0 = (i - e - first(e)) * B;                 // (offsets that decrease may leave none)
+    return CrossBlock{e, head, row0 < w.kv_rows ? (int)max(row0, -1LL) : -1, true, false};
+}
 
 // Parts of the states of a call with few tokens (cross_join adds them): part p of row r = (sequence, head, token)
 struct CrossParts {

@@ -19,7 +19,9 @@ int check(const free_cross_attn* c, bool* empty) {
         if (v < 0) return FREE_ERR_SHAPE;
     if (c->d_head > kCrossMaxD) return FREE_ERR_UNSUPPORTED;
     // rows of lse, tiles and tile copies' coordinates are counted in 31 bits
-    if ((long long)c->n_seq * c->heads > 0x7fffffffLL / (c->n_q / 64 + 1) || (long long)c->n_enc * c->kv_heads > 0x7fffffffLL / (c->n_kv / 64 + 1)) return FREE_ERR_UNSUPPORTED;
+    long long blocks = (long long)c->n_enc * (c->n_kv / 64 + 1);
+    if (c->kv_offsets && blocks > c->n_enc + (long long)(c->kv_rows / 64)) blocks = c->n_enc + (long long)(c->kv_rows / 64);
+    if ((long long)c->n_seq * c->heads > 0x7fffffffLL / (c->n_q / 64 + 1) || blocks > 0x7fffffffLL / c->kv_heads) return FREE_ERR_UNSUPPORTED;
     *empty = c->n_seq == 0 || c->n_q == 0;
     return FREE_OK;
 }

@@ -49,7 +49,7 @@ struct Args {
     CrossWhere where;
     int n_seq, n_q, heads, kv_heads, d, group;
     int q_seq_mul, q_head_mul, g_seq_mul, g_head_mul, k_seq_mul, k_head_mul, v_seq_mul, v_head_mul;     // 0 where one matrix serves all
-    int blocks, parts;                        // row blocks of a (sequence, head) or (encoder sequence, key head); parts of the columns
+    int blocks, parts;                        // row blocks of a (sequence, head), or cross_block's of an encoder sequence; parts of the columns
     long long items;
     float c, scale;
     const float *lse, *delta;
@@ -82,22 +82,20 @@ template <bool DKV> __device__ __forceinline__ Item item_of(const Args& a, long 
     it.tiles = it.part = it.first = 0;
     if (!it.live) return it;
     if (DKV) {
-        it.part = (int)(i % a.parts); i /= a.parts;
-    }
-    const int blk = (int)(i % a.blocks); i /= a.blocks;
-    if (DKV) {
-        it.head = it.kv_head = (int)(i % a.kv_heads);
-        it.idx = (int)(i / a.kv_heads);
+        it.part = (int)(i % a.parts);
+        const CrossBlock b = cross_block<BR>(a.where, a.kv_heads, a.blocks, i / a.parts);
+        it.live = b.more; it.idx = b.e; it.head = it.kv_head = b.head; it.row0 = b.row0; it.limit = 0;
+        if (b.row0 < 0) return it;
         const CrossSpan sp = cross_span_of_enc(a.where, it.idx);
-        it.row0 = blk * BR;
         it.enc = sp.enc; it.row = sp.row0 + it.row0; it.left = sp.len - it.row0;
-        it.limit = blk + 1 < a.blocks ? min(sp.rows - it.row0, BR) : sp.rows - it.row0;
+        it.limit = b.last ? sp.rows - it.row0 : min(sp.rows - it.row0, BR);
         if (it.left > 0) {
             const long long all = (long long)sequences_of<DKV>(a, it.idx) * a.group * ((a.n_q + BC - 1) / BC);
             it.first = (int)(all * it.part / a.parts);
             it.tiles = (int)(all * (it.part + 1) / a.parts) - it.first;
         }
     } else {
+        const int blk = (int)(i % a.blocks); i /= a.blocks;
         it.head = (int)(i % a.heads); it.idx = (int)(i / a.heads);
         it.kv_head = it.head / a.group;
         const CrossSpan sp = cross_span(a.where, it.idx);
@@ -605,6 +603,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
             // ------------------------------------------------------------------ rows that nothing reaches
             for (long long i = blockIdx.x; i < a.items; i += gridDim.x) {
                 const Item it = item_of<DKV>(a, i);
+                if (!it.live) break;
                 const int skip = it.tiles > 0 ? BR : 0, rows = (DKV || it.limit < BR ? it.limit : BR) - skip, seq = DKV ? it.enc : it.idx, tok0 = (DKV ? it.row : it.row0) + skip;
                 if (rows <= 0) continue;
                 for (int o = 0; o < (DKV ? 2 : 1); ++o) {
@@ -686,7 +685,7 @@ bool cross_bwd_tc_supported(const CrossArgs& c) {
 // Parts of the tokens' tiles where the blocks of states leave SMs without one: two tiles at least, an fp32 row of dk and dv each.  Items of
 // more than a million tiles, a second's work, are split too: waits for them give up after two.
 int cross_bwd_tc_parts(const CrossArgs& c) {
-    const long long items = (long long)c.where.n_enc * c.kv_heads * cross_blocks(c.where, BR);
+    const long long items = cross_blocks(c.where, BR) * c.kv_heads;
     const long long all = (long long)c.n_seq * c.group * ((c.n_q + BC - 1) / BC), tiles = all / (c.where.n_enc > 0 ? c.where.n_enc : 1);
     long long p = items >= kSms || items < 1 ? 1 : (2 * kSms + items - 1) / items;
     if (p > tiles / 2) p = tiles / 2;
@@ -717,9 +716,9 @@ int cross_bwd_tc_dq(const CrossArgs& c, cudaStream_t s) {
 int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_t s) {
     Args a = args_of(c);
     const int enc = c.where.offsets ? 1 : c.where.n_enc, rows = c.where.kv_rows;
-    a.blocks = cross_blocks(c.where, BR);
+    a.blocks = cross_blocks_per(c.where, BR);
     a.parts = parts; a.part_out = part_out; a.part_rows = (long long)enc * rows * c.kv_heads;
-    a.items = (long long)c.where.n_enc * c.kv_heads * a.blocks * parts;
+    a.items = cross_blocks(c.where, BR) * c.kv_heads * parts;
     a.next = c.next;
     a.o1 = c.dk; a.o2 = c.dv;
     CUtensorMap m[4];

@@ -330,18 +330,19 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
     store_rows<E, ND>(at_out<E>(a.dq, s, 0, h), a.dq.tok, q0, a.n_q, d, ty, tx, acc);
 }
 
-// A CTA per (64 states, key head, encoder sequence, part); it walks over its part of the tiles of tokens: of every sequence that reads the
-// states, in order, the query heads of the key head and 64 tokens.
-template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_simt_dkv_kernel(const CrossArgs a, int parts, float* part_out) {
-    extern __shared__ float smem[];
+// An item is (64 states, key head, encoder sequence, part); its CTA walks over its part of the tiles of tokens: of every sequence that reads
+// the states, in order, the query heads of the key head and 64 tokens.  False: there is no item from this one on.
+template <typename E, int ND> __device__ __forceinline__ bool dkv_item(const CrossArgs& a, long long item, int blocks, int parts, float* part_out, float* smem) {
     const int d = a.d, P = pitch(d);
     float *K = smem, *V = K + T * P, *Q = V + T * P, *G = Q + T * P, *W = G + T * P, *L = W + T * PS, *D = L + T;
-    const int tiles = cross_blocks(a.where, T);
-    const int part = (int)(blockIdx.x % parts), te = (int)(blockIdx.x / parts), tile = te % tiles, eh = te / tiles, kh = eh % a.kv_heads, e = eh / a.kv_heads;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, j0 = tile * T;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, part = (int)(item % parts);
+    const CrossBlock block = cross_block<T>(a.where, a.kv_heads, blocks, item / parts);
+    if (block.row0 < 0) return block.more;
+    const int kh = block.head, e = block.e, j0 = block.row0;
     const CrossSpan sp = cross_span_of_enc(a.where, e);
-    const int rows = tile + 1 < tiles ? min(sp.rows, j0 + T) : sp.rows;      // that are written up to
-    if (j0 >= rows) return;
+    const int rows = block.last || sp.rows - j0 < T ? sp.rows : j0 + T;      // that are written up to
+    if (j0 >= rows) return true;
+    __syncthreads();                                               // the item before has been read
     const uint8_t* mask = cross_mask(a.where, sp);
     auto counts = [&](int j) { return j < sp.len && (!mask || mask[j]); };
     load_tile<E>(K, at<E>(a.k, sp.enc, sp.row0, kh), a.k.tok, j0, d, P, counts);
@@ -419,12 +420,17 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
         store_rows<float, ND>(out + all, step, j0, rows, d, ty, tx, dv);
         zero_rows(out, step, j0 + T, rows, d);
         zero_rows(out + all, step, j0 + T, rows, d);
-        return;
+        return true;
     }
     store_rows<E, ND>(at_out<E>(a.dk, sp.enc, sp.row0, kh), a.dk.tok, j0, rows, d, ty, tx, dk);
     store_rows<E, ND>(at_out<E>(a.dv, sp.enc, sp.row0, kh), a.dv.tok, j0, rows, d, ty, tx, dv);
     zero_rows(at_out<E>(a.dk, sp.enc, sp.row0, kh), a.dk.tok, j0 + T, rows, d);
     zero_rows(at_out<E>(a.dv, sp.enc, sp.row0, kh), a.dv.tok, j0 + T, rows, d);
+    return true;
+}
+template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_simt_dkv_kernel(const CrossArgs a, long long items, int blocks, int parts, float* part_out) {
+    extern __shared__ float smem[];
+    for (long long i = blockIdx.x; i < items && dkv_item<E, ND>(a, i, blocks, parts, part_out, smem); i += gridDim.x) { }
 }
 
 template <typename K, typename... A> int launch(K kernel, long long ctas, int tiles_held, int extra, cudaStream_t s, const CrossArgs& a, A... rest) {
@@ -472,14 +478,11 @@ int cross_simt_dq(int dtype, const CrossArgs& a, cudaStream_t s) {
     if (dtype == FREE_FP32) return a.d <= 64 ? launch(cross_simt_dq_kernel<float, 1>, q_tiles(a), 4, 0, s, a) : launch(cross_simt_dq_kernel<float, 2>, q_tiles(a), 4, 0, s, a);
     return a.d <= 64 ? launch(cross_simt_dq_kernel<__nv_bfloat16, 1>, q_tiles(a), 4, 0, s, a) : launch(cross_simt_dq_kernel<__nv_bfloat16, 2>, q_tiles(a), 4, 0, s, a);
 }
-namespace {
-long long dkv_items(const CrossArgs& a) { return (long long)cross_blocks(a.where, T) * a.where.n_enc * a.kv_heads; }
-}  // namespace
 
 // Parts of the tokens where the blocks of states leave SMs without one (all gradients of 2 x 512 tokens, 8 heads of 64, 300 states: 158 ->
 // 139 us; of 3 x 333 tokens, 77 states, 6 heads of 40: 84 -> 52)
 int cross_simt_dkv_parts(const CrossArgs& a) {
-    const long long items = dkv_items(a), tiles = (long long)a.n_seq * a.group * ((a.n_q + T - 1) / T) / (a.where.n_enc > 0 ? a.where.n_enc : 1);
+    const long long items = cross_blocks(a.where, T) * a.kv_heads, tiles = (long long)a.n_seq * a.group * ((a.n_q + T - 1) / T) / (a.where.n_enc > 0 ? a.where.n_enc : 1);
     if (items < 1 || items >= 2 * 148) return 1;
     long long p = (3 * 148 + items - 1) / items;
     if (p > tiles) p = tiles;
@@ -487,10 +490,11 @@ int cross_simt_dkv_parts(const CrossArgs& a) {
     return p < 1 ? 1 : (int)p;
 }
 int cross_simt_dkv(int dtype, const CrossArgs& a, int parts, float* part_out, cudaStream_t s) {
-    const long long n = dkv_items(a) * parts;
+    // a CTA per item, up to sixteen on an SM: few of the blocks of packed states may hold any
+    const long long n = cross_blocks(a.where, T) * a.kv_heads * parts;
     const bool slim = a.d <= 64;
     auto kernel = dtype == FREE_FP32 ? slim ? cross_simt_dkv_kernel<float, 1> : cross_simt_dkv_kernel<float, 2>
                                      : slim ? cross_simt_dkv_kernel<__nv_bfloat16, 1> : cross_simt_dkv_kernel<__nv_bfloat16, 2>;
-    FREE_TRY(launch(kernel, n, 4, 2 * T, s, a, parts, part_out));
+    FREE_TRY(launch(kernel, n < 148 * 16 ? n : 148 * 16, 4, 2 * T, s, a, n, cross_blocks_per(a.where, T), parts, part_out));
     return parts > 1 ? cross_bwd_join(dtype, a, parts, part_out, s) : FREE_OK;
 }
