@@ -205,7 +205,8 @@ template <typename E, int V, int L> __global__ void __launch_bounds__(256) cross
     free_grid_dep_launch();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.next = 0;
     const long long rows = (long long)a.n_seq * a.n_q * a.heads;
-    const int lane = threadIdx.x % L, groups = (int)(gridDim.x * (256 / L)), step_t = groups / a.heads, step_h = groups % a.heads;
+    const int lane = threadIdx.x % L, groups = (int)(gridDim.x * (256 / L)), step_h = groups % a.heads;
+    const int step_t = groups / a.heads % a.n_q, step_s = groups / a.heads / a.n_q;
     long long i = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
     int h = (int)(i % a.heads), t, s;
     { const long long st = i / a.heads; t = (int)(st % a.n_q); s = (int)(st / a.n_q); }
@@ -224,9 +225,9 @@ template <typename E, int V, int L> __global__ void __launch_bounds__(256) cross
                 o[r][p].load(po + p * L * V, ok && lane * V + p * L * V < a.d);
             }
             out[r] = ok ? ((long long)s * a.heads + h) * a.n_q + t : -1;
-            i += groups; h += step_h; t += step_t;
+            i += groups; h += step_h; t += step_t; s += step_s;
             if (h >= a.heads) { h -= a.heads; ++t; }
-            while (t >= a.n_q) { t -= a.n_q; ++s; }
+            if (t >= a.n_q) { t -= a.n_q; ++s; }
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
