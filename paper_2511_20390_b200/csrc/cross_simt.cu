@@ -12,7 +12,6 @@
 // up to 77 states: 17 us).
 // States that do not count are read as zeros and their scores are masked, so nothing in them reaches a result.
 #include "cross.h"
-#include <mutex>
 
 namespace {
 
@@ -436,8 +435,10 @@ template <typename E, int ND> __global__ void __launch_bounds__(kThreads) cross_
 
 template <typename K, typename... A> int launch(K kernel, long long ctas, int tiles_held, int extra, cudaStream_t s, const CrossArgs& a, A... rest) {
     if (ctas > 0x7fffffffLL) return FREE_ERR_SHAPE;
-    const int smem = (tiles_held * T * pitch(a.d) + T * PS + extra) * (int)sizeof(float);
-    FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    auto bytes = [&](int d) { return (tiles_held * T * pitch(d) + T * PS + extra) * (int)sizeof(float); };
+    const int smem = bytes(a.d);
+    // the most that the kernel takes: another thread's smaller call must not set it below this one's
+    FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes(a.d <= 64 ? 64 : kCrossMaxD)));
     kernel<<<(unsigned)ctas, kThreads, smem, s>>>(a, rest...);
     return free_check_launch();
 }
