@@ -756,8 +756,10 @@ int launch_fwd(const NormArgs& a, cudaStream_t s) {
 template <typename TX, typename TY, int C, int VW, int MAXT, int T, int R, bool RMS>
 int start_bwd(const NormArgs& a, int threads, cudaStream_t s) {
     auto kernel = layer_norm_bwd_kernel<TX, TY, C, VW, MAXT, T, R, RMS>;
-    const size_t smem = kAhead<TX, TY, VW> ? (size_t)threads * 2 * R * C * (2 * sizeof(TX) + sizeof(TY)) : 0;
-    if (smem > 47 * 1024) FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    constexpr size_t per = kAhead<TX, TY, VW> ? 2 * R * C * (2 * sizeof(TX) + sizeof(TY)) : 0;
+    const size_t smem = threads * per;
+    // the most that the kernel takes: another thread's call with narrower rows must not set it below this one's
+    if (smem > 47 * 1024) FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(MAXT * per)));
     return free_launch(free_overlap_for_rows(a.M), kernel, dim3((unsigned)a.groups * (unsigned)a.chunks), dim3(threads), smem, s, a);
 }
 template <typename TX, typename TY, int VW, bool RMS>

@@ -53,3 +53,18 @@ def test_attention_with_heads_of_different_size():
         results += list(zip(got, grads))
     _at_once(calls, 3000)
     assert all(torch.equal(a, b) for a, b in results)
+
+
+def test_norm_backward_of_rows_of_different_width():
+    import paper_2511_20390_b200 as free
+    from paper_2511_20390_b200 import binding
+    L, calls, results = binding.lib(), [], []
+    for D in (2048, 8192, 2560, 6144):
+        x, g = torch.randn(2, D, device="cuda"), torch.randn(2, D, device="cuda")
+        r = free.op_rms_norm(x, want_rstd=True).rstd
+        want, dx = free.op_rms_norm_bwd(x, g, r, want_dweight=False)[0], torch.empty_like(x)
+        args = [0, 0, 1, 2, 1, D, x.data_ptr(), D, 0, g.data_ptr(), D, 0, r.data_ptr(), None, 0, 0, None, 0, 0, dx.data_ptr(), D, 0, None, D, None, 0]
+        calls.append(lambda s, args=args, keep=(x, g, r): L.free_op_rms_norm_bwd(*args, s))
+        results.append((dx, want))
+    _at_once(calls, 4000)
+    assert all(torch.equal(a, b) for a, b in results)
