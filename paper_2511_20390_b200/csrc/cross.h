@@ -2,7 +2,7 @@
 #pragma once
 #include "internal.h"
 
-constexpr int kCrossMaxD = 128;
+constexpr int kCrossMaxD = 128, kCrossMaxLength = 0x7fff0000;
 
 // A matrix of heads: element (s, t, h, c) at p[s * seq + t * tok + h * head + c].
 struct CrossMat {

@@ -18,6 +18,9 @@ int check(const free_cross_attn* c, bool* empty) {
     for (long long v : {c->q_seq, c->q_tok, c->q_head, c->k_seq, c->k_tok, c->k_head, c->v_seq, c->v_tok, c->v_head})
         if (v < 0) return FREE_ERR_SHAPE;
     if (c->d_head > kCrossMaxD) return FREE_ERR_UNSUPPORTED;
+    // kernels count tokens, states and sequences in steps of up to 2048 behind the last one
+    for (int n : {c->n_seq, c->n_q, c->n_enc, c->n_kv, c->kv_rows})
+        if (n > kCrossMaxLength) return FREE_ERR_UNSUPPORTED;
     // rows of lse, tiles and tile copies' coordinates are counted in 31 bits
     long long blocks = (long long)c->n_enc * (c->n_kv / 64 + 1);
     if (c->kv_offsets && blocks > c->n_enc + (long long)(c->kv_rows / 64)) blocks = c->n_enc + (long long)(c->kv_rows / 64);
