@@ -632,7 +632,7 @@ int free_op_rope_axes(int dtype, int pairing, int freq_mode, int inverse, int n_
  *   dtype      FREE_FP32 (CUDA cores) or FREE_BF16 (tcgen05, fp32 accumulation and softmax; probabilities are rounded to bf16,
  *              which their product takes).  bf16 matrices that are not 16-byte aligned in every stride take the CUDA cores;
  *              so do, in a kernel of their own, tokens times heads per key head of up to eight, whose probabilities stay fp32
- *   d_head     up to 128, else UNSUPPORTED;  heads a multiple of kv_heads;  scale > 0
+ *   d_head     up to 128, else UNSUPPORTED;  heads a multiple of kv_heads;  scale > 0, up to 2.3e38
  *   n_seq, n_q, n_enc, n_kv, kv_rows   up to 0x7fff0000 each, tiles of 64 tokens over all sequences and heads, and blocks of 64 states over all
  *              encoder sequences and key heads, up to 2^31 - 1, else UNSUPPORTED
  * What does not count is not used: NaN and infinities in it change nothing.  NaN that counts gives NaN, in out, lse and gradients.

@@ -10,7 +10,7 @@ int check(const free_cross_attn* c, bool* empty) {
     *empty = false;
     if (!c) return FREE_ERR_ARG;
     if (c->dtype != FREE_FP32 && c->dtype != FREE_BF16) return FREE_ERR_ARG;
-    if (!(c->scale > 0.f) || c->scale > 3.4e38f) return FREE_ERR_ARG;
+    if (!(c->scale > 0.f) || c->scale > 2.3e38f) return FREE_ERR_ARG;      // (times log2 e it is finite)
     if (c->n_seq < 0 || c->n_q < 0 || c->heads < 1 || c->kv_heads < 1 || c->heads % c->kv_heads || c->d_head < 1) return FREE_ERR_SHAPE;
     if (c->n_enc < 0 || c->n_kv < 0 || c->kv_rows < 0) return FREE_ERR_SHAPE;
     if (c->kv_offsets && c->kv_lens) return FREE_ERR_ARG;

@@ -32,3 +32,8 @@ def test_lengths_near_the_end_of_31_bits(L):
             assert L.free_op_cross_attention_workspace_bytes(_pack(**{**one, **kw})) == 0
             assert L.free_op_cross_attention_bwd_workspace_bytes(_pack(**{**one, **kw})) == 0
     assert _both(L, n_kv=0x7fff0000, k=0, **one) == {ARG}          # allowed: the next check is told
+
+
+def test_scales_whose_exponent_in_base_two_overflows(L):
+    assert _both(L, scale=2.4e38) == {ARG} and _both(L, scale=3.4e38) == {ARG}
+    assert _fwd(L, scale=2.2e38, n_seq=0) == 0
