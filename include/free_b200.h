@@ -555,8 +555,8 @@ int free_op_layer_norm_bwd(int x_dtype, int y_dtype, int n_groups, int rows_per_
  *              0: the row) shares the scale max |y_i| / 448, stored at scales[i * scale_stride + run] (scale 1 for runs without
  *              anything above 2^-100, NaN for runs with a NaN).  heads = 1 only
  *   rstd       DEVICE fp32 [rows] or NULL: r, what the backward pass needs
- * Outputs must not overlap the inputs otherwise.  Squares are summed in fp32: rows of up to 1e18 are handled, larger ones overflow
- * (r = 0).  D % 4 == 0 with strides and addresses that are multiples of four elements is the fast form.
+ * Outputs must not overlap the inputs otherwise.  Squares are summed in fp32: rows whose sum of squares stays below 3.4e38 are handled
+ * (their 2-norm below 1.8e19: with 8192 columns magnitudes of up to 2e17, with 300 up to 1e18), larger ones overflow (r = 0, y = 0).  D % 4 == 0 with strides and addresses that are multiples of four elements is the fast form.
  * Errors: ARG, SHAPE, ALIGN, UNSUPPORTED (D > 8192), CUDA.
  *
  * free_op_rms_norm_bwd -- its gradients, from dy, the h and the r that the forward call kept.  With xh = h r, v = dy w:
