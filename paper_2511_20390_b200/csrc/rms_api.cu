@@ -44,12 +44,18 @@ extern "C" int free_op_rms_norm(int x_dtype, int res_dtype, int y_dtype, int n_g
     const long long strides = x_tok | y_tok | (heads > 1 ? x_head | y_head : 0) | (residual ? res_stride : 0) | (res_out ? res_out_stride : 0) |
                               (weight && n_groups > 1 ? mod_stride : 0) | place(x, x_dtype) | place(y, y_dtype) |
                               (residual ? place(residual, res_dtype) : 0) | (res_out ? place(res_out, res_dtype) : 0);
-    // (eight where every type has 16 bits or fewer, but for widths that whole blocks of 128 columns in one warp serve as well, and for
-    // heads that would leave lanes idle: 24 x 1024 tokens, 16 heads of 72, 25 us by four, 27 by eight; of 64, 22 by eight)
+    // (eight where every type has 16 bits or fewer, but for widths that have a kernel of whole blocks of 128 columns: 200 MB of bf16 rows in bf16
+    // results take as long either way, 384 columns 87 and 88 us by eight, 768 80 and 80, or longer, 640 78 and 86, 1152 77 and 93.  Their
+    // 8-bit results with scales per 128 columns halve the exchanges by eight, which pays where the row fills three quarters of that
+    // kernel's 256, 512 or 1024 columns: 512 columns 86 us, by four 113, 384 116 and 121, 896 96 and 126, but 640 121 and 112, 128 205 and 179)
     int vw = D % 4 == 0 && strides % 4 == 0 && free_aligned16(weight) ? 4 : 1;
     const bool thin = x_dtype == FREE_BF16 && y_dtype != FREE_FP32 && (!residual || res_dtype == FREE_BF16);
-    const bool idle = !residual && y_dtype != FREE_E4M3 && D > 64 && D < 96;
-    if (vw == 4 && thin && D % 8 == 0 && strides % 8 == 0 && (D > 1152 || D % 128) && !idle) vw = 8;
+    // heads that would leave lanes idle: 24 x 1024 tokens, 16 heads of 72, 25 us by four, 27 by eight; 12 of 96 20 and 21; 11 of 104 25 and 21;
+    // 9 of 128 23 and 19
+    const bool as_heads = !residual && y_dtype != FREE_E4M3 && D <= 128, idle = as_heads && D > 64 && D <= 96;
+    const bool exact = !as_heads && D <= 1152 && D % 128 == 0, eight_bits = y_dtype == FREE_E4M3 && scale_block != 0;
+    const int held = D <= 256 ? 256 : D <= 512 ? 512 : (D + 1023) / 1024 * 1024;
+    if (vw == 4 && thin && D % 8 == 0 && strides % 8 == 0 && !idle && (!exact || (eight_bits && 4 * D >= 3 * held))) vw = 8;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     const bool rf = residual && res_dtype == FREE_FP32;            // without a residual its type does not matter
     if (x_dtype == FREE_FP32) return rf ? rms_norm_ff(a, vw, y_dtype, s) : rms_norm_fb(a, vw, y_dtype, s);

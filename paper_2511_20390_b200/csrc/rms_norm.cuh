@@ -4,9 +4,9 @@
 //   8 bits: for every run of 128 columns (or the row) s = max |y| / 448, q = e4m3(y / s)
 //
 // One pass over the data, bound by HBM: every row is read once and kept in registers as h in fp32 (the norm is of the unrounded
-// sum; what is stored of h is rounded to the residual's type).  Rows of up to 2048 columns take one warp, P pieces of 128 columns
-// (four consecutive ones per lane: whole 16- or 8-byte accesses, and one piece is one run of an 8-bit result's scale); wider
-// rows take several warps of a CTA, joined through shared memory.  The next row's loads are in flight while this one is reduced.
+// sum; what is stored of h is rounded to the residual's type).  Rows of up to 1024 columns (512 of single accesses, and 1152) take one warp, P
+// pieces of 128 columns (four consecutive ones per lane: whole 16- or 8-byte accesses, and one piece is one run of an 8-bit result's
+// scale) or of 256 (eight); wider rows take several warps of a CTA, joined through shared memory.  The next row's loads are in flight while this one is reduced.
 // Heads of up to 128 columns: four rows share a warp, or eight (rms_norm_heads_kernel).
 // Measured, 24 x 1024 rows of 1152, bf16 onto an fp32 residual, per sequence: 53 us on its own, 61 one call after another (what they
 // wrote leaves the L2 meanwhile; 340 MB, 52 us at a copy's rate).  16 heads of 72 in as many tokens: 25 us (18).  4100 rows of 4096 onto
@@ -306,7 +306,12 @@ template <typename TX, typename TY, int L, int C, int VW> int start_heads(RmsArg
     return free_launch(free_overlap_for_rows(a.M), rms_norm_heads_kernel<TX, TY, L, C, VW>, dim3((unsigned)grid), dim3(256), 0, s, a);
 }
 
-// As many pieces of 128 columns per warp as the row needs (registers decide how many rows an SM holds), several warps beyond 2048 columns.
+// As many pieces per warp as the row needs (registers decide how many rows an SM holds), several warps beyond 1024 columns.  Whole pieces of 128
+// columns, up to nine, have kernels of their own, without guards and the lanes behind the row's end (200 MB of bf16 rows of 640 columns
+// onto fp32 ones: 208 us, in the kernel for up to 1024 columns 224; 8-bit results with a scale per run: 112 and 174).
+template <typename TX, typename TR, typename TY, int P> int start_exact(const RmsArgs& a, cudaStream_t s) {
+    return start<TX, TR, TY, P, 4, true, 128, P <= 2 ? 8 : P <= 4 ? 6 : P == 5 ? 5 : P <= 8 ? 4 : 3>(a, 1, s);
+}
 template <typename TX, typename TR, typename TY, int VW> int launch(const RmsArgs& a, cudaStream_t s) {
     if constexpr (sizeof(TY) > 1) {
         if (!a.res && a.D <= 128) {
@@ -326,10 +331,15 @@ template <typename TX, typename TR, typename TY, int VW> int launch(const RmsArg
         return start<TX, TR, TY, 4, 8, false, 256, 2>(a, (D + 1023) / 1024, s);
     } else if constexpr (VW == 4) {
         switch (D % 128 == 0 ? D / 128 : 0) {
-            case 3: return start<TX, TR, TY, 3, 4, true, 128, 6>(a, 1, s);
-            case 6: return start<TX, TR, TY, 6, 4, true, 128, 4>(a, 1, s);
-            case 8: return start<TX, TR, TY, 8, 4, true, 128, 4>(a, 1, s);
-            case 9: return start<TX, TR, TY, 9, 4, true, 128, 3>(a, 1, s);
+            case 1: return start_exact<TX, TR, TY, 1>(a, s);
+            case 2: return start_exact<TX, TR, TY, 2>(a, s);
+            case 3: return start_exact<TX, TR, TY, 3>(a, s);
+            case 4: return start_exact<TX, TR, TY, 4>(a, s);
+            case 5: return start_exact<TX, TR, TY, 5>(a, s);
+            case 6: return start_exact<TX, TR, TY, 6>(a, s);
+            case 7: return start_exact<TX, TR, TY, 7>(a, s);
+            case 8: return start_exact<TX, TR, TY, 8>(a, s);
+            case 9: return start_exact<TX, TR, TY, 9>(a, s);
             default: break;
         }
         if (D > 1024 && D % 1024 == 0) return start<TX, TR, TY, 8, 4, true, 256, 2>(a, D / 1024, s);
