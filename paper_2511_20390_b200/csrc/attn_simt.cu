@@ -64,13 +64,14 @@ int attention_simt(int dtype, int n_seq, int n_tok, int heads, int d_head, const
     if (n_seq < 1 || n_tok < 1 || heads < 1 || d_head < 1 || !qkv || !out) return FREE_ERR_ARG;
     if (d_head > kMaxDh) return FREE_ERR_UNSUPPORTED;
     size_t smem = ((size_t)kRowsPerCta * n_tok + kRowsPerCta * kMaxDh) * sizeof(float);
-    if (smem > 200 * 1024) return FREE_ERR_UNSUPPORTED;
+    constexpr int most = 200 * 1024;          // allowed whatever this call takes: another thread's smaller call must not set it below
+    if (smem > most) return FREE_ERR_UNSUPPORTED;
     dim3 grid((n_tok + kRowsPerCta - 1) / kRowsPerCta, heads, n_seq);
     if (dtype == FREE_FP32) {
-        FREE_CUDA_TRY(cudaFuncSetAttribute(attention_simt_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        FREE_CUDA_TRY(cudaFuncSetAttribute(attention_simt_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
         attention_simt_kernel<float><<<grid, kRowsPerCta * 32, smem, s>>>(n_tok, heads, d_head, (const float*)qkv, (float*)out);
     } else {
-        FREE_CUDA_TRY(cudaFuncSetAttribute(attention_simt_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        FREE_CUDA_TRY(cudaFuncSetAttribute(attention_simt_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
         attention_simt_kernel<__nv_bfloat16><<<grid, kRowsPerCta * 32, smem, s>>>(n_tok, heads, d_head, (const __nv_bfloat16*)qkv, (__nv_bfloat16*)out);
     }
     return free_check_launch();

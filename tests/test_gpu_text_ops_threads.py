@@ -68,3 +68,20 @@ def test_norm_backward_of_rows_of_different_width():
         results.append((dx, want))
     _at_once(calls, 4000)
     assert all(torch.equal(a, b) for a, b in results)
+
+
+def test_self_attention_of_different_lengths():
+    import paper_2511_20390_b200 as free
+    from paper_2511_20390_b200 import binding
+    L, calls, results = binding.lib(), [], []
+    for n in (8, 2600, 16, 2000):
+        qkv = torch.randn(1, n, 48, device="cuda")
+        want = free.op_attention(qkv, 1)
+        out = torch.empty_like(want)
+        need = L.free_op_attention_workspace_bytes(0, 1, n, 1, 16)
+        ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+        args = [0, 1, n, 1, 16, qkv.data_ptr(), out.data_ptr(), ws.data_ptr(), need]
+        calls.append(lambda s, args=args, keep=(qkv, ws): L.free_op_attention(*args, s))
+        results.append((out, want))
+    _at_once(calls, 2000)
+    assert all(torch.equal(a, b) for a, b in results)
