@@ -160,6 +160,13 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
         tc::fence_proxy_async();
     }
     if (warp == 12) { tc::tmem_alloc(tmem_slot, kTmemCols); tc::tmem_relinquish(); }
+    if (const int used = a.tt * a.group; used < BQ) {
+        // rows that whole tokens do not fill are zeros: their scores have a say in when a warp's rows move their maxima, which decides roundings
+        const uint32_t pieces = (uint32_t)(BQ - used) * 8;
+        for (uint32_t i = threadIdx.x; i < QB * 2 * NCH * pieces; i += kThreads)
+            *reinterpret_cast<uint4*>(sQ + i / pieces * kChunk + used * 128 + i % pieces * 16) = make_uint4(0u, 0u, 0u, 0u);
+        tc::fence_proxy_async();
+    }
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
