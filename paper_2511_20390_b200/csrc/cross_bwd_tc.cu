@@ -13,7 +13,7 @@
 // others four where they are dealt out), one that loads tiles, one that brings the tokens' lse and delta (dk, dv); one each that issues S,
 // dP and either accumulating product, in order, so that sums have a fixed order whichever CTA forms them.  Nothing is added atomically; S
 // and dP are formed twice instead (once here, once for the other direction).
-// What bounds it: the way of a tile through the warps.  Those 24 x 1024 tokens take 92 us for dq and 107 for dk, dv; the tensor cores
+// What bounds it: the way of a tile through the warps.  Those 24 x 1024 tokens take 89 us for dq and 107 for dk, dv; the tensor cores
 // work for 20% of that, the exponentials' unit for 22%; a tile's elementwise part takes 1300 to 2000 clocks, its copies 2300 when they
 // compete with a block of rows, a wait 115 when it is over already.  Before S, dP, dk and dv had a warp each, and dP its own tensor memory,
 // free once it is read: 95 and 160.
@@ -66,7 +66,7 @@ struct alignas(16) Item {
     int left, first, limit, kv_head;          // states from `row` on; first column tile of the part; rows that are written (the last block of states: behind it, too)
 };
 
-template <bool DKV> __device__ __forceinline__ int sequences_of(const Args& a, int e) {      // that read encoder sequence e; whole warp
+__device__ __forceinline__ int sequences_of(const Args& a, int e) {      // that read encoder sequence e; whole warp
     if (!a.where.seq_of) return a.n_seq ? a.where.share : 0;
     int n = 0;
     for (int s0 = 0; s0 < a.n_seq; s0 += 32) {
@@ -90,7 +90,7 @@ template <bool DKV> __device__ __forceinline__ Item item_of(const Args& a, long 
         it.enc = sp.enc; it.row = sp.row0 + it.row0; it.left = sp.len - it.row0;
         it.limit = b.last ? sp.rows - it.row0 : min(sp.rows - it.row0, BR);
         if (it.left > 0) {
-            const long long all = (long long)sequences_of<DKV>(a, it.idx) * a.group * ((a.n_q + BC - 1) / BC);
+            const long long all = (long long)sequences_of(a, it.idx) * a.group * ((a.n_q + BC - 1) / BC);
             it.first = (int)(all * it.part / a.parts);
             it.tiles = (int)(all * (it.part + 1) / a.parts) - it.first;
         }

@@ -9,8 +9,8 @@
 // with its own (row, state) and takes its exponential; the probabilities are then passed to all lanes of the group.  The parts of a
 // CTA's groups are joined through shared memory; long state sequences are split over CTAs as well and joined by cross_join_kernel.
 // Measured: 4 sequences of 77 states, 6 heads of 64: 4.4 us (8.7 by the tensor cores' kernel).  8 of up to 16384 states, 32 heads of 128
-// on 8: 78 us and 6 for the join, 4.6 TB/s of K and V, bound by issue slots (120 us with every score summed over all lanes).  What is left
-// are the ends: lengths that only the device knows fill the last round of CTAs in part.
+// on 8: 80 us with the join, 4.5 TB/s of K and V (120 us with every score summed over all lanes).  Neither issue slots (0.67) nor HBM (0.55)
+// are full; what is left are the ends: parts of unequal length, which only the device knows, make two rounds of CTAs and a bit.
 #include "cross_tc.cuh"
 
 namespace {

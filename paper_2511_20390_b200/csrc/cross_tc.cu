@@ -16,7 +16,9 @@
 // Long states and few rows: the states are split into parts, each with its own softmax, joined by cross_join_kernel.
 // What bounds it: a block's way through the softmax warps, some 1700 clocks for 64 states where the exponentials and conversions of its
 // two warps per scheduler are 1050; the tensor cores work for 16% of the time, the exponentials' unit for 29%.  24 x 1024 tokens, 16 heads
-// of 72, up to 300 states: 72 us (0.31 PFLOP/s); 8 x 4096 tokens, 16 heads of 128, up to 512 states: 131 us (0.70).
+// of 72, up to 300 states: 68 us in a graph, 71 as calls (0.32 PFLOP/s); 8 x 4096 tokens, 16 heads of 128, up to 512 states: 126 to 136 and 143 (0.64 to 0.73).
+// Heads of a key head that do not divide 32 (three, five, six): results leave by single elements, 24 x 1024 tokens, 300 states, heads of 72, 12 on 4
+// 276 us, 12 on 3 or 6 67.
 #include "cross_tc.cuh"
 
 namespace cross_tc {

@@ -65,7 +65,7 @@ __device__ __forceinline__ uint64_t desc_mn(uint32_t saddr, uint32_t block) {
 }
 constexpr uint32_t kBMajorMN = 1u << 16;      // instruction descriptor: B's contraction runs along rows
 
-// The 128 states from j0 on that count, one bit each.
+// The 32 * WORDS states from j0 on that count, one bit each.
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 template <int WORDS> __device__ __forceinline__ void count_bits(uint32_t (&w)[WORDS], const uint8_t* mask, int j0, int len, int lane) {   // whole warp
 #pragma unroll

@@ -8,9 +8,9 @@
 // pieces of 128 columns (four consecutive ones per lane: whole 16- or 8-byte accesses, and one piece is one run of an 8-bit result's
 // scale) or of 256 (eight); wider rows take several warps of a CTA, joined through shared memory.  The next row's loads are in flight while this one is reduced.
 // Heads of up to 128 columns: four rows share a warp, or eight (rms_norm_heads_kernel).
-// Measured, 24 x 1024 rows of 1152, bf16 onto an fp32 residual, per sequence: 53 us on its own, 61 one call after another (what they
-// wrote leaves the L2 meanwhile; 340 MB, 52 us at a copy's rate).  16 heads of 72 in as many tokens: 25 us (18).  4100 rows of 4096 onto
-// a bf16 residual, 8-bit values and a scale per 128 columns: 24 us (18).  256 rows of 384: 4 us, the launch.
+// Measured, 24 x 1024 rows of 1152, bf16 onto an fp32 residual, per sequence: 53 us on its own, 59 to 62 one call after another (what they
+// wrote leaves the L2 meanwhile; 340 MB, 52 us at a copy's rate).  16 heads of 72 in as many tokens: 23 us (18).  4100 rows of 4096 onto
+// a bf16 residual, 8-bit values and a scale per 128 columns: 23 us (18).  256 rows of 384: 2 us in a graph of them, the launch.
 #pragma once
 #include "rms_norm.h"
 #include <cuda_fp8.h>
