@@ -33,7 +33,7 @@ def test_offsets_that_leave_the_rows(n_q, dt):
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("n_q", [1, 70, 1100])
-@pytest.mark.parametrize("most", [0, 20, 64, 130, 300])
+@pytest.mark.parametrize("most", [0, 20, 64, 130, 250, 260, 300])
 def test_rows_behind_the_longest(most, n_q, dt):
     """dk and dv that hold rubbish: rows of a sequence behind the states that may count become zeros, rows of none stay as they are."""
     import paper_2511_20390_b200 as free
