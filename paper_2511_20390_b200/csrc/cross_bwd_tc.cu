@@ -76,16 +76,16 @@ __device__ __forceinline__ int sequences_of(const Args& a, int e) {      // that
     return n;
 }
 
-template <bool DKV> __device__ __forceinline__ Item item_of(const Args& a, long long i) {     // whole warp
+template <bool DKV, bool ROWS> __device__ __forceinline__ Item item_of(const Args& a, long long i) {     // whole warp
     Item it;
     it.live = i < a.items;
     it.tiles = it.part = it.first = 0;
     if (!it.live) return it;
     if (DKV) {
         it.part = (int)(i % a.parts);
-        const CrossBlock b = cross_block<BR>(a.where, a.kv_heads, a.blocks, i / a.parts);
+        const CrossBlock b = cross_block<BR, ROWS>(a.where, a.kv_heads, a.blocks, i / a.parts);
         it.live = b.more; it.idx = b.e; it.head = it.kv_head = b.head; it.row0 = b.row0; it.limit = 0;
-        if (b.row0 < 0) return it;
+        if (ROWS && b.row0 < 0) return it;
         const CrossSpan sp = cross_span_of_enc(a.where, it.idx);
         it.enc = sp.enc; it.row = sp.row0 + it.row0; it.left = sp.len - it.row0;
         it.limit = b.last ? sp.rows - it.row0 : min(sp.rows - it.row0, BR);
@@ -132,7 +132,7 @@ struct Columns {
     }
 };
 
-template <bool DKV, int NCH, int W, int AB, int N1, int N2, int NS, int ND, int NA>
+template <bool DKV, bool ROWS, int NCH, int W, int AB, int N1, int N2, int NS, int ND, int NA>
 __global__ void __launch_bounds__(kThreads, 1)
 cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constant__ CUtensorMap mapA2, const __grid_constant__ CUtensorMap mapB1,
                  const __grid_constant__ CUtensorMap mapB2, const Args a) {
@@ -578,7 +578,7 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
                     if (lane == 0) v = atomicAdd(a.next, 1ull);
                     i = (long long)__shfl_sync(0xffffffffu, v, 0);
                 }
-                const Item it = item_of<DKV>(a, i);
+                const Item it = item_of<DKV, ROWS>(a, i);
                 if (!DKV) i += gridDim.x;
                 return it;
             };
@@ -602,8 +602,8 @@ cross_bwd_kernel(const __grid_constant__ CUtensorMap mapA1, const __grid_constan
         } else if (warp == 16) {
             // ------------------------------------------------------------------ rows that nothing reaches
             for (long long i = blockIdx.x; i < a.items; i += gridDim.x) {
-                const Item it = item_of<DKV>(a, i);
-                if (!it.live) break;
+                const Item it = item_of<DKV, ROWS>(a, i);
+                if (ROWS && !it.live) break;
                 const int skip = it.tiles > 0 ? BR : 0, rows = (DKV || it.limit < BR ? it.limit : BR) - skip, seq = DKV ? it.enc : it.idx, tok0 = (DKV ? it.row : it.row0) + skip;
                 if (rows <= 0) continue;
                 for (int o = 0; o < (DKV ? 2 : 1); ++o) {
@@ -652,13 +652,19 @@ template <typename E> __global__ void __launch_bounds__(256) cross_bwd_join_kern
     }
 }
 
-template <bool DKV, int NCH, int W, int AB, int N1, int N2, int NS, int ND, int NA>
+template <bool DKV, bool ROWS, int NCH, int W, int AB, int N1, int N2, int NS, int ND, int NA>
 int launch(const CUtensorMap (&m)[4], const Args& a, cudaStream_t s) {
-    auto kernel = cross_bwd_kernel<DKV, NCH, W, AB, N1, N2, NS, ND, NA>;
+    auto kernel = cross_bwd_kernel<DKV, ROWS, NCH, W, AB, N1, N2, NS, ND, NA>;
     constexpr uint32_t bytes = Mem<DKV, NCH, W, AB, N1, N2, NS, ND, NA>::bytes;
     FREE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
     const int grid = (int)(a.items < kSms ? a.items : kSms);
     return free_launch(free_overlap_for_rows((long long)a.n_seq * a.n_q), kernel, dim3(grid), dim3(kThreads), bytes, s, m[0], m[1], m[2], m[3], a);
+}
+
+// (heads of 72 with two buffers of S instead of three: 116 us for 107; with five and three slots of the ring for four each 114)
+template <bool ROWS> int launch_dkv(int d, const CUtensorMap (&m)[4], const Args& a, cudaStream_t s) {
+    return d <= 64 ? launch<true, ROWS, 1, 64, 2, 6, 6, 3, 3, 1>(m, a, s) : d <= 96 ? launch<true, ROWS, 2, 96, 1, 4, 4, 3, 2, 1>(m, a, s) :
+                     launch<true, ROWS, 2, 128, 1, 4, 4, 2, 2, 1>(m, a, s);
 }
 
 Args args_of(const CrossArgs& c) {
@@ -709,8 +715,8 @@ int cross_bwd_tc_dq(const CrossArgs& c, cudaStream_t s) {
     FREE_TRY(map_heads(&m[3], c.v, enc, rows, c.kv_heads, c.d, 1, BC));
     // two sets of sums, so that results leave while the next item's are formed (24 x 1024 tokens of 16 heads of 72: 92 us; one set and a
     // third buffer of dP 95)
-    if (c.d <= 64) return launch<false, 1, 64, 2, 6, 4, 3, 3, 2>(m, a, s);
-    return c.d <= 96 ? launch<false, 2, 96, 2, 3, 2, 3, 2, 2>(m, a, s) : launch<false, 2, 128, 2, 3, 2, 2, 2, 2>(m, a, s);
+    if (c.d <= 64) return launch<false, false, 1, 64, 2, 6, 4, 3, 3, 2>(m, a, s);
+    return c.d <= 96 ? launch<false, false, 2, 96, 2, 3, 2, 3, 2, 2>(m, a, s) : launch<false, false, 2, 128, 2, 3, 2, 2, 2, 2>(m, a, s);
 }
 
 int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_t s) {
@@ -727,10 +733,7 @@ int cross_bwd_tc_dkv(const CrossArgs& c, int parts, float* part_out, cudaStream_
     FREE_TRY(map_heads(&m[1], c.v, enc, rows, c.kv_heads, c.d, 1, BR));
     FREE_TRY(map_heads(&m[2], c.q, c.n_seq, c.n_q, c.heads, c.d, 1, BC));
     FREE_TRY(map_heads(&m[3], c.g, c.n_seq, c.n_q, c.heads, c.d, 1, BC));
-    // (heads of 72 with two buffers of S instead of three: 116 us for 107; with five and three slots of the ring for four each 114)
-    const int code = c.d <= 64 ? launch<true, 1, 64, 2, 6, 6, 3, 3, 1>(m, a, s) : c.d <= 96 ? launch<true, 2, 96, 1, 4, 4, 3, 2, 1>(m, a, s) :
-                                 launch<true, 2, 128, 1, 4, 4, 2, 2, 1>(m, a, s);
-    FREE_TRY(code);
+    FREE_TRY(a.blocks ? launch_dkv<false>(c.d, m, a, s) : launch_dkv<true>(c.d, m, a, s));
     if (parts == 1) return FREE_OK;
     return cross_bwd_join(FREE_BF16, c, parts, part_out, s);
 }

@@ -236,8 +236,8 @@ template <typename E, int R, int L> __global__ void __launch_bounds__(kThreads, 
             l = fmaf(f, stats[g][r].y, l);
             o = fmaf(f, acc_of[(g * R + r) * L * V + ch], o);
         }
-        // no state: the sum tells, which a NaN among the scores reaches; the maximum leaves it out
-        const float out = l == 0.f ? 0.f : o / l, lse = l == 0.f ? -INFINITY : m * a.scale + logf(l);
+        // no state: the sum tells, which a NaN among the scores reaches (the maximum leaves it out), and both terms of lse are -inf
+        const float out = l == 0.f ? 0.f : o / l, lse = m * a.scale + logf(l);
         const int t = r / a.group, h = kh * a.group + r % a.group;
         const long long row = ((long long)s * a.heads + h) * a.n_q + t;
         if (parts.n > 1) {

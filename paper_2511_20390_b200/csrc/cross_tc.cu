@@ -325,7 +325,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 const bool row_ok = row_t < a.tt && t < a.n_q;
                 const long long row = ((long long)it.s * a.heads + h) * a.n_q + t;
                 if (row_ok && (a.parts > 1 || a.lse)) {
-                    const float lse = sum == 0.f ? -INFINITY : top * a.scale + logf(sum);
+                    const float lse = top * a.scale + logf(sum);        // no state: both -inf
                     if (a.parts > 1) a.part_lse[it.part * a.rows + row] = lse;
                     else a.lse[row] = lse;
                 }
@@ -593,7 +593,7 @@ template <typename E, int THREADS> __global__ void __launch_bounds__(THREADS) cr
         if constexpr (sizeof(E) == 4) out[ch] = v;
         else out[ch] = __float2bfloat16(v);
     }
-    if (a.lse && threadIdx.x == 0) a.lse[i] = sum == 0.f ? -INFINITY : top + logf(sum);
+    if (a.lse && threadIdx.x == 0) a.lse[i] = top + logf(sum);
 }
 
 int tokens_per_tile(const CrossArgs& a) { return BQ / a.group; }
